@@ -38,3 +38,11 @@ from .binding import (  # noqa: F401
     sk_queue_params_default, sk_queue_create, sk_queue_submit, sk_queue_poll, sk_queue_get_stats, sk_queue_destroy,
     SK_QUEUE_SEQUENTIAL, SK_QUEUE_COALESCE, SK_QUEUE_OOO, QUEUE_POLICY,
 )
+from .cache import (  # noqa: F401
+    CACHE_SYMBOLS,
+    AttnParams, AttnPlan, Pages, sk_attn_problem, sk_page_array,
+    cache_lib, cache_lib_path,
+    make_attn_problem, make_ids, make_page_arrays,
+    sk_attn_append, sk_attn_launch, sk_attn_params_default, sk_attn_plan_create, sk_attn_plan_destroy, sk_attn_plan_info,
+    sk_pages_apply, sk_pages_compact, sk_pages_copy, sk_pages_create, sk_pages_destroy, sk_pages_fork, sk_pages_resize, sk_pages_state,
+)

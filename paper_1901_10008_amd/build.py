@@ -1,4 +1,4 @@
-"""Build libsuperkernel.so (HIP, gfx950 only) in-tree next to this file."""
+"""Build libsuperkernel.so and libsk_cache.so (HIP, gfx950 only) in-tree next to this file."""
 from __future__ import annotations
 
 import os
@@ -14,6 +14,10 @@ SOURCES = ["superkernel.hip", "planner.cpp", "queue.cpp", "instances.hip", "scra
 UNITS = 7  # units of compilation of instances.hip
 HEADERS = ["kernels.hip.h", "sk_internal.h", os.path.join(ROOT, "include", "superkernel.h")]
 
+CACHE_LIB = os.path.join(HERE, "libsk_cache.so")  # attention's side of decoder layers (include/sk_cache.h)
+CACHE_SOURCES = ["cache.hip", "cache_plan.cpp", "cache_instances.hip"]
+CACHE_UNITS = 8  # units of compilation of cache_instances.hip
+
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -27,6 +31,21 @@ HIPCC_FLAGS = [
 
 DIAG_LIB = os.path.join(HERE, "libsuperkernel_diag.so")  # -DSK_DIAG_CLOCKS: per-tile phase stamps (tile_phases.py)
 DIAG_ALL_LIB = os.path.join(HERE, "libsuperkernel_diag_all.so")  # the same with every workgroup of a launch stamped
+
+
+def _runner(verbose: bool):
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        res = subprocess.run(cmd, capture_output=True, text=True)
+        # the host pass warns that it does not know the packed-fp32 feature: harmless noise
+        err = "\n".join(l for l in res.stderr.splitlines() if "packed-fp32-ops" not in l)
+        if res.returncode != 0:
+            raise RuntimeError("build step failed: " + " ".join(cmd) + "\n" + err)
+        if verbose and err.strip():
+            print(err)
+
+    return run
 
 
 def build_diag(verbose: bool = False, all_workgroups: bool = False) -> str:
@@ -71,22 +90,34 @@ def build(force: bool = True, verbose: bool = False, extra=(), lib: str = LIB, c
                          os.path.join(CSRC, "ceilings.hip"), "-o", CEILINGS_LIB])
     link = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", o_hip, *o_units, o_cpp, o_queue, o_scratch, "-o", lib]
 
-    def run(cmd):
-        if verbose:
-            print(" ".join(cmd), flush=True)
-        res = subprocess.run(cmd, capture_output=True, text=True)
-        # the host pass warns that it does not know the packed-fp32 feature: harmless noise
-        err = "\n".join(l for l in res.stderr.splitlines() if "packed-fp32-ops" not in l)
-        if res.returncode != 0:
-            raise RuntimeError("build step failed: " + " ".join(cmd) + "\n" + err)
-        if verbose and err.strip():
-            print(err)
-
+    run = _runner(verbose)
     with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:
         list(pool.map(run, compiles))
     run(link)
     return lib
 
 
+def build_cache(verbose: bool = False, extra=(), lib: str = CACHE_LIB) -> str:
+    """libsk_cache.so, linked to the libsuperkernel.so beside it (statuses and error texts are that library's)."""
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    srcs = [os.path.join(CSRC, s) for s in CACHE_SOURCES]
+    inc = ["-I", os.path.join(ROOT, "include"), "-I", CSRC]
+    obj_dir = os.path.join(HERE, "_build")
+    os.makedirs(obj_dir, exist_ok=True)
+    o_hip, o_cpp = os.path.join(obj_dir, "cache.o"), os.path.join(obj_dir, "cache_plan.o")
+    o_units = [os.path.join(obj_dir, f"cache_instances{u}.o") for u in range(CACHE_UNITS)]
+    compiles = [[hipcc, *HIPCC_FLAGS, *extra, *inc, f"-DSK_UNIT={u}", "-c", srcs[2], "-o", o] for u, o in enumerate(o_units)] + [
+        [hipcc, *HIPCC_FLAGS, *extra, *inc, "-c", srcs[0], "-o", o_hip],
+        ["g++", "-O2", "-std=c++17", "-fPIC", "-Wall", *inc, "-c", srcs[1], "-o", o_cpp],
+    ]
+    run = _runner(verbose)
+    with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:
+        list(pool.map(run, compiles))
+    run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", o_hip, *o_units, o_cpp, "-L", HERE, "-l:libsuperkernel.so", "-Wl,-rpath,$ORIGIN",
+         "-Wl,--no-undefined", "-o", lib])
+    return lib
+
+
 if __name__ == "__main__":
     print(build(force=True, verbose=True))
+    print(build_cache(verbose=True))

@@ -1,0 +1,122 @@
+// Internal declarations of libsk_cache.so, shared by its host planning and its kernels.  Not part of the public ABI
+// (include/sk_cache.h is).
+#pragma once
+
+#include <cstddef>
+#include <cstdint>
+#include <string>
+#include <vector>
+
+#include "sk_cache.h"
+
+namespace sk {
+
+constexpr int CACHE_THREADS = 256;
+// Rows of a unit of work (a key-value head of a sequence): few rows go in blocks of ROWS_FEW, whose four waves share the
+// keys among them; more than MOST_FEW rows go in blocks of ROWS_MANY, whose waves share the rows.
+constexpr int ROWS_FEW = 16, ROWS_MANY = 128, MOST_FEW = 32;
+constexpr int KEYS_FEW = 32, KEYS_MANY = 64;  // keys per step
+constexpr int MOST_SPLITS = 256;              // workgroups that share a unit's keys, at most
+
+// A problem as the kernels see it (strides in elements).
+struct AttnDev {
+  const void *qkv, *q_weight, *k_weight;
+  const float *cos, *sin;
+  void *q, *out, *k, *v;
+  const int32_t *table, *lengths, *first_row;
+  int64_t page_stride, head_stride, token_stride, qkv_row, q_row, q_head, out_row, out_head;
+  int32_t dtype, q_heads, kv_heads, group, dim, page_shift, num_pages, columns, sequences, rows, max_new, window, sinks;
+  int32_t rotary, neighbours, positions;
+  float eps, scale_log2;
+  // append: a wave takes `parts`-th of a row's heads, `heads_at_once` (of 8 elements a lane) in each of `turns`
+  int32_t lanes_per_head, turns, parts;
+  int32_t pad;
+};
+
+// A sequence of a launch: what a workgroup needs to know of it to count its units.
+struct AttnSeq {
+  const int32_t *length, *first;
+  int32_t problem, seq, kv_heads, group, window, sinks, rows, max_new;
+  int64_t capacity;  // tokens that its row of the page table can hold
+};
+
+// One kernel launch of sk_attn_launch: the sequences of the problems of one element type and class of head sizes.
+struct AttnGroup {
+  int32_t dtype, dim_class;         // 64, 96, 128, 256
+  int64_t first_seq, sequences;     // in the plan's list
+  int64_t grid_many, grid_few;      // workgroups: at least as many as there can be units, and some for splitting
+};
+
+struct AttnPlanHost {
+  std::vector<AttnDev> problems;
+  std::vector<AttnSeq> seqs;
+  std::vector<AttnGroup> groups;
+  std::vector<uint32_t> append_first;  // first workgroup of each problem, and the number of all
+  bool any_qkv = false, all_qkv = true, any_out = false, all_out = true;
+  int64_t workspace_floats = 0, counters = 0;  // of the largest group: launches of a plan do not overlap
+};
+
+// Checks and plans for that many workgroups (no HIP call).  Returns SK_OK or an error with `err` set.
+sk_status plan_attn(const sk_attn_problem *problems, int32_t n, int32_t workgroups, AttnPlanHost &out, std::string &err);
+
+// Floats of a split unit's partial result: outputs, running maximum and sum of each row.
+constexpr int64_t part_floats(int64_t rows, int64_t dim_class) { return rows * (dim_class + 2); }
+
+// One launch of page copies, by value: at most so many arrays and copies.
+constexpr int COPY_ARRAYS = 64, COPY_MOVES = 300;
+struct PageMove {
+  int32_t from, to;
+};
+struct CopyArgs {
+  struct {
+    char *base;
+    int64_t bytes;
+  } arrays[COPY_ARRAYS];
+  PageMove moves[COPY_MOVES];
+  int32_t n_arrays, n_moves;
+  int32_t *table;            // device page table (null: none)
+  const int32_t *rows;       // host memory: n_rows row numbers, then the rows
+  int32_t n_rows, columns;
+  int64_t chunks;            // of COPY_CHUNK bytes per page, of the array with the largest pages
+};
+static_assert(sizeof(CopyArgs) <= 4096, "kernel arguments");
+constexpr int64_t COPY_CHUNK = 32768;
+
+// The account of pages.
+class PageAccount {
+ public:
+  PageAccount(int32_t num_pages, int32_t page_tokens, int32_t sequences, int32_t columns);
+  sk_status resize(const int32_t *seqs, const int32_t *tokens, int32_t n, std::string &err);
+  sk_status fork(int32_t from, const int32_t *to, int32_t n, std::string &err);
+  sk_status compact();
+  // The copies called for so far, in waves: the copies of one wave do not depend on each other, waves go in order.
+  const std::vector<std::vector<PageMove>> &waves() const { return waves_; }
+  const std::vector<int32_t> &dirty_rows() const { return dirty_; }
+  void applied();
+  int32_t num_pages() const { return (int32_t)refs_.size(); }
+  int32_t sequences() const { return (int32_t)tokens_.size(); }
+  int32_t columns() const { return columns_; }
+  int32_t free_pages() const { return free_; }
+  int32_t pending() const;
+  int32_t tokens(int32_t s) const { return tokens_[s]; }
+  const int32_t *row(int32_t s) const { return table_.data() + (size_t)s * columns_; }
+
+ private:
+  int32_t held(int32_t tokens) const { return (int32_t)(((int64_t)tokens + page_tokens_ - 1) / page_tokens_); }
+  int32_t take();
+  void give(int32_t page);
+  void move(int32_t from, int32_t to);
+  void touch(int32_t s);
+  sk_status check_list(const int32_t *seqs, int32_t n, std::string &err);
+
+  int32_t page_tokens_, columns_, free_, lowest_ = 0;  // no page below lowest_ is free
+  std::vector<int32_t> refs_;                          // per page: sequences that hold it
+  std::vector<int32_t> tokens_;                        // per sequence
+  std::vector<int32_t> table_;
+  std::vector<std::vector<PageMove>> waves_;
+  std::vector<int32_t> read_, written_;  // per page: last wave that reads / writes it, from 1 on
+  std::vector<int32_t> dirty_;
+  std::vector<uint8_t> is_dirty_, mark_;
+};
+
+}  // namespace sk

@@ -1,0 +1,141 @@
+// Host code of the operators over paged caches (cache_plan.cpp) on seeded random plans and accounts, for a build with sanitizers.
+#include <cstdio>
+#include <cstdlib>
+#include <random>
+#include <set>
+
+#include "cache_internal.h"
+
+static void need(bool ok, const char *what) {
+  if (!ok) {
+    std::printf("cache_driver: %s\n", what);
+    std::exit(1);
+  }
+}
+
+static void plans(std::mt19937 &rng) {
+  auto pick = [&](int lo, int hi) { return (int)(lo + rng() % (unsigned)(hi - lo + 1)); };
+  for (int round = 0; round < 2000; ++round) {
+    std::vector<sk_attn_problem> ps((size_t)pick(0, 6));
+    uintptr_t at = (uintptr_t)1 << 40;
+    for (sk_attn_problem &p : ps) {
+      p = sk_attn_problem{};
+      p.dtype = pick(0, 20) ? pick(1, 2) : pick(-1, 3);
+      p.kv_heads = pick(1, 9);
+      p.q_heads = p.kv_heads * pick(1, 17);
+      p.head_dim = pick(0, 9) ? 8 * pick(1, 32) : pick(0, 300);
+      p.page_tokens = 16 << pick(0, 4);
+      p.num_pages = pick(1, 100000);
+      p.sequences = pick(1, 300);
+      p.pages_per_sequence = pick(1, 3000);
+      p.rows = pick(1, 5000);
+      p.max_new = pick(0, 1) ? 0 : pick(1, 6000);
+      p.window = pick(0, 1) ? 0 : pick(1, 5000);
+      p.sinks = pick(0, 9);
+      p.k = (void *)at, p.v = (void *)at, p.page_table = p.lengths = p.first_row = (int32_t *)at;
+      at += (uintptr_t)1 << 36;
+      p.q = (void *)at;
+      at += (uintptr_t)1 << 36;
+      p.out = pick(0, 5) ? (void *)at : nullptr;
+      at += (uintptr_t)1 << 36;
+      p.qkv = pick(0, 3) ? (void *)at : nullptr;
+      if (pick(0, 30) == 0) p.token_stride = 8 * pick(0, 100), p.kv_head_stride = 8 * pick(0, 1000), p.page_stride = 8 * pick(0, 100000);
+    }
+    sk::AttnPlanHost h;
+    std::string err;
+    const sk_status st = sk::plan_attn(ps.data(), (int32_t)ps.size(), 512, h, err);
+    need((st == SK_OK) == err.empty(), "an error without a text, or a text without an error");
+    if (st != SK_OK) continue;
+    need(h.problems.size() == ps.size() && h.append_first.size() == ps.size() + 1, "sizes");
+    int64_t seqs = 0;
+    for (size_t i = 0; i < ps.size(); ++i) {
+      const sk::AttnDev &d = h.problems[i];
+      if (d.out) seqs += d.sequences;
+      const int64_t per_row = (int64_t)d.parts * d.turns * (64 / d.lanes_per_head);
+      need(per_row >= d.q_heads + 2 * d.kv_heads, "append leaves heads out");
+      if (d.qkv) need(((int64_t)h.append_first[i + 1] - h.append_first[i]) * 4 >= (int64_t)d.rows * d.parts, "append leaves rows out");
+    }
+    need((int64_t)h.seqs.size() == seqs, "sequences");
+    // units of the largest steps that the bounds allow fit the grids
+    for (const sk::AttnGroup &g : h.groups) {
+      int64_t few = 0, many = 0;
+      for (int64_t s = g.first_seq; s < g.first_seq + g.sequences; ++s) {
+        const sk::AttnSeq &q = h.seqs[(size_t)s];
+        few += (int64_t)q.kv_heads * ((std::min<int64_t>((int64_t)q.group * q.max_new, sk::MOST_FEW) + sk::ROWS_FEW - 1) / sk::ROWS_FEW);
+        if ((int64_t)q.max_new * q.group > sk::MOST_FEW && q.seq == 0) many += (int64_t)q.kv_heads * (((int64_t)q.rows * q.group + sk::ROWS_MANY - 1) / sk::ROWS_MANY);
+      }
+      need(g.grid_few >= few && g.grid_many >= many, "units without a workgroup");
+      need(h.counters >= g.grid_few + g.grid_many, "counters");
+      need(h.workspace_floats >= g.grid_few * sk::part_floats(sk::ROWS_FEW, g.dim_class) + g.grid_many * sk::part_floats(sk::ROWS_MANY, g.dim_class), "workspace");
+    }
+  }
+}
+
+static void accounts(std::mt19937 &rng) {
+  auto pick = [&](int lo, int hi) { return (int)(lo + rng() % (unsigned)(hi - lo + 1)); };
+  for (int round = 0; round < 60; ++round) {
+    const int pages = pick(1, 80), page = pick(1, 20), seqs = pick(1, 9), columns = pick(1, 12);
+    sk::PageAccount a(pages, page, seqs, columns);
+    // what lies in the pages: the copies move it, writes renew it
+    std::vector<int> content((size_t)pages, 0);
+    std::vector<std::vector<int>> want((size_t)seqs);  // per sequence: content of each of its pages
+    int next = 0;
+    for (int step = 0; step < 300; ++step) {
+      std::string err;
+      const int what = pick(0, 9);
+      if (what == 0) {
+        a.compact();
+      } else if (what <= 2) {
+        const int32_t from = pick(0, seqs - 1), to = pick(0, seqs - 1);
+        if (a.fork(from, &to, 1, err) == SK_OK) want[(size_t)to] = want[(size_t)from];
+      } else {
+        std::vector<int32_t> ids, tokens;
+        for (int s = 0; s < seqs; ++s)
+          if (pick(0, 2) == 0) ids.push_back(s), tokens.push_back(pick(0, 1) ? std::min(a.tokens(s) + pick(0, 3), page * columns) : pick(0, page * columns));
+        const std::vector<std::vector<int>> before = want;
+        std::vector<int32_t> had;
+        for (int32_t s : ids) had.push_back(a.tokens(s));
+        if (a.resize(ids.data(), tokens.data(), (int32_t)ids.size(), err) == SK_OK)
+          for (size_t i = 0; i < ids.size(); ++i) want[(size_t)ids[i]].resize((size_t)((tokens[i] + page - 1) / page), -1);
+      }
+      if (pick(0, 2) == 0) {
+        for (const auto &w : a.waves()) {
+          std::set<int32_t> read, written;
+          for (const sk::PageMove &m : w) {
+            read.insert(m.from);
+            need(written.insert(m.to).second, "a page written twice in a wave");
+          }
+          for (int32_t p : written) need(!read.count(p), "a page read and written in a wave");
+          for (const sk::PageMove &m : w) content[(size_t)m.to] = content[(size_t)m.from];
+        }
+        a.applied();
+        need(a.pending() == 0 && a.dirty_rows().empty(), "something pending behind applied()");
+        // pages new since the last time are written now, by those that hold them
+        for (int s = 0; s < seqs; ++s)
+          for (size_t c = 0; c < want[(size_t)s].size(); ++c) {
+            int &x = content[(size_t)a.row(s)[c]];
+            if (want[(size_t)s][c] == -1) {
+              x = ++next;
+              for (int t = 0; t < seqs; ++t)  // forked before it was written
+                for (size_t d = 0; d < want[(size_t)t].size(); ++d)
+                  if (a.row(t)[d] == a.row(s)[c]) want[(size_t)t][d] = x;
+            }
+            need(x == want[(size_t)s][c], "a page's content got lost");
+          }
+      }
+      std::set<int32_t> used;
+      for (int s = 0; s < seqs; ++s)
+        for (int c = 0; c < columns; ++c)
+          if (a.row(s)[c] >= 0) used.insert(a.row(s)[c]);
+      need((int)used.size() == pages - a.free_pages(), "free pages");
+    }
+  }
+}
+
+int main() {
+  std::mt19937 rng(7);
+  plans(rng);
+  accounts(rng);
+  std::printf("cache_driver: ok\n");
+  return 0;
+}
