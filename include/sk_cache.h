@@ -96,7 +96,7 @@ typedef struct {
 
 typedef struct {
   int32_t host_only;  /* 1: check and plan on the host only (launches then give SK_ERR_STATE)                     */
-  int32_t workgroups; /* workgroups that the work of few rows is split for; 0 = 2 per compute unit of the device  */
+  int32_t workgroups; /* workgroups at a time that the work is split for; 0 = as many as the device holds         */
   int32_t reserved[2];
 } sk_attn_params;
 
@@ -108,7 +108,7 @@ void sk_attn_params_default(sk_attn_params *params);
  * Plan for n problems (n = 0: launches do nothing).  Errors: SK_ERR_INVALID_ARG (null pointers, sizes < 1, strides that let
  * heads or tokens overlap, cos and sin with too few rows), SK_ERR_UNSUPPORTED (SK_F32; a head_dim that is no multiple of
  * 8 or larger than 256; page_tokens that is no power of two from 16 on; pointers or strides that are no multiples of 16 bytes;
- * sequences of 2^31 tokens and more; sizes that a launch's grid cannot hold), SK_ERR_OVERLAP (q or out of two problems, or of one,
+ * sequences of 2^31 tokens and more; a token_stride of 2^26 elements and more; sizes that a launch's grid cannot hold), SK_ERR_OVERLAP (q or out of two problems, or of one,
  * intersect), SK_ERR_ALLOC, SK_ERR_HIP.
  */
 sk_status sk_attn_plan_create(const sk_attn_problem *problems, int32_t n, const sk_attn_params *params, sk_attn_plan **out);
@@ -116,7 +116,7 @@ sk_status sk_attn_plan_create(const sk_attn_problem *problems, int32_t n, const 
 sk_status sk_attn_plan_destroy(sk_attn_plan *plan);
 /* Norms, rotation and append of every problem: one kernel launch. */
 sk_status sk_attn_append(sk_attn_plan *plan, void *hip_stream);
-/* Attention of every problem: one kernel launch per element type and class of head sizes (up to 64, 96, 128, 256). */
+/* Attention of every problem: one kernel launch for all problems with heads of up to 128 elements, one for those with larger ones. */
 sk_status sk_attn_launch(sk_attn_plan *plan, void *hip_stream);
 /* Kernel launches that sk_attn_launch makes, and bytes of the plan's workspace (either may be null). */
 sk_status sk_attn_plan_info(const sk_attn_plan *plan, int32_t *launches, int64_t *workspace_bytes);

@@ -16,7 +16,7 @@ HEADERS = ["kernels.hip.h", "sk_internal.h", os.path.join(ROOT, "include", "supe
 
 CACHE_LIB = os.path.join(HERE, "libsk_cache.so")  # attention's side of decoder layers (include/sk_cache.h)
 CACHE_SOURCES = ["cache.hip", "cache_plan.cpp", "cache_instances.hip"]
-CACHE_UNITS = 8  # units of compilation of cache_instances.hip
+CACHE_UNITS = 4  # units of compilation of cache_instances.hip
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

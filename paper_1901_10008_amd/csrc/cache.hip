@@ -9,16 +9,10 @@
 #include "sk_internal.h"
 
 namespace sk {
-#define SK_ATTEND(dt, dp) extern template __global__ void sk_attend<dt, dp>(AttnArgs);
-SK_ATTEND(SK_BF16, 64)
-SK_ATTEND(SK_BF16, 96)
-SK_ATTEND(SK_BF16, 128)
-SK_ATTEND(SK_BF16, 256)
-SK_ATTEND(SK_F16, 64)
-SK_ATTEND(SK_F16, 96)
-SK_ATTEND(SK_F16, 128)
-SK_ATTEND(SK_F16, 256)
-#undef SK_ATTEND
+extern template __global__ void sk_attend<false, false>(AttnArgs);
+extern template __global__ void sk_attend<true, false>(AttnArgs);
+extern template __global__ void sk_attend<false, true>(AttnArgs);
+extern template __global__ void sk_attend<true, true>(AttnArgs);
 }  // namespace sk
 
 namespace {
@@ -116,13 +110,8 @@ sk_status launch(K kernel, int64_t grid, hipStream_t stream, hipEvent_t behind, 
 }
 
 void (*attend_kernel(const sk::AttnGroup &g))(sk::AttnArgs) {
-  const bool bf16 = g.dtype == SK_BF16;
-  switch (g.dim_class) {
-    case 64: return bf16 ? sk::sk_attend<SK_BF16, 64> : sk::sk_attend<SK_F16, 64>;
-    case 96: return bf16 ? sk::sk_attend<SK_BF16, 96> : sk::sk_attend<SK_F16, 96>;
-    case 128: return bf16 ? sk::sk_attend<SK_BF16, 128> : sk::sk_attend<SK_F16, 128>;
-    default: return bf16 ? sk::sk_attend<SK_BF16, 256> : sk::sk_attend<SK_F16, 256>;
-  }
+  if (g.wide) return g.many ? sk::sk_attend<true, true> : sk::sk_attend<false, true>;
+  return g.many ? sk::sk_attend<true, false> : sk::sk_attend<false, false>;
 }
 
 void release(sk_attn_plan *plan) {
@@ -224,7 +213,7 @@ sk_status sk_attn_plan_create(const sk_attn_problem *problems, int32_t n, const 
     try {
       plan->device = device;
       std::string err;
-      sk_status st = sk::plan_attn(problems, n, prm.workgroups ? prm.workgroups : 2 * cus, plan->host, err);
+      sk_status st = sk::plan_attn(problems, n, cus, prm.workgroups, plan->host, err);
       if (st != SK_OK) st = set_last_error(st, err);
       if (st == SK_OK && !prm.host_only) st = make_resident(plan);
       if (st != SK_OK) {
@@ -291,8 +280,9 @@ sk_status sk_attn_launch(sk_attn_plan *plan, void *hip_stream) {
       a.sequences = (int32_t)g.sequences;
       a.grid_many = (uint32_t)g.grid_many;
       a.grid_few = (uint32_t)g.grid_few;
+      a.workgroups = (int32_t)g.workgroups;
       a.ws_many = plan->workspace;
-      a.ws_few = plan->workspace + g.grid_many * sk::part_floats(sk::ROWS_MANY, g.dim_class);
+      a.ws_few = plan->workspace + g.grid_many * sk::part_floats(sk::ROWS_MANY, g.wide ? 256 : 128);
       a.arrivals = plan->arrivals;
       st = launch(attend_kernel(g), g.grid_many + g.grid_few, stream, &g == &plan->host.groups.back() ? behind : nullptr, a);
       if (st != SK_OK) break;

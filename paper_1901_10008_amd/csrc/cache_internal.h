@@ -15,7 +15,8 @@ constexpr int CACHE_THREADS = 256;
 // Rows of a unit of work (a key-value head of a sequence): few rows go in blocks of ROWS_FEW, whose four waves share the
 // keys among them; more than MOST_FEW rows go in blocks of ROWS_MANY, whose waves share the rows.
 constexpr int ROWS_FEW = 16, ROWS_MANY = 128, MOST_FEW = 32;
-constexpr int KEYS_FEW = 32, KEYS_MANY = 64;  // keys per step
+constexpr int KEYS_FEW = 32;                                  // keys per step
+constexpr int keys_many(int dim) { return dim <= 128 ? 64 : 32; }  // (heads of 256: what a thread has in flight has to fit its registers)
 constexpr int MOST_SPLITS = 256;              // workgroups that share a unit's keys, at most
 
 // A problem as the kernels see it (strides in elements).
@@ -40,12 +41,15 @@ struct AttnSeq {
   int64_t capacity;  // tokens that its row of the page table can hold
 };
 
-// One kernel launch of sk_attn_launch: the sequences of the problems of one element type and class of head sizes.
+// One kernel launch of sk_attn_launch: the sequences of the problems with heads of up to 128 elements, or those with larger ones.
 struct AttnGroup {
-  int32_t dtype, dim_class;         // 64, 96, 128, 256
-  int64_t first_seq, sequences;     // in the plan's list
-  int64_t grid_many, grid_few;      // workgroups: at least as many as there can be units, and some for splitting
+  bool wide, many;              // larger heads; units of many rows are possible
+  int64_t first_seq, sequences; // in the plan's list
+  int64_t grid_many, grid_few;  // workgroups: at least as many as there can be units, and some for splitting
+  int64_t workgroups;           // that the device runs at a time
 };
+// Workgroups of a kernel that a compute unit holds (its registers and LDS).
+constexpr int resident(bool wide, bool many) { return wide ? 1 : 2; }
 
 struct AttnPlanHost {
   std::vector<AttnDev> problems;
@@ -56,11 +60,12 @@ struct AttnPlanHost {
   int64_t workspace_floats = 0, counters = 0;  // of the largest group: launches of a plan do not overlap
 };
 
-// Checks and plans for that many workgroups (no HIP call).  Returns SK_OK or an error with `err` set.
-sk_status plan_attn(const sk_attn_problem *problems, int32_t n, int32_t workgroups, AttnPlanHost &out, std::string &err);
+// Checks and plans for a device of that many compute units, or for that many workgroups at a time (0: what its compute units hold); no HIP
+// call.  Returns SK_OK or an error with `err` set.
+sk_status plan_attn(const sk_attn_problem *problems, int32_t n, int32_t compute_units, int32_t workgroups, AttnPlanHost &out, std::string &err);
 
 // Floats of a split unit's partial result: outputs, running maximum and sum of each row.
-constexpr int64_t part_floats(int64_t rows, int64_t dim_class) { return rows * (dim_class + 2); }
+constexpr int64_t part_floats(int64_t rows, int64_t most_dim) { return rows * (most_dim + 2); }
 
 // One launch of page copies, by value: at most so many arrays and copies.
 constexpr int COPY_ARRAYS = 64, COPY_MOVES = 300;

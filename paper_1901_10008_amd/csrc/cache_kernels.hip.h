@@ -76,6 +76,50 @@ __device__ __forceinline__ void mma32(const u32x4 &a, const u32x4 &b, f32x16 &c)
 __device__ __forceinline__ u32x2 read_transposed(const unsigned char *p) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(unsigned char *)p));
 }
+// What nothing writes while the kernel runs, read through the scalar cache (its address the same in all lanes).
+#define SK_CONSTANT __attribute__((address_space(4)))
+// Sum over the lanes up to this one, in the vector unit: within rows of 16, then from row to row.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int32_t shifted(int32_t v) {
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int64_t shifted(int64_t v) {
+  const uint32_t lo = (uint32_t)shifted<CTRL, ROWS>((int32_t)v), hi = (uint32_t)shifted<CTRL, ROWS>((int32_t)(v >> 32));
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+template <class T>
+__device__ __forceinline__ T wave_scan(T v) {
+  v += shifted<0x111, 0xf>(v);  // row_shr:1, 2, 4, 8
+  v += shifted<0x112, 0xf>(v);
+  v += shifted<0x114, 0xf>(v);
+  v += shifted<0x118, 0xf>(v);
+  v += shifted<0x142, 0xa>(v);  // row_bcast:15 into the second and fourth row
+  v += shifted<0x143, 0xc>(v);  // row_bcast:31 into the upper half
+  return v;
+}
+__device__ __forceinline__ int32_t lane_of(int32_t v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+__device__ __forceinline__ int64_t lane_of(int64_t v, int lane) {
+  return (int64_t)((uint64_t)(uint32_t)lane_of((int32_t)(v >> 32), lane) << 32 | (uint32_t)lane_of((int32_t)v, lane));
+}
+// The larger (or the sum) of a lane's value and that of the lane 16, or 32, places away, without a trip through LDS.
+__device__ __forceinline__ void across16(float v, float &a, float &b) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+  const uint32_t x = r[0], y = r[1];  // (a bit cast of a single vector element reads element 0)
+  a = __builtin_bit_cast(float, x);
+  b = __builtin_bit_cast(float, y);
+}
+__device__ __forceinline__ void across32(float v, float &a, float &b) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+  const uint32_t x = r[0], y = r[1];  // (a bit cast of a single vector element reads element 0)
+  a = __builtin_bit_cast(float, x);
+  b = __builtin_bit_cast(float, y);
+}
+__device__ __forceinline__ float max16(float v) { float a, b; across16(v, a, b); return fmaxf(a, b); }
+__device__ __forceinline__ float max32(float v) { float a, b; across32(v, a, b); return fmaxf(a, b); }
+__device__ __forceinline__ float sum16(float v) { float a, b; across16(v, a, b); return a + b; }
+__device__ __forceinline__ float sum32(float v) { float a, b; across32(v, a, b); return a + b; }
+
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Partial results that another workgroup reads, maybe behind another L2: written through to memory and read from there
@@ -94,27 +138,19 @@ __device__ __forceinline__ f32x2 load_shared(const float *p) {
 // keys) are counted on the device: every workgroup looks at all sequences of the launch and finds its own unit from the sums
 // before it.  Units of many rows come first, those of late rows (which see the most) before those of early ones; key-value heads
 // vary fastest, so that with eight of them each has a die (and its L2) of its own.
-struct Unit {
-  int32_t problem, seq;
-  int32_t head, block;          // key-value head, block of rows
-  int32_t split, splits;
-  uint32_t slot;                // this workgroup's place in the workspace
-  uint32_t first_slot;          // of the unit's first slice: also its arrival counter
-  bool many, any;
-};
 
 // A sequence in this step: rows and lengths cut to the bounds that the grid was made for.
 struct Step {
   int32_t first, fresh, length, behind;  // first row, rows to compute, tokens, position of the first new token
 };
-__device__ __forceinline__ Step step_of(const int32_t *length, const int32_t *first, int32_t rows, int32_t max_new, int64_t capacity) {
-  const int32_t a = load_i32(first), b = load_i32(first + 1), n = load_i32(length);
+__device__ __forceinline__ Step step_of(const AttnSeq &q) {
+  const int32_t a = load_i32(q.first), b = load_i32(q.first + 1), n = load_i32(q.length);
   Step s;
-  s.first = min(max(a, 0), rows);
-  const int32_t all = min(max(b, s.first), rows) - s.first;
-  s.length = (int32_t)min((int64_t)max(n, 0), capacity);
+  s.first = min(max(a, 0), q.rows);
+  const int32_t all = min(max(b, s.first), q.rows) - s.first;
+  s.length = (int32_t)min((int64_t)max(n, 0), q.capacity);
   s.behind = s.length - all;
-  s.fresh = min(all, max_new);
+  s.fresh = min(all, q.max_new);
   return s;
 }
 // The keys that rows at positions p0 .. p1 see: blocks of KEYS from 0 on that hold sinks, then blocks from `low` on.
@@ -124,10 +160,9 @@ struct Span {
 template <int KEYS>
 __device__ __forceinline__ Span span_of(int32_t p0, int32_t p1, int32_t window, int32_t sinks) {
   Span s;
-  s.low = window ? max(0, (int32_t)max((int64_t)p0 - window + 1, (int64_t)0)) & ~(KEYS - 1) : 0;
-  s.sink_blocks = window ? (int32_t)(((int64_t)min(sinks, s.low) + KEYS - 1) / KEYS) : 0;
+  s.low = window ? (p0 >= window ? p0 - window + 1 : 0) & ~(KEYS - 1) : 0;
+  s.sink_blocks = window ? (min(sinks, s.low) + KEYS - 1) / KEYS : 0;
   s.blocks = p1 < 0 ? 0 : s.sink_blocks + (p1 - s.low) / KEYS + 1;
-  if (p1 < 0) s.sink_blocks = 0;
   return s;
 }
 
@@ -135,54 +170,41 @@ struct Count {
   int32_t units, blocks;  // blocks of keys of an average unit
   bool many;
 };
+template <bool MANY, bool WIDE>
 __device__ __forceinline__ Count count_units(const Step &s, int32_t kv_heads, int32_t group, int32_t window, int32_t sinks) {
   Count c;
   const int64_t rows = (int64_t)s.fresh * group;
-  c.many = rows > MOST_FEW;
-  const int32_t per = c.many ? ROWS_MANY : ROWS_FEW;
-  const int32_t row_blocks = (int32_t)((rows + per - 1) / per);
-  c.units = row_blocks * kv_heads;
-  const int32_t tokens = (per + group - 1) / group, last = s.behind + s.fresh - 1;
+  const int32_t last = s.behind + s.fresh - 1;
+  c.many = MANY && rows > MOST_FEW;
   if (c.many) {
-    const Span a = span_of<KEYS_MANY>(s.behind, min(s.behind + tokens - 1, last), window, sinks);
-    const Span b = span_of<KEYS_MANY>(max(last - tokens + 1, s.behind), last, window, sinks);
+    c.units = (int32_t)((rows + ROWS_MANY - 1) / ROWS_MANY) * kv_heads;
+    const int32_t tokens = (ROWS_MANY + group - 1) / group;
+    constexpr int KEYS = keys_many(WIDE ? 256 : 128);
+    const Span a = span_of<KEYS>(s.behind, min(s.behind + tokens - 1, last), window, sinks);
+    const Span b = span_of<KEYS>(max(last - tokens + 1, s.behind), last, window, sinks);
     c.blocks = (a.blocks + b.blocks + 1) / 2;
   } else {
+    c.units = (int32_t)((rows + ROWS_FEW - 1) / ROWS_FEW) * kv_heads;
     c.blocks = span_of<KEYS_FEW>(s.behind, last, window, sinks).blocks;
   }
   return c;
 }
 
-struct FindScratch {
-  int64_t total[2][4];  // blocks of keys over all units (many, few), per wave
-  int32_t units[2][4];
-  int32_t items[2][4];
-  Unit unit;
+struct Unit {
+  int32_t problem, seq;
+  int32_t head, block;          // key-value head, block of rows
+  int32_t split, splits;
+  uint32_t slot;                // this workgroup's place in the workspace
+  uint32_t first_slot;          // of the unit's first slice: also its arrival counter
+  Step step;
+  bool any;
 };
-
-__device__ __forceinline__ int64_t wave_sum64(int64_t v) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
-  return v;
-}
-__device__ __forceinline__ int32_t wave_sum(int32_t v) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
-  return v;
-}
-__device__ __forceinline__ int32_t wave_scan(int32_t v, int lane) {  // inclusive
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int32_t o = __shfl_up(v, d);
-    if (lane >= d) v += o;
-  }
-  return v;
-}
 
 struct AttnArgs {
   const AttnDev *problems;
   const AttnSeq *seqs;
   int32_t sequences;
+  int32_t workgroups;  // that the card runs at a time
   uint32_t grid_many, grid_few;
   float *ws_many, *ws_few;
   uint32_t *arrivals;  // grid_many + grid_few, zero between launches
@@ -190,7 +212,9 @@ struct AttnArgs {
 
 // How many blocks of keys a slice takes so that all slices fit `grid` workgroups: ceil(blocks / that) over the units adds up to
 // total / that + units at most.  No unit is split where the units alone do not leave room.
-__device__ __forceinline__ int32_t blocks_per_slice(int64_t total, int64_t units, int64_t grid, int32_t least) {
+__device__ __forceinline__ int32_t blocks_per_slice(int64_t total, int64_t units, int64_t grid, int64_t workgroups, int32_t least) {
+  // One round of workgroups where the units leave room for it, else as many as the grid has.
+  if (2 * units <= workgroups) grid = min(grid, workgroups);
   if (units >= grid) return 0x7fffffff;
   const int64_t per = (total + (grid - units) - 1) / (grid - units);
   return (int32_t)min(max(per, (int64_t)least), (int64_t)0x7fffffff);
@@ -199,90 +223,134 @@ __device__ __forceinline__ int32_t splits_of(int32_t blocks, int32_t per) {
   return min(max((int32_t)(((int64_t)blocks + per - 1) / per), 1), MOST_SPLITS);
 }
 constexpr int LEAST_FEW = 4;   // a block of keys for each wave
-constexpr int LEAST_MANY = 4;  // 256 keys
+constexpr int LEAST_MANY = 4;
 
-__device__ __forceinline__ void find_unit(const AttnArgs &a, FindScratch *f) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int per = (a.sequences + CACHE_THREADS - 1) / CACHE_THREADS;
-  const int s0 = tid * per, s1 = min(s0 + per, a.sequences);
-  auto look = [&](int s) {
-    const AttnSeq q = a.seqs[s];
-    return count_units(step_of(q.length, q.first, q.rows, q.max_new, q.capacity), q.kv_heads, q.group, q.window, q.sinks);
-  };
-  int64_t total_many = 0, total_few = 0;
-  int32_t units_many = 0, units_few = 0;
-  Count mine = {};  // (the only one, with at most CACHE_THREADS sequences)
-  for (int s = s0; s < s1; ++s) {
-    mine = look(s);
-    (mine.many ? total_many : total_few) += (int64_t)mine.units * mine.blocks;
-    (mine.many ? units_many : units_few) += mine.units;
+struct FindScratch {
+  int64_t total[2][4];  // blocks of keys over all units (many, few), per wave
+  int32_t units[2][4], items[2][4];
+  Unit unit;
+};
+
+// Unit number i of a sequence's.
+__device__ __forceinline__ Unit unit_of(const AttnSeq &q, const Step &s, const Count &c, int32_t splits, int32_t i, uint32_t item) {
+  const int32_t rest = i / q.kv_heads;
+  Unit u;
+  u.problem = q.problem;
+  u.seq = q.seq;
+  u.head = i % q.kv_heads;
+  u.split = rest % splits;
+  u.splits = splits;
+  u.block = c.units / q.kv_heads - 1 - rest / splits;
+  u.slot = item;
+  u.first_slot = item - (uint32_t)(u.split * q.kv_heads);
+  u.step = s;
+  u.any = true;
+  return u;
+}
+__device__ __forceinline__ Unit unit_in_lane(const Unit &u, int lane) {
+  Unit r;
+  r.problem = lane_of(u.problem, lane);
+  r.seq = lane_of(u.seq, lane);
+  r.head = lane_of(u.head, lane);
+  r.block = lane_of(u.block, lane);
+  r.split = lane_of(u.split, lane);
+  r.splits = lane_of(u.splits, lane);
+  r.slot = (uint32_t)lane_of((int32_t)u.slot, lane);
+  r.first_slot = (uint32_t)lane_of((int32_t)u.first_slot, lane);
+  r.step.first = lane_of(u.step.first, lane);
+  r.step.fresh = lane_of(u.step.fresh, lane);
+  r.step.length = lane_of(u.step.length, lane);
+  r.step.behind = lane_of(u.step.behind, lane);
+  r.any = true;
+  return r;
+}
+
+// MANY: units of many rows may be there.  Workgroups below grid_many take them, the others those of few.
+template <bool MANY, bool WIDE>
+__device__ __forceinline__ Unit find_unit(const AttnArgs &a, FindScratch *f) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const bool many = MANY && blockIdx.x < a.grid_many;
+  const int32_t item = (int32_t)(many ? blockIdx.x : blockIdx.x - a.grid_many);
+  if (a.sequences <= 64) {
+    // a sequence per lane, every wave for itself
+    AttnSeq q{};
+    q.kv_heads = 1;
+    Step s{};
+    Count c{0, 0, false};
+    if (lane < a.sequences) {
+      q = a.seqs[lane];
+      s = step_of(q);
+      c = count_units<MANY, WIDE>(s, q.kv_heads, q.group, q.window, q.sinks);
+    }
+    const bool ours = c.many == many;
+    const int32_t units = ours ? c.units : 0;
+    const int64_t all_blocks = lane_of(wave_scan((int64_t)units * c.blocks), 63);
+    const int32_t all_units = lane_of(wave_scan(units), 63);
+    const int32_t per = blocks_per_slice(all_blocks, all_units, many ? a.grid_many : a.grid_few, a.workgroups, many ? LEAST_MANY : LEAST_FEW);
+    const int32_t splits = splits_of(c.blocks, per), n = units * splits, upto = wave_scan(n);
+    const uint64_t hit = __ballot(item >= upto - n && item < upto);
+    Unit u{};
+    u.any = hit != 0;
+    if (!u.any) return u;
+    const int who = __builtin_ctzll(hit);
+    return unit_in_lane(unit_of(q, s, c, splits, item - (upto - n), (uint32_t)item), who);
   }
-  total_many = wave_sum64(total_many);
-  total_few = wave_sum64(total_few);
-  const int32_t um = wave_sum(units_many), uf = wave_sum(units_few);
+  // a run of sequences per thread
+  const int per_thread = (a.sequences + CACHE_THREADS - 1) / CACHE_THREADS;
+  const int s0 = tid * per_thread, s1 = min(s0 + per_thread, a.sequences);
+  auto look = [&](int i, AttnSeq &q, Step &s) {
+    q = a.seqs[i];
+    s = step_of(q);
+    return count_units<MANY, WIDE>(s, q.kv_heads, q.group, q.window, q.sinks);
+  };
+  AttnSeq q{};
+  Step s{};
+  Count c{0, 0, false};
+  int64_t total = 0;
+  int32_t units = 0;
+  for (int i = s0; i < s1; ++i) {
+    c = look(i, q, s);
+    if (c.many != many) continue;
+    total += (int64_t)c.units * c.blocks;
+    units += c.units;
+  }
+  total = lane_of(wave_scan(total), 63);
+  units = lane_of(wave_scan(units), 63);
   if (lane == 0) {
-    f->total[0][wave] = total_many;
-    f->total[1][wave] = total_few;
-    f->units[0][wave] = um;
-    f->units[1][wave] = uf;
+    f->total[0][wave] = total;
+    f->units[0][wave] = units;
   }
   if (tid == 0) f->unit.any = false;
   __syncthreads();
-  int64_t total[2] = {0, 0}, units[2] = {0, 0};
-#pragma unroll
-  for (int w = 0; w < 4; ++w)
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      total[k] += f->total[k][w];
-      units[k] += f->units[k][w];
-    }
-  const int32_t per_many = blocks_per_slice(total[0], units[0], a.grid_many, LEAST_MANY);
-  const int32_t per_few = blocks_per_slice(total[1], units[1], a.grid_few, LEAST_FEW);
-  int32_t items_many = 0, items_few = 0;
-  for (int s = s0; s < s1; ++s) {
-    const Count c = per == 1 ? mine : look(s);
-    (c.many ? items_many : items_few) += c.units * splits_of(c.blocks, c.many ? per_many : per_few);
+  total = f->total[0][0] + f->total[0][1] + f->total[0][2] + f->total[0][3];
+  const int64_t all_units = (int64_t)f->units[0][0] + f->units[0][1] + f->units[0][2] + f->units[0][3];
+  const int32_t per = blocks_per_slice(total, all_units, many ? a.grid_many : a.grid_few, a.workgroups, many ? LEAST_MANY : LEAST_FEW);
+  int32_t n = 0;
+  for (int i = s0; i < s1; ++i) {
+    if (per_thread > 1) c = look(i, q, s);
+    if (c.many == many) n += c.units * splits_of(c.blocks, per);
   }
-  const int32_t scan_many = wave_scan(items_many, lane), scan_few = wave_scan(items_few, lane);
-  if (lane == 63) {
-    f->items[0][wave] = scan_many;
-    f->items[1][wave] = scan_few;
-  }
+  const int32_t upto = wave_scan(n);
+  if (lane == 63) f->items[0][wave] = upto;
   __syncthreads();
-  // workgroups below grid_many take units of many rows, the others those of few
-  const bool many = blockIdx.x < a.grid_many;
-  const int k = many ? 0 : 1;
-  const int32_t item = (int32_t)(many ? blockIdx.x : blockIdx.x - a.grid_many);
-  int32_t before = (many ? scan_many - items_many : scan_few - items_few);
-  for (int w = 0; w < wave; ++w) before += f->items[k][w];
-  if (item >= before && item < before + (many ? items_many : items_few)) {
+  int32_t before = upto - n;
+  for (int w = 0; w < wave; ++w) before += f->items[0][w];
+  if (item >= before && item < before + n) {
     int32_t at = before;
-    for (int s = s0; s < s1; ++s) {
-      const Count c = per == 1 ? mine : look(s);
+    for (int i = s0; i < s1; ++i) {
+      if (per_thread > 1) c = look(i, q, s);
       if (c.many != many) continue;
-      const int32_t splits = splits_of(c.blocks, many ? per_many : per_few);
-      const int32_t n = c.units * splits;
-      if (item < at + n) {
-        const AttnSeq q = a.seqs[s];
-        const int32_t i = item - at, rest = i / q.kv_heads;
-        Unit u;
-        u.problem = q.problem;
-        u.seq = q.seq;
-        u.head = i % q.kv_heads;
-        u.split = rest % splits;
-        u.splits = splits;
-        u.block = c.units / q.kv_heads - 1 - rest / splits;
-        u.slot = (uint32_t)item;
-        u.first_slot = (uint32_t)(item - u.split * q.kv_heads);
-        u.many = many;
-        u.any = true;
-        f->unit = u;
+      const int32_t splits = splits_of(c.blocks, per), here = c.units * splits;
+      if (item < at + here) {
+        f->unit = unit_of(q, s, c, splits, item - at, (uint32_t)item);
         break;
       }
-      at += n;
+      at += here;
     }
   }
   __syncthreads();
+  if (!f->unit.any) return f->unit;
+  return unit_in_lane(f->unit, 0);
 }
 
 // The slices of a unit but the last to arrive leave; true for that one.  Every wave's partial results have gone through to memory
@@ -304,8 +372,8 @@ __device__ __forceinline__ bool last_to_arrive(uint32_t *arrivals, int32_t split
 // pages
 // ---------------------------------------------------------------------------
 // Sixteen consecutive keys from a multiple of 16 on lie in one page.  Page numbers are read through the scalar cache (nothing writes the
-// table while the kernel runs), a step ahead of the keys and values that need them.
-#define SK_CONSTANT __attribute__((address_space(4)))
+// table while the kernel runs), a step ahead of the keys and values that need them; addresses are a scalar base for the sixteen keys and an
+// offset per lane that never changes.
 struct Pages {
   const int32_t *row;
   int32_t shift, num_pages, columns;
@@ -315,9 +383,9 @@ struct Pages {
     return c < columns ? ((const SK_CONSTANT int32_t *)(uintptr_t)row)[c] : -1;
   }
   __device__ __forceinline__ bool there(int32_t page) const { return (uint32_t)page < (uint32_t)num_pages; }
-  // element offset of a key in a page that is there
-  __device__ __forceinline__ int64_t offset(int32_t page, int32_t key) const {
-    return (int64_t)page * page_stride + (int64_t)(key & ((1 << shift) - 1)) * token_stride;
+  // Byte offset of a key.  Where its page is not there, of one in page 0, whose memory can be read: what is read there does not enter a result.
+  __device__ __forceinline__ int64_t bytes(int32_t page, int32_t key) const {
+    return 2 * ((int64_t)(there(page) ? page : 0) * page_stride + (int64_t)(key & ((1 << shift) - 1)) * token_stride);
   }
 };
 
@@ -325,10 +393,49 @@ struct Pages {
 // M = max(m, m'), l = l exp2(m - M) + sum exp2(s - M), and the outputs so far are scaled by the same exp2(m - M).  A row that
 // has seen nothing has m = -inf; exp2 is then taken relative to 0, so that it stays at l = 0.
 __device__ __forceinline__ float base_of(float m) { return m == -__builtin_inff() ? 0.f : m; }
+__device__ __forceinline__ float inverse(float sum) { return sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum); }  // (nothing seen: 0)
 
 // Whether the token at position p sees key j.
 __device__ __forceinline__ bool sees(int32_t p, int32_t j, int32_t window, int32_t sinks) {
   return j <= p && (window == 0 || p - j < window || j < sinks);
+}
+
+// Values that some rows of a unit see and others do not must not reach the others, whatever they are; finite ones do not (their
+// weight is 0), but 0 * inf is NaN.  Where a step's keys are not seen by all rows alike, values that are not finite are taken out
+// on the way into LDS and, if there were any, added to the rows that see them at the end.  A row that sees one ends up not finite.
+template <int DT>
+__device__ __forceinline__ uint32_t odd_halves(uint32_t w) {  // 0xffff in each half that is not finite
+  constexpr uint32_t E = DT == SK_BF16 ? 0x7f80u : 0x7c00u;
+  return ((w & E) == E ? 0xffffu : 0u) | ((w >> 16 & E) == E ? 0xffff0000u : 0u);
+}
+template <int DT>
+__device__ __forceinline__ bool clean(u32x4 &v) {
+  uint32_t any = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t odd = odd_halves<DT>(v[i]);
+    any |= odd;
+    v[i] &= ~odd;
+  }
+  return any != 0;
+}
+// The sum of what is not finite in four elements (at `v` in the cache's first page) of the values that a row sees in some blocks of keys.  Rare, so
+// it reads them again from memory, key by key.
+template <int DT, class K>
+__device__ __forceinline__ f32x4 odd_sum(const Pages &pages, const char *v, int32_t b0, int32_t b1, int32_t step, const K &key_of, int32_t keys, int32_t pos,
+                                         int32_t window, int32_t sinks) {
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+  for (int32_t b = b0; b < b1; b += step)
+#pragma unroll 1
+    for (int32_t j = key_of(b), end = j + keys; j < end; ++j) {
+      const int32_t page = pages.page_of(j);
+      if (!pages.there(page) || !sees(pos, j, window, sinks)) continue;
+      const u32x2 w = *(const u32x2 SK_GLOBAL *)(uintptr_t)(v + pages.bytes(page, j));
+      const uint32_t lo = w.x & odd_halves<DT>(w.x), hi = w.y & odd_halves<DT>(w.y);
+      sum += f32x4{elem<DT>(lo & 0xffffu), elem<DT>(lo >> 16), elem<DT>(hi & 0xffffu), elem<DT>(hi >> 16)};
+    }
+  return sum;
 }
 
 // ---------------------------------------------------------------------------
@@ -345,38 +452,38 @@ struct ValueRows {
   }
 };
 
+template <int DT>
+__device__ __forceinline__ u32x4 load_query(const void *p, bool ok, bool negate) {
+  u32x4 v = load16(ok ? p : (const void *)g_zeros);
+  if (negate) v ^= 0x80008000u;
+  return v;
+}
+
 template <int DT, int DP>
-__device__ __forceinline__ void attend_few(const AttnArgs &a, const AttnDev &P, const Unit &u, unsigned char *lds, uint32_t *flag) {
-  constexpr int KS = DP / 32, NB = DP / 16, PR = DP / 8, VI = PR / 2;  // VI pieces of values per lane and block of keys
+__device__ __forceinline__ void attend_few(const AttnArgs &a, const SK_CONSTANT AttnDev &P, const Unit &u, unsigned char *lds, uint32_t *flag) {
+  constexpr int64_t SLOT = part_floats(ROWS_FEW, DP <= 128 ? 128 : 256);
+  constexpr int KS = DP / 32, NB = DP / 16, PR = DP / 8, VH = PR / 4;  // VH pieces of values per lane and 16 keys
   using VR = ValueRows<DP>;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
-  const Step st = step_of(P.lengths + u.seq, P.first_row + u.seq, P.rows, P.max_new, (int64_t)P.columns << P.page_shift);
-  const int32_t all_rows = st.fresh * P.group, row0 = u.block * ROWS_FEW, rows = min(ROWS_FEW, all_rows - row0);
+  const Step &st = u.step;
+  const int32_t row0 = u.block * ROWS_FEW, rows = min(ROWS_FEW, st.fresh * P.group - row0);
   const int32_t p0 = st.behind + row0 / P.group, p1 = st.behind + (row0 + rows - 1) / P.group;
   const Span span = span_of<KEYS_FEW>(p0, p1, P.window, P.sinks);
   const int32_t b0 = (int32_t)((int64_t)span.blocks * u.split / u.splits), b1 = (int32_t)((int64_t)span.blocks * (u.split + 1) / u.splits);
 
-  const int32_t my_row = row0 + min(c, rows - 1);
-  const int32_t my_token = my_row / P.group, my_head = u.head * P.group + my_row % P.group;
-  const int32_t my_pos = c < rows ? st.behind + my_token : -1;
-  const char *q = (const char *)P.q + 2 * ((int64_t)(st.first + my_token) * P.q_row + (int64_t)my_head * P.q_head);
-  u32x4 qf[KS];
-#pragma unroll
-  for (int s = 0; s < KS; ++s) {
-    const int e = 32 * s + 8 * g;
-    qf[s] = load16(c < rows && e < P.dim ? (const void *)(q + 2 * e) : (const void *)g_zeros);
-  }
   const Pages pages{P.table + (int64_t)u.seq * P.columns, P.page_shift, P.num_pages, P.columns, P.page_stride, P.token_stride};
   const char *kh = (const char *)P.k + 2 * (int64_t)u.head * P.head_stride, *vh = (const char *)P.v + 2 * (int64_t)u.head * P.head_stride;
   auto key_of = [&](int32_t b) { return b < span.sink_blocks ? b * KEYS_FEW : span.low + (b - span.sink_blocks) * KEYS_FEW; };
-
-  unsigned char *mine = lds + wave * (KEYS_FEW * VR::BYTES);
-  f32x4 o[NB];
+  // offsets of this lane's pieces of 16 keys; pieces beyond the head's end are read from its start and count as zeros
+  uint32_t ko[KS], vo[VH];
 #pragma unroll
-  for (int i = 0; i < NB; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m = -__builtin_inff(), l = 0.f;
-
-  u32x4 kf[2][KS], vf[VI];
+  for (int s = 0; s < KS; ++s) ko[s] = 2u * (uint32_t)(c * P.token_stride + (32 * s + 8 * g < P.dim ? 32 * s + 8 * g : 0));
+#pragma unroll
+  for (int i = 0; i < VH; ++i) {
+    const int n = i * 64 + lane, e = n % PR * 8;
+    vo[i] = 2u * (uint32_t)(n / PR * P.token_stride + (e < P.dim ? e : 0));
+  }
+  u32x4 kf[2][KS], vf[2][VH];
   int32_t page[2];  // of the block that is loaded next
   auto look = [&](int32_t b) {
     const int32_t key0 = key_of(min(b, b1 - 1));
@@ -385,28 +492,19 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, const AttnDev &P, 
   };
   auto load = [&](int32_t b) -> uint32_t {  // which halves are there
     const int32_t key0 = key_of(b);
-    uint32_t present = 0;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-      const int32_t key = key0 + 16 * half;
-      const bool there = pages.there(page[half]);
-      const int64_t off = pages.offset(page[half], key);
-      present |= there ? 1u << half : 0u;
+      const char *kb = kh + pages.bytes(page[half], key0 + 16 * half);
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const int e = 32 * s + 8 * g;
-        kf[half][s] = load16(there && e < P.dim ? (const void *)(kh + 2 * (off + c * P.token_stride + e)) : (const void *)g_zeros);
-      }
-#pragma unroll
-      for (int i = 0; i < VI / 2; ++i) {
-        const int n = (i + half * (VI / 2)) * 64 + lane, row = n / PR, e = n % PR * 8;
-        const int32_t j = key0 + row;
-        // values that no row sees are not read: what lies there may be anything
-        const bool ok = there && e < P.dim && j <= p1 && (P.window == 0 || p0 - j < P.window || j < P.sinks);
-        vf[i + half * (VI / 2)] = load16(ok ? (const void *)(vh + 2 * (off + (row & 15) * P.token_stride + e)) : (const void *)g_zeros);
-      }
+      for (int s = 0; s < KS; ++s) kf[half][s] = load16(kb + ko[s]);
     }
-    return present;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const char *vb = vh + pages.bytes(page[half], key0 + 16 * half);
+#pragma unroll
+      for (int i = 0; i < VH; ++i) vf[half][i] = load16(vb + vo[i]);
+    }
+    return (pages.there(page[0]) ? 1u : 0u) | (pages.there(page[1]) ? 2u : 0u);
   };
   uint32_t present = 0;
   if (b0 + wave < b1) {
@@ -414,59 +512,105 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, const AttnDev &P, 
     present = load(b0 + wave);
     look(b0 + wave + 4);
   }
+
+  const int32_t my_row = row0 + min(c, rows - 1);
+  const int32_t my_token = my_row / P.group, my_head = u.head * P.group + my_row % P.group;
+  const int32_t my_pos = c < rows ? st.behind + my_token : -1;
+  const char *q = (const char *)P.q + 2 * ((int64_t)(st.first + my_token) * P.q_row + (int64_t)my_head * P.q_head);
+  const float scale = fabsf(P.scale_log2);  // (its sign goes into the queries)
+  u32x4 qf[KS];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) qf[s] = load_query<DT>(q + 2 * (32 * s + 8 * g), c < rows && 32 * s + 8 * g < P.dim, P.scale_log2 < 0.f);
+
+  unsigned char *mine = lds + wave * (KEYS_FEW * VR::BYTES);
+  f32x4 o[NB];
+#pragma unroll
+  for (int i = 0; i < NB; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -__builtin_inff(), l = 0.f;
+  bool cleaned = false;
+
   for (int32_t b = b0 + wave; b < b1; b += 4) {
     const int32_t key0 = key_of(b);
     const uint32_t now = present;
+    if (P.dim != DP) {
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+        if (32 * k + 8 * g >= P.dim) kf[0][k] = kf[1][k] = u32x4{0u, 0u, 0u, 0u};
+    }
     f32x4 s[2];
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       s[half] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int k = 0; k < KS; ++k) mma16<DT>(kf[half][k], qf[k], s[half]);
+      for (int k = 0; k < KS; ++k) {
+        mma16<DT>(kf[half][k], qf[k], s[half]);
+      }
+    }
+    // whether all keys are seen by all rows
+    const bool whole = now == 3 && key0 + KEYS_FEW - 1 <= p0 && (P.window == 0 || p1 - key0 < P.window);
+    if (!whole || P.dim != DP) {
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int i = 0; i < VH; ++i) {
+          const int n = i * 64 + lane;
+          const int32_t j = key0 + 16 * half + n / PR;
+          // values that no row sees: what lies there may be anything
+          const bool ok = (now >> half & 1) && n % PR * 8 < P.dim && j <= p1 && (P.window == 0 || p0 - j < P.window || j < P.sinks);
+          if (!ok) vf[half][i] = u32x4{0u, 0u, 0u, 0u};
+          if (!whole && p0 != p1) cleaned |= clean<DT>(vf[half][i]);
+        }
     }
 #pragma unroll
-    for (int i = 0; i < VI; ++i) {
-      const int n = i * 64 + lane, row = n / PR, e = n % PR * 8;
-      *(u32x4 *)(mine + VR::at(row, 2 * e)) = vf[i];
-    }
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int i = 0; i < VH; ++i) {
+        const int n = i * 64 + lane;
+        *(u32x4 *)(mine + VR::at(16 * half + n / PR, n % PR * 16)) = vf[half][i];
+      }
     if (b + 4 < b1) {
       present = load(b + 4);
       look(b + 8);
     }
     // lane (g, c) has the scores of row c and keys key0 + 16 half + 4 g + i
-    float top = -__builtin_inff();
+    if (!whole) {
 #pragma unroll
-    for (int half = 0; half < 2; ++half)
+      for (int half = 0; half < 2; ++half)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int32_t j = key0 + 16 * half + 4 * g + i;
-        s[half][i] = (now >> half & 1) && sees(my_pos, j, P.window, P.sinks) ? s[half][i] * P.scale_log2 : -__builtin_inff();
-        top = fmaxf(top, s[half][i]);
-      }
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
+        for (int i = 0; i < 4; ++i)
+          if (!((now >> half & 1) && sees(my_pos, key0 + 16 * half + 4 * g + i, P.window, P.sinks))) s[half][i] = -__builtin_inff();
+    }
+    float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+    top = max32(max16(top)) * scale;
     const float next = fmaxf(m, top), base = base_of(next), keep = exp2_fast(m - base);
-    m = next;
     float sum = 0.f;
 #pragma unroll
     for (int half = 0; half < 2; ++half)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        s[half][i] = exp2_fast(s[half][i] - base);
+        s[half][i] = exp2_fast(fmaf(s[half][i], scale, -base));
         sum += s[half][i];
       }
     l = l * keep + sum;
+    if (__ballot(next > m)) {
+#pragma unroll
+      for (int i = 0; i < NB; ++i) o[i] *= keep;
+    }
+    m = next;
     const u32x4 pf = {pack2<DT>(s[0][0], s[0][1]), pack2<DT>(s[0][2], s[0][3]), pack2<DT>(s[1][0], s[1][1]), pack2<DT>(s[1][2], s[1][3])};
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
       const int byte = 2 * (16 * i + 4 * (c & 3)), row = 4 * g + (c >> 2);
       const u32x2 lo = read_transposed(mine + VR::at(row, byte)), hi = read_transposed(mine + VR::at(row + 16, byte));
-      o[i] *= keep;
       mma16<DT>(u32x4{lo.x, lo.y, hi.x, hi.y}, pf, o[i]);
     }
   }
-  l += __shfl_xor(l, 16);
-  l += __shfl_xor(l, 32);
+  if (__builtin_expect(__ballot(cleaned) != 0, 0)) {
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+      if (16 * i + 4 * g < P.dim) o[i] += odd_sum<DT>(pages, vh + 2 * (16 * i + 4 * g), b0 + wave, b1, 4, key_of, KEYS_FEW, my_pos, P.window, P.sinks);
+  }
+  l = sum32(sum16(l));
 
   // the waves' results together: [wave][row] maximum and sum, [wave][row][element] outputs relative to the common maximum
   float *stats = (float *)(lds + 4 * KEYS_FEW * VR::BYTES);
@@ -484,7 +628,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, const AttnDev &P, 
 #pragma unroll
   for (int i = 0; i < NB; ++i) *(f32x4 *)(out + c * DP + 16 * i + 4 * g) = o[i] * part;
   __syncthreads();
-  float *ws = a.ws_few + (int64_t)u.slot * part_floats(ROWS_FEW, DP);
+  float *ws = a.ws_few + (int64_t)u.slot * SLOT;
   for (int n = tid; n < rows * (DP / 4); n += CACHE_THREADS) {
     const int r = n / (DP / 4), e = n % (DP / 4) * 4;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
@@ -497,7 +641,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, const AttnDev &P, 
 #pragma unroll
     for (int w = 0; w < 4; ++w) sum += stats[w * 32 + 16 + r] * exp2_fast(stats[w * 32 + r] - base_of(big));
     if (u.splits == 1) {
-      const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);
+      const float inv = inverse(sum);
       const int32_t row = row0 + r;
       char *dst = (char *)P.out + 2 * ((int64_t)(st.first + row / P.group) * P.out_row + (int64_t)(u.head * P.group + row % P.group) * P.out_head + e);
       if (e < P.dim) store8(dst, u32x2{pack2<DT>(v.x * inv, v.y * inv), pack2<DT>(v.z * inv, v.w * inv)});
@@ -510,12 +654,13 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, const AttnDev &P, 
   if (u.splits == 1) return;
   if (!last_to_arrive(a.arrivals + a.grid_many + u.first_slot, u.splits, flag)) return;
   // the slices in order: the result does not depend on who came last
-  const float *ws0 = a.ws_few + (int64_t)u.first_slot * part_floats(ROWS_FEW, DP);
-  const int64_t step = (int64_t)P.kv_heads * part_floats(ROWS_FEW, DP);
+  const float *ws0 = a.ws_few + (int64_t)u.first_slot * SLOT;
+  const int64_t step = (int64_t)P.kv_heads * SLOT;
   for (int n = tid; n < rows * (DP / 4); n += CACHE_THREADS) {
     const int r = n / (DP / 4), e = n % (DP / 4) * 4;
     float big = -__builtin_inff(), sum = 0.f;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
     for (int s = 0; s < u.splits; ++s) {
       const float *w = ws0 + s * step;
       const f32x2 ms = load_shared(w + ROWS_FEW * DP + 2 * r), x = load_shared(w + r * DP + e), y = load_shared(w + r * DP + e + 2);
@@ -524,7 +669,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, const AttnDev &P, 
       v = v * keep + f32x4{x.x, x.y, y.x, y.y} * mul;
       big = next;
     }
-    const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);
+    const float inv = inverse(sum);
     const int32_t row = row0 + r;
     char *dst = (char *)P.out + 2 * ((int64_t)(st.first + row / P.group) * P.out_row + (int64_t)(u.head * P.group + row % P.group) * P.out_head + e);
     if (e < P.dim) store8(dst, u32x2{pack2<DT>(v.x * inv, v.y * inv), pack2<DT>(v.z * inv, v.w * inv)});
@@ -544,18 +689,89 @@ struct KeyRows {
     return row * BYTES + (byte ^ (turn << 4));
   }
 };
+// Two tiles of keys and values in LDS in turn.
+template <int DP>
+struct ManyLds {
+  static constexpr int TILE = keys_many(DP) * (KeyRows<DP>::BYTES + ValueRows<DP>::BYTES), TILES = 2, BYTES = TILES * TILE + 16;
+};
 
 template <int DT, int DP>
-__device__ __forceinline__ void attend_many(const AttnArgs &a, const AttnDev &P, const Unit &u, unsigned char *lds, uint32_t *flag) {
-  constexpr int KS = DP / 16, NB = DP / 32, PR = DP / 8, LI = KEYS_MANY * PR / CACHE_THREADS;  // LI pieces per thread and tile, keys and values each
+__device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT AttnDev &P, const Unit &u, unsigned char *lds, uint32_t *flag) {
+  constexpr int64_t SLOT = part_floats(ROWS_MANY, DP <= 128 ? 128 : 256);
+  constexpr int KEYS = keys_many(DP), HALVES = KEYS / 32;
+  constexpr int KS = DP / 16, NB = DP / 32, PR = DP / 8, LI = KEYS * PR / CACHE_THREADS;  // LI pieces per thread and tile, keys and values each
   using KR = KeyRows<DP>;
   using VR = ValueRows<DP>;
+  constexpr int TILE = ManyLds<DP>::TILE;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, c = lane & 31;
-  const Step st = step_of(P.lengths + u.seq, P.first_row + u.seq, P.rows, P.max_new, (int64_t)P.columns << P.page_shift);
-  const int32_t all_rows = st.fresh * P.group, row0 = u.block * ROWS_MANY, rows = min(ROWS_MANY, all_rows - row0);
+  const Step &st = u.step;
+  const int32_t row0 = u.block * ROWS_MANY, rows = min(ROWS_MANY, st.fresh * P.group - row0);
   const int32_t p0 = st.behind + row0 / P.group, p1 = st.behind + (row0 + rows - 1) / P.group;
-  const Span span = span_of<KEYS_MANY>(p0, p1, P.window, P.sinks);
+  const Span span = span_of<KEYS>(p0, p1, P.window, P.sinks);
   const int32_t b0 = (int32_t)((int64_t)span.blocks * u.split / u.splits), b1 = (int32_t)((int64_t)span.blocks * (u.split + 1) / u.splits);
+
+  const Pages pages{P.table + (int64_t)u.seq * P.columns, P.page_shift, P.num_pages, P.columns, P.page_stride, P.token_stride};
+  const char *kh = (const char *)P.k + 2 * (int64_t)u.head * P.head_stride, *vh = (const char *)P.v + 2 * (int64_t)u.head * P.head_stride;
+  auto key_of = [&](int32_t b) { return b < span.sink_blocks ? b * KEYS : span.low + (b - span.sink_blocks) * KEYS; };
+  // offsets of this thread's pieces in their 16 keys; pieces beyond the head's end are read from its start and count as zeros
+  uint32_t lo[LI];
+#pragma unroll
+  for (int i = 0; i < LI; ++i) {
+    const int n = i * CACHE_THREADS + tid, e = n % PR * 8;
+    lo[i] = 2u * (uint32_t)((n / PR & 15) * P.token_stride + (e < P.dim ? e : 0));
+  }
+  u32x4 kr[LI], vr[LI];
+  int32_t page[KEYS / 16];  // of the tile that is loaded next
+  auto look = [&](int32_t b) {
+    const int32_t key0 = key_of(min(b, b1 - 1));
+#pragma unroll
+    for (int i = 0; i < KEYS / 16; ++i) page[i] = pages.page_of(key0 + 16 * i);
+  };
+  auto load = [&](int32_t b) -> uint32_t {  // which of its blocks of 16 keys are there
+    const int32_t key0 = key_of(b);
+    uint32_t present = 0;
+#pragma unroll
+    for (int i = 0; i < KEYS / 16; ++i) present |= pages.there(page[i]) ? 1u << i : 0u;
+#pragma unroll
+    for (int i = 0; i < LI; ++i) {
+      const int block = (i * 4 + wave) * 4 / PR;  // the wave's pieces lie in one block of 16 keys
+      const int32_t id = block == 0 ? page[0] : block == 1 || KEYS == 32 ? page[1] : block == 2 ? page[2 % (KEYS / 16)] : page[3 % (KEYS / 16)];
+      const int64_t at = pages.bytes(id, key0 + 16 * block);
+      kr[i] = load16(kh + at + lo[i]);
+      vr[i] = load16(vh + at + lo[i]);
+    }
+    return present;
+  };
+  bool cleaned = false;  // values that are not finite were taken out
+  // the loaded pieces of tile b to LDS
+  auto put = [&](int32_t b, uint32_t present, unsigned char *to) {
+    const int32_t key0 = key_of(b);
+    const bool whole = present == (1u << KEYS / 16) - 1 && key0 + KEYS - 1 <= p0 && (P.window == 0 || p1 - key0 < P.window);
+    if (!whole || P.dim != DP) {
+#pragma unroll
+      for (int i = 0; i < LI; ++i) {
+        const int n = i * CACHE_THREADS + tid;
+        const int32_t j = key0 + n / PR;
+        if (n % PR * 8 >= P.dim) kr[i] = u32x4{0u, 0u, 0u, 0u};
+        // values that no row sees: what lies there may be anything
+        const bool ok = (present >> (n / PR / 16) & 1) && n % PR * 8 < P.dim && j <= p1 && (P.window == 0 || p0 - j < P.window || j < P.sinks);
+        if (!ok) vr[i] = u32x4{0u, 0u, 0u, 0u};
+        if (!whole) cleaned |= clean<DT>(vr[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < LI; ++i) {
+      const int n = i * CACHE_THREADS + tid;
+      *(u32x4 *)(to + KR::at(n / PR, n % PR * 16)) = kr[i];
+      *(u32x4 *)(to + KEYS * KR::BYTES + VR::at(n / PR, n % PR * 16)) = vr[i];
+    }
+  };
+  uint32_t present = 0;
+  if (b0 < b1) {
+    look(b0);
+    present = load(b0);
+    look(b0 + 1);
+  }
 
   const int32_t in_block = wave * 32 + c;
   const bool row_ok = in_block < rows;
@@ -566,17 +782,12 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const AttnDev &P,
   const bool wave_ok = wave * 32 < rows;
   const int32_t w0 = st.behind + (row0 + min(wave * 32, rows - 1)) / P.group, w1 = st.behind + (row0 + min(wave * 32 + 31, rows - 1)) / P.group;
   const char *q = (const char *)P.q + 2 * ((int64_t)(st.first + my_token) * P.q_row + (int64_t)my_head * P.q_head);
+  const float scale = fabsf(P.scale_log2);  // (its sign goes into the queries)
   u32x4 qf[KS];
 #pragma unroll
-  for (int s = 0; s < KS; ++s) {
-    const int e = 16 * s + 8 * h;
-    qf[s] = load16(row_ok && e < P.dim ? (const void *)(q + 2 * e) : (const void *)g_zeros);
-  }
-  const Pages pages{P.table + (int64_t)u.seq * P.columns, P.page_shift, P.num_pages, P.columns, P.page_stride, P.token_stride};
-  const char *kh = (const char *)P.k + 2 * (int64_t)u.head * P.head_stride, *vh = (const char *)P.v + 2 * (int64_t)u.head * P.head_stride;
-  auto key_of = [&](int32_t b) { return b < span.sink_blocks ? b * KEYS_MANY : span.low + (b - span.sink_blocks) * KEYS_MANY; };
+  for (int s = 0; s < KS; ++s) qf[s] = load_query<DT>(q + 2 * (16 * s + 8 * h), row_ok && 16 * s + 8 * h < P.dim, P.scale_log2 < 0.f);
 
-  unsigned char *ks = lds, *vs = lds + KEYS_MANY * KR::BYTES;
+  uint32_t *odd = (uint32_t *)(lds + ManyLds<DP>::TILES * TILE);  // whether any thread took values out
   f32x16 o[NB];
 #pragma unroll
   for (int i = 0; i < NB; ++i)
@@ -584,116 +795,111 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const AttnDev &P,
     for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
   float m = -__builtin_inff(), l = 0.f;
 
-  u32x4 kr[LI], vr[LI];
-  int32_t page[4];  // of the tile that is loaded next
-  auto look = [&](int32_t b) {
-    const int32_t key0 = key_of(min(b, b1 - 1));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) page[i] = pages.page_of(key0 + 16 * i);
-  };
-  auto load = [&](int32_t b) -> uint32_t {  // which of its blocks of 16 keys are there
-    const int32_t key0 = key_of(b);
-    uint32_t present = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) present |= pages.there(page[i]) ? 1u << i : 0u;
-#pragma unroll
-    for (int i = 0; i < LI; ++i) {
-      const int n = i * CACHE_THREADS + tid, row = n / PR, e = n % PR * 8;
-      const int block = (i * 4 + wave) * 4 / PR;  // the wave's pieces lie in one block of 16 keys
-      const int32_t id = block == 0 ? page[0] : block == 1 ? page[1] : block == 2 ? page[2] : page[3];
-      const int32_t j = key0 + row;
-      const int64_t at = 2 * (pages.offset(id, key0 + 16 * block) + (row & 15) * P.token_stride + e);
-      const bool there = pages.there(id) && e < P.dim;
-      kr[i] = load16(there ? (const void *)(kh + at) : (const void *)g_zeros);
-      // values that no row sees are not read: what lies there may be anything
-      const bool seen = j <= p1 && (P.window == 0 || p0 - j < P.window || j < P.sinks);
-      vr[i] = load16(there && seen ? (const void *)(vh + at) : (const void *)g_zeros);
-    }
-    return present;
-  };
-  uint32_t present = 0;
+  if (tid == 0) *odd = 0;
+  uint32_t now = present;
   if (b0 < b1) {
-    look(b0);
-    present = load(b0);
-    look(b0 + 1);
+    put(b0, present, lds);
+    if (b0 + 1 < b1) {
+      present = load(b0 + 1);
+      look(b0 + 2);
+    }
   }
+  __syncthreads();
   for (int32_t b = b0; b < b1; ++b) {
     const int32_t key0 = key_of(b);
-    const uint32_t now = present;
-    __syncthreads();
+    unsigned char *ks = lds + ((b - b0) & 1) * TILE, *vs = ks + KEYS * KR::BYTES;
+    // whether any row of the wave sees any of these keys, and whether all see all
+    const bool use = wave_ok && key0 <= w1 && (P.window == 0 || w0 - (key0 + KEYS - 1) < P.window || key0 < P.sinks);
+    if (use) {
+      const bool whole = now == (1u << KEYS / 16) - 1 && key0 + KEYS - 1 <= w0 && (P.window == 0 || w1 - key0 < P.window);
+      f32x16 s[HALVES];
 #pragma unroll
-    for (int i = 0; i < LI; ++i) {
-      const int n = i * CACHE_THREADS + tid, row = n / PR, e = n % PR * 8;
-      *(u32x4 *)(ks + KR::at(row, 2 * e)) = kr[i];
-      *(u32x4 *)(vs + VR::at(row, 2 * e)) = vr[i];
-    }
-    __syncthreads();
-    if (b + 1 < b1) {
-      present = load(b + 1);
-      look(b + 2);
-    }
-    // whether any row of the wave sees any of these keys
-    const bool use = wave_ok && key0 <= w1 && (P.window == 0 || (int64_t)w0 - (key0 + KEYS_MANY - 1) < P.window || key0 < P.sinks);
-    if (!use) continue;
-    const bool whole = now == 15 && key0 + KEYS_MANY - 1 <= w0 && (P.window == 0 || (int64_t)w1 - key0 < P.window);
-    f32x16 s[2];
+      for (int half = 0; half < HALVES; ++half) {
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
+        for (int j = 0; j < 16; ++j) s[half][j] = 0.f;
 #pragma unroll
-      for (int j = 0; j < 16; ++j) s[half][j] = 0.f;
-#pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        const u32x4 kf = *(const u32x4 *)(ks + KR::at(32 * half + c, 2 * (16 * k + 8 * h)));
-        mma32<DT>(kf, qf[k], s[half]);
-      }
-    }
-    // lane (h, c) has the scores of row c and keys key0 + 32 half + 8 (i / 4) + 4 h + i % 4
-    float top = -__builtin_inff();
-#pragma unroll
-    for (int half = 0; half < 2; ++half)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[half][i] *= P.scale_log2;
-        if (!whole) {
-          const int32_t j = key0 + 32 * half + 8 * (i / 4) + 4 * h + i % 4;
-          s[half][i] = (now >> (2 * half + i / 8) & 1) && sees(my_pos, j, P.window, P.sinks) ? s[half][i] : -__builtin_inff();
+        for (int k = 0; k < KS; ++k) {
+          const u32x4 kf = *(const u32x4 *)(ks + KR::at(32 * half + c, 2 * (16 * k + 8 * h)));
+          mma32<DT>(kf, qf[k], s[half]);
         }
-        top = fmaxf(top, s[half][i]);
       }
-    top = fmaxf(top, __shfl_xor(top, 32));
-    const float next = fmaxf(m, top), base = base_of(next), keep = exp2_fast(m - base);
-    m = next;
-    float sum = 0.f;
-    u32x4 pf[4];
+      // lane (h, c) has the scores of row c and keys key0 + 32 half + 8 (i / 4) + 4 h + i % 4
+      if (!whole) {
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
+        for (int half = 0; half < HALVES; ++half)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[half][i] = exp2_fast(s[half][i] - base);
-        sum += s[half][i];
+          for (int i = 0; i < 16; ++i) {
+            const int32_t j = key0 + 32 * half + 8 * (i / 4) + 4 * h + i % 4;
+            if (!((now >> (2 * half + i / 8) & 1) && sees(my_pos, j, P.window, P.sinks))) s[half][i] = -__builtin_inff();
+          }
       }
+      float top = -__builtin_inff();
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
-        pf[2 * half + t] = u32x4{pack2<DT>(s[half][8 * t], s[half][8 * t + 1]), pack2<DT>(s[half][8 * t + 2], s[half][8 * t + 3]),
-                                 pack2<DT>(s[half][8 * t + 4], s[half][8 * t + 5]), pack2<DT>(s[half][8 * t + 6], s[half][8 * t + 7])};
+      for (int half = 0; half < HALVES; ++half)
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) top = fmaxf(fmaxf(top, s[half][i]), s[half][i + 1]);
+      top = max32(top) * scale;
+      const float next = fmaxf(m, top), base = base_of(next), keep = exp2_fast(m - base);
+      float sum = 0.f;
+      u32x4 pf[2 * HALVES];
+#pragma unroll
+      for (int half = 0; half < HALVES; ++half) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          s[half][i] = exp2_fast(fmaf(s[half][i], scale, -base));
+          sum += s[half][i];
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          pf[2 * half + t] = u32x4{pack2<DT>(s[half][8 * t], s[half][8 * t + 1]), pack2<DT>(s[half][8 * t + 2], s[half][8 * t + 3]),
+                                   pack2<DT>(s[half][8 * t + 4], s[half][8 * t + 5]), pack2<DT>(s[half][8 * t + 6], s[half][8 * t + 7])};
+      }
+      l = l * keep + sum;
+      if (__ballot(next > m)) {  // (no row's maximum has grown: nothing to scale)
+#pragma unroll
+        for (int i = 0; i < NB; ++i) o[i] *= keep;
+      }
+      m = next;
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+#pragma unroll
+        for (int t = 0; t < 2 * HALVES; ++t) {
+          const int row = 16 * t + 4 * h + ((lane & 15) >> 2), byte = 2 * (32 * i + 16 * ((lane >> 4) & 1) + 4 * (lane & 3));
+          const u32x2 x = read_transposed(vs + VR::at(row, byte)), y = read_transposed(vs + VR::at(row + 8, byte));
+          mma32<DT>(u32x4{x.x, x.y, y.x, y.y}, pf[t], o[i]);
+        }
+      }
     }
-    l = l * keep + sum;
-#pragma unroll
-    for (int i = 0; i < NB; ++i) {
-      o[i] *= keep;
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const int row = 16 * t + 4 * h + ((lane & 15) >> 2), byte = 2 * (32 * i + 16 * ((lane >> 4) & 1) + 4 * (lane & 3));
-        const u32x2 lo = read_transposed(vs + VR::at(row, byte)), hi = read_transposed(vs + VR::at(row + 8, byte));
-        mma32<DT>(u32x4{lo.x, lo.y, hi.x, hi.y}, pf[t], o[i]);
+    if (b + 1 < b1) {
+      // the next tile into the other place, which all waves have left behind the last barrier
+      const int place = (b + 1 - b0) & 1;
+      now = present;
+      put(b + 1, present, lds + place * TILE);
+      if (b + 2 < b1) {
+        present = load(b + 2);
+        look(b + 3);
       }
     }
+    __syncthreads();
   }
-  l += __shfl_xor(l, 32);
+  if (cleaned) *odd = 1;
+  __syncthreads();
+  if (__builtin_expect(*odd != 0, 0)) {
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (32 * i + 8 * k + 4 * h < P.dim) {
+          const f32x4 x = odd_sum<DT>(pages, vh + 2 * (32 * i + 8 * k + 4 * h), b0, b1, 1, key_of, KEYS, my_pos, P.window, P.sinks);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[i][4 * k + e] += x[e];
+        }
+  }
+  l = sum32(l);
 
   if (u.splits > 1) {
     // partial results as they stand in the registers: [wave][register pair][lane], then maximum and sum of each row
-    float *ws = a.ws_many + (int64_t)u.slot * part_floats(ROWS_MANY, DP);
+    float *ws = a.ws_many + (int64_t)u.slot * SLOT;
     if (wave_ok) {
 #pragma unroll
       for (int i = 0; i < NB; ++i)
@@ -703,8 +909,8 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const AttnDev &P,
     }
     if (!last_to_arrive(a.arrivals + u.first_slot, u.splits, flag)) return;
     if (!wave_ok) return;
-    const float *ws0 = a.ws_many + (int64_t)u.first_slot * part_floats(ROWS_MANY, DP);
-    const int64_t step = (int64_t)P.kv_heads * part_floats(ROWS_MANY, DP);
+    const float *ws0 = a.ws_many + (int64_t)u.first_slot * SLOT;
+    const int64_t step = (int64_t)P.kv_heads * SLOT;
     m = -__builtin_inff();
     l = 0.f;
 #pragma unroll
@@ -728,7 +934,7 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const AttnDev &P,
     }
   }
   if (!row_ok) return;
-  const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+  const float inv = inverse(l);
   char *dst = (char *)P.out + 2 * ((int64_t)(st.first + my_token) * P.out_row + (int64_t)my_head * P.out_head);
 #pragma unroll
   for (int i = 0; i < NB; ++i)
@@ -740,30 +946,48 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const AttnDev &P,
     }
 }
 
-template <int DT, int DP>
-__global__ void __launch_bounds__(CACHE_THREADS, DP <= 128 ? 2 : 1) sk_attend(AttnArgs a) {
-  constexpr int FEW = 4 * KEYS_FEW * ValueRows<DP>::BYTES + 4 * 2 * ROWS_FEW * 4, MANY = KEYS_MANY * (KeyRows<DP>::BYTES + ValueRows<DP>::BYTES);
-  __shared__ __attribute__((aligned(16))) unsigned char lds[FEW > MANY ? FEW : MANY];
+// The kernels: heads of up to 128 elements of either type in one, so that the tenants of a plan share a launch; heads of up to 256, whose
+// sums take twice the registers, in another.  A plan that can only have units of few rows has kernels of its own, of which more workgroups
+// fit a compute unit.
+template <bool MANY, bool WIDE>
+struct AttendLds {
+  static constexpr int DP = WIDE ? 256 : 128, FEW = 4 * KEYS_FEW * ValueRows<DP>::BYTES + 4 * 2 * ROWS_FEW * 4;
+  static constexpr int BYTES = MANY && ManyLds<DP>::BYTES > FEW ? ManyLds<DP>::BYTES : FEW;
+};
+
+template <int DT, int DP, bool MANY>
+__device__ __forceinline__ void attend(const AttnArgs &a, const SK_CONSTANT AttnDev &P, const Unit &u, unsigned char *lds, uint32_t *flag) {
+  if (MANY && blockIdx.x < a.grid_many)
+    attend_many<DT, DP>(a, P, u, lds, flag);
+  else
+    attend_few<DT, DP>(a, P, u, lds, flag);
+}
+
+template <bool MANY, bool WIDE>
+__global__ void __launch_bounds__(CACHE_THREADS, resident(WIDE, MANY)) sk_attend(AttnArgs a) {
+  __shared__ __attribute__((aligned(256))) unsigned char lds[AttendLds<MANY, WIDE>::BYTES];
   __shared__ FindScratch found;
   __shared__ uint32_t flag;
-  find_unit(a, &found);
-  if (!found.unit.any) return;
-  const Unit u = found.unit;
-  const AttnDev &P = a.problems[__builtin_amdgcn_readfirstlane(u.problem)];
-  Unit v;  // the same in scalar registers
-  v.problem = 0;
-  v.seq = __builtin_amdgcn_readfirstlane(u.seq);
-  v.head = __builtin_amdgcn_readfirstlane(u.head);
-  v.block = __builtin_amdgcn_readfirstlane(u.block);
-  v.split = __builtin_amdgcn_readfirstlane(u.split);
-  v.splits = __builtin_amdgcn_readfirstlane(u.splits);
-  v.slot = __builtin_amdgcn_readfirstlane(u.slot);
-  v.first_slot = __builtin_amdgcn_readfirstlane(u.first_slot);
-  v.many = v.any = true;
-  if (__builtin_amdgcn_readfirstlane((int)u.many))
-    attend_many<DT, DP>(a, P, v, lds, &flag);
-  else
-    attend_few<DT, DP>(a, P, v, lds, &flag);
+  const Unit u = find_unit<MANY, WIDE>(a, &found);
+  if (!u.any) return;
+  // (read through the scalar cache where it is needed)
+  const SK_CONSTANT AttnDev &P = *(const SK_CONSTANT AttnDev *)(uintptr_t)(a.problems + u.problem);
+  if constexpr (WIDE) {
+    if (P.dtype == SK_BF16)
+      attend<SK_BF16, 256, MANY>(a, P, u, lds, &flag);
+    else
+      attend<SK_F16, 256, MANY>(a, P, u, lds, &flag);
+  } else {
+    const int kind = (P.dtype == SK_BF16 ? 0 : 3) + (P.dim <= 64 ? 0 : P.dim <= 96 ? 1 : 2);
+    switch (kind) {
+      case 0: return attend<SK_BF16, 64, MANY>(a, P, u, lds, &flag);
+      case 1: return attend<SK_BF16, 96, MANY>(a, P, u, lds, &flag);
+      case 2: return attend<SK_BF16, 128, MANY>(a, P, u, lds, &flag);
+      case 3: return attend<SK_F16, 64, MANY>(a, P, u, lds, &flag);
+      case 4: return attend<SK_F16, 96, MANY>(a, P, u, lds, &flag);
+      default: return attend<SK_F16, 128, MANY>(a, P, u, lds, &flag);
+    }
+  }
 }
 
 }  // namespace sk

@@ -31,8 +31,6 @@ bool apart(int64_t outer_n, int64_t outer, int64_t inner_n, int64_t inner, int64
   return nested(outer, inner_n, inner) || nested(inner, outer_n, outer);
 }
 
-int dim_class(int dim) { return dim <= 64 ? 64 : dim <= 96 ? 96 : dim <= 128 ? 128 : 256; }
-
 sk_status check_problem(const sk_attn_problem &p, AttnDev &d, std::string &err) {
   if (p.dtype != SK_BF16 && p.dtype != SK_F16) return refuse(err, SK_ERR_UNSUPPORTED, "dtype must be SK_BF16 or SK_F16");
   if (p.q_heads < 1 || p.kv_heads < 1 || p.head_dim < 1 || p.page_tokens < 1 || p.num_pages < 1 || p.sequences < 1 || p.pages_per_sequence < 1 || p.rows < 1)
@@ -81,6 +79,7 @@ sk_status check_problem(const sk_attn_problem &p, AttnDev &d, std::string &err) 
                               d.head_stride >= all + (__int128)(p.page_tokens - 1) * d.token_stride + dim;
     if (!inside_heads) return refuse(err, SK_ERR_INVALID_ARG, "the cache's strides let pages overlap");
   }
+  if (d.token_stride >= (int64_t)1 << 26) return refuse(err, SK_ERR_UNSUPPORTED, "token_stride of 2^26 elements and more");
   for (int64_t s : {d.page_stride, d.head_stride, d.token_stride, d.qkv_row, d.q_row, d.q_head, d.out_row, d.out_head})
     if (s % 8) return refuse(err, SK_ERR_UNSUPPORTED, "strides must be multiples of 16 bytes");
   for (const void *q : {(const void *)p.k, (const void *)p.v, p.qkv, p.q_weight, p.k_weight, (const void *)p.cos, (const void *)p.sin, (const void *)p.q, (const void *)p.out})
@@ -104,7 +103,7 @@ sk_status check_problem(const sk_attn_problem &p, AttnDev &d, std::string &err) 
 
 }  // namespace
 
-sk_status plan_attn(const sk_attn_problem *problems, int32_t n, int32_t workgroups, AttnPlanHost &out, std::string &err) {
+sk_status plan_attn(const sk_attn_problem *problems, int32_t n, int32_t compute_units, int32_t workgroups, AttnPlanHost &out, std::string &err) {
   if (n < 0 || (n > 0 && !problems)) return refuse(err, SK_ERR_INVALID_ARG, "problems is null or n is negative");
   std::vector<std::pair<uintptr_t, uintptr_t>> written;
   int64_t append_grid = 0;
@@ -136,35 +135,38 @@ sk_status plan_attn(const sk_attn_problem *problems, int32_t n, int32_t workgrou
   for (size_t i = 1; i < written.size(); ++i)
     if (written[i].first < written[i - 1].second) return refuse(err, SK_ERR_OVERLAP, "ranges of q and out overlap");
 
-  for (int dtype : {(int)SK_BF16, (int)SK_F16})
-    for (int cls : {64, 96, 128, 256}) {
-      AttnGroup g{};
-      g.dtype = dtype, g.dim_class = cls, g.first_seq = (int64_t)out.seqs.size();
-      int64_t few = 0, many = 0, few_most = 0;  // units; slices of units of few rows, at most
-      for (int32_t i = 0; i < n; ++i) {
-        const AttnDev &d = out.problems[(size_t)i];
-        if (!d.out || d.dtype != dtype || dim_class(d.dim) != cls) continue;
-        const int64_t capacity = (int64_t)d.columns << d.page_shift, most_rows = (int64_t)d.max_new * d.group;
-        const int64_t blocks = (std::min<int64_t>(most_rows, MOST_FEW) + ROWS_FEW - 1) / ROWS_FEW;
-        few += (int64_t)d.sequences * d.kv_heads * blocks;
-        few_most += (int64_t)d.sequences * d.kv_heads * blocks * ((capacity + 4 * KEYS_FEW - 1) / (4 * KEYS_FEW));
-        if (most_rows > MOST_FEW) {
-          // sequences of many rows: their blocks are full but for one each
-          const int64_t rows = (int64_t)d.rows * d.group;
-          many += d.kv_heads * (rows / ROWS_MANY + std::min<int64_t>(d.sequences, rows / (MOST_FEW + 1) + 1));
-        }
-        for (int32_t s = 0; s < d.sequences; ++s)
-          out.seqs.push_back(AttnSeq{d.lengths + s, d.first_row + s, i, s, d.kv_heads, d.group, d.window, d.sinks, d.rows, d.max_new, capacity});
+  for (bool wide : {false, true}) {
+    AttnGroup g{};
+    g.wide = wide, g.first_seq = (int64_t)out.seqs.size();
+    int64_t few = 0, many = 0, few_most = 0, many_most = 0;  // units, and slices of them, at most
+    for (int32_t i = 0; i < n; ++i) {
+      const AttnDev &d = out.problems[(size_t)i];
+      if (!d.out || (d.dim > 128) != wide) continue;
+      const int64_t capacity = (int64_t)d.columns << d.page_shift, most_rows = (int64_t)d.max_new * d.group;
+      const int64_t blocks = (std::min<int64_t>(most_rows, MOST_FEW) + ROWS_FEW - 1) / ROWS_FEW, units = (int64_t)d.sequences * d.kv_heads * blocks;
+      few += units;
+      few_most += units * (capacity / (4 * KEYS_FEW) + 2);
+      if (most_rows > MOST_FEW) {
+        // sequences of many rows: their blocks are full but for one each
+        const int64_t rows = (int64_t)d.rows * d.group, full = d.kv_heads * (rows / ROWS_MANY + std::min<int64_t>(d.sequences, rows / (MOST_FEW + 1) + 1));
+        many += full;
+        many_most += full * (capacity / (4 * keys_many(d.dim)) + 2);
       }
-      g.sequences = (int64_t)out.seqs.size() - g.first_seq;
-      if (!g.sequences) continue;
-      g.grid_few = std::min(few + workgroups, few_most);
-      g.grid_many = many ? many + workgroups : 0;
-      if (g.grid_few + g.grid_many >= (int64_t)1 << 31) return refuse(err, SK_ERR_UNSUPPORTED, "more units of work than a launch's grid can hold");
-      out.workspace_floats = std::max(out.workspace_floats, g.grid_few * part_floats(ROWS_FEW, cls) + g.grid_many * part_floats(ROWS_MANY, cls));
-      out.counters = std::max(out.counters, g.grid_few + g.grid_many);
-      out.groups.push_back(g);
+      for (int32_t s = 0; s < d.sequences; ++s)
+        out.seqs.push_back(AttnSeq{d.lengths + s, d.first_row + s, i, s, d.kv_heads, d.group, d.window, d.sinks, d.rows, d.max_new, capacity});
     }
+    g.sequences = (int64_t)out.seqs.size() - g.first_seq;
+    if (!g.sequences) continue;
+    g.many = many > 0;
+    g.workgroups = workgroups ? workgroups : (int64_t)resident(g.wide, g.many) * compute_units;
+    g.grid_few = std::min(few + g.workgroups, few_most);
+    g.grid_many = std::min(many + g.workgroups, many_most);
+    if (g.grid_few + g.grid_many >= (int64_t)1 << 31) return refuse(err, SK_ERR_UNSUPPORTED, "more units of work than a launch's grid can hold");
+    const int64_t dim = wide ? 256 : 128;
+    out.workspace_floats = std::max(out.workspace_floats, g.grid_few * part_floats(ROWS_FEW, dim) + g.grid_many * part_floats(ROWS_MANY, dim));
+    out.counters = std::max(out.counters, g.grid_few + g.grid_many);
+    out.groups.push_back(g);
+  }
   return SK_OK;
 }
 

@@ -43,7 +43,7 @@ static void plans(std::mt19937 &rng) {
     }
     sk::AttnPlanHost h;
     std::string err;
-    const sk_status st = sk::plan_attn(ps.data(), (int32_t)ps.size(), 512, h, err);
+    const sk_status st = sk::plan_attn(ps.data(), (int32_t)ps.size(), 256, pick(0, 2) ? 0 : pick(1, 2000), h, err);
     need((st == SK_OK) == err.empty(), "an error without a text, or a text without an error");
     if (st != SK_OK) continue;
     need(h.problems.size() == ps.size() && h.append_first.size() == ps.size() + 1, "sizes");
@@ -66,7 +66,7 @@ static void plans(std::mt19937 &rng) {
       }
       need(g.grid_few >= few && g.grid_many >= many, "units without a workgroup");
       need(h.counters >= g.grid_few + g.grid_many, "counters");
-      need(h.workspace_floats >= g.grid_few * sk::part_floats(sk::ROWS_FEW, g.dim_class) + g.grid_many * sk::part_floats(sk::ROWS_MANY, g.dim_class), "workspace");
+      need(h.workspace_floats >= g.grid_few * sk::part_floats(sk::ROWS_FEW, g.wide ? 256 : 128) + g.grid_many * sk::part_floats(sk::ROWS_MANY, g.wide ? 256 : 128), "workspace");
     }
   }
 }
