@@ -108,7 +108,7 @@ def build_cache(verbose: bool = False, extra=(), lib: str = CACHE_LIB) -> str:
     o_units = [os.path.join(obj_dir, f"cache_instances{u}.o") for u in range(CACHE_UNITS)]
     compiles = [[hipcc, *HIPCC_FLAGS, *extra, *inc, f"-DSK_UNIT={u}", "-c", srcs[2], "-o", o] for u, o in enumerate(o_units)] + [
         [hipcc, *HIPCC_FLAGS, *extra, *inc, "-c", srcs[0], "-o", o_hip],
-        ["g++", "-O2", "-std=c++17", "-fPIC", "-Wall", *inc, "-c", srcs[1], "-o", o_cpp],
+        ["g++", "-O2", "-std=c++17", "-fPIC", "-Wall", *(e for e in extra if e.startswith("-D")), *inc, "-c", srcs[1], "-o", o_cpp],
     ]
     run = _runner(verbose)
     with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:

@@ -17,6 +17,7 @@ constexpr int CACHE_THREADS = 256;
 constexpr int ROWS_FEW = 16, ROWS_MANY = 128, MOST_FEW = 32;
 constexpr int KEYS_FEW = 32;                                  // keys per step
 constexpr int keys_many(int dim) { return dim <= 128 ? 64 : 32; }  // (heads of 256: what a thread has in flight has to fit its registers)
+constexpr int APPEND_WAVES = 8192;  // append: a problem's rows are cut into parts for at least that many waves where they have the heads for it
 constexpr int MOST_SPLITS = 256;              // workgroups that share a unit's keys, at most
 
 // A problem as the kernels see it (strides in elements).

@@ -24,7 +24,6 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 // (pointers out of descriptors: said to be global, so that loads are not flat ones)
 #define SK_GLOBAL __attribute__((address_space(1)))
 __device__ __forceinline__ u32x4 load16(const void *p) { return *(const u32x4 SK_GLOBAL *)(uintptr_t)p; }
-__device__ __forceinline__ f32x4 load_f4(const void *p) { return *(const f32x4 SK_GLOBAL *)(uintptr_t)p; }
 __device__ __forceinline__ int32_t load_i32(const int32_t *p) { return *(const int32_t SK_GLOBAL *)(uintptr_t)p; }
 __device__ __forceinline__ void store16(void *p, u32x4 v) { *(u32x4 SK_GLOBAL *)(uintptr_t)p = v; }
 __device__ __forceinline__ void store8(void *p, u32x2 v) { *(u32x2 SK_GLOBAL *)(uintptr_t)p = v; }
@@ -695,6 +694,10 @@ struct ManyLds {
   static constexpr int TILE = keys_many(DP) * (KeyRows<DP>::BYTES + ValueRows<DP>::BYTES), TILES = 2, BYTES = TILES * TILE + 16;
 };
 
+// Matrix instructions whose LDS operands are read a group ahead.  (Left alone the scheduler puts every read right above its use, and a wave
+// waits out the way to LDS and back each time: prompts of 8000 tokens PERF_BEFORE us against PERF_NOW.)
+__device__ __forceinline__ void fixed_order() { __builtin_amdgcn_sched_barrier(0); }
+
 template <int DT, int DP>
 __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT AttnDev &P, const Unit &u, unsigned char *lds, uint32_t *flag) {
   constexpr int64_t SLOT = part_floats(ROWS_MANY, DP <= 128 ? 128 : 256);
@@ -814,13 +817,25 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
       const bool whole = now == (1u << KEYS / 16) - 1 && key0 + KEYS - 1 <= w0 && (P.window == 0 || w1 - key0 < P.window);
       f32x16 s[HALVES];
 #pragma unroll
-      for (int half = 0; half < HALVES; ++half) {
+      for (int half = 0; half < HALVES; ++half)
 #pragma unroll
         for (int j = 0; j < 16; ++j) s[half][j] = 0.f;
+      {
+        constexpr int N = HALVES * KS, G = KS % 4 == 0 ? 4 : 2;
+        u32x4 kf[2][G];
+        auto read = [&](int n, u32x4 (&f)[G]) {
 #pragma unroll
-        for (int k = 0; k < KS; ++k) {
-          const u32x4 kf = *(const u32x4 *)(ks + KR::at(32 * half + c, 2 * (16 * k + 8 * h)));
-          mma32<DT>(kf, qf[k], s[half]);
+          for (int i = 0; i < G; ++i) f[i] = *(const u32x4 *)(ks + KR::at(32 * ((n + i) / KS) + c, 2 * (16 * ((n + i) % KS) + 8 * h)));
+        };
+        read(0, kf[0]);
+        fixed_order();
+#pragma unroll
+        for (int n = 0; n < N; n += G) {
+          if (n + G < N) read(n + G, kf[n / G + 1 & 1]);
+          fixed_order();
+#pragma unroll
+          for (int i = 0; i < G; ++i) mma32<DT>(kf[n / G & 1][i], qf[(n + i) % KS], s[(n + i) / KS]);
+          fixed_order();
         }
       }
       // lane (h, c) has the scores of row c and keys key0 + 32 half + 8 (i / 4) + 4 h + i % 4
@@ -860,13 +875,26 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
         for (int i = 0; i < NB; ++i) o[i] *= keep;
       }
       m = next;
+      {
+        constexpr int G = 2 * HALVES;  // of a block of 32 elements: all its keys
+        u32x4 vf[2][G];
+        auto read = [&](int i, u32x4 (&f)[G]) {
 #pragma unroll
-      for (int i = 0; i < NB; ++i) {
+          for (int t = 0; t < G; ++t) {
+            const int row = 16 * t + 4 * h + ((lane & 15) >> 2), byte = 2 * (32 * i + 16 * ((lane >> 4) & 1) + 4 * (lane & 3));
+            const u32x2 x = read_transposed(vs + VR::at(row, byte)), y = read_transposed(vs + VR::at(row + 8, byte));
+            f[t] = u32x4{x.x, x.y, y.x, y.y};
+          }
+        };
+        read(0, vf[0]);
+        fixed_order();
 #pragma unroll
-        for (int t = 0; t < 2 * HALVES; ++t) {
-          const int row = 16 * t + 4 * h + ((lane & 15) >> 2), byte = 2 * (32 * i + 16 * ((lane >> 4) & 1) + 4 * (lane & 3));
-          const u32x2 x = read_transposed(vs + VR::at(row, byte)), y = read_transposed(vs + VR::at(row + 8, byte));
-          mma32<DT>(u32x4{x.x, x.y, y.x, y.y}, pf[t], o[i]);
+        for (int i = 0; i < NB; ++i) {
+          if (i + 1 < NB) read(i + 1, vf[i + 1 & 1]);
+          fixed_order();
+#pragma unroll
+          for (int t = 0; t < G; ++t) mma32<DT>(vf[i & 1][t], pf[t], o[i]);
+          fixed_order();
         }
       }
     }

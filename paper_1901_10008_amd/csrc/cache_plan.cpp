@@ -124,7 +124,7 @@ sk_status plan_attn(const sk_attn_problem *problems, int32_t n, int32_t compute_
     d.lanes_per_head = 1;
     while (d.lanes_per_head * 8 < d.dim) d.lanes_per_head *= 2;
     const int64_t at_once = 64 / d.lanes_per_head, most = (heads + at_once - 1) / at_once;
-    d.turns = (int32_t)std::max<int64_t>(1, std::min(most, (int64_t)d.rows * most / 8192));
+    d.turns = (int32_t)std::max<int64_t>(1, std::min(most, (int64_t)d.rows * most / APPEND_WAVES));
     d.parts = (int32_t)((most + d.turns - 1) / d.turns);
     append_grid += d.qkv ? ((int64_t)d.rows * d.parts + 3) / 4 : 0;
     if (append_grid >= (int64_t)1 << 31) return refuse(err, SK_ERR_UNSUPPORTED, "more rows than a launch's grid can hold");

@@ -8,6 +8,11 @@ namespace sk {
 // ---------------------------------------------------------------------------
 // norm, rotation, append
 // ---------------------------------------------------------------------------
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+__device__ __forceinline__ f32x4 load_f4_any(const float *p) { return *(const f32x4_any SK_GLOBAL *)(uintptr_t)p; }
+__device__ __forceinline__ float load_f(const float *p) { return *(const float SK_GLOBAL *)(uintptr_t)p; }
+__device__ __forceinline__ uint32_t load_u16(const void *p) { return *(const uint16_t SK_GLOBAL *)(uintptr_t)p; }
+
 struct AppendArgs {
   const AttnDev *problems;
   const uint32_t *first;  // first workgroup of each problem
@@ -28,85 +33,178 @@ __device__ __forceinline__ int32_t last_not_above(const T *first, int32_t n, int
   return lo;
 }
 
-template <int DT>
-__device__ __forceinline__ void append_row(const AttnDev &P, int32_t row, int32_t part, int lane) {
-  const int32_t seq = last_not_above(P.first_row, P.sequences, row, lane);
-  const int32_t a = load_i32(P.first_row + seq), b = load_i32(P.first_row + seq + 1);
-  if (row < a || row >= b) return;
-  const int64_t capacity = (int64_t)P.columns << P.page_shift;
-  const int64_t length = min((int64_t)max(load_i32(P.lengths + seq), 0), capacity);
-  const int64_t pos = length - (min(b, P.rows) - a) + (row - a);
-  const bool in_cache = pos >= 0 && pos < capacity;
-  const int32_t page = in_cache ? load_i32(P.table + (int64_t)seq * P.columns + (pos >> P.page_shift)) : -1;
-  const bool there = (uint32_t)page < (uint32_t)P.num_pages;
-  const int64_t slot = (int64_t)page * P.page_stride + (pos & ((1 << P.page_shift) - 1)) * P.token_stride;
-  const int half = P.rotary / 2;
-  const int64_t angle = min(max(pos, (int64_t)0), (int64_t)max(P.positions - 1, 0)) * half;
+// The sum over groups of 1, 2, 4, .. 32 neighbouring lanes, in each of them.
+template <int CTRL>
+__device__ __forceinline__ float other_lane(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int32_t, v), CTRL, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float sum_over(float v, int lanes) {
+  if (lanes >= 2) v += other_lane<0xb1>(v);    // quad_perm: the other of two
+  if (lanes >= 4) v += other_lane<0x4e>(v);    // quad_perm: the other two of four
+  if (lanes >= 8) v += other_lane<0x141>(v);   // row_half_mirror
+  if (lanes >= 16) v += other_lane<0x140>(v);  // row_mirror
+  if (lanes >= 32) v = sum16(v);
+  return v;
+}
 
-  const int lph = P.lanes_per_head, e0 = (lane & (lph - 1)) * 8, heads = P.q_heads + 2 * P.kv_heads;
-  const int at_once = 64 / lph;
-  const char *x_row = (const char *)P.qkv + 2 * (int64_t)row * P.qkv_row;
-  for (int t = 0; t < P.turns; ++t) {
-    const int head = (part * P.turns + t) * at_once + lane / lph;
-    const bool ok = head < heads && e0 < P.dim;
-    const char *xp = x_row + 2 * ((int64_t)head * P.dim + e0);
-    u32x4 raw = load16(ok ? (const void *)xp : (const void *)g_zeros);
-    const int kind = head < P.q_heads ? 0 : head < P.q_heads + P.kv_heads ? 1 : 2;
-    if (kind < 2) {
-      const void *w = kind == 0 ? P.q_weight : P.k_weight;
-      float y[8];
-      unpack8<DT>(raw, y);
-      float scale = 1.f;
-      if (w) {
-        float sum = 0.f;
+// How a row's heads are rotated: not at all; pairs of elements half the rotated length apart, where that is whole pieces of 8; neighbours, in
+// whole pieces; element by element.
+enum { ROTATE_NONE, ROTATE_HALVES, ROTATE_NEIGHBOURS, ROTATE_ANY };
+
+// A wave takes some heads of a row, 8 elements a lane, in turns of as many heads as it has lanes for.  What a lane needs of the angles and weights is
+// the same in every turn and stays in registers; the other element of a pair is read from memory once more (the line is in the L1)
+// and normalised like the first.
+template <int DT, int ROTATE>
+__device__ __forceinline__ void append_heads(const SK_CONSTANT AttnDev &P, int64_t row, int32_t part, int lane, int64_t angle, bool there, int64_t slot) {
+  const int lph = P.lanes_per_head, e0 = (lane & (lph - 1)) * 8, at_once = 64 / lph, dim = P.dim, half = P.rotary / 2;
+  const int q_heads = P.q_heads, kv_heads = P.kv_heads, heads = q_heads + 2 * kv_heads;
+  const char *x = (const char *)P.qkv + 2 * (row * P.qkv_row + e0);
+  const bool in_head = e0 < dim, turned = ROTATE != ROTATE_NONE && e0 < P.rotary;
+  const bool low = e0 < half;
+  const int other = ROTATE == ROTATE_HALVES && turned ? (low ? half : -half) : 0;  // from a lane's elements to the others of their pairs
+  const bool q_norm = P.q_weight != nullptr, k_norm = P.k_weight != nullptr;
+
+  u32x4 qw = {0, 0, 0, 0}, kw = qw, qo = qw, ko = qw;
+  if (q_norm) {
+    qw = load16(in_head ? (const char *)P.q_weight + 2 * e0 : (const char *)g_zeros);
+    if (ROTATE == ROTATE_HALVES) qo = load16(in_head ? (const char *)P.q_weight + 2 * (e0 + other) : (const char *)g_zeros);
+  }
+  if (k_norm) {
+    kw = load16(in_head ? (const char *)P.k_weight + 2 * e0 : (const char *)g_zeros);
+    if (ROTATE == ROTATE_HALVES) ko = load16(in_head ? (const char *)P.k_weight + 2 * (e0 + other) : (const char *)g_zeros);
+  }
+  // (a, b) -> (a co - b si, b co + a si): of halves a lane holds eight a or eight b, and si has the sign it needs
+  float co[8], si[8];
+  if constexpr (ROTATE == ROTATE_HALVES || ROTATE == ROTATE_NEIGHBOURS) {
+    constexpr int N = ROTATE == ROTATE_HALVES ? 8 : 4;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum += y[i] * y[i];
-        for (int d = 1; d < lph; d *= 2) sum += __shfl_xor(sum, d);
-        scale = 1.f / sqrtf(sum / (float)P.dim + P.eps);
-        float f[8];
-        unpack8<DT>(load16(e0 < P.dim ? (const void *)((const char *)w + 2 * e0) : (const void *)g_zeros), f);
+    for (int i = 0; i < 8; ++i) co[i] = 1.f, si[i] = 0.f;
+    if (turned) {
+      const int64_t at = angle + (ROTATE == ROTATE_HALVES ? (low ? e0 : e0 - half) : e0 / 2);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] *= scale * f[i];
+      for (int i = 0; i < N; i += 4) {
+        const f32x4 c4 = load_f4_any(P.cos + at + i), s4 = load_f4_any(P.sin + at + i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          co[i + j] = c4[j];
+          si[i + j] = ROTATE == ROTATE_HALVES && low ? -s4[j] : s4[j];
+        }
       }
-      if (ok && e0 < P.rotary) {
-        if (P.neighbours) {
+    }
+  }
+    u32x4 raw, pair;  // of the next turn
+  const int first = part * P.turns * at_once + lane / lph;
+  auto load = [&](int t, u32x4 &v, u32x4 &w) {
+    const int head = first + t * at_once;
+    const bool ok = head < heads && in_head && t < P.turns;
+    const char *p = x + 2 * (int64_t)head * dim;
+    v = load16(ok ? p : (const char *)g_zeros);
+    if (ROTATE == ROTATE_HALVES) w = load16(ok ? p + 2 * other : (const char *)g_zeros);
+  };
+  load(0, raw, pair);
+  for (int t = 0; t < P.turns; ++t) {
+    const int head = first + t * at_once;
+    u32x4 v = raw;
+    const u32x4 w = pair;
+    load(t + 1, raw, pair);
+    const int kind = head < q_heads ? 0 : head < q_heads + kv_heads ? 1 : 2;
+    const bool norm = kind == 0 ? q_norm : kind == 1 && k_norm;
+    float y[8];
+    unpack8<DT>(v, y);
+    float scale = 1.f;
+    if (__ballot(norm)) {
+      float sum = 0.f;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (e0 + 2 * i >= P.rotary) break;
-            const float co = P.cos[angle + e0 / 2 + i], si = P.sin[angle + e0 / 2 + i], u = y[2 * i], v = y[2 * i + 1];
-            y[2 * i] = u * co - v * si;
-            y[2 * i + 1] = v * co + u * si;
-          }
-        } else {
-          // the other element of a pair, normalised like this one
+      for (int k = 0; k < 8; ++k) sum += y[k] * y[k];
+      sum = sum_over(sum, lph);
+      if (norm) {
+        scale = 1.f / sqrtf(sum / (float)dim + P.eps);
+        float f[8];
+        unpack8<DT>(kind == 0 ? qw : kw, f);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int e = e0 + i;
+        for (int k = 0; k < 8; ++k) y[k] *= scale * f[k];
+      }
+    }
+    if (kind < 2) {
+      if constexpr (ROTATE == ROTATE_HALVES) {
+        float z[8], f[8];
+        unpack8<DT>(w, z);
+        unpack8<DT>(kind == 0 ? qo : ko, f);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float r = y[k] * co[k] + (norm ? z[k] * (scale * f[k]) : z[k]) * si[k];
+          y[k] = turned ? r : y[k];  // (an infinite element that is not rotated stays what it is)
+        }
+      } else if constexpr (ROTATE == ROTATE_NEIGHBOURS) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float a = y[2 * k], b = y[2 * k + 1];
+          y[2 * k] = turned ? a * co[k] - b * si[k] : a;
+          y[2 * k + 1] = turned ? b * co[k] + a * si[k] : b;
+        }
+      } else if constexpr (ROTATE == ROTATE_ANY) {
+        if (turned && head < heads && in_head) {
+          const char *xp = x + 2 * (int64_t)head * dim;
+          const char *wp = (const char *)(kind == 0 ? P.q_weight : P.k_weight) + 2 * e0;
+          for (int k = 0; k < 8; ++k) {
+            const int e = e0 + k;
             if (e >= P.rotary) break;
-            const bool low = e < half;
-            const int other = low ? e + half : e - half, at = low ? e : other;
-            const float co = P.cos[angle + at], si = P.sin[angle + at];
-            float z = elem<DT>(*(const uint16_t SK_GLOBAL *)(uintptr_t)(xp + 2 * (other - e0)));
-            if (w) z *= scale * elem<DT>(*(const uint16_t SK_GLOBAL *)(uintptr_t)((const char *)w + 2 * other));
-            y[i] = low ? y[i] * co - z * si : y[i] * co + z * si;
+            const bool a = P.neighbours ? (e & 1) == 0 : e < half;
+            const int to = P.neighbours ? (a ? 1 : -1) : (a ? half : -half), at = P.neighbours ? e / 2 : (a ? e : e - half);
+            float z = elem<DT>(load_u16(xp + 2 * (k + to)));
+            if (norm) z *= scale * elem<DT>(load_u16(wp + 2 * (k + to)));
+            const float c1 = load_f(P.cos + angle + at), s1 = load_f(P.sin + angle + at), o = elem<DT>(load_u16(xp + 2 * k));
+            const float n = norm ? o * (scale * elem<DT>(load_u16(wp + 2 * k))) : o;
+            const float r = a ? n * c1 - z * s1 : n * c1 + z * s1;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = j == k ? r : y[j];
           }
         }
       }
-      raw = u32x4{pack2<DT>(y[0], y[1]), pack2<DT>(y[2], y[3]), pack2<DT>(y[4], y[5]), pack2<DT>(y[6], y[7])};
+      if (norm || ROTATE != ROTATE_NONE) v = u32x4{pack2<DT>(y[0], y[1]), pack2<DT>(y[2], y[3]), pack2<DT>(y[4], y[5]), pack2<DT>(y[6], y[7])};
     }
-    if (!ok) continue;
+    if (head >= heads || !in_head) continue;
     if (kind == 0)
-      store16((char *)P.q + 2 * ((int64_t)row * P.q_row + (int64_t)head * P.q_head + e0), raw);
+      store16((char *)P.q + 2 * (row * P.q_row + (int64_t)head * P.q_head + e0), v);
     else if (there)
-      store16((char *)(kind == 1 ? P.k : P.v) + 2 * (slot + (int64_t)(head - P.q_heads - (kind == 1 ? 0 : P.kv_heads)) * P.head_stride + e0), raw);
+      store16((char *)(kind == 1 ? P.k : P.v) + 2 * (slot + (int64_t)(head - q_heads - (kind == 1 ? 0 : kv_heads)) * P.head_stride + e0), v);
+  }
+}
+
+template <int DT>
+__device__ __forceinline__ void append_row(const SK_CONSTANT AttnDev &P, int32_t row, int32_t part, int lane) {
+  int32_t seq, a, b, n;
+  if (P.sequences <= 64) {  // a sequence per lane
+    const int s = min(lane, P.sequences - 1);
+    const int32_t first = load_i32(P.first_row + s), next = load_i32(P.first_row + s + 1), length = load_i32(P.lengths + s);
+    seq = max(1, (int32_t)__popcll(__ballot(lane < P.sequences && first <= row))) - 1;
+    a = lane_of(first, seq), b = lane_of(next, seq), n = lane_of(length, seq);
+  } else {
+    seq = __builtin_amdgcn_readfirstlane(last_not_above(P.first_row, P.sequences, row, lane));
+    a = load_i32(P.first_row + seq), b = load_i32(P.first_row + seq + 1), n = load_i32(P.lengths + seq);
+  }
+  if (row < a || row >= b) return;
+  const int64_t capacity = (int64_t)P.columns << P.page_shift;
+  const int64_t pos = min((int64_t)max(n, 0), capacity) - (min(b, P.rows) - a) + (row - a);
+  const int32_t page = pos >= 0 ? load_i32(P.table + (int64_t)seq * P.columns + (pos >> P.page_shift)) : -1;
+  const bool there = (uint32_t)page < (uint32_t)P.num_pages;
+  const int64_t slot = (int64_t)page * P.page_stride + (pos & ((1 << P.page_shift) - 1)) * P.token_stride;
+  const int64_t angle = max(pos, (int64_t)0) * (P.rotary / 2);
+  const int kind = P.rotary == 0 ? ROTATE_NONE : !P.neighbours && P.rotary % 16 == 0 ? ROTATE_HALVES : P.neighbours && P.rotary % 8 == 0 ? ROTATE_NEIGHBOURS : ROTATE_ANY;
+  switch (kind) {
+    case ROTATE_NONE: return append_heads<DT, ROTATE_NONE>(P, row, part, lane, angle, there, slot);
+    case ROTATE_HALVES: return append_heads<DT, ROTATE_HALVES>(P, row, part, lane, angle, there, slot);
+    case ROTATE_NEIGHBOURS: return append_heads<DT, ROTATE_NEIGHBOURS>(P, row, part, lane, angle, there, slot);
+    default: return append_heads<DT, ROTATE_ANY>(P, row, part, lane, angle, there, slot);
   }
 }
 
 __global__ void __launch_bounds__(CACHE_THREADS) sk_append(AppendArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int32_t problem = __builtin_amdgcn_readfirstlane(last_not_above(a.first, a.n, (int64_t)blockIdx.x, lane));
-  const AttnDev &P = a.problems[problem];
-  const int64_t n = ((int64_t)blockIdx.x - a.first[problem]) * 4 + wave;
+  const SK_CONSTANT AttnDev &P = *(const SK_CONSTANT AttnDev *)(uintptr_t)(a.problems + problem);
+  const uint32_t first = a.n == 1 ? 0u : ((const SK_CONSTANT uint32_t *)(uintptr_t)a.first)[problem];
+  const int64_t n = ((int64_t)blockIdx.x - first) * 4 + wave;
   const int64_t row = n / P.parts;
   if (row >= P.rows) return;
   if (P.dtype == SK_BF16)

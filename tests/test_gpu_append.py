@@ -78,6 +78,24 @@ def test_zeros_and_large_values():
     check_append([t], "zeros and large values")
 
 
+@pytest.mark.parametrize("neighbours", [False, True])
+def test_infinite_elements_touch_their_pair_alone(neighbours):
+    t = tenant("bf16", (4, 2, 64), ((5, 2),), rotary=32, neighbours=neighbours, norm=False, seed=9)
+    want_t = tenant("bf16", (4, 2, 64), ((5, 2),), rotary=32, neighbours=neighbours, norm=False, seed=9)
+    t.qkv[0, :, 40], t.qkv[1, :, 3] = math.inf, -math.inf
+    problem = t.to_device()
+    with sk.sk_attn_plan_create([problem]) as plan:
+        sk.sk_attn_append(plan, H.stream_handle())
+        torch.cuda.synchronize()
+    (q, k, v), (tq, tk) = want_t.append()
+    got = t.dq.cpu().double()
+    pair = [3, 2] if neighbours else [3, 19]
+    assert (got[0, :, 40] == math.inf).all() and not torch.isfinite(got[1][:, pair]).any()
+    for row, odd in ((0, [40]), (1, pair)):
+        fine = [e for e in range(64) if e not in odd]
+        H.assert_close(got[row][:, fine], q[row][:, fine], tq[row][:, fine], f"row {row}")
+
+
 def test_append_then_attend_as_a_step():
     """The queries that append has written are attend's, and the keys and values it has appended are seen."""
     t = Tenant("bf16", (4, 2, 64), STEP, with_qkv=True, rotary=64, window=30, sinks=2, seed=8)
