@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "cache_internal.h"
 
 #if defined(__HIP_DEVICE_COMPILE__) && !defined(__gfx950__)
@@ -388,9 +390,12 @@ struct Pages {
   }
 };
 
-// The softmax of a row, piece after piece: with m the maximum so far and l = sum exp2(s - m), a piece with maximum m' makes
-// M = max(m, m'), l = l exp2(m - M) + sum exp2(s - M), and the outputs so far are scaled by the same exp2(m - M).  A row that
+// The softmax of a row, piece after piece: weights are exp2(s - m) with a base m, l is their sum.  m is the maximum of the first piece
+// that the row sees anything of; a later piece moves it (and l and the outputs so far are scaled by exp2(m - new m)) only where its
+// maximum is more than RISE above it: until then weights of up to 2^RISE are as exact in 16 bits as those up to 1, and sums in fp32
+// do not mind.  (With rows of random scores some row of 32 meets a new maximum in more than half of the steps of a prompt.)  A row that
 // has seen nothing has m = -inf; exp2 is then taken relative to 0, so that it stays at l = 0.
+constexpr float RISE = 8.f;
 __device__ __forceinline__ float base_of(float m) { return m == -__builtin_inff() ? 0.f : m; }
 __device__ __forceinline__ float inverse(float sum) { return sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum); }  // (nothing seen: 0)
 
@@ -581,21 +586,21 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, const SK_CONSTANT 
     }
     float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
     top = max32(max16(top)) * scale;
-    const float next = fmaxf(m, top), base = base_of(next), keep = exp2_fast(m - base);
-    float sum = 0.f;
+    if (__ballot(top > m + RISE)) {
+      const float next = fmaxf(m, top), keep = exp2_fast(m - base_of(next));
+      m = next;
+      l *= keep;
+#pragma unroll
+      for (int i = 0; i < NB; ++i) o[i] *= keep;
+    }
+    const float base = base_of(m);
 #pragma unroll
     for (int half = 0; half < 2; ++half)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         s[half][i] = exp2_fast(fmaf(s[half][i], scale, -base));
-        sum += s[half][i];
+        l += s[half][i];
       }
-    l = l * keep + sum;
-    if (__ballot(next > m)) {
-#pragma unroll
-      for (int i = 0; i < NB; ++i) o[i] *= keep;
-    }
-    m = next;
     const u32x4 pf = {pack2<DT>(s[0][0], s[0][1]), pack2<DT>(s[0][2], s[0][3]), pack2<DT>(s[1][0], s[1][1]), pack2<DT>(s[1][2], s[1][3])};
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
@@ -688,133 +693,171 @@ struct KeyRows {
     return row * BYTES + (byte ^ (turn << 4));
   }
 };
-// Two tiles of keys and values in LDS in turn.
+// Two tiles of keys and values in LDS in turn, behind them which blocks of 16 keys of each are there, and whether values were taken out.
 template <int DP>
 struct ManyLds {
-  static constexpr int TILE = keys_many(DP) * (KeyRows<DP>::BYTES + ValueRows<DP>::BYTES), TILES = 2, BYTES = TILES * TILE + 16;
+  static constexpr int TILE = keys_many(DP) * (KeyRows<DP>::BYTES + ValueRows<DP>::BYTES), PRESENT = 2 * TILE, ODD = PRESENT + 8, BYTES = ODD + 8;
 };
 
 // Matrix instructions whose LDS operands are read a group ahead.  (Left alone the scheduler puts every read right above its use, and a wave
-// waits out the way to LDS and back each time: prompts of 8000 tokens PERF_BEFORE us against PERF_NOW.)
+// waits out the way to LDS and back each time.)
 __device__ __forceinline__ void fixed_order() { __builtin_amdgcn_sched_barrier(0); }
 
+// N pieces of 16 bytes a lane from memory into LDS: lane i's arrive at lds_addr + 1024 n + 16 i.  The instruction's own offset counts on both
+// sides, so the lanes' offsets are lowered by as much and the descriptor begins DMA_FRONT bytes in front.  What lies outside the descriptor
+// arrives as zeros.  In one statement, opened with the wait states that scalar registers written by vector instructions want before a memory
+// instruction reads them; the compiler does not know of the loads, so they are waited for by hand (wait_dma).
+constexpr int DMA_FRONT = 3072;
+constexpr uint32_t DMA_OUTSIDE = 0x80000000u;
+template <int N>
+__device__ __forceinline__ void dma(__amdgpu_buffer_rsrc_t desc, const uint32_t (&at)[N], uint32_t lds_addr) {
+  static_assert(N == 2 || N == 4, "written out for these");
+  if constexpr (N == 4)
+    asm volatile("s_nop 4\n\t"
+                 "buffer_load_dwordx4 %0, %4, 0 offen lds\n\t"
+                 "buffer_load_dwordx4 %1, %4, 0 offen offset:1024 lds\n\t"
+                 "buffer_load_dwordx4 %2, %4, 0 offen offset:2048 lds\n\t"
+                 "buffer_load_dwordx4 %3, %4, 0 offen offset:3072 lds"
+                 :
+                 : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "s"(desc), "{m0}"(lds_addr)
+                 : "memory");
+  else
+    asm volatile("s_nop 4\n\t"
+                 "buffer_load_dwordx4 %0, %2, 0 offen lds\n\t"
+                 "buffer_load_dwordx4 %1, %2, 0 offen offset:1024 lds"
+                 :
+                 : "v"(at[0]), "v"(at[1]), "s"(desc), "{m0}"(lds_addr)
+                 : "memory");
+}
+__device__ __forceinline__ void wait_dma() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+#ifdef PRIO
+#define SETPRIO(x) __builtin_amdgcn_s_setprio((x) * PRIO)
+#else
+#define SETPRIO(x)
+#endif
 template <int DT, int DP>
 __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT AttnDev &P, const Unit &u, unsigned char *lds, uint32_t *flag) {
   constexpr int64_t SLOT = part_floats(ROWS_MANY, DP <= 128 ? 128 : 256);
-  constexpr int KEYS = keys_many(DP), HALVES = KEYS / 32;
-  constexpr int KS = DP / 16, NB = DP / 32, PR = DP / 8, LI = KEYS * PR / CACHE_THREADS;  // LI pieces per thread and tile, keys and values each
   using KR = KeyRows<DP>;
   using VR = ValueRows<DP>;
-  constexpr int TILE = ManyLds<DP>::TILE;
+  constexpr int KEYS = keys_many(DP), HALVES = KEYS / 32, KS = DP / 16, NB = DP / 32, TILE = ManyLds<DP>::TILE, VALUES = KEYS * KR::BYTES;
+  // a wave brings NI KB of keys and as much of values: ROWS consecutive keys, which lie in one block of 16
+  constexpr int NI = KEYS * KR::BYTES / 4096, SLOTS = KR::BYTES / 16, ROWS = KEYS / 4;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, c = lane & 31;
   const Step &st = u.step;
-  const int32_t row0 = u.block * ROWS_MANY, rows = min(ROWS_MANY, st.fresh * P.group - row0);
-  const int32_t p0 = st.behind + row0 / P.group, p1 = st.behind + (row0 + rows - 1) / P.group;
-  const Span span = span_of<KEYS>(p0, p1, P.window, P.sinks);
+  const int32_t group = P.group, dim = P.dim, window = P.window, sinks = P.sinks;
+  const int32_t row0 = u.block * ROWS_MANY, rows = min(ROWS_MANY, st.fresh * group - row0);
+  const int32_t p0 = st.behind + row0 / group, p1 = st.behind + (row0 + rows - 1) / group;
+  const Span span = span_of<KEYS>(p0, p1, window, sinks);
   const int32_t b0 = (int32_t)((int64_t)span.blocks * u.split / u.splits), b1 = (int32_t)((int64_t)span.blocks * (u.split + 1) / u.splits);
 
   const Pages pages{P.table + (int64_t)u.seq * P.columns, P.page_shift, P.num_pages, P.columns, P.page_stride, P.token_stride};
   const char *kh = (const char *)P.k + 2 * (int64_t)u.head * P.head_stride, *vh = (const char *)P.v + 2 * (int64_t)u.head * P.head_stride;
   auto key_of = [&](int32_t b) { return b < span.sink_blocks ? b * KEYS : span.low + (b - span.sink_blocks) * KEYS; };
-  // offsets of this thread's pieces in their 16 keys; pieces beyond the head's end are read from its start and count as zeros
-  uint32_t lo[LI];
+  // Where this lane's pieces come from, counted from the first of the block's 16 keys.  Pieces beyond the head's end come as zeros.
+  const int32_t first_key = wave * ROWS, block = first_key / 16;  // of the wave, in a tile
+  uint32_t ko[NI], vo[NI];
 #pragma unroll
-  for (int i = 0; i < LI; ++i) {
-    const int n = i * CACHE_THREADS + tid, e = n % PR * 8;
-    lo[i] = 2u * (uint32_t)((n / PR & 15) * P.token_stride + (e < P.dim ? e : 0));
+  for (int i = 0; i < NI; ++i) {
+    const int key = first_key + i * (64 / SLOTS) + lane / SLOTS, place = lane % SLOTS * 16;
+    const int ke = (KR::at(key, place) - key * KR::BYTES) / 2, ve = (VR::at(key, place) - key * VR::BYTES) / 2;  // (turning over twice changes nothing)
+    const uint32_t at = 2u * (uint32_t)((key & 15) * P.token_stride) + DMA_FRONT - 1024 * i;
+    ko[i] = ke < dim ? at + 2 * ke : DMA_OUTSIDE;
+    vo[i] = ve < dim ? at + 2 * ve : DMA_OUTSIDE;
   }
-  u32x4 kr[LI], vr[LI];
-  int32_t page[KEYS / 16];  // of the tile that is loaded next
-  auto look = [&](int32_t b) {
-    const int32_t key0 = key_of(min(b, b1 - 1));
-#pragma unroll
-    for (int i = 0; i < KEYS / 16; ++i) page[i] = pages.page_of(key0 + 16 * i);
-  };
-  auto load = [&](int32_t b) -> uint32_t {  // which of its blocks of 16 keys are there
+  int32_t page = -1;  // of the wave's keys in the tile that is brought next
+  auto look = [&](int32_t b) { page = pages.page_of(key_of(min(b, b1 - 1)) + 16 * block); };
+  // whether every row of the unit sees all keys of a tile alike
+  auto alike = [&](int32_t key0) { return key0 + KEYS - 1 <= p0 && (window == 0 || p1 - key0 < window); };
+  auto bring = [&](int32_t b, int place) {
     const int32_t key0 = key_of(b);
-    uint32_t present = 0;
+    const bool there = pages.there(page);
+    const int64_t at = pages.bytes(page, key0 + 16 * block) - DMA_FRONT;
+    const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)(lds + place * TILE + wave * NI * 1024);
+    const int records = there ? (int)DMA_OUTSIDE : 0;
+    dma<NI>(__builtin_amdgcn_make_buffer_rsrc((void *)(kh + at), 0, records, 0x00020000), ko, to);
+    const __amdgpu_buffer_rsrc_t values = __builtin_amdgcn_make_buffer_rsrc((void *)(vh + at), 0, records, 0x00020000);
+    if (alike(key0)) {
+      dma<NI>(values, vo, to + VALUES);
+    } else {
+      // values that no row sees: what lies there may be anything
+      uint32_t some[NI];
 #pragma unroll
-    for (int i = 0; i < KEYS / 16; ++i) present |= pages.there(page[i]) ? 1u << i : 0u;
-#pragma unroll
-    for (int i = 0; i < LI; ++i) {
-      const int block = (i * 4 + wave) * 4 / PR;  // the wave's pieces lie in one block of 16 keys
-      const int32_t id = block == 0 ? page[0] : block == 1 || KEYS == 32 ? page[1] : block == 2 ? page[2 % (KEYS / 16)] : page[3 % (KEYS / 16)];
-      const int64_t at = pages.bytes(id, key0 + 16 * block);
-      kr[i] = load16(kh + at + lo[i]);
-      vr[i] = load16(vh + at + lo[i]);
+      for (int i = 0; i < NI; ++i) {
+        const int32_t j = key0 + first_key + i * (64 / SLOTS) + lane / SLOTS;
+        some[i] = j <= p1 && (window == 0 || p0 - j < window || j < sinks) ? vo[i] : DMA_OUTSIDE;
+      }
+      dma<NI>(values, some, to + VALUES);
     }
-    return present;
+    if (lane == 0) lds[ManyLds<DP>::PRESENT + 4 * place + wave] = there;
   };
-  bool cleaned = false;  // values that are not finite were taken out
-  // the loaded pieces of tile b to LDS
-  auto put = [&](int32_t b, uint32_t present, unsigned char *to) {
-    const int32_t key0 = key_of(b);
-    const bool whole = present == (1u << KEYS / 16) - 1 && key0 + KEYS - 1 <= p0 && (P.window == 0 || p1 - key0 < P.window);
-    if (!whole || P.dim != DP) {
+  // Behind bring(b): the wave's pieces are there; values that are not finite are taken out where rows differ in what they see.
+  bool cleaned = false;
+  auto arrived = [&](int32_t b, int place) {
+    wait_dma();
+    if (!alike(key_of(b))) {
 #pragma unroll
-      for (int i = 0; i < LI; ++i) {
-        const int n = i * CACHE_THREADS + tid;
-        const int32_t j = key0 + n / PR;
-        if (n % PR * 8 >= P.dim) kr[i] = u32x4{0u, 0u, 0u, 0u};
-        // values that no row sees: what lies there may be anything
-        const bool ok = (present >> (n / PR / 16) & 1) && n % PR * 8 < P.dim && j <= p1 && (P.window == 0 || p0 - j < P.window || j < P.sinks);
-        if (!ok) vr[i] = u32x4{0u, 0u, 0u, 0u};
-        if (!whole) cleaned |= clean<DT>(vr[i]);
+      for (int i = 0; i < NI; ++i) {
+        u32x4 *p = (u32x4 *)(lds + place * TILE + VALUES + wave * NI * 1024 + i * 1024 + 16 * lane);
+        u32x4 v = *p;
+        if (clean<DT>(v)) {
+          *p = v;
+          cleaned = true;
+        }
       }
     }
-#pragma unroll
-    for (int i = 0; i < LI; ++i) {
-      const int n = i * CACHE_THREADS + tid;
-      *(u32x4 *)(to + KR::at(n / PR, n % PR * 16)) = kr[i];
-      *(u32x4 *)(to + KEYS * KR::BYTES + VR::at(n / PR, n % PR * 16)) = vr[i];
-    }
   };
-  uint32_t present = 0;
   if (b0 < b1) {
     look(b0);
-    present = load(b0);
+    bring(b0, 0);
     look(b0 + 1);
   }
 
   const int32_t in_block = wave * 32 + c;
   const bool row_ok = in_block < rows;
   const int32_t my_row = row0 + min(in_block, rows - 1);
-  const int32_t my_token = my_row / P.group, my_head = u.head * P.group + my_row % P.group;
+  const int32_t my_token = my_row / group, my_head = u.head * group + my_row % group;
   const int32_t my_pos = row_ok ? st.behind + my_token : -1;
   // positions of the wave's rows (uniform)
   const bool wave_ok = wave * 32 < rows;
-  const int32_t w0 = st.behind + (row0 + min(wave * 32, rows - 1)) / P.group, w1 = st.behind + (row0 + min(wave * 32 + 31, rows - 1)) / P.group;
+  const int32_t w0 = st.behind + (row0 + min(wave * 32, rows - 1)) / group, w1 = st.behind + (row0 + min(wave * 32 + 31, rows - 1)) / group;
   const char *q = (const char *)P.q + 2 * ((int64_t)(st.first + my_token) * P.q_row + (int64_t)my_head * P.q_head);
   const float scale = fabsf(P.scale_log2);  // (its sign goes into the queries)
   u32x4 qf[KS];
 #pragma unroll
-  for (int s = 0; s < KS; ++s) qf[s] = load_query<DT>(q + 2 * (16 * s + 8 * h), row_ok && 16 * s + 8 * h < P.dim, P.scale_log2 < 0.f);
+  for (int s = 0; s < KS; ++s) qf[s] = load_query<DT>(q + 2 * (16 * s + 8 * h), row_ok && 16 * s + 8 * h < dim, P.scale_log2 < 0.f);
 
-  uint32_t *odd = (uint32_t *)(lds + ManyLds<DP>::TILES * TILE);  // whether any thread took values out
   f32x16 o[NB];
 #pragma unroll
   for (int i = 0; i < NB; ++i)
 #pragma unroll
     for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
   float m = -__builtin_inff(), l = 0.f;
+  // where this lane's operands stand in a tile
+  const unsigned char *ka[KS], *va[NB];
+#pragma unroll
+  for (int k = 0; k < KS; ++k) ka[k] = lds + KR::at(c, 2 * (16 * k + 8 * h));
+#pragma unroll
+  for (int i = 0; i < NB; ++i) va[i] = lds + VALUES + VR::at(4 * h + ((lane & 15) >> 2), 2 * (32 * i + 16 * ((lane >> 4) & 1) + 4 * (lane & 3)));
 
+  uint32_t *odd = (uint32_t *)(lds + ManyLds<DP>::ODD);  // whether any thread took values out
   if (tid == 0) *odd = 0;
-  uint32_t now = present;
-  if (b0 < b1) {
-    put(b0, present, lds);
-    if (b0 + 1 < b1) {
-      present = load(b0 + 1);
-      look(b0 + 2);
-    }
-  }
+  if (b0 < b1) arrived(b0, 0);
   __syncthreads();
-  for (int32_t b = b0; b < b1; ++b) {
+  auto step = [&](int32_t b, auto which) {
+    constexpr int PLACE = decltype(which)::value;
+    if (b + 1 < b1) {  // into the other place, which all waves have left behind the last barrier
+      bring(b + 1, 1 - PLACE);
+      look(b + 2);
+    }
     const int32_t key0 = key_of(b);
-    unsigned char *ks = lds + ((b - b0) & 1) * TILE, *vs = ks + KEYS * KR::BYTES;
     // whether any row of the wave sees any of these keys, and whether all see all
-    const bool use = wave_ok && key0 <= w1 && (P.window == 0 || w0 - (key0 + KEYS - 1) < P.window || key0 < P.sinks);
+    const bool use = wave_ok && key0 <= w1 && (window == 0 || w0 - (key0 + KEYS - 1) < window || key0 < sinks);
     if (use) {
-      const bool whole = now == (1u << KEYS / 16) - 1 && key0 + KEYS - 1 <= w0 && (P.window == 0 || w1 - key0 < P.window);
+      constexpr uint32_t ALL = 0x01010101u;
+      const uint32_t now = __builtin_amdgcn_readfirstlane(*(const uint32_t *)(lds + ManyLds<DP>::PRESENT + 4 * PLACE));
+      const bool whole = now == ALL && key0 + KEYS - 1 <= w0 && (window == 0 || w1 - key0 < window);
       f32x16 s[HALVES];
 #pragma unroll
       for (int half = 0; half < HALVES; ++half)
@@ -825,9 +868,10 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
         u32x4 kf[2][G];
         auto read = [&](int n, u32x4 (&f)[G]) {
 #pragma unroll
-          for (int i = 0; i < G; ++i) f[i] = *(const u32x4 *)(ks + KR::at(32 * ((n + i) / KS) + c, 2 * (16 * ((n + i) % KS) + 8 * h)));
+          for (int i = 0; i < G; ++i) f[i] = *(const u32x4 *)(ka[(n + i) % KS] + PLACE * TILE + (n + i) / KS * 32 * KR::BYTES);
         };
         read(0, kf[0]);
+        SETPRIO(1);
         fixed_order();
 #pragma unroll
         for (int n = 0; n < N; n += G) {
@@ -837,6 +881,7 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
           for (int i = 0; i < G; ++i) mma32<DT>(kf[n / G & 1][i], qf[(n + i) % KS], s[(n + i) / KS]);
           fixed_order();
         }
+        SETPRIO(0);
       }
       // lane (h, c) has the scores of row c and keys key0 + 32 half + 8 (i / 4) + 4 h + i % 4
       if (!whole) {
@@ -844,8 +889,8 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
         for (int half = 0; half < HALVES; ++half)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const int32_t j = key0 + 32 * half + 8 * (i / 4) + 4 * h + i % 4;
-            if (!((now >> (2 * half + i / 8) & 1) && sees(my_pos, j, P.window, P.sinks))) s[half][i] = -__builtin_inff();
+            const int32_t key = 32 * half + 8 * (i / 4), j = key0 + key + 4 * h + i % 4;
+            if (!((now >> (8 * (key / ROWS)) & 1) && sees(my_pos, j, window, sinks))) s[half][i] = -__builtin_inff();
           }
       }
       float top = -__builtin_inff();
@@ -854,39 +899,40 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
 #pragma unroll
         for (int i = 0; i < 16; i += 2) top = fmaxf(fmaxf(top, s[half][i]), s[half][i + 1]);
       top = max32(top) * scale;
-      const float next = fmaxf(m, top), base = base_of(next), keep = exp2_fast(m - base);
-      float sum = 0.f;
+      if (__ballot(top > m + RISE)) {
+        const float next = fmaxf(m, top), keep = exp2_fast(m - base_of(next));
+        m = next;
+        l *= keep;
+#pragma unroll
+        for (int i = 0; i < NB; ++i) o[i] *= keep;
+      }
+      const float base = base_of(m);
       u32x4 pf[2 * HALVES];
 #pragma unroll
       for (int half = 0; half < HALVES; ++half) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           s[half][i] = exp2_fast(fmaf(s[half][i], scale, -base));
-          sum += s[half][i];
+          l += s[half][i];
         }
 #pragma unroll
         for (int t = 0; t < 2; ++t)
           pf[2 * half + t] = u32x4{pack2<DT>(s[half][8 * t], s[half][8 * t + 1]), pack2<DT>(s[half][8 * t + 2], s[half][8 * t + 3]),
                                    pack2<DT>(s[half][8 * t + 4], s[half][8 * t + 5]), pack2<DT>(s[half][8 * t + 6], s[half][8 * t + 7])};
       }
-      l = l * keep + sum;
-      if (__ballot(next > m)) {  // (no row's maximum has grown: nothing to scale)
-#pragma unroll
-        for (int i = 0; i < NB; ++i) o[i] *= keep;
-      }
-      m = next;
       {
         constexpr int G = 2 * HALVES;  // of a block of 32 elements: all its keys
         u32x4 vf[2][G];
         auto read = [&](int i, u32x4 (&f)[G]) {
 #pragma unroll
           for (int t = 0; t < G; ++t) {
-            const int row = 16 * t + 4 * h + ((lane & 15) >> 2), byte = 2 * (32 * i + 16 * ((lane >> 4) & 1) + 4 * (lane & 3));
-            const u32x2 x = read_transposed(vs + VR::at(row, byte)), y = read_transposed(vs + VR::at(row + 8, byte));
+            const unsigned char *p = va[i] + PLACE * TILE + 16 * t * VR::BYTES;
+            const u32x2 x = read_transposed(p), y = read_transposed(p + 8 * VR::BYTES);
             f[t] = u32x4{x.x, x.y, y.x, y.y};
           }
         };
         read(0, vf[0]);
+        SETPRIO(1);
         fixed_order();
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
@@ -896,19 +942,15 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
           for (int t = 0; t < G; ++t) mma32<DT>(vf[i & 1][t], pf[t], o[i]);
           fixed_order();
         }
+        SETPRIO(0);
       }
     }
-    if (b + 1 < b1) {
-      // the next tile into the other place, which all waves have left behind the last barrier
-      const int place = (b + 1 - b0) & 1;
-      now = present;
-      put(b + 1, present, lds + place * TILE);
-      if (b + 2 < b1) {
-        present = load(b + 2);
-        look(b + 3);
-      }
-    }
+    if (b + 1 < b1) arrived(b + 1, 1 - PLACE);
     __syncthreads();
+  };
+  for (int32_t b = b0; b < b1; b += 2) {
+    step(b, std::integral_constant<int, 0>{});
+    if (b + 1 < b1) step(b + 1, std::integral_constant<int, 1>{});
   }
   if (cleaned) *odd = 1;
   __syncthreads();
@@ -917,8 +959,8 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
     for (int i = 0; i < NB; ++i)
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        if (32 * i + 8 * k + 4 * h < P.dim) {
-          const f32x4 x = odd_sum<DT>(pages, vh + 2 * (32 * i + 8 * k + 4 * h), b0, b1, 1, key_of, KEYS, my_pos, P.window, P.sinks);
+        if (32 * i + 8 * k + 4 * h < dim) {
+          const f32x4 x = odd_sum<DT>(pages, vh + 2 * (32 * i + 8 * k + 4 * h), b0, b1, 1, key_of, KEYS, my_pos, window, sinks);
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[i][4 * k + e] += x[e];
         }
