@@ -154,15 +154,17 @@ __device__ __forceinline__ Step step_of(const AttnSeq &q) {
   s.fresh = min(all, q.max_new);
   return s;
 }
-// The keys that rows at positions p0 .. p1 see: blocks of KEYS from 0 on that hold sinks, then blocks from `low` on.
+// The keys that rows at positions p0 .. p1 see: blocks of KEYS from `low` on (a multiple of 16), ahead of them blocks from 0 on for the sinks below
+// it.  The last of these may reach beyond `low`: of its keys only the first `sinks` of the span count.
 struct Span {
-  int32_t low, sink_blocks, blocks;
+  int32_t low, sinks, sink_blocks, blocks;
 };
 template <int KEYS>
 __device__ __forceinline__ Span span_of(int32_t p0, int32_t p1, int32_t window, int32_t sinks) {
   Span s;
-  s.low = window ? (p0 >= window ? p0 - window + 1 : 0) & ~(KEYS - 1) : 0;
-  s.sink_blocks = window ? (min(sinks, s.low) + KEYS - 1) / KEYS : 0;
+  s.low = window ? (p0 >= window ? p0 - window + 1 : 0) & ~15 : 0;
+  s.sinks = min(sinks, s.low);
+  s.sink_blocks = (s.sinks + KEYS - 1) / KEYS;
   s.blocks = p1 < 0 ? 0 : s.sink_blocks + (p1 - s.low) / KEYS + 1;
   return s;
 }
@@ -399,9 +401,9 @@ constexpr float RISE = 8.f;
 __device__ __forceinline__ float base_of(float m) { return m == -__builtin_inff() ? 0.f : m; }
 __device__ __forceinline__ float inverse(float sum) { return sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum); }  // (nothing seen: 0)
 
-// Whether the token at position p sees key j.
+// Whether the token at position p sees key j.  (No branches: a mask per element.)
 __device__ __forceinline__ bool sees(int32_t p, int32_t j, int32_t window, int32_t sinks) {
-  return j <= p && (window == 0 || p - j < window || j < sinks);
+  return (j <= p) & ((window == 0) | (p - j < window) | (j < sinks));
 }
 
 // Values that some rows of a unit see and others do not must not reach the others, whatever they are; finite ones do not (their
@@ -472,7 +474,9 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, const SK_CONSTANT 
   const Step &st = u.step;
   const int32_t row0 = u.block * ROWS_FEW, rows = min(ROWS_FEW, st.fresh * P.group - row0);
   const int32_t p0 = st.behind + row0 / P.group, p1 = st.behind + (row0 + rows - 1) / P.group;
-  const Span span = span_of<KEYS_FEW>(p0, p1, P.window, P.sinks);
+  const int32_t window = P.window, sinks = P.sinks;
+  const Span span = span_of<KEYS_FEW>(p0, p1, window, sinks);
+  const bool two_spans = window && sinks > span.low;  // a row may see two runs of keys in a block
   const int32_t b0 = (int32_t)((int64_t)span.blocks * u.split / u.splits), b1 = (int32_t)((int64_t)span.blocks * (u.split + 1) / u.splits);
 
   const Pages pages{P.table + (int64_t)u.seq * P.columns, P.page_shift, P.num_pages, P.columns, P.page_stride, P.token_stride};
@@ -550,8 +554,9 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, const SK_CONSTANT 
         mma16<DT>(kf[half][k], qf[k], s[half]);
       }
     }
+    const bool sink = b < span.sink_blocks;
     // whether all keys are seen by all rows
-    const bool whole = now == 3 && key0 + KEYS_FEW - 1 <= p0 && (P.window == 0 || p1 - key0 < P.window);
+    const bool whole = now == 3 && (sink ? key0 + KEYS_FEW <= span.sinks : key0 + KEYS_FEW - 1 <= p0 && (window == 0 || p1 - key0 < window));
     if (!whole || P.dim != DP) {
 #pragma unroll
       for (int half = 0; half < 2; ++half)
@@ -560,9 +565,9 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, const SK_CONSTANT 
           const int n = i * 64 + lane;
           const int32_t j = key0 + 16 * half + n / PR;
           // values that no row sees: what lies there may be anything
-          const bool ok = (now >> half & 1) && n % PR * 8 < P.dim && j <= p1 && (P.window == 0 || p0 - j < P.window || j < P.sinks);
+          const bool ok = (now >> half & 1) && n % PR * 8 < P.dim && (sink ? j < span.sinks : j <= p1 && (window == 0 || p0 - j < window || j < sinks));
           if (!ok) vf[half][i] = u32x4{0u, 0u, 0u, 0u};
-          if (!whole && p0 != p1) cleaned |= clean<DT>(vf[half][i]);
+          if (!whole && !sink && p0 != p1) cleaned |= clean<DT>(vf[half][i]);
         }
     }
 #pragma unroll
@@ -578,11 +583,22 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, const SK_CONSTANT 
     }
     // lane (g, c) has the scores of row c and keys key0 + 16 half + 4 g + i
     if (!whole) {
+      if (now == 3 && !two_spans) {
+        const uint32_t last = (uint32_t)((sink ? span.sinks - 1 : my_pos) - key0 - 4 * g), width = sink || window == 0 ? 0x7fffffffu : (uint32_t)window - 1;
 #pragma unroll
-      for (int half = 0; half < 2; ++half)
+        for (int half = 0; half < 2; ++half)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (!((now >> half & 1) && sees(my_pos, key0 + 16 * half + 4 * g + i, P.window, P.sinks))) s[half][i] = -__builtin_inff();
+          for (int i = 0; i < 4; ++i) s[half][i] = last - (uint32_t)(16 * half + i) <= width ? s[half][i] : -__builtin_inff();
+      } else {
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int32_t j = key0 + 16 * half + 4 * g + i;
+            const bool ok = ((now >> half & 1) != 0) & sees(sink ? 0x7fffffff : my_pos, j, sink ? 1 : window, sink ? span.sinks : sinks);
+            s[half][i] = ok ? s[half][i] : -__builtin_inff();
+          }
+      }
     }
     float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
     top = max32(max16(top)) * scale;
@@ -612,7 +628,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, const SK_CONSTANT 
   if (__builtin_expect(__ballot(cleaned) != 0, 0)) {
 #pragma unroll
     for (int i = 0; i < NB; ++i)
-      if (16 * i + 4 * g < P.dim) o[i] += odd_sum<DT>(pages, vh + 2 * (16 * i + 4 * g), b0 + wave, b1, 4, key_of, KEYS_FEW, my_pos, P.window, P.sinks);
+      if (16 * i + 4 * g < P.dim) o[i] += odd_sum<DT>(pages, vh + 2 * (16 * i + 4 * g), b0 + wave, b1, 4, key_of, KEYS_FEW, my_pos, window, sinks);
   }
   l = sum32(sum16(l));
 
@@ -731,11 +747,6 @@ __device__ __forceinline__ void dma(__amdgpu_buffer_rsrc_t desc, const uint32_t 
 }
 __device__ __forceinline__ void wait_dma() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
-#ifdef PRIO
-#define SETPRIO(x) __builtin_amdgcn_s_setprio((x) * PRIO)
-#else
-#define SETPRIO(x)
-#endif
 template <int DT, int DP>
 __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT AttnDev &P, const Unit &u, unsigned char *lds, uint32_t *flag) {
   constexpr int64_t SLOT = part_floats(ROWS_MANY, DP <= 128 ? 128 : 256);
@@ -750,6 +761,7 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
   const int32_t row0 = u.block * ROWS_MANY, rows = min(ROWS_MANY, st.fresh * group - row0);
   const int32_t p0 = st.behind + row0 / group, p1 = st.behind + (row0 + rows - 1) / group;
   const Span span = span_of<KEYS>(p0, p1, window, sinks);
+  const bool two_spans = window && sinks > span.low;  // a row may see two runs of keys in a tile
   const int32_t b0 = (int32_t)((int64_t)span.blocks * u.split / u.splits), b1 = (int32_t)((int64_t)span.blocks * (u.split + 1) / u.splits);
 
   const Pages pages{P.table + (int64_t)u.seq * P.columns, P.page_shift, P.num_pages, P.columns, P.page_stride, P.token_stride};
@@ -768,8 +780,11 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
   }
   int32_t page = -1;  // of the wave's keys in the tile that is brought next
   auto look = [&](int32_t b) { page = pages.page_of(key_of(min(b, b1 - 1)) + 16 * block); };
-  // whether every row of the unit sees all keys of a tile alike
-  auto alike = [&](int32_t key0) { return key0 + KEYS - 1 <= p0 && (window == 0 || p1 - key0 < window); };
+  // whether every row of the unit sees all keys of a tile, and whether rows differ in what they see of it
+  auto all_see = [&](int32_t b, int32_t key0) {
+    return b < span.sink_blocks ? key0 + KEYS <= span.sinks : key0 + KEYS - 1 <= p0 && (window == 0 || p1 - key0 < window);
+  };
+  auto differ = [&](int32_t b) { return b >= span.sink_blocks && !all_see(b, key_of(b)); };
   auto bring = [&](int32_t b, int place) {
     const int32_t key0 = key_of(b);
     const bool there = pages.there(page);
@@ -778,7 +793,7 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
     const int records = there ? (int)DMA_OUTSIDE : 0;
     dma<NI>(__builtin_amdgcn_make_buffer_rsrc((void *)(kh + at), 0, records, 0x00020000), ko, to);
     const __amdgpu_buffer_rsrc_t values = __builtin_amdgcn_make_buffer_rsrc((void *)(vh + at), 0, records, 0x00020000);
-    if (alike(key0)) {
+    if (all_see(b, key0)) {
       dma<NI>(values, vo, to + VALUES);
     } else {
       // values that no row sees: what lies there may be anything
@@ -786,7 +801,8 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         const int32_t j = key0 + first_key + i * (64 / SLOTS) + lane / SLOTS;
-        some[i] = j <= p1 && (window == 0 || p0 - j < window || j < sinks) ? vo[i] : DMA_OUTSIDE;
+        const bool ok = b < span.sink_blocks ? j < span.sinks : j <= p1 && (window == 0 || p0 - j < window || j < sinks);
+        some[i] = ok ? vo[i] : DMA_OUTSIDE;
       }
       dma<NI>(values, some, to + VALUES);
     }
@@ -796,7 +812,7 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
   bool cleaned = false;
   auto arrived = [&](int32_t b, int place) {
     wait_dma();
-    if (!alike(key_of(b))) {
+    if (differ(b)) {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         u32x4 *p = (u32x4 *)(lds + place * TILE + VALUES + wave * NI * 1024 + i * 1024 + 16 * lane);
@@ -853,11 +869,12 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
     }
     const int32_t key0 = key_of(b);
     // whether any row of the wave sees any of these keys, and whether all see all
-    const bool use = wave_ok && key0 <= w1 && (window == 0 || w0 - (key0 + KEYS - 1) < window || key0 < sinks);
+    const bool sink = b < span.sink_blocks;
+    const bool use = wave_ok && (sink || (key0 <= w1 && (window == 0 || w0 - (key0 + KEYS - 1) < window || key0 < sinks)));
     if (use) {
       constexpr uint32_t ALL = 0x01010101u;
       const uint32_t now = __builtin_amdgcn_readfirstlane(*(const uint32_t *)(lds + ManyLds<DP>::PRESENT + 4 * PLACE));
-      const bool whole = now == ALL && key0 + KEYS - 1 <= w0 && (window == 0 || w1 - key0 < window);
+      const bool whole = now == ALL && (sink ? key0 + KEYS <= span.sinks : key0 + KEYS - 1 <= w0 && (window == 0 || w1 - key0 < window));
       f32x16 s[HALVES];
 #pragma unroll
       for (int half = 0; half < HALVES; ++half)
@@ -871,7 +888,6 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
           for (int i = 0; i < G; ++i) f[i] = *(const u32x4 *)(ka[(n + i) % KS] + PLACE * TILE + (n + i) / KS * 32 * KR::BYTES);
         };
         read(0, kf[0]);
-        SETPRIO(1);
         fixed_order();
 #pragma unroll
         for (int n = 0; n < N; n += G) {
@@ -881,17 +897,26 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
           for (int i = 0; i < G; ++i) mma32<DT>(kf[n / G & 1][i], qf[(n + i) % KS], s[(n + i) / KS]);
           fixed_order();
         }
-        SETPRIO(0);
       }
       // lane (h, c) has the scores of row c and keys key0 + 32 half + 8 (i / 4) + 4 h + i % 4
       if (!whole) {
+        if (now == ALL && !two_spans) {
+          // keys key0 + e up to `last`, and no more than `width` before it
+          const uint32_t last = (uint32_t)((sink ? span.sinks - 1 : my_pos) - key0 - 4 * h), width = sink || window == 0 ? 0x7fffffffu : (uint32_t)window - 1;
 #pragma unroll
-        for (int half = 0; half < HALVES; ++half)
+          for (int half = 0; half < HALVES; ++half)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int32_t key = 32 * half + 8 * (i / 4), j = key0 + key + 4 * h + i % 4;
-            if (!((now >> (8 * (key / ROWS)) & 1) && sees(my_pos, j, window, sinks))) s[half][i] = -__builtin_inff();
-          }
+            for (int i = 0; i < 16; ++i) s[half][i] = last - (uint32_t)(32 * half + 8 * (i / 4) + i % 4) <= width ? s[half][i] : -__builtin_inff();
+        } else {
+#pragma unroll
+          for (int half = 0; half < HALVES; ++half)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int32_t key = 32 * half + 8 * (i / 4), j = key0 + key + 4 * h + i % 4;
+              const bool ok = ((now >> (8 * (key / ROWS)) & 1) != 0) & sees(sink ? 0x7fffffff : my_pos, j, sink ? 1 : window, sink ? span.sinks : sinks);
+              s[half][i] = ok ? s[half][i] : -__builtin_inff();
+            }
+        }
       }
       float top = -__builtin_inff();
 #pragma unroll
@@ -932,7 +957,6 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
           }
         };
         read(0, vf[0]);
-        SETPRIO(1);
         fixed_order();
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
@@ -942,7 +966,6 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
           for (int t = 0; t < G; ++t) mma32<DT>(vf[i & 1][t], pf[t], o[i]);
           fixed_order();
         }
-        SETPRIO(0);
       }
     }
     if (b + 1 < b1) arrived(b + 1, 1 - PLACE);
