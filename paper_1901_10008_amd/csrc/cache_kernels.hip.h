@@ -709,10 +709,20 @@ struct KeyRows {
     return row * BYTES + (byte ^ (turn << 4));
   }
 };
+// And one that holds a key's values: 64 bytes turned over with the row, so that the four rows of which half a wave reads 64 bytes each
+// (transposing) lie in different banks.
+template <int DP>
+struct TileValueRows {
+  static constexpr int BYTES = KeyRows<DP>::BYTES;
+  static __device__ __forceinline__ int at(int row, int byte) {
+    const int turn = BYTES == 128 ? (row >> 1) & 1 : row & 3;
+    return row * BYTES + (byte ^ (turn << 6));
+  }
+};
 // Two tiles of keys and values in LDS in turn, behind them which blocks of 16 keys of each are there, and whether values were taken out.
 template <int DP>
 struct ManyLds {
-  static constexpr int TILE = keys_many(DP) * (KeyRows<DP>::BYTES + ValueRows<DP>::BYTES), PRESENT = 2 * TILE, ODD = PRESENT + 8, BYTES = ODD + 8;
+  static constexpr int TILE = keys_many(DP) * (KeyRows<DP>::BYTES + TileValueRows<DP>::BYTES), PRESENT = 2 * TILE, ODD = PRESENT + 8, BYTES = ODD + 8;
 };
 
 // Matrix instructions whose LDS operands are read a group ahead.  (Left alone the scheduler puts every read right above its use, and a wave
@@ -747,11 +757,13 @@ __device__ __forceinline__ void dma(__amdgpu_buffer_rsrc_t desc, const uint32_t 
 }
 __device__ __forceinline__ void wait_dma() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
+constexpr int SETS = 3;  // groups of LDS operands in registers: one in use, two on their way
+
 template <int DT, int DP>
 __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT AttnDev &P, const Unit &u, unsigned char *lds, uint32_t *flag) {
   constexpr int64_t SLOT = part_floats(ROWS_MANY, DP <= 128 ? 128 : 256);
   using KR = KeyRows<DP>;
-  using VR = ValueRows<DP>;
+  using VR = TileValueRows<DP>;
   constexpr int KEYS = keys_many(DP), HALVES = KEYS / 32, KS = DP / 16, NB = DP / 32, TILE = ManyLds<DP>::TILE, VALUES = KEYS * KR::BYTES;
   // a wave brings NI KB of keys and as much of values: ROWS consecutive keys, which lie in one block of 16
   constexpr int NI = KEYS * KR::BYTES / 4096, SLOTS = KR::BYTES / 16, ROWS = KEYS / 4;
@@ -778,22 +790,24 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
     ko[i] = ke < dim ? at + 2 * ke : DMA_OUTSIDE;
     vo[i] = ve < dim ? at + 2 * ve : DMA_OUTSIDE;
   }
-  int32_t page = -1;  // of the wave's keys in the tile that is brought next
-  auto look = [&](int32_t b) { page = pages.page_of(key_of(min(b, b1 - 1)) + 16 * block); };
-  // whether every row of the unit sees all keys of a tile, and whether rows differ in what they see of it
-  auto all_see = [&](int32_t b, int32_t key0) {
-    return b < span.sink_blocks ? key0 + KEYS <= span.sinks : key0 + KEYS - 1 <= p0 && (window == 0 || p1 - key0 < window);
-  };
-  auto differ = [&](int32_t b) { return b >= span.sink_blocks && !all_see(b, key_of(b)); };
+  // Tiles f0 .. f0 + nf - 1: every row of the unit sees all of their keys.  What is decided for the others tile by tile is settled for these.
+  const int32_t f0 = span.sink_blocks + (window && p1 - window >= span.low ? (p1 - window - span.low) / KEYS + 1 : 0);
+  const int32_t f1 = span.sink_blocks + (p0 - span.low >= KEYS - 1 ? (p0 - span.low - (KEYS - 1)) / KEYS + 1 : 0);
+  const uint32_t nf = (uint32_t)max(f1 - f0, 0);
+  auto all_see = [&](int32_t b) { return (uint32_t)(b - f0) < nf; };
+  int32_t next_key = key_of(b0), page = -1;  // first key of the tile that is brought next, and the page of the wave's keys in it
+  auto look = [&]() { page = pages.page_of(next_key + 16 * block); };
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds + wave * NI * 1024;
+  uint32_t gone = 0;  // places where the wave's keys are not there
   auto bring = [&](int32_t b, int place) {
-    const int32_t key0 = key_of(b);
+    const int32_t key0 = next_key;
     const bool there = pages.there(page);
     const int64_t at = pages.bytes(page, key0 + 16 * block) - DMA_FRONT;
-    const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)(lds + place * TILE + wave * NI * 1024);
+    const uint32_t to = lds0 + place * TILE;
     const int records = there ? (int)DMA_OUTSIDE : 0;
     dma<NI>(__builtin_amdgcn_make_buffer_rsrc((void *)(kh + at), 0, records, 0x00020000), ko, to);
     const __amdgpu_buffer_rsrc_t values = __builtin_amdgcn_make_buffer_rsrc((void *)(vh + at), 0, records, 0x00020000);
-    if (all_see(b, key0)) {
+    if (all_see(b)) {
       dma<NI>(values, vo, to + VALUES);
     } else {
       // values that no row sees: what lies there may be anything
@@ -801,18 +815,22 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         const int32_t j = key0 + first_key + i * (64 / SLOTS) + lane / SLOTS;
-        const bool ok = b < span.sink_blocks ? j < span.sinks : j <= p1 && (window == 0 || p0 - j < window || j < sinks);
+        const bool ok = b < span.sink_blocks ? j < span.sinks : (j <= p1) & ((window == 0) | (p0 - j < window) | (j < sinks));
         some[i] = ok ? vo[i] : DMA_OUTSIDE;
       }
       dma<NI>(values, some, to + VALUES);
     }
-    if (lane == 0) lds[ManyLds<DP>::PRESENT + 4 * place + wave] = there;
+    if (there == ((gone >> place & 1) != 0)) {
+      gone ^= 1u << place;
+      lds[ManyLds<DP>::PRESENT + 4 * place + wave] = there;
+    }
+    next_key = b + 1 == span.sink_blocks ? span.low : key0 + KEYS;
   };
   // Behind bring(b): the wave's pieces are there; values that are not finite are taken out where rows differ in what they see.
   bool cleaned = false;
   auto arrived = [&](int32_t b, int place) {
     wait_dma();
-    if (differ(b)) {
+    if (!all_see(b) && b >= span.sink_blocks) {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         u32x4 *p = (u32x4 *)(lds + place * TILE + VALUES + wave * NI * 1024 + i * 1024 + 16 * lane);
@@ -824,10 +842,12 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
       }
     }
   };
+  if (tid < 2) ((uint32_t *)(lds + ManyLds<DP>::PRESENT))[tid] = 0x01010101u;
+  __syncthreads();
   if (b0 < b1) {
-    look(b0);
+    look();
     bring(b0, 0);
-    look(b0 + 1);
+    look();
   }
 
   const int32_t in_block = wave * 32 + c;
@@ -861,40 +881,47 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
   if (tid == 0) *odd = 0;
   if (b0 < b1) arrived(b0, 0);
   __syncthreads();
+  int32_t this_key = key_of(b0);
   auto step = [&](int32_t b, auto which) {
     constexpr int PLACE = decltype(which)::value;
     if (b + 1 < b1) {  // into the other place, which all waves have left behind the last barrier
       bring(b + 1, 1 - PLACE);
-      look(b + 2);
+      look();
     }
-    const int32_t key0 = key_of(b);
+    const int32_t key0 = this_key;
+    this_key = b + 1 == span.sink_blocks ? span.low : key0 + KEYS;
     // whether any row of the wave sees any of these keys, and whether all see all
     const bool sink = b < span.sink_blocks;
-    const bool use = wave_ok && (sink || (key0 <= w1 && (window == 0 || w0 - (key0 + KEYS - 1) < window || key0 < sinks)));
+    bool use = true, all = true;
+    if (!all_see(b)) {
+      use = wave_ok && (sink || (key0 <= w1 && (window == 0 || w0 - (key0 + KEYS - 1) < window || key0 < sinks)));
+      all = sink ? key0 + KEYS <= span.sinks : key0 + KEYS - 1 <= w0 && (window == 0 || w1 - key0 < window);
+    }
     if (use) {
       constexpr uint32_t ALL = 0x01010101u;
       const uint32_t now = __builtin_amdgcn_readfirstlane(*(const uint32_t *)(lds + ManyLds<DP>::PRESENT + 4 * PLACE));
-      const bool whole = now == ALL && (sink ? key0 + KEYS <= span.sinks : key0 + KEYS - 1 <= w0 && (window == 0 || w1 - key0 < window));
+      const bool whole = all && now == ALL;
       f32x16 s[HALVES];
 #pragma unroll
       for (int half = 0; half < HALVES; ++half)
 #pragma unroll
         for (int j = 0; j < 16; ++j) s[half][j] = 0.f;
       {
-        constexpr int N = HALVES * KS, G = KS % 4 == 0 ? 4 : 2;
-        u32x4 kf[2][G];
-        auto read = [&](int n, u32x4 (&f)[G]) {
+        constexpr int N = HALVES * KS / 4;  // groups of four
+        u32x4 kf[SETS][4];
+        auto read = [&](int n) {
 #pragma unroll
-          for (int i = 0; i < G; ++i) f[i] = *(const u32x4 *)(ka[(n + i) % KS] + PLACE * TILE + (n + i) / KS * 32 * KR::BYTES);
+          for (int i = 0; i < 4; ++i) kf[n % SETS][i] = *(const u32x4 *)(ka[(4 * n + i) % KS] + PLACE * TILE + (4 * n + i) / KS * 32 * KR::BYTES);
         };
-        read(0, kf[0]);
+#pragma unroll
+        for (int n = 0; n < SETS - 1 && n < N; ++n) read(n);
         fixed_order();
 #pragma unroll
-        for (int n = 0; n < N; n += G) {
-          if (n + G < N) read(n + G, kf[n / G + 1 & 1]);
+        for (int n = 0; n < N; ++n) {
+          if (n + SETS - 1 < N) read(n + SETS - 1);
           fixed_order();
 #pragma unroll
-          for (int i = 0; i < G; ++i) mma32<DT>(kf[n / G & 1][i], qf[(n + i) % KS], s[(n + i) / KS]);
+          for (int i = 0; i < 4; ++i) mma32<DT>(kf[n % SETS][i], qf[(4 * n + i) % KS], s[(4 * n + i) / KS]);
           fixed_order();
         }
       }
@@ -947,23 +974,24 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
       }
       {
         constexpr int G = 2 * HALVES;  // of a block of 32 elements: all its keys
-        u32x4 vf[2][G];
-        auto read = [&](int i, u32x4 (&f)[G]) {
+        u32x4 vf[SETS][G];
+        auto read = [&](int i) {
 #pragma unroll
           for (int t = 0; t < G; ++t) {
             const unsigned char *p = va[i] + PLACE * TILE + 16 * t * VR::BYTES;
             const u32x2 x = read_transposed(p), y = read_transposed(p + 8 * VR::BYTES);
-            f[t] = u32x4{x.x, x.y, y.x, y.y};
+            vf[i % SETS][t] = u32x4{x.x, x.y, y.x, y.y};
           }
         };
-        read(0, vf[0]);
+#pragma unroll
+        for (int i = 0; i < SETS - 1 && i < NB; ++i) read(i);
         fixed_order();
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
-          if (i + 1 < NB) read(i + 1, vf[i + 1 & 1]);
+          if (i + SETS - 1 < NB) read(i + SETS - 1);
           fixed_order();
 #pragma unroll
-          for (int t = 0; t < G; ++t) mma32<DT>(vf[i & 1][t], pf[t], o[i]);
+          for (int t = 0; t < G; ++t) mma32<DT>(vf[i % SETS][t], pf[t], o[i]);
           fixed_order();
         }
       }
