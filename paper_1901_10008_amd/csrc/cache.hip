@@ -278,13 +278,13 @@ sk_status sk_attn_launch(sk_attn_plan *plan, void *hip_stream) {
       a.problems = plan->problems;
       a.seqs = plan->seqs + g.first_seq;
       a.sequences = (int32_t)g.sequences;
-      a.grid_many = (uint32_t)g.grid_many;
-      a.grid_few = (uint32_t)g.grid_few;
+      a.slots_many = (uint32_t)g.slots_many;
+      a.slots_few = (uint32_t)g.slots_few;
       a.workgroups = (int32_t)g.workgroups;
       a.ws_many = plan->workspace;
-      a.ws_few = plan->workspace + g.grid_many * sk::part_floats(sk::ROWS_MANY, g.wide ? 256 : 128);
+      a.ws_few = plan->workspace + g.slots_many * sk::part_floats(sk::ROWS_MANY, g.wide ? 256 : 128);
       a.arrivals = plan->arrivals;
-      st = launch(attend_kernel(g), g.grid_many + g.grid_few, stream, &g == &plan->host.groups.back() ? behind : nullptr, a);
+      st = launch(attend_kernel(g), g.grid, stream, &g == &plan->host.groups.back() ? behind : nullptr, a);
       if (st != SK_OK) break;
     }
     plan->ledger.after_launch((uintptr_t)stream, in_capture, behind && st == SK_OK);  // also after a failure: some launches may be out

@@ -46,11 +46,12 @@ struct AttnSeq {
 struct AttnGroup {
   bool wide, many;              // larger heads; units of many rows are possible
   int64_t first_seq, sequences; // in the plan's list
-  int64_t grid_many, grid_few;  // workgroups: at least as many as there can be units, and some for splitting
   int64_t workgroups;           // that the device runs at a time
+  int64_t grid;                 // of the launch: the most units there can be, and that many for slices
+  int64_t slots_many, slots_few;  // places of the workspace: as many as there can be units and slices of either kind
 };
 // Workgroups of a kernel that a compute unit holds (its registers and LDS).
-constexpr int resident(bool wide, bool many) { return wide ? 1 : 2; }
+constexpr int resident(bool wide, bool many) { return wide ? 1 : many ? 2 : 3; }
 
 struct AttnPlanHost {
   std::vector<AttnDev> problems;

@@ -137,7 +137,7 @@ __device__ __forceinline__ f32x2 load_shared(const float *p) {
 // ---------------------------------------------------------------------------
 // The lengths are in device memory, so the units (a block of rows of a key-value head of a sequence, and a slice of its
 // keys) are counted on the device: every workgroup looks at all sequences of the launch and finds its own unit from the sums
-// before it.  Units of many rows come first, those of late rows (which see the most) before those of early ones; key-value heads
+// before it; workgroups beyond the last leave.  Units of many rows come first, those of late rows (which see the most) before those of early ones; key-value heads
 // vary fastest, so that with eight of them each has a die (and its L2) of its own.
 
 // A sequence in this step: rows and lengths cut to the bounds that the grid was made for.
@@ -200,7 +200,7 @@ struct Unit {
   uint32_t slot;                // this workgroup's place in the workspace
   uint32_t first_slot;          // of the unit's first slice: also its arrival counter
   Step step;
-  bool any;
+  bool many, any;
 };
 
 struct AttnArgs {
@@ -208,29 +208,25 @@ struct AttnArgs {
   const AttnSeq *seqs;
   int32_t sequences;
   int32_t workgroups;  // that the card runs at a time
-  uint32_t grid_many, grid_few;
+  uint32_t slots_many, slots_few;  // places of the workspace for slices of either kind
   float *ws_many, *ws_few;
-  uint32_t *arrivals;  // grid_many + grid_few, zero between launches
+  uint32_t *arrivals;  // slots_many, then as many as there are for few; zero between launches
 };
 
-// How many blocks of keys a slice takes so that all slices fit `grid` workgroups: ceil(blocks / that) over the units adds up to
-// total / that + units at most.  No unit is split where the units alone do not leave room.
-__device__ __forceinline__ int32_t blocks_per_slice(int64_t total, int64_t units, int64_t grid, int64_t workgroups, int32_t least) {
-  // One round of workgroups where the units leave room for it, else as many as the grid has.
-  if (2 * units <= workgroups) grid = min(grid, workgroups);
-  if (units >= grid) return 0x7fffffff;
-  const int64_t per = (total + (grid - units) - 1) / (grid - units);
-  return (int32_t)min(max(per, (int64_t)least), (int64_t)0x7fffffff);
+// Units of many keys are cut into slices, so that few units fill the card and no unit is what the launch waits for.  A slice takes at most `most`
+// blocks of keys of few rows, or half as many tiles of many (which take twice as long).
+constexpr int LEAST = 4;  // a block for each wave; tiles
+__device__ __forceinline__ int32_t splits_of(const Count &c, int32_t most) {
+  const int32_t per = max(c.many ? (most + 1) / 2 : most, LEAST);
+  return min((int32_t)(((int64_t)max(c.blocks, 1) + per - 1) / per), MOST_SPLITS);
 }
-__device__ __forceinline__ int32_t splits_of(int32_t blocks, int32_t per) {
-  return min(max((int32_t)(((int64_t)blocks + per - 1) / per), 1), MOST_SPLITS);
-}
-constexpr int LEAST_FEW = 4;   // a block of keys for each wave
-constexpr int LEAST_MANY = 4;
+// work: blocks of few rows and twice the tiles of many.  That many for each workgroup the card runs at a time: with it all slices
+// are no more than these workgroups and the units together.
+__device__ __forceinline__ int32_t even_share(int64_t work, int64_t workgroups) { return (int32_t)min((work + workgroups - 1) / workgroups, (int64_t)0x7ffffffe); }
 
 struct FindScratch {
-  int64_t total[2][4];  // blocks of keys over all units (many, few), per wave
-  int32_t units[2][4], items[2][4];
+  int64_t work[4];  // per wave
+  int32_t units[4], items[2][4];
   Unit unit;
 };
 
@@ -247,6 +243,7 @@ __device__ __forceinline__ Unit unit_of(const AttnSeq &q, const Step &s, const C
   u.slot = item;
   u.first_slot = item - (uint32_t)(u.split * q.kv_heads);
   u.step = s;
+  u.many = c.many;
   u.any = true;
   return u;
 }
@@ -264,16 +261,16 @@ __device__ __forceinline__ Unit unit_in_lane(const Unit &u, int lane) {
   r.step.fresh = lane_of(u.step.fresh, lane);
   r.step.length = lane_of(u.step.length, lane);
   r.step.behind = lane_of(u.step.behind, lane);
+  r.many = lane_of((int32_t)u.many, lane) != 0;
   r.any = true;
   return r;
 }
 
-// MANY: units of many rows may be there.  Workgroups below grid_many take them, the others those of few.
+// The unit, or slice of one, that a workgroup takes: those of many rows first.  MANY: there may be such.
 template <bool MANY, bool WIDE>
 __device__ __forceinline__ Unit find_unit(const AttnArgs &a, FindScratch *f) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const bool many = MANY && blockIdx.x < a.grid_many;
-  const int32_t item = (int32_t)(many ? blockIdx.x : blockIdx.x - a.grid_many);
+  int32_t item = (int32_t)blockIdx.x;
   if (a.sequences <= 64) {
     // a sequence per lane, every wave for itself
     AttnSeq q{};
@@ -285,65 +282,93 @@ __device__ __forceinline__ Unit find_unit(const AttnArgs &a, FindScratch *f) {
       s = step_of(q);
       c = count_units<MANY, WIDE>(s, q.kv_heads, q.group, q.window, q.sinks);
     }
-    const bool ours = c.many == many;
-    const int32_t units = ours ? c.units : 0;
-    const int64_t all_blocks = lane_of(wave_scan((int64_t)units * c.blocks), 63);
-    const int32_t all_units = lane_of(wave_scan(units), 63);
-    const int32_t per = blocks_per_slice(all_blocks, all_units, many ? a.grid_many : a.grid_few, a.workgroups, many ? LEAST_MANY : LEAST_FEW);
-    const int32_t splits = splits_of(c.blocks, per), n = units * splits, upto = wave_scan(n);
-    const uint64_t hit = __ballot(item >= upto - n && item < upto);
+    const int32_t units = lane_of(wave_scan(c.units), 63);
+    const int64_t work = lane_of(wave_scan((int64_t)c.units * c.blocks * (c.many ? 2 : 1)), 63);
+    int32_t most = even_share(work, a.workgroups), splits = splits_of(c, most);
+    // Few units: slices as short as leaves all of them running at once.  (A slice costs its workgroup 5 us besides the keys: six caches
+    // of 50 to 120 thousand tokens take 271 us in one round of slices, 281 in two, 288 in four.)
+    for (int i = 0; i < 8 && 2 * units <= a.workgroups && lane_of(wave_scan(c.units * splits), 63) > a.workgroups; ++i) {
+      most += most / 8 + 1;
+      splits = splits_of(c, most);
+    }
+    int32_t n, n_many, upto_many, all_many, upto_few;
+    auto sums = [&]() {
+      n = c.units * splits, n_many = MANY && c.many ? n : 0;
+      upto_many = MANY ? wave_scan(n_many) : 0, all_many = MANY ? lane_of(upto_many, 63) : 0, upto_few = wave_scan(n - n_many);
+    };
+    sums();
+    if (all_many > (int32_t)a.slots_many || lane_of(upto_few, 63) > (int32_t)a.slots_few) {  // (a first_row that decreases: no slices, no places needed)
+      splits = 1;
+      sums();
+    }
+    const bool many = MANY && item < all_many;
+    if (!many) item -= all_many;
+    const int32_t upto = many ? upto_many : upto_few, mine = c.many == many ? n : 0;
+    const uint64_t hit = __ballot(item >= upto - mine && item < upto);
     Unit u{};
     u.any = hit != 0;
     if (!u.any) return u;
     const int who = __builtin_ctzll(hit);
-    return unit_in_lane(unit_of(q, s, c, splits, item - (upto - n), (uint32_t)item), who);
+    return unit_in_lane(unit_of(q, s, c, splits, item - (upto - mine), (uint32_t)item), who);
   }
   // a run of sequences per thread
   const int per_thread = (a.sequences + CACHE_THREADS - 1) / CACHE_THREADS;
   const int s0 = tid * per_thread, s1 = min(s0 + per_thread, a.sequences);
-  auto look = [&](int i, AttnSeq &q, Step &s) {
-    q = a.seqs[i];
-    s = step_of(q);
-    return count_units<MANY, WIDE>(s, q.kv_heads, q.group, q.window, q.sinks);
-  };
   AttnSeq q{};
   Step s{};
   Count c{0, 0, false};
-  int64_t total = 0;
-  int32_t units = 0;
+  auto look = [&](int i) {
+    q = a.seqs[i];
+    s = step_of(q);
+    c = count_units<MANY, WIDE>(s, q.kv_heads, q.group, q.window, q.sinks);
+  };
+  int64_t work = 0;
   for (int i = s0; i < s1; ++i) {
-    c = look(i, q, s);
-    if (c.many != many) continue;
-    total += (int64_t)c.units * c.blocks;
-    units += c.units;
+    look(i);
+    work += (int64_t)c.units * c.blocks * (c.many ? 2 : 1);
   }
-  total = lane_of(wave_scan(total), 63);
-  units = lane_of(wave_scan(units), 63);
-  if (lane == 0) {
-    f->total[0][wave] = total;
-    f->units[0][wave] = units;
-  }
+  work = lane_of(wave_scan(work), 63);
+  if (lane == 0) f->work[wave] = work;
   if (tid == 0) f->unit.any = false;
   __syncthreads();
-  total = f->total[0][0] + f->total[0][1] + f->total[0][2] + f->total[0][3];
-  const int64_t all_units = (int64_t)f->units[0][0] + f->units[0][1] + f->units[0][2] + f->units[0][3];
-  const int32_t per = blocks_per_slice(total, all_units, many ? a.grid_many : a.grid_few, a.workgroups, many ? LEAST_MANY : LEAST_FEW);
-  int32_t n = 0;
-  for (int i = s0; i < s1; ++i) {
-    if (per_thread > 1) c = look(i, q, s);
-    if (c.many == many) n += c.units * splits_of(c.blocks, per);
+  int32_t most = even_share(f->work[0] + f->work[1] + f->work[2] + f->work[3], a.workgroups);
+  int32_t n_many, n_few, upto_many, upto_few, all_many;
+  for (int round = 0; round < 2; ++round) {
+    n_many = n_few = 0;
+    for (int i = s0; i < s1; ++i) {
+      if (per_thread > 1) look(i);
+      const int32_t n = c.units * splits_of(c, most);
+      n_many += MANY && c.many ? n : 0;
+      n_few += MANY && c.many ? 0 : n;
+    }
+    upto_many = MANY ? wave_scan(n_many) : 0, upto_few = wave_scan(n_few);
+    if (lane == 63) {
+      f->items[0][wave] = upto_many;
+      f->items[1][wave] = upto_few;
+    }
+    __syncthreads();
+    all_many = 0;
+    int32_t all_few = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      all_many += MANY ? f->items[0][w] : 0;
+      all_few += f->items[1][w];
+    }
+    if (all_many <= (int32_t)a.slots_many && all_few <= (int32_t)a.slots_few) break;
+    most = 0x7ffffffe;  // (a first_row that decreases: no slices, no places needed)
+    __syncthreads();
   }
-  const int32_t upto = wave_scan(n);
-  if (lane == 63) f->items[0][wave] = upto;
-  __syncthreads();
-  int32_t before = upto - n;
-  for (int w = 0; w < wave; ++w) before += f->items[0][w];
-  if (item >= before && item < before + n) {
+  const bool many = MANY && item < all_many;
+  if (!many) item -= all_many;
+  const int32_t mine = many ? n_many : n_few;
+  int32_t before = (many ? upto_many : upto_few) - mine;
+  for (int w = 0; w < wave; ++w) before += f->items[many ? 0 : 1][w];
+  if (item >= before && item < before + mine) {
     int32_t at = before;
     for (int i = s0; i < s1; ++i) {
-      if (per_thread > 1) c = look(i, q, s);
+      if (per_thread > 1) look(i);
       if (c.many != many) continue;
-      const int32_t splits = splits_of(c.blocks, per), here = c.units * splits;
+      const int32_t splits = splits_of(c, most), here = c.units * splits;
       if (item < at + here) {
         f->unit = unit_of(q, s, c, splits, item - at, (uint32_t)item);
         break;
@@ -458,6 +483,42 @@ struct ValueRows {
   }
 };
 
+// Nothing moves across.  Matrix instructions whose LDS operands are to be read a group ahead need it: left alone the scheduler puts every read
+// right above its use, and a wave waits out the way to LDS and back each time.
+__device__ __forceinline__ void fixed_order() { __builtin_amdgcn_sched_barrier(0); }
+
+// N pieces of 16 bytes a lane from memory into LDS: lane i's arrive at lds_addr + 1024 n + 16 i.  The instruction's own offset counts on both
+// sides, so the lanes' offsets are lowered by as much and the descriptor begins DMA_FRONT bytes in front.  What lies outside the descriptor
+// arrives as zeros.  In one statement, opened with the wait states that scalar registers written by vector instructions want before a memory
+// instruction reads them; the compiler does not know of the loads, so they are waited for by hand (wait_dma).
+constexpr int DMA_FRONT = 3072;
+constexpr uint32_t DMA_OUTSIDE = 0x80000000u;
+template <int N>
+__device__ __forceinline__ void dma(__amdgpu_buffer_rsrc_t desc, const uint32_t (&at)[N], uint32_t lds_addr) {
+  static_assert(N == 2 || N == 4, "written out for these");
+  if constexpr (N == 4)
+    asm volatile("s_nop 4\n\t"
+                 "buffer_load_dwordx4 %0, %4, 0 offen lds\n\t"
+                 "buffer_load_dwordx4 %1, %4, 0 offen offset:1024 lds\n\t"
+                 "buffer_load_dwordx4 %2, %4, 0 offen offset:2048 lds\n\t"
+                 "buffer_load_dwordx4 %3, %4, 0 offen offset:3072 lds"
+                 :
+                 : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "s"(desc), "{m0}"(lds_addr)
+                 : "memory");
+  else
+    asm volatile("s_nop 4\n\t"
+                 "buffer_load_dwordx4 %0, %2, 0 offen lds\n\t"
+                 "buffer_load_dwordx4 %1, %2, 0 offen offset:1024 lds"
+                 :
+                 : "v"(at[0]), "v"(at[1]), "s"(desc), "{m0}"(lds_addr)
+                 : "memory");
+}
+// Until all but the last N loads are there.
+template <int N>
+__device__ __forceinline__ void wait_dma() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
 template <int DT>
 __device__ __forceinline__ u32x4 load_query(const void *p, bool ok, bool negate) {
   u32x4 v = load16(ok ? p : (const void *)g_zeros);
@@ -468,13 +529,13 @@ __device__ __forceinline__ u32x4 load_query(const void *p, bool ok, bool negate)
 template <int DT, int DP>
 __device__ __forceinline__ void attend_few(const AttnArgs &a, const SK_CONSTANT AttnDev &P, const Unit &u, unsigned char *lds, uint32_t *flag) {
   constexpr int64_t SLOT = part_floats(ROWS_FEW, DP <= 128 ? 128 : 256);
-  constexpr int KS = DP / 32, NB = DP / 16, PR = DP / 8, VH = PR / 4;  // VH pieces of values per lane and 16 keys
   using VR = ValueRows<DP>;
+  constexpr int KS = DP / 32, NB = DP / 16, SLOTS = VR::BYTES / 16, VH = SLOTS / 4;  // VH KB of values per 16 keys
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
   const Step &st = u.step;
   const int32_t row0 = u.block * ROWS_FEW, rows = min(ROWS_FEW, st.fresh * P.group - row0);
   const int32_t p0 = st.behind + row0 / P.group, p1 = st.behind + (row0 + rows - 1) / P.group;
-  const int32_t window = P.window, sinks = P.sinks;
+  const int32_t window = P.window, sinks = P.sinks, dim = P.dim;
   const Span span = span_of<KEYS_FEW>(p0, p1, window, sinks);
   const bool two_spans = window && sinks > span.low;  // a row may see two runs of keys in a block
   const int32_t b0 = (int32_t)((int64_t)span.blocks * u.split / u.splits), b1 = (int32_t)((int64_t)span.blocks * (u.split + 1) / u.splits);
@@ -482,23 +543,31 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, const SK_CONSTANT 
   const Pages pages{P.table + (int64_t)u.seq * P.columns, P.page_shift, P.num_pages, P.columns, P.page_stride, P.token_stride};
   const char *kh = (const char *)P.k + 2 * (int64_t)u.head * P.head_stride, *vh = (const char *)P.v + 2 * (int64_t)u.head * P.head_stride;
   auto key_of = [&](int32_t b) { return b < span.sink_blocks ? b * KEYS_FEW : span.low + (b - span.sink_blocks) * KEYS_FEW; };
-  // offsets of this lane's pieces of 16 keys; pieces beyond the head's end are read from its start and count as zeros
+  // Offsets of this lane's pieces of 16 keys.  Keys go into registers: pieces beyond the head's end are read from its start and count as zeros.
+  // Values go into LDS (see dma), a wave's to a place of its own: there such pieces come as zeros.
+  constexpr int VI = VH < 4 ? VH : 4;  // loads per statement
   uint32_t ko[KS], vo[VH];
 #pragma unroll
-  for (int s = 0; s < KS; ++s) ko[s] = 2u * (uint32_t)(c * P.token_stride + (32 * s + 8 * g < P.dim ? 32 * s + 8 * g : 0));
+  for (int s = 0; s < KS; ++s) ko[s] = 2u * (uint32_t)(c * P.token_stride + (32 * s + 8 * g < dim ? 32 * s + 8 * g : 0));
 #pragma unroll
   for (int i = 0; i < VH; ++i) {
-    const int n = i * 64 + lane, e = n % PR * 8;
-    vo[i] = 2u * (uint32_t)(n / PR * P.token_stride + (e < P.dim ? e : 0));
+    const int key = i * (64 / SLOTS) + lane / SLOTS, e = (VR::at(key, lane % SLOTS * 16) - key * VR::BYTES) / 2;
+    vo[i] = e < dim ? 2u * (uint32_t)(key * P.token_stride + e) + DMA_FRONT - 1024 * (i % 4) : DMA_OUTSIDE;
   }
-  u32x4 kf[2][KS], vf[2][VH];
+  unsigned char *mine = lds + wave * (KEYS_FEW * VR::BYTES);
+  const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds + wave * (KEYS_FEW * VR::BYTES);
+  u32x4 kf[2][KS];
   int32_t page[2];  // of the block that is loaded next
   auto look = [&](int32_t b) {
     const int32_t key0 = key_of(min(b, b1 - 1));
     page[0] = pages.page_of(key0);
     page[1] = pages.page_of(key0 + 16);
   };
-  auto load = [&](int32_t b) -> uint32_t {  // which halves are there
+  // whether all keys of a block are seen by all rows
+  auto all_see = [&](int32_t b, int32_t key0) {
+    return b < span.sink_blocks ? key0 + KEYS_FEW <= span.sinks : (key0 + KEYS_FEW - 1 <= p0) & ((window == 0) | (p1 - key0 < window));
+  };
+  auto load_keys = [&](int32_t b) {
     const int32_t key0 = key_of(b);
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
@@ -506,18 +575,38 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, const SK_CONSTANT 
 #pragma unroll
       for (int s = 0; s < KS; ++s) kf[half][s] = load16(kb + ko[s]);
     }
+  };
+  auto bring_values = [&](int32_t b, const int32_t (&of)[2]) {
+    const int32_t key0 = key_of(b);
+    const bool whole = all_see(b, key0);
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-      const char *vb = vh + pages.bytes(page[half], key0 + 16 * half);
+      const int64_t at = pages.bytes(of[half], key0 + 16 * half) - DMA_FRONT;
+      const __amdgpu_buffer_rsrc_t values = __builtin_amdgcn_make_buffer_rsrc((void *)(vh + at), 0, pages.there(of[half]) ? (int)DMA_OUTSIDE : 0, 0x00020000);
 #pragma unroll
-      for (int i = 0; i < VH; ++i) vf[half][i] = load16(vb + vo[i]);
+      for (int i = 0; i < VH; i += VI) {
+        uint32_t some[VI];
+#pragma unroll
+        for (int n = 0; n < VI; ++n) some[n] = vo[i + n];
+        if (!whole) {
+          // values that no row sees: what lies there may be anything
+#pragma unroll
+          for (int n = 0; n < VI; ++n) {
+            const int32_t j = key0 + 16 * half + (i + n) * (64 / SLOTS) + lane / SLOTS;
+            const bool ok = b < span.sink_blocks ? j < span.sinks : (j <= p1) & ((window == 0) | (p0 - j < window) | (j < sinks));
+            some[n] = ok ? some[n] : DMA_OUTSIDE;
+          }
+        }
+        dma<VI>(values, some, to + (half * VH + i) * 1024);
+      }
     }
-    return (pages.there(page[0]) ? 1u : 0u) | (pages.there(page[1]) ? 2u : 0u);
   };
-  uint32_t present = 0;
+  int32_t here[2] = {-1, -1};  // pages of the block in hand
   if (b0 + wave < b1) {
     look(b0 + wave);
-    present = load(b0 + wave);
+    here[0] = page[0], here[1] = page[1];
+    load_keys(b0 + wave);
+    bring_values(b0 + wave, here);
     look(b0 + wave + 4);
   }
 
@@ -528,9 +617,8 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, const SK_CONSTANT 
   const float scale = fabsf(P.scale_log2);  // (its sign goes into the queries)
   u32x4 qf[KS];
 #pragma unroll
-  for (int s = 0; s < KS; ++s) qf[s] = load_query<DT>(q + 2 * (32 * s + 8 * g), c < rows && 32 * s + 8 * g < P.dim, P.scale_log2 < 0.f);
+  for (int s = 0; s < KS; ++s) qf[s] = load_query<DT>(q + 2 * (32 * s + 8 * g), c < rows && 32 * s + 8 * g < dim, P.scale_log2 < 0.f);
 
-  unsigned char *mine = lds + wave * (KEYS_FEW * VR::BYTES);
   f32x4 o[NB];
 #pragma unroll
   for (int i = 0; i < NB; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -539,46 +627,25 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, const SK_CONSTANT 
 
   for (int32_t b = b0 + wave; b < b1; b += 4) {
     const int32_t key0 = key_of(b);
-    const uint32_t now = present;
-    if (P.dim != DP) {
+    const uint32_t now = (pages.there(here[0]) ? 1u : 0u) | (pages.there(here[1]) ? 2u : 0u);
+    if (dim != DP) {
 #pragma unroll
       for (int k = 0; k < KS; ++k)
-        if (32 * k + 8 * g >= P.dim) kf[0][k] = kf[1][k] = u32x4{0u, 0u, 0u, 0u};
+        if (32 * k + 8 * g >= dim) kf[0][k] = kf[1][k] = u32x4{0u, 0u, 0u, 0u};
     }
     f32x4 s[2];
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       s[half] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        mma16<DT>(kf[half][k], qf[k], s[half]);
-      }
+      for (int k = 0; k < KS; ++k) mma16<DT>(kf[half][k], qf[k], s[half]);
     }
-    const bool sink = b < span.sink_blocks;
-    // whether all keys are seen by all rows
-    const bool whole = now == 3 && (sink ? key0 + KEYS_FEW <= span.sinks : key0 + KEYS_FEW - 1 <= p0 && (window == 0 || p1 - key0 < window));
-    if (!whole || P.dim != DP) {
-#pragma unroll
-      for (int half = 0; half < 2; ++half)
-#pragma unroll
-        for (int i = 0; i < VH; ++i) {
-          const int n = i * 64 + lane;
-          const int32_t j = key0 + 16 * half + n / PR;
-          // values that no row sees: what lies there may be anything
-          const bool ok = (now >> half & 1) && n % PR * 8 < P.dim && (sink ? j < span.sinks : j <= p1 && (window == 0 || p0 - j < window || j < sinks));
-          if (!ok) vf[half][i] = u32x4{0u, 0u, 0u, 0u};
-          if (!whole && !sink && p0 != p1) cleaned |= clean<DT>(vf[half][i]);
-        }
-    }
-#pragma unroll
-    for (int half = 0; half < 2; ++half)
-#pragma unroll
-      for (int i = 0; i < VH; ++i) {
-        const int n = i * 64 + lane;
-        *(u32x4 *)(mine + VR::at(16 * half + n / PR, n % PR * 16)) = vf[half][i];
-      }
-    if (b + 4 < b1) {
-      present = load(b + 4);
+    const bool sink = b < span.sink_blocks, alike = all_see(b, key0), whole = now == 3 && alike;
+    const bool more = b + 4 < b1;
+    if (more) {
+      here[0] = page[0], here[1] = page[1];
+      load_keys(b + 4);
+      fixed_order();  // (they are counted on below)
       look(b + 8);
     }
     // lane (g, c) has the scores of row c and keys key0 + 16 half + 4 g + i
@@ -617,12 +684,32 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, const SK_CONSTANT 
         s[half][i] = exp2_fast(fmaf(s[half][i], scale, -base));
         l += s[half][i];
       }
+    // this block's values: behind them only the next block's keys are out
+    if (more)
+      wait_dma<2 * KS>();
+    else
+      wait_dma<0>();
+    if (!alike && !sink && p0 != p1) {
+#pragma unroll
+      for (int i = 0; i < 2 * VH; ++i) {
+        u32x4 *p = (u32x4 *)(mine + i * 1024 + 16 * lane);
+        u32x4 v = *p;
+        if (clean<DT>(v)) {
+          *p = v;
+          cleaned = true;
+        }
+      }
+    }
     const u32x4 pf = {pack2<DT>(s[0][0], s[0][1]), pack2<DT>(s[0][2], s[0][3]), pack2<DT>(s[1][0], s[1][1]), pack2<DT>(s[1][2], s[1][3])};
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
       const int byte = 2 * (16 * i + 4 * (c & 3)), row = 4 * g + (c >> 2);
       const u32x2 lo = read_transposed(mine + VR::at(row, byte)), hi = read_transposed(mine + VR::at(row + 16, byte));
       mma16<DT>(u32x4{lo.x, lo.y, hi.x, hi.y}, pf, o[i]);
+    }
+    if (more) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the reads are done before the next values take their place
+      bring_values(b + 4, here);
     }
   }
   if (__builtin_expect(__ballot(cleaned) != 0, 0)) {
@@ -672,7 +759,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, const SK_CONSTANT 
     }
   }
   if (u.splits == 1) return;
-  if (!last_to_arrive(a.arrivals + a.grid_many + u.first_slot, u.splits, flag)) return;
+  if (!last_to_arrive(a.arrivals + a.slots_many + u.first_slot, u.splits, flag)) return;
   // the slices in order: the result does not depend on who came last
   const float *ws0 = a.ws_few + (int64_t)u.first_slot * SLOT;
   const int64_t step = (int64_t)P.kv_heads * SLOT;
@@ -724,38 +811,6 @@ template <int DP>
 struct ManyLds {
   static constexpr int TILE = keys_many(DP) * (KeyRows<DP>::BYTES + TileValueRows<DP>::BYTES), PRESENT = 2 * TILE, ODD = PRESENT + 8, BYTES = ODD + 8;
 };
-
-// Matrix instructions whose LDS operands are read a group ahead.  (Left alone the scheduler puts every read right above its use, and a wave
-// waits out the way to LDS and back each time.)
-__device__ __forceinline__ void fixed_order() { __builtin_amdgcn_sched_barrier(0); }
-
-// N pieces of 16 bytes a lane from memory into LDS: lane i's arrive at lds_addr + 1024 n + 16 i.  The instruction's own offset counts on both
-// sides, so the lanes' offsets are lowered by as much and the descriptor begins DMA_FRONT bytes in front.  What lies outside the descriptor
-// arrives as zeros.  In one statement, opened with the wait states that scalar registers written by vector instructions want before a memory
-// instruction reads them; the compiler does not know of the loads, so they are waited for by hand (wait_dma).
-constexpr int DMA_FRONT = 3072;
-constexpr uint32_t DMA_OUTSIDE = 0x80000000u;
-template <int N>
-__device__ __forceinline__ void dma(__amdgpu_buffer_rsrc_t desc, const uint32_t (&at)[N], uint32_t lds_addr) {
-  static_assert(N == 2 || N == 4, "written out for these");
-  if constexpr (N == 4)
-    asm volatile("s_nop 4\n\t"
-                 "buffer_load_dwordx4 %0, %4, 0 offen lds\n\t"
-                 "buffer_load_dwordx4 %1, %4, 0 offen offset:1024 lds\n\t"
-                 "buffer_load_dwordx4 %2, %4, 0 offen offset:2048 lds\n\t"
-                 "buffer_load_dwordx4 %3, %4, 0 offen offset:3072 lds"
-                 :
-                 : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "s"(desc), "{m0}"(lds_addr)
-                 : "memory");
-  else
-    asm volatile("s_nop 4\n\t"
-                 "buffer_load_dwordx4 %0, %2, 0 offen lds\n\t"
-                 "buffer_load_dwordx4 %1, %2, 0 offen offset:1024 lds"
-                 :
-                 : "v"(at[0]), "v"(at[1]), "s"(desc), "{m0}"(lds_addr)
-                 : "memory");
-}
-__device__ __forceinline__ void wait_dma() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 constexpr int SETS = 3;  // groups of LDS operands in registers: one in use, two on their way
 
@@ -829,7 +884,7 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
   // Behind bring(b): the wave's pieces are there; values that are not finite are taken out where rows differ in what they see.
   bool cleaned = false;
   auto arrived = [&](int32_t b, int place) {
-    wait_dma();
+    wait_dma<0>();
     if (!all_see(b) && b >= span.sink_blocks) {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
@@ -1078,7 +1133,7 @@ struct AttendLds {
 
 template <int DT, int DP, bool MANY>
 __device__ __forceinline__ void attend(const AttnArgs &a, const SK_CONSTANT AttnDev &P, const Unit &u, unsigned char *lds, uint32_t *flag) {
-  if (MANY && blockIdx.x < a.grid_many)
+  if (MANY && u.many)
     attend_many<DT, DP>(a, P, u, lds, flag);
   else
     attend_few<DT, DP>(a, P, u, lds, flag);

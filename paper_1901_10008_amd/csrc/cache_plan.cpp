@@ -159,12 +159,13 @@ sk_status plan_attn(const sk_attn_problem *problems, int32_t n, int32_t compute_
     if (!g.sequences) continue;
     g.many = many > 0;
     g.workgroups = workgroups ? workgroups : (int64_t)resident(g.wide, g.many) * compute_units;
-    g.grid_few = std::min(few + g.workgroups, few_most);
-    g.grid_many = std::min(many + g.workgroups, many_most);
-    if (g.grid_few + g.grid_many >= (int64_t)1 << 31) return refuse(err, SK_ERR_UNSUPPORTED, "more units of work than a launch's grid can hold");
+    g.slots_few = std::min(few + g.workgroups, few_most);
+    g.slots_many = std::min(many + g.workgroups, many_most);
+    g.grid = std::min(few + many + g.workgroups, g.slots_few + g.slots_many);
+    if (g.grid >= (int64_t)1 << 31) return refuse(err, SK_ERR_UNSUPPORTED, "more units of work than a launch's grid can hold");
     const int64_t dim = wide ? 256 : 128;
-    out.workspace_floats = std::max(out.workspace_floats, g.grid_few * part_floats(ROWS_FEW, dim) + g.grid_many * part_floats(ROWS_MANY, dim));
-    out.counters = std::max(out.counters, g.grid_few + g.grid_many);
+    out.workspace_floats = std::max(out.workspace_floats, g.slots_few * part_floats(ROWS_FEW, dim) + g.slots_many * part_floats(ROWS_MANY, dim));
+    out.counters = std::max(out.counters, g.slots_few + g.slots_many);
     out.groups.push_back(g);
   }
   return SK_OK;

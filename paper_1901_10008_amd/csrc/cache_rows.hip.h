@@ -185,7 +185,7 @@ __device__ __forceinline__ void append_row(const SK_CONSTANT AttnDev &P, int32_t
   }
   if (row < a || row >= b) return;
   const int64_t capacity = (int64_t)P.columns << P.page_shift;
-  const int64_t pos = min((int64_t)max(n, 0), capacity) - (min(b, P.rows) - a) + (row - a);
+  const int64_t pos = min((int64_t)max(n, 0), capacity) - min(b, P.rows) + row;  // (below the capacity, whatever first_row holds)
   const int32_t page = pos >= 0 ? load_i32(P.table + (int64_t)seq * P.columns + (pos >> P.page_shift)) : -1;
   const bool there = (uint32_t)page < (uint32_t)P.num_pages;
   const int64_t slot = (int64_t)page * P.page_stride + (pos & ((1 << P.page_shift) - 1)) * P.token_stride;

@@ -64,9 +64,10 @@ static void plans(std::mt19937 &rng) {
         few += (int64_t)q.kv_heads * ((std::min<int64_t>((int64_t)q.group * q.max_new, sk::MOST_FEW) + sk::ROWS_FEW - 1) / sk::ROWS_FEW);
         if ((int64_t)q.max_new * q.group > sk::MOST_FEW && q.seq == 0) many += (int64_t)q.kv_heads * (((int64_t)q.rows * q.group + sk::ROWS_MANY - 1) / sk::ROWS_MANY);
       }
-      need(g.grid_few >= few && g.grid_many >= many, "units without a workgroup");
-      need(h.counters >= g.grid_few + g.grid_many, "counters");
-      need(h.workspace_floats >= g.grid_few * sk::part_floats(sk::ROWS_FEW, g.wide ? 256 : 128) + g.grid_many * sk::part_floats(sk::ROWS_MANY, g.wide ? 256 : 128), "workspace");
+      need(g.grid >= std::max(few, many), "units without a workgroup");
+      need(h.counters >= g.slots_few + g.slots_many, "counters");
+      need(g.grid <= g.slots_few + g.slots_many, "slices without a place");
+      need(h.workspace_floats >= g.slots_few * sk::part_floats(sk::ROWS_FEW, g.wide ? 256 : 128) + g.slots_many * sk::part_floats(sk::ROWS_MANY, g.wide ? 256 : 128), "workspace");
     }
   }
 }

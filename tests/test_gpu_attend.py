@@ -109,6 +109,26 @@ def test_lengths_beyond_the_table_are_cut():
     H.assert_close(t.out()[:3], want[:3], tol[:3])
 
 
+@pytest.mark.parametrize("count", [5, 90])
+def test_rows_out_of_order_stay_inside(count):
+    """first_row that decreases, or points outside: nothing is promised for such a step, but the next one is right."""
+    seqs = ((300, 3), (500, 40), (64, 1), (700, 9), (90, 90)) * (count // 5)
+    t = Tenant("bf16", (4, 2, 64), seqs, seed=12)
+    want, tol = t.attend()
+    problem = t.to_device()
+    g = torch.Generator().manual_seed(count)
+    with sk.sk_attn_plan_create([problem], sk.sk_attn_params_default(workgroups=60)) as plan:
+        for low, high in ((0, t.rows + 1), (-2 ** 31, 2 ** 31 - 1)):
+            t.keep[2].copy_(torch.randint(low, high, (count + 1,), generator=g, dtype=torch.int64).to(torch.int32))
+            sk.sk_attn_launch(plan, H.stream_handle())
+        t.keep[2].copy_(torch.tensor([0, t.rows] * count, dtype=torch.int32)[:count + 1])
+        sk.sk_attn_launch(plan, H.stream_handle())
+        t.keep[2].copy_(t.firsts)
+        sk.sk_attn_launch(plan, H.stream_handle())
+        torch.cuda.synchronize()
+    H.assert_close(t.out(), want, tol)
+
+
 def test_offsets_beyond_32_bits():
     """A cache of 2^32 elements and more for each of keys and values, tokens in its last pages."""
     dim, heads, page = 128, 8, 64
