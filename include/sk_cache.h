@@ -22,7 +22,7 @@
  *   - What changes from step to step is read on the device: the lengths, the rows of each sequence and the page table.  A
  *     plan therefore serves step after step, and its launches may be captured into a HIP graph (outside a capture an event
  *     is recorded with them).  The host states only upper bounds (rows, max_new, pages_per_sequence), which fix the grids.
- *   - A plan owns a workspace: its launches must not overlap.  Launches on one stream are ordered by it; a launch on
+ *   - A plan owns a workspace: its attention launches must not overlap.  Those on one stream are ordered by it; sk_attn_launch on
  *     another stream gives SK_ERR_BUSY while the last one has not completed (best effort; launches of a graph are not tracked).
  */
 #ifndef SK_CACHE_H

@@ -57,7 +57,8 @@ struct sk_attn_plan {
   uint32_t *arrivals = nullptr;
   float *workspace = nullptr;
   hipEvent_t last_use = nullptr;  // completes with the latest launch made outside a stream capture
-  sk::LaunchLedger ledger;
+  sk::LaunchLedger ledger;        // of sk_attn_launch
+  bool appended = false;          // sk_attn_append has been called
 };
 
 struct sk_pages {
@@ -73,17 +74,23 @@ struct sk_pages {
 
 namespace {
 
-// As for the plans of superkernel.h: SK_ERR_BUSY while the previous launch still runs on another stream.
-sk_status admit(sk_attn_plan *plan, hipStream_t stream, bool *in_capture) {
+sk_status check_resident(const sk_attn_plan *plan) {
   if (!plan) return set_last_error(SK_ERR_INVALID_ARG, "plan is null");
   if (!plan->resident) return set_last_error(SK_ERR_STATE, "plan was created host-only; it has no device tables");
   int dev = -1;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return hip_error("hipGetDevice", e);
   if (dev != plan->device) return set_last_error(SK_ERR_STATE, "plan belongs to another device than the current one");
+  return SK_OK;
+}
+
+// As for the plans of superkernel.h: SK_ERR_BUSY while the previous launch still runs on another stream.
+sk_status admit(sk_attn_plan *plan, hipStream_t stream, bool *in_capture) {
+  const sk_status st = check_resident(plan);
+  if (st != SK_OK) return st;
   *in_capture = capturing(stream);
   if (plan->ledger.before_launch((uintptr_t)stream, *in_capture) == sk::LaunchLedger::QUERY_EVENT) {
-    e = hipEventQuery(plan->last_use);
+    const hipError_t e = hipEventQuery(plan->last_use);
     if (e == hipErrorNotReady) {
       (void)hipGetLastError();
       return set_last_error(SK_ERR_BUSY, "the plan's previous launch is still running on another stream");
@@ -146,32 +153,47 @@ sk_status make_resident(sk_attn_plan *plan) {
   return SK_OK;
 }
 
-// The copies in waves, then (or with the last launch) the rows of the page table.
-sk_status launch_copies(const sk_page_array *arrays, int32_t n_arrays, const sk::PageMove *moves, size_t n_moves, hipStream_t stream, int32_t *table, const int32_t *rows,
-                        int32_t n_rows, int32_t columns, hipEvent_t behind) {
-  sk::CopyArgs a{};
+// The copies of one wave and, with the last launch, n_rows rows of the page table: in host memory that the device can read (`pinned`), or as
+// `put` writes them into the launch's arguments.
+template <class F>
+sk_status launch_copies(const sk_page_array *arrays, int32_t n_arrays, const sk::PageMove *moves, size_t n_moves, hipStream_t stream, int32_t *table, int32_t n_rows,
+                        int32_t columns, const int32_t *pinned, F put, hipEvent_t behind) {
+  sk::CopyArgs a;
   a.table = table;
-  a.rows = rows;
   a.columns = columns;
   for (int32_t a0 = 0;; a0 += sk::COPY_ARRAYS) {
     a.n_arrays = n_moves ? std::max(0, std::min(n_arrays - a0, sk::COPY_ARRAYS)) : 0;
     a.chunks = 0;
     for (int32_t i = 0; i < a.n_arrays; ++i) {
-      a.arrays[i].base = (char *)arrays[a0 + i].base;
-      a.arrays[i].bytes = arrays[a0 + i].page_bytes;
+      std::memcpy(a.words + 4 * i, &arrays[a0 + i].base, 8);
+      std::memcpy(a.words + 4 * i + 2, &arrays[a0 + i].page_bytes, 8);
       a.chunks = std::max(a.chunks, (arrays[a0 + i].page_bytes + sk::COPY_CHUNK - 1) / sk::COPY_CHUNK);
     }
     const bool last_arrays = a0 + sk::COPY_ARRAYS >= n_arrays || !n_moves;
     for (size_t m0 = 0;; m0 += sk::COPY_MOVES) {
       a.n_moves = a.n_arrays ? (int32_t)std::min(n_moves - m0, (size_t)sk::COPY_MOVES) : 0;
-      if (a.n_moves) std::memcpy(a.moves, moves + m0, (size_t)a.n_moves * sizeof(sk::PageMove));
+      if (a.n_moves) std::memcpy(a.words + 4 * a.n_arrays, moves + m0, (size_t)a.n_moves * sizeof(sk::PageMove));
       const bool last = last_arrays && m0 + sk::COPY_MOVES >= n_moves;
-      a.n_rows = last ? n_rows : 0;
-      const int64_t grid = a.chunks * a.n_arrays * a.n_moves + a.n_rows;
-      if (grid >= (int64_t)1 << 31) return set_last_error(SK_ERR_UNSUPPORTED, "pages too large for a launch's grid");
-      if (grid) {
-        const sk_status st = launch(sk::sk_copy_pages, grid, stream, last ? behind : nullptr, a);
+      const int64_t copies = a.chunks * a.n_arrays * a.n_moves;
+      bool with_rows = last && n_rows;
+      a.rows = pinned;
+      if (with_rows && !pinned) {
+        const int64_t at = 4 * a.n_arrays + 2 * a.n_moves, words = n_rows * (1 + (int64_t)columns);
+        if (at + words <= sk::COPY_WORDS) put(a.words + at);
+        else with_rows = false;  // they get a launch of their own
+      }
+      a.n_rows = with_rows ? n_rows : 0;
+      if (copies + a.n_rows >= (int64_t)1 << 31) return set_last_error(SK_ERR_UNSUPPORTED, "pages too large for a launch's grid");
+      const bool alone = last && n_rows && !with_rows;
+      if (copies + a.n_rows) {
+        const sk_status st = launch(sk::sk_copy_pages, copies + a.n_rows, stream, last && !alone ? behind : nullptr, a);
         if (st != SK_OK) return st;
+      }
+      if (alone) {
+        a.n_arrays = a.n_moves = 0;
+        a.n_rows = n_rows;
+        put(a.words);
+        return launch(sk::sk_copy_pages, n_rows, stream, behind, a);
       }
       if (m0 + sk::COPY_MOVES >= n_moves) break;
     }
@@ -233,7 +255,7 @@ sk_status sk_attn_plan_destroy(sk_attn_plan *plan) {
   if (!plan) return SK_OK;
   return guarded([&]() -> sk_status {
     hipError_t e = hipSuccess;
-    const sk::LaunchLedger::Wait wait = plan->ledger.before_destroy();
+    const sk::LaunchLedger::Wait wait = plan->appended ? sk::LaunchLedger::DEVICE : plan->ledger.before_destroy();
     if (wait == sk::LaunchLedger::EVENT) {
       e = hipEventSynchronize(plan->last_use);
     } else if (wait == sk::LaunchLedger::DEVICE) {
@@ -253,14 +275,14 @@ sk_status sk_attn_plan_destroy(sk_attn_plan *plan) {
 sk_status sk_attn_append(sk_attn_plan *plan, void *hip_stream) {
   return guarded([&]() -> sk_status {
     const hipStream_t stream = (hipStream_t)hip_stream;
-    bool in_capture = false;
-    sk_status st = admit(plan, stream, &in_capture);
+    sk_status st = check_resident(plan);
     if (st != SK_OK || plan->host.problems.empty()) return st;
     if (!plan->host.all_qkv) return set_last_error(SK_ERR_STATE, "a problem of the plan has no qkv");
     const sk::AppendArgs a{plan->problems, plan->append_first, (int32_t)plan->host.problems.size()};
-    const hipEvent_t behind = in_capture ? nullptr : plan->last_use;
-    st = launch(sk::sk_append, (int64_t)plan->host.append_first.back(), stream, behind, a);
-    plan->ledger.after_launch((uintptr_t)stream, in_capture, behind && st == SK_OK);
+    // It writes nothing of the plan's, so no later launch has to wait for it, only the plan's end (for the device: an event with
+    // the launch makes who waits for the device behind it wait up to 10 us longer).
+    st = launch(sk::sk_append, (int64_t)plan->host.append_first.back(), stream, nullptr, a);
+    plan->appended = true;
     return st;
   });
 }
@@ -377,9 +399,14 @@ sk_status sk_pages_apply(sk_pages *pages, const sk_page_array *arrays, int32_t n
       acc.applied();
       return SK_OK;
     }
+    auto put = [&](int32_t *to) {
+      std::memcpy(to, dirty.data(), (size_t)n_rows * 4);
+      for (int32_t r = 0; r < n_rows; ++r) std::memcpy(to + n_rows + (size_t)r * columns, acc.row(dirty[r]), (size_t)columns * 4);
+    };
     const int i = pages->next;
     hipError_t e = hipSuccess;
-    if (n_rows) {
+    const bool pinned = n_rows && n_rows * (1 + (int64_t)columns) > sk::COPY_WORDS;  // more than a launch's arguments hold
+    if (pinned) {
       if (!pages->rows[i]) {
         const size_t bytes = ((size_t)acc.sequences() * (columns + 1)) * 4;
         if ((e = hipHostMalloc((void **)&pages->rows[i], bytes, hipHostMallocDefault)) != hipSuccess) {
@@ -391,19 +418,17 @@ sk_status sk_pages_apply(sk_pages *pages, const sk_page_array *arrays, int32_t n
       if (!pages->done[i] && (e = hipEventCreateWithFlags(&pages->done[i], hipEventDisableTiming)) != hipSuccess) return hip_error("hipEventCreate", e);
       if (pages->used[i] && (e = hipEventSynchronize(pages->done[i])) != hipSuccess) return hip_error("hipEventSynchronize", e);
       pages->used[i] = false;
-      int32_t *to = pages->rows[i];
-      std::memcpy(to, dirty.data(), (size_t)n_rows * 4);
-      for (int32_t r = 0; r < n_rows; ++r) std::memcpy(to + n_rows + (size_t)r * columns, acc.row(dirty[r]), (size_t)columns * 4);
+      put(pages->rows[i]);
     }
     const auto &waves = acc.waves();
     const size_t launches = std::max<size_t>(waves.size(), 1);
     for (size_t w = 0; w < launches; ++w) {
       const bool last = w + 1 == launches;
-      st = launch_copies(arrays, n_arrays, waves.empty() ? nullptr : waves[w].data(), waves.empty() ? 0 : waves[w].size(), stream, page_table, pages->rows[i],
-                         last ? n_rows : 0, columns, last && n_rows ? pages->done[i] : nullptr);
+      st = launch_copies(arrays, n_arrays, waves.empty() ? nullptr : waves[w].data(), waves.empty() ? 0 : waves[w].size(), stream, page_table, last ? n_rows : 0,
+                         columns, pinned ? pages->rows[i] : nullptr, put, last && pinned ? pages->done[i] : nullptr);
       if (st != SK_OK) return st;
     }
-    if (n_rows) {
+    if (pinned) {
       pages->used[i] = true;
       pages->next = (i + 1) % sk_pages::SLOTS;
     }
@@ -428,7 +453,7 @@ sk_status sk_pages_copy(const sk_page_array *arrays, int32_t n_arrays, int32_t n
     for (int32_t i = 0; i < n; ++i)
       if (seen[from[i]]) return set_last_error(SK_ERR_OVERLAP, "copy " + std::to_string(i) + ": its page is read and written");
     if (!n || !n_arrays) return SK_OK;
-    return launch_copies(arrays, n_arrays, moves.data(), moves.size(), (hipStream_t)hip_stream, nullptr, nullptr, 0, 0, nullptr);
+    return launch_copies(arrays, n_arrays, moves.data(), moves.size(), (hipStream_t)hip_stream, nullptr, 0, 0, nullptr, [](int32_t *) {}, nullptr);
   });
 }
 

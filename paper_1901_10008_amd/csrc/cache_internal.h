@@ -69,24 +69,21 @@ sk_status plan_attn(const sk_attn_problem *problems, int32_t n, int32_t compute_
 // Floats of a split unit's partial result: outputs, running maximum and sum of each row.
 constexpr int64_t part_floats(int64_t rows, int64_t most_dim) { return rows * (most_dim + 2); }
 
-// One launch of page copies, by value: at most so many arrays and copies.
-constexpr int COPY_ARRAYS = 64, COPY_MOVES = 300;
+// One launch of page copies and of changed rows of the page table, by value.  words: n_arrays times base and bytes of a page (64 bits each), n_moves
+// times from and to, then (if `rows` is null) n_rows row numbers and the rows; otherwise those stand in host memory.
 struct PageMove {
   int32_t from, to;
 };
+constexpr int COPY_WORDS = 1008;
 struct CopyArgs {
-  struct {
-    char *base;
-    int64_t bytes;
-  } arrays[COPY_ARRAYS];
-  PageMove moves[COPY_MOVES];
-  int32_t n_arrays, n_moves;
-  int32_t *table;            // device page table (null: none)
-  const int32_t *rows;       // host memory: n_rows row numbers, then the rows
-  int32_t n_rows, columns;
-  int64_t chunks;            // of COPY_CHUNK bytes per page, of the array with the largest pages
+  int32_t n_arrays, n_moves, n_rows, columns;
+  int64_t chunks;       // of COPY_CHUNK bytes per page, of the array with the largest pages
+  int32_t *table;       // device page table
+  const int32_t *rows;  // host memory that the device can read, or null
+  int32_t words[COPY_WORDS];
 };
 static_assert(sizeof(CopyArgs) <= 4096, "kernel arguments");
+constexpr int COPY_ARRAYS = 64, COPY_MOVES = (COPY_WORDS - 4 * COPY_ARRAYS) / 2;  // of a launch, at most
 constexpr int64_t COPY_CHUNK = 32768;
 
 // The account of pages.

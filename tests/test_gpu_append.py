@@ -216,3 +216,30 @@ def test_account_and_device_agree_under_random_calls():
     assert deepest > 2
     torch.cuda.synchronize()
     account.close()
+
+
+@pytest.mark.parametrize("columns,seqs", [(12, 9), (120, 9), (300, 40)])
+def test_rows_of_the_table_of_any_length(columns, seqs):
+    """Rows that fit a launch's arguments, alone or beside the copies, and rows that go through host memory."""
+    page, pages = 16, 2000
+    pool = torch.randint(0, 1 << 30, (pages, 64), dtype=torch.int32, device="cuda")
+    table = torch.full((seqs, columns), -7, dtype=torch.int32, device="cuda")
+    arrays = arrays_of([pool] * 1)
+    with sk.sk_pages_create(pages, page, seqs, columns) as account:
+        for step in range(9):
+            sk.sk_pages_resize(account, list(range(1, seqs)), [0] * (seqs - 1))
+            sk.sk_pages_resize(account, [0], [min(columns * page - 20, 100 + 37 * step)])
+            sk.sk_pages_fork(account, 0, list(range(1, seqs)))
+            tokens = sk.sk_pages_state(account, 0)[0]
+            sk.sk_pages_resize(account, list(range(1, seqs)), [tokens + 17] * (seqs - 1))
+            before = pool.clone()
+            copies = sk.sk_pages_state(account)[1]
+            sk.sk_pages_apply(account, arrays, table.data_ptr(), H.stream_handle())
+            torch.cuda.synchronize()
+            rows = [sk.sk_pages_state(account, s)[1] for s in range(seqs)]
+            assert table.cpu().tolist() == rows
+            last = tokens // page
+            assert copies == (seqs - 1 if tokens % page else 0)
+            if tokens % page:
+                for s in range(1, seqs):
+                    assert torch.equal(pool[rows[s][last]], before[rows[0][last]])
