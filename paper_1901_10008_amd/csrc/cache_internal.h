@@ -13,8 +13,12 @@ namespace sk {
 
 constexpr int CACHE_THREADS = 256;
 // Rows of a unit of work (a key-value head of a sequence): few rows go in blocks of ROWS_FEW, whose four waves share the
-// keys among them; more than MOST_FEW rows go in blocks of ROWS_MANY, whose waves share the rows.
-constexpr int ROWS_FEW = 16, ROWS_MANY = 128, MOST_FEW = 32;
+// keys among them; more than most_few() rows go in blocks of ROWS_MANY, whose waves share the rows.
+constexpr int ROWS_FEW = 16, ROWS_MANY = 128;
+// Two blocks of few rows read the keys twice (the second time mostly out of the caches), a block of many rows keeps fewer loads in flight: 20 rows on
+// caches of 8000 tokens, 16 sequences of 8 heads of 128 elements, 123 us as few and 105 as many, of 4000 tokens with heads of 64, 31 and 37, one head
+// of 256 on 8000, 24 rows, 40 and 69.
+constexpr int most_few(int dim) { return dim > 64 && dim <= 128 ? 16 : 32; }
 constexpr int KEYS_FEW = 32;                                  // keys per step
 constexpr int keys_many(int dim) { return dim <= 128 ? 64 : 32; }  // (heads of 256: what a thread has in flight has to fit its registers)
 constexpr int APPEND_WAVES = 8192;  // append: a problem's rows are cut into parts for at least that many waves where they have the heads for it
@@ -38,7 +42,7 @@ struct AttnDev {
 // A sequence of a launch: what a workgroup needs to know of it to count its units.
 struct AttnSeq {
   const int32_t *length, *first;
-  int32_t problem, seq, kv_heads, group, window, sinks, rows, max_new;
+  int32_t problem, seq, kv_heads, group, window, sinks, rows, max_new, most_few, pad;
   int64_t capacity;  // tokens that its row of the page table can hold
 };
 

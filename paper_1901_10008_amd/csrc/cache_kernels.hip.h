@@ -174,11 +174,12 @@ struct Count {
   bool many;
 };
 template <bool MANY, bool WIDE>
-__device__ __forceinline__ Count count_units(const Step &s, int32_t kv_heads, int32_t group, int32_t window, int32_t sinks) {
+__device__ __forceinline__ Count count_units(const Step &s, const AttnSeq &q) {
+  const int32_t kv_heads = q.kv_heads, group = q.group, window = q.window, sinks = q.sinks;
   Count c;
   const int64_t rows = (int64_t)s.fresh * group;
   const int32_t last = s.behind + s.fresh - 1;
-  c.many = MANY && rows > MOST_FEW;
+  c.many = MANY && rows > q.most_few;
   if (c.many) {
     c.units = (int32_t)((rows + ROWS_MANY - 1) / ROWS_MANY) * kv_heads;
     const int32_t tokens = (ROWS_MANY + group - 1) / group;
@@ -280,7 +281,7 @@ __device__ __forceinline__ Unit find_unit(const AttnArgs &a, FindScratch *f) {
     if (lane < a.sequences) {
       q = a.seqs[lane];
       s = step_of(q);
-      c = count_units<MANY, WIDE>(s, q.kv_heads, q.group, q.window, q.sinks);
+      c = count_units<MANY, WIDE>(s, q);
     }
     const int32_t units = lane_of(wave_scan(c.units), 63);
     const int64_t work = lane_of(wave_scan((int64_t)c.units * c.blocks * (c.many ? 2 : 1)), 63);
@@ -320,7 +321,7 @@ __device__ __forceinline__ Unit find_unit(const AttnArgs &a, FindScratch *f) {
   auto look = [&](int i) {
     q = a.seqs[i];
     s = step_of(q);
-    c = count_units<MANY, WIDE>(s, q.kv_heads, q.group, q.window, q.sinks);
+    c = count_units<MANY, WIDE>(s, q);
   };
   int64_t work = 0;
   for (int i = s0; i < s1; ++i) {
@@ -767,14 +768,23 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, const SK_CONSTANT 
     const int r = n / (DP / 4), e = n % (DP / 4) * 4;
     float big = -__builtin_inff(), sum = 0.f;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int s = 0; s < u.splits; ++s) {
-      const float *w = ws0 + s * step;
-      const f32x2 ms = load_shared(w + ROWS_FEW * DP + 2 * r), x = load_shared(w + r * DP + e), y = load_shared(w + r * DP + e + 2);
-      const float next = fmaxf(big, ms.x), keep = exp2_fast(big - base_of(next)), mul = exp2_fast(ms.x - base_of(next));
-      sum = sum * keep + ms.y * mul;
-      v = v * keep + f32x4{x.x, x.y, y.x, y.y} * mul;
-      big = next;
+    constexpr int AT_ONCE = 8;  // slices whose loads go out together (one by one each would be waited for)
+    for (int s = 0; s < u.splits; s += AT_ONCE) {
+      f32x2 ms[AT_ONCE], x[AT_ONCE], y[AT_ONCE];
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i) {
+        const float *w = ws0 + min(s + i, u.splits - 1) * step;
+        ms[i] = load_shared(w + ROWS_FEW * DP + 2 * r), x[i] = load_shared(w + r * DP + e), y[i] = load_shared(w + r * DP + e + 2);
+      }
+      fixed_order();
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i) {
+        if (s + i >= u.splits) break;
+        const float next = fmaxf(big, ms[i].x), keep = exp2_fast(big - base_of(next)), mul = exp2_fast(ms[i].x - base_of(next));
+        sum = sum * keep + ms[i].y * mul;
+        v = v * keep + f32x4{x[i].x, x[i].y, y[i].x, y[i].y} * mul;
+        big = next;
+      }
     }
     const float inv = inverse(sum);
     const int32_t row = row0 + r;
@@ -1087,26 +1097,56 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
     if (!wave_ok) return;
     const float *ws0 = a.ws_many + (int64_t)u.first_slot * SLOT;
     const int64_t step = (int64_t)P.kv_heads * SLOT;
+    // maximum and sum first, then the outputs, a block of 32 elements of a slice after the other with the next one's loads out
     m = -__builtin_inff();
     l = 0.f;
+    constexpr int AT_ONCE = 8;
+    for (int s = 0; s < u.splits; s += AT_ONCE) {
+      f32x2 ms[AT_ONCE];
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i) ms[i] = load_shared(ws0 + min(s + i, u.splits - 1) * step + ROWS_MANY * DP + 2 * in_block);
+      fixed_order();
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i) {
+        if (s + i >= u.splits) break;
+        const float next = fmaxf(m, ms[i].x);
+        l = l * exp2_fast(m - base_of(next)) + ms[i].y * exp2_fast(ms[i].x - base_of(next));
+        m = next;
+      }
+    }
 #pragma unroll
     for (int i = 0; i < NB; ++i)
 #pragma unroll
       for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
+    const float base = base_of(m);
+    f32x2 x[2][8], ms[2];
+    auto read = [&](int s, int i, int to) {
+      const float *w = ws0 + min(s, u.splits - 1) * step;
+      ms[to] = load_shared(w + ROWS_MANY * DP + 2 * in_block);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[to][j] = load_shared(w + ((wave * NB + i) * 8 + j) * 128 + 2 * lane);
+      fixed_order();
+    };
+    auto add = [&](int i, int from) {
+      const float mul = exp2_fast(ms[from].x - base);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        o[i][2 * j] += x[from][j].x * mul;
+        o[i][2 * j + 1] += x[from][j].y * mul;
+      }
+      fixed_order();
+    };
+    static_assert(NB >= 2, "two blocks at least");
+    read(0, 0, 0);
     for (int s = 0; s < u.splits; ++s) {
-      const float *w = ws0 + s * step;
-      const f32x2 ms = load_shared(w + ROWS_MANY * DP + 2 * in_block);
-      const float next = fmaxf(m, ms.x), keep = exp2_fast(m - base_of(next)), mul = exp2_fast(ms.x - base_of(next));
-      l = l * keep + ms.y * mul;
-      m = next;
+      // (an odd number of blocks leaves the places in another order behind each slice: then the last block's place is used twice)
 #pragma unroll
-      for (int i = 0; i < NB; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const f32x2 x = load_shared(w + ((wave * NB + i) * 8 + j) * 128 + 2 * lane);
-          o[i][2 * j] = o[i][2 * j] * keep + x.x * mul;
-          o[i][2 * j + 1] = o[i][2 * j + 1] * keep + x.y * mul;
-        }
+      for (int i = 0; i < NB; ++i) {
+        if (i + 1 < NB) read(s, i + 1, (i + 1) & 1);
+        else if (NB % 2 == 0) read(s + 1, 0, 0);
+        add(i, i & 1);
+      }
+      if (NB % 2) read(s + 1, 0, 0);
     }
   }
   if (!row_ok) return;

@@ -143,17 +143,17 @@ sk_status plan_attn(const sk_attn_problem *problems, int32_t n, int32_t compute_
       const AttnDev &d = out.problems[(size_t)i];
       if (!d.out || (d.dim > 128) != wide) continue;
       const int64_t capacity = (int64_t)d.columns << d.page_shift, most_rows = (int64_t)d.max_new * d.group;
-      const int64_t blocks = (std::min<int64_t>(most_rows, MOST_FEW) + ROWS_FEW - 1) / ROWS_FEW, units = (int64_t)d.sequences * d.kv_heads * blocks;
+      const int64_t blocks = (std::min<int64_t>(most_rows, most_few(d.dim)) + ROWS_FEW - 1) / ROWS_FEW, units = (int64_t)d.sequences * d.kv_heads * blocks;
       few += units;
       few_most += units * (capacity / (4 * KEYS_FEW) + 2);
-      if (most_rows > MOST_FEW) {
+      if (most_rows > most_few(d.dim)) {
         // sequences of many rows: their blocks are full but for one each
-        const int64_t rows = (int64_t)d.rows * d.group, full = d.kv_heads * (rows / ROWS_MANY + std::min<int64_t>(d.sequences, rows / (MOST_FEW + 1) + 1));
+        const int64_t rows = (int64_t)d.rows * d.group, full = d.kv_heads * (rows / ROWS_MANY + std::min<int64_t>(d.sequences, rows / (most_few(d.dim) + 1) + 1));
         many += full;
         many_most += full * (capacity / (4 * keys_many(d.dim)) + 2);
       }
       for (int32_t s = 0; s < d.sequences; ++s)
-        out.seqs.push_back(AttnSeq{d.lengths + s, d.first_row + s, i, s, d.kv_heads, d.group, d.window, d.sinks, d.rows, d.max_new, capacity});
+        out.seqs.push_back(AttnSeq{d.lengths + s, d.first_row + s, i, s, d.kv_heads, d.group, d.window, d.sinks, d.rows, d.max_new, most_few(d.dim), 0, capacity});
     }
     g.sequences = (int64_t)out.seqs.size() - g.first_seq;
     if (!g.sequences) continue;

@@ -61,8 +61,8 @@ static void plans(std::mt19937 &rng) {
       int64_t few = 0, many = 0;
       for (int64_t s = g.first_seq; s < g.first_seq + g.sequences; ++s) {
         const sk::AttnSeq &q = h.seqs[(size_t)s];
-        few += (int64_t)q.kv_heads * ((std::min<int64_t>((int64_t)q.group * q.max_new, sk::MOST_FEW) + sk::ROWS_FEW - 1) / sk::ROWS_FEW);
-        if ((int64_t)q.max_new * q.group > sk::MOST_FEW && q.seq == 0) many += (int64_t)q.kv_heads * (((int64_t)q.rows * q.group + sk::ROWS_MANY - 1) / sk::ROWS_MANY);
+        few += (int64_t)q.kv_heads * ((std::min<int64_t>((int64_t)q.group * q.max_new, q.most_few) + sk::ROWS_FEW - 1) / sk::ROWS_FEW);
+        if ((int64_t)q.max_new * q.group > q.most_few && q.seq == 0) many += (int64_t)q.kv_heads * (((int64_t)q.rows * q.group + sk::ROWS_MANY - 1) / sk::ROWS_MANY);
       }
       need(g.grid >= std::max(few, many), "units without a workgroup");
       need(h.counters >= g.slots_few + g.slots_many, "counters");
