@@ -52,7 +52,7 @@ struct AttnGroup {
   int64_t first_seq, sequences; // in the plan's list
   int64_t workgroups;           // that the device runs at a time
   int64_t grid;                 // of the launch: the most units there can be, and that many for slices
-  int64_t slots_many, slots_few;  // places of the workspace: as many as there can be units and slices of either kind
+  int64_t slots_many, slots_few;  // places of the workspace: as many as there can be slices of either kind
 };
 // Workgroups of a kernel that a compute unit holds (its registers and LDS).
 constexpr int resident(bool wide, bool many) { return wide ? 1 : many ? 2 : 3; }

@@ -221,18 +221,19 @@ __device__ __forceinline__ int32_t splits_of(const Count &c, int32_t most) {
   const int32_t per = max(c.many ? (most + 1) / 2 : most, LEAST);
   return min((int32_t)(((int64_t)max(c.blocks, 1) + per - 1) / per), MOST_SPLITS);
 }
-// work: blocks of few rows and twice the tiles of many.  That many for each workgroup the card runs at a time: with it all slices
-// are no more than these workgroups and the units together.
+// work: blocks of few rows and twice the tiles of many.  That many for each workgroup the card runs at a time: with it units and slices
+// are no more than these workgroups and the units together, and the slices of units that are cut (each of more than `most`) no more than twice
+// these workgroups.
 __device__ __forceinline__ int32_t even_share(int64_t work, int64_t workgroups) { return (int32_t)min((work + workgroups - 1) / workgroups, (int64_t)0x7ffffffe); }
 
 struct FindScratch {
   int64_t work[4];  // per wave
-  int32_t units[4], items[2][4];
+  int32_t items[2][4], cut[2][4];
   Unit unit;
 };
 
-// Unit number i of a sequence's.
-__device__ __forceinline__ Unit unit_of(const AttnSeq &q, const Step &s, const Count &c, int32_t splits, int32_t i, uint32_t item) {
+// Unit number i of a sequence's, whose slices have the places from `slot` on.
+__device__ __forceinline__ Unit unit_of(const AttnSeq &q, const Step &s, const Count &c, int32_t splits, int32_t i, int32_t slot) {
   const int32_t rest = i / q.kv_heads;
   Unit u;
   u.problem = q.problem;
@@ -241,8 +242,8 @@ __device__ __forceinline__ Unit unit_of(const AttnSeq &q, const Step &s, const C
   u.split = rest % splits;
   u.splits = splits;
   u.block = c.units / q.kv_heads - 1 - rest / splits;
-  u.slot = item;
-  u.first_slot = item - (uint32_t)(u.split * q.kv_heads);
+  u.slot = (uint32_t)(slot + i);
+  u.first_slot = (uint32_t)(slot + i - u.split * q.kv_heads);
   u.step = s;
   u.many = c.many;
   u.any = true;
@@ -292,25 +293,29 @@ __device__ __forceinline__ Unit find_unit(const AttnArgs &a, FindScratch *f) {
       most += most / 8 + 1;
       splits = splits_of(c, most);
     }
-    int32_t n, n_many, upto_many, all_many, upto_few;
+    // units and slices, and those of them that are slices, up to and with this lane's
+    int32_t n_many, n_few, upto_many, upto_few, cut_many, cut_few;
     auto sums = [&]() {
-      n = c.units * splits, n_many = MANY && c.many ? n : 0;
-      upto_many = MANY ? wave_scan(n_many) : 0, all_many = MANY ? lane_of(upto_many, 63) : 0, upto_few = wave_scan(n - n_many);
+      const int32_t n = c.units * splits;
+      n_many = MANY && c.many ? n : 0, n_few = n - n_many;
+      upto_many = MANY ? wave_scan(n_many) : 0, upto_few = wave_scan(n_few);
+      cut_many = MANY ? wave_scan(splits > 1 ? n_many : 0) : 0, cut_few = wave_scan(splits > 1 ? n_few : 0);
     };
     sums();
-    if (all_many > (int32_t)a.slots_many || lane_of(upto_few, 63) > (int32_t)a.slots_few) {  // (a first_row that decreases: no slices, no places needed)
+    if (lane_of(cut_many, 63) > (int32_t)a.slots_many || lane_of(cut_few, 63) > (int32_t)a.slots_few) {  // (a first_row that decreases: no slices, no places needed)
       splits = 1;
       sums();
     }
+    const int32_t all_many = MANY ? lane_of(upto_many, 63) : 0;
     const bool many = MANY && item < all_many;
     if (!many) item -= all_many;
-    const int32_t upto = many ? upto_many : upto_few, mine = c.many == many ? n : 0;
+    const int32_t upto = many ? upto_many : upto_few, mine = many ? n_many : n_few;
     const uint64_t hit = __ballot(item >= upto - mine && item < upto);
     Unit u{};
     u.any = hit != 0;
     if (!u.any) return u;
     const int who = __builtin_ctzll(hit);
-    return unit_in_lane(unit_of(q, s, c, splits, item - (upto - mine), (uint32_t)item), who);
+    return unit_in_lane(unit_of(q, s, c, splits, item - (upto - mine), (many ? cut_many : cut_few) - mine), who);
   }
   // a run of sequences per thread
   const int per_thread = (a.sequences + CACHE_THREADS - 1) / CACHE_THREADS;
@@ -333,37 +338,39 @@ __device__ __forceinline__ Unit find_unit(const AttnArgs &a, FindScratch *f) {
   if (tid == 0) f->unit.any = false;
   __syncthreads();
   int32_t most = even_share(f->work[0] + f->work[1] + f->work[2] + f->work[3], a.workgroups);
-  int32_t n_many, n_few, upto_many, upto_few, all_many;
+  int32_t n[2], cut[2], upto[2], cut_upto[2];  // of many rows and of few
   for (int round = 0; round < 2; ++round) {
-    n_many = n_few = 0;
+    n[0] = n[1] = cut[0] = cut[1] = 0;
     for (int i = s0; i < s1; ++i) {
       if (per_thread > 1) look(i);
-      const int32_t n = c.units * splits_of(c, most);
-      n_many += MANY && c.many ? n : 0;
-      n_few += MANY && c.many ? 0 : n;
+      const int32_t splits = splits_of(c, most), here = c.units * splits, sliced = splits > 1 ? here : 0;
+      n[0] += MANY && c.many ? here : 0, cut[0] += MANY && c.many ? sliced : 0;
+      n[1] += MANY && c.many ? 0 : here, cut[1] += MANY && c.many ? 0 : sliced;
     }
-    upto_many = MANY ? wave_scan(n_many) : 0, upto_few = wave_scan(n_few);
-    if (lane == 63) {
-      f->items[0][wave] = upto_many;
-      f->items[1][wave] = upto_few;
+#pragma unroll
+    for (int k = MANY ? 0 : 1; k < 2; ++k) {
+      upto[k] = wave_scan(n[k]);
+      cut_upto[k] = wave_scan(cut[k]);
+      if (lane == 63) {
+        f->items[k][wave] = upto[k];
+        f->cut[k][wave] = cut_upto[k];
+      }
     }
     __syncthreads();
-    all_many = 0;
-    int32_t all_few = 0;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      all_many += MANY ? f->items[0][w] : 0;
-      all_few += f->items[1][w];
-    }
-    if (all_many <= (int32_t)a.slots_many && all_few <= (int32_t)a.slots_few) break;
+    const int32_t all_cut_many = MANY ? f->cut[0][0] + f->cut[0][1] + f->cut[0][2] + f->cut[0][3] : 0;
+    if (all_cut_many <= (int32_t)a.slots_many && f->cut[1][0] + f->cut[1][1] + f->cut[1][2] + f->cut[1][3] <= (int32_t)a.slots_few) break;
     most = 0x7ffffffe;  // (a first_row that decreases: no slices, no places needed)
     __syncthreads();
   }
+  const int32_t all_many = MANY ? f->items[0][0] + f->items[0][1] + f->items[0][2] + f->items[0][3] : 0;
   const bool many = MANY && item < all_many;
   if (!many) item -= all_many;
-  const int32_t mine = many ? n_many : n_few;
-  int32_t before = (many ? upto_many : upto_few) - mine;
-  for (int w = 0; w < wave; ++w) before += f->items[many ? 0 : 1][w];
+  const int32_t mine = many ? n[0] : n[1];
+  int32_t before = (many ? upto[0] : upto[1]) - mine, slot = many ? cut_upto[0] - cut[0] : cut_upto[1] - cut[1];
+  for (int w = 0; w < wave; ++w) {
+    before += f->items[many ? 0 : 1][w];
+    slot += f->cut[many ? 0 : 1][w];
+  }
   if (item >= before && item < before + mine) {
     int32_t at = before;
     for (int i = s0; i < s1; ++i) {
@@ -371,10 +378,11 @@ __device__ __forceinline__ Unit find_unit(const AttnArgs &a, FindScratch *f) {
       if (c.many != many) continue;
       const int32_t splits = splits_of(c, most), here = c.units * splits;
       if (item < at + here) {
-        f->unit = unit_of(q, s, c, splits, item - at, (uint32_t)item);
+        f->unit = unit_of(q, s, c, splits, item - at, slot);
         break;
       }
       at += here;
+      slot += splits > 1 ? here : 0;
     }
   }
   __syncthreads();

@@ -35,6 +35,7 @@ sk_status check_problem(const sk_attn_problem &p, AttnDev &d, std::string &err) 
   if (p.dtype != SK_BF16 && p.dtype != SK_F16) return refuse(err, SK_ERR_UNSUPPORTED, "dtype must be SK_BF16 or SK_F16");
   if (p.q_heads < 1 || p.kv_heads < 1 || p.head_dim < 1 || p.page_tokens < 1 || p.num_pages < 1 || p.sequences < 1 || p.pages_per_sequence < 1 || p.rows < 1)
     return refuse(err, SK_ERR_INVALID_ARG, "a size is less than 1");
+  if (p.sequences > 1 << 20) return refuse(err, SK_ERR_UNSUPPORTED, "more than 2^20 sequences");
   if (p.max_new < 0 || p.window < 0 || p.sinks < 0 || p.rotary_dim < 0 || p.reserved != 0)
     return refuse(err, SK_ERR_INVALID_ARG, "max_new, window, sinks or rotary_dim is negative, or reserved is not 0");
   if (p.q_heads % p.kv_heads) return refuse(err, SK_ERR_INVALID_ARG, "q_heads must be a multiple of kv_heads");
@@ -159,9 +160,9 @@ sk_status plan_attn(const sk_attn_problem *problems, int32_t n, int32_t compute_
     if (!g.sequences) continue;
     g.many = many > 0;
     g.workgroups = workgroups ? workgroups : (int64_t)resident(g.wide, g.many) * compute_units;
-    g.slots_few = std::min(few + g.workgroups, few_most);
-    g.slots_many = std::min(many + g.workgroups, many_most);
-    g.grid = std::min(few + many + g.workgroups, g.slots_few + g.slots_many);
+    g.grid = std::min(few + many + g.workgroups, few_most + many_most);
+    g.slots_few = std::min(2 * g.workgroups, few_most);
+    g.slots_many = std::min(2 * g.workgroups, many_most);
     if (g.grid >= (int64_t)1 << 31) return refuse(err, SK_ERR_UNSUPPORTED, "more units of work than a launch's grid can hold");
     const int64_t dim = wide ? 256 : 128;
     out.workspace_floats = std::max(out.workspace_floats, g.slots_few * part_floats(ROWS_FEW, dim) + g.slots_many * part_floats(ROWS_MANY, dim));

@@ -66,7 +66,7 @@ static void plans(std::mt19937 &rng) {
       }
       need(g.grid >= std::max(few, many), "units without a workgroup");
       need(h.counters >= g.slots_few + g.slots_many, "counters");
-      need(g.grid <= g.slots_few + g.slots_many, "slices without a place");
+      need(g.slots_few + g.slots_many <= 4 * g.workgroups, "more places than slices");
       need(h.workspace_floats >= g.slots_few * sk::part_floats(sk::ROWS_FEW, g.wide ? 256 : 128) + g.slots_many * sk::part_floats(sk::ROWS_MANY, g.wide ? 256 : 128), "workspace");
     }
   }

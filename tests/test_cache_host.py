@@ -40,7 +40,7 @@ INVALID, UNSUPPORTED, OVERLAP = -1, -2, -3
 REFUSALS = [
     (dict(dtype="f32"), UNSUPPORTED), (dict(dtype=7), UNSUPPORTED), (dict(head_dim=60), UNSUPPORTED), (dict(head_dim=264), UNSUPPORTED), (dict(head_dim=0), INVALID),
     (dict(q_heads=0), INVALID), (dict(kv_heads=0), INVALID), (dict(q_heads=7), INVALID), (dict(page_tokens=8), UNSUPPORTED), (dict(page_tokens=48), UNSUPPORTED),
-    (dict(page_tokens=1 << 17), UNSUPPORTED), (dict(page_tokens=0), INVALID), (dict(num_pages=0), INVALID), (dict(sequences=-1), INVALID),
+    (dict(page_tokens=1 << 17), UNSUPPORTED), (dict(page_tokens=0), INVALID), (dict(num_pages=0), INVALID), (dict(sequences=-1), INVALID), (dict(sequences=(1 << 20) + 1), UNSUPPORTED),
     (dict(pages_per_sequence=0), INVALID), (dict(pages_per_sequence=1 << 27, rotary_dim=0), UNSUPPORTED), (dict(rows=0), INVALID), (dict(max_new=-1), INVALID),
     (dict(window=-1), INVALID), (dict(sinks=-1), INVALID), (dict(reserved=1), INVALID), (dict(rotary_dim=63), INVALID), (dict(rotary_dim=66), INVALID),
     (dict(rotary_dim=-2), INVALID), (dict(neighbours=2), INVALID), (dict(positions=159), INVALID), (dict(cos=0), INVALID), (dict(sin=0), INVALID),
