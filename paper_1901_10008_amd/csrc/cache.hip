@@ -161,6 +161,9 @@ sk_status launch_copies(const sk_page_array *arrays, int32_t n_arrays, const sk:
   sk::CopyArgs a;
   a.table = table;
   a.columns = columns;
+  int64_t bytes = 0;
+  for (int32_t i = 0; i < n_arrays; ++i) bytes += arrays[i].page_bytes;
+  void (*const kernel)(sk::CopyArgs) = (double)bytes * 2.0 * (double)n_moves > (double)sk::PAST_CACHES ? sk::sk_copy_pages<true> : sk::sk_copy_pages<false>;
   for (int32_t a0 = 0;; a0 += sk::COPY_ARRAYS) {
     a.n_arrays = n_moves ? std::max(0, std::min(n_arrays - a0, sk::COPY_ARRAYS)) : 0;
     a.chunks = 0;
@@ -186,14 +189,14 @@ sk_status launch_copies(const sk_page_array *arrays, int32_t n_arrays, const sk:
       if (copies + a.n_rows >= (int64_t)1 << 31) return set_last_error(SK_ERR_UNSUPPORTED, "pages too large for a launch's grid");
       const bool alone = last && n_rows && !with_rows;
       if (copies + a.n_rows) {
-        const sk_status st = launch(sk::sk_copy_pages, copies + a.n_rows, stream, last && !alone ? behind : nullptr, a);
+        const sk_status st = launch(kernel, copies + a.n_rows, stream, last && !alone ? behind : nullptr, a);
         if (st != SK_OK) return st;
       }
       if (alone) {
         a.n_arrays = a.n_moves = 0;
         a.n_rows = n_rows;
         put(a.words);
-        return launch(sk::sk_copy_pages, n_rows, stream, behind, a);
+        return launch(kernel, n_rows, stream, behind, a);
       }
       if (m0 + sk::COPY_MOVES >= n_moves) break;
     }
@@ -281,7 +284,7 @@ sk_status sk_attn_append(sk_attn_plan *plan, void *hip_stream) {
     const sk::AppendArgs a{plan->problems, plan->append_first, (int32_t)plan->host.problems.size()};
     // It writes nothing of the plan's, so no later launch has to wait for it, only the plan's end (for the device: an event with
     // the launch makes who waits for the device behind it wait up to 10 us longer).
-    st = launch(sk::sk_append, (int64_t)plan->host.append_first.back(), stream, nullptr, a);
+    st = launch(plan->host.append_once ? sk::sk_append<true> : sk::sk_append<false>, (int64_t)plan->host.append_first.back(), stream, nullptr, a);
     plan->appended = true;
     return st;
   });

@@ -21,6 +21,7 @@ constexpr int ROWS_FEW = 16, ROWS_MANY = 128;
 constexpr int most_few(int dim) { return dim > 64 && dim <= 128 ? 16 : 32; }
 constexpr int KEYS_FEW = 32;                                  // keys per step
 constexpr int keys_many(int dim) { return dim <= 128 ? 64 : 32; }  // (heads of 256: what a thread has in flight has to fit its registers)
+constexpr int64_t PAST_CACHES = (int64_t)160 << 20;  // bytes that a launch reads and writes (the last-level cache holds 256 MiB)
 constexpr int APPEND_WAVES = 8192;  // append: a problem's rows are cut into parts for at least that many waves where they have the heads for it
 constexpr int MOST_SPLITS = 256;              // workgroups that share a unit's keys, at most
 
@@ -62,6 +63,7 @@ struct AttnPlanHost {
   std::vector<AttnSeq> seqs;
   std::vector<AttnGroup> groups;
   std::vector<uint32_t> append_first;  // first workgroup of each problem, and the number of all
+  bool append_once = false;            // append moves more than PAST_CACHES bytes
   bool any_qkv = false, all_qkv = true, any_out = false, all_out = true;
   int64_t workspace_floats = 0, counters = 0;  // of the largest group: launches of a plan do not overlap
 };

@@ -132,6 +132,9 @@ sk_status plan_attn(const sk_attn_problem *problems, int32_t n, int32_t compute_
     out.append_first.push_back((uint32_t)append_grid);
     out.problems.push_back(d);
   }
+  int64_t moved = 0;
+  for (const AttnDev &d : out.problems) moved += d.qkv ? 4 * (int64_t)d.rows * (d.q_heads + 2 * (int64_t)d.kv_heads) * d.dim : 0;
+  out.append_once = moved > PAST_CACHES;
   std::sort(written.begin(), written.end());
   for (size_t i = 1; i < written.size(); ++i)
     if (written[i].first < written[i - 1].second) return refuse(err, SK_ERR_OVERLAP, "ranges of q and out overlap");

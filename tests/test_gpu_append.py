@@ -130,6 +130,20 @@ def test_copies(sizes):
         assert torch.equal(x, w)
 
 
+def test_launches_that_go_past_the_caches():
+    """More than 160 MiB in a launch: copies, and an append whose rows have room for as much."""
+    n = 50
+    x = torch.randint(0, 256, (n, 4 << 20), dtype=torch.uint8, device="cuda")
+    want = x.clone()
+    frm, to = list(range(0, 25)), list(range(25, 50))
+    want[to] = want[frm]
+    sk.sk_pages_copy(arrays_of([x]), n, frm, to, H.stream_handle())
+    torch.cuda.synchronize()
+    assert torch.equal(x, want)
+    t = tenant("bf16", (32, 8, 128), ((130, 100), (20, 20)), rotary=128, spare_rows=8000, seed=4)
+    check_append([t], "past the caches")
+
+
 def test_more_arrays_and_copies_than_a_launch_holds():
     n, g = 2001, torch.Generator().manual_seed(1)
     tensors = [torch.randint(0, 256, (n, 32), dtype=torch.uint8, device="cuda") for _ in range(150)]
