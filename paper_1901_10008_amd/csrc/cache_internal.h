@@ -8,6 +8,7 @@
 #include <vector>
 
 #include "sk_cache.h"
+#include "sk_internal.h"
 
 namespace sk {
 
@@ -38,6 +39,7 @@ struct AttnDev {
   // append: a wave takes `parts`-th of a row's heads, `heads_at_once` (of 8 elements a lane) in each of `turns`
   int32_t lanes_per_head, turns, parts;
   int32_t pad;
+  FastDiv by_group;  // divides by `group`
 };
 
 // A sequence of a launch: what a workgroup needs to know of it to count its units.

@@ -170,7 +170,7 @@ __device__ __forceinline__ Span span_of(int32_t p0, int32_t p1, int32_t window, 
 }
 
 struct Count {
-  int32_t units, blocks;  // blocks of keys of an average unit
+  int32_t row_blocks, units, blocks;  // blocks of keys of an average unit
   bool many;
 };
 template <bool MANY, bool WIDE>
@@ -181,16 +181,17 @@ __device__ __forceinline__ Count count_units(const Step &s, const AttnSeq &q) {
   const int32_t last = s.behind + s.fresh - 1;
   c.many = MANY && rows > q.most_few;
   if (c.many) {
-    c.units = (int32_t)((rows + ROWS_MANY - 1) / ROWS_MANY) * kv_heads;
-    const int32_t tokens = (ROWS_MANY + group - 1) / group;
+    c.row_blocks = (int32_t)((rows + ROWS_MANY - 1) / ROWS_MANY);
+    const int32_t tokens = (int32_t)((uint32_t)(ROWS_MANY + group - 1) / (uint32_t)group);
     constexpr int KEYS = keys_many(WIDE ? 256 : 128);
     const Span a = span_of<KEYS>(s.behind, min(s.behind + tokens - 1, last), window, sinks);
     const Span b = span_of<KEYS>(max(last - tokens + 1, s.behind), last, window, sinks);
     c.blocks = (a.blocks + b.blocks + 1) / 2;
   } else {
-    c.units = (int32_t)((rows + ROWS_FEW - 1) / ROWS_FEW) * kv_heads;
+    c.row_blocks = (int32_t)((rows + ROWS_FEW - 1) / ROWS_FEW);
     c.blocks = span_of<KEYS_FEW>(s.behind, last, window, sinks).blocks;
   }
+  c.units = c.row_blocks * kv_heads;
   return c;
 }
 
@@ -214,17 +215,25 @@ struct AttnArgs {
   uint32_t *arrivals;  // slots_many, then as many as there are for few; zero between launches
 };
 
+// n / d for 0 <= n < 2^52 and d > 0: the rounded quotient of the exact values does not reach the next whole number, which is 1 / d away or more.
+// (Whole numbers of 64 bits take the compiler a hundred instructions more.)
+__device__ __forceinline__ int64_t divide(int64_t n, int64_t d) { return (int64_t)((double)n / (double)d); }
+// The first of `blocks` that slice number `split` of a unit takes.
+__device__ __forceinline__ int32_t slice_start(int32_t blocks, int32_t split, int32_t splits) { return splits == 1 ? split * blocks : (int32_t)divide((int64_t)blocks * split, splits); }
+// n / d for 0 <= n < 2^31.
+__device__ __forceinline__ int32_t fast_div(int32_t n, FastDiv d) { return (int32_t)((uint64_t)(uint32_t)n * d.mul >> d.shift); }
+
 // Units of many keys are cut into slices, so that few units fill the card and no unit is what the launch waits for.  A slice takes at most `most`
 // blocks of keys of few rows, or half as many tiles of many (which take twice as long).
 constexpr int LEAST = 4;  // a block for each wave; tiles
 __device__ __forceinline__ int32_t splits_of(const Count &c, int32_t most) {
-  const int32_t per = max(c.many ? (most + 1) / 2 : most, LEAST);
-  return min((int32_t)(((int64_t)max(c.blocks, 1) + per - 1) / per), MOST_SPLITS);
+  const uint32_t per = (uint32_t)max(c.many ? (most + 1) / 2 : most, LEAST);
+  return (int32_t)min(((uint32_t)max(c.blocks, 1) + per - 1) / per, (uint32_t)MOST_SPLITS);
 }
 // work: blocks of few rows and twice the tiles of many.  That many for each workgroup the card runs at a time: with it units and slices
 // are no more than these workgroups and the units together, and the slices of units that are cut (each of more than `most`) no more than twice
 // these workgroups.
-__device__ __forceinline__ int32_t even_share(int64_t work, int64_t workgroups) { return (int32_t)min((work + workgroups - 1) / workgroups, (int64_t)0x7ffffffe); }
+__device__ __forceinline__ int32_t even_share(int64_t work, int64_t workgroups) { return (int32_t)min(divide(work + workgroups - 1, workgroups), (int64_t)0x7ffffffe); }
 
 struct FindScratch {
   int64_t work[4];  // per wave
@@ -234,14 +243,14 @@ struct FindScratch {
 
 // Unit number i of a sequence's, whose slices have the places from `slot` on.
 __device__ __forceinline__ Unit unit_of(const AttnSeq &q, const Step &s, const Count &c, int32_t splits, int32_t i, int32_t slot) {
-  const int32_t rest = i / q.kv_heads;
+  const int32_t rest = (int32_t)((uint32_t)i / (uint32_t)q.kv_heads), block = (int32_t)((uint32_t)rest / (uint32_t)splits);
   Unit u;
   u.problem = q.problem;
   u.seq = q.seq;
-  u.head = i % q.kv_heads;
-  u.split = rest % splits;
+  u.head = i - rest * q.kv_heads;
+  u.split = rest - block * splits;
   u.splits = splits;
-  u.block = c.units / q.kv_heads - 1 - rest / splits;
+  u.block = c.row_blocks - 1 - block;
   u.slot = (uint32_t)(slot + i);
   u.first_slot = (uint32_t)(slot + i - u.split * q.kv_heads);
   u.step = s;
@@ -278,7 +287,7 @@ __device__ __forceinline__ Unit find_unit(const AttnArgs &a, FindScratch *f) {
     AttnSeq q{};
     q.kv_heads = 1;
     Step s{};
-    Count c{0, 0, false};
+    Count c{0, 0, 0, false};
     if (lane < a.sequences) {
       q = a.seqs[lane];
       s = step_of(q);
@@ -322,7 +331,7 @@ __device__ __forceinline__ Unit find_unit(const AttnArgs &a, FindScratch *f) {
   const int s0 = tid * per_thread, s1 = min(s0 + per_thread, a.sequences);
   AttnSeq q{};
   Step s{};
-  Count c{0, 0, false};
+  Count c{0, 0, 0, false};
   auto look = [&](int i) {
     q = a.seqs[i];
     s = step_of(q);
@@ -543,11 +552,12 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, const SK_CONSTANT 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
   const Step &st = u.step;
   const int32_t row0 = u.block * ROWS_FEW, rows = min(ROWS_FEW, st.fresh * P.group - row0);
-  const int32_t p0 = st.behind + row0 / P.group, p1 = st.behind + (row0 + rows - 1) / P.group;
+  const FastDiv by_group = {P.by_group.mul, P.by_group.shift};
+  const int32_t p0 = st.behind + fast_div(row0, by_group), p1 = st.behind + fast_div(row0 + rows - 1, by_group);
   const int32_t window = P.window, sinks = P.sinks, dim = P.dim;
   const Span span = span_of<KEYS_FEW>(p0, p1, window, sinks);
   const bool two_spans = window && sinks > span.low;  // a row may see two runs of keys in a block
-  const int32_t b0 = (int32_t)((int64_t)span.blocks * u.split / u.splits), b1 = (int32_t)((int64_t)span.blocks * (u.split + 1) / u.splits);
+  const int32_t b0 = slice_start(span.blocks, u.split, u.splits), b1 = slice_start(span.blocks, u.split + 1, u.splits);
 
   const Pages pages{P.table + (int64_t)u.seq * P.columns, P.page_shift, P.num_pages, P.columns, P.page_stride, P.token_stride};
   const char *kh = (const char *)P.k + 2 * (int64_t)u.head * P.head_stride, *vh = (const char *)P.v + 2 * (int64_t)u.head * P.head_stride;
@@ -620,7 +630,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, const SK_CONSTANT 
   }
 
   const int32_t my_row = row0 + min(c, rows - 1);
-  const int32_t my_token = my_row / P.group, my_head = u.head * P.group + my_row % P.group;
+  const int32_t my_token = fast_div(my_row, by_group), my_head = u.head * P.group + my_row - my_token * P.group;
   const int32_t my_pos = c < rows ? st.behind + my_token : -1;
   const char *q = (const char *)P.q + 2 * ((int64_t)(st.first + my_token) * P.q_row + (int64_t)my_head * P.q_head);
   const float scale = fabsf(P.scale_log2);  // (its sign goes into the queries)
@@ -759,7 +769,8 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, const SK_CONSTANT 
     if (u.splits == 1) {
       const float inv = inverse(sum);
       const int32_t row = row0 + r;
-      char *dst = (char *)P.out + 2 * ((int64_t)(st.first + row / P.group) * P.out_row + (int64_t)(u.head * P.group + row % P.group) * P.out_head + e);
+      const int32_t token = fast_div(row, by_group);
+      char *dst = (char *)P.out + 2 * ((int64_t)(st.first + token) * P.out_row + (int64_t)(u.head * P.group + row - token * P.group) * P.out_head + e);
       if (e < P.dim) store8(dst, u32x2{pack2<DT>(v.x * inv, v.y * inv), pack2<DT>(v.z * inv, v.w * inv)});
     } else {
       store_shared(ws + r * DP + e, f32x2{v.x, v.y});
@@ -796,7 +807,8 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, const SK_CONSTANT 
     }
     const float inv = inverse(sum);
     const int32_t row = row0 + r;
-    char *dst = (char *)P.out + 2 * ((int64_t)(st.first + row / P.group) * P.out_row + (int64_t)(u.head * P.group + row % P.group) * P.out_head + e);
+    const int32_t token = fast_div(row, by_group);
+    char *dst = (char *)P.out + 2 * ((int64_t)(st.first + token) * P.out_row + (int64_t)(u.head * P.group + row - token * P.group) * P.out_head + e);
     if (e < P.dim) store8(dst, u32x2{pack2<DT>(v.x * inv, v.y * inv), pack2<DT>(v.z * inv, v.w * inv)});
   }
 }
@@ -844,10 +856,11 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
   const Step &st = u.step;
   const int32_t group = P.group, dim = P.dim, window = P.window, sinks = P.sinks;
   const int32_t row0 = u.block * ROWS_MANY, rows = min(ROWS_MANY, st.fresh * group - row0);
-  const int32_t p0 = st.behind + row0 / group, p1 = st.behind + (row0 + rows - 1) / group;
+  const FastDiv by_group = {P.by_group.mul, P.by_group.shift};
+  const int32_t p0 = st.behind + fast_div(row0, by_group), p1 = st.behind + fast_div(row0 + rows - 1, by_group);
   const Span span = span_of<KEYS>(p0, p1, window, sinks);
   const bool two_spans = window && sinks > span.low;  // a row may see two runs of keys in a tile
-  const int32_t b0 = (int32_t)((int64_t)span.blocks * u.split / u.splits), b1 = (int32_t)((int64_t)span.blocks * (u.split + 1) / u.splits);
+  const int32_t b0 = slice_start(span.blocks, u.split, u.splits), b1 = slice_start(span.blocks, u.split + 1, u.splits);
 
   const Pages pages{P.table + (int64_t)u.seq * P.columns, P.page_shift, P.num_pages, P.columns, P.page_stride, P.token_stride};
   const char *kh = (const char *)P.k + 2 * (int64_t)u.head * P.head_stride, *vh = (const char *)P.v + 2 * (int64_t)u.head * P.head_stride;
@@ -926,11 +939,11 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
   const int32_t in_block = wave * 32 + c;
   const bool row_ok = in_block < rows;
   const int32_t my_row = row0 + min(in_block, rows - 1);
-  const int32_t my_token = my_row / group, my_head = u.head * group + my_row % group;
+  const int32_t my_token = fast_div(my_row, by_group), my_head = u.head * group + my_row - my_token * group;
   const int32_t my_pos = row_ok ? st.behind + my_token : -1;
   // positions of the wave's rows (uniform)
   const bool wave_ok = wave * 32 < rows;
-  const int32_t w0 = st.behind + (row0 + min(wave * 32, rows - 1)) / group, w1 = st.behind + (row0 + min(wave * 32 + 31, rows - 1)) / group;
+  const int32_t w0 = st.behind + fast_div(row0 + min(wave * 32, rows - 1), by_group), w1 = st.behind + fast_div(row0 + min(wave * 32 + 31, rows - 1), by_group);
   const char *q = (const char *)P.q + 2 * ((int64_t)(st.first + my_token) * P.q_row + (int64_t)my_head * P.q_head);
   const float scale = fabsf(P.scale_log2);  // (its sign goes into the queries)
   u32x4 qf[KS];

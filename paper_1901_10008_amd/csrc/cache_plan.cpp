@@ -94,6 +94,7 @@ sk_status check_problem(const sk_attn_problem &p, AttnDev &d, std::string &err) 
       return refuse(err, SK_ERR_INVALID_ARG, "cos and sin have fewer rows than a sequence can have tokens");
   }
   d.dtype = p.dtype, d.q_heads = p.q_heads, d.kv_heads = p.kv_heads, d.group = p.q_heads / p.kv_heads, d.dim = p.head_dim;
+  d.by_group = fast_div_of((uint32_t)d.group);
   while ((1 << d.page_shift) < p.page_tokens) ++d.page_shift;
   d.num_pages = p.num_pages, d.columns = p.pages_per_sequence, d.sequences = p.sequences, d.rows = p.rows;
   d.max_new = p.max_new && p.max_new < p.rows ? p.max_new : p.rows;
