@@ -21,7 +21,7 @@ constexpr int ROWS_FEW = 16, ROWS_MANY = 128;
 // of 256 on 8000, 24 rows, 40 and 69.
 constexpr int most_few(int dim) { return dim > 64 && dim <= 128 ? 16 : 32; }
 constexpr int KEYS_FEW = 32;                                  // keys per step
-constexpr int keys_many(int dim) { return dim <= 128 ? 64 : 32; }  // (heads of 256: what a thread has in flight has to fit its registers)
+constexpr int keys_many(int dim) { return dim <= 128 ? 64 : 32; }  // keys of a tile (heads of 256: two tiles of 64 would take 128 KB of LDS and 64 more registers)
 constexpr int64_t PAST_CACHES = (int64_t)160 << 20;  // bytes that a launch reads and writes (the last-level cache holds 256 MiB)
 constexpr int APPEND_WAVES = 8192;  // append: a problem's rows are cut into parts for at least that many waves where they have the heads for it
 constexpr int MOST_SPLITS = 256;              // workgroups that share a unit's keys, at most

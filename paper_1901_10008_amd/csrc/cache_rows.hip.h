@@ -69,7 +69,8 @@ enum { ROTATE_NONE, ROTATE_HALVES, ROTATE_NEIGHBOURS, ROTATE_ANY };
 
 // A wave takes some heads of a row, 8 elements a lane, in turns of as many heads as it has lanes for.  What a lane needs of the angles and weights is
 // the same in every turn and stays in registers; the other element of a pair is read from memory once more (the line is in the L1)
-// and normalised like the first.
+// and normalised like the first.  Bound by memory: every element is read and written once; 19000 rows of 48 heads of 128, 469 MB in 97 us,
+// 4.8 TB/s (a large copy 5.15).  A step of few rows is bound by a launch and its chain of loads (row, sequence, page, heads): 3 rows 3.7 us.
 template <int DT, int ROTATE, bool ONCE>
 __device__ __forceinline__ void append_heads(const SK_CONSTANT AttnDev &P, int64_t row, int32_t part, int lane, int64_t angle, bool there, int64_t slot) {
   const int lph = P.lanes_per_head, e0 = (lane & (lph - 1)) * 8, at_once = 64 / lph, dim = P.dim, half = P.rotary / 2;
@@ -108,7 +109,7 @@ __device__ __forceinline__ void append_heads(const SK_CONSTANT AttnDev &P, int64
       }
     }
   }
-    u32x4 raw, pair;  // of the next turn
+  u32x4 raw, pair;  // of the next turn
   const int first = part * P.turns * at_once + lane / lph;
   auto load = [&](int t, u32x4 &v, u32x4 &w) {
     const int head = first + t * at_once;
@@ -233,7 +234,7 @@ __global__ void __launch_bounds__(CACHE_THREADS) sk_append(AppendArgs a) {
 // ---------------------------------------------------------------------------
 // copies of pages
 // ---------------------------------------------------------------------------
-// A workgroup copies a chunk of a page of an array; those behind the copies bring changed rows of the page table, out of the launch's arguments
+// Bound by memory: 500 pages of 32 KB in each of 32 arrays, 1.05 GB read and written in 210 us, 5.0 TB/s.  A workgroup copies a chunk of a page of an array; those behind the copies bring changed rows of the page table, out of the launch's arguments
 // where they fit (a fork into sixteen sequences of 50 pages: 4.2 us so, 6.0 with the rows in host memory).
 template <bool ONCE>
 __global__ void __launch_bounds__(CACHE_THREADS) sk_copy_pages(CopyArgs a) {
