@@ -174,7 +174,7 @@ def make_ids(numbers: Iterable[int]):
 
 
 def _ids(numbers):
-    return numbers if isinstance(numbers, C.Array) else make_ids(numbers)
+    return numbers if isinstance(numbers, C.Array) and numbers._type_ is C.c_int32 else make_ids(numbers)
 
 
 def make_page_arrays(arrays):

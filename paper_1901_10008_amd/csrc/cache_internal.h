@@ -114,7 +114,7 @@ class PageAccount {
   const int32_t *row(int32_t s) const { return table_.data() + (size_t)s * columns_; }
 
  private:
-  int32_t held(int32_t tokens) const { return (int32_t)(((int64_t)tokens + page_tokens_ - 1) / page_tokens_); }
+  int32_t held(int32_t tokens) const { return (int32_t)(((uint32_t)tokens + (uint32_t)page_tokens_ - 1) / (uint32_t)page_tokens_); }
   int32_t take();
   void give(int32_t page);
   void move(int32_t from, int32_t to);

@@ -237,3 +237,19 @@ def test_no_kernel_spills_or_has_a_stack():
     n = 8  # four of attention, two each of append and copies
     assert len(_all(blob, b".vgpr_count")) == n
     assert _all(blob, b".vgpr_spill_count") == [0] * n and _all(blob, b".private_segment_fixed_size") == [0] * n
+
+
+def test_ids_of_any_kind():
+    """Lists, iterators and arrays of other types mean the numbers in them; tokens up to the last that an account can hold."""
+    with sk.sk_pages_create(60, 16, 4, 20) as pages:
+        sk.sk_pages_resize(pages, [0], (ctypes.c_int64 * 1)(33))
+        sk.sk_pages_fork(pages, 0, (ctypes.c_int16 * 2)(1, 3))
+        assert [sk.sk_pages_state(pages, s)[0] for s in range(4)] == [33, 33, 0, 33]
+        assert sk.sk_pages_state(pages) == (57, 0)
+        sk.sk_pages_resize(pages, [1, 3], sk.make_ids(n for n in (34, 0)))
+        assert [sk.sk_pages_state(pages, s)[0] for s in range(4)] == [33, 34, 0, 0]
+        assert sk.sk_pages_state(pages) == (56, 1)
+    with sk.sk_pages_create(32768, 65536, 1, 32768) as pages:
+        sk.sk_pages_resize(pages, [0], [2**31 - 1])
+        assert sk.sk_pages_state(pages) == (0, 0)
+        assert sk.sk_pages_state(pages, 0)[1] == list(range(32768))
