@@ -249,7 +249,7 @@ def test_ids_of_any_kind():
         sk.sk_pages_resize(pages, [1, 3], sk.make_ids(n for n in (34, 0)))
         assert [sk.sk_pages_state(pages, s)[0] for s in range(4)] == [33, 34, 0, 0]
         assert sk.sk_pages_state(pages) == (56, 1)
-    with sk.sk_pages_create(32768, 65536, 1, 32768) as pages:
-        sk.sk_pages_resize(pages, [0], [2**31 - 1])
+    with sk.sk_pages_create(32767, 65536, 1, 32767) as pages:  # one page more would be 2^31 tokens, which are refused
+        sk.sk_pages_resize(pages, [0], [2**31 - 65536])
         assert sk.sk_pages_state(pages) == (0, 0)
-        assert sk.sk_pages_state(pages, 0)[1] == list(range(32768))
+        assert sk.sk_pages_state(pages, 0)[1] == list(range(32767))
