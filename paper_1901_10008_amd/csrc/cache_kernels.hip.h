@@ -224,13 +224,15 @@ __device__ __forceinline__ int32_t slice_start(int32_t blocks, int32_t split, in
 __device__ __forceinline__ int32_t fast_div(int32_t n, FastDiv d) { return (int32_t)((uint64_t)(uint32_t)n * d.mul >> d.shift); }
 
 // Units of many keys are cut into slices, so that few units fill the card and no unit is what the launch waits for.  A slice takes at most `most`
-// blocks of keys of few rows, or half as many tiles of many (which take twice as long).
+// blocks of keys of few rows, or a TILE_WORK-th as many tiles of many: a tile takes 2 us, a block 0.5 where memory is not what bounds it (chunks beside
+// single tokens, twelve sequences: 56.9 us with a ratio of 2, 55.2 of 4 and of 6; launches of one kind do not care).
+constexpr int TILE_WORK = 4;
 constexpr int LEAST = 4;  // a block for each wave; tiles
 __device__ __forceinline__ int32_t splits_of(const Count &c, int32_t most) {
-  const uint32_t per = (uint32_t)max(c.many ? (most + 1) / 2 : most, LEAST);
+  const uint32_t per = max(c.many ? ((uint32_t)most + TILE_WORK - 1) / TILE_WORK : (uint32_t)most, (uint32_t)LEAST);
   return (int32_t)min(((uint32_t)max(c.blocks, 1) + per - 1) / per, (uint32_t)MOST_SPLITS);
 }
-// work: blocks of few rows and twice the tiles of many.  That many for each workgroup the card runs at a time: with it units and slices
+// work: blocks of few rows and TILE_WORK times the tiles of many.  That many for each workgroup the card runs at a time: with it units and slices
 // are no more than these workgroups and the units together, and the slices of units that are cut (each of more than `most`) no more than twice
 // these workgroups.
 __device__ __forceinline__ int32_t even_share(int64_t work, int64_t workgroups) { return (int32_t)min(divide(work + workgroups - 1, workgroups), (int64_t)0x7ffffffe); }
@@ -294,7 +296,7 @@ __device__ __forceinline__ Unit find_unit(const AttnArgs &a, FindScratch *f) {
       c = count_units<MANY, WIDE>(s, q);
     }
     const int32_t units = lane_of(wave_scan(c.units), 63);
-    const int64_t work = lane_of(wave_scan((int64_t)c.units * c.blocks * (c.many ? 2 : 1)), 63);
+    const int64_t work = lane_of(wave_scan((int64_t)c.units * c.blocks * (c.many ? TILE_WORK : 1)), 63);
     int32_t most = even_share(work, a.workgroups), splits = splits_of(c, most);
     // Few units: slices as short as leaves all of them running at once.  (A slice costs its workgroup 5 us besides the keys: six caches
     // of 50 to 120 thousand tokens take 271 us in one round of slices, 281 in two, 288 in four.)
@@ -340,7 +342,7 @@ __device__ __forceinline__ Unit find_unit(const AttnArgs &a, FindScratch *f) {
   int64_t work = 0;
   for (int i = s0; i < s1; ++i) {
     look(i);
-    work += (int64_t)c.units * c.blocks * (c.many ? 2 : 1);
+    work += (int64_t)c.units * c.blocks * (c.many ? TILE_WORK : 1);
   }
   work = lane_of(wave_scan(work), 63);
   if (lane == 0) f->work[wave] = work;
@@ -1133,7 +1135,7 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
     if (!wave_ok) return;
     const float *ws0 = a.ws_many + (int64_t)u.first_slot * SLOT;
     const int64_t step = (int64_t)P.kv_heads * SLOT;
-    // maximum and sum first, then the outputs, a block of 32 elements of a slice after the other with the next one's loads out
+    // maximum and sum first, then the outputs, slice after slice, the next one's loads out
     m = -__builtin_inff();
     l = 0.f;
     constexpr int AT_ONCE = 8;
@@ -1155,34 +1157,32 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
 #pragma unroll
       for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
     const float base = base_of(m);
-    f32x2 x[2][8], ms[2];
-    auto read = [&](int s, int i, int to) {
+    f32x2 x[NB][8];
+    float ms[2];
+    auto read_max = [&](int s) { return load_shared(ws0 + min(s, u.splits - 1) * step + ROWS_MANY * DP + 2 * in_block).x; };
+    auto read = [&](int s, int i) {
       const float *w = ws0 + min(s, u.splits - 1) * step;
-      ms[to] = load_shared(w + ROWS_MANY * DP + 2 * in_block);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[to][j] = load_shared(w + ((wave * NB + i) * 8 + j) * 128 + 2 * lane);
+      for (int j = 0; j < 8; ++j) x[i][j] = load_shared(w + ((wave * NB + i) * 8 + j) * 128 + 2 * lane);
       fixed_order();
     };
-    auto add = [&](int i, int from) {
-      const float mul = exp2_fast(ms[from].x - base);
+    ms[0] = read_max(0);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        o[i][2 * j] += x[from][j].x * mul;
-        o[i][2 * j + 1] += x[from][j].y * mul;
-      }
-      fixed_order();
-    };
-    static_assert(NB >= 2, "two blocks at least");
-    read(0, 0, 0);
+    for (int i = 0; i < NB; ++i) read(0, i);
     for (int s = 0; s < u.splits; ++s) {
-      // (an odd number of blocks leaves the places in another order behind each slice: then the last block's place is used twice)
+      ms[1] = read_max(s + 1);
+      const float mul = exp2_fast(ms[0] - base);
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
-        if (i + 1 < NB) read(s, i + 1, (i + 1) & 1);
-        else if (NB % 2 == 0) read(s + 1, 0, 0);
-        add(i, i & 1);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          o[i][2 * j] += x[i][j].x * mul;
+          o[i][2 * j + 1] += x[i][j].y * mul;
+        }
+        fixed_order();
+        read(s + 1, i);
       }
-      if (NB % 2) read(s + 1, 0, 0);
+      ms[0] = ms[1];
     }
   }
   if (!row_ok) return;
