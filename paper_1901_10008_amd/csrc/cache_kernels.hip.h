@@ -224,9 +224,9 @@ __device__ __forceinline__ int32_t slice_start(int32_t blocks, int32_t split, in
 __device__ __forceinline__ int32_t fast_div(int32_t n, FastDiv d) { return (int32_t)((uint64_t)(uint32_t)n * d.mul >> d.shift); }
 
 // Units of many keys are cut into slices, so that few units fill the card and no unit is what the launch waits for.  A slice takes at most `most`
-// blocks of keys of few rows, or a TILE_WORK-th as many tiles of many: a tile takes 2 us, a block 0.5 where memory is not what bounds it (chunks beside
-// single tokens, twelve sequences: 56.9 us with a ratio of 2, 55.2 of 4 and of 6; launches of one kind do not care).
-constexpr int TILE_WORK = 4;
+// blocks of keys of few rows, or a TILE_WORK-th as many tiles of many: a tile takes 2 us, a block 0.5 to 1 (chunks beside single tokens, twelve
+// sequences: 58.1 us with a ratio of 2, 55.5 of 3, 58.8 of 4; launches of one kind do not care).
+constexpr int TILE_WORK = 3;
 constexpr int LEAST = 4;  // a block for each wave; tiles
 __device__ __forceinline__ int32_t splits_of(const Count &c, int32_t most) {
   const uint32_t per = max(c.many ? ((uint32_t)most + TILE_WORK - 1) / TILE_WORK : (uint32_t)most, (uint32_t)LEAST);
