@@ -856,9 +856,9 @@ struct ManyLds {
 // above: a lane holds half the scores of one row, and P needs no trip through LDS.  Matrix instructions of 32x32x16, which need half the operand
 // bytes a product of the 16x16x32 ones.  Tiles come by direct loads into the other of two places while one is used; pieces are turned over
 // so that neither reads of keys nor the transposing reads of values meet in a bank (conflicts 0; 59 million without).  Operands are read from
-// LDS two groups of four ahead.  Bound by issue and power: prompts of 7000 to 8100 tokens, 32 query heads of 128, 963 us, 1003 TFLOP/s of the
-// pairs that are seen (a large library product 1483): the matrix units are busy 48 % of the cycles, LDS 24 %; leaving out the softmax,
-// either product or the loads in turn saves 10 to 20 % each.
+// LDS two groups of four ahead.  Bound by what a wave can issue, and power: prompts of 7000 to 8100 tokens, 32 query heads of 128, 967 us,
+// 1000 TFLOP/s of the pairs that are seen (a large library product 1483): 360 instructions a tile, 32 of them matrix instructions, one in about five
+// cycles; the matrix units are busy 48 % of the cycles, LDS 24 %.  Scores of the next tile beside the softmax of this one gave nothing.
 constexpr int SETS = 3;  // groups of LDS operands in registers: one in use, two on their way
 
 template <int DT, int DP>
