@@ -7,6 +7,7 @@
 #include <type_traits>
 
 #include "cache_internal.h"
+#include "cache_units.h"
 
 #if defined(__HIP_DEVICE_COMPILE__) && !defined(__gfx950__)
 #error "written for gfx950"
@@ -154,21 +155,6 @@ __device__ __forceinline__ Step step_of(const AttnSeq &q) {
   s.fresh = min(all, q.max_new);
   return s;
 }
-// The keys that rows at positions p0 .. p1 see: blocks of KEYS from `low` on (a multiple of 16), ahead of them blocks from 0 on for the sinks below
-// it.  The last of these may reach beyond `low`: of its keys only the first `sinks` of the span count.
-struct Span {
-  int32_t low, sinks, sink_blocks, blocks;
-};
-template <int KEYS>
-__device__ __forceinline__ Span span_of(int32_t p0, int32_t p1, int32_t window, int32_t sinks) {
-  Span s;
-  s.low = window ? (p0 >= window ? p0 - window + 1 : 0) & ~15 : 0;
-  s.sinks = min(sinks, s.low);
-  s.sink_blocks = (s.sinks + KEYS - 1) / KEYS;
-  s.blocks = p1 < 0 ? 0 : s.sink_blocks + (p1 - s.low) / KEYS + 1;
-  return s;
-}
-
 struct Count {
   int32_t row_blocks, units, blocks;  // blocks of keys of an average unit
   bool many;
@@ -427,8 +413,8 @@ struct Pages {
   int32_t shift, num_pages, columns;
   int64_t page_stride, token_stride;
   __device__ __forceinline__ int32_t page_of(int32_t key) const {  // (key the same in all lanes)
-    const int32_t c = key >> shift;
-    return c < columns ? ((const SK_CONSTANT int32_t *)(uintptr_t)row)[c] : -1;
+    const int32_t c = column_of(key, shift, columns);
+    return c >= 0 ? ((const SK_CONSTANT int32_t *)(uintptr_t)row)[c] : -1;
   }
   __device__ __forceinline__ bool there(int32_t page) const { return (uint32_t)page < (uint32_t)num_pages; }
   // Byte offset of a key.  Where its page is not there, of one in page 0, whose memory can be read: what is read there does not enter a result.
@@ -445,11 +431,6 @@ struct Pages {
 constexpr float RISE = 8.f;
 __device__ __forceinline__ float base_of(float m) { return m == -__builtin_inff() ? 0.f : m; }
 __device__ __forceinline__ float inverse(float sum) { return sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum); }  // (nothing seen: 0)
-
-// Whether the token at position p sees key j.  (No branches: a mask per element.)
-__device__ __forceinline__ bool sees(int32_t p, int32_t j, int32_t window, int32_t sinks) {
-  return (j <= p) & ((window == 0) | (p - j < window) | (j < sinks));
-}
 
 // Values that some rows of a unit see and others do not must not reach the others, whatever they are; finite ones do not (their
 // weight is 0), but 0 * inf is NaN.  Where a step's keys are not seen by all rows alike, values that are not finite are taken out
@@ -479,7 +460,7 @@ __device__ __forceinline__ f32x4 odd_sum(const Pages &pages, const char *v, int3
 #pragma unroll 1
   for (int32_t b = b0; b < b1; b += step)
 #pragma unroll 1
-    for (int32_t j = key_of(b), end = j + keys; j < end; ++j) {
+    for (int32_t i = 0, j = key_of(b); i < keys; ++i, j = key_behind(j, 1)) {
       const int32_t page = pages.page_of(j);
       if (!pages.there(page) || !sees(pos, j, window, sinks)) continue;
       const u32x2 w = *(const u32x2 SK_GLOBAL *)(uintptr_t)(v + pages.bytes(page, j));
@@ -571,7 +552,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, const SK_CONSTANT 
 
   const Pages pages{P.table + (int64_t)u.seq * P.columns, P.page_shift, P.num_pages, P.columns, P.page_stride, P.token_stride};
   const char *kh = (const char *)P.k + 2 * (int64_t)u.head * P.head_stride, *vh = (const char *)P.v + 2 * (int64_t)u.head * P.head_stride;
-  auto key_of = [&](int32_t b) { return b < span.sink_blocks ? b * KEYS_FEW : span.low + (b - span.sink_blocks) * KEYS_FEW; };
+  auto key_of = [&](int32_t b) { return block_key<KEYS_FEW>(span, b); };
   // Offsets of this lane's pieces of 16 keys.  Keys go into registers: pieces beyond the head's end are read from its start and count as zeros.
   // Values go into LDS (see dma), a wave's to a place of its own: there such pieces come as zeros.
   constexpr int VI = VH < 4 ? VH : 4;  // loads per statement
@@ -593,9 +574,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, const SK_CONSTANT 
     page[1] = pages.page_of(key0 + 16);
   };
   // whether all keys of a block are seen by all rows
-  auto all_see = [&](int32_t b, int32_t key0) {
-    return b < span.sink_blocks ? key0 + KEYS_FEW <= span.sinks : (key0 + KEYS_FEW - 1 <= p0) & ((window == 0) | (p1 - key0 < window));
-  };
+  auto all_see = [&](int32_t b, int32_t key0) { return all_see_block<KEYS_FEW>(span, b, key0, p0, p1, window); };
   auto load_keys = [&](int32_t b) {
     const int32_t key0 = key_of(b);
 #pragma unroll
@@ -622,8 +601,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, const SK_CONSTANT 
 #pragma unroll
           for (int n = 0; n < VI; ++n) {
             const int32_t j = key0 + 16 * half + (i + n) * (64 / SLOTS) + lane / SLOTS;
-            const bool ok = b < span.sink_blocks ? j < span.sinks : (j <= p1) & ((window == 0) | (p0 - j < window) | (j < sinks));
-            some[n] = ok ? some[n] : DMA_OUTSIDE;
+            some[n] = some_see(span, b, j, p0, p1, window, sinks) ? some[n] : DMA_OUTSIDE;
           }
         }
         dma<VI>(values, some, to + (half * VH + i) * 1024);
@@ -881,7 +859,7 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
 
   const Pages pages{P.table + (int64_t)u.seq * P.columns, P.page_shift, P.num_pages, P.columns, P.page_stride, P.token_stride};
   const char *kh = (const char *)P.k + 2 * (int64_t)u.head * P.head_stride, *vh = (const char *)P.v + 2 * (int64_t)u.head * P.head_stride;
-  auto key_of = [&](int32_t b) { return b < span.sink_blocks ? b * KEYS : span.low + (b - span.sink_blocks) * KEYS; };
+  auto key_of = [&](int32_t b) { return block_key<KEYS>(span, b); };
   // Where this lane's pieces come from, counted from the first of the block's 16 keys.  Pieces beyond the head's end come as zeros.
   const int32_t first_key = wave * ROWS, block = first_key / 16;  // of the wave, in a tile
   uint32_t ko[NI], vo[NI];
@@ -893,19 +871,17 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
     ko[i] = ke < dim ? at + 2 * ke : DMA_OUTSIDE;
     vo[i] = ve < dim ? at + 2 * ve : DMA_OUTSIDE;
   }
-  // Tiles f0 .. f0 + nf - 1: every row of the unit sees all of their keys.  What is decided for the others tile by tile is settled for these.
-  const int32_t f0 = span.sink_blocks + (window && p1 - window >= span.low ? (p1 - window - span.low) / KEYS + 1 : 0);
-  const int32_t f1 = span.sink_blocks + (p0 - span.low >= KEYS - 1 ? (p0 - span.low - (KEYS - 1)) / KEYS + 1 : 0);
-  const uint32_t nf = (uint32_t)max(f1 - f0, 0);
-  auto all_see = [&](int32_t b) { return (uint32_t)(b - f0) < nf; };
+  // Tiles of whose keys every row of the unit sees all.  What is decided for the others tile by tile is settled for these.
+  const WholeBlocks full = whole_blocks<KEYS>(span, p0, p1, window);
+  auto all_see = [&](int32_t b) { return (uint32_t)(b - full.first) < full.n; };
   int32_t next_key = key_of(b0), page = -1;  // first key of the tile that is brought next, and the page of the wave's keys in it
-  auto look = [&]() { page = pages.page_of(next_key + 16 * block); };
+  auto look = [&]() { page = pages.page_of(key_behind(next_key, 16 * block)); };
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds + wave * NI * 1024;
   uint32_t gone = 0;  // places where the wave's keys are not there
   auto bring = [&](int32_t b, int place) {
     const int32_t key0 = next_key;
     const bool there = pages.there(page);
-    const int64_t at = pages.bytes(page, key0 + 16 * block) - DMA_FRONT;
+    const int64_t at = pages.bytes(page, key_behind(key0, 16 * block)) - DMA_FRONT;
     const uint32_t to = lds0 + place * TILE;
     const int records = there ? (int)DMA_OUTSIDE : 0;
     dma<NI>(__builtin_amdgcn_make_buffer_rsrc((void *)(kh + at), 0, records, 0x00020000), ko, to);
@@ -917,9 +893,8 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
       uint32_t some[NI];
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        const int32_t j = key0 + first_key + i * (64 / SLOTS) + lane / SLOTS;
-        const bool ok = b < span.sink_blocks ? j < span.sinks : (j <= p1) & ((window == 0) | (p0 - j < window) | (j < sinks));
-        some[i] = ok ? vo[i] : DMA_OUTSIDE;
+        const int32_t j = key_behind(key0, first_key + i * (64 / SLOTS) + lane / SLOTS);
+        some[i] = some_see(span, b, j, p0, p1, window, sinks) ? vo[i] : DMA_OUTSIDE;
       }
       dma<NI>(values, some, to + VALUES);
     }
@@ -927,7 +902,7 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
       gone ^= 1u << place;
       lds[ManyLds<DP>::PRESENT + 4 * place + wave] = there;
     }
-    next_key = b + 1 == span.sink_blocks ? span.low : key0 + KEYS;
+    next_key = next_block_key<KEYS>(span, b, key0);
   };
   // Behind bring(b): the wave's pieces are there; values that are not finite are taken out where rows differ in what they see.
   bool cleaned = false;
@@ -992,13 +967,13 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
       look();
     }
     const int32_t key0 = this_key;
-    this_key = b + 1 == span.sink_blocks ? span.low : key0 + KEYS;
+    this_key = next_block_key<KEYS>(span, b, key0);
     // whether any row of the wave sees any of these keys, and whether all see all
     const bool sink = b < span.sink_blocks;
     bool use = true, all = true;
     if (!all_see(b)) {
-      use = wave_ok && (sink || (key0 <= w1 && (window == 0 || w0 - (key0 + KEYS - 1) < window || key0 < sinks)));
-      all = sink ? key0 + KEYS <= span.sinks : key0 + KEYS - 1 <= w0 && (window == 0 || w1 - key0 < window);
+      use = wave_ok && some_see_block<KEYS>(span, b, key0, w0, w1, window, sinks);
+      all = all_see_block<KEYS>(span, b, key0, w0, w1, window);
     }
     if (use) {
       constexpr uint32_t ALL = 0x01010101u;
@@ -1042,7 +1017,7 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
           for (int half = 0; half < HALVES; ++half)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              const int32_t key = 32 * half + 8 * (i / 4), j = key0 + key + 4 * h + i % 4;
+              const int32_t key = 32 * half + 8 * (i / 4), j = key_behind(key0, key + 4 * h + i % 4);
               const bool ok = ((now >> (8 * (key / ROWS)) & 1) != 0) & sees(sink ? 0x7fffffff : my_pos, j, sink ? 1 : window, sink ? span.sinks : sinks);
               s[half][i] = ok ? s[half][i] : -__builtin_inff();
             }

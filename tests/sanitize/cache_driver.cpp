@@ -1,10 +1,12 @@
-// Host code of the operators over paged caches (cache_plan.cpp) on seeded random plans and accounts, for a build with sanitizers.
+// Host code of the operators over paged caches (cache_plan.cpp, and the arithmetic of cache_units.h that the kernels share) on seeded random
+// plans, steps and accounts, for a build with sanitizers.
 #include <cstdio>
 #include <cstdlib>
 #include <random>
 #include <set>
 
 #include "cache_internal.h"
+#include "cache_units.h"
 
 static void need(bool ok, const char *what) {
   if (!ok) {
@@ -133,9 +135,64 @@ static void accounts(std::mt19937 &rng) {
   }
 }
 
+// The blocks of keys of a run of rows against the definition, in 64 bits: sequences of any length that a plan takes, the longest among them.
+template <int KEYS>
+static void blocks_of_keys(std::mt19937 &rng) {
+  auto pick = [&](int64_t lo, int64_t hi) { return lo + (int64_t)((((uint64_t)rng() << 32) | rng()) % (uint64_t)(hi - lo + 1)); };
+  for (int round = 0; round < 4000; ++round) {
+    const int shift = (int)pick(4, 16);
+    const int64_t most = ((int64_t)1 << 31 >> shift) - 1, columns = pick(0, 2) ? pick(std::max<int64_t>(1, most - 5), most) : pick(1, std::min<int64_t>(most, 100));
+    const int64_t capacity = columns << shift;
+    const int64_t p1 = pick(0, 3) ? pick(std::max<int64_t>(0, capacity - 200), capacity - 1) : pick(0, capacity - 1), p0 = p1 - pick(0, 127);
+    const int32_t window = (int32_t)(pick(0, 1) ? 0 : pick(0, 3) ? pick(1, 300) : pick(1, 0x7fffffff)), sinks = (int32_t)(pick(0, 1) ? pick(0, 70) : pick(0, 5) ? 0 : 0x7fffffff);
+    const sk::Span s = sk::span_of<KEYS>((int32_t)p0, (int32_t)p1, window, sinks);
+    auto row_sees = [&](int64_t p, int64_t j) { return j <= p && (window == 0 || p - j < window || j < sinks); };
+    need(s.low >= 0 && s.low % 16 == 0 && s.sink_blocks >= 0 && s.blocks > s.sink_blocks, "span");
+    for (int64_t j = std::max<int64_t>(0, p0); j <= p1; ++j) need(j >= s.low, "a key left out");
+    const int64_t first_seen = window ? std::max<int64_t>(0, p0 - window + 1) : 0;
+    need(s.low <= first_seen && (s.low == first_seen || s.low + 15 >= first_seen), "low");
+    need((int64_t)s.low + (int64_t)(s.blocks - s.sink_blocks) * KEYS > p1 && (int64_t)s.sink_blocks * KEYS >= s.sinks, "blocks");
+    const sk::WholeBlocks whole = sk::whole_blocks<KEYS>(s, (int32_t)p0, (int32_t)p1, window);
+    std::set<int32_t> some;
+    for (int i = 0; i < 3; ++i) some.insert({i, s.blocks - 1 - i, s.sink_blocks + i, s.sink_blocks - 1 - i, (int32_t)pick(0, s.blocks - 1)});
+    for (int32_t b : some) {
+      if (b < 0 || b >= s.blocks) continue;
+      const bool sink = b < s.sink_blocks;
+      const int64_t key = sink ? (int64_t)b * KEYS : s.low + (int64_t)(b - s.sink_blocks) * KEYS;
+      need(sk::block_key<KEYS>(s, b) == key, "a block's key");
+      // the block behind this one, which is looked up ahead, whether the rows need it or not
+      const int64_t behind = b + 1 == s.sink_blocks ? s.low : key + KEYS;
+      for (int i = 0; i < KEYS; i += 16) {
+        const int32_t c = sk::column_of(sk::key_behind(sk::next_block_key<KEYS>(s, b, (int32_t)key), i), shift, (int32_t)columns);
+        need(c == (behind + i < capacity ? (behind + i) >> shift : -1), "a column outside the table");
+      }
+      bool all = true, any = false, all_there = true;
+      for (int i = 0; i < KEYS; ++i) {
+        const int64_t j = key + i;
+        bool every = j < capacity, one = false;
+        for (int64_t p : {p0, p1, std::min(p0 + 1, p1), std::max(p1 - 1, p0), (p0 + p1) / 2}) {
+          const bool here = sink ? j < s.sinks : row_sees(p, j);
+          need(!sink || j >= s.sinks || row_sees(p, j), "a sink that a row does not see");
+          every = every && here, one = one || here;
+          if (j < capacity && p >= 0) need(sk::sees((int32_t)p, (int32_t)j, window, sinks) == row_sees(p, j), "sees");
+        }
+        need(sk::some_see(s, b, sk::key_behind((int32_t)key, i), (int32_t)p0, (int32_t)p1, window, sinks) >= one, "a value left out");
+        if (j >= capacity && !sink) need(!sk::some_see(s, b, sk::key_behind((int32_t)key, i), (int32_t)p0, (int32_t)p1, window, sinks), "a value that nobody sees");
+        all = all && every, any = any || one, all_there = all_there && j < capacity;
+      }
+      need(!sk::all_see_block<KEYS>(s, b, (int32_t)key, (int32_t)p0, (int32_t)p1, window) || all, "a block that not all see");
+      need(!all || sinks || sk::all_see_block<KEYS>(s, b, (int32_t)key, (int32_t)p0, (int32_t)p1, window), "a block that all see");
+      need(!any || sk::some_see_block<KEYS>(s, b, (int32_t)key, (int32_t)p0, (int32_t)p1, window, sinks), "a block that some see");
+      need((uint32_t)(b - whole.first) >= whole.n || (all && all_there), "whole blocks");
+    }
+  }
+}
+
 int main() {
   std::mt19937 rng(7);
   plans(rng);
+  blocks_of_keys<32>(rng);
+  blocks_of_keys<64>(rng);
   accounts(rng);
   std::printf("cache_driver: ok\n");
   return 0;

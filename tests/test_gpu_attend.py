@@ -148,6 +148,25 @@ def test_offsets_beyond_32_bits():
     H.assert_close(t.out(), want, tol)
 
 
+@pytest.mark.parametrize("dtype,dim", [("bf16", 64), ("f16", 256)])
+def test_the_longest_sequences(dtype, dim):
+    """All but 16 of 2^31 tokens, of which the rows see the first few and a window: tiles reach beyond 2^31, and no page number is read outside the
+    table.  To the formula only distances count, so the first 16 tokens and the last 256 stand for the sequence."""
+    columns, page, tail = 2 ** 27 - 1, 16, 16
+    table = torch.full((columns,), -1, dtype=torch.int32, device="cuda")
+    for new, window in ((1, 90), (3, 17), (40, 33), (40, 100), (90, 64)):
+        t = Tenant(dtype, (4, 2, dim), (((1 + tail) * page, new),), page=page, window=window, sinks=3, seed=new + window)
+        want, tol = t.attend()
+        problem = t.to_device()
+        table[0], table[columns - tail:] = int(t.table[0, 0]), t.table[0, 1:1 + tail].cuda()
+        t.keep[1].fill_(columns * page)
+        problem.page_table, problem.pages_per_sequence = table.data_ptr(), columns
+        with sk.sk_attn_plan_create([problem]) as plan:
+            sk.sk_attn_launch(plan, H.stream_handle())
+            torch.cuda.synchronize()
+        H.assert_close(t.out(), want, tol, f"{new} new, window {window}")
+
+
 def test_a_plan_serves_steps_in_a_graph_and_on_another_stream():
     """One plan, lengths and rows that change: captured once, replayed with each step's numbers, eager work between."""
     steps = [((20, 1), (200, 1), (5, 1)), ((21, 1), (201, 1), (6, 1)), ((400, 3), (1, 0), (77, 40)), ((22, 1), (202, 1), (7, 1))]
