@@ -108,7 +108,8 @@ void sk_attn_params_default(sk_attn_params *params);
  * Plan for n problems (n = 0: launches do nothing).  Errors: SK_ERR_INVALID_ARG (null pointers, sizes < 1, strides that let
  * heads or tokens overlap, cos and sin with too few rows), SK_ERR_UNSUPPORTED (SK_F32; a head_dim that is no multiple of
  * 8 or larger than 256; page_tokens that is no power of two from 16 on; pointers or strides that are no multiples of 16 bytes;
- * sequences of 2^31 tokens and more; more than 2^20 sequences; a token_stride of 2^26 elements and more; sizes that a launch's grid cannot hold), SK_ERR_OVERLAP (q or out of two problems, or of one,
+ * sequences of 2^31 tokens and more; more than 2^20 sequences; more than 2^30 heads; a token_stride of 2^26 elements and more;
+ * more units of work than the 2^24 - 1 workgroups of a launch), SK_ERR_OVERLAP (q or out of two problems, or of one,
  * intersect), SK_ERR_ALLOC, SK_ERR_HIP.
  */
 sk_status sk_attn_plan_create(const sk_attn_problem *problems, int32_t n, const sk_attn_params *params, sk_attn_plan **out);

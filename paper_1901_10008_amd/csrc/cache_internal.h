@@ -13,6 +13,8 @@
 namespace sk {
 
 constexpr int CACHE_THREADS = 256;
+// Workgroups of a launch: the runtime refuses 2^32 threads and more.
+constexpr int64_t MOST_GRID = (((int64_t)1 << 32) - 1) / CACHE_THREADS;
 // Rows of a unit of work (a key-value head of a sequence): few rows go in blocks of ROWS_FEW, whose four waves share the
 // keys among them; more than most_few() rows go in blocks of ROWS_MANY, whose waves share the rows.
 constexpr int ROWS_FEW = 16, ROWS_MANY = 128;

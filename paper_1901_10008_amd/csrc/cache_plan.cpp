@@ -36,6 +36,7 @@ sk_status check_problem(const sk_attn_problem &p, AttnDev &d, std::string &err) 
   if (p.q_heads < 1 || p.kv_heads < 1 || p.head_dim < 1 || p.page_tokens < 1 || p.num_pages < 1 || p.sequences < 1 || p.pages_per_sequence < 1 || p.rows < 1)
     return refuse(err, SK_ERR_INVALID_ARG, "a size is less than 1");
   if (p.sequences > 1 << 20) return refuse(err, SK_ERR_UNSUPPORTED, "more than 2^20 sequences");
+  if ((int64_t)p.q_heads + 2 * (int64_t)p.kv_heads > (int64_t)1 << 30) return refuse(err, SK_ERR_UNSUPPORTED, "more than 2^30 heads");
   if (p.max_new < 0 || p.window < 0 || p.sinks < 0 || p.rotary_dim < 0 || p.reserved != 0)
     return refuse(err, SK_ERR_INVALID_ARG, "max_new, window, sinks or rotary_dim is negative, or reserved is not 0");
   if (p.q_heads % p.kv_heads) return refuse(err, SK_ERR_INVALID_ARG, "q_heads must be a multiple of kv_heads");
@@ -129,7 +130,7 @@ sk_status plan_attn(const sk_attn_problem *problems, int32_t n, int32_t compute_
     d.turns = (int32_t)std::max<int64_t>(1, std::min(most, (int64_t)d.rows * most / APPEND_WAVES));
     d.parts = (int32_t)((most + d.turns - 1) / d.turns);
     append_grid += d.qkv ? ((int64_t)d.rows * d.parts + 3) / 4 : 0;
-    if (append_grid >= (int64_t)1 << 31) return refuse(err, SK_ERR_UNSUPPORTED, "more rows than a launch's grid can hold");
+    if (append_grid > MOST_GRID) return refuse(err, SK_ERR_UNSUPPORTED, "more rows than a launch's grid can hold");
     out.append_first.push_back((uint32_t)append_grid);
     out.problems.push_back(d);
   }
@@ -150,11 +151,13 @@ sk_status plan_attn(const sk_attn_problem *problems, int32_t n, int32_t compute_
       const int64_t capacity = (int64_t)d.columns << d.page_shift, most_rows = (int64_t)d.max_new * d.group;
       const int64_t blocks = (std::min<int64_t>(most_rows, most_few(d.dim)) + ROWS_FEW - 1) / ROWS_FEW, units = (int64_t)d.sequences * d.kv_heads * blocks;
       few += units;
+      if (few > MOST_GRID) return refuse(err, SK_ERR_UNSUPPORTED, "more units of work than a launch's grid can hold");
       few_most += units * (capacity / (4 * KEYS_FEW) + 2);
       if (most_rows > most_few(d.dim)) {
         // sequences of many rows: their blocks are full but for one each
         const int64_t rows = (int64_t)d.rows * d.group, full = d.kv_heads * (rows / ROWS_MANY + std::min<int64_t>(d.sequences, rows / (most_few(d.dim) + 1) + 1));
         many += full;
+        if (many > MOST_GRID) return refuse(err, SK_ERR_UNSUPPORTED, "more units of work than a launch's grid can hold");
         many_most += full * (capacity / (4 * keys_many(d.dim)) + 2);
       }
       for (int32_t s = 0; s < d.sequences; ++s)
@@ -167,7 +170,7 @@ sk_status plan_attn(const sk_attn_problem *problems, int32_t n, int32_t compute_
     g.grid = std::min(few + many + g.workgroups, few_most + many_most);
     g.slots_few = std::min(2 * g.workgroups, few_most);
     g.slots_many = std::min(2 * g.workgroups, many_most);
-    if (g.grid >= (int64_t)1 << 31) return refuse(err, SK_ERR_UNSUPPORTED, "more units of work than a launch's grid can hold");
+    if (g.grid > MOST_GRID) return refuse(err, SK_ERR_UNSUPPORTED, "more units of work than a launch's grid can hold");
     const int64_t dim = wide ? 256 : 128;
     out.workspace_floats = std::max(out.workspace_floats, g.slots_few * part_floats(ROWS_FEW, dim) + g.slots_many * part_floats(ROWS_MANY, dim));
     out.counters = std::max(out.counters, g.slots_few + g.slots_many);

@@ -66,6 +66,25 @@ def test_refusals(change, status):
     assert e.value.detail
 
 
+@pytest.mark.parametrize("change", [
+    dict(sequences=1 << 20, q_heads=8, kv_heads=8, rows=1 << 21),  # two blocks of rows for each of 2^20 sequences' 8 heads: 2^24 workgroups of 256
+    dict(rows=1 << 27),  # rows of append: four a workgroup, 2^25
+    dict(rows=1 << 24, q_heads=127, kv_heads=127, qkv=0, sequences=1000),  # blocks of 128 rows: 127 x 2^17, and one for the last rows of each sequence
+    dict(sequences=1 << 20, q_heads=1 << 28, kv_heads=1 << 28, rows=1, head_dim=8, num_pages=1, rotary_dim=0, qkv=0, q=1 << 44, out=1 << 45),  # 2^48
+    dict(q_heads=1 << 30, kv_heads=1 << 29, rows=1, head_dim=8, num_pages=1, rotary_dim=0, q=1 << 44, out=1 << 45)])  # numbers of heads beyond 2^30
+def test_more_workgroups_than_a_launch_can_have(change):
+    """The runtime refuses launches of 2^32 threads and more: plans of more than 2^24 - 1 workgroups are refused, not their launches."""
+    with pytest.raises(sk.SkError) as e:
+        plan(GOOD | change)
+    assert e.value.status == UNSUPPORTED, e.value.detail
+    assert "grid" in e.value.detail or "heads" in e.value.detail
+
+
+def test_the_largest_grids_are_planned():
+    plan(GOOD | dict(sequences=1 << 20, q_heads=8, kv_heads=8, rows=1 << 20, max_new=1)).close()
+    plan(GOOD | dict(rows=(1 << 26) - 64, out=0)).close()
+
+
 def test_strides_that_are_fine():
     for change in (dict(token_stride=128, kv_head_stride=64, page_stride=2048), dict(token_stride=128, kv_head_stride=64, page_stride=2048 * 2),
                    dict(token_stride=64, kv_head_stride=1024, page_stride=2048 + 8), dict(token_stride=64, kv_head_stride=1024 * 100, page_stride=1024),
