@@ -146,7 +146,7 @@ sk_status sk_attn_plan_info(const sk_attn_plan *plan, int32_t *launches, int64_t
  */
 typedef struct {
   void *base;         /* device; a multiple of 16                                 */
-  int64_t page_bytes; /* distance of two pages, and bytes of one; a multiple of 16 */
+  int64_t page_bytes; /* distance of two pages, and bytes of one; a multiple of 16, at most 2^38 */
 } sk_page_array;
 
 typedef struct sk_pages sk_pages; /* opaque, owned by the library */

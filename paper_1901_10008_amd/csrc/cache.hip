@@ -161,22 +161,27 @@ sk_status launch_copies(const sk_page_array *arrays, int32_t n_arrays, const sk:
   sk::CopyArgs a;
   a.table = table;
   a.columns = columns;
-  int64_t bytes = 0;
-  for (int32_t i = 0; i < n_arrays; ++i) bytes += arrays[i].page_bytes;
-  void (*const kernel)(sk::CopyArgs) = (double)bytes * 2.0 * (double)n_moves > (double)sk::PAST_CACHES ? sk::sk_copy_pages<true> : sk::sk_copy_pages<false>;
-  for (int32_t a0 = 0;; a0 += sk::COPY_ARRAYS) {
-    a.n_arrays = n_moves ? std::max(0, std::min(n_arrays - a0, sk::COPY_ARRAYS)) : 0;
+  double bytes = 0.0;
+  int64_t most_chunks = 1;
+  for (int32_t i = 0; i < n_arrays; ++i) {
+    bytes += (double)arrays[i].page_bytes;
+    most_chunks = std::max(most_chunks, (arrays[i].page_bytes + sk::COPY_CHUNK - 1) / sk::COPY_CHUNK);
+  }
+  const sk::CopyBatch batch = sk::copy_batch(most_chunks);
+  void (*const kernel)(sk::CopyArgs) = bytes * 2.0 * (double)n_moves > (double)sk::PAST_CACHES ? sk::sk_copy_pages<true> : sk::sk_copy_pages<false>;
+  for (int32_t a0 = 0;; a0 += batch.arrays) {
+    a.n_arrays = n_moves ? std::max(0, std::min(n_arrays - a0, batch.arrays)) : 0;
     a.chunks = 0;
     for (int32_t i = 0; i < a.n_arrays; ++i) {
       std::memcpy(a.words + 4 * i, &arrays[a0 + i].base, 8);
       std::memcpy(a.words + 4 * i + 2, &arrays[a0 + i].page_bytes, 8);
       a.chunks = std::max(a.chunks, (arrays[a0 + i].page_bytes + sk::COPY_CHUNK - 1) / sk::COPY_CHUNK);
     }
-    const bool last_arrays = a0 + sk::COPY_ARRAYS >= n_arrays || !n_moves;
-    for (size_t m0 = 0;; m0 += sk::COPY_MOVES) {
-      a.n_moves = a.n_arrays ? (int32_t)std::min(n_moves - m0, (size_t)sk::COPY_MOVES) : 0;
+    const bool last_arrays = n_arrays - a0 <= batch.arrays || !n_moves;
+    for (size_t m0 = 0;; m0 += (size_t)batch.moves) {
+      a.n_moves = a.n_arrays ? (int32_t)std::min(n_moves - m0, (size_t)batch.moves) : 0;
       if (a.n_moves) std::memcpy(a.words + 4 * a.n_arrays, moves + m0, (size_t)a.n_moves * sizeof(sk::PageMove));
-      const bool last = last_arrays && m0 + sk::COPY_MOVES >= n_moves;
+      const bool last = last_arrays && m0 + (size_t)batch.moves >= n_moves;
       const int64_t copies = a.chunks * a.n_arrays * a.n_moves;
       bool with_rows = last && n_rows;
       a.rows = pinned;
@@ -186,19 +191,18 @@ sk_status launch_copies(const sk_page_array *arrays, int32_t n_arrays, const sk:
         else with_rows = false;  // they get a launch of their own
       }
       a.n_rows = with_rows ? n_rows : 0;
-      if (copies + a.n_rows >= (int64_t)1 << 31) return set_last_error(SK_ERR_UNSUPPORTED, "pages too large for a launch's grid");
       const bool alone = last && n_rows && !with_rows;
       if (copies + a.n_rows) {
-        const sk_status st = launch(kernel, copies + a.n_rows, stream, last && !alone ? behind : nullptr, a);
+        const sk_status st = launch(kernel, copies + std::min(a.n_rows, sk::ROW_GROUPS), stream, last && !alone ? behind : nullptr, a);
         if (st != SK_OK) return st;
       }
       if (alone) {
         a.n_arrays = a.n_moves = 0;
         a.n_rows = n_rows;
         put(a.words);
-        return launch(kernel, n_rows, stream, behind, a);
+        return launch(kernel, std::min(n_rows, sk::ROW_GROUPS), stream, behind, a);
       }
-      if (m0 + sk::COPY_MOVES >= n_moves) break;
+      if (m0 + (size_t)batch.moves >= n_moves) break;
     }
     if (last_arrays) return SK_OK;
   }
@@ -209,6 +213,7 @@ sk_status check_arrays(const sk_page_array *arrays, int32_t n_arrays) {
   for (int32_t i = 0; i < n_arrays; ++i) {
     if (!arrays[i].base || arrays[i].page_bytes < 1) return set_last_error(SK_ERR_INVALID_ARG, "an array without memory or with empty pages");
     if (((uintptr_t)arrays[i].base | (uintptr_t)arrays[i].page_bytes) & 15) return set_last_error(SK_ERR_UNSUPPORTED, "arrays and pages must be multiples of 16 bytes");
+    if (arrays[i].page_bytes > sk::COPY_PAGE) return set_last_error(SK_ERR_UNSUPPORTED, "a page of more than 2^38 bytes");
   }
   return SK_OK;
 }

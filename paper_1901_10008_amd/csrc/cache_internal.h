@@ -95,6 +95,19 @@ struct CopyArgs {
 static_assert(sizeof(CopyArgs) <= 4096, "kernel arguments");
 constexpr int COPY_ARRAYS = 64, COPY_MOVES = (COPY_WORDS - 4 * COPY_ARRAYS) / 2;  // of a launch, at most
 constexpr int64_t COPY_CHUNK = 32768;
+constexpr int64_t COPY_PAGE = (int64_t)1 << 38;  // bytes of a page, at most
+constexpr int32_t ROW_GROUPS = 1 << 16;          // workgroups that bring rows of the page table, at most
+// Arrays and copies of one launch, at most, for arrays whose largest pages have that many chunks: what its arguments and its grid hold.
+struct CopyBatch {
+  int32_t arrays, moves;
+};
+constexpr CopyBatch copy_batch(int64_t chunks) {
+  const int64_t groups = MOST_GRID - ROW_GROUPS;
+  const int32_t arrays = chunks * COPY_ARRAYS <= groups ? COPY_ARRAYS : (int32_t)(groups / chunks);
+  const int64_t moves = groups / (chunks * arrays);
+  return CopyBatch{arrays, moves < COPY_MOVES ? (int32_t)moves : COPY_MOVES};
+}
+static_assert(copy_batch(1).moves == COPY_MOVES && copy_batch((COPY_PAGE + COPY_CHUNK - 1) / COPY_CHUNK).moves >= 1, "every page fits a launch");
 
 // The account of pages.
 class PageAccount {

@@ -259,11 +259,11 @@ __global__ void __launch_bounds__(CACHE_THREADS) sk_copy_pages(CopyArgs a) {
     }
     for (; i < end; i += STEP) store16(dst + i, load16(src + i));
   } else {
-    const int32_t r = (int32_t)(blockIdx.x - copies);
-    if (r >= a.n_rows) return;
-    const int32_t at = 4 * a.n_arrays + 2 * a.n_moves, first = a.n_rows + r * a.columns;
-    const int64_t row = a.rows ? a.rows[r] : a.words[at + r];
-    for (int32_t i = threadIdx.x; i < a.columns; i += CACHE_THREADS) a.table[row * a.columns + i] = a.rows ? a.rows[first + i] : a.words[at + first + i];
+    const int32_t at = 4 * a.n_arrays + 2 * a.n_moves, groups = (int32_t)(gridDim.x - copies);
+    for (int32_t r = (int32_t)(blockIdx.x - copies); r < a.n_rows; r += groups) {
+      const int64_t row = a.rows ? a.rows[r] : a.words[at + r], first = a.n_rows + (int64_t)r * a.columns;
+      for (int32_t i = threadIdx.x; i < a.columns; i += CACHE_THREADS) a.table[row * a.columns + i] = a.rows ? a.rows[first + i] : a.words[at + first + i];
+    }
   }
 }
 

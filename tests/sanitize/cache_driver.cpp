@@ -188,12 +188,22 @@ static void blocks_of_keys(std::mt19937 &rng) {
   }
 }
 
+static void copies() {
+  for (int64_t chunks = 1; chunks * sk::COPY_CHUNK <= sk::COPY_PAGE; chunks += 1 + chunks / 7) {
+    const sk::CopyBatch b = sk::copy_batch(chunks);
+    need(b.arrays >= 1 && b.arrays <= sk::COPY_ARRAYS && b.moves >= 1 && b.moves <= sk::COPY_MOVES, "a batch that a launch's arguments do not hold");
+    need(chunks * b.arrays * b.moves + sk::ROW_GROUPS <= sk::MOST_GRID, "a batch that a launch's grid does not hold");
+    need(b.moves == sk::COPY_MOVES || chunks * b.arrays * (b.moves + 1) + sk::ROW_GROUPS > sk::MOST_GRID, "a batch smaller than need be");
+  }
+}
+
 int main() {
   std::mt19937 rng(7);
   plans(rng);
   blocks_of_keys<32>(rng);
   blocks_of_keys<64>(rng);
   accounts(rng);
+  copies();
   std::printf("cache_driver: ok\n");
   return 0;
 }

@@ -157,6 +157,35 @@ def test_more_arrays_and_copies_than_a_launch_holds():
     assert all(torch.equal(x, w) for x, w in zip(tensors, want))
 
 
+def test_copies_of_more_workgroups_than_a_launch_can_have():
+    """Large pages in one of many arrays: 2048 chunks x 64 arrays x 130 copies are more than 2^24 workgroups."""
+    n, moves = 140, 130
+    big = torch.empty((n, 64 << 20), dtype=torch.uint8, device="cuda")
+    for i in range(n):
+        big[i] = i
+        big[i, -16:] = torch.arange(16, dtype=torch.uint8, device="cuda") + i
+    small = [torch.randint(0, 256, (n, 48), dtype=torch.uint8, device="cuda") for _ in range(63)]
+    frm, to = [i % 10 for i in range(moves)], list(range(10, 10 + moves))
+    want = [x.clone() for x in small]
+    for w in want:
+        w[to] = w[frm]
+    sk.sk_pages_copy(arrays_of([big] + small), n, frm, to, H.stream_handle())
+    torch.cuda.synchronize()
+    for f, t in zip(frm, to):
+        assert torch.equal(big[t], big[f]) and int(big[f, 5]) == f and int(big[f, -1]) == f + 15
+    assert all(torch.equal(x, w) for x, w in zip(small, want))
+
+
+def test_more_rows_of_the_table_than_a_launch_can_have_workgroups():
+    seqs = (1 << 24) + 5
+    table = torch.full((seqs, 1), -7, dtype=torch.int32, device="cuda")
+    with sk.sk_pages_create(3, 16, seqs, 1) as account:
+        sk.sk_pages_resize(account, [0, 77, seqs - 1], [1, 2, 3])
+        sk.sk_pages_apply(account, arrays_of([torch.zeros((3, 16), dtype=torch.uint8, device="cuda")]), table.data_ptr(), H.stream_handle())
+        torch.cuda.synchronize()
+        assert [int(table[s, 0]) for s in (0, 77, seqs - 1)] == [0, 1, 2] and int((table == -1).sum()) == seqs - 3
+
+
 def test_copies_in_a_graph():
     x = torch.arange(10 * 64, dtype=torch.int32, device="cuda").view(10, 64)
     arrays = arrays_of([x])
