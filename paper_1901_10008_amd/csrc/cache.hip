@@ -308,6 +308,7 @@ sk_status sk_attn_launch(sk_attn_plan *plan, void *hip_stream) {
       a.problems = plan->problems;
       a.seqs = plan->seqs + g.first_seq;
       a.sequences = (int32_t)g.sequences;
+      a.grid = (uint32_t)g.grid;
       a.slots_many = (uint32_t)g.slots_many;
       a.slots_few = (uint32_t)g.slots_few;
       a.workgroups = (int32_t)g.workgroups;

@@ -141,45 +141,7 @@ __device__ __forceinline__ f32x2 load_shared(const float *p) {
 // before it; workgroups beyond the last leave.  Units of many rows come first, those of late rows (which see the most) before those of early ones; key-value heads
 // vary fastest, so that with eight of them each has a die (and its L2) of its own.
 
-// A sequence in this step: rows and lengths cut to the bounds that the grid was made for.
-struct Step {
-  int32_t first, fresh, length, behind;  // first row, rows to compute, tokens, position of the first new token
-};
-__device__ __forceinline__ Step step_of(const AttnSeq &q) {
-  const int32_t a = load_i32(q.first), b = load_i32(q.first + 1), n = load_i32(q.length);
-  Step s;
-  s.first = min(max(a, 0), q.rows);
-  const int32_t all = min(max(b, s.first), q.rows) - s.first;
-  s.length = (int32_t)min((int64_t)max(n, 0), q.capacity);
-  s.behind = s.length - all;
-  s.fresh = min(all, q.max_new);
-  return s;
-}
-struct Count {
-  int32_t row_blocks, units, blocks;  // blocks of keys of an average unit
-  bool many;
-};
-template <bool MANY, bool WIDE>
-__device__ __forceinline__ Count count_units(const Step &s, const AttnSeq &q) {
-  const int32_t kv_heads = q.kv_heads, group = q.group, window = q.window, sinks = q.sinks;
-  Count c;
-  const int64_t rows = (int64_t)s.fresh * group;
-  const int32_t last = s.behind + s.fresh - 1;
-  c.many = MANY && rows > q.most_few;
-  if (c.many) {
-    c.row_blocks = (int32_t)((rows + ROWS_MANY - 1) / ROWS_MANY);
-    const int32_t tokens = (int32_t)((uint32_t)(ROWS_MANY + group - 1) / (uint32_t)group);
-    constexpr int KEYS = keys_many(WIDE ? 256 : 128);
-    const Span a = span_of<KEYS>(s.behind, min(s.behind + tokens - 1, last), window, sinks);
-    const Span b = span_of<KEYS>(max(last - tokens + 1, s.behind), last, window, sinks);
-    c.blocks = (a.blocks + b.blocks + 1) / 2;
-  } else {
-    c.row_blocks = (int32_t)((rows + ROWS_FEW - 1) / ROWS_FEW);
-    c.blocks = span_of<KEYS_FEW>(s.behind, last, window, sinks).blocks;
-  }
-  c.units = c.row_blocks * kv_heads;
-  return c;
-}
+__device__ __forceinline__ Step step_of(const AttnSeq &q) { return step_of(q, load_i32(q.first), load_i32(q.first + 1), load_i32(q.length)); }
 
 struct Unit {
   int32_t problem, seq;
@@ -196,32 +158,14 @@ struct AttnArgs {
   const AttnSeq *seqs;
   int32_t sequences;
   int32_t workgroups;  // that the card runs at a time
+  uint32_t grid;       // workgroups of the launch
   uint32_t slots_many, slots_few;  // places of the workspace for slices of either kind
   float *ws_many, *ws_few;
   uint32_t *arrivals;  // slots_many, then as many as there are for few; zero between launches
 };
 
-// n / d for 0 <= n < 2^52 and d > 0: the rounded quotient of the exact values does not reach the next whole number, which is 1 / d away or more.
-// (Whole numbers of 64 bits take the compiler a hundred instructions more.)
-__device__ __forceinline__ int64_t divide(int64_t n, int64_t d) { return (int64_t)((double)n / (double)d); }
-// The first of `blocks` that slice number `split` of a unit takes.
-__device__ __forceinline__ int32_t slice_start(int32_t blocks, int32_t split, int32_t splits) { return splits == 1 ? split * blocks : (int32_t)divide((int64_t)blocks * split, splits); }
 // n / d for 0 <= n < 2^31.
 __device__ __forceinline__ int32_t fast_div(int32_t n, FastDiv d) { return (int32_t)((uint64_t)(uint32_t)n * d.mul >> d.shift); }
-
-// Units of many keys are cut into slices, so that few units fill the card and no unit is what the launch waits for.  A slice takes at most `most`
-// blocks of keys of few rows, or a TILE_WORK-th as many tiles of many: a tile takes 2 us, a block 0.5 to 1 (chunks beside single tokens, twelve
-// sequences: 58.1 us with a ratio of 2, 55.5 of 3, 58.8 of 4; launches of one kind do not care).
-constexpr int TILE_WORK = 3;
-constexpr int LEAST = 4;  // a block for each wave; tiles
-__device__ __forceinline__ int32_t splits_of(const Count &c, int32_t most) {
-  const uint32_t per = max(c.many ? ((uint32_t)most + TILE_WORK - 1) / TILE_WORK : (uint32_t)most, (uint32_t)LEAST);
-  return (int32_t)min(((uint32_t)max(c.blocks, 1) + per - 1) / per, (uint32_t)MOST_SPLITS);
-}
-// work: blocks of few rows and TILE_WORK times the tiles of many.  That many for each workgroup the card runs at a time: with it units and slices
-// are no more than these workgroups and the units together, and the slices of units that are cut (each of more than `most`) no more than twice
-// these workgroups.
-__device__ __forceinline__ int32_t even_share(int64_t work, int64_t workgroups) { return (int32_t)min(divide(work + workgroups - 1, workgroups), (int64_t)0x7ffffffe); }
 
 struct FindScratch {
   int64_t work[4];  // per wave
@@ -281,25 +225,25 @@ __device__ __forceinline__ Unit find_unit(const AttnArgs &a, FindScratch *f) {
       s = step_of(q);
       c = count_units<MANY, WIDE>(s, q);
     }
-    const int32_t units = lane_of(wave_scan(c.units), 63);
-    const int64_t work = lane_of(wave_scan((int64_t)c.units * c.blocks * (c.many ? TILE_WORK : 1)), 63);
+    const int32_t units = lane_of(wave_scan(items_of(c, 1)), 63);
+    const int64_t work = lane_of(wave_scan(work_of(c)), 63);
     int32_t most = even_share(work, a.workgroups), splits = splits_of(c, most);
     // Few units: slices as short as leaves all of them running at once.  (A slice costs its workgroup 5 us besides the keys: six caches
     // of 50 to 120 thousand tokens take 271 us in one round of slices, 281 in two, 288 in four.)
-    for (int i = 0; i < 8 && 2 * units <= a.workgroups && lane_of(wave_scan(c.units * splits), 63) > a.workgroups; ++i) {
+    for (int i = 0; i < 8 && units <= a.workgroups / 2 && lane_of(wave_scan(c.units * splits), 63) > a.workgroups; ++i) {
       most += most / 8 + 1;
       splits = splits_of(c, most);
     }
     // units and slices, and those of them that are slices, up to and with this lane's
     int32_t n_many, n_few, upto_many, upto_few, cut_many, cut_few;
     auto sums = [&]() {
-      const int32_t n = c.units * splits;
+      const int32_t n = items_of(c, splits);
       n_many = MANY && c.many ? n : 0, n_few = n - n_many;
       upto_many = MANY ? wave_scan(n_many) : 0, upto_few = wave_scan(n_few);
       cut_many = MANY ? wave_scan(splits > 1 ? n_many : 0) : 0, cut_few = wave_scan(splits > 1 ? n_few : 0);
     };
     sums();
-    if (lane_of(cut_many, 63) > (int32_t)a.slots_many || lane_of(cut_few, 63) > (int32_t)a.slots_few) {  // (a first_row that decreases: no slices, no places needed)
+    if (!slices_fit(lane_of(upto_many + upto_few, 63), lane_of(cut_many, 63), lane_of(cut_few, 63), a.grid, a.slots_many, a.slots_few)) {
       splits = 1;
       sums();
     }
@@ -328,7 +272,7 @@ __device__ __forceinline__ Unit find_unit(const AttnArgs &a, FindScratch *f) {
   int64_t work = 0;
   for (int i = s0; i < s1; ++i) {
     look(i);
-    work += (int64_t)c.units * c.blocks * (c.many ? TILE_WORK : 1);
+    work += work_of(c);
   }
   work = lane_of(wave_scan(work), 63);
   if (lane == 0) f->work[wave] = work;
@@ -340,23 +284,25 @@ __device__ __forceinline__ Unit find_unit(const AttnArgs &a, FindScratch *f) {
     n[0] = n[1] = cut[0] = cut[1] = 0;
     for (int i = s0; i < s1; ++i) {
       if (per_thread > 1) look(i);
-      const int32_t splits = splits_of(c, most), here = c.units * splits, sliced = splits > 1 ? here : 0;
+      const int32_t splits = splits_of(c, most), here = items_of(c, splits), sliced = splits > 1 ? here : 0;
       n[0] += MANY && c.many ? here : 0, cut[0] += MANY && c.many ? sliced : 0;
       n[1] += MANY && c.many ? 0 : here, cut[1] += MANY && c.many ? 0 : sliced;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) n[k] = min(n[k], MOST_ITEMS), cut[k] = min(cut[k], MOST_ITEMS);
     }
 #pragma unroll
     for (int k = MANY ? 0 : 1; k < 2; ++k) {
       upto[k] = wave_scan(n[k]);
       cut_upto[k] = wave_scan(cut[k]);
       if (lane == 63) {
-        f->items[k][wave] = upto[k];
-        f->cut[k][wave] = cut_upto[k];
+        f->items[k][wave] = min(upto[k], MOST_ITEMS);
+        f->cut[k][wave] = min(cut_upto[k], MOST_ITEMS);
       }
     }
     __syncthreads();
-    const int32_t all_cut_many = MANY ? f->cut[0][0] + f->cut[0][1] + f->cut[0][2] + f->cut[0][3] : 0;
-    if (all_cut_many <= (int32_t)a.slots_many && f->cut[1][0] + f->cut[1][1] + f->cut[1][2] + f->cut[1][3] <= (int32_t)a.slots_few) break;
-    most = 0x7ffffffe;  // (a first_row that decreases: no slices, no places needed)
+    auto all = [](const int32_t (&w)[4]) { return w[0] + w[1] + w[2] + w[3]; };
+    if (slices_fit((MANY ? all(f->items[0]) : 0) + all(f->items[1]), MANY ? all(f->cut[0]) : 0, all(f->cut[1]), a.grid, a.slots_many, a.slots_few)) break;
+    most = 0x7ffffffe;
     __syncthreads();
   }
   const int32_t all_many = MANY ? f->items[0][0] + f->items[0][1] + f->items[0][2] + f->items[0][3] : 0;
@@ -373,7 +319,7 @@ __device__ __forceinline__ Unit find_unit(const AttnArgs &a, FindScratch *f) {
     for (int i = s0; i < s1; ++i) {
       if (per_thread > 1) look(i);
       if (c.many != many) continue;
-      const int32_t splits = splits_of(c, most), here = c.units * splits;
+      const int32_t splits = splits_of(c, most), here = items_of(c, splits);
       if (item < at + here) {
         f->unit = unit_of(q, s, c, splits, item - at, slot);
         break;

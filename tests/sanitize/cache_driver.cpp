@@ -1,5 +1,6 @@
 // Host code of the operators over paged caches (cache_plan.cpp, and the arithmetic of cache_units.h that the kernels share) on seeded random
 // plans, steps and accounts, for a build with sanitizers.
+#include <algorithm>
 #include <cstdio>
 #include <cstdlib>
 #include <random>
@@ -188,6 +189,91 @@ static void blocks_of_keys(std::mt19937 &rng) {
   }
 }
 
+// What every workgroup of a launch of sequences finds, from the lengths and rows that the device has: units and slices in the order of the
+// sequences, those of many rows first.
+struct Found {
+  int64_t items, cut_many, cut_few;
+  bool fits;
+  struct Seq {
+    int64_t first_item;
+    int32_t units, splits;
+  };
+  std::vector<Seq> seqs;
+};
+template <bool MANY, bool WIDE>
+static Found find(const std::vector<sk::AttnSeq> &seqs, const std::vector<int32_t> &first, const std::vector<int32_t> &length, const sk::AttnGroup &g) {
+  std::vector<sk::Count> counts;
+  int64_t work = 0, units = 0;
+  for (size_t s = 0; s < seqs.size(); ++s) {
+    counts.push_back(sk::count_units<MANY, WIDE>(sk::step_of(seqs[s], first[s], first[s + 1], length[s]), seqs[s]));
+    work += sk::work_of(counts.back());
+    units += counts.back().units;
+  }
+  int32_t most = sk::even_share(work, g.workgroups);
+  auto items = [&]() {
+    int64_t n = 0;
+    for (const sk::Count &c : counts) n += (int64_t)c.units * sk::splits_of(c, most);
+    return n;
+  };
+  for (int i = 0; i < 8 && seqs.size() <= 64 && units <= g.workgroups / 2 && items() > g.workgroups; ++i) most += most / 8 + 1;
+  Found f{};
+  for (int pass = 0; pass < 2; ++pass)
+    for (const sk::Count &c : counts) {
+      const int32_t splits = sk::splits_of(c, most);
+      const int64_t n = (int64_t)c.units * splits;
+      if (pass == 0) (c.many ? f.cut_many : f.cut_few) += splits > 1 ? n : 0;
+      if (c.many != (pass == 0)) continue;
+      f.seqs.push_back(Found::Seq{f.items, c.units, splits});
+      f.items += n;
+    }
+  auto sum32 = [](int64_t n) { return (int32_t)std::min<int64_t>(n, (int64_t)1 << 30); };
+  f.fits = sk::slices_fit(sum32(f.items), sum32(f.cut_many), sum32(f.cut_few), (uint32_t)g.grid, (uint32_t)g.slots_many, (uint32_t)g.slots_few);
+  return f;
+}
+
+// Steps with rows in order always fit what their plan's launch has; of steps with rows in any order, those that do not are told.
+static void steps(std::mt19937 &rng) {
+  auto pick = [&](int lo, int hi) { return (int)(lo + rng() % (unsigned)(hi - lo + 1)); };
+  int caught = 0, sliced = 0;
+  for (int round = 0; round < 6000; ++round) {
+    sk_attn_problem p{};
+    p.dtype = 1;
+    p.kv_heads = pick(1, 8);
+    p.q_heads = p.kv_heads * pick(1, 8);
+    p.head_dim = 8 * pick(1, 32);
+    p.page_tokens = 16;
+    p.num_pages = 10;
+    p.sequences = pick(0, 3) ? pick(1, 64) : pick(65, 400);
+    p.pages_per_sequence = pick(0, 1) ? pick(1, 100) : pick(100, 20000);
+    p.rows = pick(0, 1) ? pick(1, 400) : pick(400, 4000);
+    p.max_new = pick(0, 1) ? 0 : pick(1, 300);
+    p.window = pick(0, 2) ? 0 : pick(1, 5000);
+    p.sinks = pick(0, 9);
+    const uintptr_t at = (uintptr_t)1 << 40;
+    p.k = p.v = p.q = (void *)at, p.page_table = p.lengths = p.first_row = (int32_t *)at, p.out = (void *)(at << 1);
+    sk::AttnPlanHost h;
+    std::string err;
+    need(sk::plan_attn(&p, 1, 256, pick(0, 1) ? 0 : pick(1, 700), h, err) == SK_OK && h.groups.size() == 1, "a plan of one problem");
+    const sk::AttnGroup &g = h.groups[0];
+    std::vector<int32_t> length, first{0};
+    const int32_t capacity = p.pages_per_sequence * p.page_tokens;
+    for (int s = 0; s < p.sequences; ++s) length.push_back(pick(0, 2) ? pick(0, capacity) : pick(0, 1) ? capacity : pick(0, 100));
+    const bool in_order = round % 2;
+    const bool alternate = round % 4 == 0;  // every second sequence has all rows
+    for (int s = 1; s <= p.sequences; ++s) first.push_back(alternate ? s % 2 * p.rows : pick(0, 4) ? pick(0, p.rows) : pick(-5, p.rows + 5));
+    if (in_order) std::sort(first.begin(), first.end());
+    const Found f = g.wide ? (g.many ? find<true, true>(h.seqs, first, length, g) : find<false, true>(h.seqs, first, length, g))
+                           : (g.many ? find<true, false>(h.seqs, first, length, g) : find<false, false>(h.seqs, first, length, g));
+    need(!in_order || f.fits, "a step in order that does not fit its launch");
+    bool straddles = false;  // a sequence that is cut, of whose slices only some have a workgroup
+    for (const Found::Seq &s : f.seqs) straddles = straddles || (s.splits > 1 && s.first_item < g.grid && s.first_item + (int64_t)s.units * s.splits > g.grid);
+    need(!straddles || !f.fits, "slices without a workgroup");
+    caught += straddles;
+    sliced += in_order && f.cut_many + f.cut_few > 0;
+  }
+  need(caught > 20 && sliced > 500, "steps that show nothing");
+}
+
 static void copies() {
   for (int64_t chunks = 1; chunks * sk::COPY_CHUNK <= sk::COPY_PAGE; chunks += 1 + chunks / 7) {
     const sk::CopyBatch b = sk::copy_batch(chunks);
@@ -203,6 +289,7 @@ int main() {
   blocks_of_keys<32>(rng);
   blocks_of_keys<64>(rng);
   accounts(rng);
+  steps(rng);
   copies();
   std::printf("cache_driver: ok\n");
   return 0;

@@ -129,6 +129,24 @@ def test_rows_out_of_order_stay_inside(count):
     H.assert_close(t.out(), want, tol)
 
 
+def test_rows_out_of_order_leave_no_slices_behind():
+    """Every second sequence with all rows: 175 units and slices for a launch of 166 workgroups, cut where one of two slices of a unit has none.  The next
+    step uses that unit's count of arrivals."""
+    t = Tenant("bf16", (4, 1, 64), ((1949, 1106),) + ((1949, 0),) * 6, seed=13)
+    problem = t.to_device()
+    with sk.sk_attn_plan_create([problem], sk.sk_attn_params_default(workgroups=111)) as plan:
+        t.keep[1].copy_(torch.tensor([1245, 1949, 1909, 1289, 1257, 1350, 1949], dtype=torch.int32))
+        t.keep[2].copy_(torch.tensor([0, 1106] * 4, dtype=torch.int32))
+        sk.sk_attn_launch(plan, H.stream_handle())
+        t.keep[1].copy_(t.lengths)
+        t.keep[2].copy_(t.firsts)
+        t.dout.fill_(math.nan)
+        sk.sk_attn_launch(plan, H.stream_handle())
+        torch.cuda.synchronize()
+    want, tol = t.attend()
+    H.assert_close(t.out(), want, tol)
+
+
 def test_offsets_beyond_32_bits():
     """A cache of 2^32 elements and more for each of keys and values, tokens in its last pages."""
     dim, heads, page = 128, 8, 64
