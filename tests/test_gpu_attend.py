@@ -47,6 +47,22 @@ def test_slices_of_the_keys(workgroups, dim):
     H.check_attend([Tenant("f16", (4, 2, dim), seqs, window=300, sinks=5, seed=workgroups)], f"{workgroups} window", workgroups=workgroups)
 
 
+@pytest.mark.parametrize("dtype,dim", [("bf16", 64), ("f16", 256)])
+@pytest.mark.parametrize("count", [65, 90, 300])
+def test_slices_of_many_sequences(count, dtype, dim):
+    """More sequences than lanes, more than threads; every tenth is long, some with many rows: these are cut, at the least number of blocks a slice."""
+    def seq(i):
+        return ((1500, 1), (700, 40), (900, 2))[i // 10 % 3] if i % 10 == 3 else (1 + 7 * i % 60, i % 3)
+
+    H.check_attend([Tenant(dtype, (2, 1, dim), [seq(i) for i in range(count)], seed=count)], f"{count}", workgroups=5000)
+
+
+@pytest.mark.parametrize("dtype,tokens,new", [("bf16", 33000, 1), ("f16", 33000, 3), ("bf16", 66000, 40), ("bf16", 5000, 1), ("f16", 9000, 40)])
+def test_as_many_slices_as_there_can_be(dtype, tokens, new):
+    """256 slices of a unit of few rows (33000 tokens) and of many (66000), and 35 to 40 of them."""
+    H.check_attend([Tenant(dtype, (2, 1, 64), ((tokens, new), (5, 1)), seed=tokens)], f"{tokens}", workgroups=5000)
+
+
 def test_more_sequences_than_threads():
     seqs = tuple((1 + 37 * i % 90, 1 + (i % 7 == 0) * (i % 30) if (1 + 37 * i % 90) > 30 else 1) for i in range(600))
     H.check_attend([Tenant("bf16", (2, 1, 64), seqs, seed=1), Tenant("bf16", (2, 2, 40), seqs[:100], seed=2, window=20, sinks=2)], "many sequences")
