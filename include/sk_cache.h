@@ -135,7 +135,8 @@ sk_status sk_attn_plan_info(const sk_attn_plan *plan, int32_t *launches, int64_t
  * sk_pages_compact  moves the pages in use to the lowest numbers.
  * sk_pages_apply    makes the device follow: the page copies that the calls since the last sk_pages_apply have called for, in every
  *                   array, in an order in which none overwrites what another still has to read; and the rows that have changed of
- *                   the device's page table, [sequences][pages_per_sequence] int32 with -1 where a sequence has no page (null: no table).  One kernel launch
+ *                   the device's page table, [sequences][pages_per_sequence] int32 with -1 where a sequence has no page.  Without a table
+ *                   (null) the rows wait for a call that has one; without arrays the copies count as made.  One kernel launch
  *                   where no copy depends on another.  Asynchronous; not inside a stream capture (SK_ERR_STATE).  After SK_ERR_HIP
  *                   some of the copies may have been made and others not.
  * sk_pages_state    counts; row (of pages_per_sequence entries) and tokens of a sequence.  Any pointer may be null.

@@ -119,7 +119,8 @@ class PageAccount {
   // The copies called for so far, in waves: the copies of one wave do not depend on each other, waves go in order.
   const std::vector<std::vector<PageMove>> &waves() const { return waves_; }
   const std::vector<int32_t> &dirty_rows() const { return dirty_; }
-  void applied();
+  // The copies have been made and, if `rows`, the changed rows brought to the device's table.
+  void applied(bool rows = true);
   int32_t num_pages() const { return (int32_t)refs_.size(); }
   int32_t sequences() const { return (int32_t)tokens_.size(); }
   int32_t columns() const { return columns_; }

@@ -224,10 +224,11 @@ int32_t PageAccount::pending() const {
   return (int32_t)n;
 }
 
-void PageAccount::applied() {
+void PageAccount::applied(bool rows) {
   for (const auto &w : waves_)
     for (const PageMove &m : w) read_[m.from] = written_[m.from] = read_[m.to] = written_[m.to] = 0;
   waves_.clear();
+  if (!rows) return;
   for (int32_t s : dirty_) is_dirty_[s] = 0;
   dirty_.clear();
 }

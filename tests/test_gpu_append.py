@@ -261,6 +261,32 @@ def test_account_and_device_agree_under_random_calls():
     account.close()
 
 
+@pytest.mark.parametrize("columns", [6, 600])
+def test_rows_wait_for_a_table(columns):
+    """Calls without a page table make the copies alone: rows changed by then come with the next call that has one."""
+    pool = torch.arange(50 * 4, dtype=torch.int32, device="cuda").view(50, 4)
+    table = torch.full((5, columns), -7, dtype=torch.int32, device="cuda")
+    arrays = arrays_of([pool])
+    with sk.sk_pages_create(50, 16, 5, columns) as account:
+        sk.sk_pages_resize(account, [0], [40])
+        sk.sk_pages_apply(account, arrays, 0, H.stream_handle())
+        sk.sk_pages_fork(account, 0, [1, 3])
+        sk.sk_pages_resize(account, [1, 3], [41, 41])
+        assert sk.sk_pages_state(account)[1] == 2
+        sk.sk_pages_apply(account, arrays, 0, H.stream_handle())
+        assert sk.sk_pages_state(account)[1] == 0
+        torch.cuda.synchronize()
+        assert (table == -7).all() and torch.equal(pool[3:5], pool[2].expand(2, 4))
+        sk.sk_pages_apply(account, arrays, table.data_ptr(), H.stream_handle())
+        torch.cuda.synchronize()
+        assert table.cpu().tolist() == [sk.sk_pages_state(account, s)[1] for s in range(5)]
+        table.fill_(-9)
+        sk.sk_pages_resize(account, [3], [60])
+        sk.sk_pages_apply(account, arrays, table.data_ptr(), H.stream_handle())  # what has not changed since is not brought again
+        torch.cuda.synchronize()
+        assert table[3].tolist() == sk.sk_pages_state(account, 3)[1] and (table[:3] == -9).all() and (table[4] == -9).all()
+
+
 @pytest.mark.parametrize("columns,seqs", [(12, 9), (120, 9), (300, 40)])
 def test_rows_of_the_table_of_any_length(columns, seqs):
     """Rows that fit a launch's arguments, alone or beside the copies, and rows that go through host memory."""
