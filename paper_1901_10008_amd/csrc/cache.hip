@@ -404,7 +404,8 @@ sk_status sk_pages_apply(sk_pages *pages, const sk_page_array *arrays, int32_t n
     sk::PageAccount &acc = pages->account;
     const std::vector<int32_t> &dirty = acc.dirty_rows();
     const int32_t n_rows = page_table ? (int32_t)dirty.size() : 0, columns = acc.columns();
-    if (acc.waves().empty() && !n_rows) return SK_OK;
+    const std::vector<std::vector<sk::PageMove>> waves = acc.waves();
+    if (waves.empty() && !n_rows) return SK_OK;
     auto put = [&](int32_t *to) {
       std::memcpy(to, dirty.data(), (size_t)n_rows * 4);
       for (int32_t r = 0; r < n_rows; ++r) std::memcpy(to + n_rows + (size_t)r * columns, acc.row(dirty[r]), (size_t)columns * 4);
@@ -426,7 +427,6 @@ sk_status sk_pages_apply(sk_pages *pages, const sk_page_array *arrays, int32_t n
       pages->used[i] = false;
       put(pages->rows[i]);
     }
-    const auto &waves = acc.waves();
     const size_t launches = std::max<size_t>(waves.size(), 1);
     for (size_t w = 0; w < launches; ++w) {
       const bool last = w + 1 == launches;

@@ -109,7 +109,7 @@ constexpr CopyBatch copy_batch(int64_t chunks) {
 }
 static_assert(copy_batch(1).moves == COPY_MOVES && copy_batch((COPY_PAGE + COPY_CHUNK - 1) / COPY_CHUNK).moves >= 1, "every page fits a launch");
 
-// The account of pages.
+// The account of pages.  A call that throws (std::bad_alloc) has changed nothing.
 class PageAccount {
  public:
   PageAccount(int32_t num_pages, int32_t page_tokens, int32_t sequences, int32_t columns);
@@ -117,7 +117,7 @@ class PageAccount {
   sk_status fork(int32_t from, const int32_t *to, int32_t n, std::string &err);
   sk_status compact();
   // The copies called for so far, in waves: the copies of one wave do not depend on each other, waves go in order.
-  const std::vector<std::vector<PageMove>> &waves() const { return waves_; }
+  std::vector<std::vector<PageMove>> waves() const;
   const std::vector<int32_t> &dirty_rows() const { return dirty_; }
   // The copies have been made and, if `rows`, the changed rows brought to the device's table.
   void applied(bool rows = true);
@@ -125,7 +125,7 @@ class PageAccount {
   int32_t sequences() const { return (int32_t)tokens_.size(); }
   int32_t columns() const { return columns_; }
   int32_t free_pages() const { return free_; }
-  int32_t pending() const;
+  int32_t pending() const { return (int32_t)moves_.size(); }
   int32_t tokens(int32_t s) const { return tokens_[s]; }
   const int32_t *row(int32_t s) const { return table_.data() + (size_t)s * columns_; }
 
@@ -133,6 +133,7 @@ class PageAccount {
   int32_t held(int32_t tokens) const { return (int32_t)(((uint32_t)tokens + (uint32_t)page_tokens_ - 1) / (uint32_t)page_tokens_); }
   int32_t take();
   void give(int32_t page);
+  void room_for(size_t moves);
   void move(int32_t from, int32_t to);
   void touch(int32_t s);
   sk_status check_list(const int32_t *seqs, int32_t n, std::string &err);
@@ -141,8 +142,9 @@ class PageAccount {
   std::vector<int32_t> refs_;                          // per page: sequences that hold it
   std::vector<int32_t> tokens_;                        // per sequence
   std::vector<int32_t> table_;
-  std::vector<std::vector<PageMove>> waves_;
-  std::vector<int32_t> read_, written_;  // per page: last wave that reads / writes it, from 1 on
+  std::vector<PageMove> moves_;          // the copies, and the wave of each, from 1 on
+  std::vector<int32_t> wave_;
+  std::vector<int32_t> read_, written_;  // per page: last wave that reads / writes it
   std::vector<int32_t> dirty_;
   std::vector<uint8_t> is_dirty_, mark_;
 };

@@ -209,25 +209,33 @@ void PageAccount::give(int32_t page) {
   if (page < lowest_) lowest_ = page;
 }
 
+// Room for so many more copies: nothing behind it needs memory.
+void PageAccount::room_for(size_t moves) {
+  const size_t wanted = moves_.size() + moves;
+  if (wanted <= std::min(moves_.capacity(), wave_.capacity())) return;
+  moves_.reserve(std::max(wanted, 2 * moves_.size()));
+  wave_.reserve(std::max(wanted, 2 * moves_.size()));
+}
+
 // A copy goes into the first wave behind all that wrote its source or read or wrote its target.
 void PageAccount::move(int32_t from, int32_t to) {
   const int32_t w = std::max(written_[from], std::max(read_[to], written_[to])) + 1;
-  if ((size_t)w > waves_.size()) waves_.resize((size_t)w);
-  waves_[(size_t)w - 1].push_back(PageMove{from, to});
+  moves_.push_back(PageMove{from, to});
+  wave_.push_back(w);
   read_[from] = std::max(read_[from], w);
   written_[to] = w;
 }
 
-int32_t PageAccount::pending() const {
-  size_t n = 0;
-  for (const auto &w : waves_) n += w.size();
-  return (int32_t)n;
+std::vector<std::vector<PageMove>> PageAccount::waves() const {
+  std::vector<std::vector<PageMove>> waves(wave_.empty() ? 0 : (size_t)*std::max_element(wave_.begin(), wave_.end()));
+  for (size_t i = 0; i < moves_.size(); ++i) waves[(size_t)wave_[i] - 1].push_back(moves_[i]);
+  return waves;
 }
 
 void PageAccount::applied(bool rows) {
-  for (const auto &w : waves_)
-    for (const PageMove &m : w) read_[m.from] = written_[m.from] = read_[m.to] = written_[m.to] = 0;
-  waves_.clear();
+  for (const PageMove &m : moves_) read_[m.from] = written_[m.from] = read_[m.to] = written_[m.to] = 0;
+  moves_.clear();
+  wave_.clear();
   if (!rows) return;
   for (int32_t s : dirty_) is_dirty_[s] = 0;
   dirty_.clear();
@@ -255,6 +263,7 @@ sk_status PageAccount::resize(const int32_t *seqs, const int32_t *tokens, int32_
     if (tokens[i] < 0) return refuse(err, SK_ERR_INVALID_ARG, "a negative number of tokens");
     if ((int64_t)tokens[i] > (int64_t)columns_ * page_tokens_) return refuse(err, SK_ERR_INVALID_ARG, "more tokens than a row of the page table can hold");
   }
+  room_for((size_t)n);
   // Sequences that shrink go first, so that what they give back serves the others; pages that two of them share are counted as they go.
   for (int32_t i = 0; i < n; ++i) {
     const int32_t s = seqs[i], has = held(tokens_[s]), will = held(tokens[i]);
@@ -330,6 +339,9 @@ sk_status PageAccount::fork(int32_t from, const int32_t *to, int32_t n, std::str
 sk_status PageAccount::compact() {
   const int32_t used = num_pages() - free_;
   std::vector<int32_t> now((size_t)num_pages(), -1);
+  size_t high = 0;
+  for (int32_t p = used; p < num_pages(); ++p) high += refs_[p] != 0;
+  room_for(high);
   int32_t to = 0;
   for (int32_t p = used; p < num_pages(); ++p) {
     if (!refs_[p]) continue;

@@ -241,6 +241,17 @@ def test_host_code_under_sanitizers(tmp_path):
     assert res.returncode == 0 and "cache_driver: ok" in res.stdout, res.stdout + res.stderr
 
 
+@pytest.mark.skipif(shutil.which("g++") is None, reason="no host C++ compiler")
+def test_account_without_memory(tmp_path):
+    """Calls that run out of host memory, at whichever allocation, leave the account as it was."""
+    exe, csrc = str(tmp_path / "cache_memory_driver"), os.path.join(ROOT, "paper_1901_10008_amd", "csrc")
+    res = subprocess.run(["g++", "-std=c++17", "-g", "-O1", "-Wall", "-D_GLIBCXX_ASSERTIONS", "-I", os.path.join(ROOT, "include"), "-I", csrc,
+                          os.path.join(ROOT, "tests", "sanitize", "cache_memory_driver.cpp"), os.path.join(csrc, "cache_plan.cpp"), "-o", exe], capture_output=True, text=True)
+    assert res.returncode == 0, res.stderr
+    res = subprocess.run([exe], capture_output=True, text=True)
+    assert res.returncode == 0 and "cache_memory_driver: ok" in res.stdout, res.stdout + res.stderr
+
+
 def _all(blob, key):
     found = []
     for m in re.finditer(re.escape(key), blob):
