@@ -376,6 +376,16 @@ struct Pages {
 // has seen nothing has m = -inf; exp2 is then taken relative to 0, so that it stays at l = 0.
 constexpr float RISE = 8.f;
 __device__ __forceinline__ float base_of(float m) { return m == -__builtin_inff() ? 0.f : m; }
+// A weight is exp2(fma(score, scale, -base)), and the base a score times the scale, rounded: all weights of a row are off by the same factor, which
+// the division by their sum takes out.  From scores of 2^24 on it is no small one (half a unit of the base in the exponent).  Where a row's
+// base is beyond FAR scores are rounded to products first, as the base was: the difference is exact then, and no weight exceeds 2^RISE.
+constexpr float FAR = 65536.f;
+__device__ __forceinline__ bool any_far(float base) { return __builtin_expect(__ballot(fabsf(base) >= FAR) != 0, 0); }
+__device__ __forceinline__ float rounded_difference(float score, float scale, float base) {
+#pragma clang fp contract(off)
+  const float product = score * scale;
+  return product - base;
+}
 __device__ __forceinline__ float inverse(float sum) { return sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum); }  // (nothing seen: 0)
 
 // Values that some rows of a unit see and others do not must not reach the others, whatever they are; finite ones do not (their
@@ -630,11 +640,22 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, const SK_CONSTANT 
       for (int i = 0; i < NB; ++i) o[i] *= keep;
     }
     const float base = base_of(m);
+    if (any_far(base)) {
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[half][i] = rounded_difference(s[half][i], scale, base);
+    } else {
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[half][i] = fmaf(s[half][i], scale, -base);
+    }
 #pragma unroll
     for (int half = 0; half < 2; ++half)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        s[half][i] = exp2_fast(fmaf(s[half][i], scale, -base));
+        s[half][i] = exp2_fast(s[half][i]);
         l += s[half][i];
       }
     // this block's values: behind them only the next block's keys are out
@@ -983,12 +1004,23 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
         for (int i = 0; i < NB; ++i) o[i] *= keep;
       }
       const float base = base_of(m);
+      if (any_far(base)) {
+#pragma unroll
+        for (int half = 0; half < HALVES; ++half)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[half][i] = rounded_difference(s[half][i], scale, base);
+      } else {
+#pragma unroll
+        for (int half = 0; half < HALVES; ++half)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[half][i] = fmaf(s[half][i], scale, -base);
+      }
       u32x4 pf[2 * HALVES];
 #pragma unroll
       for (int half = 0; half < HALVES; ++half) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          s[half][i] = exp2_fast(fmaf(s[half][i], scale, -base));
+          s[half][i] = exp2_fast(s[half][i]);
           l += s[half][i];
         }
 #pragma unroll

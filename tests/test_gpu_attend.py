@@ -84,6 +84,41 @@ def test_scales(scale):
     H.check_attend([Tenant("bf16", (4, 2, 64), MIXED, scale=scale, q_scale=2.0, seed=11)], f"{scale}")
 
 
+@pytest.mark.parametrize("dtype,size", [("bf16", 2.0 ** 10), ("bf16", 2.0 ** 20), ("bf16", 2.0 ** 50), ("f16", 2.0 ** 9), ("f16", 2.0 ** 13)])
+@pytest.mark.parametrize("dim", [64, 256])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_large_scores(dtype, size, dim, sign):
+    """Scores of up to 2^108 that lie far apart: a row's result is the value of its largest score, exactly up to the last rounding.  With sign -1 all
+    scores are far below zero, the largest is the least of them."""
+    seqs = ((1, 1), (700, 3), (90, 1), (400, 60), (130, 130), (33, 2))
+    t = Tenant(dtype, (4, 2, dim), seqs, seed=dim)
+    g = torch.Generator().manual_seed(dim)
+    shape = torch.where(torch.rand((dim,), generator=g) < 0.5, -1.0, 1.0)
+    t.q = (shape * size * (1 + torch.rand((t.rows, t.hq, dim), generator=g) / 2)).to(t.q.dtype)
+    best = {}
+    for s, (n, new) in enumerate(seqs):
+        for j in range(n):
+            # 1, 2, 4, 8 times the size in turn over runs of tokens, larger for few of them
+            factor = 2.0 ** (j // 40 % 3) * (1 if j % 40 == 17 else 0.25)
+            p, slot = int(t.table[s, j // t.page]), j % t.page
+            t.k[p, :, slot] = (sign * shape * size * factor).to(t.k.dtype)
+            best[s, j] = sign * factor
+    with sk.sk_attn_plan_create([t.to_device()], sk.sk_attn_params_default(workgroups=200)) as plan:
+        sk.sk_attn_launch(plan, H.stream_handle())
+        torch.cuda.synchronize()
+    got = t.out().double()
+    for s, (n, new) in enumerate(seqs):
+        for i in range(new):
+            pos, row = n - new + i, int(t.firsts[s]) + i
+            top = max(best[s, j] for j in range(pos + 1))
+            winners = [j for j in range(pos + 1) if best[s, j] == top]
+            for h in range(t.hq):
+                v = torch.stack([t.v[int(t.table[s, j // t.page]), h // 2, j % t.page] for j in winners]).double()
+                want = v.mean(0)
+                tol = v.abs().mean(0) * (2 * H.U[dtype] + (len(winners) + 64) * 2.0 ** -23) + H.TINY[dtype]
+                H.assert_close(got[row, h], want, tol, f"sequence {s} position {pos} head {h}")
+
+
 def test_rows_beyond_the_bound_are_left_alone():
     t = Tenant("bf16", (4, 2, 64), ((50, 9), (60, 3)), max_new=4, seed=1)
     problem = t.to_device()
