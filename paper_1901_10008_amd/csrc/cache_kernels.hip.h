@@ -386,6 +386,10 @@ __device__ __forceinline__ float rounded_difference(float score, float scale, fl
   const float product = score * scale;
   return product - base;
 }
+// Weights are rounded to 16 bits for the matrix units.  f16 has nothing below 2^-25: there they are 2^7 times as large (with RISE up to 2^15, and 65504
+// is the largest number), so that weights down to 2^-32 of the base count, and are as exact as others down to 2^-21.  Sums are larger by as much.
+template <int DT>
+constexpr float LIFT = DT == SK_F16 ? 7.f : 0.f;
 __device__ __forceinline__ float inverse(float sum) { return sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum); }  // (nothing seen: 0)
 
 // Values that some rows of a unit see and others do not must not reach the others, whatever they are; finite ones do not (their
@@ -644,12 +648,12 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, const SK_CONSTANT 
 #pragma unroll
       for (int half = 0; half < 2; ++half)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[half][i] = rounded_difference(s[half][i], scale, base);
+        for (int i = 0; i < 4; ++i) s[half][i] = rounded_difference(s[half][i], scale, base) + LIFT<DT>;
     } else {
 #pragma unroll
       for (int half = 0; half < 2; ++half)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[half][i] = fmaf(s[half][i], scale, -base);
+        for (int i = 0; i < 4; ++i) s[half][i] = fmaf(s[half][i], scale, LIFT<DT> - base);
     }
 #pragma unroll
     for (int half = 0; half < 2; ++half)
@@ -1008,12 +1012,12 @@ __device__ __forceinline__ void attend_many(const AttnArgs &a, const SK_CONSTANT
 #pragma unroll
         for (int half = 0; half < HALVES; ++half)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) s[half][i] = rounded_difference(s[half][i], scale, base);
+          for (int i = 0; i < 16; ++i) s[half][i] = rounded_difference(s[half][i], scale, base) + LIFT<DT>;
       } else {
 #pragma unroll
         for (int half = 0; half < HALVES; ++half)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) s[half][i] = fmaf(s[half][i], scale, -base);
+          for (int i = 0; i < 16; ++i) s[half][i] = fmaf(s[half][i], scale, LIFT<DT> - base);
       }
       u32x4 pf[2 * HALVES];
 #pragma unroll

@@ -119,6 +119,27 @@ def test_large_scores(dtype, size, dim, sign):
                 H.assert_close(got[row, h], want, tol, f"sequence {s} position {pos} head {h}")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("new", [1, 40])
+def test_many_small_weights(dtype, new):
+    """60000 tokens of weight 2^-25.6 beside four of weight 1, one for each wave: in f16 such weights are kept relative to a base that leaves them
+    2^-32 of it as rounding, so that what they add up to is not lost."""
+    t = Tenant(dtype, (2, 1, 64), ((60000, new),), page=64, seed=1)
+    t.q[:], t.k[:], t.v[:] = 0, 0, 1
+    t.q[:, :, 0] = 8
+    for j in (0, 32, 64, 96):
+        p, slot = int(t.table[0, j // 64]), j % 64
+        t.k[p, 0, slot, 0], t.v[p, 0, slot] = 17.75, 0
+    with sk.sk_attn_plan_create([t.to_device()], sk.sk_attn_params_default(workgroups=1)) as plan:
+        sk.sk_attn_launch(plan, H.stream_handle())
+        torch.cuda.synchronize()
+    n = torch.arange(60000 - new + 1, 60001, dtype=torch.float64)[:, None, None] - 4
+    small = n * math.exp(-17.75)
+    want = (small / (4 + small)).expand(new, 2, 64)
+    tol = want * (2 * H.U[dtype] + 2.0 ** -18) + H.TINY[dtype] + (n / 4 * 2.0 ** -32 if dtype == "f16" else 0)
+    H.assert_close(t.out(), want, tol.expand(new, 2, 64), f"{new}")
+
+
 def test_rows_beyond_the_bound_are_left_alone():
     t = Tenant("bf16", (4, 2, 64), ((50, 9), (60, 3)), max_new=4, seed=1)
     problem = t.to_device()
