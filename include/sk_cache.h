@@ -79,7 +79,7 @@ typedef struct {
   int32_t neighbours;  /* which elements are pairs, see above                                                   */
   int32_t positions;   /* rows of cos and sin                                                                   */
   float eps;
-  float scale;         /* of the scores; 0 = 1 / sqrt(head_dim)                                                 */
+  float scale;         /* of the scores, up to 2.3e38; 0 = 1 / sqrt(head_dim)                                   */
   int32_t reserved;    /* 0                                                                                     */
   int64_t page_stride, kv_head_stride, token_stride;
   int64_t qkv_row_stride, q_row_stride, q_head_stride, out_row_stride, out_head_stride;

@@ -47,7 +47,7 @@ sk_status check_problem(const sk_attn_problem &p, AttnDev &d, std::string &err) 
   if ((int64_t)p.rows * p.q_heads >= (int64_t)1 << 31) return refuse(err, SK_ERR_UNSUPPORTED, "2^31 query vectors and more");
   if (p.rotary_dim % 2 || p.rotary_dim > p.head_dim) return refuse(err, SK_ERR_INVALID_ARG, "rotary_dim must be even and at most head_dim");
   if (p.neighbours != 0 && p.neighbours != 1) return refuse(err, SK_ERR_INVALID_ARG, "neighbours must be 0 or 1");
-  if (!(p.eps >= 0.f) || !std::isfinite(p.eps) || !std::isfinite(p.scale)) return refuse(err, SK_ERR_INVALID_ARG, "eps or scale is negative or not finite");
+  if (!(p.eps >= 0.f) || !std::isfinite(p.eps) || !std::isfinite(p.scale)) return refuse(err, SK_ERR_INVALID_ARG, "eps is negative, or eps or scale is not finite");
   if (!p.k || !p.v || !p.page_table || !p.lengths || !p.first_row || !p.q) return refuse(err, SK_ERR_INVALID_ARG, "null pointer");
   if (!p.qkv && !p.out) return refuse(err, SK_ERR_INVALID_ARG, "neither qkv nor out is given");
   for (int64_t s : {p.page_stride, p.kv_head_stride, p.token_stride, p.qkv_row_stride, p.q_row_stride, p.q_head_stride, p.out_row_stride, p.out_head_stride})
@@ -101,6 +101,7 @@ sk_status check_problem(const sk_attn_problem &p, AttnDev &d, std::string &err) 
   d.max_new = p.max_new && p.max_new < p.rows ? p.max_new : p.rows;
   d.window = p.window, d.sinks = p.sinks, d.rotary = p.qkv ? p.rotary_dim : 0, d.neighbours = p.neighbours, d.positions = p.positions, d.eps = p.eps;
   d.scale_log2 = (float)((p.scale != 0.f ? (double)p.scale : 1.0 / std::sqrt((double)dim)) * 1.4426950408889634);
+  if (!std::isfinite(d.scale_log2)) return refuse(err, SK_ERR_INVALID_ARG, "scale times log2(e) is not finite");
   return SK_OK;
 }
 

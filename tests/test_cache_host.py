@@ -80,6 +80,15 @@ def test_more_workgroups_than_a_launch_can_have(change):
     assert "grid" in e.value.detail or "heads" in e.value.detail
 
 
+@pytest.mark.parametrize("scale", [3e38, -2.4e38])
+def test_scales_beyond_fp32(scale):
+    """Scores are kept in powers of two: the scale times log2(e) has to be a number too."""
+    with pytest.raises(sk.SkError) as e:
+        plan(GOOD | dict(scale=scale))
+    assert e.value.status == INVALID and "scale" in e.value.detail
+    plan(GOOD | dict(scale=2.3e38)).close()
+
+
 def test_the_largest_grids_are_planned():
     plan(GOOD | dict(sequences=1 << 20, q_heads=8, kv_heads=8, rows=1 << 20, max_new=1)).close()
     plan(GOOD | dict(rows=(1 << 26) - 64, out=0)).close()
