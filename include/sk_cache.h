@@ -45,20 +45,23 @@ extern "C" {
  *   first_row[s+1]-1 of qkv, q and out (first_row has sequences + 1 entries that do not decrease; none for a sequence is fine), and
  *   the last ones of the sequence: row first_row[s] + t is the token at position lengths[s] - (first_row[s+1] - first_row[s]) + t.
  *   Values beyond the bounds given to the plan are cut to them on the device (lengths to pages_per_sequence * page_tokens, rows to
- *   `rows`; new tokens beyond max_new of a sequence are not computed); tokens whose page number is outside [0, num_pages) count as not there.
+ *   `rows`); tokens whose page number is outside [0, num_pages) count as not there.  sk_attn_launch leaves the rows of new tokens beyond
+ *   max_new of a sequence as they are; sk_attn_append, whose grid does not depend on max_new, appends all new tokens.
  *
  * sk_attn_append, for every new row x = qkv[row] (q_heads query heads, then kv_heads key heads, then kv_heads value heads, of
  *   head_dim elements each, rows qkv_row_stride elements apart, 0 = packed) at position p:
  *     y = x * w / sqrt(mean(x^2) + eps)           per head; queries with q_weight, keys with k_weight; null: y = x
  *     (a, b) -> (a*cos - b*sin, b*cos + a*sin)    for the pairs of the first rotary_dim elements: elements i and i + rotary_dim/2,
  *                                                 or with neighbours = 1 elements 2i and 2i+1, with cos = cos[p*rotary_dim/2 + i]
- *   Queries go to q, keys and values into their pages.  fp32 inside, one rounding at the end.  cos and sin have `positions` rows,
- *   at least pages_per_sequence * page_tokens.  Rows at a position below 0 (more new rows than tokens) or in no page are
+ *   Queries go to q, keys and values into their pages.  fp32 inside, one rounding at the end; the squares are summed in fp32 as they
+ *   are, which elements beyond 2^59 in size overflow and, with eps = 0, elements below 2^-60 may vanish in.  cos and sin have `positions`
+ *   rows, at least pages_per_sequence * page_tokens.  Rows at a position below 0 (more new rows than tokens) or in no page are
  *   not appended; their queries are rotated as at the nearest position.
  *
  * sk_attn_launch, for query head h (key-value head h / (q_heads / kv_heads)) of every new row at position p:
  *     out = sum_j softmax_j(scale * q.k_j) v_j    over the tokens j <= p with: window == 0, or p - j < window, or j < sinks
- *   A row that sees nothing gets zeros; keys and values that a row does not see do not enter its result, whatever they hold.
+ *   A row that sees nothing gets zeros, and so does one all of whose scores are -infinity: such a score is a weight of zero, as one
+ *   that is hidden.  Keys and values that a row does not see do not enter its result, whatever they hold.
  *   Scores, the softmax's running maximum and sum, and the output's sums are fp32; the softmax's weights are rounded to dtype
  *   for the matrix units (their sum is not).
  *

@@ -58,6 +58,10 @@ def test_prompts_take_several_heads_a_wave():
     check_append([tenant("bf16", (8, 2, 64), ((700, 700), (1, 1), (333, 300)), page=64, rotary=64, seed=3), tenant("f16", (2, 1, 128), STEP, rotary=128, seed=4)], "prompts")
 
 
+def test_new_tokens_beyond_the_bound_of_attention_are_appended():
+    check_append([tenant("bf16", (4, 2, 64), ((50, 9), (60, 3)), rotary=64, max_new=2, seed=10)], "max_new")
+
+
 def test_many_sequences_and_several_tenants():
     seqs = tuple((1 + i % 50, i % 2) for i in range(5000))
     check_append([tenant("bf16", (1, 1, 8), seqs, rotary=8, seed=5)] + [tenant("f16", (2, 1, 16), STEP, rotary=16, seed=i) for i in range(70)], "many")

@@ -140,6 +140,27 @@ def test_many_small_weights(dtype, new):
     H.assert_close(t.out(), want, tol.expand(new, 2, 64), f"{new}")
 
 
+@pytest.mark.parametrize("dtype,dim", [("bf16", 64), ("f16", 256)])
+@pytest.mark.parametrize("window", [0, 30])
+def test_scores_of_minus_infinity_are_hidden(dtype, dim, window):
+    """Keys with which every query's product is -inf are as keys that are not there, down to rows that see no others."""
+    seqs = ((60, 1), (60, 60), (300, 3), (200, 90))
+    t = Tenant(dtype, (4, 2, dim), seqs, window=window, seed=dim)
+    t.q[..., 3] = t.q[..., 3].abs() + 0.5
+    gone = Tenant(dtype, (4, 2, dim), seqs, window=window, seed=dim)
+    gone.q = t.q.clone()
+    for s, pages in {0: (0, 1, 2, 3), 1: (0, 1, 3), 2: (2, 5, 17, 18), 3: (0, 7, 8, 9, 10, 11, 12)}.items():
+        for c in pages:
+            t.k[int(t.table[s, c]), :, :, 3] = -math.inf
+            gone.table[s, c] = -1
+    want, tol = gone.attend()
+    with sk.sk_attn_plan_create([t.to_device()]) as plan:
+        sk.sk_attn_launch(plan, H.stream_handle())
+        torch.cuda.synchronize()
+    assert (want[0] == 0).all() and (want[1:17] == 0).all()
+    H.assert_close(t.out(), want, tol)
+
+
 def test_rows_beyond_the_bound_are_left_alone():
     t = Tenant("bf16", (4, 2, 64), ((50, 9), (60, 3)), max_new=4, seed=1)
     problem = t.to_device()
