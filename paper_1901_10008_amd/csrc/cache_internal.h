@@ -68,7 +68,7 @@ struct AttnPlanHost {
   std::vector<AttnGroup> groups;
   std::vector<uint32_t> append_first;  // first workgroup of each problem, and the number of all
   bool append_once = false;            // append moves more than PAST_CACHES bytes
-  bool any_qkv = false, all_qkv = true, any_out = false, all_out = true;
+  bool all_qkv = true, all_out = true;
   int64_t workspace_floats = 0, counters = 0;  // of the largest group: launches of a plan do not overlap
 };
 

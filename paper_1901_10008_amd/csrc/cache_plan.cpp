@@ -119,8 +119,8 @@ sk_status plan_attn(const sk_attn_problem *problems, int32_t n, int32_t compute_
       err = "problem " + std::to_string(i) + ": " + err;
       return st;
     }
-    (d.qkv ? out.any_qkv : out.all_qkv) = d.qkv != nullptr;
-    (d.out ? out.any_out : out.all_out) = d.out != nullptr;
+    out.all_qkv = out.all_qkv && d.qkv;
+    out.all_out = out.all_out && d.out;
     if (d.qkv) written.emplace_back((uintptr_t)d.q, (uintptr_t)d.q + 2 * (uintptr_t)extent(d.rows, d.q_row, d.q_heads, d.q_head, d.dim));
     if (d.out) written.emplace_back((uintptr_t)d.out, (uintptr_t)d.out + 2 * (uintptr_t)extent(d.rows, d.out_row, d.q_heads, d.out_head, d.dim));
     // append: 8 elements a lane; a wave takes a whole row's heads where there are rows enough to fill the card, a part of them otherwise
