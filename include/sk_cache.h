@@ -112,8 +112,8 @@ void sk_attn_params_default(sk_attn_params *params);
  * heads or tokens overlap, cos and sin with too few rows), SK_ERR_UNSUPPORTED (SK_F32; a head_dim that is no multiple of
  * 8 or larger than 256; page_tokens that is no power of two from 16 on; pointers or strides that are no multiples of 16 bytes;
  * sequences of 2^31 tokens and more; more than 2^20 sequences; more than 2^30 heads; a token_stride of 2^26 elements and more;
- * more units of work than the 2^24 - 1 workgroups of a launch), SK_ERR_OVERLAP (q or out of two problems, or of one,
- * intersect), SK_ERR_ALLOC, SK_ERR_HIP.
+ * more units of work than the 2^24 - 1 workgroups of a launch), SK_ERR_OVERLAP (what q or out of two problems, or of
+ * one, span from their first to their last element intersects), SK_ERR_ALLOC, SK_ERR_HIP.
  */
 sk_status sk_attn_plan_create(const sk_attn_problem *problems, int32_t n, const sk_attn_params *params, sk_attn_plan **out);
 /* Waits for the plan's launches and frees it; null is accepted. */

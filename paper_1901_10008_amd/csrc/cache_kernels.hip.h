@@ -138,8 +138,8 @@ __device__ __forceinline__ f32x2 load_shared(const float *p) {
 // ---------------------------------------------------------------------------
 // The lengths are in device memory, so the units (a block of rows of a key-value head of a sequence, and a slice of its
 // keys) are counted on the device: every workgroup looks at all sequences of the launch and finds its own unit from the sums
-// before it; workgroups beyond the last leave.  Units of many rows come first, those of late rows (which see the most) before those of early ones; key-value heads
-// vary fastest, so that with eight of them each has a die (and its L2) of its own.
+// before it; workgroups beyond the last leave.  Units of many rows come first, those of late rows (which see the most) before those of early
+// ones; key-value heads vary fastest, so that with eight of them each has a die (and its L2) of its own.
 
 __device__ __forceinline__ Step step_of(const AttnSeq &q) { return step_of(q, load_i32(q.first), load_i32(q.first + 1), load_i32(q.length)); }
 
@@ -228,8 +228,8 @@ __device__ __forceinline__ Unit find_unit(const AttnArgs &a, FindScratch *f) {
     const int32_t units = lane_of(wave_scan(items_of(c, 1)), 63);
     const int64_t work = lane_of(wave_scan(work_of(c)), 63);
     int32_t most = even_share(work, a.workgroups), splits = splits_of(c, most);
-    // Few units: slices as short as leaves all of them running at once.  (A slice costs its workgroup 5 us besides the keys: six caches
-    // of 50 to 120 thousand tokens take 271 us in one round of slices, 281 in two, 288 in four.)
+    // Few units: slices as short as leaves all of them running at once.  (A slice costs its workgroup 5 us besides the keys: six caches of 50
+    // to 120 thousand tokens take 7 and 5 % longer in two and four rounds of slices, 96 caches with a window of 1024 12 and 32 %.)
     for (int i = 0; i < 8 && units <= a.workgroups / 2 && lane_of(wave_scan(c.units * splits), 63) > a.workgroups; ++i) {
       most += most / 8 + 1;
       splits = splits_of(c, most);
@@ -492,9 +492,9 @@ __device__ __forceinline__ u32x4 load_query(const void *p, bool ok, bool negate)
 // right operand of V^T P.  Keys go from memory straight into the left operand's registers (no wave needs another's), a step ahead; values
 // have to be turned round, so they go by direct loads into LDS that is the wave's own and come back by transposing reads: no barrier in the
 // loop.  The four waves take steps in turn and add up through LDS at the end.  Bound by memory: keys and values are read once, and what
-// matters is bytes in flight: three workgroups of four waves on a compute unit, each wave with 16 KB (heads of 128) on their way.  Six caches of 50 to 120
-// thousand tokens, 8 heads of 128: 1.6 GB in 277 us, 5.8 TB/s (a streaming read 6.6, a copy 5.2); 96 caches of up to 8000 tokens 72 us,
-// 4.5 TB/s with the ends of units; one of 800 tokens 7.5 us, of which 2 are finding the unit and 2 the way of the first keys.
+// matters is bytes in flight: three workgroups of four waves on a compute unit, each wave with 16 KB (heads of 128) on their way.  Six caches
+// of 50 to 120 thousand tokens, 8 heads of 128: 1.6 GB in 278 us, 5.8 TB/s (a streaming read 6.6, a copy 5.2); 96 caches of up to 8000 tokens
+// 71.6 us, 4.5 TB/s with the ends of units; one of 800 tokens 7.7 us a call, of which 2 are finding the unit and 2 the way of the first keys.
 template <int DT, int DP>
 __device__ __forceinline__ void attend_few(const AttnArgs &a, const SK_CONSTANT AttnDev &P, const Unit &u, unsigned char *lds, uint32_t *flag) {
   constexpr int64_t SLOT = part_floats(ROWS_FEW, DP <= 128 ? 128 : 256);
@@ -805,8 +805,8 @@ struct ManyLds {
 // above: a lane holds half the scores of one row, and P needs no trip through LDS.  Matrix instructions of 32x32x16, which need half the operand
 // bytes a product of the 16x16x32 ones.  Tiles come by direct loads into the other of two places while one is used; pieces are turned over
 // so that neither reads of keys nor the transposing reads of values meet in a bank (conflicts 0; 59 million without).  Operands are read from
-// LDS two groups of four ahead.  Bound by what a wave can issue, and power: prompts of 7000 to 8100 tokens, 32 query heads of 128, 967 us,
-// 1000 TFLOP/s of the pairs that are seen (a large library product 1483): 360 instructions a tile, 32 of them matrix instructions, one in about five
+// LDS two groups of four ahead.  Bound by what a wave can issue, and power: prompts of 7000 to 8100 tokens, 32 query heads of 128, 969 us,
+// 996 TFLOP/s of the pairs that are seen (a large library product 1483): 360 instructions a tile, 32 of them matrix instructions, one in about five
 // cycles; the matrix units are busy 48 % of the cycles, LDS 24 %.  Scores of the next tile beside the softmax of this one gave nothing.
 constexpr int SETS = 3;  // groups of LDS operands in registers: one in use, two on their way
 

@@ -34,7 +34,7 @@ __device__ __forceinline__ int32_t last_not_above(const T *first, int32_t n, int
 }
 
 // Loads and stores of what a launch will not see again, past the caches (ONCE) where it moves more than PAST_CACHES bytes: what is there
-// stays there, and the launch is faster by as much (19000 rows of 48 heads of 128 104 -> 97 us, 1 GB of pages 217 -> 210).  A smaller launch's
+// stays there, and the launch is faster by as much (19000 rows of 48 heads of 128 by 7 %, 1 GB of pages by 3 %).  A smaller launch's
 // outputs would be found in the caches by the one that reads them.
 template <bool ONCE>
 __device__ __forceinline__ u32x4 load16_once(const void *p) {
@@ -69,8 +69,8 @@ enum { ROTATE_NONE, ROTATE_HALVES, ROTATE_NEIGHBOURS, ROTATE_ANY };
 
 // A wave takes some heads of a row, 8 elements a lane, in turns of as many heads as it has lanes for.  What a lane needs of the angles and weights is
 // the same in every turn and stays in registers; the other element of a pair is read from memory once more (the line is in the L1)
-// and normalised like the first.  Bound by memory: every element is read and written once; 19000 rows of 48 heads of 128, 469 MB in 97 us,
-// 4.8 TB/s (a large copy 5.15).  A step of few rows is bound by a launch and its chain of loads (row, sequence, page, heads): 3 rows 3.7 us.
+// and normalised like the first.  Bound by memory: every element is read and written once; 19000 rows of 48 heads of 128, 469 MB in 96 us,
+// 4.9 TB/s (a large copy 5.15).  A step of few rows is bound by a launch and its chain of loads (row, sequence, page, heads): 3 rows 3.6 us.
 template <int DT, int ROTATE, bool ONCE>
 __device__ __forceinline__ void append_heads(const SK_CONSTANT AttnDev &P, int64_t row, int32_t part, int lane, int64_t angle, bool there, int64_t slot) {
   const int lph = P.lanes_per_head, e0 = (lane & (lph - 1)) * 8, at_once = 64 / lph, dim = P.dim, half = P.rotary / 2;
@@ -234,8 +234,9 @@ __global__ void __launch_bounds__(CACHE_THREADS) sk_append(AppendArgs a) {
 // ---------------------------------------------------------------------------
 // copies of pages
 // ---------------------------------------------------------------------------
-// Bound by memory: 500 pages of 32 KB in each of 32 arrays, 1.05 GB read and written in 210 us, 5.0 TB/s.  A workgroup copies a chunk of a page of an array; those behind the copies bring changed rows of the page table, out of the launch's arguments
-// where they fit (a fork into sixteen sequences of 50 pages: 4.2 us so, 6.0 with the rows in host memory).
+// Bound by memory: 500 pages of 32 KB in each of 32 arrays, 1.05 GB read and written in 211 us, 5.0 TB/s.  A workgroup copies a chunk of a page
+// of an array; those behind the copies bring changed rows of the page table, out of the launch's arguments where they fit (a fork into sixteen
+// sequences of 50 pages: 4.4 us so, 6.0 with the rows in host memory).
 template <bool ONCE>
 __global__ void __launch_bounds__(CACHE_THREADS) sk_copy_pages(CopyArgs a) {
   const int64_t per_move = a.chunks * a.n_arrays;

@@ -124,8 +124,9 @@ SK_BOTH int64_t divide(int64_t n, int64_t d) { return (int64_t)((double)n / (dou
 SK_BOTH int32_t slice_start(int32_t blocks, int32_t split, int32_t splits) { return splits == 1 ? split * blocks : (int32_t)divide((int64_t)blocks * split, splits); }
 
 // Units of many keys are cut into slices, so that few units fill the card and no unit is what the launch waits for.  A slice takes at most `most`
-// blocks of keys of few rows, or a TILE_WORK-th as many tiles of many: a tile takes 2 us, a block 0.5 to 1 (chunks beside single tokens, twelve
-// sequences: 58.1 us with a ratio of 2, 55.5 of 3, 58.8 of 4; launches of one kind do not care).
+// blocks of keys of few rows, or a TILE_WORK-th as many tiles of many: a tile takes 2 us, a block 0.5 to 1.  Of sixteen launches
+// that mix chunks and single tokens one is 5 % slower with a ratio of 2 and 2 % faster with 4, one 8 % faster with 2 and 10 % slower with 4; the
+// others take the same time within 2 %.
 constexpr int TILE_WORK = 3;
 constexpr int LEAST = 4;  // a block for each wave; tiles
 SK_BOTH int32_t splits_of(const Count &c, int32_t most) {
