@@ -46,3 +46,12 @@ from .cache import (  # noqa: F401
     sk_attn_append, sk_attn_launch, sk_attn_params_default, sk_attn_plan_create, sk_attn_plan_destroy, sk_attn_plan_info,
     sk_pages_apply, sk_pages_compact, sk_pages_copy, sk_pages_create, sk_pages_destroy, sk_pages_fork, sk_pages_resize, sk_pages_state,
 )
+from .layer import (  # noqa: F401
+    LAYER_SYMBOLS,
+    LayerParams, MoePlan, NormPlan, VerifyPlan, sk_moe_problem, sk_norm_problem, sk_verify_problem,
+    SK_ACT_NONE, SK_ACT_SIGMOID, SK_ACT_SILU, SK_ACT_TANH, SK_ACT_GELU, SK_ACT_RELU, SK_NORM_RMS, SK_NORM_LAYER, SK_MOE_SOFTMAX, SK_MOE_SIGMOID,
+    layer_lib, layer_lib_path,
+    make_moe_problem, make_norm_problem, make_verify_problem, sk_layer_params_default,
+    sk_moe_launch, sk_moe_plan_create, sk_moe_plan_destroy, sk_moe_plan_info, sk_norm_launch, sk_norm_plan_create, sk_norm_plan_destroy,
+    sk_verify_launch, sk_verify_plan_create, sk_verify_plan_destroy, sk_verify_plan_info,
+)

@@ -1,4 +1,4 @@
-"""Build libsuperkernel.so and libsk_cache.so (HIP, gfx950 only) in-tree next to this file."""
+"""Build libsuperkernel.so, libsk_cache.so and libsk_layer.so (HIP, gfx950 only) in-tree next to this file."""
 from __future__ import annotations
 
 import os
@@ -17,6 +17,9 @@ HEADERS = ["kernels.hip.h", "sk_internal.h", os.path.join(ROOT, "include", "supe
 CACHE_LIB = os.path.join(HERE, "libsk_cache.so")  # attention's side of decoder layers (include/sk_cache.h)
 CACHE_SOURCES = ["cache.hip", "cache_plan.cpp", "cache_instances.hip"]
 CACHE_UNITS = 4  # units of compilation of cache_instances.hip
+
+LAYER_LIB = os.path.join(HERE, "libsk_layer.so")  # the rest of a decoder step (include/sk_layer.h)
+LAYER_SOURCES = ["layer_norm.hip", "layer_moe.hip", "layer_verify.hip", "layer_plan.cpp"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -118,6 +121,23 @@ def build_cache(verbose: bool = False, extra=(), lib: str = CACHE_LIB) -> str:
     return lib
 
 
+def build_layer(verbose: bool = False, extra=(), lib: str = LAYER_LIB) -> str:
+    """libsk_layer.so, linked to the libsuperkernel.so beside it (statuses and error texts are that library's)."""
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    inc = ["-I", os.path.join(ROOT, "include"), "-I", CSRC]
+    obj_dir = os.path.join(HERE, "_build")
+    os.makedirs(obj_dir, exist_ok=True)
+    objects = [os.path.join(obj_dir, os.path.splitext(s)[0] + ".o") for s in LAYER_SOURCES]
+    compiles = [[hipcc, *HIPCC_FLAGS, *extra, *inc, "-c", os.path.join(CSRC, s), "-o", o] if s.endswith(".hip") else
+                ["g++", "-O2", "-std=c++17", "-fPIC", "-Wall", *inc, "-c", os.path.join(CSRC, s), "-o", o] for s, o in zip(LAYER_SOURCES, objects)]
+    run = _runner(verbose)
+    with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:
+        list(pool.map(run, compiles))
+    run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *objects, "-L", HERE, "-l:libsuperkernel.so", "-Wl,-rpath,$ORIGIN", "-Wl,--no-undefined", "-o", lib])
+    return lib
+
+
 if __name__ == "__main__":
     print(build(force=True, verbose=True))
     print(build_cache(verbose=True))
+    print(build_layer(verbose=True))

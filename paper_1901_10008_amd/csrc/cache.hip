@@ -1,12 +1,8 @@
 // Entry points of libsk_cache.so: attention plans and their launches, the account of pages and its copies.
-#include <hip/hip_ext.h>
-#include <hip/hip_runtime.h>
-
 #include <cstring>
-#include <new>
 
 #include "cache_rows.hip.h"
-#include "sk_internal.h"
+#include "hip_host.h"
 
 namespace sk {
 extern template __global__ void sk_attend<false, false>(AttnArgs);
@@ -17,48 +13,25 @@ extern template __global__ void sk_attend<true, true>(AttnArgs);
 
 namespace {
 
+using sk::admit;
+using sk::align_up;
+using sk::capturing;
+using sk::check_resident;
+using sk::guarded;
+using sk::hip_error;
+using sk::launch;
 using sk::set_last_error;
-
-sk_status hip_error(const char *what, hipError_t e) { return set_last_error(SK_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e)); }
-
-size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-
-// Every entry point's body runs in here: no exception leaves the library.
-template <class F>
-sk_status guarded(F f) {
-  try {
-    return f();
-  } catch (const std::bad_alloc &) {
-    try {
-      return set_last_error(SK_ERR_ALLOC, "host allocation failed");
-    } catch (...) {
-      return SK_ERR_ALLOC;
-    }
-  } catch (...) {
-    return SK_ERR_INVALID_ARG;
-  }
-}
-
-bool capturing(hipStream_t stream) {
-  hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
-  return hipStreamIsCapturing(stream, &cs) != hipSuccess || cs != hipStreamCaptureStatusNone;
-}
 
 }  // namespace
 
-struct sk_attn_plan {
+struct sk_attn_plan : sk::PlanOnDevice {
   sk::AttnPlanHost host;
-  int device = -1;
-  bool resident = false;
-  char *blob = nullptr;
   const sk::AttnDev *problems = nullptr;
   const sk::AttnSeq *seqs = nullptr;
   const uint32_t *append_first = nullptr;
   uint32_t *arrivals = nullptr;
   float *workspace = nullptr;
-  hipEvent_t last_use = nullptr;  // completes with the latest launch made outside a stream capture
-  sk::LaunchLedger ledger;        // of sk_attn_launch
-  bool appended = false;          // sk_attn_append has been called
+  bool appended = false;  // sk_attn_append has been called
 };
 
 struct sk_pages {
@@ -73,48 +46,6 @@ struct sk_pages {
 };
 
 namespace {
-
-sk_status check_resident(const sk_attn_plan *plan) {
-  if (!plan) return set_last_error(SK_ERR_INVALID_ARG, "plan is null");
-  if (!plan->resident) return set_last_error(SK_ERR_STATE, "plan was created host-only; it has no device tables");
-  int dev = -1;
-  hipError_t e = hipGetDevice(&dev);
-  if (e != hipSuccess) return hip_error("hipGetDevice", e);
-  if (dev != plan->device) return set_last_error(SK_ERR_STATE, "plan belongs to another device than the current one");
-  return SK_OK;
-}
-
-// As for the plans of superkernel.h: SK_ERR_BUSY while the previous launch still runs on another stream.
-sk_status admit(sk_attn_plan *plan, hipStream_t stream, bool *in_capture) {
-  const sk_status st = check_resident(plan);
-  if (st != SK_OK) return st;
-  *in_capture = capturing(stream);
-  if (plan->ledger.before_launch((uintptr_t)stream, *in_capture) == sk::LaunchLedger::QUERY_EVENT) {
-    const hipError_t e = hipEventQuery(plan->last_use);
-    if (e == hipErrorNotReady) {
-      (void)hipGetLastError();
-      return set_last_error(SK_ERR_BUSY, "the plan's previous launch is still running on another stream");
-    }
-    if (e != hipSuccess) return hip_error("hipEventQuery", e);
-  }
-  if (!*in_capture && !plan->last_use && hipEventCreateWithFlags(&plan->last_use, hipEventDisableTiming) != hipSuccess) {
-    (void)hipGetLastError();
-    plan->last_use = nullptr;
-  }
-  return SK_OK;
-}
-
-// A launch whose completion is an event's signal (null: none).
-template <class K, class A>
-sk_status launch(K kernel, int64_t grid, hipStream_t stream, hipEvent_t behind, const A &args) {
-  const dim3 g((unsigned)grid), b(sk::CACHE_THREADS);
-  if (behind)
-    hipExtLaunchKernelGGL(kernel, g, b, 0, stream, nullptr, behind, 0, args);
-  else
-    hipLaunchKernelGGL(kernel, g, b, 0, stream, args);
-  const hipError_t e = hipGetLastError();
-  return e == hipSuccess ? SK_OK : hip_error("kernel launch", e);
-}
 
 void (*attend_kernel(const sk::AttnGroup &g))(sk::AttnArgs) {
   if (g.wide) return g.many ? sk::sk_attend<true, true> : sk::sk_attend<false, true>;
@@ -262,17 +193,7 @@ sk_status sk_attn_plan_create(const sk_attn_problem *problems, int32_t n, const 
 sk_status sk_attn_plan_destroy(sk_attn_plan *plan) {
   if (!plan) return SK_OK;
   return guarded([&]() -> sk_status {
-    hipError_t e = hipSuccess;
-    const sk::LaunchLedger::Wait wait = plan->appended ? sk::LaunchLedger::DEVICE : plan->ledger.before_destroy();
-    if (wait == sk::LaunchLedger::EVENT) {
-      e = hipEventSynchronize(plan->last_use);
-    } else if (wait == sk::LaunchLedger::DEVICE) {
-      int cur = -1;
-      e = hipGetDevice(&cur);
-      if (e == hipSuccess && cur != plan->device) e = hipSetDevice(plan->device);
-      if (e == hipSuccess) e = hipDeviceSynchronize();
-      if (cur >= 0 && cur != plan->device) (void)hipSetDevice(cur);
-    }
+    const hipError_t e = sk::wait_for(plan, plan->appended);
     const sk_status st = e == hipSuccess ? SK_OK : hip_error("waiting for the plan's launches", e);
     if (e != hipSuccess) plan->blob = nullptr;  // not freed under a kernel that may still run
     release(plan);

@@ -7,14 +7,12 @@
 #include <string>
 #include <vector>
 
+#include "launch_limits.h"
 #include "sk_cache.h"
 #include "sk_internal.h"
 
 namespace sk {
 
-constexpr int CACHE_THREADS = 256;
-// Workgroups of a launch: the runtime refuses 2^32 threads and more.
-constexpr int64_t MOST_GRID = (((int64_t)1 << 32) - 1) / CACHE_THREADS;
 // Rows of a unit of work (a key-value head of a sequence): few rows go in blocks of ROWS_FEW, whose four waves share the
 // keys among them; more than most_few() rows go in blocks of ROWS_MANY, whose waves share the rows.
 constexpr int ROWS_FEW = 16, ROWS_MANY = 128;
@@ -24,7 +22,6 @@ constexpr int ROWS_FEW = 16, ROWS_MANY = 128;
 constexpr int most_few(int dim) { return dim > 64 && dim <= 128 ? 16 : 32; }
 constexpr int KEYS_FEW = 32;                                  // keys per step
 constexpr int keys_many(int dim) { return dim <= 128 ? 64 : 32; }  // keys of a tile (heads of 256: two tiles of 64 would take 128 KB of LDS and 64 more registers)
-constexpr int64_t PAST_CACHES = (int64_t)160 << 20;  // bytes that a launch reads and writes (the last-level cache holds 256 MiB)
 constexpr int APPEND_WAVES = 8192;  // append: a problem's rows are cut into parts for at least that many waves where they have the heads for it
 constexpr int MOST_SPLITS = 256;              // workgroups that share a unit's keys, at most
 

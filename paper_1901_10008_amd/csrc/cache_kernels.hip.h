@@ -1,137 +1,14 @@
 // Device code of libsk_cache.so (gfx950 / CDNA4 only): attention over paged caches, and what its kernels share with cache_rows.hip.h.
 #pragma once
 
-#include <hip/hip_runtime.h>
-#include <stdint.h>
+#include "device.hip.h"
 
 #include <type_traits>
 
 #include "cache_internal.h"
 #include "cache_units.h"
 
-#if defined(__HIP_DEVICE_COMPILE__) && !defined(__gfx950__)
-#error "written for gfx950"
-#endif
-
 namespace sk {
-
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-
-// (pointers out of descriptors: said to be global, so that loads are not flat ones)
-#define SK_GLOBAL __attribute__((address_space(1)))
-__device__ __forceinline__ u32x4 load16(const void *p) { return *(const u32x4 SK_GLOBAL *)(uintptr_t)p; }
-__device__ __forceinline__ int32_t load_i32(const int32_t *p) { return *(const int32_t SK_GLOBAL *)(uintptr_t)p; }
-__device__ __forceinline__ void store16(void *p, u32x4 v) { *(u32x4 SK_GLOBAL *)(uintptr_t)p = v; }
-__device__ __forceinline__ void store8(void *p, u32x2 v) { *(u32x2 SK_GLOBAL *)(uintptr_t)p = v; }
-
-// What a lane reads that must count as zeros: its address is replaced, so that no load stands under a branch.
-__device__ __attribute__((aligned(16))) const uint32_t g_zeros[4] = {0u, 0u, 0u, 0u};
-
-template <int DT>
-__device__ __forceinline__ float elem(uint32_t bits) {
-  if constexpr (DT == SK_BF16) return __builtin_bit_cast(float, bits << 16);
-  return (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
-}
-template <int DT>
-__device__ __forceinline__ void unpack8(const u32x4 &v, float (&x)[8]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = elem<DT>(v[i] & 0xffffu);
-    x[2 * i + 1] = elem<DT>(v[i] >> 16);
-  }
-}
-// Two values rounded to nearest even, the first in the low half.
-template <int DT>
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-  const f32x2 v = {lo, hi};
-  if constexpr (DT == SK_BF16) {
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
-  } else {
-    typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
-  }
-}
-template <int DT>
-__device__ __forceinline__ void mma16(const u32x4 &a, const u32x4 &b, f32x4 &c) {
-  if constexpr (DT == SK_BF16)
-    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-  else
-    c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-}
-template <int DT>
-__device__ __forceinline__ void mma32(const u32x4 &a, const u32x4 &b, f32x16 &c) {
-  if constexpr (DT == SK_BF16)
-    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-  else
-    c = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-}
-// The transposing LDS read: each group of 16 lanes reads four rows of 16 16-bit elements, lane i of the group elements
-// 4 (i % 4) .. + 3 of row i / 4, and gets column i: four elements, one per row.
-__device__ __forceinline__ u32x2 read_transposed(const unsigned char *p) {
-  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(unsigned char *)p));
-}
-// What nothing writes while the kernel runs, read through the scalar cache (its address the same in all lanes).
-#define SK_CONSTANT __attribute__((address_space(4)))
-// Sum over the lanes up to this one, in the vector unit: within rows of 16, then from row to row.
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int32_t shifted(int32_t v) {
-  return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
-}
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int64_t shifted(int64_t v) {
-  const uint32_t lo = (uint32_t)shifted<CTRL, ROWS>((int32_t)v), hi = (uint32_t)shifted<CTRL, ROWS>((int32_t)(v >> 32));
-  return (int64_t)((uint64_t)hi << 32 | lo);
-}
-template <class T>
-__device__ __forceinline__ T wave_scan(T v) {
-  v += shifted<0x111, 0xf>(v);  // row_shr:1, 2, 4, 8
-  v += shifted<0x112, 0xf>(v);
-  v += shifted<0x114, 0xf>(v);
-  v += shifted<0x118, 0xf>(v);
-  v += shifted<0x142, 0xa>(v);  // row_bcast:15 into the second and fourth row
-  v += shifted<0x143, 0xc>(v);  // row_bcast:31 into the upper half
-  return v;
-}
-__device__ __forceinline__ int32_t lane_of(int32_t v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
-__device__ __forceinline__ int64_t lane_of(int64_t v, int lane) {
-  return (int64_t)((uint64_t)(uint32_t)lane_of((int32_t)(v >> 32), lane) << 32 | (uint32_t)lane_of((int32_t)v, lane));
-}
-// The larger (or the sum) of a lane's value and that of the lane 16, or 32, places away, without a trip through LDS.
-__device__ __forceinline__ void across16(float v, float &a, float &b) {
-  const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
-  const uint32_t x = r[0], y = r[1];  // (a bit cast of a single vector element reads element 0)
-  a = __builtin_bit_cast(float, x);
-  b = __builtin_bit_cast(float, y);
-}
-__device__ __forceinline__ void across32(float v, float &a, float &b) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
-  const uint32_t x = r[0], y = r[1];  // (a bit cast of a single vector element reads element 0)
-  a = __builtin_bit_cast(float, x);
-  b = __builtin_bit_cast(float, y);
-}
-__device__ __forceinline__ float max16(float v) { float a, b; across16(v, a, b); return fmaxf(a, b); }
-__device__ __forceinline__ float max32(float v) { float a, b; across32(v, a, b); return fmaxf(a, b); }
-__device__ __forceinline__ float sum16(float v) { float a, b; across16(v, a, b); return a + b; }
-__device__ __forceinline__ float sum32(float v) { float a, b; across32(v, a, b); return a + b; }
-
-__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
-
-// Partial results that another workgroup reads, maybe behind another L2: written through to memory and read from there
-// (device scope).
-__device__ __forceinline__ void store_shared(float *p, f32x2 v) {
-  __hip_atomic_store((unsigned long long *)p, __builtin_bit_cast(unsigned long long, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ f32x2 load_shared(const float *p) {
-  return __builtin_bit_cast(f32x2, __hip_atomic_load((const unsigned long long *)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-}
 
 // ---------------------------------------------------------------------------
 // which unit of work a workgroup takes
@@ -331,21 +208,6 @@ __device__ __forceinline__ Unit find_unit(const AttnArgs &a, FindScratch *f) {
   __syncthreads();
   if (!f->unit.any) return f->unit;
   return unit_in_lane(f->unit, 0);
-}
-
-// The slices of a unit but the last to arrive leave; true for that one.  Every wave's partial results have gone through to memory
-// (device-scope stores, waited for) before one thread counts the workgroup in, so a relaxed count is enough on this hardware; the
-// last one reads them with device-scope loads.  It also sets the count back for the next launch.
-__device__ __forceinline__ bool last_to_arrive(uint32_t *arrivals, int32_t splits, uint32_t *flag) {
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    const uint32_t n = __hip_atomic_fetch_add(arrivals, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    *flag = n;
-    if (n + 1 == (uint32_t)splits) __hip_atomic_store(arrivals, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  }
-  __syncthreads();
-  return *flag + 1 == (uint32_t)splits;
 }
 
 // ---------------------------------------------------------------------------

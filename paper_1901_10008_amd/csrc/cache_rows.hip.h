@@ -8,60 +8,11 @@ namespace sk {
 // ---------------------------------------------------------------------------
 // norm, rotation, append
 // ---------------------------------------------------------------------------
-typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
-__device__ __forceinline__ f32x4 load_f4_any(const float *p) { return *(const f32x4_any SK_GLOBAL *)(uintptr_t)p; }
-__device__ __forceinline__ float load_f(const float *p) { return *(const float SK_GLOBAL *)(uintptr_t)p; }
-__device__ __forceinline__ uint32_t load_u16(const void *p) { return *(const uint16_t SK_GLOBAL *)(uintptr_t)p; }
-
 struct AppendArgs {
   const AttnDev *problems;
   const uint32_t *first;  // first workgroup of each problem
   int32_t n;
 };
-
-// The last index i of [0, n) with first[i] <= x, 64 candidates at a time (first[0] <= x, not decreasing; x the same in all lanes).
-template <class T>
-__device__ __forceinline__ int32_t last_not_above(const T *first, int32_t n, int64_t x, int lane) {
-  int32_t lo = 0;
-  while (n > 1) {
-    const int32_t step = (n + 63) / 64, i = lo + lane * step;
-    const bool le = lane * step < n && (int64_t)(*(const T SK_GLOBAL *)(uintptr_t)(first + i)) <= x;
-    const int32_t hit = max(1, (int32_t)__popcll(__ballot(le))) - 1;
-    lo += hit * step;
-    n = min(step, n - hit * step);
-  }
-  return lo;
-}
-
-// Loads and stores of what a launch will not see again, past the caches (ONCE) where it moves more than PAST_CACHES bytes: what is there
-// stays there, and the launch is faster by as much (19000 rows of 48 heads of 128 by 7 %, 1 GB of pages by 3 %).  A smaller launch's
-// outputs would be found in the caches by the one that reads them.
-template <bool ONCE>
-__device__ __forceinline__ u32x4 load16_once(const void *p) {
-  if constexpr (ONCE) return __builtin_nontemporal_load((const u32x4 SK_GLOBAL *)(uintptr_t)p);
-  return load16(p);
-}
-template <bool ONCE>
-__device__ __forceinline__ void store16_once(void *p, u32x4 v) {
-  if constexpr (ONCE)
-    __builtin_nontemporal_store(v, (u32x4 SK_GLOBAL *)(uintptr_t)p);
-  else
-    store16(p, v);
-}
-
-// The sum over groups of 1, 2, 4, .. 32 neighbouring lanes, in each of them.
-template <int CTRL>
-__device__ __forceinline__ float other_lane(float v) {
-  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int32_t, v), CTRL, 0xf, 0xf, false));
-}
-__device__ __forceinline__ float sum_over(float v, int lanes) {
-  if (lanes >= 2) v += other_lane<0xb1>(v);    // quad_perm: the other of two
-  if (lanes >= 4) v += other_lane<0x4e>(v);    // quad_perm: the other two of four
-  if (lanes >= 8) v += other_lane<0x141>(v);   // row_half_mirror
-  if (lanes >= 16) v += other_lane<0x140>(v);  // row_mirror
-  if (lanes >= 32) v = sum16(v);
-  return v;
-}
 
 // How a row's heads are rotated: not at all; pairs of elements half the rotated length apart, where that is whole pieces of 8; neighbours, in
 // whole pieces; element by element.

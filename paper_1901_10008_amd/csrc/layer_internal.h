@@ -1,0 +1,133 @@
+// Internal declarations of libsk_layer.so, shared by its host planning and its kernels.  Not part of the public ABI
+// (include/sk_layer.h is).
+#pragma once
+
+#include <cstddef>
+#include <cstdint>
+#include <string>
+#include <vector>
+
+#include "launch_limits.h"
+#include "sk_internal.h"
+#include "sk_layer.h"
+
+namespace sk {
+
+// ---- norms -----------------------------------------------------------------------------------------------------------------
+
+// A problem as the kernel sees it (strides in elements), in the launch's arguments: a step's norms take a launch and two trips to memory, so a
+// third one for descriptors would be felt.
+struct NormDev {
+  const int32_t *n_rows;
+  const void *block, *gate, *residual, *post_weight, *post_bias, *pre_weight, *pre_bias;
+  void *residual_out, *next;
+  int64_t block_stride, gate_stride, residual_stride, residual_out_stride, next_stride;  // (gate_stride 0: one gate for all rows)
+  int32_t rows, dim;
+  float eps, residual_scale, block_scale;
+  int8_t dtype, residual_dtype, kind, post, act, pad[3];
+};
+constexpr int NORM_PROBLEMS = 16;  // of a launch
+struct NormArgs {
+  uint32_t first[NORM_PROBLEMS];  // workgroup of the launch; none: the largest number
+  NormDev problems[NORM_PROBLEMS];
+};
+static_assert(sizeof(NormArgs) <= 4096, "kernel arguments");
+
+// What a row gets: a wave (rows of up to 2048 elements), a workgroup of four waves, or one of sixteen; up to 4 pieces of 8 elements a thread.
+enum NormForm { NORM_WAVE, NORM_GROUP, NORM_LONG, NORM_FORMS };
+constexpr int NORM_LONG_THREADS = 1024;
+constexpr int64_t NORM_LONG_GRID = (((int64_t)1 << 32) - 1) / NORM_LONG_THREADS;
+constexpr int norm_most_dim(NormForm f) { return f == NORM_WAVE ? 2048 : f == NORM_GROUP ? 8192 : 32768; }
+
+struct NormLaunch {
+  NormForm form;
+  bool once;  // it moves more than PAST_CACHES bytes
+  int32_t n;
+  int64_t grid;
+  NormArgs args;
+};
+struct NormPlanHost {
+  std::vector<NormLaunch> launches;
+};
+
+// ---- mixture of experts ----------------------------------------------------------------------------------------------------
+
+constexpr int MOE_ROWS = 512;     // rows that are routed together; problems of more are cut
+constexpr int MOE_EXPERTS = 512, MOE_TOP = 32;
+constexpr int MOE_GROUP = 64;     // rows of an expert that a unit of work takes at most
+constexpr int ROUTE_EXPERTS = 8, ROUTE_ROWS = 4;  // of a unit of the router
+
+// Rows of an expert that go together: its number (or -1: the shared one), the first of their places, how many.
+struct MoeGroup {
+  int32_t expert, first, rows, pad;
+};
+
+// Up to MOE_ROWS rows of a problem, as the kernels see them (strides in bytes but for logits; `h` and `part` have a place for every pair of a row and
+// an expert that it chose, then one for every row).
+struct MoeDev {
+  const int32_t *n_rows;
+  const char *x, *router, *gate, *up, *down, *shared_gate, *shared_up, *shared_down;
+  const float *bias;
+  char *out;
+  int32_t *user_ids;
+  float *user_weights;
+  int64_t x_stride, out_stride, router_stride, up_expert, down_expert, up_row, down_row;
+  int32_t row0, rows, dim, experts, top_k, ffn, shared_ffn, act, scoring, normalize, dtype, router_f32;
+  float scale;
+  int32_t up_rows, down_rows;                        // rows of weights of a unit
+  int32_t up_tiles, shared_tiles, down_tiles;        // units of a group
+  int32_t most_groups;
+  // workspace
+  double *logits;         // [rows][experts]
+  int32_t *ids, *places;  // [rows][top_k]: chosen experts, and the pair's place
+  float *weights;         // [rows][top_k]
+  int32_t *row_of;        // [rows * top_k]: of a place
+  MoeGroup *groups;       // [most_groups]
+  int32_t *n_groups;
+  uint32_t *routed;       // counters: of units of the router per ROUTE_ROWS rows, of such blocks, of units of down per tile
+  uint32_t *blocks_routed, *summed;
+  char *h;                // [rows * top_k + rows], h_stride bytes apart
+  float *part;            // [rows * top_k + rows], part_stride floats apart
+  int64_t h_stride, part_stride;
+};
+
+struct MoePlanHost {
+  std::vector<MoeDev> parts;  // workspace pointers: offsets until the plan is on the device
+  std::vector<uint32_t> route_first, up_first, down_first;  // first workgroup of each part, and the number of all
+  size_t workspace = 0, counters = 0;  // bytes; the counters stand first
+};
+
+// ---- verification ----------------------------------------------------------------------------------------------------------
+
+// What a workgroup found in a part of a row of logits: sum of 2^((l - top) * c) for c = log2(e) / temperature, the largest and the first place where it
+// stands.  A sum that is not finite: there is a NaN or +infinity.
+struct VerifyStat {
+  double sum;
+  float top;
+  int32_t at;
+};
+struct VerifyDev {
+  const int32_t *first_row, *drafted;
+  const char *logits, *draft_logits;
+  const float *temperatures, *accept_random, *sample_random;
+  int32_t *tokens, *accepted;
+  int64_t logits_stride, draft_stride;  // bytes
+  int32_t dtype, sequences, rows, vocab;
+  float temperature;
+  int32_t pieces, chunks;  // a chunk is 2048 * pieces logits
+  VerifyStat *stats;       // [rows][2][chunks]
+  double *sums;            // [sequences][chunks]
+  uint32_t *arrived;       // [sequences]
+};
+struct VerifyPlanHost {
+  std::vector<VerifyDev> problems;
+  std::vector<uint32_t> stat_first, sum_first;
+  size_t workspace = 0, counters = 0;
+};
+
+// Checks and plans; no HIP call.  SK_OK or an error with `err` set.
+sk_status plan_norm(const sk_norm_problem *problems, int32_t n, int32_t workgroups, NormPlanHost &out, std::string &err);
+sk_status plan_moe(const sk_moe_problem *problems, int32_t n, int32_t workgroups, MoePlanHost &out, std::string &err);
+sk_status plan_verify(const sk_verify_problem *problems, int32_t n, int32_t workgroups, VerifyPlanHost &out, std::string &err);
+
+}  // namespace sk

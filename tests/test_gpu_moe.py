@@ -1,0 +1,161 @@
+"""Mixture-of-experts layers against 64 bits: numbers of rows, experts and choices, sizes that fill no tile, ties, rows counted on the device."""
+import pytest
+import torch
+
+import paper_1901_10008_amd as sk
+import layer_harness as H
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("rows", [1, 2, 3, 4, 5, 15, 16, 17, 31, 33, 63, 64, 65, 100, 200, 511, 512, 513, 1100])
+def test_rows(rows):
+    H.run_moe([H.Moe(rows=rows, dim=72, experts=6, top_k=2, ffn=40, seed=rows)], f"{rows} rows")
+
+
+@pytest.mark.parametrize("dim,ffn", [(8, 8), (8, 64), (16, 24), (64, 8), (56, 56), (64, 64), (72, 136), (128, 256), (520, 16), (1000, 680), (24, 1032)])
+@pytest.mark.parametrize("gated", [True, False])
+def test_sizes(dim, ffn, gated):
+    H.run_moe([H.Moe(rows=7, dim=dim, ffn=ffn, experts=5, top_k=3, gated=gated, shared=24, act="gelu", seed=dim + ffn),
+               H.Moe(rows=21, dim=dim, ffn=ffn, experts=2, top_k=2, gated=gated, dtype="f16", pad=8, seed=dim)], f"{dim} x {ffn}")
+
+
+@pytest.mark.parametrize("experts,top_k", [(1, 1), (2, 1), (2, 2), (3, 3), (63, 4), (64, 8), (65, 8), (129, 6), (512, 32), (33, 32)])
+@pytest.mark.parametrize("scoring,bias", [("softmax", False), ("softmax", True), ("sigmoid", False), ("sigmoid", True)])
+def test_experts(experts, top_k, scoring, bias):
+    H.run_moe([H.Moe(rows=9, dim=48, ffn=16, experts=experts, top_k=top_k, scoring=scoring, bias=bias, normalize=experts % 2, scale=2.5, seed=experts, router="f32" if bias else "own")],
+              f"{experts}/{top_k} {scoring}")
+
+
+@pytest.mark.parametrize("act", ["none", "sigmoid", "silu", "tanh", "gelu", "relu"])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_activations(act, dtype):
+    H.run_moe([H.Moe(rows=19, dim=64, ffn=48, act=act, dtype=dtype, gated=g, shared=40) for g in (True, False)], act)
+
+
+def test_tenants():
+    H.run_moe([H.Moe(rows=4, dim=256, ffn=128, experts=16, top_k=4, seed=1), H.Moe(rows=40, dim=64, ffn=32, experts=3, top_k=1, dtype="f16", shared=64, seed=2),
+               H.Moe(rows=600, dim=40, ffn=24, experts=7, top_k=2, gated=False, seed=3, used=530), H.Moe(rows=1, dim=8, ffn=8, experts=1, top_k=1, seed=4, outputs=False),
+               H.Moe(rows=70, dim=64, ffn=64, experts=4, top_k=2, used=0, seed=5)])
+    with sk.sk_moe_plan_create([]) as plan:
+        sk.sk_moe_launch(plan, H.stream_handle())
+        assert sk.sk_moe_plan_info(plan) == (0, 0)
+
+
+def test_equal_scores_go_to_the_lowest_number():
+    m = H.Moe(rows=20, dim=64, experts=10, top_k=4, seed=3)
+    m.router[5] = m.router[2]
+    m.router[7] = m.router[2]
+    m.router[9] = m.router[0]
+    m.x[3] = 0.0  # all scores are 0
+    m.x[4] = -0.0
+    H.run_moe([m])
+    assert m.ids[3].tolist() == [0, 1, 2, 3] and m.ids[4].tolist() == [0, 1, 2, 3]
+
+
+def test_scores_next_to_each_other():
+    """Scores that differ by 2^-30 of their size, in an order that sums in fp32 would not see."""
+    m = H.Moe(rows=8, dim=1024, experts=8, top_k=3, ffn=16, seed=4, router="f32")
+    base = m.router[0].clone()
+    m.x.fill_(1.0)
+    for e in range(8):
+        m.router[e] = base
+        m.router[e, 100 + e] += ((e * 5) % 8) * 2.0 ** -22
+    H.run_moe([m])
+    assert m.ids[0].tolist() != [0, 1, 2]
+
+
+def test_all_rows_to_one_expert():
+    bias = [0.0] * 9
+    bias[4], bias[7] = 100.0, 50.0
+    for rows in (64, 65, 150, 512, 700):
+        m = H.Moe(rows=rows, dim=64, experts=9, top_k=2, ffn=24, scoring="sigmoid", bias_value=bias, seed=rows)
+        H.run_moe([m])
+        assert (m.ids == torch.tensor([4, 7], device="cuda", dtype=torch.int32)).all()
+
+
+def test_a_row_keeps_its_nan_to_itself():
+    dirty, clean = H.Moe(rows=40, dim=64, experts=5, top_k=2, shared=16), H.Moe(rows=40, dim=64, experts=5, top_k=2, shared=16)
+    dirty.x[11, 5], dirty.x[30, 0] = float("nan"), float("inf")
+    for m in (dirty, clean):
+        with sk.sk_moe_plan_create([m.problem()]) as plan:
+            sk.sk_moe_launch(plan, H.stream_handle())
+            torch.cuda.synchronize()
+    assert dirty.ids[11].tolist() == [0, 1] and torch.isnan(dirty.out[11]).all() and not torch.isfinite(dirty.out[30]).any()
+    out, tol, ids, w = clean.reference()
+    keep = [r for r in range(40) if r not in (11, 30)]
+    assert torch.equal(dirty.ids[keep], clean.ids[keep]) and torch.equal(dirty.weights[keep], clean.weights[keep])
+    H.check(dirty.out[keep], out[keep], tol[keep])
+
+
+def test_one_plan_for_steps_of_any_number_of_rows():
+    ms = [H.Moe(rows=90, dim=64, experts=8, top_k=2, ffn=40, shared=16, used=90, seed=1), H.Moe(rows=600, dim=64, experts=30, top_k=4, ffn=40, used=600, seed=2, dtype="f16")]
+    with sk.sk_moe_plan_create([m.problem() for m in ms], keepalive=ms) as plan:
+        for step, used in enumerate([(90, 600), (1, 1), (0, 513), (-3, 0), (17, 512), (1000, 1000)]):
+            for m, n in zip(ms, used):
+                m.n_rows.fill_(n)
+                m.out_b.fill_(float("nan")), m.ids.fill_(-7), m.weights.fill_(float("nan"))
+            sk.sk_moe_launch(plan, H.stream_handle())
+            torch.cuda.synchronize()
+            for m, n in zip(ms, used):
+                H.check_moe(m, f"step {step}", max(0, min(n, m.rows)))
+
+
+def test_captured_and_replayed_between_other_launches():
+    m = H.Moe(rows=33, dim=64, experts=8, top_k=2, ffn=40, used=33, seed=1)
+    with sk.sk_moe_plan_create([m.problem()], keepalive=m) as plan:
+        sk.sk_moe_launch(plan, H.stream_handle())
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            sk.sk_moe_launch(plan, torch.cuda.current_stream().cuda_stream)
+        for step, used in enumerate((33, 2, 0, 20, 33)):
+            m.n_rows.fill_(used)
+            m.x.copy_(torch.randn_like(m.x))
+            m.out_b.fill_(float("nan")), m.ids.fill_(-7), m.weights.fill_(float("nan"))
+            graph.replay()
+            torch.cuda.synchronize()
+            H.check_moe(m, f"replay {step}", used)
+            again = m.out.clone()
+            sk.sk_moe_launch(plan, H.stream_handle())
+            torch.cuda.synchronize()
+            assert torch.equal(again[:used], m.out[:used])
+        del graph
+
+
+def test_busy_on_another_stream():
+    m = H.Moe(rows=8, dim=64, experts=8, top_k=2, ffn=40)
+    with sk.sk_moe_plan_create([m.problem()], keepalive=m) as plan:
+        one, two = torch.cuda.Stream(), torch.cuda.Stream()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(one):
+            torch.cuda._sleep(200_000_000)
+        sk.sk_moe_launch(plan, one.cuda_stream)
+        with pytest.raises(sk.SkError) as e:
+            sk.sk_moe_launch(plan, two.cuda_stream)
+        assert e.value.status == sk.SK_ERR_BUSY
+        one.synchronize()
+        H.check_moe(m)
+        sk.sk_moe_launch(plan, two.cuda_stream)
+        two.synchronize()
+        H.check_moe(m)
+
+
+def test_experts_beyond_4_gib():
+    """The last of five experts lies more than 4 GiB behind the first."""
+    m = H.Moe(rows=3, dim=64, experts=5, top_k=1, ffn=16, bias_value=[0, 0, 0, 0, 100.0], scoring="sigmoid")
+    stride = 1 << 29  # elements: 1 GiB
+    buffer = torch.empty(4 * stride + 3 * 16 * 64, dtype=torch.bfloat16, device="cuda")
+    parts = []
+    for k, (b, rows, cols) in enumerate(((m.gate_b, 16, 64), (m.up_b, 16, 64), (m.down_b, 64, 16))):
+        parts.append(buffer[k * 1024:])
+        for e in range(5):
+            parts[k][e * stride:e * stride + 1024] = b[e].reshape(-1)
+    p = m.problem()
+    p.gate, p.up, p.down = (x.data_ptr() for x in parts)
+    p.up_expert_stride = p.down_expert_stride = stride
+    with sk.sk_moe_plan_create([p], keepalive=(m, buffer)) as plan:
+        sk.sk_moe_launch(plan, H.stream_handle())
+        torch.cuda.synchronize()
+    H.check_moe(m)
+    assert (m.ids == 4).all()

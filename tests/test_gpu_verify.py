@@ -1,0 +1,171 @@
+"""Verification of drafted tokens against 64 bits: vocabularies, numbers of drafts, temperatures, what has no distribution, random numbers at their ends."""
+import math
+
+import pytest
+import torch
+
+import paper_1901_10008_amd as sk
+import layer_harness as H
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("vocab", [1, 2, 7, 8, 9, 300, 2047, 2048, 2049, 4100, 16385, 50257, 131073])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_vocabularies(vocab, dtype):
+    H.check_verify([H.Verify(dtype=dtype, vocab=vocab, counts=(3, 1, 6), seed=vocab), H.Verify(dtype=dtype, vocab=vocab, counts=(5, 2), draft="certain", spread=0.5, pad=3, seed=vocab + 1),
+                    H.Verify(dtype=dtype, vocab=vocab, counts=(1, 1, 1, 2), draft="none", temperature=0.7, seed=vocab + 2)], f"{vocab} {dtype}")
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_batches(seed):
+    g = torch.Generator().manual_seed(seed)
+    counts = [int(x) for x in torch.randint(0, 10, (20,), generator=g)]
+    temperatures = [float(x) for x in torch.rand((20,), generator=g) * 2]
+    temperatures[seed % 20] = 0.0
+    H.check_verify([H.Verify(dtype=("bf16", "f16", "f32")[seed % 3], vocab=1000 + 77 * seed, counts=counts, temperatures=temperatures, draft=("logits", "certain")[seed % 2], seed=seed,
+                             spread=1.0 + seed / 3, spare=2)], f"seed {seed}")
+
+
+def test_many_rows_in_larger_chunks():
+    """Enough rows that a chunk is 4096 or 8192 logits."""
+    for rows, vocab in ((300, 30011), (400, 60000)):
+        H.check_verify([H.Verify(vocab=vocab, counts=[4] * (rows // 4), seed=rows)], f"{rows} rows")
+
+
+@pytest.mark.parametrize("temperature", [0.0, -1.0, math.nan, 1e-30, 1e-3, 0.5, 10.0, 1e30, math.inf])
+def test_temperatures(temperature):
+    for draft in ("logits", "certain"):
+        H.check_verify([H.Verify(vocab=500, counts=(4, 1, 3), temperature=temperature, draft=draft, seed=5)], f"{temperature}")
+
+
+def test_same_model_accepts_all():
+    v = H.Verify(vocab=3000, counts=(5, 8, 2), seed=1)
+    v.draft_logits.copy_(v.logits)
+    v.accept_random.fill_(1 - 2.0 ** -24)
+    H.check_verify([v])
+    assert v.accepted.tolist() == [4, 7, 1]
+
+
+def test_masked_tokens_are_never_drawn():
+    v = H.Verify(vocab=5000, counts=(1,) * 40, draft="none", seed=2)
+    v.logits[:, :] = -math.inf
+    for s in range(40):
+        v.logits[s, 100 * s + 3] = float(s)
+        v.logits[s, 100 * s + 1037] = 0.0
+    v.sample_random[::3] = 0.0
+    v.sample_random[1::3] = 1 - 2.0 ** -24
+    H.check_verify([v])
+
+
+def test_rows_without_a_distribution():
+    v = H.Verify(vocab=2500, counts=(3, 3, 3, 3, 1, 4, 4, 3), seed=3)
+    v.accept_random.fill_(0.0)  # drafts are accepted where p > 0
+    v.logits[0] = -math.inf
+    v.logits[4, 2100] = math.nan
+    v.logits[8, 5] = math.inf
+    v.logits[12] = math.nan
+    v.draft_logits[13, 7] = math.nan  # counts as certain
+    v.draft_logits[17] = -math.inf
+    v.accept_random[17] = 1 - 2.0 ** -24
+    v.draft_logits[23, 0] = math.nan  # the last row's: not read
+    H.check_verify([v])
+    assert v.tokens[0] == -1 and v.accepted.tolist()[:5] == [0, 1, 2, 2, 0]
+    greedy = H.Verify(vocab=2500, counts=(2, 2, 1), temperature=0.0, seed=4)
+    greedy.logits[0, 9] = math.nan
+    greedy.logits[2] = -math.inf
+    greedy.logits[4, 2499] = math.inf
+    H.check_verify([greedy])
+    assert greedy.tokens.tolist() == [-1, -1, -1, -1, -1]
+
+
+def test_greedy_takes_the_first_of_the_largest():
+    v = H.Verify(vocab=9000, counts=(4, 1), temperature=0.0, seed=6)
+    v.logits.clamp_(max=4.0)
+    for i, first in enumerate((5, 2047, 2048, 8999, 4097)):
+        v.logits[i, :first] = torch.minimum(v.logits[i, :first], torch.tensor(3.5, device="cuda", dtype=v.logits.dtype))
+        v.logits[i, first] = 4.0
+    v.logits[3] = torch.where(v.logits[3] == 0, v.logits[3], -v.logits[3].abs())
+    v.logits[3, 17], v.logits[3, 4] = 0.0, -0.0
+    v.drafted[:3] = H.int32(5, 2047, 2049)
+    H.check_verify([v])
+    assert v.accepted.tolist() == [2, 0] and v.tokens[0] == 5 and v.tokens[2] == 2048
+
+
+def test_random_numbers_at_and_beyond_their_ends():
+    v = H.Verify(vocab=700, counts=(3,) * 8, seed=7)
+    ends = torch.tensor([0.0, 1 - 2.0 ** -24, 1.0, -0.5, math.nan, math.inf, -math.inf, 0.5], device="cuda")
+    v.sample_random.copy_(ends)
+    v.accept_random.copy_(ends.repeat(3))
+    H.check_verify([v])
+
+
+def test_drafted_numbers_outside_the_vocabulary():
+    v = H.Verify(vocab=64, counts=(4, 4, 4), seed=8)
+    v.drafted[0], v.drafted[5], v.drafted[8] = -1, 64, 2 ** 31 - 1
+    v.accept_random.fill_(0.0)
+    H.check_verify([v])
+    assert v.accepted.tolist() == [0, 1, 0]
+
+
+def test_rows_of_no_sequence_and_numbers_beyond_the_rows():
+    v = H.Verify(vocab=100, counts=(2, 0, 3), spare=4, seed=9)
+    H.check_verify([v])
+    # sequences whose rows would lie outside are cut; none of it is written elsewhere
+    v.first_row.copy_(H.int32(-4, 2, 2, 1000))
+    v.firsts, v.counts = [0, 2, 2, 9], [2, 0, 7]
+    H.check_verify([v])
+
+
+def test_one_token_holds_nearly_everything():
+    """p of the drafted token is 1 - 2^-30 and it is rejected: the rest is what the sum without it says, not a difference of sums."""
+    v = H.Verify(dtype="f32", vocab=4000, counts=(2, 2), draft="certain", seed=10)
+    v.logits.fill_(-30.0 * math.log(2.0) - math.log(4000.0))
+    v.logits[:, 1234] = 0.0
+    v.drafted.fill_(1234)
+    v.accept_random.fill_(1 - 2.0 ** -24)
+    H.check_verify([v])  # (accepted: 1 - 2^-24 < 1 - 2^-30)
+    assert v.accepted.tolist() == [1, 1]
+    v.logits[:, 1234] = -2.0 ** -20
+    v.logits[:, 7] = 12.0
+    H.check_verify([v])
+    assert v.accepted.tolist() == [0, 0] and v.tokens[0] == 7
+
+
+def test_equal_distributions_where_only_the_token_differs():
+    """A certain draft that is rejected is never drawn again."""
+    v = H.Verify(dtype="f32", vocab=16, counts=(2,) * 64, draft="certain", spread=0.0, seed=11)
+    v.accept_random.fill_(0.5)  # p = 1/16
+    H.check_verify([v])
+    assert (v.tokens[::2] != v.drafted[::2]).all() and (v.accepted == 0).all()
+
+
+def test_captured_and_replayed_between_other_launches():
+    v = H.Verify(vocab=3000, counts=(3, 2, 5), temperatures=[1.0, 0.0, 0.8], seed=12)
+    with sk.sk_verify_plan_create([v.problem()], keepalive=v) as plan:
+        sk.sk_verify_launch(plan, H.stream_handle())
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            sk.sk_verify_launch(plan, torch.cuda.current_stream().cuda_stream)
+        for step in range(5):
+            v.logits.copy_(torch.randn_like(v.logits) * 2)
+            v.accept_random.uniform_()
+            v.sample_random.uniform_()
+            want = v.reference()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert (v.tokens.tolist(), v.accepted.tolist()) == want, step
+            v.tokens.fill_(-9)
+            sk.sk_verify_launch(plan, H.stream_handle())
+            torch.cuda.synchronize()
+            assert (v.tokens.tolist(), v.accepted.tolist()) == want, step
+        del graph
+
+
+def test_tenants():
+    H.check_verify([H.Verify(vocab=5000, counts=(3, 3), seed=1), H.Verify(dtype="f32", vocab=30, counts=(1,) * 70, draft="none", seed=2), H.Verify(dtype="f16", vocab=9, counts=(0, 0), spare=1, seed=3),
+                    H.Verify(dtype="f16", vocab=70001, counts=(7,), draft="certain", pad=1, seed=4)])
+    with sk.sk_verify_plan_create([]) as plan:
+        sk.sk_verify_launch(plan, H.stream_handle())
+        assert sk.sk_verify_plan_info(plan) == (0, 0)
