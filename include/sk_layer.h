@@ -98,11 +98,12 @@ sk_status sk_norm_launch(sk_norm_plan *plan, void *hip_stream);
  *     the top_k experts with the largest s_e + router_bias_e, in that order; equal ones by their number; NaN below all others
  *     w_e = scale * s_e, with normalize = 1 divided by the sum of the chosen s_e
  *     h_e = act(gate_e . x) * (up_e . x),               without gate: act(up_e . x)
- *     out = sum over the chosen, in their order, w_e * (down_e . h_e), and the same of the shared expert, which every row passes, with w = 1
+ *     out = sum over the chosen, w_e * (down_e . h_e), and the same of the shared expert, which every row passes, with w = 1
  * Scores are computed in 64 bits, so that the choice between experts whose scores are next to each other does not depend on the order of sums.
  * Products of the experts are summed in fp32, h is rounded to dtype for the matrix units, outputs are summed in fp32 and rounded
  * once.  An h beyond the type's range is infinite.  Each row's result depends on that row and the weights alone, up to the order of sums.
- * The weights are read once for up to 64 rows of an expert; made for the rows of decoder steps, it takes any number.
+ * The weights are read once for up to 32 rows of an expert; made for the rows of decoder steps, it takes any number.  A row's sum goes over its experts
+ * in the order of their numbers, the shared one last.
  */
 typedef enum { SK_MOE_SOFTMAX = 0, SK_MOE_SIGMOID = 1 } sk_moe_scoring;
 
@@ -135,7 +136,8 @@ typedef struct sk_moe_plan sk_moe_plan; /* opaque, owned by the library */
 
 /*
  * Errors as above; also SK_ERR_UNSUPPORTED: SK_F32, dim or widths that are no multiples of 8, x, weights, router and out or their strides
- * that are no multiples of 16 bytes, more than 512 experts or 32 chosen; SK_ERR_ALLOC also where the workspace does not fit the device.
+ * that are no multiples of 16 bytes, more than 512 experts or 32 chosen, dim or a stride of x from 2^21 on, widths beyond 2^24 or strides of
+ * rows of weights from 2^26 on; SK_ERR_ALLOC also where the workspace does not fit the device.
  */
 sk_status sk_moe_plan_create(const sk_moe_problem *problems, int32_t n, const sk_layer_params *params, sk_moe_plan **out);
 /* Waits for the plan's launches and frees it; null is accepted. */

@@ -95,12 +95,12 @@ inline hipError_t wait_for(const PlanOnDevice *plan, bool all) {
 
 // A launch whose completion is an event's signal (null: none).
 template <class K, class A>
-sk_status launch(K kernel, int64_t grid, hipStream_t stream, hipEvent_t behind, const A &args, int threads = CACHE_THREADS) {
+sk_status launch(K kernel, int64_t grid, hipStream_t stream, hipEvent_t behind, const A &args, int threads = CACHE_THREADS, size_t lds = 0) {
   const dim3 g((unsigned)grid), b((unsigned)threads);
   if (behind)
-    hipExtLaunchKernelGGL(kernel, g, b, 0, stream, nullptr, behind, 0, args);
+    hipExtLaunchKernelGGL(kernel, g, b, (unsigned)lds, stream, nullptr, behind, 0, args);
   else
-    hipLaunchKernelGGL(kernel, g, b, 0, stream, args);
+    hipLaunchKernelGGL(kernel, g, b, lds, stream, args);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? SK_OK : hip_error("kernel launch", e);
 }

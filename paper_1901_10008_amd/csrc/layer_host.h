@@ -44,7 +44,7 @@ sk_status create_plan(const sk_layer_params *params, Plan **out, F check, G uplo
     try {
       plan->device = device;
       std::string err;
-      sk_status st = check(*plan, prm.workgroups ? prm.workgroups : cus, err);
+      sk_status st = check(*plan, cus, prm.workgroups, err);
       if (st != SK_OK) st = set_last_error(st, err);
       if (st == SK_OK && !prm.host_only) {
         st = upload(*plan);

@@ -54,16 +54,22 @@ struct NormPlanHost {
 
 constexpr int MOE_ROWS = 512;     // rows that are routed together; problems of more are cut
 constexpr int MOE_EXPERTS = 512, MOE_TOP = 32;
-constexpr int MOE_GROUP = 64;     // rows of an expert that a unit of work takes at most
+constexpr int MOE_GROUP = 32;     // rows of an expert that a unit of work takes at most
+constexpr int MOE_UP_RESIDENT = 3, MOE_DOWN_RESIDENT = 3;  // workgroups of the products that a compute unit holds (its registers)
 constexpr int ROUTE_EXPERTS = 8, ROUTE_ROWS = 4;  // of a unit of the router
 
 // Rows of an expert that go together: its number (or -1: the shared one), the first of their places, how many.
 struct MoeGroup {
   int32_t expert, first, rows, pad;
 };
+// What the router found: groups, rows; all work of the first products, and of a tile of the second ones; the longest of a group in such a tile.
+struct MoeCount {
+  int32_t groups, rows;
+  int64_t first_work, second_work, longest;
+};
 
-// Up to MOE_ROWS rows of a problem, as the kernels see them (strides in bytes but for logits; `h` and `part` have a place for every pair of a row and
-// an expert that it chose, then one for every row).
+// Up to MOE_ROWS rows of a problem, as the kernels see them (strides in bytes but for logits; `h` has a place for every pair of a row and an expert
+// that it chose, then one for every row).
 struct MoeDev {
   const int32_t *n_rows;
   const char *x, *router, *gate, *up, *down, *shared_gate, *shared_up, *shared_down;
@@ -74,27 +80,32 @@ struct MoeDev {
   int64_t x_stride, out_stride, router_stride, up_expert, down_expert, up_row, down_row;
   int32_t row0, rows, dim, experts, top_k, ffn, shared_ffn, act, scoring, normalize, dtype, router_f32;
   float scale;
-  int32_t up_rows, down_rows;                        // rows of weights of a unit
-  int32_t up_tiles, shared_tiles, down_tiles;        // units of a group
-  int32_t most_groups;
+  int32_t up_tiles, shared_tiles, down_tiles;        // tiles of 16 rows of weights
+  int32_t most_groups;                               // with those of the shared expert
   // workspace
   double *logits;         // [rows][experts]
-  int32_t *ids, *places;  // [rows][top_k]: chosen experts, and the pair's place
+  int32_t *ids;           // [rows][top_k]: chosen experts
   float *weights;         // [rows][top_k]
   int32_t *row_of;        // [rows * top_k]: of a place
-  MoeGroup *groups;       // [most_groups]
-  int32_t *n_groups;
-  uint32_t *routed;       // counters: of units of the router per ROUTE_ROWS rows, of such blocks, of units of down per tile
+  float *weight_of;       // [rows * top_k]: of a place
+  MoeGroup *groups;       // [most_groups]; those of the shared expert last
+  int64_t *first_begin, *second_begin;  // [most_groups]: where a group's work begins, among the first products and within a tile of the second ones
+  MoeCount *count;
+  uint32_t *routed;       // counters: of units of the router per ROUTE_ROWS rows, of such blocks, of slices per tile of the output
   uint32_t *blocks_routed, *summed;
   char *h;                // [rows * top_k + rows], h_stride bytes apart
-  float *part;            // [rows * top_k + rows], part_stride floats apart
-  int64_t h_stride, part_stride;
+  int64_t h_stride;
 };
 
 struct MoePlanHost {
-  std::vector<MoeDev> parts;  // workspace pointers: offsets until the plan is on the device
-  std::vector<uint32_t> route_first, up_first, down_first;  // first workgroup of each part, and the number of all
-  size_t workspace = 0, counters = 0;  // bytes; the counters stand first
+  std::vector<MoeDev> parts;          // workspace pointers: offsets until the plan is on the device
+  std::vector<uint32_t> route_first;  // first workgroup of the router of each part, and the number of all
+  MoeCount *counts = nullptr;         // of all parts (an offset)
+  float *slices = nullptr;            // two of each workgroup (an offset)
+  int64_t slice_floats = 0;
+  int64_t up_workgroups = 0, down_workgroups = 0;  // of the products
+  size_t lds = 0;                     // bytes that a workgroup of the second products keeps its sums in
+  size_t workspace = 0, counters = 0; // bytes; the counters stand first
 };
 
 // ---- verification ----------------------------------------------------------------------------------------------------------
@@ -125,9 +136,9 @@ struct VerifyPlanHost {
   size_t workspace = 0, counters = 0;
 };
 
-// Checks and plans; no HIP call.  SK_OK or an error with `err` set.
-sk_status plan_norm(const sk_norm_problem *problems, int32_t n, int32_t workgroups, NormPlanHost &out, std::string &err);
-sk_status plan_moe(const sk_moe_problem *problems, int32_t n, int32_t workgroups, MoePlanHost &out, std::string &err);
-sk_status plan_verify(const sk_verify_problem *problems, int32_t n, int32_t workgroups, VerifyPlanHost &out, std::string &err);
+// Checks and plans, for a device of that many compute units or for that many workgroups at a time (0: what its compute units hold); no HIP call.  SK_OK or an error with `err` set.
+sk_status plan_norm(const sk_norm_problem *problems, int32_t n, NormPlanHost &out, std::string &err);
+sk_status plan_moe(const sk_moe_problem *problems, int32_t n, int32_t compute_units, int32_t workgroups, MoePlanHost &out, std::string &err);
+sk_status plan_verify(const sk_verify_problem *problems, int32_t n, VerifyPlanHost &out, std::string &err);
 
 }  // namespace sk

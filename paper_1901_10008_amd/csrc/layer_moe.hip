@@ -1,18 +1,37 @@
 // A mixture-of-experts layer: the kernels and their entry points.
 #include "layer_host.h"
 #include "layer_math.hip.h"
+#include "layer_units.h"
 
 namespace sk {
 
 struct MoeArgs {
   const MoeDev *parts;
-  const uint32_t *first;  // first workgroup of each part
+  const uint32_t *first;  // of the router: first workgroup of each part
+  MoeCount *counts;       // of each part: what the router found
+  float *slices;          // partial sums of the second products, see down_share
+  int64_t slice_floats;
   int32_t n;
 };
 
 __device__ __forceinline__ int32_t rows_of(const SK_CONSTANT MoeDev &P) {
   const int32_t n = P.n_rows ? load_i32(P.n_rows) : 0x7fffffff;
   return __builtin_amdgcn_readfirstlane(min(max(n - P.row0, 0), P.rows));
+}
+
+// What a workgroup needs to find its part.
+struct Place {
+  const SK_CONSTANT MoeDev *part;
+  int32_t unit;
+};
+__device__ __forceinline__ Place place_of(const MoeArgs &a) {
+  int32_t part = 0;
+  uint32_t first = 0;
+  if (a.n > 1) {
+    part = __builtin_amdgcn_readfirstlane(last_not_above(a.first, a.n, (int64_t)blockIdx.x, threadIdx.x & 63));
+    first = ((const SK_CONSTANT uint32_t *)(uintptr_t)a.first)[part];
+  }
+  return Place{(const SK_CONSTANT MoeDev *)(uintptr_t)(a.parts + part), (int32_t)(blockIdx.x - first)};
 }
 
 // ---------------------------------------------------------------------------
@@ -22,13 +41,14 @@ __device__ __forceinline__ int32_t rows_of(const SK_CONSTANT MoeDev &P) {
 // so, are their sums: which of two experts is chosen does not depend on the order of a sum.  Vector instructions of 64 bits have the rate of
 // those of 32 here, and E * D multiplications a row are little beside the experts' products.
 template <int DT, bool F32>
-__device__ __forceinline__ void route_scores(const SK_CONSTANT MoeDev &P, int32_t rows, int32_t block, int32_t e0, int lane) {
+__device__ __forceinline__ void route_scores(const SK_CONSTANT MoeDev &P, int32_t block, int32_t e0, int lane) {
   double sum[2][ROUTE_ROWS] = {};
   const int32_t last = P.experts - 1;
   const char *w[2] = {P.router + (int64_t)min(e0, last) * P.router_stride, P.router + (int64_t)min(e0 + 1, last) * P.router_stride};
   const char *x[ROUTE_ROWS];
 #pragma unroll
-  for (int r = 0; r < ROUTE_ROWS; ++r) x[r] = P.x + (int64_t)min(block * ROUTE_ROWS + r, rows - 1) * P.x_stride;
+  for (int r = 0; r < ROUTE_ROWS; ++r) x[r] = P.x + (int64_t)min(block * ROUTE_ROWS + r, P.rows - 1) * P.x_stride;  // (that there is a row is known later)
+#pragma unroll 2
   for (int32_t k = lane * 8; k < P.dim; k += 512) {
     float a[2][8], b[ROUTE_ROWS][8];
 #pragma unroll
@@ -52,7 +72,7 @@ __device__ __forceinline__ void route_scores(const SK_CONSTANT MoeDev &P, int32_
     for (int r = 0; r < ROUTE_ROWS; ++r) {
       const double s = wave_sum(sum[i][r]);
       const int32_t row = block * ROUTE_ROWS + r;
-      if (lane == 0 && e0 + i < P.experts && row < rows) put(P.logits + (int64_t)row * P.experts + e0 + i, s);
+      if (lane == 0 && e0 + i < P.experts && row < P.rows) put(P.logits + (int64_t)row * P.experts + e0 + i, s);
     }
 }
 
@@ -61,71 +81,73 @@ __device__ __forceinline__ uint64_t ordered(double v) {
   const uint64_t b = __builtin_bit_cast(uint64_t, v + 0.0);  // (-0 becomes 0)
   return v != v ? 1u : (b >> 63 ? ~b : b | (uint64_t)1 << 63);
 }
-__device__ __forceinline__ uint64_t wave_max(uint64_t v) {
-  auto larger = [](uint64_t a, uint64_t b) { return a > b ? a : b; };
-  auto as_d = [](uint64_t x) { return __builtin_bit_cast(double, x); };
-  auto as_u = [](double x) { return __builtin_bit_cast(uint64_t, x); };
-  v = larger(v, as_u(other_lane<0xb1>(as_d(v))));
-  v = larger(v, as_u(other_lane<0x4e>(as_d(v))));
-  v = larger(v, as_u(other_lane<0x141>(as_d(v))));
-  v = larger(v, as_u(other_lane<0x140>(as_d(v))));
-  double a, b;
-  across<16>(as_d(v), a, b);
-  v = larger(as_u(a), as_u(b));
-  across<32>(as_d(v), a, b);
-  return larger(as_u(a), as_u(b));
+// The largest of a wave's numbers, the same in all lanes.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t larger(uint32_t v) {
+  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int32_t)v, CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  v = larger<0x111, 0xf>(v);  // row_shr:1, 2, 4, 8
+  v = larger<0x112, 0xf>(v);
+  v = larger<0x114, 0xf>(v);
+  v = larger<0x118, 0xf>(v);
+  v = larger<0x142, 0xa>(v);  // row_bcast:15, 31
+  v = larger<0x143, 0xc>(v);
+  return (uint32_t)lane_of((int32_t)v, 63);
 }
 
-// The top_k experts of a row, by one wave: the largest score is taken out top_k times.
-__device__ __forceinline__ void choose(const SK_CONSTANT MoeDev &P, int32_t row, int lane) {
-  constexpr int N = MOE_EXPERTS / 64;
-  const int32_t most = (P.experts + 63) / 64;
+// The top_k experts of a row, by one wave: the largest score is taken out top_k times (upper halves first, lower halves among those that are
+// equal in them).  N * 64 experts at most.
+template <int N>
+__device__ __forceinline__ void choose(const SK_CONSTANT MoeDev &P, int32_t row, int lane, int32_t *ids, float *weights) {
   double score[N];
-  uint64_t key[N];
+  uint32_t hi[N], lo[N];
+  auto set = [&](int i, uint64_t key) { hi[i] = (uint32_t)(key >> 32), lo[i] = (uint32_t)key; };
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const int32_t e = i * 64 + lane;
-    score[i] = i < most && e < P.experts ? got(P.logits + (int64_t)row * P.experts + e) : -__builtin_inf();
+    score[i] = e < P.experts ? got(P.logits + (int64_t)row * P.experts + e) : -__builtin_inf();
   }
 #pragma unroll
-  for (int i = 0; i < N; ++i) key[i] = i * 64 + lane < P.experts ? ordered(score[i]) : 0u;
+  for (int i = 0; i < N; ++i) set(i, i * 64 + lane < P.experts ? ordered(score[i]) : 0u);
   if (P.scoring == SK_MOE_SOFTMAX) {
     double top = -__builtin_inf(), sum = 0.0;
 #pragma unroll
     for (int i = 0; i < N; ++i) top = fmax(top, score[i]);
     top = wave_max(top);
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (i < most) {
-        score[i] = exp(score[i] - top);
-        sum += i * 64 + lane < P.experts ? score[i] : 0.0;
-      }
+    for (int i = 0; i < N; ++i) {
+      score[i] = exp(score[i] - top);
+      sum += i * 64 + lane < P.experts ? score[i] : 0.0;
+    }
     sum = wave_sum(sum);
 #pragma unroll
     for (int i = 0; i < N; ++i) score[i] /= sum;
   } else {
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (i < most) score[i] = 1.0 / (1.0 + exp(-score[i]));
+    for (int i = 0; i < N; ++i) score[i] = 1.0 / (1.0 + exp(-score[i]));
   }
   if (P.bias || P.scoring != SK_MOE_SOFTMAX) {  // (a softmax keeps the order of its logits, which tell apart what it rounds to the same)
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int32_t e = i * 64 + lane;
-      if (e < P.experts) key[i] = ordered(score[i] + (P.bias ? (double)load_f(P.bias + e) : 0.0));
+      if (e < P.experts) set(i, ordered(score[i] + (P.bias ? (double)load_f(P.bias + e) : 0.0)));
     }
   }
   int32_t mine = 0;  // lane j: the j-th choice
   double mine_score = 0.0, sum = 0.0;
   for (int32_t j = 0; j < P.top_k; ++j) {
-    uint64_t best = 0;
+    uint32_t best = 0, second = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) best = key[i] > best ? key[i] : best;
+    for (int i = 0; i < N; ++i) best = max(best, hi[i]);
     best = wave_max(best);
+#pragma unroll
+    for (int i = 0; i < N; ++i) second = hi[i] == best ? max(second, lo[i]) : second;
+    second = wave_max(second);
     bool found = false;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const uint64_t hit = __ballot(key[i] == best);
+      const uint64_t hit = __ballot(hi[i] == best && lo[i] == second);
       if (found || !hit) continue;
       found = true;
       const int l = (int)__builtin_ctzll(hit);
@@ -133,14 +155,14 @@ __device__ __forceinline__ void choose(const SK_CONSTANT MoeDev &P, int32_t row,
       const double s = __builtin_bit_cast(double, (uint64_t)(uint32_t)lane_of((int32_t)(b >> 32), l) << 32 | (uint32_t)lane_of((int32_t)b, l));
       sum += s;
       if (lane == j) mine = i * 64 + l, mine_score = s;
-      if (lane == l) key[i] = 0;
+      if (lane == l) hi[i] = lo[i] = 0;
     }
   }
   if (lane < P.top_k) {
     const int64_t at = (int64_t)row * P.top_k + lane;
     const float weight = (float)((P.normalize ? mine_score / sum : mine_score) * (double)P.scale);
-    put(P.ids + at, mine);
-    put(P.weights + at, weight);
+    if (ids) ids[lane] = mine, weights[lane] = weight;
+    else put(P.ids + at, mine), put(P.weights + at, weight);
     if (P.user_ids) P.user_ids[at] = mine;
     if (P.user_weights) P.user_weights[at] = weight;
   }
@@ -149,16 +171,40 @@ __device__ __forceinline__ void choose(const SK_CONSTANT MoeDev &P, int32_t row,
 // Which rows go to which expert: every chosen pair gets a place, those of one expert side by side in the order of their rows; and the list of
 // groups of up to MOE_GROUP places of an expert.  A bit for every row and expert stands in LDS, so that nothing depends on the order
 // of the atomics that set them.
+constexpr int SORT_PAIRS = 2048;  // that LDS keeps
 struct Sorting {
   uint32_t bits[MOE_EXPERTS][MOE_ROWS / 32];
   int32_t count[MOE_EXPERTS], first[MOE_EXPERTS];
+  int32_t ids[SORT_PAIRS];
+  float weights[SORT_PAIRS];
 };
-__device__ __forceinline__ void sort_pairs(const SK_CONSTANT MoeDev &P, int32_t rows, Sorting &s, int tid) {
+// Counts of an expert's groups, and sums of them, in one number of 64 bits: rows in the lowest 16 bits, then groups of modes 8, 16 and 32, 16 bits each.  (A
+// part has at most 512 experts and 2^14 pairs, so none reaches 2^15.)
+__device__ __forceinline__ int64_t groups_of(int32_t n) {
+  const int32_t g = (n + MOE_GROUP - 1) / MOE_GROUP, last = moe::mode_of(n - (g - 1) * MOE_GROUP);
+  return n ? (int64_t)n + ((int64_t)(g - 1) << 48) + ((int64_t)1 << (last == 8 ? 16 : last == 16 ? 32 : 48)) : 0;
+}
+__device__ __forceinline__ int32_t rows_in(int64_t counts) { return (int32_t)(counts & 0xffff); }
+__device__ __forceinline__ int32_t of_mode(int64_t counts, int mode) { return (int32_t)(counts >> (mode == 8 ? 16 : mode == 16 ? 32 : 48)) & 0xffff; }
+__device__ __forceinline__ int32_t groups_in(int64_t counts) { return of_mode(counts, 8) + of_mode(counts, 16) + of_mode(counts, 32); }
+// (costs of modes 8, 16 and 32)
+struct Costs {
+  int64_t of[3];
+  __device__ __forceinline__ int64_t sum(int64_t counts) const { return of_mode(counts, 8) * of[0] + of_mode(counts, 16) * of[1] + of_mode(counts, 32) * of[2]; }
+};
+__device__ __forceinline__ Costs costs_of(int32_t k_len, int32_t matrices) {
+  return Costs{{moe::cost(k_len, matrices, 8), moe::cost(k_len, matrices, 16), moe::cost(k_len, matrices, 32)}};
+}
+
+// here: ids and weights are in LDS already.
+__device__ __forceinline__ void sort_pairs(const SK_CONSTANT MoeDev &P, int32_t rows, Sorting &s, bool here, int tid) {
   const int32_t pairs = rows * P.top_k, words = (rows + 31) / 32;
-  for (int32_t i = tid; i < P.experts * (MOE_ROWS / 32); i += CACHE_THREADS) (&s.bits[0][0])[i] = 0;
+  for (int32_t i = tid; i < P.experts * (MOE_ROWS / 32); i += CACHE_THREADS)
+    if (i % (MOE_ROWS / 32) < words) s.bits[i / (MOE_ROWS / 32)][i % (MOE_ROWS / 32)] = 0;
   __syncthreads();
   for (int32_t i = tid; i < pairs; i += CACHE_THREADS) {
-    const int32_t row = i / P.top_k, e = got(P.ids + i);
+    const int32_t row = i / P.top_k, e = here ? s.ids[i] : got(P.ids + i);
+    if (!here && i < SORT_PAIRS) s.ids[i] = e, s.weights[i] = got(P.weights + i);
     atomicOr(&s.bits[e][row / 32], 1u << (row % 32));
   }
   __syncthreads();
@@ -169,29 +215,44 @@ __device__ __forceinline__ void sort_pairs(const SK_CONSTANT MoeDev &P, int32_t 
   }
   __syncthreads();
   if (tid < 64) {
-    int32_t places = 0, groups = 0;
+    const Costs up = costs_of(P.dim, P.gate ? 2 : 1), down = costs_of(P.ffn, 1);
+    int64_t all = 0;
     for (int32_t e0 = 0; e0 < P.experts; e0 += 64) {
       const int32_t e = e0 + tid, n = e < P.experts ? s.count[e] : 0, g = (n + MOE_GROUP - 1) / MOE_GROUP;
-      const int32_t to_n = wave_scan(n), to_g = wave_scan(g);
-      if (e < P.experts) s.first[e] = places + to_n - n;
-      for (int32_t i = 0; i < g; ++i) {
-        MoeGroup *at = P.groups + groups + to_g - g + i;
-        put(&at->expert, e);
-        put(&at->first, places + to_n - n + i * MOE_GROUP);
-        put(&at->rows, min(MOE_GROUP, n - i * MOE_GROUP));
+      const int64_t mine = groups_of(n), upto = wave_scan(mine), before = all + upto - mine;
+      const int32_t place = rows_in(before), at = groups_in(before);
+      if (e < P.experts) s.first[e] = place;
+      for (int32_t i = 0; i < g; ++i) {  // (all but the last are full)
+        P.groups[at + i] = MoeGroup{e, place + i * MOE_GROUP, min(MOE_GROUP, n - i * MOE_GROUP), 0};
+        P.first_begin[at + i] = (up.sum(before) + i * up.of[2]) * P.up_tiles;
+        P.second_begin[at + i] = down.sum(before) + i * down.of[2];
       }
-      places += lane_of(to_n, 63);
-      groups += lane_of(to_g, 63);
+      all += lane_of(upto, 63);
     }
-    if (tid == 0) put(P.n_groups, groups);
+    MoeCount c{groups_in(all), rows, up.sum(all) * P.up_tiles, down.sum(all), of_mode(all, 32) ? down.of[2] : of_mode(all, 16) ? down.of[1] : all ? down.of[0] : 0};
+    if (P.shared_ffn) {  // (at most 16 groups)
+      const int32_t g = (rows + MOE_GROUP - 1) / MOE_GROUP, n = min(MOE_GROUP, rows - tid * MOE_GROUP);
+      const Costs shared = costs_of(P.shared_ffn, 1);
+      if (tid < g) {
+        P.groups[c.groups + tid] = MoeGroup{-1, tid * MOE_GROUP, n, 0};
+        P.first_begin[c.groups + tid] = c.first_work + tid * up.of[2] * P.shared_tiles;
+        P.second_begin[c.groups + tid] = c.second_work + tid * shared.of[2];
+      }
+      const int64_t counts = groups_of(rows);
+      c.groups += g;
+      c.first_work += up.sum(counts) * P.shared_tiles;
+      c.second_work += shared.sum(counts);
+      c.longest = max(c.longest, of_mode(counts, 32) ? shared.of[2] : of_mode(counts, 16) ? shared.of[1] : g ? shared.of[0] : 0);
+    }
+    if (tid == 0) *P.count = c;
   }
   __syncthreads();
   for (int32_t i = tid; i < pairs; i += CACHE_THREADS) {
-    const int32_t row = i / P.top_k, e = got(P.ids + i);
+    const int32_t row = i / P.top_k, e = i < SORT_PAIRS ? s.ids[i] : got(P.ids + i);
     int32_t at = s.first[e] + __popc(s.bits[e][row / 32] & ((1u << (row % 32)) - 1));
     for (int32_t w = 0; w < row / 32; ++w) at += __popc(s.bits[e][w]);
-    put(P.places + i, at);
-    put(P.row_of + at, row);
+    P.row_of[at] = row;
+    P.weight_of[at] = i < SORT_PAIRS ? s.weights[i] : got(P.weights + i);
   }
 }
 
@@ -199,30 +260,38 @@ __global__ void __launch_bounds__(CACHE_THREADS) sk_moe_route(MoeArgs a) {
   __shared__ Sorting sorting;
   __shared__ uint32_t flag;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int32_t part = __builtin_amdgcn_readfirstlane(last_not_above(a.first, a.n, (int64_t)blockIdx.x, lane));
-  const SK_CONSTANT MoeDev &P = *(const SK_CONSTANT MoeDev *)(uintptr_t)(a.parts + part);
-  const int32_t unit = (int32_t)(blockIdx.x - ((const SK_CONSTANT uint32_t *)(uintptr_t)a.first)[part]);
+  const Place place = place_of(a);
+  const SK_CONSTANT MoeDev &P = *place.part;
+  const int32_t unit = place.unit;
   const int32_t by_experts = (P.experts + ROUTE_EXPERTS - 1) / ROUTE_EXPERTS, blocks = (P.rows + ROUTE_ROWS - 1) / ROUTE_ROWS;
   const int32_t block = unit / by_experts, e0 = unit % by_experts * ROUTE_EXPERTS + 2 * wave, rows = rows_of(P);
-  if (block * ROUTE_ROWS < rows && e0 < P.experts) {
-    if (P.dtype == SK_BF16) P.router_f32 ? route_scores<SK_BF16, true>(P, rows, block, e0, lane) : route_scores<SK_BF16, false>(P, rows, block, e0, lane);
-    else P.router_f32 ? route_scores<SK_F16, true>(P, rows, block, e0, lane) : route_scores<SK_F16, false>(P, rows, block, e0, lane);
+  if (e0 < P.experts) {
+    if (P.dtype == SK_BF16) P.router_f32 ? route_scores<SK_BF16, true>(P, block, e0, lane) : route_scores<SK_BF16, false>(P, block, e0, lane);
+    else P.router_f32 ? route_scores<SK_F16, true>(P, block, e0, lane) : route_scores<SK_F16, false>(P, block, e0, lane);
   }
   if (!last_to_arrive(P.routed + block, by_experts, &flag)) return;
   const int32_t row = block * ROUTE_ROWS + wave;
-  if (row < rows) choose(P, row, lane);
-  if (!last_to_arrive(P.blocks_routed, blocks, &flag)) return;
-  sort_pairs(P, rows, sorting, tid);
+  int32_t *ids = blocks == 1 ? sorting.ids + row * P.top_k : nullptr;  // (then there are at most ROUTE_ROWS rows, and no other workgroup has any)
+  float *weights = sorting.weights + row * P.top_k;
+  if (row < rows) {
+    if (P.experts <= 64) choose<1>(P, row, lane, ids, weights);
+    else if (P.experts <= 128) choose<2>(P, row, lane, ids, weights);
+    else choose<MOE_EXPERTS / 64>(P, row, lane, ids, weights);
+  }
+  if (blocks > 1 && !last_to_arrive(P.blocks_routed, blocks, &flag)) return;
+  sort_pairs(P, rows, sorting, blocks == 1, tid);
 }
 
 // ---------------------------------------------------------------------------
 // the experts' products
 // ---------------------------------------------------------------------------
-// Rows of weights times up to 16 * NB rows of activations, both with their reduction in blocks of 64 elements (128 bytes a row): the four waves of a
-// workgroup take the blocks in turn, and their sums are added up in LDS.
-//
-// An instruction loads eight whole lines of 128 bytes: lane (r, q) of the 16 x 4 that the matrix instruction sees has row r % 8 (+ 8), bytes
-// 16 (q + 4 (r / 8)).  Half of the lanes' pieces change places within their row of 16 lanes, and the matrix instruction's operands are there.
+// A tile is 16 rows of an expert's weights times the rows of activations of a group; the four waves of a workgroup take the blocks of 64 elements
+// (128 bytes a row) of its reduction in turn, and add their sums up in LDS.  Bound by the memory that the weights come from: an instruction loads
+// eight whole lines of 128 bytes, lane (r, q) of the 16 x 4 that the matrix instruction sees row r % 8 (+ 8), bytes 16 (q + 4 (r / 8)).
+//   Up to 8 rows of activations (MODE 8): the matrix instruction takes the weights as they came, rows 0 .. 7 with the lower half of the block and once
+//     more with the upper; its other operand is laid out the same way, by one load.  Of the 16 x 16 sums the 8 x 8 on the diagonal count.
+//   Up to 16 or 32: half of the lanes' pieces change places within their row of 16 lanes, and the operands are 16 rows with the lower, and with the upper
+//     half of the block.
 __device__ __forceinline__ u32x4 low_half(const u32x4 &first, const u32x4 &second) {
   u32x4 r;
 #pragma unroll
@@ -236,240 +305,404 @@ __device__ __forceinline__ u32x4 high_half(const u32x4 &first, const u32x4 &seco
   return r;
 }
 
-// W matrices of weights with the same rows and the same activations (gate and up).
-template <int DT, int NB, int W>
-__device__ __forceinline__ void product(const char *const (&weights)[W], int64_t row_stride, int32_t row0, int32_t rows_end, const char *const (&x)[NB], int32_t k_len, int wave, int lane,
-                                        f32x4 (&acc)[W][NB]) {
-  constexpr int R = NB == 4 ? 2 : NB == 2 ? 3 : 4;  // blocks in flight
+constexpr int TILE = 16;
+constexpr int RUN_PLACES = 512;  // rows of groups that LDS knows
+// A workgroup walks through a run of tiles: groups of one mode one after the other, of each `tiles` tiles (first products) or one (second products).
+struct Run {
+  int32_t group, tile, n;  // the first tile; how many
+};
+// What the waves of a workgroup hand each other: [turn][wave][matrix][row of activations (twice with MODE 8)][row of weights].
+template <int W>
+__device__ __forceinline__ f32x4 *joint_at(float *joint, int t, int wave, int m, int32_t i, int32_t row) {
+  return (f32x4 *)(joint + ((((t & 1) * 4 + wave) * W + m) * MOE_GROUP + i) * TILE + row);
+}
+constexpr int joint_floats(int w) { return 2 * 4 * w * MOE_GROUP * TILE; }
+// Of each place of a run's groups: its row and weight.
+struct Places {
+  int32_t row[RUN_PLACES];
+  float weight[RUN_PLACES];
+};
+// Loads by way of a buffer descriptor: a scalar base, and in each lane an offset below 2^31; a lane with OUTSIDE gets zeros and asks for nothing, so
+// that no load stands under a branch (which would leave the compiler in doubt how many are on their way).
+constexpr uint32_t OUTSIDE = 0x80000000u;
+__device__ __forceinline__ u32x4 load_from(const char *base, uint32_t lane_offset, int32_t offset) {
+  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)OUTSIDE, 0x00027000);
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)lane_offset, offset, 0));
+}
+
+// (an address that is the same in all lanes, where the compiler cannot see it)
+__device__ __forceinline__ const char *uniform(const char *p) {
+  const uint64_t a = (uint64_t)(uintptr_t)p;
+  return (const char *)(uintptr_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int32_t)(a >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int32_t)a));
+}
+
+// W matrices of weights with the same rows and the same activations (gate and up).  The stream of loads runs R blocks ahead of the matrix instructions, from
+// tile to tile, so it is only empty at the beginning and the end of a run.  group(i) is the i-th group, base(g, m) its matrix m, x_base(g) and x_offset(g, i)
+// where its i-th row of activations stands; done(t, group, tile) takes up the sums of turn t.
+template <int DT, int MODE, int W, int R, class G, class B, class XB, class XO, class D>
+__device__ __forceinline__ void stream(const Run &run, int32_t tiles, int64_t row_stride, int32_t rows_end, int32_t k_len, G group, B base, XB x_base, XO x_offset, D done, float *joint,
+                                       int wave, int lane) {
+  constexpr int NB = MODE == 32 ? 2 : 1, H = MODE == 8 ? 1 : 2, A = MODE == 8 ? 2 : NB;  // loads of activations for 16 rows, sums
   const int r16 = lane & 15, q = lane >> 4;
-  const int32_t blocks = (k_len + 63) / 64, mine = blocks > wave ? (blocks - wave + 3) / 4 : 0;
-  const char *at[W][2];
+  const int32_t steps = (k_len + 255) / 256;  // of the four waves' blocks each
+  const uint32_t w_piece = 16 * (q + 4 * (r16 >> 3)), x_piece = MODE == 8 ? w_piece : 16 * q;
+  u32x4 w[R][W][2], b[R][NB][H];
+  f32x4 acc[W][A] = {};
+
+  // loads
+  int32_t p_left = run.n, p_group = run.group, p_tile = run.tile, p_step = 0;
+  MoeGroup pg = group(p_group);
+  const char *w_base[W], *x_at;
+  uint32_t w_row[2], x_row[NB];
+  auto new_rows = [&]() {
 #pragma unroll
-  for (int m = 0; m < W; ++m)
+    for (int m = 0; m < W; ++m) w_base[m] = uniform(base(pg, m) + (int64_t)p_tile * TILE * row_stride);
 #pragma unroll
-    for (int j = 0; j < 2; ++j) at[m][j] = weights[m] + (int64_t)min(row0 + 8 * j + (r16 & 7), rows_end - 1) * row_stride;
-  u32x4 w[R][W][2], b[R][NB][2];
-  auto load = [&](int32_t i, u32x4(&w)[W][2], u32x4(&b)[NB][2]) {
-    const int32_t block = wave + 4 * i, k = block * 64 + 8 * (q + 4 * (r16 >> 3));
-    const bool in = i < mine && k < k_len;
+    for (int j = 0; j < 2; ++j) w_row[j] = (uint32_t)min(8 * j + (r16 & 7), rows_end - 1 - p_tile * TILE) * (uint32_t)row_stride + w_piece;
+  };
+  auto new_group = [&]() {
+    x_at = uniform(x_base(pg));
 #pragma unroll
-    for (int m = 0; m < W; ++m)
+    for (int n = 0; n < NB; ++n) x_row[n] = x_offset(pg, min(MODE == 8 ? r16 & 7 : n * 16 + r16, pg.rows - 1)) + x_piece;  // (columns behind the last repeat it and are not used)
+  };
+  new_group();
+  new_rows();
+  auto load = [&](u32x4(&w)[W][2], u32x4(&b)[NB][H]) {
+    // zeros behind the end of the reduction and behind the last tile
+    const int32_t k = (wave + 4 * p_step) * 128, left = p_left > 0 ? 2 * k_len - k : 0;
+    const bool in = (int32_t)w_piece < left;
 #pragma unroll
-      for (int j = 0; j < 2; ++j) w[m][j] = load16(in ? at[m][j] + 2 * (int64_t)k : (const char *)g_zeros);
+    for (int j = 0; j < 2; ++j) {
+      const uint32_t at = in ? w_row[j] : OUTSIDE;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int32_t kx = block * 64 + 32 * h + 8 * q;
-      const bool in_x = i < mine && kx < k_len;
+      for (int m = 0; m < W; ++m) w[m][j] = load_from(w_base[m], at, k);
+    }
 #pragma unroll
-      for (int n = 0; n < NB; ++n) b[n][h] = load16(in_x ? x[n] + 2 * (int64_t)kx : (const char *)g_zeros);
+    for (int h = 0; h < H; ++h) {
+      const bool in_x = (int32_t)x_piece + 64 * h < left;
+#pragma unroll
+      for (int n = 0; n < NB; ++n) b[n][h] = load_from(x_at, in_x ? x_row[n] + 64 * h : OUTSIDE, k);
+    }
+    if (++p_step == steps) {
+      p_step = 0;
+      if (--p_left > 0) {
+        if (++p_tile >= tiles) {
+          p_tile = tiles == 1 ? p_tile - 1 : 0;
+          pg = group(++p_group);
+          new_group();
+        }
+        new_rows();
+      }
     }
   };
 #pragma unroll
-  for (int u = 0; u < R; ++u) load(u, w[u], b[u]);
-  for (int32_t i = 0; i < mine; i += R) {
+  for (int u = 0; u < R; ++u) load(w[u], b[u]);
+
+  int32_t c_step = 0, c_group = run.group, c_tile = run.tile, t = 0;
+  while (t < run.n) {
 #pragma unroll
     for (int u = 0; u < R; ++u) {
 #pragma unroll
       for (int m = 0; m < W; ++m) {
-        const u32x4 lo = low_half(w[u][m][0], w[u][m][1]), hi = high_half(w[u][m][0], w[u][m][1]);
+        if constexpr (MODE == 8) {
+          mma16<DT>(w[u][m][0], b[u][0][0], acc[m][0]);
+          mma16<DT>(w[u][m][1], b[u][0][0], acc[m][1]);
+        } else {
+          const u32x4 lo = low_half(w[u][m][0], w[u][m][1]), hi = high_half(w[u][m][0], w[u][m][1]);
 #pragma unroll
-        for (int n = 0; n < NB; ++n) {
-          mma16<DT>(lo, b[u][n][0], acc[m][n]);
-          mma16<DT>(hi, b[u][n][1], acc[m][n]);
+          for (int n = 0; n < NB; ++n) {
+            mma16<DT>(lo, b[u][n][0], acc[m][n]);
+            mma16<DT>(hi, b[u][n][1], acc[m][n]);
+          }
         }
       }
-      load(i + u + R, w[u], b[u]);
+      load(w[u], b[u]);
+      if (++c_step == steps) {
+        c_step = 0;
+        if (t < run.n) {  // (the steps behind the last tile multiply zeros)
+          // lane (r, q) has, for row r of activations, rows 4q .. 4q + 3 of weights
+#pragma unroll
+          for (int m = 0; m < W; ++m)
+#pragma unroll
+            for (int n = 0; n < A; ++n) {
+              if constexpr (MODE == 8) {
+                if ((q >> 1) == (r16 >> 3)) *joint_at<W>(joint, t, wave, m, r16, 8 * n + 4 * (q & 1)) = acc[m][n];
+              } else {
+                *joint_at<W>(joint, t, wave, m, n * 16 + r16, 4 * q) = acc[m][n];
+              }
+              acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+          // (only LDS has to be there: the loads ahead stay on their way; the other turn's sums have been read by all that come here)
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          __builtin_amdgcn_s_barrier();
+          asm volatile("" ::: "memory");
+          done(t, c_group, c_tile);
+          ++t;
+          if (++c_tile >= tiles) {
+            c_tile = tiles == 1 ? c_tile - 1 : 0;
+            ++c_group;
+          }
+        }
+      }
     }
   }
+  __syncthreads();
+}
+// Four rows of weights times row i of activations.
+template <int MODE, int W>
+__device__ __forceinline__ f32x4 joined(float *joint, int t, int m, int32_t i, int quad) {
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int wave = 0; wave < 4; ++wave) {
+    v += *joint_at<W>(joint, t, wave, m, i, 4 * quad);
+    if constexpr (MODE == 8) v += *joint_at<W>(joint, t, wave, m, i + 8, 4 * quad);
+  }
+  return v;
 }
 
-// The waves' sums, in LDS: [wave][matrix][block of 16 rows][lane].  Returns the sum of what the waves have for (matrix, block) in lane `lane`.
-template <int NB, int W>
-struct Joined {
-  f32x4 (*red)[W][NB][64];
-  __device__ __forceinline__ void put(int wave, int lane, const f32x4 (&acc)[W][NB]) {
-#pragma unroll
-    for (int m = 0; m < W; ++m)
-#pragma unroll
-      for (int n = 0; n < NB; ++n) red[wave][m][n][lane] = acc[m][n];
-    __syncthreads();
-  }
-  __device__ __forceinline__ f32x4 get(int m, int n, int lane) const { return (red[0][m][n][lane] + red[1][m][n][lane]) + (red[2][m][n][lane] + red[3][m][n][lane]); }
-};
+// (What the router wrote is read through the scalar cache: it was another launch.)
+__device__ __forceinline__ MoeGroup group_of(const SK_CONSTANT MoeDev &P, int32_t i) {
+  const SK_CONSTANT MoeGroup &g = ((const SK_CONSTANT MoeGroup *)(uintptr_t)P.groups)[i];
+  return MoeGroup{g.expert, g.first, g.rows, 0};
+}
+__device__ __forceinline__ const SK_CONSTANT MoeCount &count_of(const MoeArgs &a, int32_t part) { return ((const SK_CONSTANT MoeCount *)(uintptr_t)a.counts)[part]; }
+__device__ __forceinline__ const SK_CONSTANT MoeDev &part_of(const MoeArgs &a, int32_t part) { return *(const SK_CONSTANT MoeDev *)(uintptr_t)(a.parts + part); }
+// The last group of n that begins at or before a place.
+__device__ __forceinline__ int32_t group_at(const int64_t *begin, int32_t n, int64_t at, int lane) { return __builtin_amdgcn_readfirstlane(last_not_above(begin, n, at, lane)); }
+__device__ __forceinline__ int64_t begin_of(const int64_t *begin, int32_t i) { return ((const SK_CONSTANT int64_t *)(uintptr_t)begin)[i]; }
 
-// h of 16 columns of an expert for the rows of a group.
-template <int DT, int NB, bool GATED>
-__device__ __forceinline__ void up_tile(const SK_CONSTANT MoeDev &P, const char *gate, const char *up, int64_t row_stride, int32_t width, int32_t f0, const MoeGroup &g, unsigned char *lds,
-                                        int tid) {
-  constexpr int W = GATED ? 2 : 1;
-  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, q = lane >> 4;
-  const char *x[NB];
-#pragma unroll
-  for (int n = 0; n < NB; ++n) {
-    const int32_t i = min(n * 16 + r16, g.rows - 1);  // (columns behind the last repeat it and are not stored)
-    x[n] = P.x + (int64_t)(g.expert < 0 ? g.first + i : got(P.row_of + g.first + i)) * P.x_stride;
+// Work is cut into equal shares, one for each workgroup of a launch that fills the card once.
+
+// The run that begins with a group: those behind it of the same kind (shared or not) and mode, up to group `end` and as many as LDS has places for.
+// Their rows and weights go to LDS.
+__device__ __forceinline__ int32_t run_end(const SK_CONSTANT MoeDev &P, int32_t begin, int32_t end, Places &places_of, int tid) {
+  const MoeGroup g = group_of(P, begin);
+  int32_t at = begin + 1, places = g.rows;
+  while (at < end) {
+    const MoeGroup next = group_of(P, at);
+    if ((next.expert < 0) != (g.expert < 0) || moe::mode_of(next.rows) != moe::mode_of(g.rows) || places + next.rows > RUN_PLACES) break;
+    places += next.rows;
+    ++at;
   }
-  f32x4 acc[W][NB] = {};
-  const char *weights[W];
-  weights[0] = up;
-  if constexpr (GATED) weights[1] = gate;
-  product<DT, NB, W>(weights, row_stride, f0, width, x, P.dim, wave, lane, acc);
-  Joined<NB, W> joined{(f32x4(*)[W][NB][64])lds};
-  joined.put(wave, lane, acc);
-  for (int n = wave; n < NB; n += 4) {
-    f32x4 h = joined.get(0, n, lane);
+  for (int32_t i = tid; i < places; i += CACHE_THREADS) {
+    places_of.row[i] = g.expert < 0 ? g.first + i : load_i32(P.row_of + g.first + i);
+    places_of.weight[i] = g.expert < 0 ? 1.f : load_f(P.weight_of + g.first + i);
+  }
+  __syncthreads();
+  return at;
+}
+
+template <int DT, int MODE, bool GATED>
+__device__ __forceinline__ void up_run(const SK_CONSTANT MoeDev &P, const Run &run, bool shared, float *joint, Places &places, int tid) {
+  constexpr int W = GATED ? 2 : 1;
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int32_t width = shared ? P.shared_ffn : P.ffn, place0 = group_of(P, run.group).first;
+  auto base = [&](const MoeGroup &g, int m) {
+    if (shared) return m ? P.shared_gate : P.shared_up;
+    return (m ? P.gate : P.up) + g.expert * P.up_expert;
+  };
+  auto done = [&](int32_t t, int32_t group, int32_t tile) {
+    const MoeGroup g = group_of(P, group);
+    const int32_t i = tid >> 2, f = tile * TILE + 4 * (tid & 3);
+    if (i >= g.rows || f >= width) return;  // (width is a multiple of 8)
+    f32x4 h = joined<MODE, W>(joint, t, 0, i, tid & 3);
     if constexpr (GATED) {
-      const f32x4 z = joined.get(1, n, lane);
+      const f32x4 z = joined<MODE, W>(joint, t, 1, i, tid & 3);
 #pragma unroll
       for (int k = 0; k < 4; ++k) h[k] *= activated(P.act, z[k]);
     } else {
 #pragma unroll
       for (int k = 0; k < 4; ++k) h[k] = activated(P.act, h[k]);
     }
-    const int32_t i = n * 16 + r16, f = f0 + 4 * q;
-    if (i < g.rows && f < width) {  // (width is a multiple of 8)
-      const int64_t place = g.expert < 0 ? (int64_t)P.rows * P.top_k + g.first + i : g.first + i;
-      put((uint64_t *)(P.h + place * P.h_stride + 2 * f), (uint64_t)pack2<DT>(h[2], h[3]) << 32 | pack2<DT>(h[0], h[1]));
-    }
+    const int64_t place = (shared ? (int64_t)P.rows * P.top_k : 0) + g.first + i;
+    store8(P.h + place * P.h_stride + 2 * f, u32x2{pack2<DT>(h[0], h[1]), pack2<DT>(h[2], h[3])});
+  };
+  stream<DT, MODE, W, MODE == 8 ? 3 : 2>(
+      run, shared ? P.shared_tiles : P.up_tiles, shared ? 2 * (int64_t)P.dim : P.up_row, width, P.dim, [&](int32_t i) { return group_of(P, i); }, base, [&](const MoeGroup &) { return P.x; },
+      [&](const MoeGroup &g, int32_t i) { return (uint32_t)places.row[g.first - place0 + i] * (uint32_t)P.x_stride; }, done, joint, wave, lane);
+}
+
+// The tiles of the first products from tile `tile` of group `group` on, up to (not with) tile `last_tile` of group `last`.
+template <int DT, bool GATED>
+__device__ __forceinline__ void up_tiles(const SK_CONSTANT MoeDev &P, int32_t group, int32_t tile, int32_t last, int32_t last_tile, float *joint, Places &places, int tid) {
+  while (group < last || (group == last && tile < last_tile)) {
+    const int32_t end = run_end(P, group, last_tile > 0 ? last + 1 : last, places, tid);
+    const MoeGroup g = group_of(P, group);
+    const bool shared = g.expert < 0;
+    const int32_t tiles = shared ? P.shared_tiles : P.up_tiles, mode = moe::mode_of(g.rows);
+    const Run run{group, tile, (end - group) * tiles - tile - (end > last ? tiles - last_tile : 0)};
+    if (mode == 8) up_run<DT, 8, GATED>(P, run, shared, joint, places, tid);
+    else if (mode == 16) up_run<DT, 16, GATED>(P, run, shared, joint, places, tid);
+    else up_run<DT, 32, GATED>(P, run, shared, joint, places, tid);
+    group = end, tile = 0;
   }
 }
 
-constexpr int MOE_LDS = 4 * 2 * 4 * 64 * 16;
-
-template <int DT>
-__device__ __forceinline__ void up_unit(const SK_CONSTANT MoeDev &P, const MoeGroup &g, int32_t tile, unsigned char *lds, int tid) {
-  const bool shared = g.expert < 0;
-  const char *gate = shared ? P.shared_gate : P.gate + g.expert * P.up_expert, *up = shared ? P.shared_up : P.up + g.expert * P.up_expert;
-  const int64_t stride = shared ? 2 * (int64_t)P.dim : P.up_row;
-  const int32_t width = shared ? P.shared_ffn : P.ffn, f0 = tile * P.up_rows;
-  if (P.gate) {
-    if (g.rows <= 16) up_tile<DT, 1, true>(P, gate, up, stride, width, f0, g, lds, tid);
-    else if (g.rows <= 32) up_tile<DT, 2, true>(P, gate, up, stride, width, f0, g, lds, tid);
-    else up_tile<DT, 4, true>(P, gate, up, stride, width, f0, g, lds, tid);
-  } else {
-    if (g.rows <= 16) up_tile<DT, 1, false>(P, gate, up, stride, width, f0, g, lds, tid);
-    else if (g.rows <= 32) up_tile<DT, 2, false>(P, gate, up, stride, width, f0, g, lds, tid);
-    else up_tile<DT, 4, false>(P, gate, up, stride, width, f0, g, lds, tid);
-  }
-}
-
-template <int DT, int NB>
-__device__ __forceinline__ void down_tile(const SK_CONSTANT MoeDev &P, const char *weights, int64_t row_stride, int32_t width, int32_t d0, const MoeGroup &g, unsigned char *lds, int tid) {
-  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, q = lane >> 4;
-  const int64_t place0 = g.expert < 0 ? (int64_t)P.rows * P.top_k + g.first : g.first;
-  const char *x[NB];
+__global__ void __launch_bounds__(CACHE_THREADS, MOE_UP_RESIDENT) sk_moe_up(MoeArgs a) {
+  __shared__ __attribute__((aligned(16))) float joint[joint_floats(2)];
+  __shared__ Places places;
+  const int lane = threadIdx.x & 63;
+  int64_t total = 0;
+  for (int32_t i = 0; i < a.n; ++i) total += count_of(a, i).first_work;
+  const moe::Share share = moe::share_of(total, gridDim.x, blockIdx.x);
+  int64_t offset = 0;
+  for (int32_t i = 0; i < a.n && offset < share.end; ++i) {
+    const SK_CONSTANT MoeDev &P = part_of(a, i);
+    const int64_t here = count_of(a, i).first_work;
+    if (share.begin < offset + here && here > 0) {
+      const int32_t groups = count_of(a, i).groups;
+      int32_t group[2], tile[2];
 #pragma unroll
-  for (int n = 0; n < NB; ++n) x[n] = P.h + (place0 + min(n * 16 + r16, g.rows - 1)) * P.h_stride;
-  f32x4 acc[1][NB] = {};
-  const char *const w[1] = {weights};
-  product<DT, NB, 1>(w, row_stride, d0, P.dim, x, width, wave, lane, acc);
-  Joined<NB, 1> joined{(f32x4(*)[1][NB][64])lds};
-  joined.put(wave, lane, acc);
-  for (int n = wave; n < NB; n += 4) {
-    const f32x4 v = joined.get(0, n, lane);
-    const int32_t i = n * 16 + r16, d = d0 + 4 * q;
-    if (i < g.rows && d < P.dim) {
-      float *at = P.part + (place0 + i) * P.part_stride + d;
-      store_shared(at, f32x2{v[0], v[1]});
-      store_shared(at + 2, f32x2{v[2], v[3]});
+      for (int e = 0; e < 2; ++e) {  // beginning and end
+        const int64_t at = e ? share.end - offset : max(share.begin - offset, (int64_t)0);
+        group[e] = group_at(P.first_begin, groups, at, lane);
+        const MoeGroup g = group_of(P, group[e]);
+        const int32_t tiles = g.expert < 0 ? P.shared_tiles : P.up_tiles;
+        tile[e] = __builtin_amdgcn_readfirstlane(moe::tile_from(at, begin_of(P.first_begin, group[e]), moe::cost(P.dim, P.gate ? 2 : 1, moe::mode_of(g.rows)), tiles));
+        if (tile[e] == tiles) ++group[e], tile[e] = 0;
+      }
+      if (P.dtype == SK_BF16) P.gate ? up_tiles<SK_BF16, true>(P, group[0], tile[0], group[1], tile[1], joint, places, threadIdx.x) : up_tiles<SK_BF16, false>(P, group[0], tile[0], group[1], tile[1], joint, places, threadIdx.x);
+      else P.gate ? up_tiles<SK_F16, true>(P, group[0], tile[0], group[1], tile[1], joint, places, threadIdx.x) : up_tiles<SK_F16, false>(P, group[0], tile[0], group[1], tile[1], joint, places, threadIdx.x);
     }
+    offset += here;
+  }
+}
+
+// The second products: the tiles of 16 columns of the output, and for each of them all groups, one after the other.  A workgroup's sums over the groups
+// of its share, weighted, stand in LDS (16 columns of every row of the part).  Where a share has all groups of a tile, they are the output; otherwise they go
+// to memory as a slice, and the workgroup whose slice arrives last adds the slices up, in their order.  A share begins and ends within a
+// tile, so a workgroup has two places for slices: the second for a tile that it begins, the first for one that another has begun.
+template <int DT, int MODE>
+__device__ __forceinline__ void down_run(const SK_CONSTANT MoeDev &P, const Run &run, float *joint, Places &places, float *sums, int tid) {
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const MoeGroup first = group_of(P, run.group);
+  const bool shared = first.expert < 0;
+  const int64_t place0 = shared ? (int64_t)P.rows * P.top_k : 0;
+  const int32_t width = shared ? P.shared_ffn : P.ffn;
+  auto done = [&](int32_t t, int32_t group, int32_t) {
+    const MoeGroup g = group_of(P, group);
+    const int32_t i = tid >> 2;
+    if (i >= g.rows) return;  // (a row stands in a group once)
+    f32x4 *at = (f32x4 *)(sums + places.row[g.first - first.first + i] * TILE + 4 * (tid & 3));
+    *at += places.weight[g.first - first.first + i] * joined<MODE, 1>(joint, t, 0, i, tid & 3);
+  };
+  stream<DT, MODE, 1, MODE == 8 ? 4 : MODE == 16 ? 3 : 2>(
+      run, 1, shared ? 2 * (int64_t)width : P.down_row, P.dim, width, [&](int32_t i) { return group_of(P, i); },
+      [&](const MoeGroup &g, int) { return shared ? P.shared_down : P.down + g.expert * P.down_expert; }, [&](const MoeGroup &g) { return P.h + (place0 + g.first) * P.h_stride; },
+      [&](const MoeGroup &, int32_t i) { return (uint32_t)i * (uint32_t)P.h_stride; }, done, joint, wave, lane);
+}
+
+// Groups [g0, g1) of a tile of the output.
+template <int DT>
+__device__ __forceinline__ void down_groups(const SK_CONSTANT MoeDev &P, int32_t tile, int32_t g0, int32_t g1, float *joint, Places &places, float *sums, int tid) {
+  while (g0 < g1) {
+    const int32_t end = run_end(P, g0, g1, places, tid);
+    const Run run{g0, tile, end - g0};
+    const int32_t mode = moe::mode_of(group_of(P, g0).rows);
+    if (mode == 8) down_run<DT, 8>(P, run, joint, places, sums, tid);
+    else if (mode == 16) down_run<DT, 16>(P, run, joint, places, sums, tid);
+    else down_run<DT, 32>(P, run, joint, places, sums, tid);
+    g0 = end;
   }
 }
 
 template <int DT>
-__device__ __forceinline__ void down_unit(const SK_CONSTANT MoeDev &P, const MoeGroup &g, int32_t tile, unsigned char *lds, int tid) {
-  const bool shared = g.expert < 0;
-  const char *w = shared ? P.shared_down : P.down + g.expert * P.down_expert;
-  const int32_t width = shared ? P.shared_ffn : P.ffn, d0 = tile * P.down_rows;
-  const int64_t stride = shared ? 2 * (int64_t)width : P.down_row;
-  if (g.rows <= 16) down_tile<DT, 1>(P, w, stride, width, d0, g, lds, tid);
-  else if (g.rows <= 32) down_tile<DT, 2>(P, w, stride, width, d0, g, lds, tid);
-  else down_tile<DT, 4>(P, w, stride, width, d0, g, lds, tid);
+__device__ __forceinline__ void store_out(const SK_CONSTANT MoeDev &P, int32_t row, int32_t d, const f32x4 &v) {
+  if (d < P.dim) store8(P.out + row * P.out_stride + 2 * d, u32x2{pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3])});
 }
 
-// The weighted sum of a tile's columns for all rows, in the order of the choices.
 template <int DT>
-__device__ __forceinline__ void add_up(const SK_CONSTANT MoeDev &P, int32_t rows, int32_t tile, int tid) {
-  const int32_t quads = min(P.down_rows, P.dim - tile * P.down_rows) / 4;
-  for (int32_t i = tid; i < rows * quads; i += CACHE_THREADS) {
-    const int32_t row = i / quads, d = tile * P.down_rows + 4 * (i % quads);
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    if (P.shared_ffn) {
-      const float *at = P.part + ((int64_t)P.rows * P.top_k + row) * P.part_stride + d;
-      const f32x2 a = load_shared(at), b = load_shared(at + 2);
-      sum = f32x4{a[0], a[1], b[0], b[1]};
+__device__ __forceinline__ void down_share(const MoeArgs &a, const SK_CONSTANT MoeDev &P, const SK_CONSTANT MoeCount &c, moe::Share share, int64_t offset, int64_t total, int64_t shares,
+                                           float *joint, Places &places, float *sums, uint32_t *flag, int tid) {
+  const int64_t tile_work = c.second_work, me = blockIdx.x;
+  const int64_t begin = moe::most(share.begin - offset, 0), end = moe::least(share.end - offset, tile_work * P.down_tiles);
+  // the first group that begins at or behind a place of a tile
+  auto group_from = [&](int64_t at) {
+    if (at <= 0) return 0;
+    return group_at(P.second_begin, c.groups, at - 1, tid & 63) + 1;
+  };
+  for (int32_t tile = (int32_t)(begin / tile_work); tile * tile_work < end; ++tile) {
+    const int64_t at = tile * tile_work;
+    const int32_t g0 = group_from(begin - at), g1 = group_from(moe::least(end - at, tile_work));
+    if (g0 >= g1) continue;
+    for (int32_t k = tid; k < c.rows * TILE; k += CACHE_THREADS) sums[k] = 0.f;
+    __syncthreads();
+    down_groups<DT>(P, tile, g0, g1, joint, places, sums, tid);
+    if (g1 - g0 == c.groups) {
+      for (int32_t k = tid; k < c.rows * 4; k += CACHE_THREADS) store_out<DT>(P, k >> 2, tile * TILE + 4 * (k & 3), *(const f32x4 *)(sums + 4 * k));
+    } else {
+      // the workgroups that have groups of this tile: every one from that of the first to that of the last
+      const int64_t first = moe::owner_of(offset + at, total, shares), last = moe::owner_of(offset + at + begin_of(P.second_begin, c.groups - 1), total, shares);
+      float *slice = a.slices + (2 * me + (me == first ? 1 : 0)) * a.slice_floats;
+      for (int32_t k = tid; k < c.rows * 4; k += CACHE_THREADS) {
+        const f32x4 v = *(const f32x4 *)(sums + 4 * k);
+        store_shared(slice + 4 * k, f32x2{v[0], v[1]});
+        store_shared(slice + 4 * k + 2, f32x2{v[2], v[3]});
+      }
+      if (last_to_arrive(P.summed + tile, (int32_t)(last - first + 1), flag)) {
+        for (int32_t k = tid; k < c.rows * 4; k += CACHE_THREADS) {
+          f32x4 v = {0.f, 0.f, 0.f, 0.f};
+          constexpr int AHEAD = 8;  // slices on their way at a time
+          for (int64_t s0 = first; s0 <= last; s0 += AHEAD) {
+            f32x2 lo[AHEAD], hi[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+              const int64_t s = min(s0 + u, last);
+              const float *from = a.slices + (2 * s + (s == first ? 1 : 0)) * a.slice_floats + 4 * k;
+              lo[u] = load_shared(from), hi[u] = load_shared(from + 2);
+            }
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+              if (s0 + u <= last) v += f32x4{lo[u][0], lo[u][1], hi[u][0], hi[u][1]};
+          }
+          store_out<DT>(P, k >> 2, tile * TILE + 4 * (k & 3), v);
+        }
+      }
     }
-    for (int32_t j = 0; j < P.top_k; ++j) {
-      const float w = got(P.weights + row * P.top_k + j);
-      const float *at = P.part + (int64_t)got(P.places + row * P.top_k + j) * P.part_stride + d;
-      const f32x2 a = load_shared(at), b = load_shared(at + 2);
-      sum[0] += w * a[0], sum[1] += w * a[1], sum[2] += w * b[0], sum[3] += w * b[1];
-    }
-    store8(P.out + row * P.out_stride + 2 * d, u32x2{pack2<DT>(sum[0], sum[1]), pack2<DT>(sum[2], sum[3])});
+    __syncthreads();
   }
 }
 
-// The group of a unit, those of the shared expert first, and its tile; no rows: there is no such unit.
-__device__ __forceinline__ MoeGroup find_unit(const SK_CONSTANT MoeDev &P, int32_t rows, int32_t unit, int32_t shared_tiles, int32_t tiles, int32_t &tile) {
-  const int32_t shared = P.shared_ffn ? (rows + MOE_GROUP - 1) / MOE_GROUP * shared_tiles : 0;
-  const bool is_shared = unit < shared;
-  const int32_t of = is_shared ? shared_tiles : tiles, at = is_shared ? unit : unit - shared, i = at / of;
-  tile = at - i * of;
-  const int32_t first = i * MOE_GROUP;
-  if (is_shared) return MoeGroup{-1, first, min(MOE_GROUP, rows - first), 0};
-  if (i >= __builtin_amdgcn_readfirstlane(got(P.n_groups))) return MoeGroup{0, 0, 0, 0};
-  return MoeGroup{__builtin_amdgcn_readfirstlane(got(&P.groups[i].expert)), __builtin_amdgcn_readfirstlane(got(&P.groups[i].first)),
-                  __builtin_amdgcn_readfirstlane(got(&P.groups[i].rows)), 0};
-}
-
-__global__ void __launch_bounds__(CACHE_THREADS, 3) sk_moe_up(MoeArgs a) {
-  __shared__ __attribute__((aligned(16))) unsigned char lds[MOE_LDS];
-  const int32_t part = __builtin_amdgcn_readfirstlane(last_not_above(a.first, a.n, (int64_t)blockIdx.x, threadIdx.x & 63));
-  const SK_CONSTANT MoeDev &P = *(const SK_CONSTANT MoeDev *)(uintptr_t)(a.parts + part);
-  const int32_t unit = (int32_t)(blockIdx.x - ((const SK_CONSTANT uint32_t *)(uintptr_t)a.first)[part]);
-  int32_t tile;
-  const MoeGroup g = find_unit(P, rows_of(P), unit, P.shared_tiles, P.up_tiles, tile);
-  if (!g.rows) return;
-  if (P.dtype == SK_BF16) up_unit<SK_BF16>(P, g, tile, lds, threadIdx.x);
-  else up_unit<SK_F16>(P, g, tile, lds, threadIdx.x);
-}
-
-__global__ void __launch_bounds__(CACHE_THREADS, 3) sk_moe_down(MoeArgs a) {
-  __shared__ __attribute__((aligned(16))) unsigned char lds[MOE_LDS];
+__global__ void __launch_bounds__(CACHE_THREADS, MOE_DOWN_RESIDENT) sk_moe_down(MoeArgs a) {
+  __shared__ __attribute__((aligned(16))) float joint[joint_floats(1)];
+  __shared__ Places places;
   __shared__ uint32_t flag;
-  const int32_t part = __builtin_amdgcn_readfirstlane(last_not_above(a.first, a.n, (int64_t)blockIdx.x, threadIdx.x & 63));
-  const SK_CONSTANT MoeDev &P = *(const SK_CONSTANT MoeDev *)(uintptr_t)(a.parts + part);
-  const int32_t unit = (int32_t)(blockIdx.x - ((const SK_CONSTANT uint32_t *)(uintptr_t)a.first)[part]);
-  const int32_t rows = rows_of(P);
-  int32_t tile;
-  const MoeGroup g = find_unit(P, rows, unit, P.down_tiles, P.down_tiles, tile);
-  if (!g.rows) return;
-  if (P.dtype == SK_BF16) down_unit<SK_BF16>(P, g, tile, lds, threadIdx.x);
-  else down_unit<SK_F16>(P, g, tile, lds, threadIdx.x);
-  const int32_t groups = got(P.n_groups) + (P.shared_ffn ? (rows + MOE_GROUP - 1) / MOE_GROUP : 0);
-  if (!last_to_arrive(P.summed + tile, groups, &flag)) return;
-  if (P.dtype == SK_BF16) add_up<SK_BF16>(P, rows, tile, threadIdx.x);
-  else add_up<SK_F16>(P, rows, tile, threadIdx.x);
+  extern __shared__ __attribute__((aligned(16))) float sums[];
+  int64_t total = 0, longest = 0;
+  for (int32_t i = 0; i < a.n; ++i) {
+    total += count_of(a, i).second_work * part_of(a, i).down_tiles;
+    longest = max(longest, count_of(a, i).longest);
+  }
+  const int64_t shares = moe::shares_for(total, longest, gridDim.x);
+  if ((int64_t)blockIdx.x >= shares) return;
+  const moe::Share share = moe::share_of(total, shares, blockIdx.x);
+  int64_t offset = 0;
+  for (int32_t i = 0; i < a.n && offset < share.end; ++i) {
+    const SK_CONSTANT MoeDev &P = part_of(a, i);
+    const SK_CONSTANT MoeCount &c = count_of(a, i);
+    const int64_t here = c.second_work * P.down_tiles;
+    if (here > 0 && share.begin < offset + here) {
+      if (P.dtype == SK_BF16) down_share<SK_BF16>(a, P, c, share, offset, total, shares, joint, places, sums, &flag, threadIdx.x);
+      else down_share<SK_F16>(a, P, c, share, offset, total, shares, joint, places, sums, &flag, threadIdx.x);
+    }
+    offset += here;
+  }
 }
 
 }  // namespace sk
 
 struct sk_moe_plan : sk::PlanOnDevice {
   sk::MoePlanHost host;
-  const sk::MoeDev *parts = nullptr;
-  const uint32_t *first[3] = {};  // of the router, of up, of down
+  sk::MoeArgs args{};
 };
 
 namespace {
 
 sk_status upload(sk_moe_plan &plan) {
   sk::MoePlanHost &h = plan.host;
-  const std::vector<uint32_t> *firsts[3] = {&h.route_first, &h.up_first, &h.down_first};
-  // counters, parts, first workgroups
-  const size_t o_parts = sk::align_up(h.counters, 256);
-  size_t o_first[4] = {o_parts + sk::align_up(h.parts.size() * sizeof(sk::MoeDev), 256)};
-  for (int i = 0; i < 3; ++i) o_first[i + 1] = o_first[i] + sk::align_up(firsts[i]->size() * 4, 256);
-  std::vector<char> image(o_first[3], 0);
+  // counters, parts, first workgroups of the router
+  const size_t o_parts = sk::align_up(h.counters, 256), o_first = o_parts + sk::align_up(h.parts.size() * sizeof(sk::MoeDev), 256);
+  std::vector<char> image(o_first + h.route_first.size() * 4, 0);
   char *ws = nullptr;
   const sk_status st = sk::upload_image(plan, image, h.workspace, &ws);
   if (st != SK_OK) return st;
@@ -477,14 +710,14 @@ sk_status upload(sk_moe_plan &plan) {
   std::vector<sk::MoeDev> parts = h.parts;
   for (sk::MoeDev &d : parts) {
     moved(d.routed, plan.blob), moved(d.blocks_routed, plan.blob), moved(d.summed, plan.blob);
-    moved(d.logits, ws), moved(d.ids, ws), moved(d.places, ws), moved(d.weights, ws), moved(d.row_of, ws), moved(d.groups, ws), moved(d.n_groups, ws), moved(d.h, ws), moved(d.part, ws);
+    moved(d.logits, ws), moved(d.ids, ws), moved(d.weights, ws), moved(d.row_of, ws), moved(d.weight_of, ws), moved(d.groups, ws), moved(d.first_begin, ws), moved(d.second_begin, ws), moved(d.count, ws), moved(d.h, ws);
   }
   if (!parts.empty()) std::memcpy(image.data() + o_parts, parts.data(), parts.size() * sizeof(sk::MoeDev));
-  for (int i = 0; i < 3; ++i) {
-    std::memcpy(image.data() + o_first[i], firsts[i]->data(), firsts[i]->size() * 4);
-    plan.first[i] = (const uint32_t *)(plan.blob + o_first[i]);
-  }
-  plan.parts = (const sk::MoeDev *)(plan.blob + o_parts);
+  std::memcpy(image.data() + o_first, h.route_first.data(), h.route_first.size() * 4);
+  sk::MoeCount *counts = h.counts;
+  float *slices = h.slices;
+  moved(counts, ws), moved(slices, ws);
+  plan.args = sk::MoeArgs{(const sk::MoeDev *)(plan.blob + o_parts), (const uint32_t *)(plan.blob + o_first), counts, slices, h.slice_floats, (int32_t)parts.size()};
   return sk::copy_image(plan, image);
 }
 
@@ -493,7 +726,7 @@ sk_status upload(sk_moe_plan &plan) {
 extern "C" {
 
 sk_status sk_moe_plan_create(const sk_moe_problem *problems, int32_t n, const sk_layer_params *params, sk_moe_plan **out) {
-  return sk::create_plan<sk_moe_plan>(params, out, [&](sk_moe_plan &plan, int32_t workgroups, std::string &err) { return sk::plan_moe(problems, n, workgroups, plan.host, err); }, upload);
+  return sk::create_plan<sk_moe_plan>(params, out, [&](sk_moe_plan &plan, int32_t cus, int32_t workgroups, std::string &err) { return sk::plan_moe(problems, n, cus, workgroups, plan.host, err); }, upload);
 }
 
 sk_status sk_moe_plan_destroy(sk_moe_plan *plan) {
@@ -508,10 +741,10 @@ sk_status sk_moe_launch(sk_moe_plan *plan, void *hip_stream) {
     sk_status st = sk::admit(plan, stream, &in_capture);
     if (st != SK_OK || plan->host.parts.empty()) return st;
     const hipEvent_t behind = in_capture ? nullptr : plan->last_use;
-    auto args = [&](int i) { return sk::MoeArgs{plan->parts, plan->first[i], (int32_t)plan->host.parts.size()}; };
-    st = sk::launch(sk::sk_moe_route, (int64_t)plan->host.route_first.back(), stream, nullptr, args(0));
-    if (st == SK_OK) st = sk::launch(sk::sk_moe_up, (int64_t)plan->host.up_first.back(), stream, nullptr, args(1));
-    if (st == SK_OK) st = sk::launch(sk::sk_moe_down, (int64_t)plan->host.down_first.back(), stream, behind, args(2));
+    const sk::MoePlanHost &h = plan->host;
+    st = sk::launch(sk::sk_moe_route, (int64_t)h.route_first.back(), stream, nullptr, plan->args);
+    if (st == SK_OK) st = sk::launch(sk::sk_moe_up, h.up_workgroups, stream, nullptr, plan->args);
+    if (st == SK_OK) st = sk::launch(sk::sk_moe_down, h.down_workgroups, stream, behind, plan->args, sk::CACHE_THREADS, h.lds);
     plan->ledger.after_launch((uintptr_t)stream, in_capture, behind && st == SK_OK);  // also after a failure: some launches may be out
     return st;
   });

@@ -212,7 +212,7 @@ void sk_layer_params_default(sk_layer_params *params) {
 }
 
 sk_status sk_norm_plan_create(const sk_norm_problem *problems, int32_t n, const sk_layer_params *params, sk_norm_plan **out) {
-  return sk::create_plan<sk_norm_plan>(params, out, [&](sk_norm_plan &plan, int32_t workgroups, std::string &err) { return sk::plan_norm(problems, n, workgroups, plan.host, err); },
+  return sk::create_plan<sk_norm_plan>(params, out, [&](sk_norm_plan &plan, int32_t, int32_t, std::string &err) { return sk::plan_norm(problems, n, plan.host, err); },
                                        [](sk_norm_plan &) { return SK_OK; });
 }
 

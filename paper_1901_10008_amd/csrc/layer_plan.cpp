@@ -72,7 +72,7 @@ struct Layout {
 // Rows of up to 2048 elements get a wave each from that many rows on; fewer get a workgroup each, whose threads have a quarter of the work each.
 constexpr int32_t NORM_WAVE_ROWS = 2048;
 
-sk_status plan_norm(const sk_norm_problem *problems, int32_t n, int32_t, NormPlanHost &out, std::string &err) {
+sk_status plan_norm(const sk_norm_problem *problems, int32_t n, NormPlanHost &out, std::string &err) {
   Spans written;
   struct Item {
     NormForm form;
@@ -143,10 +143,10 @@ sk_status plan_norm(const sk_norm_problem *problems, int32_t n, int32_t, NormPla
 
 // ---- mixture of experts ----------------------------------------------------------------------------------------------------
 
-sk_status plan_moe(const sk_moe_problem *problems, int32_t n, int32_t, MoePlanHost &out, std::string &err) {
+sk_status plan_moe(const sk_moe_problem *problems, int32_t n, int32_t compute_units, int32_t workgroups, MoePlanHost &out, std::string &err) {
   Spans written;
-  out.route_first.assign(1, 0u), out.up_first.assign(1, 0u), out.down_first.assign(1, 0u);
-  int64_t route = 0, up = 0, down = 0;
+  out.route_first.assign(1, 0u);
+  int64_t route = 0, most_rows = 0, tiles = 0;
   Layout counters, work;
   const sk_status st = each(problems, n, err, [&](const sk_moe_problem &p) -> sk_status {
     if (p.dtype != SK_BF16 && p.dtype != SK_F16) return refuse(err, SK_ERR_UNSUPPORTED, "dtype must be SK_BF16 or SK_F16");
@@ -155,7 +155,7 @@ sk_status plan_moe(const sk_moe_problem *problems, int32_t n, int32_t, MoePlanHo
     if (p.top_k > p.experts) return refuse(err, SK_ERR_INVALID_ARG, "top_k is larger than the number of experts");
     if (p.experts > MOE_EXPERTS || p.top_k > MOE_TOP) return refuse(err, SK_ERR_UNSUPPORTED, "more than 512 experts or 32 chosen");
     if (p.dim % 8 || p.ffn % 8 || p.shared_ffn % 8) return refuse(err, SK_ERR_UNSUPPORTED, "dim and widths must be multiples of 8");
-    if (p.dim > 1 << 24 || p.ffn > 1 << 24 || p.shared_ffn > 1 << 24) return refuse(err, SK_ERR_UNSUPPORTED, "dim or a width of more than 2^24");
+    if (p.dim >= 1 << 21 || p.ffn > 1 << 24 || p.shared_ffn > 1 << 24) return refuse(err, SK_ERR_UNSUPPORTED, "dim of 2^21 and more, or a width of more than 2^24");
     if (p.act < SK_ACT_NONE || p.act > SK_ACT_RELU) return refuse(err, SK_ERR_INVALID_ARG, "no such act");
     if (p.scoring != SK_MOE_SOFTMAX && p.scoring != SK_MOE_SIGMOID) return refuse(err, SK_ERR_INVALID_ARG, "no such scoring");
     if ((p.normalize != 0 && p.normalize != 1) || !std::isfinite(p.scale)) return refuse(err, SK_ERR_INVALID_ARG, "normalize must be 0 or 1, scale finite");
@@ -169,6 +169,7 @@ sk_status plan_moe(const sk_moe_problem *problems, int32_t n, int32_t, MoePlanHo
       return refuse(err, SK_ERR_INVALID_ARG, "a stride is less than a row");
     for (int64_t s : {x, o, r, ur, dr})
       if (s >= (int64_t)1 << 40) return refuse(err, SK_ERR_UNSUPPORTED, "a stride reaches too far");
+    if (x >= 1 << 21 || ur >= 1 << 26 || dr >= 1 << 26) return refuse(err, SK_ERR_UNSUPPORTED, "rows of x 2^21 elements apart and more, or rows of weights 2^26");
     int64_t ue, de;
     if (!stride_of(p.up_expert_stride, (ffn - 1) * ur + dim, p.experts, ue) || !stride_of(p.down_expert_stride, (dim - 1) * dr + ffn, p.experts, de))
       return refuse(err, SK_ERR_INVALID_ARG, "a stride lets experts overlap");
@@ -200,28 +201,35 @@ sk_status plan_moe(const sk_moe_problem *problems, int32_t n, int32_t, MoePlanHo
       d.row0 = (int32_t)row0, d.rows = (int32_t)rows, d.dim = p.dim, d.experts = p.experts, d.top_k = p.top_k, d.ffn = p.ffn, d.shared_ffn = p.shared_ffn;
       d.act = p.act, d.scoring = p.scoring, d.normalize = p.normalize, d.dtype = p.dtype, d.router_f32 = p.router_dtype == SK_F32;
       d.scale = p.scale != 0.f ? p.scale : 1.f;
-      d.up_rows = d.down_rows = 16;
-      d.up_tiles = (int32_t)((ffn + d.up_rows - 1) / d.up_rows), d.shared_tiles = (int32_t)(((int64_t)p.shared_ffn + d.up_rows - 1) / d.up_rows);
-      d.down_tiles = (int32_t)((dim + d.down_rows - 1) / d.down_rows);
+      d.up_tiles = (int32_t)((ffn + 15) / 16), d.shared_tiles = (int32_t)(((int64_t)p.shared_ffn + 15) / 16), d.down_tiles = (int32_t)((dim + 15) / 16);
       // every group but the last of an expert has MOE_GROUP rows
-      d.most_groups = (int32_t)std::min<int64_t>(std::min<int64_t>(p.experts, pairs) + pairs / MOE_GROUP, pairs);
       const int64_t blocks = (rows + ROUTE_ROWS - 1) / ROUTE_ROWS, shared_groups = p.shared_ffn ? (rows + MOE_GROUP - 1) / MOE_GROUP : 0;
+      const int64_t reached = std::min<int64_t>(p.experts, pairs), routed_groups = reached + (pairs - reached) / MOE_GROUP;
+      d.most_groups = (int32_t)(routed_groups + shared_groups);
       route += blocks * ((p.experts + ROUTE_EXPERTS - 1) / ROUTE_EXPERTS);
-      up += (int64_t)d.most_groups * d.up_tiles + shared_groups * d.shared_tiles;
-      down += ((int64_t)d.most_groups + shared_groups) * d.down_tiles;
-      if (route > MOST_GRID || up > MOST_GRID || down > MOST_GRID) return refuse(err, SK_ERR_UNSUPPORTED, "more units of work than a launch's grid can hold");
-      out.route_first.push_back((uint32_t)route), out.up_first.push_back((uint32_t)up), out.down_first.push_back((uint32_t)down);
+      if (route > MOST_GRID) return refuse(err, SK_ERR_UNSUPPORTED, "more units of work than a launch's grid can hold");
+      out.route_first.push_back((uint32_t)route);
+      most_rows = std::max(most_rows, rows);
+      tiles += std::max(d.most_groups * (int64_t)d.down_tiles, routed_groups * d.up_tiles + shared_groups * d.shared_tiles);
       counters.take(d.routed, blocks, 4), counters.take(d.blocks_routed, 1, 4), counters.take(d.summed, d.down_tiles, 4);
-      work.take(d.logits, rows * p.experts), work.take(d.ids, pairs), work.take(d.places, pairs), work.take(d.weights, pairs), work.take(d.row_of, pairs);
-      work.take(d.groups, d.most_groups), work.take(d.n_groups, 1);
-      d.h_stride = (std::max<int64_t>(ffn, p.shared_ffn) + 63) / 64 * 128, d.part_stride = (dim + 31) / 32 * 32;
-      work.take(d.h, (pairs + (p.shared_ffn ? rows : 0)) * d.h_stride), work.take(d.part, (pairs + (p.shared_ffn ? rows : 0)) * d.part_stride);
+      work.take(d.logits, rows * p.experts), work.take(d.ids, pairs), work.take(d.weights, pairs), work.take(d.row_of, pairs), work.take(d.weight_of, pairs);
+      work.take(d.groups, d.most_groups), work.take(d.first_begin, d.most_groups), work.take(d.second_begin, d.most_groups);
+      d.h_stride = (std::max<int64_t>(ffn, p.shared_ffn) + 63) / 64 * 128;
+      work.take(d.h, (pairs + (p.shared_ffn ? rows : 0)) * d.h_stride);
       out.parts.push_back(d);
     }
     return SK_OK;
   });
   if (st != SK_OK) return st;
   if (written.overlap()) return refuse(err, SK_ERR_OVERLAP, "ranges of out, expert_ids and expert_weights overlap");
+  work.take(out.counts, (int64_t)out.parts.size());
+  for (size_t i = 0; i < out.parts.size(); ++i) out.parts[i].count = out.counts + i;
+  // never more than there can be tiles
+  auto cut = [&](int64_t resident) { return std::max<int64_t>(1, std::min<int64_t>(workgroups ? workgroups : resident * compute_units, tiles)); };
+  out.up_workgroups = cut(MOE_UP_RESIDENT), out.down_workgroups = cut(MOE_DOWN_RESIDENT);
+  out.slice_floats = most_rows * 16;
+  work.take(out.slices, 2 * out.down_workgroups * out.slice_floats);
+  out.lds = (size_t)most_rows * 16 * sizeof(float);
   out.counters = counters.bytes;
   out.workspace = work.bytes;
   return SK_OK;
@@ -229,7 +237,7 @@ sk_status plan_moe(const sk_moe_problem *problems, int32_t n, int32_t, MoePlanHo
 
 // ---- verification ----------------------------------------------------------------------------------------------------------
 
-sk_status plan_verify(const sk_verify_problem *problems, int32_t n, int32_t, VerifyPlanHost &out, std::string &err) {
+sk_status plan_verify(const sk_verify_problem *problems, int32_t n, VerifyPlanHost &out, std::string &err) {
   Spans written;
   out.stat_first.assign(1, 0u), out.sum_first.assign(1, 0u);
   int64_t stat = 0, sum = 0;

@@ -429,7 +429,7 @@ sk_status upload(sk_verify_plan &plan) {
 extern "C" {
 
 sk_status sk_verify_plan_create(const sk_verify_problem *problems, int32_t n, const sk_layer_params *params, sk_verify_plan **out) {
-  return sk::create_plan<sk_verify_plan>(params, out, [&](sk_verify_plan &plan, int32_t workgroups, std::string &err) { return sk::plan_verify(problems, n, workgroups, plan.host, err); }, upload);
+  return sk::create_plan<sk_verify_plan>(params, out, [&](sk_verify_plan &plan, int32_t, int32_t, std::string &err) { return sk::plan_verify(problems, n, plan.host, err); }, upload);
 }
 
 sk_status sk_verify_plan_destroy(sk_verify_plan *plan) {

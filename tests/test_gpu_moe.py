@@ -42,6 +42,13 @@ def test_tenants():
         assert sk.sk_moe_plan_info(plan) == (0, 0)
 
 
+@pytest.mark.parametrize("workgroups", [1, 2, 3, 7, 50, 333, 2000])
+def test_shares_of_any_number_of_workgroups(workgroups):
+    """Tiles of the output that one workgroup has alone, that two share, and that many do."""
+    H.run_moe([H.Moe(rows=50, dim=200, ffn=72, experts=12, top_k=3, shared=136, seed=1), H.Moe(rows=3, dim=40, ffn=1032, experts=6, top_k=2, seed=2), H.Moe(rows=5, dim=64, used=0, seed=3),
+               H.Moe(rows=1, dim=16, ffn=4000, experts=40, top_k=20, gated=False, seed=4), H.Moe(rows=530, dim=32, ffn=8, experts=2, top_k=2, seed=5)], workgroups=workgroups)
+
+
 def test_equal_scores_go_to_the_lowest_number():
     m = H.Moe(rows=20, dim=64, experts=10, top_k=4, seed=3)
     m.router[5] = m.router[2]

@@ -76,7 +76,7 @@ def test_other_good_problems(kind, good, fields):
     (dict(router_stride=66), UNSUPPORTED), (dict(up_row_stride=66), UNSUPPORTED), (dict(down_expert_stride=64 * 32 + 4), UNSUPPORTED), (dict(x=BASE + 8), UNSUPPORTED), (dict(router=BASE + 2), UNSUPPORTED),
     (dict(gate=BASE + 4), UNSUPPORTED), (dict(shared_down=BASE + 8), UNSUPPORTED), (dict(out=(BASE << 1) + 2), UNSUPPORTED), (dict(expert_ids=BASE + 2), UNSUPPORTED), (dict(n_rows=BASE + 1), UNSUPPORTED),
     (dict(expert_ids=BASE << 1), OVERLAP), (dict(expert_weights=(BASE << 2) + 32), OVERLAP), (dict(x_stride=1 << 41), UNSUPPORTED), (dict(up_expert_stride=1 << 51), UNSUPPORTED),
-    (dict(dim=1 << 25), UNSUPPORTED), (dict(rows=2**31 - 1, experts=512, top_k=32), UNSUPPORTED),
+    (dict(dim=1 << 21), UNSUPPORTED), (dict(ffn=(1 << 24) + 8), UNSUPPORTED), (dict(x_stride=1 << 21), UNSUPPORTED), (dict(up_row_stride=1 << 26), UNSUPPORTED), (dict(down_row_stride=1 << 26), UNSUPPORTED), (dict(rows=2**31 - 1, experts=512, top_k=32), UNSUPPORTED),
 ]] + [("verify", VERIFY, f, s) for f, s in [
     (dict(dtype=-1), UNSUPPORTED), (dict(sequences=0), INVALID), (dict(rows=0), INVALID), (dict(vocab=0), INVALID), (dict(sequences=(1 << 20) + 1), UNSUPPORTED), (dict(vocab=(1 << 30) + 1), UNSUPPORTED),
     (dict(reserved=1), INVALID), (dict(first_row=0), INVALID), (dict(logits=0), INVALID), (dict(sample_random=0), INVALID), (dict(tokens=0), INVALID), (dict(accepted=0), INVALID),
