@@ -106,6 +106,7 @@ __device__ __forceinline__ int32_t lane_of(int32_t v, int lane) { return __built
 __device__ __forceinline__ int64_t lane_of(int64_t v, int lane) {
   return (int64_t)((uint64_t)(uint32_t)lane_of((int32_t)(v >> 32), lane) << 32 | (uint32_t)lane_of((int32_t)v, lane));
 }
+__device__ __forceinline__ double lane_of(double v, int lane) { return __builtin_bit_cast(double, lane_of(__builtin_bit_cast(int64_t, v), lane)); }
 // The larger (or the sum) of a lane's value and that of the lane 16, or 32, places away, without a trip through LDS.
 __device__ __forceinline__ void across16(float v, float &a, float &b) {
   const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);

@@ -13,6 +13,9 @@
 
 namespace sk {
 
+// Counters of arrivals stand a line of 128 bytes apart: atomics on one line go one after the other, across the whole card.
+constexpr int COUNTER_STEP = 32;
+
 // ---- norms -----------------------------------------------------------------------------------------------------------------
 
 // A problem as the kernel sees it (strides in elements), in the launch's arguments: a step's norms take a launch and two trips to memory, so a
@@ -91,7 +94,7 @@ struct MoeDev {
   MoeGroup *groups;       // [most_groups]; those of the shared expert last
   int64_t *first_begin, *second_begin;  // [most_groups]: where a group's work begins, among the first products and within a tile of the second ones
   MoeCount *count;
-  uint32_t *routed;       // counters: of units of the router per ROUTE_ROWS rows, of such blocks, of slices per tile of the output
+  uint32_t *routed;       // counters, COUNTER_STEP apart: of units of the router per ROUTE_ROWS rows, of such blocks, of slices per tile of the output
   uint32_t *blocks_routed, *summed;
   char *h;                // [rows * top_k + rows], h_stride bytes apart
   int64_t h_stride;
@@ -125,14 +128,25 @@ struct VerifyDev {
   int64_t logits_stride, draft_stride;  // bytes
   int32_t dtype, sequences, rows, vocab;
   float temperature;
-  int32_t pieces, chunks;  // a chunk is 2048 * pieces logits
+  int32_t pieces, chunks;  // a chunk is 512 * pieces logits
   VerifyStat *stats;       // [rows][2][chunks]
   double *sums;            // [sequences][chunks]
-  uint32_t *arrived;       // [sequences]
+  uint32_t *arrived;       // [sequences], COUNTER_STEP apart
+};
+// In the launch's arguments, as those of norms.
+constexpr int VERIFY_PROBLEMS = 16;  // of a launch
+struct VerifyArgs {
+  uint32_t stat_first[VERIFY_PROBLEMS], sum_first[VERIFY_PROBLEMS];  // workgroup of the two launches; none: the largest number
+  VerifyDev problems[VERIFY_PROBLEMS];
+};
+static_assert(sizeof(VerifyArgs) <= 4096, "kernel arguments");
+struct VerifyLaunch {
+  int32_t n;
+  int64_t stat_grid, sum_grid;
+  VerifyArgs args;  // workspace pointers: offsets until the plan is on the device
 };
 struct VerifyPlanHost {
-  std::vector<VerifyDev> problems;
-  std::vector<uint32_t> stat_first, sum_first;
+  std::vector<VerifyLaunch> launches;
   size_t workspace = 0, counters = 0;
 };
 

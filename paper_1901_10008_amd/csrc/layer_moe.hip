@@ -269,7 +269,7 @@ __global__ void __launch_bounds__(CACHE_THREADS) sk_moe_route(MoeArgs a) {
     if (P.dtype == SK_BF16) P.router_f32 ? route_scores<SK_BF16, true>(P, block, e0, lane) : route_scores<SK_BF16, false>(P, block, e0, lane);
     else P.router_f32 ? route_scores<SK_F16, true>(P, block, e0, lane) : route_scores<SK_F16, false>(P, block, e0, lane);
   }
-  if (!last_to_arrive(P.routed + block, by_experts, &flag)) return;
+  if (!last_to_arrive(P.routed + block * COUNTER_STEP, by_experts, &flag)) return;
   const int32_t row = block * ROUTE_ROWS + wave;
   int32_t *ids = blocks == 1 ? sorting.ids + row * P.top_k : nullptr;  // (then there are at most ROUTE_ROWS rows, and no other workgroup has any)
   float *weights = sorting.weights + row * P.top_k;
@@ -639,7 +639,7 @@ __device__ __forceinline__ void down_share(const MoeArgs &a, const SK_CONSTANT M
         store_shared(slice + 4 * k, f32x2{v[0], v[1]});
         store_shared(slice + 4 * k + 2, f32x2{v[2], v[3]});
       }
-      if (last_to_arrive(P.summed + tile, (int32_t)(last - first + 1), flag)) {
+      if (last_to_arrive(P.summed + (int64_t)tile * COUNTER_STEP, (int32_t)(last - first + 1), flag)) {
         for (int32_t k = tid; k < c.rows * 4; k += CACHE_THREADS) {
           f32x4 v = {0.f, 0.f, 0.f, 0.f};
           constexpr int AHEAD = 8;  // slices on their way at a time

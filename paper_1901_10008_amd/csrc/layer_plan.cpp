@@ -211,7 +211,7 @@ sk_status plan_moe(const sk_moe_problem *problems, int32_t n, int32_t compute_un
       out.route_first.push_back((uint32_t)route);
       most_rows = std::max(most_rows, rows);
       tiles += std::max(d.most_groups * (int64_t)d.down_tiles, routed_groups * d.up_tiles + shared_groups * d.shared_tiles);
-      counters.take(d.routed, blocks, 4), counters.take(d.blocks_routed, 1, 4), counters.take(d.summed, d.down_tiles, 4);
+      counters.take(d.routed, blocks * COUNTER_STEP), counters.take(d.blocks_routed, 1 * COUNTER_STEP), counters.take(d.summed, (int64_t)d.down_tiles * COUNTER_STEP);
       work.take(d.logits, rows * p.experts), work.take(d.ids, pairs), work.take(d.weights, pairs), work.take(d.row_of, pairs), work.take(d.weight_of, pairs);
       work.take(d.groups, d.most_groups), work.take(d.first_begin, d.most_groups), work.take(d.second_begin, d.most_groups);
       d.h_stride = (std::max<int64_t>(ffn, p.shared_ffn) + 63) / 64 * 128;
@@ -237,10 +237,11 @@ sk_status plan_moe(const sk_moe_problem *problems, int32_t n, int32_t compute_un
 
 // ---- verification ----------------------------------------------------------------------------------------------------------
 
+// Waves that the rows of a problem are cut for, where its chunks can still grow.
+constexpr int64_t VERIFY_WAVES = 6000;
+
 sk_status plan_verify(const sk_verify_problem *problems, int32_t n, VerifyPlanHost &out, std::string &err) {
   Spans written;
-  out.stat_first.assign(1, 0u), out.sum_first.assign(1, 0u);
-  int64_t stat = 0, sum = 0;
   Layout counters, work;
   const sk_status st = each(problems, n, err, [&](const sk_verify_problem &p) -> sk_status {
     if (!known(p.dtype)) return refuse(err, SK_ERR_UNSUPPORTED, "dtype must be SK_F32, SK_BF16 or SK_F16");
@@ -266,18 +267,26 @@ sk_status plan_verify(const sk_verify_problem *problems, int32_t n, VerifyPlanHo
     d.first_row = p.first_row, d.drafted = p.drafted, d.logits = (const char *)p.logits, d.draft_logits = p.drafted ? (const char *)p.draft_logits : nullptr;
     d.temperatures = p.temperatures, d.accept_random = p.accept_random, d.sample_random = p.sample_random, d.tokens = p.tokens, d.accepted = p.accepted;
     d.dtype = p.dtype, d.sequences = p.sequences, d.rows = p.rows, d.vocab = p.vocab, d.temperature = p.temperature;
-    // larger chunks where there are enough of them
+    // larger chunks where there are enough of them (of 32-bit logits up to four pieces: a lane keeps its part in registers)
+    const int64_t lines = (int64_t)p.rows * (d.draft_logits ? 2 : 1);
     d.pieces = 1;
-    while (d.pieces < 4 && (int64_t)p.rows * ((p.vocab + 4096 * d.pieces - 1) / (4096 * d.pieces)) >= 2048) d.pieces *= 2;
-    const int64_t chunk = 2048 * (int64_t)d.pieces;
+    while (d.pieces < (p.dtype == SK_F32 ? 4 : 8) && lines * ((p.vocab + 1024 * d.pieces - 1) / (1024 * d.pieces)) >= VERIFY_WAVES) d.pieces *= 2;
+    const int64_t chunk = 512 * (int64_t)d.pieces;
     d.chunks = (int32_t)((p.vocab + chunk - 1) / chunk);
-    stat += (int64_t)p.rows * (d.draft_logits ? 2 : 1) * d.chunks;
-    sum += (int64_t)p.sequences * d.chunks;
+    const int64_t stat = (lines * d.chunks + 3) / 4, sum = (int64_t)p.sequences * d.chunks;
     if (stat > MOST_GRID || sum > MOST_GRID) return refuse(err, SK_ERR_UNSUPPORTED, "more units of work than a launch's grid can hold");
-    out.stat_first.push_back((uint32_t)stat), out.sum_first.push_back((uint32_t)sum);
-    counters.take(d.arrived, p.sequences, 4);
+    counters.take(d.arrived, (int64_t)p.sequences * COUNTER_STEP);
     work.take(d.stats, (int64_t)p.rows * 2 * d.chunks), work.take(d.sums, (int64_t)p.sequences * d.chunks);
-    out.problems.push_back(d);
+    VerifyLaunch *l = out.launches.empty() ? nullptr : &out.launches.back();
+    if (!l || l->n == VERIFY_PROBLEMS || l->stat_grid + stat > MOST_GRID || l->sum_grid + sum > MOST_GRID) {
+      out.launches.emplace_back();
+      l = &out.launches.back();
+      l->n = 0, l->stat_grid = l->sum_grid = 0;
+      for (int i = 0; i < VERIFY_PROBLEMS; ++i) l->args.stat_first[i] = l->args.sum_first[i] = 0xffffffffu;
+    }
+    l->args.problems[l->n] = d;
+    l->args.stat_first[l->n] = (uint32_t)l->stat_grid, l->args.sum_first[l->n++] = (uint32_t)l->sum_grid;
+    l->stat_grid += stat, l->sum_grid += sum;
     return SK_OK;
   });
   if (st != SK_OK) return st;

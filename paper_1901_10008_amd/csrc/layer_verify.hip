@@ -4,18 +4,12 @@
 
 namespace sk {
 
-struct VerifyArgs {
-  const VerifyDev *problems;
-  const uint32_t *first;  // first workgroup of each problem
-  int32_t n;
-};
-
-// 2^t for t <= 0, 0 below 2^-1000, to 8e-13 of itself: 2^f of the rest f in [-1/2, 1/2] by the polynomial of degree 8 with the least largest relative
-// error, which moves a border between two tokens by less than one in 10^12 of the sum.  Fused multiplications and additions of 64 bits have the
-// rate of those of 32 here; there is no exponential of 64 bits in the hardware.  (t is a NaN where a logit is: the caller looks for those.)
-__device__ __forceinline__ double exp2_64(double t) {
-  const double shift = 6755399441055744.0;  // 1.5 * 2^52: t + shift has the nearest whole number of t in its lowest bits
-  const double moved = t + shift, f = t - (moved - shift);
+// 2^(d c) to 8e-13 of itself, for -1000 < d c <= 0: 2^f of what the nearest whole number leaves, |f| <= 1/2, by the polynomial of degree 8 with the least
+// largest relative error, which moves a border between two tokens by less than one in 10^12 of the sum.  Fused multiplications and additions of
+// 64 bits have the rate of those of 32 here; there is no exponential of 64 bits in the hardware.
+__device__ __forceinline__ double exp2_of(double d, double c) {
+  const double shift = 6755399441055744.0;  // 1.5 * 2^52: behind it, the nearest whole number stands in the lowest bits
+  const double moved = fma(d, c, shift), f = fma(d, c, shift - moved);
   double r = 1.3175858118613272e-06;
   r = fma(r, f, 1.530973742145504e-05);
   r = fma(r, f, 1.5403851748706403e-04);
@@ -25,116 +19,181 @@ __device__ __forceinline__ double exp2_64(double t) {
   r = fma(r, f, 2.4022650698880368e-01);
   r = fma(r, f, 6.931471805465141e-01);
   r = fma(r, f, 9.999999999997623e-01);
-  const uint64_t b = __builtin_bit_cast(uint64_t, r);
-  const uint32_t hi = (uint32_t)(b >> 32) + ((uint32_t)__builtin_bit_cast(uint64_t, moved) << 20);
-  return t > -1000.0 ? __builtin_bit_cast(double, (uint64_t)hi << 32 | (uint32_t)b) : 0.0;
+  u32x2 bits = __builtin_bit_cast(u32x2, r);
+  const u32x2 whole = __builtin_bit_cast(u32x2, moved);
+  bits[1] += (uint32_t)whole[0] << 20;
+  return __builtin_bit_cast(double, bits);
 }
+// The same, 0 below 2^-1000 (and for a NaN).
+__device__ __forceinline__ double weight_of(double d, double c) { return d * c > -1000.0 ? exp2_of(d, c) : 0.0; }
 
 // log2(e) / temperature of a sequence; 0: the first of the largest.
-__device__ __forceinline__ double scale_of(const SK_CONSTANT VerifyDev &P, int32_t seq) {
+__device__ __forceinline__ double scale_of(const VerifyDev &P, int32_t seq) {
   const float t = P.temperatures ? load_f(P.temperatures + seq) : P.temperature;
   return t > 0.f ? fmax(1.4426950408889634074 / (double)t, 1e-300) : 0.0;  // (not 0 where t is infinite)
 }
 __device__ __forceinline__ bool greedy(double c) { return c == 0.0; }
 
-// Eight logits from place `at` on, -infinity behind the last.
+// Eight logits of a row, as they come.  A lane wants those from place `at` on (the wave as a whole 512, from `wave_at` on); where they would end behind the
+// row it reads the row's last eight and has -infinity in place of those that belong to the lanes before it.  `first` is the place of the first.
 template <int DT>
-__device__ __forceinline__ void logits8(const char *row, int64_t at, int32_t vocab, float (&x)[8]) {
-  constexpr int S = DT == SK_F32 ? 4 : 2;
-  if (at + 8 <= vocab) {
-    load8<DT, false>(row + at * S, x);
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float v = load1<DT>(row + min(at + k, (int64_t)vocab - 1) * S);
-      x[k] = at + k < vocab ? v : -__builtin_inff();
-    }
-  }
-}
-
-struct VerifyShared {
-  double d[4];
-  float f[4];
-  int32_t i[4], any[4];
-};
-
-// A chunk of a row: its largest logit, and the sum of 2^((l - largest) * c).
-template <int DT>
-__device__ __forceinline__ void chunk_stat(const SK_CONSTANT VerifyDev &P, const char *row, int32_t chunk, double c, VerifyStat *out, VerifyShared &s, int tid) {
-  constexpr int P_MOST = 4;
-  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  float x[P_MOST][8];
-  const int64_t at0 = (int64_t)chunk * 2048 * P.pieces + tid * 8;
-#pragma unroll
-  for (int i = 0; i < P_MOST; ++i)
-    if (i < P.pieces) logits8<DT>(row, at0 + i * 2048, P.vocab, x[i]);
-  float top = -__builtin_inff();
-  bool bad = false;
-#pragma unroll
-  for (int i = 0; i < P_MOST; ++i)
-    if (i < P.pieces) {
+struct Eight {
+  static constexpr int S = DT == SK_F32 ? 4 : 2;
+  u32x4 raw[S / 2];
+  int32_t first;
+  // SHORT: rows may have fewer than eight
+  template <bool SHORT>
+  __device__ __forceinline__ void load(const char *row, int32_t wave_at, int lane, int32_t vocab) {
+    constexpr uint32_t lowest = DT == SK_F32 ? 0xff800000u : DT == SK_BF16 ? 0xff80u : 0xfc00u;
+    const int32_t at = wave_at + 8 * lane;
+    uint32_t e[8];
+    if (SHORT && vocab < 8) {
+      first = 0;
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        top = fmaxf(top, x[i][k]);
-        bad |= !(x[i][k] < __builtin_inff());
+        const char *p = row + min(k, vocab - 1) * S;
+        e[k] = DT == SK_F32 ? *(const uint32_t SK_GLOBAL *)(uintptr_t)p : load_u16(p);
+        e[k] = at == 0 && k < vocab ? e[k] : lowest;
       }
+      pack(e);
+      return;
     }
-  top = wave_max(top);
-  const bool any_bad = __ballot(bad) != 0;
-  if (lane == 0) s.f[wave] = top, s.any[wave] = any_bad;
-  __syncthreads();
-  top = fmaxf(fmaxf(s.f[0], s.f[1]), fmaxf(s.f[2], s.f[3]));
-  double sum = 0.0;
-  int32_t at = 0x7fffffff;
-  if (greedy(c)) {
+    first = min(at, vocab - 8);
 #pragma unroll
-    for (int i = 0; i < P_MOST; ++i)
-      if (i < P.pieces) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (x[i][k] == top) at = min(at, (int32_t)(at0 + i * 2048) + k);
-      }
-    at = wave_min(at);
-    sum = 1.0;
-  } else if (top > -__builtin_inff()) {
-    const double m = (double)top;
-#pragma unroll
-    for (int i = 0; i < P_MOST; ++i)
-      if (i < P.pieces) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) sum += exp2_64(((double)x[i][k] - m) * c);
-      }
-    sum = wave_sum(sum);
+    for (int i = 0; i < S / 2; ++i) raw[i] = *(const u32x4_any SK_GLOBAL *)(uintptr_t)(row + (int64_t)first * S + 16 * i);
   }
-  if (lane == 0) s.d[wave] = sum, s.i[wave] = at;
-  __syncthreads();
-  if (tid == 0) {
-    const bool not_one = s.any[0] | s.any[1] | s.any[2] | s.any[3];
-    *out = VerifyStat{not_one ? __builtin_nan("") : greedy(c) ? 1.0 : (s.d[0] + s.d[1]) + (s.d[2] + s.d[3]), top, min(min(s.i[0], s.i[1]), min(s.i[2], s.i[3]))};
+  // Behind all loads: -infinity for what belongs to other lanes.
+  __device__ __forceinline__ void cut(int32_t wave_at, int lane, int32_t vocab) {
+    if (wave_at + 512 <= vocab || vocab < 8) return;  // (the same in all lanes)
+    constexpr uint32_t lowest = DT == SK_F32 ? 0xff800000u : DT == SK_BF16 ? 0xff80u : 0xfc00u;
+    const int32_t others = wave_at + 8 * lane - first;
+    uint32_t e[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      e[k] = DT == SK_F32 ? raw[S == 4 ? k / 4 : 0][k % 4] : (k & 1 ? raw[0][k / 2] >> 16 : raw[0][k / 2] & 0xffffu);
+      e[k] = k < others ? lowest : e[k];
+    }
+    pack(e);
   }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+    if constexpr (DT == SK_F32) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = __builtin_bit_cast(float, (uint32_t)raw[k / 4][k % 4]);
+    } else {
+      unpack8<DT>(raw[0], x);
+    }
+  }
+
+ private:
+  __device__ __forceinline__ void pack(const uint32_t (&e)[8]) {
+    if constexpr (DT == SK_F32) raw[0] = u32x4{e[0], e[1], e[2], e[3]}, raw[1] = u32x4{e[4], e[5], e[6], e[7]};
+    else raw[0] = u32x4{e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16};
+  }
+};
+
+struct VerifyShared {
+  double begin, bound, piece[8];
+  int32_t chunk, found;
+};
+
+__device__ __forceinline__ int32_t first_of(const VerifyDev &P, int32_t s) { return min(max(load_i32(P.first_row + s), 0), P.rows); }
+
+// The sequence that a row belongs to; none: rows of no sequence, and of sequences whose numbers of rows make no sense.
+struct Owner {
+  int32_t seq, begin, end;
+};
+__device__ __forceinline__ Owner owner_of(const VerifyDev &P, int32_t row, int lane) {
+  Owner o;
+  if (P.sequences <= 64) {  // a sequence a lane
+    const int32_t s = min(lane, P.sequences - 1), begin = first_of(P, s), end = first_of(P, s + 1);
+    o.seq = max(1, (int32_t)__popcll(__ballot(lane < P.sequences && begin <= row))) - 1;
+    o.begin = lane_of(begin, o.seq), o.end = lane_of(end, o.seq);
+  } else {
+    o.seq = __builtin_amdgcn_readfirstlane(last_not_above(P.first_row, P.sequences, row, lane));
+    o.begin = first_of(P, o.seq), o.end = first_of(P, o.seq + 1);
+  }
+  return o;
 }
 
-__device__ __forceinline__ int32_t first_of(const SK_CONSTANT VerifyDev &P, int32_t s) { return min(max(load_i32(P.first_row + s), 0), P.rows); }
+// A chunk of a row, 512 * PIECES logits, by a wave: a lane has eight of each piece, takes them relative to its own largest, and the lanes are joined at
+// the end.  Bound by the vector unit (17 instructions a logit, 16-bit logits) about as much as by memory.
+template <int DT, int PIECES>
+__device__ __forceinline__ void chunk_stat(const VerifyDev &P, const char *from, int32_t chunk, double c, VerifyStat *out, int lane) {
+  Eight<DT> raw[PIECES];
+  const int32_t at0 = chunk * 512 * PIECES;
+#pragma unroll
+  for (int i = 0; i < PIECES; ++i) raw[i].template load<PIECES == 1>(from, at0 + i * 512, lane, P.vocab);
+#pragma unroll
+  for (int i = 0; i < PIECES; ++i) raw[i].cut(at0 + i * 512, lane, P.vocab);
+  float top = -__builtin_inff();
+#pragma unroll
+  for (int i = 0; i < PIECES; ++i) {
+    float x[8];
+    raw[i].get(x);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) top = __builtin_elementwise_maximum(top, x[k]);  // (a NaN, once there, stays)
+  }
+  VerifyStat r{0.0, wave_max(top), 0x7fffffff};
+  if (__ballot(!(top < __builtin_inff()))) {
+    r.sum = __builtin_nan("");
+  } else if (greedy(c)) {
+    r.sum = 1.0;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      float x[8];
+      raw[i].get(x);
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (x[k] == r.top) r.at = min(r.at, raw[i].first + k);
+    }
+    r.at = wave_min(r.at);
+  } else if (r.top > -__builtin_inff()) {
+    const double m = (double)fmaxf(top, -3.4e38f);  // (a lane may have nothing but -infinity: it stays behind all others)
+    const double lowest = -990.0 / c;  // what is further below counts as this, for 10^-298
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      float x[8];
+      raw[i].get(x);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        if (k % 4 == 0) __builtin_amdgcn_sched_barrier(0);  // (four at a time: more would take the registers of waves)
+        sum += exp2_of(fmax((double)x[k] - m, lowest), c);
+      }
+    }
+    r.sum = wave_sum(top > -__builtin_inff() ? sum * weight_of(m - (double)r.top, c) : 0.0);
+  }
+  if (lane == 0) *out = r;
+}
 
-__global__ void __launch_bounds__(CACHE_THREADS) sk_verify_stats(VerifyArgs a) {
-  __shared__ VerifyShared shared;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int32_t problem = __builtin_amdgcn_readfirstlane(last_not_above(a.first, a.n, (int64_t)blockIdx.x, lane));
-  const SK_CONSTANT VerifyDev &P = *(const SK_CONSTANT VerifyDev *)(uintptr_t)(a.problems + problem);
-  const uint32_t unit = blockIdx.x - ((const SK_CONSTANT uint32_t *)(uintptr_t)a.first)[problem];
+template <int DT>
+__device__ __forceinline__ void row_chunk(const VerifyDev &P, uint32_t unit, int lane) {
   const uint32_t sides = P.draft_logits ? 2 : 1, line = unit / (uint32_t)P.chunks;
   const int32_t chunk = (int32_t)(unit - line * (uint32_t)P.chunks), row = (int32_t)(line / sides);
   const bool draft = sides == 2 && (line & 1);
-  const int32_t seq = __builtin_amdgcn_readfirstlane(last_not_above(P.first_row, P.sequences, row, lane));
-  const int32_t r0 = first_of(P, seq), r1 = first_of(P, seq + 1);
-  if (row < r0 || row >= r1 || (draft && row == r1 - 1)) return;
-  const double c = scale_of(P, seq);
-  if (draft && greedy(c)) return;
-  const char *at = draft ? P.draft_logits + row * P.draft_stride : P.logits + row * P.logits_stride;
+  if (row >= P.rows) return;
+  const Owner o = owner_of(P, row, lane);
+  if (row < o.begin || row >= o.end) return;
+  const double c = scale_of(P, o.seq);
+  if (draft && (row == o.end - 1 || greedy(c))) return;
+  const char *from = draft ? P.draft_logits + row * P.draft_stride : P.logits + row * P.logits_stride;
   VerifyStat *out = P.stats + ((int64_t)row * 2 + draft) * P.chunks + chunk;
-  if (P.dtype == SK_F32) chunk_stat<SK_F32>(P, at, chunk, c, out, shared, tid);
-  else if (P.dtype == SK_BF16) chunk_stat<SK_BF16>(P, at, chunk, c, out, shared, tid);
-  else chunk_stat<SK_F16>(P, at, chunk, c, out, shared, tid);
+  if (P.pieces == 1) chunk_stat<DT, 1>(P, from, chunk, c, out, lane);
+  else if (P.pieces == 2) chunk_stat<DT, 2>(P, from, chunk, c, out, lane);
+  else if (DT == SK_F32 || P.pieces == 4) chunk_stat<DT, 4>(P, from, chunk, c, out, lane);
+  else chunk_stat<DT, 8>(P, from, chunk, c, out, lane);
+}
+
+__global__ void __launch_bounds__(CACHE_THREADS, 5) sk_verify_stats(VerifyArgs a) {
+  int i = 0;
+#pragma unroll
+  for (int k = 1; k < VERIFY_PROBLEMS; ++k) i += a.stat_first[k] <= blockIdx.x ? 1 : 0;
+  const VerifyDev &P = a.problems[i];
+  const uint32_t unit = (blockIdx.x - a.stat_first[i]) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  if (P.dtype == SK_F32) row_chunk<SK_F32>(P, unit, lane);
+  else if (P.dtype == SK_BF16) row_chunk<SK_BF16>(P, unit, lane);
+  else row_chunk<SK_F16>(P, unit, lane);
 }
 
 // A row's distribution from its chunks, by a wave: p(k) = 2^((l_k - top) * c) / sum.  sum 0: it has none.
@@ -142,10 +201,14 @@ struct Row {
   double top, sum;
   int32_t at;  // (temperature 0) the only token
 };
-__device__ __forceinline__ Row row_stat(const VerifyStat *stats, int32_t chunks, double c, int lane) {
-  float top = -__builtin_inff();
-  bool bad = false;
-  for (int32_t i = lane; i < chunks; i += 64) {
+__device__ __forceinline__ VerifyStat stat_of(const VerifyStat *stats, int32_t chunks, int32_t i) {
+  return i < chunks ? stats[i] : VerifyStat{0.0, -__builtin_inff(), 0x7fffffff};
+}
+// own: this lane's chunk of the first 64.
+__device__ __forceinline__ Row row_stat(const VerifyStat &own, const VerifyStat *stats, int32_t chunks, double c, int lane) {
+  float top = own.top;
+  bool bad = own.sum != own.sum;
+  for (int32_t i = 64 + lane; i < chunks; i += 64) {
     top = fmaxf(top, stats[i].top);
     bad |= stats[i].sum != stats[i].sum;
   }
@@ -153,19 +216,15 @@ __device__ __forceinline__ Row row_stat(const VerifyStat *stats, int32_t chunks,
   Row r{(double)top, 0.0, -1};
   if (__ballot(bad) || !(top > -__builtin_inff())) return r;
   int32_t at = 0x7fffffff;
-  for (int32_t i = lane; i < chunks; i += 64) {
-    const double scale = exp2_64(((double)stats[i].top - r.top) * c);
-    r.sum += stats[i].top > -__builtin_inff() ? stats[i].sum * scale : 0.0;
-    if (stats[i].top == top) at = min(at, stats[i].at);
-  }
+  auto add = [&](const VerifyStat &s) {
+    r.sum += s.top > -__builtin_inff() ? s.sum * weight_of((double)s.top - r.top, c) : 0.0;
+    if (s.top == top) at = min(at, s.at);
+  };
+  add(own);
+  for (int32_t i = 64 + lane; i < chunks; i += 64) add(stats[i]);
   r.sum = wave_sum(r.sum);
-  r.at = wave_min(at);
+  r.at = greedy(c) ? wave_min(at) : -1;
   return r;
-}
-
-template <int DT>
-__device__ __forceinline__ double logit(const char *row, int32_t at) {
-  return (double)load1<DT>(row + (int64_t)at * (DT == SK_F32 ? 4 : 2));
 }
 
 // What the sampled token of a sequence is drawn from.
@@ -175,114 +234,141 @@ struct Draw {
   Row p, q;
 };
 
+// max(p / p_sum - q / q_sum, 0), times both sums.  Two rounded products: where p and q are the same, so are they, and nothing is left.
+__device__ __forceinline__ double difference(double p, double q_sum, double q, double p_sum) {
+#pragma clang fp contract(off)
+  const double a = p * q_sum, b = q * p_sum;
+  return fmax(a - b, 0.0);
+}
+
 // Weights of eight tokens.
 template <int DT>
-__device__ __forceinline__ void weights8(const SK_CONSTANT VerifyDev &P, const Draw &d, const char *p_row, const char *q_row, int64_t at, double c, double (&w)[8]) {
+__device__ __forceinline__ void weights8(const Draw &d, const Eight<DT> &p, const Eight<DT> &q, double c, double (&w)[8]) {
   float x[8], y[8];
-  logits8<DT>(p_row, at, P.vocab, x);
-  if (d.mode == FROM_DIFFERENCE) logits8<DT>(q_row, at, P.vocab, y);
+  p.get(x);
+  q.get(y);
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
-    w[k] = exp2_64(((double)x[k] - d.p.top) * c);
-    if (d.mode == FROM_DIFFERENCE) w[k] = fmax(w[k] / d.p.sum - exp2_64(((double)y[k] - d.q.top) * c) / d.q.sum, 0.0);
-    if (d.mode == FROM_OTHERS && at + k == d.token) w[k] = 0.0;
+    w[k] = weight_of((double)x[k] - d.p.top, c);
+    if (d.mode == FROM_DIFFERENCE) w[k] = difference(w[k], d.q.sum, weight_of((double)y[k] - d.q.top, c), d.p.sum);
+    if (d.mode == FROM_OTHERS && p.first + k == d.token) w[k] = 0.0;
   }
 }
 
-// The sum of a chunk's weights, in all threads.
+// The weights of a chunk, by a workgroup: a wave has two of its eight pieces, whose sums go to LDS.  Returns the chunk's sum.
 template <int DT>
-__device__ __forceinline__ double chunk_sum(const SK_CONSTANT VerifyDev &P, const Draw &d, const char *p_row, const char *q_row, int32_t chunk, double c, VerifyShared &s, int tid) {
-  double sum = 0.0;
-  for (int32_t i = 0; i < P.pieces; ++i) {
-    const int64_t at = ((int64_t)chunk * P.pieces + i) * 2048 + tid * 8;
-    if (at >= P.vocab) break;
-    double w[8];
-    weights8<DT>(P, d, p_row, q_row, at, c, w);
+__device__ __forceinline__ double chunk_weights(const VerifyDev &P, const Draw &d, const char *p_row, const char *q_row, int32_t chunk, double c, double (&w)[2][8], int32_t (&places)[2],
+                                                VerifyShared &s, int tid) {
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const char *other = d.mode == FROM_DIFFERENCE ? q_row : p_row;
+  Eight<DT> p[2], q[2];
+  int32_t at[2];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) sum += w[k];
+  for (int j = 0; j < 2; ++j) {
+    const int32_t i = wave + 4 * j;
+    at[j] = i < P.pieces ? (chunk * P.pieces + i) * 512 : P.vocab;
+    if (at[j] >= P.vocab) continue;  // (the same in all lanes)
+    p[j].template load<true>(p_row, at[j], lane, P.vocab);
+    q[j].template load<true>(other, at[j], lane, P.vocab);
   }
-  sum = wave_sum(sum);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    double sum = 0.0;
+    places[j] = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w[j][k] = 0.0;
+    if (at[j] < P.vocab) {
+      p[j].cut(at[j], lane, P.vocab);
+      q[j].cut(at[j], lane, P.vocab);
+      weights8<DT>(d, p[j], q[j], c, w[j]);
+      places[j] = p[j].first;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) sum += w[j][k];
+      sum = wave_sum(sum);
+    }
+    if (lane == 0) s.piece[wave + 4 * j] = sum;
+  }
   __syncthreads();
-  if ((tid & 63) == 0) s.d[tid >> 6] = sum;
-  __syncthreads();
-  return (s.d[0] + s.d[1]) + (s.d[2] + s.d[3]);
+  double all = 0.0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) all += s.piece[i];
+  return all;
 }
 
-// The first token whose weight and those before it add up to more than `random` times all.  sum_of(i) is the sum of chunk i (asked for by the first
-// wave).  -1: all weights are 0.
+// The first token whose weight and those before it add up to more than `random` times all, by a workgroup.  sum_of(i) is the sum of chunk i (asked for
+// by the first wave).  -1: all weights are 0.
 template <int DT, class F>
-__device__ __forceinline__ int32_t pick(const SK_CONSTANT VerifyDev &P, const Draw &d, const char *p_row, const char *q_row, double c, double random, F sum_of, VerifyShared &s, int tid) {
+__device__ __forceinline__ int32_t pick(const VerifyDev &P, const Draw &d, const char *p_row, const char *q_row, double c, double random, F sum_of, VerifyShared &s, int tid) {
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   __syncthreads();
   if (wave == 0) {
+    const double own = lane < P.chunks ? sum_of(lane) : 0.0;  // of the first 64 chunks
+    auto value = [&](int32_t i0) { return i0 == 0 ? own : i0 + lane < P.chunks ? sum_of(i0 + lane) : 0.0; };
     double total = 0.0;
     int32_t last = -1;
     for (int32_t i0 = 0; i0 < P.chunks; i0 += 64) {
-      const double v = i0 + lane < P.chunks ? sum_of(i0 + lane) : 0.0;
+      const double v = value(i0);
       const uint64_t some = __ballot(v > 0.0);
       if (some) last = i0 + 63 - (int)__builtin_clzll(some);
-      const double upto = total + wave_scan(v);
-      total = __shfl(upto, 63);
+      total = lane_of(total + wave_scan(v), 63);
     }
     const double bound = random * total;
-    double before = 0.0, begin = 0.0, all = 0.0;
+    double begin = 0.0, all = 0.0;
     int32_t chunk = -1;
     for (int32_t i0 = 0; i0 < P.chunks && chunk < 0; i0 += 64) {
-      const double v = i0 + lane < P.chunks ? sum_of(i0 + lane) : 0.0;
-      const double upto = all + wave_scan(v);
+      const double v = value(i0), upto = all + wave_scan(v);
       const uint64_t past = __ballot(upto > bound && v > 0.0);
-      const int l = past ? (int)__builtin_ctzll(past) : 0;
-      const double below = __shfl_up(upto, 1);
-      before = lane == 0 ? all : below;
-      if (past) chunk = i0 + l, begin = __shfl(before, l);
-      all = __shfl(upto, 63);
+      if (past) {
+        const int l = (int)__builtin_ctzll(past);
+        chunk = i0 + l;
+        begin = l ? lane_of(upto, l - 1) : all;
+      }
+      all = lane_of(upto, 63);
     }
-    if (chunk < 0) chunk = last, begin = -1.0;  // (rounding: the last token with a weight)
-    if (lane == 0) s.d[0] = begin, s.d[1] = bound, s.i[0] = chunk;
+    if (lane == 0) s.begin = begin, s.bound = chunk < 0 ? __builtin_inf() : bound, s.chunk = chunk < 0 ? last : chunk;  // (rounding: the last token with a weight)
   }
   __syncthreads();
-  const double bound = s.d[1];
-  double begin = s.d[0];
-  const int32_t chunk = s.i[0];
+  const double bound = s.bound;
+  const int32_t chunk = s.chunk;
   if (chunk < 0) return -1;
-  const bool none = begin < 0.0;
-  int32_t last = -1;
-  for (int32_t i = 0; i < P.pieces; ++i) {
-    const int64_t at = ((int64_t)chunk * P.pieces + i) * 2048 + tid * 8;
-    double w[8] = {}, mine = 0.0;
-    if (at < P.vocab) weights8<DT>(P, d, p_row, q_row, at, c, w);
-    int32_t my_last = -1;
+  double w[2][8];
+  int32_t places[2];
+  if (tid == 0) s.found = -1;
+  chunk_weights<DT>(P, d, p_row, q_row, chunk, c, w, places, s, tid);
+  // the piece that passes the bound, or the last with a weight
+  double begin = s.begin, at_begin = 0.0;
+  int32_t piece = -1;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const double sum = s.piece[i];
+    if (sum > 0.0 && (piece < 0 || !(at_begin + s.piece[piece] > bound))) piece = i, at_begin = begin;
+    begin += sum;
+  }
+  if (piece < 0) return -1;  // (not where the chunk has a weight)
+  if (piece % 4 == wave) {
+    double mine[8], upto = 0.0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) mine[k] = piece >= 4 ? w[1][k] : w[0][k], upto += mine[k];
+    const double scanned = wave_scan(upto);
+    const uint32_t lo = (uint32_t)__builtin_bit_cast(uint64_t, scanned), hi = (uint32_t)(__builtin_bit_cast(uint64_t, scanned) >> 32);
+    const uint64_t below = (uint64_t)(uint32_t)__shfl_up((int)hi, 1) << 32 | (uint32_t)__shfl_up((int)lo, 1);
+    double sum = at_begin + (lane ? __builtin_bit_cast(double, below) : 0.0);
+    const int32_t at = piece >= 4 ? places[1] : places[0];
+    int32_t found = 0x7fffffff, last = -1;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      mine += w[k];
-      if (w[k] > 0.0) my_last = (int32_t)at + k;
-    }
-    const double upto = wave_scan(mine);
-    __syncthreads();
-    if (lane == 63) s.d[wave] = upto;
-    __syncthreads();
-    double sum = begin + (wave > 0 ? s.d[0] : 0.0) + (wave > 1 ? s.d[1] : 0.0) + (wave > 2 ? s.d[2] : 0.0);
-    begin += (s.d[0] + s.d[1]) + (s.d[2] + s.d[3]);
-    const double below = __shfl_up(upto, 1);
-    sum += lane ? below : 0.0;
-    int32_t found = 0x7fffffff;
-#pragma unroll
-    for (int k = 7; k >= 0; --k) {
-      double upto_k = sum;
-#pragma unroll
-      for (int j = 0; j <= k; ++j) upto_k += w[j];
-      if (!none && upto_k > bound && w[k] > 0.0) found = (int32_t)at + k;
+      sum += mine[k];
+      if (mine[k] > 0.0) {
+        if (sum > bound) found = min(found, at + k);
+        last = at + k;
+      }
     }
     found = wave_min(found);
-    my_last = -wave_min(-my_last);
-    if (lane == 0) s.i[wave] = found, s.any[wave] = my_last;
-    __syncthreads();
-    found = min(min(s.i[0], s.i[1]), min(s.i[2], s.i[3]));
-    last = max(last, max(max(s.any[0], s.any[1]), max(s.any[2], s.any[3])));
-    __syncthreads();
-    if (found != 0x7fffffff) return found;
+    last = -wave_min(-last);
+    if (lane == 0) s.found = found != 0x7fffffff ? found : last;
   }
-  return last;
+  __syncthreads();
+  return s.found;
 }
 
 __device__ __forceinline__ double random_of(const float *p) {
@@ -292,7 +378,7 @@ __device__ __forceinline__ double random_of(const float *p) {
 
 // What becomes of a sequence's drafts: by all waves, a row each at a time.
 template <int DT>
-__device__ __forceinline__ void decide(const SK_CONSTANT VerifyDev &P, int32_t r0, int32_t n, double c, Draw *draws, int32_t *stop, int tid, Draw &out) {
+__device__ __forceinline__ void decide(const VerifyDev &P, int32_t r0, int32_t n, double c, Draw *draws, int32_t *stop, int tid, Draw &out) {
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   if (tid == 0) *stop = 0x7fffffff;
   __syncthreads();
@@ -300,25 +386,33 @@ __device__ __forceinline__ void decide(const SK_CONSTANT VerifyDev &P, int32_t r
     const int32_t i = i0 + wave;
     if (i < n) {
       const int64_t row = r0 + i;
+      const bool judged = i < n - 1 && P.drafted, two = judged && P.draft_logits && !greedy(c);
+      const int32_t token = judged ? load_i32(P.drafted + row) : -1;
+      const double random = judged ? random_of(P.accept_random + row) : 0.0;
+      const VerifyStat *p_stats = P.stats + row * 2 * P.chunks, *q_stats = p_stats + P.chunks;
+      const VerifyStat p_own = stat_of(p_stats, P.chunks, lane), q_own = stat_of(q_stats, two ? P.chunks : 0, lane);
+      const bool known = token >= 0 && token < P.vocab;
+      constexpr int S = DT == SK_F32 ? 4 : 2;
+      const double p_logit = known ? (double)load1<DT>(P.logits + row * P.logits_stride + (int64_t)token * S) : 0.0;
+      const double q_logit = known && two ? (double)load1<DT>(P.draft_logits + row * P.draft_stride + (int64_t)token * S) : 0.0;
       Draw d{};
       d.stop = i, d.token = -1;
-      d.p = row_stat(P.stats + row * 2 * P.chunks, P.chunks, c, lane);
+      d.p = row_stat(p_own, p_stats, P.chunks, c, lane);
       bool accept = false;
       if (!(d.p.sum > 0.0)) {
         d.mode = FROM_NOTHING;
       } else {
         d.mode = greedy(c) ? FROM_ONE : FROM_TARGET;
-        const int32_t token = i < n - 1 && P.drafted ? load_i32(P.drafted + row) : -1;
-        if (token >= 0 && token < P.vocab) {
+        if (known) {
           double q = 1.0;
-          bool certain = greedy(c) || !P.draft_logits;
-          if (!certain) {
-            d.q = row_stat(P.stats + (row * 2 + 1) * P.chunks, P.chunks, c, lane);
+          bool certain = !two;
+          if (two) {
+            d.q = row_stat(q_own, q_stats, P.chunks, c, lane);
             certain = !(d.q.sum > 0.0);
-            if (!certain) q = exp2_64((logit<DT>(P.draft_logits + row * P.draft_stride, token) - d.q.top) * c) / d.q.sum;
+            if (!certain) q = weight_of(q_logit - d.q.top, c) / d.q.sum;
           }
-          const double p = greedy(c) ? (token == d.p.at ? 1.0 : 0.0) : exp2_64((logit<DT>(P.logits + row * P.logits_stride, token) - d.p.top) * c) / d.p.sum;
-          accept = random_of(P.accept_random + row) * q < p;
+          const double p = greedy(c) ? (token == d.p.at ? 1.0 : 0.0) : weight_of(p_logit - d.p.top, c) / d.p.sum;
+          accept = random * q < p;
           if (!greedy(c)) d.mode = certain ? FROM_OTHERS : FROM_DIFFERENCE;
           d.token = token;
         }
@@ -340,7 +434,7 @@ __device__ __forceinline__ void decide(const SK_CONSTANT VerifyDev &P, int32_t r
 }
 
 template <int DT>
-__device__ __forceinline__ void sample(const SK_CONSTANT VerifyDev &P, int32_t seq, int32_t chunk, VerifyShared &s, Draw *draws, int32_t *stop, uint32_t *flag, int tid) {
+__device__ __forceinline__ void sample(const VerifyDev &P, int32_t seq, int32_t chunk, VerifyShared &s, Draw *draws, int32_t *stop, uint32_t *flag, int tid) {
   const int32_t r0 = first_of(P, seq), n = first_of(P, seq + 1) - r0;
   if (n <= 0) {
     if (chunk == 0 && tid == 0) P.accepted[seq] = 0;
@@ -352,19 +446,21 @@ __device__ __forceinline__ void sample(const SK_CONSTANT VerifyDev &P, int32_t s
   const char *p_row = P.logits + (int64_t)(r0 + d.stop) * P.logits_stride, *q_row = d.mode == FROM_DIFFERENCE ? P.draft_logits + (int64_t)(r0 + d.stop) * P.draft_stride : nullptr;
   const double random = random_of(P.sample_random + seq);
   const VerifyStat *stats = P.stats + (int64_t)(r0 + d.stop) * 2 * P.chunks;
-  auto from_stats = [&](int32_t i) { return stats[i].top > -__builtin_inff() ? stats[i].sum * exp2_64(((double)stats[i].top - d.p.top) * c) : 0.0; };
+  auto from_stats = [&](int32_t i) { return stats[i].top > -__builtin_inff() ? stats[i].sum * weight_of((double)stats[i].top - d.p.top, c) : 0.0; };
   int32_t token = -1;
-  if (d.mode == FROM_DIFFERENCE) {
+  double w[2][8];
+  int32_t places[2];
+  if (d.mode == FROM_DIFFERENCE) {  // a chunk a workgroup
     double *sums = P.sums + (int64_t)seq * P.chunks;
-    const double sum = chunk_sum<DT>(P, d, p_row, q_row, chunk, c, s, tid);
+    const double sum = chunk_weights<DT>(P, d, p_row, q_row, chunk, c, w, places, s, tid);
     if (tid == 0) put(sums + chunk, sum);
-    if (!last_to_arrive(P.arrived + seq, P.chunks, flag)) return;
+    if (!last_to_arrive(P.arrived + (int64_t)seq * COUNTER_STEP, P.chunks, flag)) return;
     token = pick<DT>(P, d, p_row, q_row, c, random, [&](int32_t i) { return got(sums + i); }, s, tid);
   } else if (chunk != 0) {
     return;
   } else if (d.mode == FROM_OTHERS) {
-    const int32_t without = d.token / (2048 * P.pieces);
-    const double rest = chunk_sum<DT>(P, d, p_row, q_row, without, c, s, tid);
+    const int32_t without = d.token / (512 * P.pieces);
+    const double rest = chunk_weights<DT>(P, d, p_row, q_row, without, c, w, places, s, tid);
     token = pick<DT>(P, d, p_row, q_row, c, random, [&](int32_t i) { return i == without ? rest : from_stats(i); }, s, tid);
   }
   if (d.mode == FROM_ONE) token = d.token;
@@ -376,15 +472,17 @@ __device__ __forceinline__ void sample(const SK_CONSTANT VerifyDev &P, int32_t s
   if (tid == 0) P.accepted[seq] = d.stop;
 }
 
-__global__ void __launch_bounds__(CACHE_THREADS) sk_verify_sample(VerifyArgs a) {
+__global__ void __launch_bounds__(CACHE_THREADS, 4) sk_verify_sample(VerifyArgs a) {
   __shared__ VerifyShared shared;
   __shared__ Draw draws[4];
   __shared__ int32_t stop;
   __shared__ uint32_t flag;
   const int tid = threadIdx.x;
-  const int32_t problem = __builtin_amdgcn_readfirstlane(last_not_above(a.first, a.n, (int64_t)blockIdx.x, tid & 63));
-  const SK_CONSTANT VerifyDev &P = *(const SK_CONSTANT VerifyDev *)(uintptr_t)(a.problems + problem);
-  const uint32_t unit = blockIdx.x - ((const SK_CONSTANT uint32_t *)(uintptr_t)a.first)[problem];
+  int i = 0;
+#pragma unroll
+  for (int k = 1; k < VERIFY_PROBLEMS; ++k) i += a.sum_first[k] <= blockIdx.x ? 1 : 0;
+  const VerifyDev &P = a.problems[i];
+  const uint32_t unit = blockIdx.x - a.sum_first[i];
   const int32_t seq = (int32_t)(unit / (uint32_t)P.chunks), chunk = (int32_t)(unit % (uint32_t)P.chunks);
   if (P.dtype == SK_F32) sample<SK_F32>(P, seq, chunk, shared, draws, &stop, &flag, tid);
   else if (P.dtype == SK_BF16) sample<SK_BF16>(P, seq, chunk, shared, draws, &stop, &flag, tid);
@@ -395,32 +493,24 @@ __global__ void __launch_bounds__(CACHE_THREADS) sk_verify_sample(VerifyArgs a) 
 
 struct sk_verify_plan : sk::PlanOnDevice {
   sk::VerifyPlanHost host;
-  const sk::VerifyDev *problems = nullptr;
-  const uint32_t *first[2] = {};
 };
 
 namespace {
 
+// (the problems travel in the launches' arguments; on the device are the counters and the workspace)
 sk_status upload(sk_verify_plan &plan) {
   sk::VerifyPlanHost &h = plan.host;
-  const std::vector<uint32_t> *firsts[2] = {&h.stat_first, &h.sum_first};
-  // counters, problems, first workgroups
-  const size_t o_problems = sk::align_up(h.counters, 256);
-  size_t o_first[3] = {o_problems + sk::align_up(h.problems.size() * sizeof(sk::VerifyDev), 256)};
-  for (int i = 0; i < 2; ++i) o_first[i + 1] = o_first[i] + sk::align_up(firsts[i]->size() * 4, 256);
-  std::vector<char> image(o_first[2], 0);
+  if (h.launches.empty()) return SK_OK;
+  const std::vector<char> image(h.counters, 0);
   char *ws = nullptr;
   const sk_status st = sk::upload_image(plan, image, h.workspace, &ws);
   if (st != SK_OK) return st;
   auto moved = [](auto *&p, char *base) { p = (std::decay_t<decltype(p)>)(base + (uintptr_t)p); };
-  std::vector<sk::VerifyDev> problems = h.problems;
-  for (sk::VerifyDev &d : problems) moved(d.arrived, plan.blob), moved(d.stats, ws), moved(d.sums, ws);
-  if (!problems.empty()) std::memcpy(image.data() + o_problems, problems.data(), problems.size() * sizeof(sk::VerifyDev));
-  for (int i = 0; i < 2; ++i) {
-    std::memcpy(image.data() + o_first[i], firsts[i]->data(), firsts[i]->size() * 4);
-    plan.first[i] = (const uint32_t *)(plan.blob + o_first[i]);
-  }
-  plan.problems = (const sk::VerifyDev *)(plan.blob + o_problems);
+  for (sk::VerifyLaunch &l : h.launches)
+    for (int32_t i = 0; i < l.n; ++i) {
+      sk::VerifyDev &d = l.args.problems[i];
+      moved(d.arrived, plan.blob), moved(d.stats, ws), moved(d.sums, ws);
+    }
   return sk::copy_image(plan, image);
 }
 
@@ -442,11 +532,12 @@ sk_status sk_verify_launch(sk_verify_plan *plan, void *hip_stream) {
     const hipStream_t stream = (hipStream_t)hip_stream;
     bool in_capture = false;
     sk_status st = sk::admit(plan, stream, &in_capture);
-    if (st != SK_OK || plan->host.problems.empty()) return st;
+    if (st != SK_OK || plan->host.launches.empty()) return st;
     const hipEvent_t behind = in_capture ? nullptr : plan->last_use;
-    auto args = [&](int i) { return sk::VerifyArgs{plan->problems, plan->first[i], (int32_t)plan->host.problems.size()}; };
-    st = sk::launch(sk::sk_verify_stats, (int64_t)plan->host.stat_first.back(), stream, nullptr, args(0));
-    if (st == SK_OK) st = sk::launch(sk::sk_verify_sample, (int64_t)plan->host.sum_first.back(), stream, behind, args(1));
+    for (const sk::VerifyLaunch &l : plan->host.launches) {
+      if (st == SK_OK) st = sk::launch(sk::sk_verify_stats, l.stat_grid, stream, nullptr, l.args);
+      if (st == SK_OK) st = sk::launch(sk::sk_verify_sample, l.sum_grid, stream, &l == &plan->host.launches.back() ? behind : nullptr, l.args);
+    }
     plan->ledger.after_launch((uintptr_t)stream, in_capture, behind && st == SK_OK);  // also after a failure: some launches may be out
     return st;
   });
@@ -455,7 +546,7 @@ sk_status sk_verify_launch(sk_verify_plan *plan, void *hip_stream) {
 sk_status sk_verify_plan_info(const sk_verify_plan *plan, int32_t *launches, int64_t *workspace_bytes) {
   return sk::guarded([&]() -> sk_status {
     if (!plan) return sk::set_last_error(SK_ERR_INVALID_ARG, "plan is null");
-    if (launches) *launches = plan->host.problems.empty() ? 0 : 2;
+    if (launches) *launches = 2 * (int32_t)plan->host.launches.size();
     if (workspace_bytes) *workspace_bytes = (int64_t)(plan->host.workspace + plan->host.counters);
     return SK_OK;
   });

@@ -103,7 +103,7 @@ static void moes() {
       need(out.route_first[at + 1] - out.route_first[at] == blocks * ((d.experts + sk::ROUTE_EXPERTS - 1) / sk::ROUTE_EXPERTS), "units of the router");
       need(d.h_stride >= 2 * std::max(d.ffn, d.shared_ffn) && d.h_stride % 128 == 0, "strides of the workspace");
       need(d.count == out.counts + at, "counts");
-      counters.next(d.routed, blocks), counters.next(d.blocks_routed, 1), counters.next(d.summed, d.down_tiles);
+      counters.next(d.routed, blocks * sk::COUNTER_STEP), counters.next(d.blocks_routed, sk::COUNTER_STEP), counters.next(d.summed, (int64_t)d.down_tiles * sk::COUNTER_STEP);
       work.next(d.logits, (int64_t)d.rows * d.experts), work.next(d.ids, pairs), work.next(d.weights, pairs), work.next(d.row_of, pairs), work.next(d.weight_of, pairs);
       work.next(d.groups, d.most_groups), work.next(d.first_begin, d.most_groups), work.next(d.second_begin, d.most_groups), work.next(d.h, places * d.h_stride);
     }
@@ -214,7 +214,7 @@ static void shares() {
 }
 
 static void verifications() {
-  const int n = (int)between(0, 5);
+  const int n = (int)between(0, between(0, 3) ? 5 : 40);
   std::vector<sk_verify_problem> problems;
   for (int i = 0; i < n; ++i) {
     sk_verify_problem p{};
@@ -227,16 +227,26 @@ static void verifications() {
   sk::VerifyPlanHost out;
   std::string err;
   need(sk::plan_verify(problems.data(), n, out, err) == SK_OK, err.c_str());
-  need((int)out.problems.size() == n, "problems");
   Walk work(out.workspace), counters(out.counters);
-  for (int i = 0; i < n; ++i) {
-    const sk::VerifyDev &d = out.problems[(size_t)i];
-    need(d.pieces >= 1 && d.pieces <= 4 && (int64_t)d.chunks * d.pieces * 2048 >= d.vocab && ((int64_t)d.chunks - 1) * d.pieces * 2048 < d.vocab, "chunks");
-    need(out.stat_first[i + 1] - out.stat_first[i] == (uint64_t)d.rows * (d.draft_logits ? 2 : 1) * d.chunks, "units of the rows");
-    need(out.sum_first[i + 1] - out.sum_first[i] == (uint64_t)d.sequences * d.chunks, "units of the sequences");
-    counters.next(d.arrived, d.sequences);
-    work.next(d.stats, (int64_t)d.rows * 2 * d.chunks), work.next(d.sums, (int64_t)d.sequences * d.chunks);
+  int seen = 0;
+  for (const sk::VerifyLaunch &l : out.launches) {
+    need(l.n >= 1 && l.n <= sk::VERIFY_PROBLEMS, "problems of a launch");
+    for (int i = 0; i < sk::VERIFY_PROBLEMS; ++i) {
+      if (i >= l.n) {
+        need(l.args.stat_first[i] == 0xffffffffu && l.args.sum_first[i] == 0xffffffffu, "a place without a problem can be found");
+        continue;
+      }
+      const sk::VerifyDev &d = l.args.problems[i];
+      need(d.rows == problems[(size_t)seen].rows && d.vocab == problems[(size_t)seen].vocab, "problems in their order");
+      need(d.pieces >= 1 && d.pieces <= 8 && (int64_t)d.chunks * d.pieces * 512 >= d.vocab && ((int64_t)d.chunks - 1) * d.pieces * 512 < d.vocab, "chunks");
+      need((i + 1 < l.n ? l.args.stat_first[i + 1] : l.stat_grid) - l.args.stat_first[i] == ((int64_t)d.rows * (d.draft_logits ? 2 : 1) * d.chunks + 3) / 4, "units of the rows");
+      need((i + 1 < l.n ? l.args.sum_first[i + 1] : l.sum_grid) - l.args.sum_first[i] == (int64_t)d.sequences * d.chunks, "units of the sequences");
+      counters.next(d.arrived, (int64_t)d.sequences * sk::COUNTER_STEP);
+      work.next(d.stats, (int64_t)d.rows * 2 * d.chunks), work.next(d.sums, (int64_t)d.sequences * d.chunks);
+      ++seen;
+    }
   }
+  need(seen == n, "every problem once");
 }
 
 int main() {

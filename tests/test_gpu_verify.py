@@ -163,6 +163,10 @@ def test_captured_and_replayed_between_other_launches():
         del graph
 
 
+def test_more_problems_than_a_launch_takes():
+    H.check_verify([H.Verify(dtype=("bf16", "f16", "f32")[i % 3], vocab=50 + 97 * i, counts=(1 + i % 4, i % 3), draft=("logits", "certain", "none")[i % 3], seed=i) for i in range(37)])
+
+
 def test_tenants():
     H.check_verify([H.Verify(vocab=5000, counts=(3, 3), seed=1), H.Verify(dtype="f32", vocab=30, counts=(1,) * 70, draft="none", seed=2), H.Verify(dtype="f16", vocab=9, counts=(0, 0), spare=1, seed=3),
                     H.Verify(dtype="f16", vocab=70001, counts=(7,), draft="certain", pad=1, seed=4)])
