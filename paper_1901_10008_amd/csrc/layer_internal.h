@@ -133,6 +133,7 @@ struct VerifyDev {
   double *sums;            // [sequences][chunks]
   uint32_t *arrived;       // [sequences], COUNTER_STEP apart
 };
+constexpr int32_t VERIFY_CHUNKS = 4;  // that a workgroup of the second launch takes
 // In the launch's arguments, as those of norms.
 constexpr int VERIFY_PROBLEMS = 16;  // of a launch
 struct VerifyArgs {

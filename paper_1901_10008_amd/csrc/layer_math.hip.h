@@ -111,10 +111,19 @@ __device__ __forceinline__ float wave_max(float v) {
   v = fmaxf(v, other_lane<0x140>(v));
   return max32(max16(v));
 }
+// (the same in all lanes)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int32_t lesser(int32_t v) {
+  return min(v, __builtin_amdgcn_update_dpp(v, v, CTRL, ROWS, 0xf, false));
+}
 __device__ __forceinline__ int32_t wave_min(int32_t v) {
-#pragma unroll
-  for (int d = 32; d; d /= 2) v = min(v, __shfl_xor(v, d));
-  return v;
+  v = lesser<0x111, 0xf>(v);  // row_shr:1, 2, 4, 8
+  v = lesser<0x112, 0xf>(v);
+  v = lesser<0x114, 0xf>(v);
+  v = lesser<0x118, 0xf>(v);
+  v = lesser<0x142, 0xa>(v);  // row_bcast:15, 31
+  v = lesser<0x143, 0xc>(v);
+  return lane_of(v, 63);
 }
 
 // e^x to about 2 units of the last place: what x * log2(e) loses by rounding is put back.

@@ -273,7 +273,7 @@ sk_status plan_verify(const sk_verify_problem *problems, int32_t n, VerifyPlanHo
     while (d.pieces < (p.dtype == SK_F32 ? 4 : 8) && lines * ((p.vocab + 1024 * d.pieces - 1) / (1024 * d.pieces)) >= VERIFY_WAVES) d.pieces *= 2;
     const int64_t chunk = 512 * (int64_t)d.pieces;
     d.chunks = (int32_t)((p.vocab + chunk - 1) / chunk);
-    const int64_t stat = (lines * d.chunks + 3) / 4, sum = (int64_t)p.sequences * d.chunks;
+    const int64_t stat = (lines * d.chunks + 3) / 4, sum = p.sequences * (((int64_t)d.chunks + VERIFY_CHUNKS - 1) / VERIFY_CHUNKS);
     if (stat > MOST_GRID || sum > MOST_GRID) return refuse(err, SK_ERR_UNSUPPORTED, "more units of work than a launch's grid can hold");
     counters.take(d.arrived, (int64_t)p.sequences * COUNTER_STEP);
     work.take(d.stats, (int64_t)p.rows * 2 * d.chunks), work.take(d.sums, (int64_t)p.sequences * d.chunks);

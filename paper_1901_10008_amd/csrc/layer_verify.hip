@@ -260,7 +260,7 @@ template <int DT>
 __device__ __forceinline__ double chunk_weights(const VerifyDev &P, const Draw &d, const char *p_row, const char *q_row, int32_t chunk, double c, double (&w)[2][8], int32_t (&places)[2],
                                                 VerifyShared &s, int tid) {
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const char *other = d.mode == FROM_DIFFERENCE ? q_row : p_row;
+
   Eight<DT> p[2], q[2];
   int32_t at[2];
 #pragma unroll
@@ -269,7 +269,7 @@ __device__ __forceinline__ double chunk_weights(const VerifyDev &P, const Draw &
     at[j] = i < P.pieces ? (chunk * P.pieces + i) * 512 : P.vocab;
     if (at[j] >= P.vocab) continue;  // (the same in all lanes)
     p[j].template load<true>(p_row, at[j], lane, P.vocab);
-    q[j].template load<true>(other, at[j], lane, P.vocab);
+    q[j].template load<true>(q_row, at[j], lane, P.vocab);
   }
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
@@ -293,6 +293,28 @@ __device__ __forceinline__ double chunk_weights(const VerifyDev &P, const Draw &
 #pragma unroll
   for (int i = 0; i < 8; ++i) all += s.piece[i];
   return all;
+}
+
+// The sum of a chunk's weights, by a wave, in all lanes.
+template <int DT>
+__device__ __forceinline__ double chunk_sum(const VerifyDev &P, const Draw &d, const char *p_row, const char *q_row, int32_t chunk, double c, int lane) {
+  Eight<DT> p, q, p_next, q_next;
+  int32_t at = chunk * 512 * P.pieces;
+  p.template load<true>(p_row, at, lane, P.vocab);
+  q.template load<true>(q_row, at, lane, P.vocab);
+  double sum = 0.0;
+  for (int32_t i = 0; i < P.pieces && at < P.vocab; ++i, at += 512) {
+    p_next.template load<true>(p_row, at + 512, lane, P.vocab);  // (behind the chunk: not used)
+    q_next.template load<true>(q_row, at + 512, lane, P.vocab);
+    p.cut(at, lane, P.vocab);
+    q.cut(at, lane, P.vocab);
+    double w[8];
+    weights8<DT>(d, p, q, c, w);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum += w[k];
+    p = p_next, q = q_next;
+  }
+  return wave_sum(sum);
 }
 
 // The first token whose weight and those before it add up to more than `random` times all, by a workgroup.  sum_of(i) is the sum of chunk i (asked for
@@ -434,29 +456,32 @@ __device__ __forceinline__ void decide(const VerifyDev &P, int32_t r0, int32_t n
 }
 
 template <int DT>
-__device__ __forceinline__ void sample(const VerifyDev &P, int32_t seq, int32_t chunk, VerifyShared &s, Draw *draws, int32_t *stop, uint32_t *flag, int tid) {
+__device__ __forceinline__ void sample(const VerifyDev &P, int32_t seq, int32_t part, VerifyShared &s, Draw *draws, int32_t *stop, uint32_t *flag, int tid) {
   const int32_t r0 = first_of(P, seq), n = first_of(P, seq + 1) - r0;
   if (n <= 0) {
-    if (chunk == 0 && tid == 0) P.accepted[seq] = 0;
+    if (part == 0 && tid == 0) P.accepted[seq] = 0;
     return;
   }
   const double c = scale_of(P, seq);
   Draw d;
   decide<DT>(P, r0, n, c, draws, stop, tid, d);
-  const char *p_row = P.logits + (int64_t)(r0 + d.stop) * P.logits_stride, *q_row = d.mode == FROM_DIFFERENCE ? P.draft_logits + (int64_t)(r0 + d.stop) * P.draft_stride : nullptr;
+  const char *p_row = P.logits + (int64_t)(r0 + d.stop) * P.logits_stride, *q_row = d.mode == FROM_DIFFERENCE ? P.draft_logits + (int64_t)(r0 + d.stop) * P.draft_stride : p_row;
   const double random = random_of(P.sample_random + seq);
   const VerifyStat *stats = P.stats + (int64_t)(r0 + d.stop) * 2 * P.chunks;
   auto from_stats = [&](int32_t i) { return stats[i].top > -__builtin_inff() ? stats[i].sum * weight_of((double)stats[i].top - d.p.top, c) : 0.0; };
   int32_t token = -1;
   double w[2][8];
   int32_t places[2];
-  if (d.mode == FROM_DIFFERENCE) {  // a chunk a workgroup
+  if (d.mode == FROM_DIFFERENCE) {  // a chunk a wave
     double *sums = P.sums + (int64_t)seq * P.chunks;
-    const double sum = chunk_weights<DT>(P, d, p_row, q_row, chunk, c, w, places, s, tid);
-    if (tid == 0) put(sums + chunk, sum);
-    if (!last_to_arrive(P.arrived + (int64_t)seq * COUNTER_STEP, P.chunks, flag)) return;
+    const int32_t chunk = part * VERIFY_CHUNKS + __builtin_amdgcn_readfirstlane(tid >> 6);
+    if (chunk < P.chunks) {
+      const double sum = chunk_sum<DT>(P, d, p_row, q_row, chunk, c, tid & 63);
+      if ((tid & 63) == 0) put(sums + chunk, sum);
+    }
+    if (!last_to_arrive(P.arrived + (int64_t)seq * COUNTER_STEP, (P.chunks + VERIFY_CHUNKS - 1) / VERIFY_CHUNKS, flag)) return;
     token = pick<DT>(P, d, p_row, q_row, c, random, [&](int32_t i) { return got(sums + i); }, s, tid);
-  } else if (chunk != 0) {
+  } else if (part != 0) {
     return;
   } else if (d.mode == FROM_OTHERS) {
     const int32_t without = d.token / (512 * P.pieces);
@@ -483,10 +508,11 @@ __global__ void __launch_bounds__(CACHE_THREADS, 4) sk_verify_sample(VerifyArgs 
   for (int k = 1; k < VERIFY_PROBLEMS; ++k) i += a.sum_first[k] <= blockIdx.x ? 1 : 0;
   const VerifyDev &P = a.problems[i];
   const uint32_t unit = blockIdx.x - a.sum_first[i];
-  const int32_t seq = (int32_t)(unit / (uint32_t)P.chunks), chunk = (int32_t)(unit % (uint32_t)P.chunks);
-  if (P.dtype == SK_F32) sample<SK_F32>(P, seq, chunk, shared, draws, &stop, &flag, tid);
-  else if (P.dtype == SK_BF16) sample<SK_BF16>(P, seq, chunk, shared, draws, &stop, &flag, tid);
-  else sample<SK_F16>(P, seq, chunk, shared, draws, &stop, &flag, tid);
+  const uint32_t parts = ((uint32_t)P.chunks + VERIFY_CHUNKS - 1) / VERIFY_CHUNKS;
+  const int32_t seq = (int32_t)(unit / parts), part = (int32_t)(unit % parts);
+  if (P.dtype == SK_F32) sample<SK_F32>(P, seq, part, shared, draws, &stop, &flag, tid);
+  else if (P.dtype == SK_BF16) sample<SK_BF16>(P, seq, part, shared, draws, &stop, &flag, tid);
+  else sample<SK_F16>(P, seq, part, shared, draws, &stop, &flag, tid);
 }
 
 }  // namespace sk

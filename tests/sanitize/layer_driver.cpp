@@ -240,7 +240,7 @@ static void verifications() {
       need(d.rows == problems[(size_t)seen].rows && d.vocab == problems[(size_t)seen].vocab, "problems in their order");
       need(d.pieces >= 1 && d.pieces <= 8 && (int64_t)d.chunks * d.pieces * 512 >= d.vocab && ((int64_t)d.chunks - 1) * d.pieces * 512 < d.vocab, "chunks");
       need((i + 1 < l.n ? l.args.stat_first[i + 1] : l.stat_grid) - l.args.stat_first[i] == ((int64_t)d.rows * (d.draft_logits ? 2 : 1) * d.chunks + 3) / 4, "units of the rows");
-      need((i + 1 < l.n ? l.args.sum_first[i + 1] : l.sum_grid) - l.args.sum_first[i] == (int64_t)d.sequences * d.chunks, "units of the sequences");
+      need((i + 1 < l.n ? l.args.sum_first[i + 1] : l.sum_grid) - l.args.sum_first[i] == (int64_t)d.sequences * ((d.chunks + sk::VERIFY_CHUNKS - 1) / sk::VERIFY_CHUNKS), "units of the sequences");
       counters.next(d.arrived, (int64_t)d.sequences * sk::COUNTER_STEP);
       work.next(d.stats, (int64_t)d.rows * 2 * d.chunks), work.next(d.sums, (int64_t)d.sequences * d.chunks);
       ++seen;
