@@ -18,7 +18,7 @@
  *   - Row strides are in elements; 0 means packed.  Pointers are multiples of their element's size unless stated otherwise.
  *   - n_rows (norm, moe): a number on the device, read by every launch; rows from it on are left as they are.  Values outside [0, rows]
  *     are cut to it; null means `rows`.  So a plan serves every step with up to `rows` rows, also out of a HIP graph.
- *   - Norm plans hold nothing on the device: their launches may overlap.  Plans of the other two own a workspace, so
+ *   - Norm plans have no workspace: their launches may overlap.  Plans of the other two own a workspace, so
  *     their launches must not: those on one stream are ordered by it, a launch on another stream gives SK_ERR_BUSY while the last one
  *     has not completed (best effort; launches of a graph are not tracked, and its replays are the caller's to order).
  *   - Outputs of a plan (of one problem or of several) whose spans from first to last element intersect give SK_ERR_OVERLAP.
@@ -87,7 +87,7 @@ typedef struct sk_norm_plan sk_norm_plan; /* opaque, owned by the library */
 sk_status sk_norm_plan_create(const sk_norm_problem *problems, int32_t n, const sk_layer_params *params, sk_norm_plan **out);
 /* Waits for the device's work and frees the plan; null is accepted. */
 sk_status sk_norm_plan_destroy(sk_norm_plan *plan);
-/* One kernel launch for up to 16 problems of one kind of work (rows shared by a workgroup, or a wave each; dim up to 8192, or larger). */
+/* One kernel launch for up to 16 problems of one kind of work (rows of up to 2048, 4096, 8192 or more elements; all of them if they have 1024 rows or fewer). */
 sk_status sk_norm_launch(sk_norm_plan *plan, void *hip_stream);
 
 /* ---- mixture-of-experts layer -------------------------------------------------------------------------------------------

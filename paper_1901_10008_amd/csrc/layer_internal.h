@@ -18,8 +18,7 @@ constexpr int COUNTER_STEP = 32;
 
 // ---- norms -----------------------------------------------------------------------------------------------------------------
 
-// A problem as the kernel sees it (strides in elements), in the launch's arguments: a step's norms take a launch and two trips to memory, so a
-// third one for descriptors would be felt.
+// A problem as the kernel sees it (strides in elements).
 struct NormDev {
   const int32_t *n_rows;
   const void *block, *gate, *residual, *post_weight, *post_bias, *pre_weight, *pre_bias;
@@ -30,24 +29,24 @@ struct NormDev {
   int8_t dtype, residual_dtype, kind, post, act, pad[3];
 };
 constexpr int NORM_PROBLEMS = 16;  // of a launch
-struct NormArgs {
+// Of a launch, in device memory.  (By value in the launch's arguments, which are in host memory, a step of three rows took 4.9 us.)
+struct NormTable {
   uint32_t first[NORM_PROBLEMS];  // workgroup of the launch; none: the largest number
   NormDev problems[NORM_PROBLEMS];
 };
-static_assert(sizeof(NormArgs) <= 4096, "kernel arguments");
 
-// What a row gets: a wave (rows of up to 2048 elements), a workgroup of four waves, or one of sixteen; up to 4 pieces of 8 elements a thread.
-enum NormForm { NORM_WAVE, NORM_GROUP, NORM_LONG, NORM_FORMS };
-constexpr int NORM_LONG_THREADS = 1024;
-constexpr int64_t NORM_LONG_GRID = (((int64_t)1 << 32) - 1) / NORM_LONG_THREADS;
-constexpr int norm_most_dim(NormForm f) { return f == NORM_WAVE ? 2048 : f == NORM_GROUP ? 8192 : 32768; }
+// What a row gets: a wave, or a workgroup of four, eight or sixteen, with up to 4, 2, 2 or 4 pieces of 8 elements a thread.
+enum NormForm { NORM_WAVE, NORM_GROUP, NORM_PAIR, NORM_LONG, NORM_FORMS };
+constexpr int norm_threads(NormForm f) { return f == NORM_LONG ? 1024 : f == NORM_PAIR ? 512 : 256; }  // of a workgroup
+constexpr int norm_most_dim(NormForm f) { return f == NORM_WAVE ? 2048 : f == NORM_GROUP ? 4096 : f == NORM_PAIR ? 8192 : 32768; }
+constexpr int64_t norm_most_grid(NormForm f) { return (((int64_t)1 << 32) - 1) / norm_threads(f); }
 
 struct NormLaunch {
   NormForm form;
   bool once;  // it moves more than PAST_CACHES bytes
   int32_t n;
   int64_t grid;
-  NormArgs args;
+  NormTable table;
 };
 struct NormPlanHost {
   std::vector<NormLaunch> launches;
@@ -134,17 +133,15 @@ struct VerifyDev {
   uint32_t *arrived;       // [sequences], COUNTER_STEP apart
 };
 constexpr int32_t VERIFY_CHUNKS = 4;  // that a workgroup of the second launch takes
-// In the launch's arguments, as those of norms.
 constexpr int VERIFY_PROBLEMS = 16;  // of a launch
-struct VerifyArgs {
+struct VerifyTable {
   uint32_t stat_first[VERIFY_PROBLEMS], sum_first[VERIFY_PROBLEMS];  // workgroup of the two launches; none: the largest number
   VerifyDev problems[VERIFY_PROBLEMS];
 };
-static_assert(sizeof(VerifyArgs) <= 4096, "kernel arguments");
 struct VerifyLaunch {
   int32_t n;
   int64_t stat_grid, sum_grid;
-  VerifyArgs args;  // workspace pointers: offsets until the plan is on the device
+  VerifyTable table;  // workspace pointers: offsets until the plan is on the device
 };
 struct VerifyPlanHost {
   std::vector<VerifyLaunch> launches;

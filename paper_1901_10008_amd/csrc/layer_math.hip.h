@@ -138,7 +138,7 @@ __device__ __forceinline__ float activated(int act, float z) {
   if (act == SK_ACT_NONE) return z;
   if (act == SK_ACT_RELU) return z < 0.f ? 0.f : z;
   const float t = act == SK_ACT_TANH ? 2.f * z : act == SK_ACT_GELU ? 1.5957691216f * (z + 0.044715f * z * z * z) : z;
-  const float s = 1.f / (1.f + exp_of(-t));
+  const float s = __builtin_amdgcn_rcpf(1.f + exp_of(-t));  // (to a unit of the last place; 0 of infinity)
   if (act == SK_ACT_SIGMOID) return s;
   if (act == SK_ACT_TANH) {
     const float q = z * z;  // |z| < 1/4: the next term is below 2^-25 of z

@@ -8,8 +8,12 @@ namespace sk {
 //
 //   u = N(block) w + b,  r = rs * residual + bs * u * act(gate),  next = N(r) w' + b'
 //
-// Each norm is one sum over the row, or two (the mean, then the squares of what lies beside it: nothing cancels).  All of a row's loads are on their
-// way before the first sum.
+// Each norm is one sum over the row, or two (the mean, then the squares of what lies beside it: nothing cancels).  All of a row's loads, those of the
+// weights among them, are on their way before the number of rows is known and before the first sum.
+struct NormArgs {
+  const NormTable *table;
+  int32_t n;
+};
 template <int T>
 struct RowSum {
   float (*red)[16];
@@ -29,38 +33,52 @@ struct RowSum {
 };
 
 template <int T, int P, bool ONCE, int DT, int RT>
-__device__ __forceinline__ void norm_row(const NormDev &p, int64_t row, int t, float (*red)[16]) {
+__device__ __forceinline__ void norm_row(const SK_CONSTANT NormDev &p, int64_t row, int t, float (*red)[16]) {
   constexpr int ES = DT == SK_F32 ? 4 : 2, RS = RT == SK_F32 ? 4 : 2;
+  constexpr bool LATE = T > 512 || DT == SK_F32;  // gates and weights are loaded when they are wanted: there are not the registers to keep them
   const int dim = p.dim;
   const float by = 1.f / (float)dim;
   RowSum<T> sum{red, t >> 6};
-  float u[P][8], r[P][8], g[P][8];
+  using Own = std::integral_constant<int, DT>;
+  using Res = std::integral_constant<int, RT>;
 
-  // pieces of 8 elements; the last one of a row may be shorter: only its elements are read and written
-  auto load = [&](auto type, auto once, const void *base, int64_t at, float(&x)[8], float missing) {
-    constexpr int D = decltype(type)::value;
-    constexpr int S = D == SK_F32 ? 4 : 2;
-    if (!base || at >= dim) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] = base ? 0.f : missing;
-      return;
-    }
-    const char *q = (const char *)base + at * S;
+  // pieces of 8 elements as they come; the last one of a row may be shorter: only its elements are read and written
+  auto load = [&](auto type, bool once, const void *base, int i, u32x4 *raw) {
+    constexpr int D = decltype(type)::value, S = D == SK_F32 ? 4 : 2;
+    const int at = (i * T + t) * 8;
+    const char *q = (const char *)base + (int64_t)at * S;
     if (at + 8 <= dim) {
-      load8<D, decltype(once)::value>(q, x);
+#pragma unroll
+      for (int j = 0; j < S / 2; ++j) {
+        const u32x4_any SK_GLOBAL *g = (const u32x4_any SK_GLOBAL *)(uintptr_t)(q + 16 * j);
+        raw[j] = ONCE && once ? (u32x4)__builtin_nontemporal_load(g) : (u32x4)*g;
+      }
     } else {
+      uint32_t e[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const float v = load1<D>((const char *)base + min(at + k, (int64_t)dim - 1) * S);
-        x[k] = at + k < dim ? v : 0.f;
+        const char *g = (const char *)base + (int64_t)min(at + k, dim - 1) * S;
+        e[k] = S == 4 ? *(const uint32_t SK_GLOBAL *)(uintptr_t)g : load_u16(g);
+        e[k] = at + k < dim ? e[k] : 0u;
       }
+      if constexpr (S == 4) raw[0] = u32x4{e[0], e[1], e[2], e[3]}, raw[1] = u32x4{e[4], e[5], e[6], e[7]};
+      else raw[0] = u32x4{e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16};
     }
   };
-  auto store = [&](auto type, char *base, int64_t at, const float(&x)[8]) {
+  auto values = [&](auto type, const u32x4 *raw, float(&x)[8]) {
     constexpr int D = decltype(type)::value;
-    constexpr int S = D == SK_F32 ? 4 : 2;
+    if constexpr (D == SK_F32) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = __builtin_bit_cast(float, (uint32_t)raw[k / 4][k % 4]);
+    } else {
+      unpack8<D>(raw[0], x);
+    }
+  };
+  auto store = [&](auto type, char *base, int i, const float(&x)[8]) {
+    constexpr int D = decltype(type)::value, S = D == SK_F32 ? 4 : 2;
+    const int at = (i * T + t) * 8;
     if (at >= dim) return;
-    char *q = base + at * S;
+    char *q = base + (int64_t)at * S;
     if (at + 8 <= dim) {
       store8_elements<D, ONCE>(q, x);
     } else {
@@ -69,116 +87,135 @@ __device__ __forceinline__ void norm_row(const NormDev &p, int64_t row, int t, f
         if (at + k < dim) store1<D>(q + k * S, x[k]);
     }
   };
-  using Own = std::integral_constant<int, DT>;
-  using Res = std::integral_constant<int, RT>;
-  using Once = std::integral_constant<bool, ONCE>;
-  using Again = std::integral_constant<bool, false>;
+  auto each_piece = [&](auto f) {
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+      if (i * T * 8 < dim) f(i);
+  };
 
   const char *block = p.block ? (const char *)p.block + row * p.block_stride * ES : nullptr;
   const char *gate = p.gate ? (const char *)p.gate + row * p.gate_stride * ES : nullptr;
-  constexpr bool LATE = T > 256;  // its threads have 128 registers each: gates are loaded when they are wanted
-  auto load_gate = [&](int i, int64_t at) {
-    if (p.gate_stride) load(Own{}, Once{}, gate, at, g[i], 1.f);
-    else load(Own{}, Again{}, gate, at, g[i], 1.f);
-  };
   const char *residual = p.residual ? (const char *)p.residual + row * p.residual_stride * RS : nullptr;
-#pragma unroll
-  for (int i = 0; i < P; ++i) {
-    const int64_t at = ((int64_t)i * T + t) * 8;
-    if (i * T * 8 < dim) {
-      load(Own{}, Once{}, block, at, u[i], 0.f);
-      if (gate && !LATE) load_gate(i, at);
-      load(Res{}, Once{}, residual, at, r[i], 0.f);
-    }
+  const bool post = block && p.post, post_weight = post && p.post_weight, pre_weight = p.next && p.pre_weight;
+  u32x4 block_raw[P][ES / 2], gate_raw[P][ES / 2], residual_raw[P][RS / 2], post_raw[P][ES / 2], pre_raw[P][ES / 2];
+  each_piece([&](int i) {
+    if (block) load(Own{}, true, block, i, block_raw[i]);
+    if (residual) load(Res{}, true, residual, i, residual_raw[i]);
+  });
+  if (!LATE) {
+    each_piece([&](int i) {
+      if (gate) load(Own{}, p.gate_stride != 0, gate, i, gate_raw[i]);
+      if (post_weight) load(Own{}, false, p.post_weight, i, post_raw[i]);
+      if (pre_weight) load(Own{}, false, p.pre_weight, i, pre_raw[i]);
+    });
   }
+  if (p.n_rows && row >= load_i32(p.n_rows)) return;
 
-  // x becomes (x - mean) * scale, or x * scale
+  // x becomes x - mean, and what it is to be multiplied by is returned
   auto standard = [&](float(&x)[P][8]) {
     float s = 0.f;
     if (p.kind == SK_NORM_LAYER) {
+      each_piece([&](int i) {
 #pragma unroll
-      for (int i = 0; i < P; ++i)
-        if (i * T * 8 < dim) {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) s += x[i][k];
-        }
+        for (int k = 0; k < 8; ++k) s += x[i][k];
+      });
       const float mean = sum(s) * by;
+      each_piece([&](int i) {
 #pragma unroll
-      for (int i = 0; i < P; ++i)
-        if (i * T * 8 < dim) {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) x[i][k] = (i * T + t) * 8 + k < dim ? x[i][k] - mean : 0.f;
-        }
+        for (int k = 0; k < 8; ++k) x[i][k] = (i * T + t) * 8 + k < dim ? x[i][k] - mean : 0.f;
+      });
     }
     s = 0.f;
+    each_piece([&](int i) {
 #pragma unroll
-    for (int i = 0; i < P; ++i)
-      if (i * T * 8 < dim) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) s += x[i][k] * x[i][k];
-      }
+      for (int k = 0; k < 8; ++k) s += x[i][k] * x[i][k];
+    });
     return 1.f / sqrtf(sum(s) * by + p.eps);
   };
-
-  if (block) {
-    if (p.post) {
-      const float scale = standard(u);
+  // y = x * scale * weight + bias
+  auto weighted = [&](int i, const float(&x)[8], float scale, const void *weight, u32x4 *raw, const void *bias, float(&y)[8]) {
 #pragma unroll
-      for (int i = 0; i < P; ++i)
-        if (i * T * 8 < dim) {
-          const int64_t at = ((int64_t)i * T + t) * 8;
-          float w[8], b[8];
-          load(Own{}, Again{}, p.post_weight, at, w, 1.f);
-          load(Own{}, Again{}, p.post_bias, at, b, 0.f);
+    for (int k = 0; k < 8; ++k) y[k] = x[k] * scale;
+    if (weight) {
+      float w[8];
+      if (LATE) load(Own{}, false, weight, i, raw);
+      values(Own{}, raw, w);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) u[i][k] = u[i][k] * scale * w[k] + b[k];
-        }
+      for (int k = 0; k < 8; ++k) y[k] *= w[k];
     }
+    if (bias) {
+      float b[8];
+      u32x4 bias_raw[ES / 2];
+      load(Own{}, false, bias, i, bias_raw);
+      values(Own{}, bias_raw, b);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) y[k] += b[k];
+    }
+  };
+
+  float u[P][8], r[P][8];
+  if (block) {
+    each_piece([&](int i) { values(Own{}, block_raw[i], u[i]); });
+    const float scale = post ? standard(u) : 1.f;
+    each_piece([&](int i) {
+      if (post) weighted(i, u[i], scale, p.post_weight, post_raw[i], p.post_bias, u[i]);
+    });
+    auto gated = [&](auto act) {
+      each_piece([&](int i) {
+        float g[8];
+        if (LATE) load(Own{}, p.gate_stride != 0, gate, i, gate_raw[i]);
+        values(Own{}, gate_raw[i], g);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) u[i][k] *= activated(decltype(act)::value, g[k]);
+      });
+    };
     if (gate) {
-#pragma unroll
-      for (int i = 0; i < P; ++i)
-        if (i * T * 8 < dim) {
-          if (LATE) load_gate(i, ((int64_t)i * T + t) * 8);
-#pragma unroll
-          for (int k = 0; k < 8; ++k) u[i][k] *= activated(p.act, g[i][k]);
-        }
+      switch (p.act) {
+        case SK_ACT_SIGMOID: gated(std::integral_constant<int, SK_ACT_SIGMOID>{}); break;
+        case SK_ACT_SILU: gated(std::integral_constant<int, SK_ACT_SILU>{}); break;
+        case SK_ACT_TANH: gated(std::integral_constant<int, SK_ACT_TANH>{}); break;
+        case SK_ACT_GELU: gated(std::integral_constant<int, SK_ACT_GELU>{}); break;
+        case SK_ACT_RELU: gated(std::integral_constant<int, SK_ACT_RELU>{}); break;
+        default: gated(std::integral_constant<int, SK_ACT_NONE>{});
+      }
     }
   }
+  each_piece([&](int i) {
+    // (a missing part adds nothing, not its scale times 0)
+    if (residual) values(Res{}, residual_raw[i], r[i]);
 #pragma unroll
-  for (int i = 0; i < P; ++i)
-    if (i * T * 8 < dim) {
-      // (a missing part adds nothing, not its scale times 0)
+    for (int k = 0; k < 8; ++k) r[i][k] = !block ? p.residual_scale * r[i][k] : !residual ? p.block_scale * u[i][k] : p.residual_scale * r[i][k] + p.block_scale * u[i][k];
+    if (p.post_bias) {  // (a bias stands behind the row's end as well)
 #pragma unroll
-      for (int k = 0; k < 8; ++k) r[i][k] = !block ? p.residual_scale * r[i][k] : !residual ? p.block_scale * u[i][k] : p.residual_scale * r[i][k] + p.block_scale * u[i][k];
-      if (p.residual_out) store(Res{}, (char *)p.residual_out + row * p.residual_out_stride * RS, ((int64_t)i * T + t) * 8, r[i]);
+      for (int k = 0; k < 8; ++k) r[i][k] = (i * T + t) * 8 + k < dim ? r[i][k] : 0.f;
     }
+    if (p.residual_out) store(Res{}, (char *)p.residual_out + row * p.residual_out_stride * RS, i, r[i]);
+  });
   if (!p.next) return;
   const float scale = standard(r);
-#pragma unroll
-  for (int i = 0; i < P; ++i)
-    if (i * T * 8 < dim) {
-      const int64_t at = ((int64_t)i * T + t) * 8;
-      float w[8], b[8];
-      load(Own{}, Again{}, p.pre_weight, at, w, 1.f);
-      load(Own{}, Again{}, p.pre_bias, at, b, 0.f);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) w[k] = r[i][k] * scale * w[k] + b[k];
-      store(Own{}, (char *)p.next + row * p.next_stride * ES, at, w);
-    }
+  each_piece([&](int i) {
+    float y[8];
+    weighted(i, r[i], scale, p.pre_weight, pre_raw[i], p.pre_bias, y);
+    store(Own{}, (char *)p.next + row * p.next_stride * ES, i, y);
+  });
 }
 
 template <int T, int P, bool ONCE>
 __global__ void __launch_bounds__(T > CACHE_THREADS ? T : CACHE_THREADS) sk_norm(NormArgs a) {
   __shared__ float red[4][16];
+  const SK_CONSTANT NormTable &table = *(const SK_CONSTANT NormTable *)(uintptr_t)a.table;
   int i = 0;
+  uint32_t first = 0;
+  if (a.n > 1) {
 #pragma unroll
-  for (int k = 1; k < NORM_PROBLEMS; ++k) i += a.first[k] <= blockIdx.x ? 1 : 0;
-  const NormDev &p = a.problems[i];
-  const int64_t n = p.n_rows ? min(load_i32(p.n_rows), p.rows) : p.rows;
+    for (int k = 1; k < NORM_PROBLEMS; ++k) i += table.first[k] <= blockIdx.x ? 1 : 0;
+    first = table.first[i];
+  }
+  const SK_CONSTANT NormDev &p = table.problems[i];
   const int t = (int)threadIdx.x % T;
-  int64_t row = (int64_t)(blockIdx.x - a.first[i]);
+  int64_t row = (int64_t)(blockIdx.x - first);
   if constexpr (T == 64) row = row * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
-  if (row >= n) return;
+  if (row >= p.rows) return;
   if (p.dtype == SK_F32) norm_row<T, P, ONCE, SK_F32, SK_F32>(p, row, t, red);
   else if (p.dtype == SK_BF16 && p.residual_dtype == SK_BF16) norm_row<T, P, ONCE, SK_BF16, SK_BF16>(p, row, t, red);
   else if (p.dtype == SK_BF16) norm_row<T, P, ONCE, SK_BF16, SK_F32>(p, row, t, red);
@@ -195,10 +232,21 @@ struct sk_norm_plan : sk::PlanOnDevice {
 
 namespace {
 
+sk_status upload(sk_norm_plan &plan) {
+  const std::vector<sk::NormLaunch> &launches = plan.host.launches;
+  if (launches.empty()) return SK_OK;
+  std::vector<char> image(launches.size() * sizeof(sk::NormTable));
+  for (size_t i = 0; i < launches.size(); ++i) std::memcpy(image.data() + i * sizeof(sk::NormTable), &launches[i].table, sizeof(sk::NormTable));
+  char *ws = nullptr;
+  const sk_status st = sk::upload_image(plan, image, 0, &ws);
+  return st == SK_OK ? sk::copy_image(plan, image) : st;
+}
+
 void (*norm_kernel(sk::NormForm form, bool once))(sk::NormArgs) {
   switch (form) {
     case sk::NORM_WAVE: return once ? sk::sk_norm<64, 4, true> : sk::sk_norm<64, 4, false>;
-    case sk::NORM_GROUP: return once ? sk::sk_norm<256, 4, true> : sk::sk_norm<256, 4, false>;
+    case sk::NORM_GROUP: return once ? sk::sk_norm<256, 2, true> : sk::sk_norm<256, 2, false>;
+    case sk::NORM_PAIR: return once ? sk::sk_norm<512, 2, true> : sk::sk_norm<512, 2, false>;
     default: return once ? sk::sk_norm<1024, 4, true> : sk::sk_norm<1024, 4, false>;
   }
 }
@@ -213,7 +261,7 @@ void sk_layer_params_default(sk_layer_params *params) {
 
 sk_status sk_norm_plan_create(const sk_norm_problem *problems, int32_t n, const sk_layer_params *params, sk_norm_plan **out) {
   return sk::create_plan<sk_norm_plan>(params, out, [&](sk_norm_plan &plan, int32_t, int32_t, std::string &err) { return sk::plan_norm(problems, n, plan.host, err); },
-                                       [](sk_norm_plan &) { return SK_OK; });
+                                       upload);
 }
 
 sk_status sk_norm_plan_destroy(sk_norm_plan *plan) {
@@ -225,9 +273,10 @@ sk_status sk_norm_launch(sk_norm_plan *plan, void *hip_stream) {
   return sk::guarded([&]() -> sk_status {
     sk_status st = sk::check_resident(plan);
     if (st != SK_OK) return st;
+    const sk::NormTable *table = (const sk::NormTable *)plan->blob;
     for (const sk::NormLaunch &l : plan->host.launches) {
       if (st != SK_OK) break;
-      st = sk::launch(norm_kernel(l.form, l.once), l.grid, (hipStream_t)hip_stream, nullptr, l.args, l.form == sk::NORM_LONG ? sk::NORM_LONG_THREADS : sk::CACHE_THREADS);
+      st = sk::launch(norm_kernel(l.form, l.once), l.grid, (hipStream_t)hip_stream, nullptr, sk::NormArgs{table++, l.n}, sk::norm_threads(l.form));
       plan->launched = true;
     }
     return st;

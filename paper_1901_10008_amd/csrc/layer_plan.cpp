@@ -71,6 +71,8 @@ struct Layout {
 
 // Rows of up to 2048 elements get a wave each from that many rows on; fewer get a workgroup each, whose threads have a quarter of the work each.
 constexpr int32_t NORM_WAVE_ROWS = 2048;
+// Problems of up to that many rows in all go together in the form of the longest of them: a launch costs more than idle threads.
+constexpr int64_t NORM_STEP_ROWS = 1024;
 
 sk_status plan_norm(const sk_norm_problem *problems, int32_t n, NormPlanHost &out, std::string &err) {
   Spans written;
@@ -81,6 +83,7 @@ sk_status plan_norm(const sk_norm_problem *problems, int32_t n, NormPlanHost &ou
   };
   std::vector<Item> items;
   double bytes = 0.0;
+  int64_t all_rows = 0;
   const sk_status st = each(problems, n, err, [&](const sk_norm_problem &p) -> sk_status {
     if (!known(p.dtype)) return refuse(err, SK_ERR_UNSUPPORTED, "dtype must be SK_F32, SK_BF16 or SK_F16");
     if (p.residual_dtype != p.dtype && p.residual_dtype != SK_F32) return refuse(err, SK_ERR_UNSUPPORTED, "residual_dtype must be dtype or SK_F32");
@@ -114,27 +117,36 @@ sk_status plan_norm(const sk_norm_problem *problems, int32_t n, NormPlanHost &ou
     d.rows = p.rows, d.dim = p.dim, d.eps = p.eps;
     d.residual_scale = p.residual_scale != 0.f ? p.residual_scale : 1.f, d.block_scale = p.block_scale != 0.f ? p.block_scale : 1.f;
     d.dtype = (int8_t)p.dtype, d.residual_dtype = (int8_t)p.residual_dtype, d.kind = (int8_t)p.kind, d.post = (int8_t)p.post, d.act = (int8_t)p.gate_act;
-    const NormForm form = dim > norm_most_dim(NORM_GROUP) ? NORM_LONG : dim > norm_most_dim(NORM_WAVE) || p.rows < NORM_WAVE_ROWS ? NORM_GROUP : NORM_WAVE;
+    const NormForm form = p.rows >= NORM_WAVE_ROWS && dim <= norm_most_dim(NORM_WAVE) ? NORM_WAVE
+                          : dim <= norm_most_dim(NORM_GROUP)                           ? NORM_GROUP
+                          : dim <= norm_most_dim(NORM_PAIR)                            ? NORM_PAIR
+                                                                                       : NORM_LONG;
     const int64_t groups = form == NORM_WAVE ? ((int64_t)p.rows + 3) / 4 : p.rows;
-    if (groups > (form == NORM_LONG ? NORM_LONG_GRID : MOST_GRID)) return refuse(err, SK_ERR_UNSUPPORTED, "more rows than a launch's grid can hold");
+    if (groups > norm_most_grid(form)) return refuse(err, SK_ERR_UNSUPPORTED, "more rows than a launch's grid can hold");
+    all_rows += p.rows;
     bytes += (double)p.rows * dim * (double)(one * ((p.block != nullptr) + (d.gate && p.gate_rows) + (p.next != nullptr)) + res * ((p.residual != nullptr) + (p.residual_out != nullptr)));
     items.push_back(Item{form, d, groups});
     return SK_OK;
   });
   if (st != SK_OK) return st;
   if (written.overlap()) return refuse(err, SK_ERR_OVERLAP, "ranges of residual_out and next overlap");
+  if (all_rows <= NORM_STEP_ROWS) {
+    NormForm longest = NORM_WAVE;
+    for (const Item &it : items) longest = std::max(longest, it.form);
+    for (Item &it : items) it.form = longest;  // (none of them is a wave's)
+  }
   for (int f = 0; f < NORM_FORMS; ++f) {
     NormLaunch *l = nullptr;
     for (const Item &it : items) {
       if (it.form != (NormForm)f) continue;
-      if (!l || l->n == NORM_PROBLEMS || l->grid + it.groups > (f == NORM_LONG ? NORM_LONG_GRID : MOST_GRID)) {
+      if (!l || l->n == NORM_PROBLEMS || l->grid + it.groups > norm_most_grid((NormForm)f)) {
         out.launches.emplace_back();
         l = &out.launches.back();
         l->form = (NormForm)f, l->once = bytes > (double)PAST_CACHES, l->grid = 0, l->n = 0;
-        for (uint32_t &first : l->args.first) first = 0xffffffffu;
+        for (uint32_t &first : l->table.first) first = 0xffffffffu;
       }
-      l->args.problems[l->n] = it.dev;
-      l->args.first[l->n++] = (uint32_t)l->grid;
+      l->table.problems[l->n] = it.dev;
+      l->table.first[l->n++] = (uint32_t)l->grid;
       l->grid += it.groups;
     }
   }
@@ -282,10 +294,10 @@ sk_status plan_verify(const sk_verify_problem *problems, int32_t n, VerifyPlanHo
       out.launches.emplace_back();
       l = &out.launches.back();
       l->n = 0, l->stat_grid = l->sum_grid = 0;
-      for (int i = 0; i < VERIFY_PROBLEMS; ++i) l->args.stat_first[i] = l->args.sum_first[i] = 0xffffffffu;
+      for (int i = 0; i < VERIFY_PROBLEMS; ++i) l->table.stat_first[i] = l->table.sum_first[i] = 0xffffffffu;
     }
-    l->args.problems[l->n] = d;
-    l->args.stat_first[l->n] = (uint32_t)l->stat_grid, l->args.sum_first[l->n++] = (uint32_t)l->sum_grid;
+    l->table.problems[l->n] = d;
+    l->table.stat_first[l->n] = (uint32_t)l->stat_grid, l->table.sum_first[l->n++] = (uint32_t)l->sum_grid;
     l->stat_grid += stat, l->sum_grid += sum;
     return SK_OK;
   });

@@ -4,6 +4,11 @@
 
 namespace sk {
 
+struct VerifyArgs {
+  const VerifyTable *table;
+  int32_t n;
+};
+
 // 2^(d c) to 8e-13 of itself, for -1000 < d c <= 0: 2^f of what the nearest whole number leaves, |f| <= 1/2, by the polynomial of degree 8 with the least
 // largest relative error, which moves a border between two tokens by less than one in 10^12 of the sum.  Fused multiplications and additions of
 // 64 bits have the rate of those of 32 here; there is no exponential of 64 bits in the hardware.
@@ -28,7 +33,7 @@ __device__ __forceinline__ double exp2_of(double d, double c) {
 __device__ __forceinline__ double weight_of(double d, double c) { return d * c > -1000.0 ? exp2_of(d, c) : 0.0; }
 
 // log2(e) / temperature of a sequence; 0: the first of the largest.
-__device__ __forceinline__ double scale_of(const VerifyDev &P, int32_t seq) {
+__device__ __forceinline__ double scale_of(const SK_CONSTANT VerifyDev &P, int32_t seq) {
   const float t = P.temperatures ? load_f(P.temperatures + seq) : P.temperature;
   return t > 0.f ? fmax(1.4426950408889634074 / (double)t, 1e-300) : 0.0;  // (not 0 where t is infinite)
 }
@@ -96,13 +101,13 @@ struct VerifyShared {
   int32_t chunk, found;
 };
 
-__device__ __forceinline__ int32_t first_of(const VerifyDev &P, int32_t s) { return min(max(load_i32(P.first_row + s), 0), P.rows); }
+__device__ __forceinline__ int32_t first_of(const SK_CONSTANT VerifyDev &P, int32_t s) { return min(max(load_i32(P.first_row + s), 0), P.rows); }
 
 // The sequence that a row belongs to; none: rows of no sequence, and of sequences whose numbers of rows make no sense.
 struct Owner {
   int32_t seq, begin, end;
 };
-__device__ __forceinline__ Owner owner_of(const VerifyDev &P, int32_t row, int lane) {
+__device__ __forceinline__ Owner owner_of(const SK_CONSTANT VerifyDev &P, int32_t row, int lane) {
   Owner o;
   if (P.sequences <= 64) {  // a sequence a lane
     const int32_t s = min(lane, P.sequences - 1), begin = first_of(P, s), end = first_of(P, s + 1);
@@ -118,7 +123,7 @@ __device__ __forceinline__ Owner owner_of(const VerifyDev &P, int32_t row, int l
 // A chunk of a row, 512 * PIECES logits, by a wave: a lane has eight of each piece, takes them relative to its own largest, and the lanes are joined at
 // the end.  Bound by the vector unit (17 instructions a logit, 16-bit logits) about as much as by memory.
 template <int DT, int PIECES>
-__device__ __forceinline__ void chunk_stat(const VerifyDev &P, const char *from, int32_t chunk, double c, VerifyStat *out, int lane) {
+__device__ __forceinline__ void chunk_stat(const SK_CONSTANT VerifyDev &P, const char *from, int32_t chunk, double c, VerifyStat *out, int lane) {
   Eight<DT> raw[PIECES];
   const int32_t at0 = chunk * 512 * PIECES;
 #pragma unroll
@@ -167,7 +172,7 @@ __device__ __forceinline__ void chunk_stat(const VerifyDev &P, const char *from,
 }
 
 template <int DT>
-__device__ __forceinline__ void row_chunk(const VerifyDev &P, uint32_t unit, int lane) {
+__device__ __forceinline__ void row_chunk(const SK_CONSTANT VerifyDev &P, uint32_t unit, int lane) {
   const uint32_t sides = P.draft_logits ? 2 : 1, line = unit / (uint32_t)P.chunks;
   const int32_t chunk = (int32_t)(unit - line * (uint32_t)P.chunks), row = (int32_t)(line / sides);
   const bool draft = sides == 2 && (line & 1);
@@ -185,11 +190,16 @@ __device__ __forceinline__ void row_chunk(const VerifyDev &P, uint32_t unit, int
 }
 
 __global__ void __launch_bounds__(CACHE_THREADS, 5) sk_verify_stats(VerifyArgs a) {
+  const SK_CONSTANT VerifyTable &table = *(const SK_CONSTANT VerifyTable *)(uintptr_t)a.table;
   int i = 0;
+  uint32_t first = 0;
+  if (a.n > 1) {
 #pragma unroll
-  for (int k = 1; k < VERIFY_PROBLEMS; ++k) i += a.stat_first[k] <= blockIdx.x ? 1 : 0;
-  const VerifyDev &P = a.problems[i];
-  const uint32_t unit = (blockIdx.x - a.stat_first[i]) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    for (int k = 1; k < VERIFY_PROBLEMS; ++k) i += table.stat_first[k] <= blockIdx.x ? 1 : 0;
+    first = table.stat_first[i];
+  }
+  const SK_CONSTANT VerifyDev &P = table.problems[i];
+  const uint32_t unit = (blockIdx.x - first) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   if (P.dtype == SK_F32) row_chunk<SK_F32>(P, unit, lane);
   else if (P.dtype == SK_BF16) row_chunk<SK_BF16>(P, unit, lane);
@@ -257,7 +267,7 @@ __device__ __forceinline__ void weights8(const Draw &d, const Eight<DT> &p, cons
 
 // The weights of a chunk, by a workgroup: a wave has two of its eight pieces, whose sums go to LDS.  Returns the chunk's sum.
 template <int DT>
-__device__ __forceinline__ double chunk_weights(const VerifyDev &P, const Draw &d, const char *p_row, const char *q_row, int32_t chunk, double c, double (&w)[2][8], int32_t (&places)[2],
+__device__ __forceinline__ double chunk_weights(const SK_CONSTANT VerifyDev &P, const Draw &d, const char *p_row, const char *q_row, int32_t chunk, double c, double (&w)[2][8], int32_t (&places)[2],
                                                 VerifyShared &s, int tid) {
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
@@ -297,7 +307,7 @@ __device__ __forceinline__ double chunk_weights(const VerifyDev &P, const Draw &
 
 // The sum of a chunk's weights, by a wave, in all lanes.
 template <int DT>
-__device__ __forceinline__ double chunk_sum(const VerifyDev &P, const Draw &d, const char *p_row, const char *q_row, int32_t chunk, double c, int lane) {
+__device__ __forceinline__ double chunk_sum(const SK_CONSTANT VerifyDev &P, const Draw &d, const char *p_row, const char *q_row, int32_t chunk, double c, int lane) {
   Eight<DT> p, q, p_next, q_next;
   int32_t at = chunk * 512 * P.pieces;
   p.template load<true>(p_row, at, lane, P.vocab);
@@ -320,7 +330,7 @@ __device__ __forceinline__ double chunk_sum(const VerifyDev &P, const Draw &d, c
 // The first token whose weight and those before it add up to more than `random` times all, by a workgroup.  sum_of(i) is the sum of chunk i (asked for
 // by the first wave).  -1: all weights are 0.
 template <int DT, class F>
-__device__ __forceinline__ int32_t pick(const VerifyDev &P, const Draw &d, const char *p_row, const char *q_row, double c, double random, F sum_of, VerifyShared &s, int tid) {
+__device__ __forceinline__ int32_t pick(const SK_CONSTANT VerifyDev &P, const Draw &d, const char *p_row, const char *q_row, double c, double random, F sum_of, VerifyShared &s, int tid) {
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   __syncthreads();
   if (wave == 0) {
@@ -400,7 +410,7 @@ __device__ __forceinline__ double random_of(const float *p) {
 
 // What becomes of a sequence's drafts: by all waves, a row each at a time.
 template <int DT>
-__device__ __forceinline__ void decide(const VerifyDev &P, int32_t r0, int32_t n, double c, Draw *draws, int32_t *stop, int tid, Draw &out) {
+__device__ __forceinline__ void decide(const SK_CONSTANT VerifyDev &P, int32_t r0, int32_t n, double c, Draw *draws, int32_t *stop, int tid, Draw &out) {
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   if (tid == 0) *stop = 0x7fffffff;
   __syncthreads();
@@ -456,7 +466,7 @@ __device__ __forceinline__ void decide(const VerifyDev &P, int32_t r0, int32_t n
 }
 
 template <int DT>
-__device__ __forceinline__ void sample(const VerifyDev &P, int32_t seq, int32_t part, VerifyShared &s, Draw *draws, int32_t *stop, uint32_t *flag, int tid) {
+__device__ __forceinline__ void sample(const SK_CONSTANT VerifyDev &P, int32_t seq, int32_t part, VerifyShared &s, Draw *draws, int32_t *stop, uint32_t *flag, int tid) {
   const int32_t r0 = first_of(P, seq), n = first_of(P, seq + 1) - r0;
   if (n <= 0) {
     if (part == 0 && tid == 0) P.accepted[seq] = 0;
@@ -503,11 +513,16 @@ __global__ void __launch_bounds__(CACHE_THREADS, 4) sk_verify_sample(VerifyArgs 
   __shared__ int32_t stop;
   __shared__ uint32_t flag;
   const int tid = threadIdx.x;
+  const SK_CONSTANT VerifyTable &table = *(const SK_CONSTANT VerifyTable *)(uintptr_t)a.table;
   int i = 0;
+  uint32_t first = 0;
+  if (a.n > 1) {
 #pragma unroll
-  for (int k = 1; k < VERIFY_PROBLEMS; ++k) i += a.sum_first[k] <= blockIdx.x ? 1 : 0;
-  const VerifyDev &P = a.problems[i];
-  const uint32_t unit = blockIdx.x - a.sum_first[i];
+    for (int k = 1; k < VERIFY_PROBLEMS; ++k) i += table.sum_first[k] <= blockIdx.x ? 1 : 0;
+    first = table.sum_first[i];
+  }
+  const SK_CONSTANT VerifyDev &P = table.problems[i];
+  const uint32_t unit = blockIdx.x - first;
   const uint32_t parts = ((uint32_t)P.chunks + VERIFY_CHUNKS - 1) / VERIFY_CHUNKS;
   const int32_t seq = (int32_t)(unit / parts), part = (int32_t)(unit % parts);
   if (P.dtype == SK_F32) sample<SK_F32>(P, seq, part, shared, draws, &stop, &flag, tid);
@@ -523,20 +538,24 @@ struct sk_verify_plan : sk::PlanOnDevice {
 
 namespace {
 
-// (the problems travel in the launches' arguments; on the device are the counters and the workspace)
 sk_status upload(sk_verify_plan &plan) {
   sk::VerifyPlanHost &h = plan.host;
   if (h.launches.empty()) return SK_OK;
-  const std::vector<char> image(h.counters, 0);
+  // tables, counters
+  const size_t o_counters = sk::align_up(h.launches.size() * sizeof(sk::VerifyTable), 256);
+  std::vector<char> image(o_counters + h.counters, 0);
   char *ws = nullptr;
   const sk_status st = sk::upload_image(plan, image, h.workspace, &ws);
   if (st != SK_OK) return st;
   auto moved = [](auto *&p, char *base) { p = (std::decay_t<decltype(p)>)(base + (uintptr_t)p); };
-  for (sk::VerifyLaunch &l : h.launches)
-    for (int32_t i = 0; i < l.n; ++i) {
-      sk::VerifyDev &d = l.args.problems[i];
-      moved(d.arrived, plan.blob), moved(d.stats, ws), moved(d.sums, ws);
+  for (size_t k = 0; k < h.launches.size(); ++k) {
+    sk::VerifyTable table = h.launches[k].table;
+    for (int32_t i = 0; i < h.launches[k].n; ++i) {
+      sk::VerifyDev &d = table.problems[i];
+      moved(d.arrived, plan.blob + o_counters), moved(d.stats, ws), moved(d.sums, ws);
     }
+    std::memcpy(image.data() + k * sizeof(table), &table, sizeof(table));
+  }
   return sk::copy_image(plan, image);
 }
 
@@ -560,9 +579,12 @@ sk_status sk_verify_launch(sk_verify_plan *plan, void *hip_stream) {
     sk_status st = sk::admit(plan, stream, &in_capture);
     if (st != SK_OK || plan->host.launches.empty()) return st;
     const hipEvent_t behind = in_capture ? nullptr : plan->last_use;
+    sk::VerifyArgs args{(const sk::VerifyTable *)plan->blob, 0};
     for (const sk::VerifyLaunch &l : plan->host.launches) {
-      if (st == SK_OK) st = sk::launch(sk::sk_verify_stats, l.stat_grid, stream, nullptr, l.args);
-      if (st == SK_OK) st = sk::launch(sk::sk_verify_sample, l.sum_grid, stream, &l == &plan->host.launches.back() ? behind : nullptr, l.args);
+      args.n = l.n;
+      if (st == SK_OK) st = sk::launch(sk::sk_verify_stats, l.stat_grid, stream, nullptr, args);
+      if (st == SK_OK) st = sk::launch(sk::sk_verify_sample, l.sum_grid, stream, &l == &plan->host.launches.back() ? behind : nullptr, args);
+      ++args.table;
     }
     plan->ledger.after_launch((uintptr_t)stream, in_capture, behind && st == SK_OK);  // also after a failure: some launches may be out
     return st;

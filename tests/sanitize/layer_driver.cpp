@@ -50,12 +50,12 @@ static void norms() {
     need(l.n >= 1 && l.n <= sk::NORM_PROBLEMS, "problems of a launch");
     for (int i = 0; i < sk::NORM_PROBLEMS; ++i) {
       if (i >= l.n) {
-        need(l.args.first[i] == 0xffffffffu, "a place without a problem can be found");
+        need(l.table.first[i] == 0xffffffffu, "a place without a problem can be found");
         continue;
       }
-      const sk::NormDev &d = l.args.problems[i];
+      const sk::NormDev &d = l.table.problems[i];
       need(d.dim <= sk::norm_most_dim(l.form), "a row longer than its form takes");
-      const int64_t end = i + 1 < l.n ? l.args.first[i + 1] : l.grid, groups = end - l.args.first[i];
+      const int64_t end = i + 1 < l.n ? l.table.first[i + 1] : l.grid, groups = end - l.table.first[i];
       need(l.form == sk::NORM_WAVE ? groups * 4 >= d.rows && (groups - 1) * 4 < d.rows : groups == d.rows, "workgroups of a problem");
       ++seen;
     }
@@ -233,14 +233,14 @@ static void verifications() {
     need(l.n >= 1 && l.n <= sk::VERIFY_PROBLEMS, "problems of a launch");
     for (int i = 0; i < sk::VERIFY_PROBLEMS; ++i) {
       if (i >= l.n) {
-        need(l.args.stat_first[i] == 0xffffffffu && l.args.sum_first[i] == 0xffffffffu, "a place without a problem can be found");
+        need(l.table.stat_first[i] == 0xffffffffu && l.table.sum_first[i] == 0xffffffffu, "a place without a problem can be found");
         continue;
       }
-      const sk::VerifyDev &d = l.args.problems[i];
+      const sk::VerifyDev &d = l.table.problems[i];
       need(d.rows == problems[(size_t)seen].rows && d.vocab == problems[(size_t)seen].vocab, "problems in their order");
       need(d.pieces >= 1 && d.pieces <= 8 && (int64_t)d.chunks * d.pieces * 512 >= d.vocab && ((int64_t)d.chunks - 1) * d.pieces * 512 < d.vocab, "chunks");
-      need((i + 1 < l.n ? l.args.stat_first[i + 1] : l.stat_grid) - l.args.stat_first[i] == ((int64_t)d.rows * (d.draft_logits ? 2 : 1) * d.chunks + 3) / 4, "units of the rows");
-      need((i + 1 < l.n ? l.args.sum_first[i + 1] : l.sum_grid) - l.args.sum_first[i] == (int64_t)d.sequences * ((d.chunks + sk::VERIFY_CHUNKS - 1) / sk::VERIFY_CHUNKS), "units of the sequences");
+      need((i + 1 < l.n ? l.table.stat_first[i + 1] : l.stat_grid) - l.table.stat_first[i] == ((int64_t)d.rows * (d.draft_logits ? 2 : 1) * d.chunks + 3) / 4, "units of the rows");
+      need((i + 1 < l.n ? l.table.sum_first[i + 1] : l.sum_grid) - l.table.sum_first[i] == (int64_t)d.sequences * ((d.chunks + sk::VERIFY_CHUNKS - 1) / sk::VERIFY_CHUNKS), "units of the sequences");
       counters.next(d.arrived, (int64_t)d.sequences * sk::COUNTER_STEP);
       work.next(d.stats, (int64_t)d.rows * 2 * d.chunks), work.next(d.sums, (int64_t)d.sequences * d.chunks);
       ++seen;
