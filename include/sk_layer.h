@@ -87,7 +87,8 @@ typedef struct sk_norm_plan sk_norm_plan; /* opaque, owned by the library */
 sk_status sk_norm_plan_create(const sk_norm_problem *problems, int32_t n, const sk_layer_params *params, sk_norm_plan **out);
 /* Waits for the device's work and frees the plan; null is accepted. */
 sk_status sk_norm_plan_destroy(sk_norm_plan *plan);
-/* One kernel launch for up to 16 problems of one kind of work (rows of up to 2048, 4096, 8192 or more elements; all of them if they have 1024 rows or fewer). */
+/* One kernel launch for up to 16 problems of one kind of work (rows of up to 4096, 8192 or more elements; of 2048 rows or more up to 256, 1024 or 2048; all of
+   them if they have 1024 rows or fewer). */
 sk_status sk_norm_launch(sk_norm_plan *plan, void *hip_stream);
 
 /* ---- mixture-of-experts layer -------------------------------------------------------------------------------------------

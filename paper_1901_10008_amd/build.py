@@ -20,6 +20,7 @@ CACHE_UNITS = 4  # units of compilation of cache_instances.hip
 
 LAYER_LIB = os.path.join(HERE, "libsk_layer.so")  # the rest of a decoder step (include/sk_layer.h)
 LAYER_SOURCES = ["layer_norm.hip", "layer_moe.hip", "layer_verify.hip", "layer_plan.cpp"]
+NORM_UNITS = 6  # units of compilation of layer_norm_instances.hip
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -130,10 +131,12 @@ def build_layer(verbose: bool = False, extra=(), lib: str = LAYER_LIB) -> str:
     objects = [os.path.join(obj_dir, os.path.splitext(s)[0] + ".o") for s in LAYER_SOURCES]
     compiles = [[hipcc, *HIPCC_FLAGS, *extra, *inc, "-c", os.path.join(CSRC, s), "-o", o] if s.endswith(".hip") else
                 ["g++", "-O2", "-std=c++17", "-fPIC", "-Wall", *inc, "-c", os.path.join(CSRC, s), "-o", o] for s, o in zip(LAYER_SOURCES, objects)]
+    units = [os.path.join(obj_dir, f"layer_norm_instances{u}.o") for u in range(NORM_UNITS)]
+    compiles = [[hipcc, *HIPCC_FLAGS, *extra, *inc, f"-DSK_UNIT={u}", "-c", os.path.join(CSRC, "layer_norm_instances.hip"), "-o", o] for u, o in enumerate(units)] + compiles
     run = _runner(verbose)
     with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:
         list(pool.map(run, compiles))
-    run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *objects, "-L", HERE, "-l:libsuperkernel.so", "-Wl,-rpath,$ORIGIN", "-Wl,--no-undefined", "-o", lib])
+    run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *objects, *units, "-L", HERE, "-l:libsuperkernel.so", "-Wl,-rpath,$ORIGIN", "-Wl,--no-undefined", "-o", lib])
     return lib
 
 

@@ -35,10 +35,14 @@ struct NormTable {
   NormDev problems[NORM_PROBLEMS];
 };
 
-// What a row gets: a wave, or a workgroup of four, eight or sixteen, with up to 4, 2, 2 or 4 pieces of 8 elements a thread.
-enum NormForm { NORM_WAVE, NORM_GROUP, NORM_PAIR, NORM_LONG, NORM_FORMS };
-constexpr int norm_threads(NormForm f) { return f == NORM_LONG ? 1024 : f == NORM_PAIR ? 512 : 256; }  // of a workgroup
-constexpr int norm_most_dim(NormForm f) { return f == NORM_WAVE ? 2048 : f == NORM_GROUP ? 4096 : f == NORM_PAIR ? 8192 : 32768; }
+// What a row gets, and up to how many elements it has: where there are many rows sixteen lanes (256), a wave (1024) or a workgroup of two waves (2048),
+// otherwise a workgroup of four (4096), eight (8192) or sixteen (32768).
+enum NormForm { NORM_SIXTEEN, NORM_WAVE, NORM_ROWS, NORM_GROUP, NORM_PAIR, NORM_LONG, NORM_FORMS };
+constexpr int norm_threads(NormForm f) { return f == NORM_LONG ? 1024 : f == NORM_PAIR ? 512 : f == NORM_ROWS ? 128 : 256; }  // of a workgroup
+constexpr int norm_rows_of(NormForm f) { return f == NORM_SIXTEEN ? 16 : f == NORM_WAVE ? 4 : 1; }  // of a workgroup
+constexpr int norm_most_dim(NormForm f) {
+  return f == NORM_SIXTEEN ? 256 : f == NORM_WAVE ? 1024 : f == NORM_ROWS ? 2048 : f == NORM_GROUP ? 4096 : f == NORM_PAIR ? 8192 : 32768;
+}
 constexpr int64_t norm_most_grid(NormForm f) { return (((int64_t)1 << 32) - 1) / norm_threads(f); }
 
 struct NormLaunch {

@@ -1,228 +1,18 @@
-// Norms before and after a block, with its gate and scales: the kernel and its entry points.
+// Norms before and after a block: entry points.
 #include "layer_host.h"
-#include "layer_math.hip.h"
+#include "layer_norm.hip.h"
 
 namespace sk {
-
-// A row lives in the registers of T threads, P pieces of 8 elements each, from its loads to its stores.
-//
-//   u = N(block) w + b,  r = rs * residual + bs * u * act(gate),  next = N(r) w' + b'
-//
-// Each norm is one sum over the row, or two (the mean, then the squares of what lies beside it: nothing cancels).  All of a row's loads, those of the
-// weights among them, are on their way before the number of rows is known and before the first sum.
-struct NormArgs {
-  const NormTable *table;
-  int32_t n;
-};
-template <int T>
-struct RowSum {
-  float (*red)[16];
-  int wave, turn = 0;
-  __device__ __forceinline__ float operator()(float v) {
-    v = wave_sum(v);
-    if constexpr (T > 64) {  // each sum of a row has a place of its own, so that one barrier is enough
-      red[turn][wave] = v;
-      __syncthreads();
-      v = 0.f;
-#pragma unroll
-      for (int w = 0; w < T / 64; ++w) v += red[turn][w];
-      ++turn;
-    }
-    return v;
-  }
-};
-
-template <int T, int P, bool ONCE, int DT, int RT>
-__device__ __forceinline__ void norm_row(const SK_CONSTANT NormDev &p, int64_t row, int t, float (*red)[16]) {
-  constexpr int ES = DT == SK_F32 ? 4 : 2, RS = RT == SK_F32 ? 4 : 2;
-  constexpr bool LATE = T > 512 || DT == SK_F32;  // gates and weights are loaded when they are wanted: there are not the registers to keep them
-  const int dim = p.dim;
-  const float by = 1.f / (float)dim;
-  RowSum<T> sum{red, t >> 6};
-  using Own = std::integral_constant<int, DT>;
-  using Res = std::integral_constant<int, RT>;
-
-  // pieces of 8 elements as they come; the last one of a row may be shorter: only its elements are read and written
-  auto load = [&](auto type, bool once, const void *base, int i, u32x4 *raw) {
-    constexpr int D = decltype(type)::value, S = D == SK_F32 ? 4 : 2;
-    const int at = (i * T + t) * 8;
-    const char *q = (const char *)base + (int64_t)at * S;
-    if (at + 8 <= dim) {
-#pragma unroll
-      for (int j = 0; j < S / 2; ++j) {
-        const u32x4_any SK_GLOBAL *g = (const u32x4_any SK_GLOBAL *)(uintptr_t)(q + 16 * j);
-        raw[j] = ONCE && once ? (u32x4)__builtin_nontemporal_load(g) : (u32x4)*g;
-      }
-    } else {
-      uint32_t e[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const char *g = (const char *)base + (int64_t)min(at + k, dim - 1) * S;
-        e[k] = S == 4 ? *(const uint32_t SK_GLOBAL *)(uintptr_t)g : load_u16(g);
-        e[k] = at + k < dim ? e[k] : 0u;
-      }
-      if constexpr (S == 4) raw[0] = u32x4{e[0], e[1], e[2], e[3]}, raw[1] = u32x4{e[4], e[5], e[6], e[7]};
-      else raw[0] = u32x4{e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16};
-    }
-  };
-  auto values = [&](auto type, const u32x4 *raw, float(&x)[8]) {
-    constexpr int D = decltype(type)::value;
-    if constexpr (D == SK_F32) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] = __builtin_bit_cast(float, (uint32_t)raw[k / 4][k % 4]);
-    } else {
-      unpack8<D>(raw[0], x);
-    }
-  };
-  auto store = [&](auto type, char *base, int i, const float(&x)[8]) {
-    constexpr int D = decltype(type)::value, S = D == SK_F32 ? 4 : 2;
-    const int at = (i * T + t) * 8;
-    if (at >= dim) return;
-    char *q = base + (int64_t)at * S;
-    if (at + 8 <= dim) {
-      store8_elements<D, ONCE>(q, x);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (at + k < dim) store1<D>(q + k * S, x[k]);
-    }
-  };
-  auto each_piece = [&](auto f) {
-#pragma unroll
-    for (int i = 0; i < P; ++i)
-      if (i * T * 8 < dim) f(i);
-  };
-
-  const char *block = p.block ? (const char *)p.block + row * p.block_stride * ES : nullptr;
-  const char *gate = p.gate ? (const char *)p.gate + row * p.gate_stride * ES : nullptr;
-  const char *residual = p.residual ? (const char *)p.residual + row * p.residual_stride * RS : nullptr;
-  const bool post = block && p.post, post_weight = post && p.post_weight, pre_weight = p.next && p.pre_weight;
-  u32x4 block_raw[P][ES / 2], gate_raw[P][ES / 2], residual_raw[P][RS / 2], post_raw[P][ES / 2], pre_raw[P][ES / 2];
-  each_piece([&](int i) {
-    if (block) load(Own{}, true, block, i, block_raw[i]);
-    if (residual) load(Res{}, true, residual, i, residual_raw[i]);
-  });
-  if (!LATE) {
-    each_piece([&](int i) {
-      if (gate) load(Own{}, p.gate_stride != 0, gate, i, gate_raw[i]);
-      if (post_weight) load(Own{}, false, p.post_weight, i, post_raw[i]);
-      if (pre_weight) load(Own{}, false, p.pre_weight, i, pre_raw[i]);
-    });
-  }
-  if (p.n_rows && row >= load_i32(p.n_rows)) return;
-
-  // x becomes x - mean, and what it is to be multiplied by is returned
-  auto standard = [&](float(&x)[P][8]) {
-    float s = 0.f;
-    if (p.kind == SK_NORM_LAYER) {
-      each_piece([&](int i) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) s += x[i][k];
-      });
-      const float mean = sum(s) * by;
-      each_piece([&](int i) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) x[i][k] = (i * T + t) * 8 + k < dim ? x[i][k] - mean : 0.f;
-      });
-    }
-    s = 0.f;
-    each_piece([&](int i) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) s += x[i][k] * x[i][k];
-    });
-    return 1.f / sqrtf(sum(s) * by + p.eps);
-  };
-  // y = x * scale * weight + bias
-  auto weighted = [&](int i, const float(&x)[8], float scale, const void *weight, u32x4 *raw, const void *bias, float(&y)[8]) {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) y[k] = x[k] * scale;
-    if (weight) {
-      float w[8];
-      if (LATE) load(Own{}, false, weight, i, raw);
-      values(Own{}, raw, w);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) y[k] *= w[k];
-    }
-    if (bias) {
-      float b[8];
-      u32x4 bias_raw[ES / 2];
-      load(Own{}, false, bias, i, bias_raw);
-      values(Own{}, bias_raw, b);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) y[k] += b[k];
-    }
-  };
-
-  float u[P][8], r[P][8];
-  if (block) {
-    each_piece([&](int i) { values(Own{}, block_raw[i], u[i]); });
-    const float scale = post ? standard(u) : 1.f;
-    each_piece([&](int i) {
-      if (post) weighted(i, u[i], scale, p.post_weight, post_raw[i], p.post_bias, u[i]);
-    });
-    auto gated = [&](auto act) {
-      each_piece([&](int i) {
-        float g[8];
-        if (LATE) load(Own{}, p.gate_stride != 0, gate, i, gate_raw[i]);
-        values(Own{}, gate_raw[i], g);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) u[i][k] *= activated(decltype(act)::value, g[k]);
-      });
-    };
-    if (gate) {
-      switch (p.act) {
-        case SK_ACT_SIGMOID: gated(std::integral_constant<int, SK_ACT_SIGMOID>{}); break;
-        case SK_ACT_SILU: gated(std::integral_constant<int, SK_ACT_SILU>{}); break;
-        case SK_ACT_TANH: gated(std::integral_constant<int, SK_ACT_TANH>{}); break;
-        case SK_ACT_GELU: gated(std::integral_constant<int, SK_ACT_GELU>{}); break;
-        case SK_ACT_RELU: gated(std::integral_constant<int, SK_ACT_RELU>{}); break;
-        default: gated(std::integral_constant<int, SK_ACT_NONE>{});
-      }
-    }
-  }
-  each_piece([&](int i) {
-    // (a missing part adds nothing, not its scale times 0)
-    if (residual) values(Res{}, residual_raw[i], r[i]);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) r[i][k] = !block ? p.residual_scale * r[i][k] : !residual ? p.block_scale * u[i][k] : p.residual_scale * r[i][k] + p.block_scale * u[i][k];
-    if (p.post_bias) {  // (a bias stands behind the row's end as well)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) r[i][k] = (i * T + t) * 8 + k < dim ? r[i][k] : 0.f;
-    }
-    if (p.residual_out) store(Res{}, (char *)p.residual_out + row * p.residual_out_stride * RS, i, r[i]);
-  });
-  if (!p.next) return;
-  const float scale = standard(r);
-  each_piece([&](int i) {
-    float y[8];
-    weighted(i, r[i], scale, p.pre_weight, pre_raw[i], p.pre_bias, y);
-    store(Own{}, (char *)p.next + row * p.next_stride * ES, i, y);
-  });
-}
-
-template <int T, int P, bool ONCE>
-__global__ void __launch_bounds__(T > CACHE_THREADS ? T : CACHE_THREADS) sk_norm(NormArgs a) {
-  __shared__ float red[4][16];
-  const SK_CONSTANT NormTable &table = *(const SK_CONSTANT NormTable *)(uintptr_t)a.table;
-  int i = 0;
-  uint32_t first = 0;
-  if (a.n > 1) {
-#pragma unroll
-    for (int k = 1; k < NORM_PROBLEMS; ++k) i += table.first[k] <= blockIdx.x ? 1 : 0;
-    first = table.first[i];
-  }
-  const SK_CONSTANT NormDev &p = table.problems[i];
-  const int t = (int)threadIdx.x % T;
-  int64_t row = (int64_t)(blockIdx.x - first);
-  if constexpr (T == 64) row = row * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
-  if (row >= p.rows) return;
-  if (p.dtype == SK_F32) norm_row<T, P, ONCE, SK_F32, SK_F32>(p, row, t, red);
-  else if (p.dtype == SK_BF16 && p.residual_dtype == SK_BF16) norm_row<T, P, ONCE, SK_BF16, SK_BF16>(p, row, t, red);
-  else if (p.dtype == SK_BF16) norm_row<T, P, ONCE, SK_BF16, SK_F32>(p, row, t, red);
-  else if (p.residual_dtype == SK_F16) norm_row<T, P, ONCE, SK_F16, SK_F16>(p, row, t, red);
-  else norm_row<T, P, ONCE, SK_F16, SK_F32>(p, row, t, red);
-}
-
+#define SK_NORM_FORM(T, P)                                      \
+  extern template __global__ void sk_norm<T, P, false>(NormArgs); \
+  extern template __global__ void sk_norm<T, P, true>(NormArgs);
+SK_NORM_FORM(16, 2)
+SK_NORM_FORM(64, 2)
+SK_NORM_FORM(128, 2)
+SK_NORM_FORM(256, 2)
+SK_NORM_FORM(512, 2)
+SK_NORM_FORM(1024, 4)
+#undef SK_NORM_FORM
 }  // namespace sk
 
 struct sk_norm_plan : sk::PlanOnDevice {
@@ -242,12 +32,18 @@ sk_status upload(sk_norm_plan &plan) {
   return st == SK_OK ? sk::copy_image(plan, image) : st;
 }
 
+template <int T, int P>
+void (*kernel_of(bool once))(sk::NormArgs) {
+  return once ? sk::sk_norm<T, P, true> : sk::sk_norm<T, P, false>;
+}
 void (*norm_kernel(sk::NormForm form, bool once))(sk::NormArgs) {
   switch (form) {
-    case sk::NORM_WAVE: return once ? sk::sk_norm<64, 4, true> : sk::sk_norm<64, 4, false>;
-    case sk::NORM_GROUP: return once ? sk::sk_norm<256, 2, true> : sk::sk_norm<256, 2, false>;
-    case sk::NORM_PAIR: return once ? sk::sk_norm<512, 2, true> : sk::sk_norm<512, 2, false>;
-    default: return once ? sk::sk_norm<1024, 4, true> : sk::sk_norm<1024, 4, false>;
+    case sk::NORM_SIXTEEN: return kernel_of<16, 2>(once);
+    case sk::NORM_WAVE: return kernel_of<64, 2>(once);
+    case sk::NORM_ROWS: return kernel_of<128, 2>(once);
+    case sk::NORM_GROUP: return kernel_of<256, 2>(once);
+    case sk::NORM_PAIR: return kernel_of<512, 2>(once);
+    default: return kernel_of<1024, 4>(once);
   }
 }
 

@@ -69,8 +69,10 @@ struct Layout {
 
 // ---- norms -----------------------------------------------------------------------------------------------------------------
 
-// Rows of up to 2048 elements get a wave each from that many rows on; fewer get a workgroup each, whose threads have a quarter of the work each.
-constexpr int32_t NORM_WAVE_ROWS = 2048;
+// From that many rows on a row gets no more than a wave or two, so that all of a workgroup's lanes have something of a row and more rows are on their way:
+// 768 x 8000 20.2 us against 29.8 with a workgroup of four waves for each, 64 x 50000 13.2 against 76.  Below it they are alike, or the workgroups of
+// four better (1536 x 1100: 8.0 us against 9.2).
+constexpr int32_t NORM_MANY_ROWS = 2048;
 // Problems of up to that many rows in all go together in the form of the longest of them: a launch costs more than idle threads.
 constexpr int64_t NORM_STEP_ROWS = 1024;
 
@@ -117,23 +119,21 @@ sk_status plan_norm(const sk_norm_problem *problems, int32_t n, NormPlanHost &ou
     d.rows = p.rows, d.dim = p.dim, d.eps = p.eps;
     d.residual_scale = p.residual_scale != 0.f ? p.residual_scale : 1.f, d.block_scale = p.block_scale != 0.f ? p.block_scale : 1.f;
     d.dtype = (int8_t)p.dtype, d.residual_dtype = (int8_t)p.residual_dtype, d.kind = (int8_t)p.kind, d.post = (int8_t)p.post, d.act = (int8_t)p.gate_act;
-    const NormForm form = p.rows >= NORM_WAVE_ROWS && dim <= norm_most_dim(NORM_WAVE) ? NORM_WAVE
-                          : dim <= norm_most_dim(NORM_GROUP)                           ? NORM_GROUP
-                          : dim <= norm_most_dim(NORM_PAIR)                            ? NORM_PAIR
-                                                                                       : NORM_LONG;
-    const int64_t groups = form == NORM_WAVE ? ((int64_t)p.rows + 3) / 4 : p.rows;
-    if (groups > norm_most_grid(form)) return refuse(err, SK_ERR_UNSUPPORTED, "more rows than a launch's grid can hold");
+    int form = p.rows >= NORM_MANY_ROWS && dim <= norm_most_dim(NORM_ROWS) ? NORM_SIXTEEN : NORM_GROUP;
+    while (dim > norm_most_dim((NormForm)form)) ++form;
+    const int64_t of = norm_rows_of((NormForm)form), groups = ((int64_t)p.rows + of - 1) / of;
+    if (groups > norm_most_grid((NormForm)form)) return refuse(err, SK_ERR_UNSUPPORTED, "more rows than a launch's grid can hold");
     all_rows += p.rows;
     bytes += (double)p.rows * dim * (double)(one * ((p.block != nullptr) + (d.gate && p.gate_rows) + (p.next != nullptr)) + res * ((p.residual != nullptr) + (p.residual_out != nullptr)));
-    items.push_back(Item{form, d, groups});
+    items.push_back(Item{(NormForm)form, d, groups});
     return SK_OK;
   });
   if (st != SK_OK) return st;
   if (written.overlap()) return refuse(err, SK_ERR_OVERLAP, "ranges of residual_out and next overlap");
   if (all_rows <= NORM_STEP_ROWS) {
-    NormForm longest = NORM_WAVE;
+    NormForm longest = NORM_GROUP;
     for (const Item &it : items) longest = std::max(longest, it.form);
-    for (Item &it : items) it.form = longest;  // (none of them is a wave's)
+    for (Item &it : items) it.form = longest;  // (none of them has many rows)
   }
   for (int f = 0; f < NORM_FORMS; ++f) {
     NormLaunch *l = nullptr;

@@ -56,7 +56,8 @@ static void norms() {
       const sk::NormDev &d = l.table.problems[i];
       need(d.dim <= sk::norm_most_dim(l.form), "a row longer than its form takes");
       const int64_t end = i + 1 < l.n ? l.table.first[i + 1] : l.grid, groups = end - l.table.first[i];
-      need(l.form == sk::NORM_WAVE ? groups * 4 >= d.rows && (groups - 1) * 4 < d.rows : groups == d.rows, "workgroups of a problem");
+      const int64_t of = sk::norm_rows_of(l.form);
+        need(groups == (d.rows + of - 1) / of, "workgroups of a problem");
       ++seen;
     }
   }

@@ -15,8 +15,8 @@ def test_lengths(dim):
                    H.Norm(dim=dim, rows=2, dtype="f32", kind="layer", gate="rows", act="tanh", seed=dim + 2)], f"dim {dim}")
 
 
-@pytest.mark.parametrize("dim", [1, 8, 100, 768, 1283, 2048])
-def test_rows_of_a_wave(dim):
+@pytest.mark.parametrize("dim", [1, 8, 100, 255, 256, 257, 768, 1024, 1025, 1283, 2048])
+def test_many_rows(dim):
     H.check_norms([H.Norm(dim=dim, rows=2051, post=1, stream="f32", seed=dim), H.Norm(dim=dim, rows=2050, dtype="f16", kind="layer", post=1, biases=True, gate="rows", act="silu", used=2049, seed=dim)])
 
 
