@@ -61,20 +61,21 @@ struct NormPlanHost {
 constexpr int MOE_ROWS = 512;     // rows that are routed together; problems of more are cut
 constexpr int MOE_EXPERTS = 512, MOE_TOP = 32;
 constexpr int MOE_GROUP = 32;     // rows of an expert that a unit of work takes at most
-constexpr int MOE_UP_RESIDENT = 3, MOE_DOWN_RESIDENT = 3;  // workgroups of the products that a compute unit holds (its registers)
+constexpr int MOE_UP_RESIDENT = 3, MOE_DOWN_RESIDENT = 4;  // workgroups of the products that a compute unit holds (its registers)
 constexpr int ROUTE_EXPERTS = 8, ROUTE_ROWS = 4;  // of a unit of the router
+constexpr int ADD_COLUMNS = 256;                  // of a row that a wave adds up
 
 // Rows of an expert that go together: its number (or -1: the shared one), the first of their places, how many.
 struct MoeGroup {
   int32_t expert, first, rows, pad;
 };
-// What the router found: groups, rows; all work of the first products, and of a tile of the second ones; the longest of a group in such a tile.
+// What the router found: groups, rows; all work of the first products, and of the second ones.
 struct MoeCount {
   int32_t groups, rows;
-  int64_t first_work, second_work, longest;
+  int64_t first_work, second_work;
 };
 
-// Up to MOE_ROWS rows of a problem, as the kernels see them (strides in bytes but for logits; `h` has a place for every pair of a row and an expert
+// Up to MOE_ROWS rows of a problem, as the kernels see them (strides in bytes but for logits and y; `h` and `y` have a place for every pair of a row and an expert
 // that it chose, then one for every row).
 struct MoeDev {
   const int32_t *n_rows;
@@ -93,24 +94,22 @@ struct MoeDev {
   int32_t *ids;           // [rows][top_k]: chosen experts
   float *weights;         // [rows][top_k]
   int32_t *row_of;        // [rows * top_k]: of a place
-  float *weight_of;       // [rows * top_k]: of a place
+  int32_t *place_at;      // [rows][top_k]
   MoeGroup *groups;       // [most_groups]; those of the shared expert last
-  int64_t *first_begin, *second_begin;  // [most_groups]: where a group's work begins, among the first products and within a tile of the second ones
+  int64_t *first_begin, *second_begin;  // [most_groups]: where a group's work begins, among the first and the second products
   MoeCount *count;
-  uint32_t *routed;       // counters, COUNTER_STEP apart: of units of the router per ROUTE_ROWS rows, of such blocks, of slices per tile of the output
-  uint32_t *blocks_routed, *summed;
+  uint32_t *routed;       // counters, COUNTER_STEP apart: of units of the router per ROUTE_ROWS rows, of such blocks
+  uint32_t *blocks_routed;
   char *h;                // [rows * top_k + rows], h_stride bytes apart
-  int64_t h_stride;
+  float *y;               // of the second products, y_stride elements apart
+  int64_t h_stride, y_stride;
 };
 
 struct MoePlanHost {
   std::vector<MoeDev> parts;          // workspace pointers: offsets until the plan is on the device
-  std::vector<uint32_t> route_first;  // first workgroup of the router of each part, and the number of all
+  std::vector<uint32_t> route_first, add_first;  // first workgroup of the router, and of the sums, of each part, and the number of all
   MoeCount *counts = nullptr;         // of all parts (an offset)
-  float *slices = nullptr;            // two of each workgroup (an offset)
-  int64_t slice_floats = 0;
   int64_t up_workgroups = 0, down_workgroups = 0;  // of the products
-  size_t lds = 0;                     // bytes that a workgroup of the second products keeps its sums in
   size_t workspace = 0, counters = 0; // bytes; the counters stand first
 };
 

@@ -7,10 +7,8 @@ namespace sk {
 
 struct MoeArgs {
   const MoeDev *parts;
-  const uint32_t *first;  // of the router: first workgroup of each part
-  MoeCount *counts;       // of each part: what the router found
-  float *slices;          // partial sums of the second products, see down_share
-  int64_t slice_floats;
+  const uint32_t *first, *add_first;  // of the router, and of the sums: first workgroup of each part
+  MoeCount *counts;                   // of each part: what the router found
   int32_t n;
 };
 
@@ -24,12 +22,12 @@ struct Place {
   const SK_CONSTANT MoeDev *part;
   int32_t unit;
 };
-__device__ __forceinline__ Place place_of(const MoeArgs &a) {
+__device__ __forceinline__ Place place_of(const MoeArgs &a, const uint32_t *firsts) {
   int32_t part = 0;
   uint32_t first = 0;
   if (a.n > 1) {
-    part = __builtin_amdgcn_readfirstlane(last_not_above(a.first, a.n, (int64_t)blockIdx.x, threadIdx.x & 63));
-    first = ((const SK_CONSTANT uint32_t *)(uintptr_t)a.first)[part];
+    part = __builtin_amdgcn_readfirstlane(last_not_above(firsts, a.n, (int64_t)blockIdx.x, threadIdx.x & 63));
+    first = ((const SK_CONSTANT uint32_t *)(uintptr_t)firsts)[part];
   }
   return Place{(const SK_CONSTANT MoeDev *)(uintptr_t)(a.parts + part), (int32_t)(blockIdx.x - first)};
 }
@@ -176,7 +174,7 @@ struct Sorting {
   uint32_t bits[MOE_EXPERTS][MOE_ROWS / 32];
   int32_t count[MOE_EXPERTS], first[MOE_EXPERTS];
   int32_t ids[SORT_PAIRS];
-  float weights[SORT_PAIRS];
+  float weights[ROUTE_ROWS * MOE_TOP];
 };
 // Counts of an expert's groups, and sums of them, in one number of 64 bits: rows in the lowest 16 bits, then groups of modes 8, 16 and 32, 16 bits each.  (A
 // part has at most 512 experts and 2^14 pairs, so none reaches 2^15.)
@@ -204,7 +202,7 @@ __device__ __forceinline__ void sort_pairs(const SK_CONSTANT MoeDev &P, int32_t 
   __syncthreads();
   for (int32_t i = tid; i < pairs; i += CACHE_THREADS) {
     const int32_t row = i / P.top_k, e = here ? s.ids[i] : got(P.ids + i);
-    if (!here && i < SORT_PAIRS) s.ids[i] = e, s.weights[i] = got(P.weights + i);
+    if (!here && i < SORT_PAIRS) s.ids[i] = e;
     atomicOr(&s.bits[e][row / 32], 1u << (row % 32));
   }
   __syncthreads();
@@ -225,24 +223,23 @@ __device__ __forceinline__ void sort_pairs(const SK_CONSTANT MoeDev &P, int32_t 
       for (int32_t i = 0; i < g; ++i) {  // (all but the last are full)
         P.groups[at + i] = MoeGroup{e, place + i * MOE_GROUP, min(MOE_GROUP, n - i * MOE_GROUP), 0};
         P.first_begin[at + i] = (up.sum(before) + i * up.of[2]) * P.up_tiles;
-        P.second_begin[at + i] = down.sum(before) + i * down.of[2];
+        P.second_begin[at + i] = (down.sum(before) + i * down.of[2]) * P.down_tiles;
       }
       all += lane_of(upto, 63);
     }
-    MoeCount c{groups_in(all), rows, up.sum(all) * P.up_tiles, down.sum(all), of_mode(all, 32) ? down.of[2] : of_mode(all, 16) ? down.of[1] : all ? down.of[0] : 0};
+    MoeCount c{groups_in(all), rows, up.sum(all) * P.up_tiles, down.sum(all) * P.down_tiles};
     if (P.shared_ffn) {  // (at most 16 groups)
       const int32_t g = (rows + MOE_GROUP - 1) / MOE_GROUP, n = min(MOE_GROUP, rows - tid * MOE_GROUP);
       const Costs shared = costs_of(P.shared_ffn, 1);
       if (tid < g) {
         P.groups[c.groups + tid] = MoeGroup{-1, tid * MOE_GROUP, n, 0};
         P.first_begin[c.groups + tid] = c.first_work + tid * up.of[2] * P.shared_tiles;
-        P.second_begin[c.groups + tid] = c.second_work + tid * shared.of[2];
+        P.second_begin[c.groups + tid] = c.second_work + tid * shared.of[2] * P.down_tiles;
       }
       const int64_t counts = groups_of(rows);
       c.groups += g;
       c.first_work += up.sum(counts) * P.shared_tiles;
-      c.second_work += shared.sum(counts);
-      c.longest = max(c.longest, of_mode(counts, 32) ? shared.of[2] : of_mode(counts, 16) ? shared.of[1] : g ? shared.of[0] : 0);
+      c.second_work += shared.sum(counts) * P.down_tiles;
     }
     if (tid == 0) *P.count = c;
   }
@@ -251,8 +248,8 @@ __device__ __forceinline__ void sort_pairs(const SK_CONSTANT MoeDev &P, int32_t 
     const int32_t row = i / P.top_k, e = i < SORT_PAIRS ? s.ids[i] : got(P.ids + i);
     int32_t at = s.first[e] + __popc(s.bits[e][row / 32] & ((1u << (row % 32)) - 1));
     for (int32_t w = 0; w < row / 32; ++w) at += __popc(s.bits[e][w]);
-    P.row_of[at] = row;
-    P.weight_of[at] = i < SORT_PAIRS ? s.weights[i] : got(P.weights + i);
+    P.row_of[at] = row, P.place_at[i] = at;
+    if (here) P.weights[i] = s.weights[i];
   }
 }
 
@@ -260,7 +257,7 @@ __global__ void __launch_bounds__(CACHE_THREADS) sk_moe_route(MoeArgs a) {
   __shared__ Sorting sorting;
   __shared__ uint32_t flag;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const Place place = place_of(a);
+  const Place place = place_of(a, a.first);
   const SK_CONSTANT MoeDev &P = *place.part;
   const int32_t unit = place.unit;
   const int32_t by_experts = (P.experts + ROUTE_EXPERTS - 1) / ROUTE_EXPERTS, blocks = (P.rows + ROUTE_ROWS - 1) / ROUTE_ROWS;
@@ -307,7 +304,7 @@ __device__ __forceinline__ u32x4 high_half(const u32x4 &first, const u32x4 &seco
 
 constexpr int TILE = 16;
 constexpr int RUN_PLACES = 512;  // rows of groups that LDS knows
-// A workgroup walks through a run of tiles: groups of one mode one after the other, of each `tiles` tiles (first products) or one (second products).
+// A workgroup walks through a run of tiles: groups of one mode one after the other, all tiles of each side by side.
 struct Run {
   int32_t group, tile, n;  // the first tile; how many
 };
@@ -317,11 +314,6 @@ __device__ __forceinline__ f32x4 *joint_at(float *joint, int t, int wave, int m,
   return (f32x4 *)(joint + ((((t & 1) * 4 + wave) * W + m) * MOE_GROUP + i) * TILE + row);
 }
 constexpr int joint_floats(int w) { return 2 * 4 * w * MOE_GROUP * TILE; }
-// Of each place of a run's groups: its row and weight.
-struct Places {
-  int32_t row[RUN_PLACES];
-  float weight[RUN_PLACES];
-};
 // Loads by way of a buffer descriptor: a scalar base, and in each lane an offset below 2^31; a lane with OUTSIDE gets zeros and asks for nothing, so
 // that no load stands under a branch (which would leave the compiler in doubt how many are on their way).
 constexpr uint32_t OUTSIDE = 0x80000000u;
@@ -387,7 +379,7 @@ __device__ __forceinline__ void stream(const Run &run, int32_t tiles, int64_t ro
       p_step = 0;
       if (--p_left > 0) {
         if (++p_tile >= tiles) {
-          p_tile = tiles == 1 ? p_tile - 1 : 0;
+          p_tile = 0;
           pg = group(++p_group);
           new_group();
         }
@@ -439,7 +431,7 @@ __device__ __forceinline__ void stream(const Run &run, int32_t tiles, int64_t ro
           done(t, c_group, c_tile);
           ++t;
           if (++c_tile >= tiles) {
-            c_tile = tiles == 1 ? c_tile - 1 : 0;
+            c_tile = 0;
             ++c_group;
           }
         }
@@ -473,27 +465,27 @@ __device__ __forceinline__ int64_t begin_of(const int64_t *begin, int32_t i) { r
 
 // Work is cut into equal shares, one for each workgroup of a launch that fills the card once.
 
-// The run that begins with a group: those behind it of the same kind (shared or not) and mode, up to group `end` and as many as LDS has places for.
-// Their rows and weights go to LDS.
-__device__ __forceinline__ int32_t run_end(const SK_CONSTANT MoeDev &P, int32_t begin, int32_t end, Places &places_of, int tid) {
+// The run that begins with a group: those behind it of the same kind (shared or not) and mode, up to group `end`; of the first products as many as LDS has
+// places for, which their rows go to.
+template <bool ROWS>
+__device__ __forceinline__ int32_t run_end(const SK_CONSTANT MoeDev &P, int32_t begin, int32_t end, int32_t *row_of, int tid) {
   const MoeGroup g = group_of(P, begin);
   int32_t at = begin + 1, places = g.rows;
   while (at < end) {
     const MoeGroup next = group_of(P, at);
-    if ((next.expert < 0) != (g.expert < 0) || moe::mode_of(next.rows) != moe::mode_of(g.rows) || places + next.rows > RUN_PLACES) break;
+    if ((next.expert < 0) != (g.expert < 0) || moe::mode_of(next.rows) != moe::mode_of(g.rows) || (ROWS && places + next.rows > RUN_PLACES)) break;
     places += next.rows;
     ++at;
   }
-  for (int32_t i = tid; i < places; i += CACHE_THREADS) {
-    places_of.row[i] = g.expert < 0 ? g.first + i : load_i32(P.row_of + g.first + i);
-    places_of.weight[i] = g.expert < 0 ? 1.f : load_f(P.weight_of + g.first + i);
+  if constexpr (ROWS) {
+    for (int32_t i = tid; i < places; i += CACHE_THREADS) row_of[i] = g.expert < 0 ? g.first + i : load_i32(P.row_of + g.first + i);
+    __syncthreads();
   }
-  __syncthreads();
   return at;
 }
 
 template <int DT, int MODE, bool GATED>
-__device__ __forceinline__ void up_run(const SK_CONSTANT MoeDev &P, const Run &run, bool shared, float *joint, Places &places, int tid) {
+__device__ __forceinline__ void up_run(const SK_CONSTANT MoeDev &P, const Run &run, bool shared, float *joint, const int32_t *row_of, int tid) {
   constexpr int W = GATED ? 2 : 1;
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int32_t width = shared ? P.shared_ffn : P.ffn, place0 = group_of(P, run.group).first;
@@ -519,174 +511,137 @@ __device__ __forceinline__ void up_run(const SK_CONSTANT MoeDev &P, const Run &r
   };
   stream<DT, MODE, W, MODE == 8 ? 3 : 2>(
       run, shared ? P.shared_tiles : P.up_tiles, shared ? 2 * (int64_t)P.dim : P.up_row, width, P.dim, [&](int32_t i) { return group_of(P, i); }, base, [&](const MoeGroup &) { return P.x; },
-      [&](const MoeGroup &g, int32_t i) { return (uint32_t)places.row[g.first - place0 + i] * (uint32_t)P.x_stride; }, done, joint, wave, lane);
+      [&](const MoeGroup &g, int32_t i) { return (uint32_t)row_of[g.first - place0 + i] * (uint32_t)P.x_stride; }, done, joint, wave, lane);
 }
 
-// The tiles of the first products from tile `tile` of group `group` on, up to (not with) tile `last_tile` of group `last`.
-template <int DT, bool GATED>
-__device__ __forceinline__ void up_tiles(const SK_CONSTANT MoeDev &P, int32_t group, int32_t tile, int32_t last, int32_t last_tile, float *joint, Places &places, int tid) {
-  while (group < last || (group == last && tile < last_tile)) {
-    const int32_t end = run_end(P, group, last_tile > 0 ? last + 1 : last, places, tid);
-    const MoeGroup g = group_of(P, group);
-    const bool shared = g.expert < 0;
-    const int32_t tiles = shared ? P.shared_tiles : P.up_tiles, mode = moe::mode_of(g.rows);
-    const Run run{group, tile, (end - group) * tiles - tile - (end > last ? tiles - last_tile : 0)};
-    if (mode == 8) up_run<DT, 8, GATED>(P, run, shared, joint, places, tid);
-    else if (mode == 16) up_run<DT, 16, GATED>(P, run, shared, joint, places, tid);
-    else up_run<DT, 32, GATED>(P, run, shared, joint, places, tid);
-    group = end, tile = 0;
-  }
-}
-
-__global__ void __launch_bounds__(CACHE_THREADS, MOE_UP_RESIDENT) sk_moe_up(MoeArgs a) {
-  __shared__ __attribute__((aligned(16))) float joint[joint_floats(2)];
-  __shared__ Places places;
-  const int lane = threadIdx.x & 63;
-  int64_t total = 0;
-  for (int32_t i = 0; i < a.n; ++i) total += count_of(a, i).first_work;
-  const moe::Share share = moe::share_of(total, gridDim.x, blockIdx.x);
-  int64_t offset = 0;
-  for (int32_t i = 0; i < a.n && offset < share.end; ++i) {
-    const SK_CONSTANT MoeDev &P = part_of(a, i);
-    const int64_t here = count_of(a, i).first_work;
-    if (share.begin < offset + here && here > 0) {
-      const int32_t groups = count_of(a, i).groups;
-      int32_t group[2], tile[2];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {  // beginning and end
-        const int64_t at = e ? share.end - offset : max(share.begin - offset, (int64_t)0);
-        group[e] = group_at(P.first_begin, groups, at, lane);
-        const MoeGroup g = group_of(P, group[e]);
-        const int32_t tiles = g.expert < 0 ? P.shared_tiles : P.up_tiles;
-        tile[e] = __builtin_amdgcn_readfirstlane(moe::tile_from(at, begin_of(P.first_begin, group[e]), moe::cost(P.dim, P.gate ? 2 : 1, moe::mode_of(g.rows)), tiles));
-        if (tile[e] == tiles) ++group[e], tile[e] = 0;
-      }
-      if (P.dtype == SK_BF16) P.gate ? up_tiles<SK_BF16, true>(P, group[0], tile[0], group[1], tile[1], joint, places, threadIdx.x) : up_tiles<SK_BF16, false>(P, group[0], tile[0], group[1], tile[1], joint, places, threadIdx.x);
-      else P.gate ? up_tiles<SK_F16, true>(P, group[0], tile[0], group[1], tile[1], joint, places, threadIdx.x) : up_tiles<SK_F16, false>(P, group[0], tile[0], group[1], tile[1], joint, places, threadIdx.x);
-    }
-    offset += here;
-  }
-}
-
-// The second products: the tiles of 16 columns of the output, and for each of them all groups, one after the other.  A workgroup's sums over the groups
-// of its share, weighted, stand in LDS (16 columns of every row of the part).  Where a share has all groups of a tile, they are the output; otherwise they go
-// to memory as a slice, and the workgroup whose slice arrives last adds the slices up, in their order.  A share begins and ends within a
-// tile, so a workgroup has two places for slices: the second for a tile that it begins, the first for one that another has begun.
+// The sums of a place of the second products stand in the workspace, unweighted and in 32 bits: sk_moe_add takes them from there.  (To walk over all groups
+// of 16 columns, add their rows up in LDS and join the slices of the workgroups that share the columns saves those bytes, 8 of 230 us where 128 rows have
+// eight experts each, but 250 rows of 1000 columns took 75 us instead of 45 and the second products of one row 9.7 instead of 5.2 + 2.7.)
 template <int DT, int MODE>
-__device__ __forceinline__ void down_run(const SK_CONSTANT MoeDev &P, const Run &run, float *joint, Places &places, float *sums, int tid) {
+__device__ __forceinline__ void down_run(const SK_CONSTANT MoeDev &P, const Run &run, bool shared, float *joint, int tid) {
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const MoeGroup first = group_of(P, run.group);
-  const bool shared = first.expert < 0;
   const int64_t place0 = shared ? (int64_t)P.rows * P.top_k : 0;
   const int32_t width = shared ? P.shared_ffn : P.ffn;
-  auto done = [&](int32_t t, int32_t group, int32_t) {
+  auto done = [&](int32_t t, int32_t group, int32_t tile) {
     const MoeGroup g = group_of(P, group);
     const int32_t i = tid >> 2;
-    if (i >= g.rows) return;  // (a row stands in a group once)
-    f32x4 *at = (f32x4 *)(sums + places.row[g.first - first.first + i] * TILE + 4 * (tid & 3));
-    *at += places.weight[g.first - first.first + i] * joined<MODE, 1>(joint, t, 0, i, tid & 3);
+    if (i >= g.rows) return;
+    // (a row of them has whole tiles)
+    *(f32x4 SK_GLOBAL *)(uintptr_t)(P.y + (place0 + g.first + i) * P.y_stride + tile * TILE + 4 * (tid & 3)) = joined<MODE, 1>(joint, t, 0, i, tid & 3);
   };
   stream<DT, MODE, 1, MODE == 8 ? 4 : MODE == 16 ? 3 : 2>(
-      run, 1, shared ? 2 * (int64_t)width : P.down_row, P.dim, width, [&](int32_t i) { return group_of(P, i); },
+      run, P.down_tiles, shared ? 2 * (int64_t)width : P.down_row, P.dim, width, [&](int32_t i) { return group_of(P, i); },
       [&](const MoeGroup &g, int) { return shared ? P.shared_down : P.down + g.expert * P.down_expert; }, [&](const MoeGroup &g) { return P.h + (place0 + g.first) * P.h_stride; },
       [&](const MoeGroup &, int32_t i) { return (uint32_t)i * (uint32_t)P.h_stride; }, done, joint, wave, lane);
 }
 
-// Groups [g0, g1) of a tile of the output.
-template <int DT>
-__device__ __forceinline__ void down_groups(const SK_CONSTANT MoeDev &P, int32_t tile, int32_t g0, int32_t g1, float *joint, Places &places, float *sums, int tid) {
-  while (g0 < g1) {
-    const int32_t end = run_end(P, g0, g1, places, tid);
-    const Run run{g0, tile, end - g0};
-    const int32_t mode = moe::mode_of(group_of(P, g0).rows);
-    if (mode == 8) down_run<DT, 8>(P, run, joint, places, sums, tid);
-    else if (mode == 16) down_run<DT, 16>(P, run, joint, places, sums, tid);
-    else down_run<DT, 32>(P, run, joint, places, sums, tid);
-    g0 = end;
+// A workgroup's share of the tiles of the first (UP) or second products.
+template <bool UP>
+struct Products {
+  static __device__ __forceinline__ int64_t work(const SK_CONSTANT MoeCount &c) { return UP ? c.first_work : c.second_work; }
+  static __device__ __forceinline__ int32_t tiles(const SK_CONSTANT MoeDev &P, const MoeGroup &g) { return !UP ? P.down_tiles : g.expert < 0 ? P.shared_tiles : P.up_tiles; }
+  static __device__ __forceinline__ int64_t cost(const SK_CONSTANT MoeDev &P, const MoeGroup &g) {
+    return UP ? moe::cost(P.dim, P.gate ? 2 : 1, moe::mode_of(g.rows)) : moe::cost(g.expert < 0 ? P.shared_ffn : P.ffn, 1, moe::mode_of(g.rows));
   }
-}
 
-template <int DT>
-__device__ __forceinline__ void store_out(const SK_CONSTANT MoeDev &P, int32_t row, int32_t d, const f32x4 &v) {
-  if (d < P.dim) store8(P.out + row * P.out_stride + 2 * d, u32x2{pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3])});
-}
-
-template <int DT>
-__device__ __forceinline__ void down_share(const MoeArgs &a, const SK_CONSTANT MoeDev &P, const SK_CONSTANT MoeCount &c, moe::Share share, int64_t offset, int64_t total, int64_t shares,
-                                           float *joint, Places &places, float *sums, uint32_t *flag, int tid) {
-  const int64_t tile_work = c.second_work, me = blockIdx.x;
-  const int64_t begin = moe::most(share.begin - offset, 0), end = moe::least(share.end - offset, tile_work * P.down_tiles);
-  // the first group that begins at or behind a place of a tile
-  auto group_from = [&](int64_t at) {
-    if (at <= 0) return 0;
-    return group_at(P.second_begin, c.groups, at - 1, tid & 63) + 1;
-  };
-  for (int32_t tile = (int32_t)(begin / tile_work); tile * tile_work < end; ++tile) {
-    const int64_t at = tile * tile_work;
-    const int32_t g0 = group_from(begin - at), g1 = group_from(moe::least(end - at, tile_work));
-    if (g0 >= g1) continue;
-    for (int32_t k = tid; k < c.rows * TILE; k += CACHE_THREADS) sums[k] = 0.f;
-    __syncthreads();
-    down_groups<DT>(P, tile, g0, g1, joint, places, sums, tid);
-    if (g1 - g0 == c.groups) {
-      for (int32_t k = tid; k < c.rows * 4; k += CACHE_THREADS) store_out<DT>(P, k >> 2, tile * TILE + 4 * (k & 3), *(const f32x4 *)(sums + 4 * k));
-    } else {
-      // the workgroups that have groups of this tile: every one from that of the first to that of the last
-      const int64_t first = moe::owner_of(offset + at, total, shares), last = moe::owner_of(offset + at + begin_of(P.second_begin, c.groups - 1), total, shares);
-      float *slice = a.slices + (2 * me + (me == first ? 1 : 0)) * a.slice_floats;
-      for (int32_t k = tid; k < c.rows * 4; k += CACHE_THREADS) {
-        const f32x4 v = *(const f32x4 *)(sums + 4 * k);
-        store_shared(slice + 4 * k, f32x2{v[0], v[1]});
-        store_shared(slice + 4 * k + 2, f32x2{v[2], v[3]});
+  // From tile `tile` of group `group` on, up to (not with) tile `last_tile` of group `last`.
+  template <int DT, bool GATED>
+  static __device__ __forceinline__ void between(const SK_CONSTANT MoeDev &P, int32_t group, int32_t tile, int32_t last, int32_t last_tile, float *joint, int32_t *row_of, int tid) {
+    while (group < last || (group == last && tile < last_tile)) {
+      const int32_t end = run_end<UP>(P, group, last_tile > 0 ? last + 1 : last, row_of, tid);
+      const MoeGroup g = group_of(P, group);
+      const bool shared = g.expert < 0;
+      const int32_t each = tiles(P, g), mode = moe::mode_of(g.rows);
+      const Run run{group, tile, (end - group) * each - tile - (end > last ? each - last_tile : 0)};
+      if constexpr (UP) {
+        if (mode == 8) up_run<DT, 8, GATED>(P, run, shared, joint, row_of, tid);
+        else if (mode == 16) up_run<DT, 16, GATED>(P, run, shared, joint, row_of, tid);
+        else up_run<DT, 32, GATED>(P, run, shared, joint, row_of, tid);
+      } else {
+        if (mode == 8) down_run<DT, 8>(P, run, shared, joint, tid);
+        else if (mode == 16) down_run<DT, 16>(P, run, shared, joint, tid);
+        else down_run<DT, 32>(P, run, shared, joint, tid);
       }
-      if (last_to_arrive(P.summed + (int64_t)tile * COUNTER_STEP, (int32_t)(last - first + 1), flag)) {
-        for (int32_t k = tid; k < c.rows * 4; k += CACHE_THREADS) {
-          f32x4 v = {0.f, 0.f, 0.f, 0.f};
-          constexpr int AHEAD = 8;  // slices on their way at a time
-          for (int64_t s0 = first; s0 <= last; s0 += AHEAD) {
-            f32x2 lo[AHEAD], hi[AHEAD];
-#pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-              const int64_t s = min(s0 + u, last);
-              const float *from = a.slices + (2 * s + (s == first ? 1 : 0)) * a.slice_floats + 4 * k;
-              lo[u] = load_shared(from), hi[u] = load_shared(from + 2);
-            }
-#pragma unroll
-            for (int u = 0; u < AHEAD; ++u)
-              if (s0 + u <= last) v += f32x4{lo[u][0], lo[u][1], hi[u][0], hi[u][1]};
-          }
-          store_out<DT>(P, k >> 2, tile * TILE + 4 * (k & 3), v);
-        }
-      }
+      group = end, tile = 0;
     }
-    __syncthreads();
   }
+
+  static __device__ __forceinline__ void share(const MoeArgs &a, float *joint, int32_t *row_of, int tid) {
+    const int lane = tid & 63;
+    int64_t total = 0;
+    for (int32_t i = 0; i < a.n; ++i) total += work(count_of(a, i));
+    const moe::Share share = moe::share_of(total, gridDim.x, blockIdx.x);
+    int64_t offset = 0;
+    for (int32_t i = 0; i < a.n && offset < share.end; ++i) {
+      const SK_CONSTANT MoeDev &P = part_of(a, i);
+      const int64_t here = work(count_of(a, i));
+      if (share.begin < offset + here && here > 0) {
+        const int64_t *begins = UP ? P.first_begin : P.second_begin;
+        const int32_t groups = count_of(a, i).groups;
+        int32_t group[2], tile[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {  // beginning and end
+          const int64_t at = e ? share.end - offset : max(share.begin - offset, (int64_t)0);
+          group[e] = group_at(begins, groups, at, lane);
+          const MoeGroup g = group_of(P, group[e]);
+          tile[e] = __builtin_amdgcn_readfirstlane(moe::tile_from(at, begin_of(begins, group[e]), cost(P, g), tiles(P, g)));
+          if (tile[e] == tiles(P, g)) ++group[e], tile[e] = 0;
+        }
+        auto run = [&](auto type) {
+          constexpr int DT = decltype(type)::value;
+          if (UP && P.gate) between<DT, UP>(P, group[0], tile[0], group[1], tile[1], joint, row_of, tid);
+          else between<DT, false>(P, group[0], tile[0], group[1], tile[1], joint, row_of, tid);
+        };
+        if (P.dtype == SK_BF16) run(std::integral_constant<int, SK_BF16>{});
+        else run(std::integral_constant<int, SK_F16>{});
+      }
+      offset += here;
+    }
+  }
+};
+
+__global__ void __launch_bounds__(CACHE_THREADS, MOE_UP_RESIDENT) sk_moe_up(MoeArgs a) {
+  __shared__ __attribute__((aligned(16))) float joint[joint_floats(2)];
+  __shared__ int32_t row_of[RUN_PLACES];
+  Products<true>::share(a, joint, row_of, threadIdx.x);
 }
 
 __global__ void __launch_bounds__(CACHE_THREADS, MOE_DOWN_RESIDENT) sk_moe_down(MoeArgs a) {
   __shared__ __attribute__((aligned(16))) float joint[joint_floats(1)];
-  __shared__ Places places;
-  __shared__ uint32_t flag;
-  extern __shared__ __attribute__((aligned(16))) float sums[];
-  int64_t total = 0, longest = 0;
-  for (int32_t i = 0; i < a.n; ++i) {
-    total += count_of(a, i).second_work * part_of(a, i).down_tiles;
-    longest = max(longest, count_of(a, i).longest);
+  Products<false>::share(a, joint, nullptr, threadIdx.x);
+}
+
+// out = the weighted sums of a row's places, in the order in which its experts were chosen, the shared expert last; 256 columns a wave.
+template <int DT>
+__device__ __forceinline__ void add_places(const SK_CONSTANT MoeDev &P, int32_t row, int32_t d) {
+  constexpr int AHEAD = 8;
+  const int64_t pair0 = (int64_t)row * P.top_k;
+  const SK_CONSTANT int32_t *place = (const SK_CONSTANT int32_t *)(uintptr_t)(P.place_at + pair0);
+  const SK_CONSTANT float *weight = (const SK_CONSTANT float *)(uintptr_t)(P.weights + pair0);
+  auto y = [&](int64_t at) { return *(const f32x4 SK_GLOBAL *)(uintptr_t)(P.y + at * P.y_stride + d); };
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f}, shared = {0.f, 0.f, 0.f, 0.f};
+  if (P.shared_ffn) shared = y((int64_t)P.rows * P.top_k + row);
+  for (int32_t j0 = 0; j0 < P.top_k; j0 += AHEAD) {
+    f32x4 v[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (j0 + u < P.top_k) v[u] = y(place[j0 + u]);
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (j0 + u < P.top_k) sum += weight[j0 + u] * v[u];
   }
-  const int64_t shares = moe::shares_for(total, longest, gridDim.x);
-  if ((int64_t)blockIdx.x >= shares) return;
-  const moe::Share share = moe::share_of(total, shares, blockIdx.x);
-  int64_t offset = 0;
-  for (int32_t i = 0; i < a.n && offset < share.end; ++i) {
-    const SK_CONSTANT MoeDev &P = part_of(a, i);
-    const SK_CONSTANT MoeCount &c = count_of(a, i);
-    const int64_t here = c.second_work * P.down_tiles;
-    if (here > 0 && share.begin < offset + here) {
-      if (P.dtype == SK_BF16) down_share<SK_BF16>(a, P, c, share, offset, total, shares, joint, places, sums, &flag, threadIdx.x);
-      else down_share<SK_F16>(a, P, c, share, offset, total, shares, joint, places, sums, &flag, threadIdx.x);
-    }
-    offset += here;
-  }
+  if (P.shared_ffn) sum += shared;
+  store8(P.out + row * P.out_stride + 2 * d, u32x2{pack2<DT>(sum[0], sum[1]), pack2<DT>(sum[2], sum[3])});
+}
+
+__global__ void __launch_bounds__(CACHE_THREADS) sk_moe_add(MoeArgs a) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const Place place = place_of(a, a.add_first);
+  const SK_CONSTANT MoeDev &P = *place.part;
+  const int32_t columns = (P.dim + ADD_COLUMNS - 1) / ADD_COLUMNS, unit = place.unit * 4 + wave, row = unit / columns, d = unit % columns * ADD_COLUMNS + 4 * lane;
+  if (row >= ((const SK_CONSTANT MoeCount *)(uintptr_t)P.count)->rows || d >= P.dim) return;  // (dim is a multiple of 8)
+  if (P.dtype == SK_BF16) add_places<SK_BF16>(P, row, d);
+  else add_places<SK_F16>(P, row, d);
 }
 
 }  // namespace sk
@@ -701,23 +656,24 @@ namespace {
 sk_status upload(sk_moe_plan &plan) {
   sk::MoePlanHost &h = plan.host;
   // counters, parts, first workgroups of the router
-  const size_t o_parts = sk::align_up(h.counters, 256), o_first = o_parts + sk::align_up(h.parts.size() * sizeof(sk::MoeDev), 256);
-  std::vector<char> image(o_first + h.route_first.size() * 4, 0);
+  const size_t o_parts = sk::align_up(h.counters, 256), o_first = o_parts + sk::align_up(h.parts.size() * sizeof(sk::MoeDev), 256),
+               o_add = o_first + h.route_first.size() * 4;
+  std::vector<char> image(o_add + h.add_first.size() * 4, 0);
   char *ws = nullptr;
   const sk_status st = sk::upload_image(plan, image, h.workspace, &ws);
   if (st != SK_OK) return st;
   auto moved = [](auto *&p, char *base) { p = (std::decay_t<decltype(p)>)(base + (uintptr_t)p); };
   std::vector<sk::MoeDev> parts = h.parts;
   for (sk::MoeDev &d : parts) {
-    moved(d.routed, plan.blob), moved(d.blocks_routed, plan.blob), moved(d.summed, plan.blob);
-    moved(d.logits, ws), moved(d.ids, ws), moved(d.weights, ws), moved(d.row_of, ws), moved(d.weight_of, ws), moved(d.groups, ws), moved(d.first_begin, ws), moved(d.second_begin, ws), moved(d.count, ws), moved(d.h, ws);
+    moved(d.routed, plan.blob), moved(d.blocks_routed, plan.blob);
+    moved(d.logits, ws), moved(d.ids, ws), moved(d.weights, ws), moved(d.row_of, ws), moved(d.place_at, ws), moved(d.groups, ws), moved(d.first_begin, ws), moved(d.second_begin, ws), moved(d.count, ws), moved(d.h, ws), moved(d.y, ws);
   }
   if (!parts.empty()) std::memcpy(image.data() + o_parts, parts.data(), parts.size() * sizeof(sk::MoeDev));
   std::memcpy(image.data() + o_first, h.route_first.data(), h.route_first.size() * 4);
   sk::MoeCount *counts = h.counts;
-  float *slices = h.slices;
-  moved(counts, ws), moved(slices, ws);
-  plan.args = sk::MoeArgs{(const sk::MoeDev *)(plan.blob + o_parts), (const uint32_t *)(plan.blob + o_first), counts, slices, h.slice_floats, (int32_t)parts.size()};
+  std::memcpy(image.data() + o_add, h.add_first.data(), h.add_first.size() * 4);
+  moved(counts, ws);
+  plan.args = sk::MoeArgs{(const sk::MoeDev *)(plan.blob + o_parts), (const uint32_t *)(plan.blob + o_first), (const uint32_t *)(plan.blob + o_add), counts, (int32_t)parts.size()};
   return sk::copy_image(plan, image);
 }
 
@@ -744,7 +700,8 @@ sk_status sk_moe_launch(sk_moe_plan *plan, void *hip_stream) {
     const sk::MoePlanHost &h = plan->host;
     st = sk::launch(sk::sk_moe_route, (int64_t)h.route_first.back(), stream, nullptr, plan->args);
     if (st == SK_OK) st = sk::launch(sk::sk_moe_up, h.up_workgroups, stream, nullptr, plan->args);
-    if (st == SK_OK) st = sk::launch(sk::sk_moe_down, h.down_workgroups, stream, behind, plan->args, sk::CACHE_THREADS, h.lds);
+    if (st == SK_OK) st = sk::launch(sk::sk_moe_down, h.down_workgroups, stream, nullptr, plan->args);
+    if (st == SK_OK) st = sk::launch(sk::sk_moe_add, (int64_t)h.add_first.back(), stream, behind, plan->args);
     plan->ledger.after_launch((uintptr_t)stream, in_capture, behind && st == SK_OK);  // also after a failure: some launches may be out
     return st;
   });
@@ -753,7 +710,7 @@ sk_status sk_moe_launch(sk_moe_plan *plan, void *hip_stream) {
 sk_status sk_moe_plan_info(const sk_moe_plan *plan, int32_t *launches, int64_t *workspace_bytes) {
   return sk::guarded([&]() -> sk_status {
     if (!plan) return sk::set_last_error(SK_ERR_INVALID_ARG, "plan is null");
-    if (launches) *launches = plan->host.parts.empty() ? 0 : 3;
+    if (launches) *launches = plan->host.parts.empty() ? 0 : 4;
     if (workspace_bytes) *workspace_bytes = (int64_t)(plan->host.workspace + plan->host.counters);
     return SK_OK;
   });

@@ -157,8 +157,8 @@ sk_status plan_norm(const sk_norm_problem *problems, int32_t n, NormPlanHost &ou
 
 sk_status plan_moe(const sk_moe_problem *problems, int32_t n, int32_t compute_units, int32_t workgroups, MoePlanHost &out, std::string &err) {
   Spans written;
-  out.route_first.assign(1, 0u);
-  int64_t route = 0, most_rows = 0, tiles = 0;
+  out.route_first.assign(1, 0u), out.add_first.assign(1, 0u);
+  int64_t route = 0, add = 0, tiles = 0;
   Layout counters, work;
   const sk_status st = each(problems, n, err, [&](const sk_moe_problem &p) -> sk_status {
     if (p.dtype != SK_BF16 && p.dtype != SK_F16) return refuse(err, SK_ERR_UNSUPPORTED, "dtype must be SK_BF16 or SK_F16");
@@ -219,15 +219,17 @@ sk_status plan_moe(const sk_moe_problem *problems, int32_t n, int32_t compute_un
       const int64_t reached = std::min<int64_t>(p.experts, pairs), routed_groups = reached + (pairs - reached) / MOE_GROUP;
       d.most_groups = (int32_t)(routed_groups + shared_groups);
       route += blocks * ((p.experts + ROUTE_EXPERTS - 1) / ROUTE_EXPERTS);
-      if (route > MOST_GRID) return refuse(err, SK_ERR_UNSUPPORTED, "more units of work than a launch's grid can hold");
-      out.route_first.push_back((uint32_t)route);
-      most_rows = std::max(most_rows, rows);
+      add += (rows * ((p.dim + ADD_COLUMNS - 1) / ADD_COLUMNS) + 3) / 4;
+      if (route > MOST_GRID || add > MOST_GRID) return refuse(err, SK_ERR_UNSUPPORTED, "more units of work than a launch's grid can hold");
+      out.route_first.push_back((uint32_t)route), out.add_first.push_back((uint32_t)add);
       tiles += std::max(d.most_groups * (int64_t)d.down_tiles, routed_groups * d.up_tiles + shared_groups * d.shared_tiles);
-      counters.take(d.routed, blocks * COUNTER_STEP), counters.take(d.blocks_routed, 1 * COUNTER_STEP), counters.take(d.summed, (int64_t)d.down_tiles * COUNTER_STEP);
-      work.take(d.logits, rows * p.experts), work.take(d.ids, pairs), work.take(d.weights, pairs), work.take(d.row_of, pairs), work.take(d.weight_of, pairs);
+      counters.take(d.routed, blocks * COUNTER_STEP), counters.take(d.blocks_routed, 1 * COUNTER_STEP);
+      work.take(d.logits, rows * p.experts), work.take(d.ids, pairs), work.take(d.weights, pairs), work.take(d.row_of, pairs), work.take(d.place_at, pairs);
       work.take(d.groups, d.most_groups), work.take(d.first_begin, d.most_groups), work.take(d.second_begin, d.most_groups);
       d.h_stride = (std::max<int64_t>(ffn, p.shared_ffn) + 63) / 64 * 128;
-      work.take(d.h, (pairs + (p.shared_ffn ? rows : 0)) * d.h_stride);
+      d.y_stride = (int64_t)d.down_tiles * 16;
+      const int64_t places = pairs + (p.shared_ffn ? rows : 0);
+      work.take(d.h, places * d.h_stride), work.take(d.y, places * d.y_stride);
       out.parts.push_back(d);
     }
     return SK_OK;
@@ -239,9 +241,6 @@ sk_status plan_moe(const sk_moe_problem *problems, int32_t n, int32_t compute_un
   // never more than there can be tiles
   auto cut = [&](int64_t resident) { return std::max<int64_t>(1, std::min<int64_t>(workgroups ? workgroups : resident * compute_units, tiles)); };
   out.up_workgroups = cut(MOE_UP_RESIDENT), out.down_workgroups = cut(MOE_DOWN_RESIDENT);
-  out.slice_floats = most_rows * 16;
-  work.take(out.slices, 2 * out.down_workgroups * out.slice_floats);
-  out.lds = (size_t)most_rows * 16 * sizeof(float);
   out.counters = counters.bytes;
   out.workspace = work.bytes;
   return SK_OK;

@@ -17,7 +17,6 @@ namespace sk {
 namespace moe {
 
 SK_BOTH int64_t least(int64_t a, int64_t b) { return a < b ? a : b; }
-SK_BOTH int64_t most(int64_t a, int64_t b) { return a > b ? a : b; }
 
 // Rows of activations that a tile is made for.
 SK_BOTH int32_t mode_of(int32_t rows) { return rows <= 8 ? 8 : rows <= 16 ? 16 : 32; }
@@ -31,12 +30,7 @@ struct Share {
   int64_t begin, end;
 };
 SK_BOTH Share share_of(int64_t total, int64_t shares, int64_t i) { return Share{total * i / shares, total * (i + 1) / shares}; }
-// The share that a place lies in.
-SK_BOTH int64_t owner_of(int64_t at, int64_t total, int64_t shares) { return ((at + 1) * shares - 1) / total; }
-// Second products: as many shares as there are workgroups, but none shorter than the longest tile, so that every share has the beginning of one.
-SK_BOTH int64_t shares_for(int64_t total, int64_t longest, int64_t workgroups) { return most(1, least(workgroups, total / most(longest, 1))); }
-
-// First products: all tiles of a group side by side.  The first tile that begins at or behind a place: group g is the last that begins at or before it (at
+// All tiles of a group stand side by side.  The first tile that begins at or behind a place: group g is the last that begins at or before it (at
 // `begin`, with `tiles` tiles of `each`); tile == tiles: the first of the next group.
 SK_BOTH int32_t tile_from(int64_t at, int64_t begin, int64_t each, int32_t tiles) { return (int32_t)least(tiles, (at - begin + each - 1) / each); }
 

@@ -84,7 +84,6 @@ static void moes() {
   need(sk::plan_moe(problems.data(), n, 256, workgroups, out, err) == SK_OK, err.c_str());
   Walk work(out.workspace), counters(out.counters);
   size_t at = 0;
-  int64_t most_rows = 0;
   for (int i = 0; i < n; ++i) {
     const sk_moe_problem &p = problems[(size_t)i];
     int64_t rows = 0;
@@ -93,7 +92,6 @@ static void moes() {
       const sk::MoeDev &d = out.parts[at];
       need(d.row0 == rows && d.rows >= 1 && d.rows <= sk::MOE_ROWS, "rows of a part");
       rows += d.rows;
-      most_rows = std::max<int64_t>(most_rows, d.rows);
       const int64_t pairs = (int64_t)d.rows * d.top_k, places = pairs + (d.shared_ffn ? d.rows : 0);
       // the most groups that any choice can give: every expert has a pair, and one (or some) all others
       int64_t most = std::min<int64_t>(d.experts, pairs);
@@ -103,20 +101,21 @@ static void moes() {
       need((int64_t)d.up_tiles * 16 >= d.ffn && (int64_t)d.down_tiles * 16 >= d.dim && (int64_t)d.shared_tiles * 16 >= d.shared_ffn, "tiles");
       need(out.route_first[at + 1] - out.route_first[at] == blocks * ((d.experts + sk::ROUTE_EXPERTS - 1) / sk::ROUTE_EXPERTS), "units of the router");
       need(d.h_stride >= 2 * std::max(d.ffn, d.shared_ffn) && d.h_stride % 128 == 0, "strides of the workspace");
+      need(d.y_stride >= d.dim && d.y_stride == (int64_t)d.down_tiles * 16, "strides of the sums");
+      need((int64_t)(out.add_first[at + 1] - out.add_first[at]) * 4 * sk::ADD_COLUMNS >= (int64_t)d.rows * d.dim, "units of the sums");
       need(d.count == out.counts + at, "counts");
-      counters.next(d.routed, blocks * sk::COUNTER_STEP), counters.next(d.blocks_routed, sk::COUNTER_STEP), counters.next(d.summed, (int64_t)d.down_tiles * sk::COUNTER_STEP);
-      work.next(d.logits, (int64_t)d.rows * d.experts), work.next(d.ids, pairs), work.next(d.weights, pairs), work.next(d.row_of, pairs), work.next(d.weight_of, pairs);
-      work.next(d.groups, d.most_groups), work.next(d.first_begin, d.most_groups), work.next(d.second_begin, d.most_groups), work.next(d.h, places * d.h_stride);
+      counters.next(d.routed, blocks * sk::COUNTER_STEP), counters.next(d.blocks_routed, sk::COUNTER_STEP);
+      work.next(d.logits, (int64_t)d.rows * d.experts), work.next(d.ids, pairs), work.next(d.weights, pairs), work.next(d.row_of, pairs), work.next(d.place_at, pairs);
+      work.next(d.groups, d.most_groups), work.next(d.first_begin, d.most_groups), work.next(d.second_begin, d.most_groups), work.next(d.h, places * d.h_stride), work.next(d.y, places * d.y_stride);
     }
     need(rows == p.rows, "all rows once");
   }
   need(at == out.parts.size(), "no other parts");
   for (const int64_t w : {out.up_workgroups, out.down_workgroups}) need(w >= 1 && (!workgroups || w <= workgroups), "workgroups");
-  need(out.slice_floats == most_rows * 16 && out.lds == (size_t)most_rows * 64 && out.lds <= 32768, "sums");
-  work.next(out.counts, (int64_t)out.parts.size()), work.next(out.slices, 2 * out.down_workgroups * out.slice_floats);
+  work.next(out.counts, (int64_t)out.parts.size());
 }
 
-// The shares of random work: every tile in one share, and of the second products as many slices as a tile's shares count.
+// The shares of random work: every tile in one share, in their order.
 static int32_t group_at(const std::vector<int64_t> &begin, int64_t at) {
   int32_t g = 0;
   while (g + 1 < (int32_t)begin.size() && begin[(size_t)g + 1] <= at) ++g;
@@ -124,94 +123,51 @@ static int32_t group_at(const std::vector<int64_t> &begin, int64_t at) {
 }
 static void shares() {
   struct Group {
-    int64_t each, second;
+    int64_t each;
     int32_t tiles;
   };
   struct Part {
     std::vector<Group> groups;
-    std::vector<int64_t> first_begin, second_begin;
-    int64_t first_work = 0, second_work = 0, down_tiles;
+    std::vector<int64_t> begin;
+    int64_t work = 0;
   };
   std::vector<Part> parts((size_t)between(1, 4));
-  int64_t first_total = 0, total = 0, longest = 0;
+  int64_t total = 0;
   for (Part &p : parts) {
-    const int32_t dim = (int32_t)between(1, between(0, 1) ? 300 : 9000), w = (int32_t)between(1, 2);
+    const int32_t w = (int32_t)between(1, 2);
     for (int64_t n = between(0, between(0, 1) ? 3 : 90); n > 0; --n) {
-      const int32_t mode = sk::moe::mode_of((int32_t)between(1, 32)), ffn = (int32_t)between(1, between(0, 1) ? 300 : 20000);
-      const Group g{sk::moe::cost(dim, w, mode), sk::moe::cost(ffn, 1, mode), (ffn + 15) / 16};
+      const Group g{sk::moe::cost((int32_t)between(1, between(0, 1) ? 300 : 9000), w, sk::moe::mode_of((int32_t)between(1, 32))), ((int32_t)between(1, between(0, 1) ? 300 : 20000) + 15) / 16};
       p.groups.push_back(g);
-      p.first_begin.push_back(p.first_work), p.second_begin.push_back(p.second_work);
-      p.first_work += g.each * g.tiles, p.second_work += g.second;
-      longest = std::max(longest, g.second);
+      p.begin.push_back(p.work);
+      p.work += g.each * g.tiles;
     }
-    p.down_tiles = between(1, 200);
-    first_total += p.first_work, total += p.second_work * p.down_tiles;
+    total += p.work;
   }
   const int64_t workgroups = between(1, between(0, 1) ? 20 : 1500);
   std::vector<std::pair<int32_t, int32_t>> seen(parts.size(), {0, 0});  // the next (group, tile)
   for (int64_t w = 0; w < workgroups; ++w) {
-    const sk::moe::Share s = sk::moe::share_of(first_total, workgroups, w);
+    const sk::moe::Share s = sk::moe::share_of(total, workgroups, w);
     int64_t offset = 0;
     for (size_t i = 0; i < parts.size(); ++i) {
       const Part &p = parts[i];
-      if (offset < s.end && s.begin < offset + p.first_work && p.first_work > 0) {
+      if (offset < s.end && s.begin < offset + p.work && p.work > 0) {
         std::pair<int32_t, int32_t> ends[2];
         for (int e = 0; e < 2; ++e) {
           const int64_t at = e ? s.end - offset : std::max<int64_t>(s.begin - offset, 0);
-          int32_t g = group_at(p.first_begin, at);
-          int32_t t = sk::moe::tile_from(at, p.first_begin[(size_t)g], p.groups[(size_t)g].each, p.groups[(size_t)g].tiles);
+          int32_t g = group_at(p.begin, at);
+          int32_t t = sk::moe::tile_from(at, p.begin[(size_t)g], p.groups[(size_t)g].each, p.groups[(size_t)g].tiles);
           if (t == p.groups[(size_t)g].tiles) ++g, t = 0;
           ends[e] = {g, t};
         }
         if (ends[0] < ends[1]) {
-          need(ends[0] == seen[i], "first products: a tile is left out or done twice");
+          need(ends[0] == seen[i], "a tile is left out or done twice");
           seen[i] = ends[1];
         }
       }
-      offset += p.first_work;
+      offset += p.work;
     }
   }
-  for (size_t i = 0; i < parts.size(); ++i) need(seen[i] == std::make_pair((int32_t)parts[i].groups.size(), 0), "first products: all tiles");
-
-  const int64_t shares = sk::moe::shares_for(total, longest, workgroups);
-  need(shares >= 1 && shares <= workgroups, "number of shares");
-  struct Tile {
-    int32_t next = 0;
-    int64_t slices = 0, first = -1, last = -1;
-  };
-  std::vector<std::vector<Tile>> tiles;
-  for (const Part &p : parts) tiles.emplace_back((size_t)p.down_tiles);
-  for (int64_t w = 0; w < shares; ++w) {
-    const sk::moe::Share s = sk::moe::share_of(total, shares, w);
-    int64_t offset = 0;
-    int begun = 0, ended = 0;  // tiles that this share begins but does not end, and the other way round
-    for (size_t i = 0; i < parts.size(); ++i) {
-      const Part &p = parts[i];
-      const int64_t each = p.second_work, here = each * p.down_tiles;
-      const int32_t all = (int32_t)p.groups.size();
-      if (here > 0 && s.begin < offset + here && offset < s.end) {
-        const int64_t begin = std::max<int64_t>(s.begin - offset, 0), end = std::min(s.end - offset, here);
-        auto group_from = [&](int64_t at) { return at <= 0 ? 0 : group_at(p.second_begin, at - 1) + 1; };
-        for (int64_t t = begin / each; t * each < end; ++t) {
-          const int32_t g0 = group_from(begin - t * each), g1 = group_from(std::min(end - t * each, each));
-          if (g0 >= g1) continue;
-          Tile &tile = tiles[i][(size_t)t];
-          need(g0 == tile.next && g1 <= all, "second products: a group is left out or done twice");
-          tile.next = g1;
-          if (g1 - g0 == all) continue;
-          const int64_t first = sk::moe::owner_of(offset + t * each, total, shares), last = sk::moe::owner_of(offset + t * each + p.second_begin.back(), total, shares);
-          need(tile.slices == w - first && w <= last && (tile.first < 0 || (tile.first == first && tile.last == last)), "second products: slices of a tile");
-          tile.first = first, tile.last = last;
-          ++tile.slices;
-          ++(w == first ? begun : ended);
-        }
-      }
-      offset += here;
-    }
-    need(begun <= 1 && ended <= 1, "second products: places of a workgroup's slices");
-  }
-  for (size_t i = 0; i < parts.size(); ++i)
-    for (const Tile &t : tiles[i]) need(t.next == (int32_t)parts[i].groups.size() && (t.first < 0 || t.slices == t.last - t.first + 1), "second products: all groups and slices of a tile");
+  for (size_t i = 0; i < parts.size(); ++i) need(seen[i] == std::make_pair((int32_t)parts[i].groups.size(), 0), "all tiles");
 }
 
 static void verifications() {
