@@ -515,8 +515,8 @@ __device__ __forceinline__ void up_run(const SK_CONSTANT MoeDev &P, const Run &r
 }
 
 // The sums of a place of the second products stand in the workspace, unweighted and in 32 bits: sk_moe_add takes them from there.  (To walk over all groups
-// of 16 columns, add their rows up in LDS and join the slices of the workgroups that share the columns saves those bytes, 8 of 230 us where 128 rows have
-// eight experts each, but 250 rows of 1000 columns took 75 us instead of 45 and the second products of one row 9.7 instead of 5.2 + 2.7.)
+// of 16 columns, add their rows up in LDS and join the slices of the workgroups that share the columns saves those stores, 12 of 230 us where 61 rows have
+// 4 of 60 experts each, but 250 rows of 1000 columns took 75 us instead of 45 and the second products of one row 9.7 instead of 5.2 + 2.7.)
 template <int DT, int MODE>
 __device__ __forceinline__ void down_run(const SK_CONSTANT MoeDev &P, const Run &run, bool shared, float *joint, int tid) {
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
