@@ -104,7 +104,7 @@ sk_status sk_norm_launch(sk_norm_plan *plan, void *hip_stream);
  * Products of the experts are summed in fp32, h is rounded to dtype for the matrix units, outputs are summed in fp32 and rounded
  * once.  An h beyond the type's range is infinite.  Each row's result depends on that row and the weights alone, up to the order of sums.
  * The weights are read once for up to 32 rows of an expert; made for the rows of decoder steps, it takes any number.  A row's sum goes over its experts
- * in the order of their numbers, the shared one last.
+ * in the order in which they were chosen, the shared one last.
  */
 typedef enum { SK_MOE_SOFTMAX = 0, SK_MOE_SIGMOID = 1 } sk_moe_scoring;
 

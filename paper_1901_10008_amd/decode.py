@@ -1,7 +1,7 @@
 """Decoder layers of several tenants' models, step after step: the framework's products and the operators over paged caches
 as a serving loop uses them.
 
-    python -m paper_1901_10008_amd.decode [--tenants 4] [--layers 2] [--prompt 500] [--children 4] [--steps 32]
+    python -m paper_1901_10008_amd.decode [--tenants 4] [--layers 2] [--prompt 500] [--children 4] [--steps 32] [--vocab 0] [--drafts 3] [--temperature 0.8]
 
 Every tenant has weights, pages and sequences of its own.  A layer is, for all tenants at once,
 
@@ -11,8 +11,20 @@ Every tenant has weights, pages and sequences of its own.  A layer is, for all t
     sk_launch        the products with the output weights, one launch
 
 and the hidden states take up the result (a torch addition).  First the prompts, all rows at once; then every tenant's prompt is
-forked into `children` continuations, which share its pages until they write to them, and each gets a token a step.  There is no
-vocabulary: a step's input is the last hidden state of the sequence, scaled to unit size.
+forked into `children` continuations, which share its pages until they write to them, and each gets a token a step.  Without a
+vocabulary a step's input is the last hidden state of the sequence, scaled to unit size.
+
+With --vocab the tenants are whole language models.  A layer has besides
+
+    sk_norm_launch   the block before joins the residual stream (32 bits), and the norm before the next block: around attention and experts
+    sk_moe_launch    a mixture-of-experts layer behind attention
+
+and behind the last layer come one more sk_norm_launch, the logits (sk_launch) and
+
+    sk_verify_launch which of `drafts` drafted tokens a sequence stay, and the token behind them
+
+Drafts are looked up in what the sequence holds already.  Pages of rejected ones are given back (sk_pages_resize), and a step's last tokens are
+the next one's first.
 """
 from __future__ import annotations
 
@@ -23,7 +35,9 @@ import time
 import torch
 
 from . import (SK_GEMM, make_attn_problem, make_page_arrays, sk_attn_append, sk_attn_launch, sk_attn_plan_create, sk_launch, sk_pages_apply, sk_pages_create,
-               sk_pages_fork, sk_pages_resize, sk_pages_state, sk_plan_create, sk_problem)
+               sk_pages_fork, sk_pages_resize, sk_pages_state, sk_plan_create, sk_problem,
+               SK_ACT_SILU, make_moe_problem, make_norm_problem, make_verify_problem, sk_moe_launch, sk_moe_plan_create, sk_norm_launch, sk_norm_plan_create,
+               sk_verify_launch, sk_verify_plan_create)
 
 DTYPE = torch.bfloat16
 
@@ -159,12 +173,157 @@ def serve(tenants, prompts, children, steps, stream, seen=None):
     return last, prompt_s, step_s
 
 
+class LanguageModel(Tenant):
+    """A tenant with a vocabulary, norms around its blocks and a mixture-of-experts layer behind attention."""
+
+    def __init__(self, hidden, heads, layers, sequences, most_tokens, vocab, experts=8, top_k=2, ffn=None, shared=0, seed=0, **tenant):
+        super().__init__(hidden, heads, layers, sequences, most_tokens, seed=seed, **tenant)
+        g = torch.Generator(device="cuda").manual_seed(seed + 1000003)
+
+        def normal(*shape, scale=1.0):
+            return (torch.randn(shape, generator=g, device="cuda") * scale).to(DTYPE)
+
+        self.vocab, self.experts, self.top_k, self.ffn, self.shared = vocab, experts, top_k, ffn or 2 * hidden, shared
+        self.embedding = normal(vocab, hidden)
+        self.head = normal(vocab, hidden, scale=2 * hidden ** -0.5)
+        self.norms = [1 + normal(hidden, scale=0.1) for _ in range(2 * layers + 1)]  # before attention and experts of each layer, before the head
+        self.router = [normal(experts, hidden, scale=hidden ** -0.5) for _ in range(layers)]
+        self.gate, self.up = ([normal(experts, self.ffn, hidden, scale=hidden ** -0.5) for _ in range(layers)] for _ in range(2))
+        self.down = [normal(experts, hidden, self.ffn, scale=self.ffn ** -0.5) for _ in range(layers)]
+        self.shared_gate, self.shared_up = ([normal(shared, hidden, scale=hidden ** -0.5) for _ in range(layers)] for _ in range(2))
+        self.shared_down = [normal(hidden, shared, scale=max(shared, 1) ** -0.5) for _ in range(layers)]
+
+
+class TokenStep:
+    """The launches of a step of language models: tokens in, tokens out.  Tenant i has rows[i] rows, of which the last answered[i] get logits and belong
+    to sequences[i] sequences, equally many to each; all but the last of a sequence may have a draft's token behind them."""
+
+    def __init__(self, tenants, rows, most_new, answered, sequences, temperature):
+        self.tenants, self.rows, self.answered = tenants, rows, answered
+        each = lambda dtype, *of: [torch.zeros(shape, dtype=dtype, device="cuda") for shape in zip(*of)]  # noqa: E731
+        hidden = [t.hidden for t in tenants]
+        self.tokens_in = [torch.zeros(n, dtype=torch.int64, device="cuda") for n in rows]
+        self.residual, self.x, self.y = each(torch.float32, rows, hidden), each(DTYPE, rows, hidden), each(DTYPE, rows, hidden)
+        self.qkv, self.q = each(DTYPE, rows, [(t.hq + 2 * t.hkv) * t.d for t in tenants]), each(DTYPE, rows, [t.hq * t.d for t in tenants])
+        self.out, self.logits = each(DTYPE, rows, [t.hq * t.d for t in tenants]), each(DTYPE, answered, [t.vocab for t in tenants])
+        self.drafted, self.accept, self.tokens = each(torch.int32, answered), each(torch.float32, answered), each(torch.int32, answered)
+        self.sample, self.accepted = each(torch.float32, sequences), each(torch.int32, sequences)
+        self.first_row = [torch.arange(0, n + 1, n // s, dtype=torch.int32, device="cuda") for n, s in zip(answered, sequences)]
+        layers = tenants[0].layers
+        self.chosen = [each(torch.int32, rows, [t.top_k for t in tenants]) for _ in range(layers)]
+
+        def norm(at):  # the block before into the residual stream, and the norm that stands before the next one
+            return sk_norm_plan_create([make_norm_problem(
+                dtype="bf16", residual_dtype="f32", rows=n, dim=t.hidden, eps=1e-6, block=0 if not at else y.data_ptr(), residual=r.data_ptr(), pre_weight=t.norms[at].data_ptr(),
+                residual_out=0 if not at else r.data_ptr(), next=x.data_ptr()) for t, n, r, x, y in zip(tenants, rows, self.residual, self.x, self.y)])
+
+        self.plans = []  # (launch, plan), in their order
+        for layer in range(layers):
+            attend = sk_attn_plan_create([make_attn_problem(
+                dtype="bf16", q_heads=t.hq, kv_heads=t.hkv, head_dim=t.d, page_tokens=t.page, num_pages=t.pages, sequences=t.sequences,
+                pages_per_sequence=t.columns, rows=n, max_new=most_new, window=t.window, sinks=t.sinks, rotary_dim=t.d, positions=t.cos.shape[0], eps=1e-6,
+                k=t.cache[layer, 0].data_ptr(), v=t.cache[layer, 1].data_ptr(), page_table=t.table.data_ptr(), lengths=t.lengths.data_ptr(),
+                first_row=t.first_row.data_ptr(), qkv=qkv.data_ptr(), q_weight=t.q_norm[layer].data_ptr(), k_weight=t.k_norm[layer].data_ptr(),
+                cos=t.cos.data_ptr(), sin=t.sin.data_ptr(), q=q.data_ptr(), out=out.data_ptr())
+                for t, n, qkv, q, out in zip(tenants, rows, self.qkv, self.q, self.out)])
+            experts = sk_moe_plan_create([make_moe_problem(
+                dtype="bf16", rows=n, dim=t.hidden, experts=t.experts, top_k=t.top_k, ffn=t.ffn, shared_ffn=t.shared, act=SK_ACT_SILU, normalize=1, x=x.data_ptr(),
+                router=t.router[layer].data_ptr(), gate=t.gate[layer].data_ptr(), up=t.up[layer].data_ptr(), down=t.down[layer].data_ptr(), out=y.data_ptr(),
+                expert_ids=ids.data_ptr(), **(dict(shared_gate=t.shared_gate[layer].data_ptr(), shared_up=t.shared_up[layer].data_ptr(),
+                                                   shared_down=t.shared_down[layer].data_ptr()) if t.shared else {}))
+                for t, n, x, y, ids in zip(tenants, rows, self.x, self.y, self.chosen[layer])])
+            into = sk_plan_create([_product(x, t.w_qkv[layer], c) for t, x, c in zip(tenants, self.x, self.qkv)])
+            out_of = sk_plan_create([_product(out, t.w_out[layer], y) for t, out, y in zip(tenants, self.out, self.y)])
+            self.plans += [(sk_norm_launch, norm(2 * layer)), (sk_launch, into), (sk_attn_append, attend), (sk_attn_launch, attend), (sk_launch, out_of),
+                           (sk_norm_launch, norm(2 * layer + 1)), (sk_moe_launch, experts)]
+        verify = sk_verify_plan_create([make_verify_problem(
+            dtype="bf16", sequences=s, rows=n, vocab=t.vocab, temperature=temperature, first_row=first.data_ptr(), logits=l.data_ptr(), drafted=drafted.data_ptr(),
+            accept_random=accept.data_ptr(), sample_random=sample.data_ptr(), tokens=tokens.data_ptr(), accepted=accepted.data_ptr())
+            for t, n, s, first, l, drafted, accept, sample, tokens, accepted in
+            zip(tenants, answered, sequences, self.first_row, self.logits, self.drafted, self.accept, self.sample, self.tokens, self.accepted)])
+        self.plans += [(sk_norm_launch, norm(2 * layers)), (sk_launch, sk_plan_create([_product(x[-n:], t.head, l) for t, n, x, l in zip(tenants, answered, self.x, self.logits)])),
+                       (sk_verify_launch, verify)]
+
+    def run(self, stream):
+        """self.tokens_in, drafted, accept and sample in; self.tokens and accepted out."""
+        for t, r, tokens in zip(self.tenants, self.residual, self.tokens_in):
+            r.copy_(t.embedding[tokens])
+        for launch, plan in self.plans:
+            launch(plan, stream)
+
+    def close(self):
+        for p in {id(plan): plan for _, plan in self.plans}.values():
+            p.close()
+
+
+def looked_up(history, n):
+    """n drafted tokens: what followed where the last token stood before; -1 where nothing did."""
+    for at in range(len(history) - 2, -1, -1):
+        if history[at] == history[-1]:
+            found = history[at + 1:at + 1 + n]
+            return found + [-1] * (n - len(found))
+    return [-1] * n
+
+
+def generate(tenants, prompts, children, steps, drafts, temperature, stream, seed=0, seen=None):
+    """Prompts (token numbers per tenant), a fork into `children` continuations, then `steps` steps of `drafts` drafted tokens each.  Returns the
+    continuations' tokens per tenant (the prompt first), seconds of the prompts and of a step.  seen(step, launches, histories) is called behind each step with what each
+    sequence held before it."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    one = [1] * len(tenants)
+    first = TokenStep(tenants, [len(p) for p in prompts], max(len(p) for p in prompts), one, one, temperature)
+    for t, tokens, sample, p in zip(tenants, first.tokens_in, first.sample, prompts):
+        tokens.copy_(torch.tensor(p))
+        sample.uniform_(generator=g)
+        grow(t, [0], [len(p)], [len(p)] + [0] * (t.sequences - 1), stream)
+    torch.cuda.synchronize()
+    begin = time.perf_counter()
+    first.run(stream)
+    torch.cuda.synchronize()
+    prompt_s = time.perf_counter() - begin
+    if seen:
+        seen(0, first, [[[]] for _ in tenants])
+    histories = [[p + [int(tokens[-1])] for _ in range(children)] for p, tokens in zip(prompts, first.tokens)]
+    for t in tenants:
+        sk_pages_fork(t.account, 0, range(1, children))
+    width = drafts + 1
+    each = TokenStep(tenants, [children * width] * len(tenants), width, [children * width] * len(tenants), [children] * len(tenants), temperature)
+    begin = time.perf_counter()
+    for n in range(steps):
+        for i, t in enumerate(tenants):
+            guess = [looked_up(h, drafts) for h in histories[i]]
+            each.tokens_in[i].copy_(torch.tensor([[h[-1]] + [max(d, 0) for d in ds] for h, ds in zip(histories[i], guess)]).flatten())
+            each.drafted[i].copy_(torch.tensor([ds + [-1] for ds in guess], dtype=torch.int32).flatten())
+            each.accept[i].uniform_(generator=g)
+            each.sample[i].uniform_(generator=g)
+            grow(t, list(range(children)), [len(h) + drafts for h in histories[i]], [width] * children + [0] * (t.sequences - children), stream)
+        each.run(stream)
+        if seen:
+            seen(n + 1, each, [[list(h) for h in hs] for hs in histories])
+        for i, t in enumerate(tenants):
+            tokens = each.tokens[i].view(children, width).tolist()
+            for h, new in zip(histories[i], tokens):
+                h += [x for x in new if x >= 0]
+            # the last token is the next step's first: its keys and values are not there yet
+            sk_pages_resize(t.account, list(range(children)), [len(h) - 1 for h in histories[i]])
+    torch.cuda.synchronize()
+    step_s = (time.perf_counter() - begin) / max(steps, 1)
+    first.close()
+    each.close()
+    return histories, prompt_s, step_s
+
+
 def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     for name, value in (("tenants", 4), ("layers", 2), ("prompt", 500), ("children", 4), ("steps", 32)):
         ap.add_argument("--" + name, type=int, default=value)
+    ap.add_argument("--vocab", type=int, default=0, help="tokens of the models' vocabularies; 0: no vocabulary")
+    ap.add_argument("--drafts", type=int, default=3, help="drafted tokens a step (with --vocab)")
+    ap.add_argument("--temperature", type=float, default=0.8, help="of the tokens (with --vocab)")
     a = ap.parse_args(argv)
     kinds = [(768, (12, 12, 64), 0, 0), (2048, (16, 4, 128), 0, 0), (1024, (16, 4, 80), 256, 4)]
+    if a.vocab:
+        return _main_tokens(a, kinds)
     tenants = [Tenant(h, heads, a.layers, a.children, a.prompt + 64 + a.steps, window=w, sinks=s, seed=i)
                for i, (h, heads, w, s) in ((i, kinds[i % len(kinds)]) for i in range(a.tenants))]
     g = torch.Generator(device="cuda").manual_seed(99)
@@ -178,6 +337,18 @@ def main(argv=None):
         free, _ = sk_pages_state(t.account)
         print(f"  tenant {i}: {t.hq}/{t.hkv} heads of {t.d}, {t.pages - free} pages for {a.children} sequences of {t.lengths[0].item()} tokens, "
               f"last hidden states of size {x.float().square().mean().sqrt().item():.3f}")
+
+
+
+def _main_tokens(a, kinds):
+    tenants = [LanguageModel(h, heads, a.layers, a.children, a.prompt + 64 + a.steps * (a.drafts + 1), a.vocab, window=w, sinks=s, seed=i, shared=h if i % 2 else 0)
+               for i, (h, heads, w, s) in ((i, kinds[i % len(kinds)]) for i in range(a.tenants))]
+    g = torch.Generator().manual_seed(99)
+    prompts = [torch.randint(0, a.vocab, (a.prompt + 7 * i,), generator=g).tolist() for i in range(a.tenants)]
+    histories, prompt_s, step_s = generate(tenants, prompts, a.children, a.steps, a.drafts, a.temperature, torch.cuda.current_stream().cuda_stream)
+    made = sum(len(h) - len(p) - 1 for p, hs in zip(prompts, histories) for h in hs)
+    print(f"{a.tenants} language models, {a.layers} layers, {a.vocab} tokens: prompts of {sum(map(len, prompts))} rows {prompt_s * 1e3:.2f} ms; {a.children} continuations of each, "
+          f"{a.steps} steps of {a.drafts} drafts, {step_s * 1e3:.3f} ms a step, {made / max(a.steps * a.tenants * a.children, 1):.2f} tokens a sequence and step")
 
 
 if __name__ == "__main__":
