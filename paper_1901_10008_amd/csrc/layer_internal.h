@@ -87,7 +87,6 @@ struct MoeDev {
   int64_t x_stride, out_stride, router_stride, up_expert, down_expert, up_row, down_row;
   int32_t row0, rows, dim, experts, top_k, ffn, shared_ffn, act, scoring, normalize, dtype, router_f32;
   float scale;
-  int32_t up_tiles, shared_tiles, down_tiles;        // tiles of 16 rows of weights
   int32_t most_groups;                               // with those of the shared expert
   // workspace
   double *logits;         // [rows][experts]

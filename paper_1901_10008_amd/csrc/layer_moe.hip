@@ -190,8 +190,10 @@ struct Costs {
   int64_t of[3];
   __device__ __forceinline__ int64_t sum(int64_t counts) const { return of_mode(counts, 8) * of[0] + of_mode(counts, 16) * of[1] + of_mode(counts, 32) * of[2]; }
 };
-__device__ __forceinline__ Costs costs_of(int32_t k_len, int32_t matrices) {
-  return Costs{{moe::cost(k_len, matrices, 8), moe::cost(k_len, matrices, 16), moe::cost(k_len, matrices, 32)}};
+// (of all tiles of a group)
+__device__ __forceinline__ Costs costs_of(int32_t k_len, int32_t matrices, int32_t rows) {
+  return Costs{{moe::cost(k_len, matrices, 8) * moe::tiles_of(rows, matrices, 8), moe::cost(k_len, matrices, 16) * moe::tiles_of(rows, matrices, 16),
+                moe::cost(k_len, matrices, 32) * moe::tiles_of(rows, matrices, 32)}};
 }
 
 // here: ids and weights are in LDS already.
@@ -213,7 +215,8 @@ __device__ __forceinline__ void sort_pairs(const SK_CONSTANT MoeDev &P, int32_t 
   }
   __syncthreads();
   if (tid < 64) {
-    const Costs up = costs_of(P.dim, P.gate ? 2 : 1), down = costs_of(P.ffn, 1);
+    const int32_t matrices = P.gate ? 2 : 1;
+    const Costs up = costs_of(P.dim, matrices, P.ffn), down = costs_of(P.ffn, 1, P.dim);
     int64_t all = 0;
     for (int32_t e0 = 0; e0 < P.experts; e0 += 64) {
       const int32_t e = e0 + tid, n = e < P.experts ? s.count[e] : 0, g = (n + MOE_GROUP - 1) / MOE_GROUP;
@@ -222,24 +225,24 @@ __device__ __forceinline__ void sort_pairs(const SK_CONSTANT MoeDev &P, int32_t 
       if (e < P.experts) s.first[e] = place;
       for (int32_t i = 0; i < g; ++i) {  // (all but the last are full)
         P.groups[at + i] = MoeGroup{e, place + i * MOE_GROUP, min(MOE_GROUP, n - i * MOE_GROUP), 0};
-        P.first_begin[at + i] = (up.sum(before) + i * up.of[2]) * P.up_tiles;
-        P.second_begin[at + i] = (down.sum(before) + i * down.of[2]) * P.down_tiles;
+        P.first_begin[at + i] = up.sum(before) + i * up.of[2];
+        P.second_begin[at + i] = down.sum(before) + i * down.of[2];
       }
       all += lane_of(upto, 63);
     }
-    MoeCount c{groups_in(all), rows, up.sum(all) * P.up_tiles, down.sum(all) * P.down_tiles};
+    MoeCount c{groups_in(all), rows, up.sum(all), down.sum(all)};
     if (P.shared_ffn) {  // (at most 16 groups)
       const int32_t g = (rows + MOE_GROUP - 1) / MOE_GROUP, n = min(MOE_GROUP, rows - tid * MOE_GROUP);
-      const Costs shared = costs_of(P.shared_ffn, 1);
+      const Costs shared_up = costs_of(P.dim, matrices, P.shared_ffn), shared_down = costs_of(P.shared_ffn, 1, P.dim);
       if (tid < g) {
         P.groups[c.groups + tid] = MoeGroup{-1, tid * MOE_GROUP, n, 0};
-        P.first_begin[c.groups + tid] = c.first_work + tid * up.of[2] * P.shared_tiles;
-        P.second_begin[c.groups + tid] = c.second_work + tid * shared.of[2] * P.down_tiles;
+        P.first_begin[c.groups + tid] = c.first_work + tid * shared_up.of[2];
+        P.second_begin[c.groups + tid] = c.second_work + tid * shared_down.of[2];
       }
       const int64_t counts = groups_of(rows);
       c.groups += g;
-      c.first_work += up.sum(counts) * P.shared_tiles;
-      c.second_work += shared.sum(counts) * P.down_tiles;
+      c.first_work += shared_up.sum(counts);
+      c.second_work += shared_down.sum(counts);
     }
     if (tid == 0) *P.count = c;
   }
@@ -282,7 +285,7 @@ __global__ void __launch_bounds__(CACHE_THREADS) sk_moe_route(MoeArgs a) {
 // ---------------------------------------------------------------------------
 // the experts' products
 // ---------------------------------------------------------------------------
-// A tile is 16 rows of an expert's weights times the rows of activations of a group; the four waves of a workgroup take the blocks of 64 elements
+// A tile is 16 or 32 rows of an expert's weights times the rows of activations of a group; the four waves of a workgroup take the blocks of 64 elements
 // (128 bytes a row) of its reduction in turn, and add their sums up in LDS.  Bound by the memory that the weights come from: an instruction loads
 // eight whole lines of 128 bytes, lane (r, q) of the 16 x 4 that the matrix instruction sees row r % 8 (+ 8), bytes 16 (q + 4 (r / 8)).
 //   Up to 8 rows of activations (MODE 8): the matrix instruction takes the weights as they came, rows 0 .. 7 with the lower half of the block and once
@@ -328,29 +331,34 @@ __device__ __forceinline__ const char *uniform(const char *p) {
   return (const char *)(uintptr_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int32_t)(a >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int32_t)a));
 }
 
-// W matrices of weights with the same rows and the same activations (gate and up).  The stream of loads runs R blocks ahead of the matrix instructions, from
+// W matrices of weights with the same rows and the same activations (gate and up), of each S times 16 rows.  The stream of loads runs R blocks ahead of the matrix instructions, from
 // tile to tile, so it is only empty at the beginning and the end of a run.  group(i) is the i-th group, base(g, m) its matrix m, x_base(g) and x_offset(g, i)
 // where its i-th row of activations stands; done(t, group, tile) takes up the sums of turn t.
-template <int DT, int MODE, int W, int R, class G, class B, class XB, class XO, class D>
+template <int DT, int MODE, int W, int S, int R, class G, class B, class XB, class XO, class D>
 __device__ __forceinline__ void stream(const Run &run, int32_t tiles, int64_t row_stride, int32_t rows_end, int32_t k_len, G group, B base, XB x_base, XO x_offset, D done, float *joint,
                                        int wave, int lane) {
   constexpr int NB = MODE == 32 ? 2 : 1, H = MODE == 8 ? 1 : 2, A = MODE == 8 ? 2 : NB;  // loads of activations for 16 rows, sums
   const int r16 = lane & 15, q = lane >> 4;
   const int32_t steps = (k_len + 255) / 256;  // of the four waves' blocks each
   const uint32_t w_piece = 16 * (q + 4 * (r16 >> 3)), x_piece = MODE == 8 ? w_piece : 16 * q;
-  u32x4 w[R][W][2], b[R][NB][H];
-  f32x4 acc[W][A] = {};
+  constexpr int WS = W * S;  // (matrix m, rows s at m * S + s)
+  u32x4 w[R][WS][2], b[R][NB][H];
+  f32x4 acc[WS][A] = {};
 
   // loads
   int32_t p_left = run.n, p_group = run.group, p_tile = run.tile, p_step = 0;
   MoeGroup pg = group(p_group);
-  const char *w_base[W], *x_at;
-  uint32_t w_row[2], x_row[NB];
+  const char *w_base[WS], *x_at;
+  uint32_t w_row[S][2], x_row[NB];
   auto new_rows = [&]() {
 #pragma unroll
-    for (int m = 0; m < W; ++m) w_base[m] = uniform(base(pg, m) + (int64_t)p_tile * TILE * row_stride);
+    for (int s = 0; s < S; ++s) {
+      const int32_t row = min((p_tile * S + s) * TILE, rows_end - 1);  // (rows behind the last repeat it and are not used)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) w_row[j] = (uint32_t)min(8 * j + (r16 & 7), rows_end - 1 - p_tile * TILE) * (uint32_t)row_stride + w_piece;
+      for (int m = 0; m < W; ++m) w_base[m * S + s] = uniform(base(pg, m) + (int64_t)row * row_stride);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) w_row[s][j] = (uint32_t)min(8 * j + (r16 & 7), rows_end - 1 - row) * (uint32_t)row_stride + w_piece;
+    }
   };
   auto new_group = [&]() {
     x_at = uniform(x_base(pg));
@@ -359,15 +367,18 @@ __device__ __forceinline__ void stream(const Run &run, int32_t tiles, int64_t ro
   };
   new_group();
   new_rows();
-  auto load = [&](u32x4(&w)[W][2], u32x4(&b)[NB][H]) {
+  auto load = [&](u32x4(&w)[WS][2], u32x4(&b)[NB][H]) {
     // zeros behind the end of the reduction and behind the last tile
     const int32_t k = (wave + 4 * p_step) * 128, left = p_left > 0 ? 2 * k_len - k : 0;
     const bool in = (int32_t)w_piece < left;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const uint32_t at = in ? w_row[j] : OUTSIDE;
 #pragma unroll
-      for (int m = 0; m < W; ++m) w[m][j] = load_from(w_base[m], at, k);
+      for (int s = 0; s < S; ++s) {
+        const uint32_t at = in ? w_row[s][j] : OUTSIDE;
+#pragma unroll
+        for (int m = 0; m < W; ++m) w[m * S + s][j] = load_from(w_base[m * S + s], at, k);
+      }
     }
 #pragma unroll
     for (int h = 0; h < H; ++h) {
@@ -395,7 +406,7 @@ __device__ __forceinline__ void stream(const Run &run, int32_t tiles, int64_t ro
 #pragma unroll
     for (int u = 0; u < R; ++u) {
 #pragma unroll
-      for (int m = 0; m < W; ++m) {
+      for (int m = 0; m < WS; ++m) {
         if constexpr (MODE == 8) {
           mma16<DT>(w[u][m][0], b[u][0][0], acc[m][0]);
           mma16<DT>(w[u][m][1], b[u][0][0], acc[m][1]);
@@ -414,13 +425,13 @@ __device__ __forceinline__ void stream(const Run &run, int32_t tiles, int64_t ro
         if (t < run.n) {  // (the steps behind the last tile multiply zeros)
           // lane (r, q) has, for row r of activations, rows 4q .. 4q + 3 of weights
 #pragma unroll
-          for (int m = 0; m < W; ++m)
+          for (int m = 0; m < WS; ++m)
 #pragma unroll
             for (int n = 0; n < A; ++n) {
               if constexpr (MODE == 8) {
-                if ((q >> 1) == (r16 >> 3)) *joint_at<W>(joint, t, wave, m, r16, 8 * n + 4 * (q & 1)) = acc[m][n];
+                if ((q >> 1) == (r16 >> 3)) *joint_at<WS>(joint, t, wave, m, r16, 8 * n + 4 * (q & 1)) = acc[m][n];
               } else {
-                *joint_at<W>(joint, t, wave, m, n * 16 + r16, 4 * q) = acc[m][n];
+                *joint_at<WS>(joint, t, wave, m, n * 16 + r16, 4 * q) = acc[m][n];
               }
               acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
             }
@@ -486,7 +497,7 @@ __device__ __forceinline__ int32_t run_end(const SK_CONSTANT MoeDev &P, int32_t 
 
 template <int DT, int MODE, bool GATED>
 __device__ __forceinline__ void up_run(const SK_CONSTANT MoeDev &P, const Run &run, bool shared, float *joint, const int32_t *row_of, int tid) {
-  constexpr int W = GATED ? 2 : 1;
+  constexpr int W = GATED ? 2 : 1, S = moe::rows_of_tile(W, MODE) / TILE;
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int32_t width = shared ? P.shared_ffn : P.ffn, place0 = group_of(P, run.group).first;
   auto base = [&](const MoeGroup &g, int m) {
@@ -495,11 +506,11 @@ __device__ __forceinline__ void up_run(const SK_CONSTANT MoeDev &P, const Run &r
   };
   auto done = [&](int32_t t, int32_t group, int32_t tile) {
     const MoeGroup g = group_of(P, group);
-    const int32_t i = tid >> 2, f = tile * TILE + 4 * (tid & 3);
-    if (i >= g.rows || f >= width) return;  // (width is a multiple of 8)
-    f32x4 h = joined<MODE, W>(joint, t, 0, i, tid & 3);
+    const int32_t i = (tid >> 2) % MOE_GROUP, s = tid / (4 * MOE_GROUP), f = (tile * S + s) * TILE + 4 * (tid & 3);
+    if (i >= g.rows || s >= S || f >= width) return;  // (width is a multiple of 8)
+    f32x4 h = joined<MODE, W * S>(joint, t, s, i, tid & 3);
     if constexpr (GATED) {
-      const f32x4 z = joined<MODE, W>(joint, t, 1, i, tid & 3);
+      const f32x4 z = joined<MODE, W * S>(joint, t, S + s, i, tid & 3);
 #pragma unroll
       for (int k = 0; k < 4; ++k) h[k] *= activated(P.act, z[k]);
     } else {
@@ -509,8 +520,8 @@ __device__ __forceinline__ void up_run(const SK_CONSTANT MoeDev &P, const Run &r
     const int64_t place = (shared ? (int64_t)P.rows * P.top_k : 0) + g.first + i;
     store8(P.h + place * P.h_stride + 2 * f, u32x2{pack2<DT>(h[0], h[1]), pack2<DT>(h[2], h[3])});
   };
-  stream<DT, MODE, W, MODE == 8 ? 3 : 2>(
-      run, shared ? P.shared_tiles : P.up_tiles, shared ? 2 * (int64_t)P.dim : P.up_row, width, P.dim, [&](int32_t i) { return group_of(P, i); }, base, [&](const MoeGroup &) { return P.x; },
+  stream<DT, MODE, W, S, MODE == 8 ? 3 : 2>(
+      run, moe::tiles_of(width, W, MODE), shared ? 2 * (int64_t)P.dim : P.up_row, width, P.dim, [&](int32_t i) { return group_of(P, i); }, base, [&](const MoeGroup &) { return P.x; },
       [&](const MoeGroup &g, int32_t i) { return (uint32_t)row_of[g.first - place0 + i] * (uint32_t)P.x_stride; }, done, joint, wave, lane);
 }
 
@@ -519,18 +530,18 @@ __device__ __forceinline__ void up_run(const SK_CONSTANT MoeDev &P, const Run &r
 // 4 of 60 experts each, but 250 rows of 1000 columns took 75 us instead of 45 and the second products of one row 9.7 instead of 5.2 + 2.7.)
 template <int DT, int MODE>
 __device__ __forceinline__ void down_run(const SK_CONSTANT MoeDev &P, const Run &run, bool shared, float *joint, int tid) {
+  constexpr int S = moe::rows_of_tile(1, MODE) / TILE;
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t place0 = shared ? (int64_t)P.rows * P.top_k : 0;
   const int32_t width = shared ? P.shared_ffn : P.ffn;
   auto done = [&](int32_t t, int32_t group, int32_t tile) {
     const MoeGroup g = group_of(P, group);
-    const int32_t i = tid >> 2;
-    if (i >= g.rows) return;
-    // (a row of them has whole tiles)
-    *(f32x4 SK_GLOBAL *)(uintptr_t)(P.y + (place0 + g.first + i) * P.y_stride + tile * TILE + 4 * (tid & 3)) = joined<MODE, 1>(joint, t, 0, i, tid & 3);
+    const int32_t i = (tid >> 2) % MOE_GROUP, s = tid / (4 * MOE_GROUP), d = (tile * S + s) * TILE + 4 * (tid & 3);
+    if (i >= g.rows || s >= S || d >= P.dim) return;  // (dim is a multiple of 8)
+    *(f32x4 SK_GLOBAL *)(uintptr_t)(P.y + (place0 + g.first + i) * P.y_stride + d) = joined<MODE, S>(joint, t, s, i, tid & 3);
   };
-  stream<DT, MODE, 1, MODE == 8 ? 4 : MODE == 16 ? 3 : 2>(
-      run, P.down_tiles, shared ? 2 * (int64_t)width : P.down_row, P.dim, width, [&](int32_t i) { return group_of(P, i); },
+  stream<DT, MODE, 1, S, MODE == 8 ? 4 : 2>(
+      run, moe::tiles_of(P.dim, 1, MODE), shared ? 2 * (int64_t)width : P.down_row, P.dim, width, [&](int32_t i) { return group_of(P, i); },
       [&](const MoeGroup &g, int) { return shared ? P.shared_down : P.down + g.expert * P.down_expert; }, [&](const MoeGroup &g) { return P.h + (place0 + g.first) * P.h_stride; },
       [&](const MoeGroup &, int32_t i) { return (uint32_t)i * (uint32_t)P.h_stride; }, done, joint, wave, lane);
 }
@@ -539,7 +550,9 @@ __device__ __forceinline__ void down_run(const SK_CONSTANT MoeDev &P, const Run 
 template <bool UP>
 struct Products {
   static __device__ __forceinline__ int64_t work(const SK_CONSTANT MoeCount &c) { return UP ? c.first_work : c.second_work; }
-  static __device__ __forceinline__ int32_t tiles(const SK_CONSTANT MoeDev &P, const MoeGroup &g) { return !UP ? P.down_tiles : g.expert < 0 ? P.shared_tiles : P.up_tiles; }
+  static __device__ __forceinline__ int32_t tiles(const SK_CONSTANT MoeDev &P, const MoeGroup &g) {
+    return moe::tiles_of(!UP ? P.dim : g.expert < 0 ? P.shared_ffn : P.ffn, UP && P.gate ? 2 : 1, moe::mode_of(g.rows));
+  }
   static __device__ __forceinline__ int64_t cost(const SK_CONSTANT MoeDev &P, const MoeGroup &g) {
     return UP ? moe::cost(P.dim, P.gate ? 2 : 1, moe::mode_of(g.rows)) : moe::cost(g.expert < 0 ? P.shared_ffn : P.ffn, 1, moe::mode_of(g.rows));
   }
@@ -607,7 +620,7 @@ __global__ void __launch_bounds__(CACHE_THREADS, MOE_UP_RESIDENT) sk_moe_up(MoeA
 }
 
 __global__ void __launch_bounds__(CACHE_THREADS, MOE_DOWN_RESIDENT) sk_moe_down(MoeArgs a) {
-  __shared__ __attribute__((aligned(16))) float joint[joint_floats(1)];
+  __shared__ __attribute__((aligned(16))) float joint[joint_floats(2)];
   Products<false>::share(a, joint, nullptr, threadIdx.x);
 }
 

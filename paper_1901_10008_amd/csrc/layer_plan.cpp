@@ -213,7 +213,6 @@ sk_status plan_moe(const sk_moe_problem *problems, int32_t n, int32_t compute_un
       d.row0 = (int32_t)row0, d.rows = (int32_t)rows, d.dim = p.dim, d.experts = p.experts, d.top_k = p.top_k, d.ffn = p.ffn, d.shared_ffn = p.shared_ffn;
       d.act = p.act, d.scoring = p.scoring, d.normalize = p.normalize, d.dtype = p.dtype, d.router_f32 = p.router_dtype == SK_F32;
       d.scale = p.scale != 0.f ? p.scale : 1.f;
-      d.up_tiles = (int32_t)((ffn + 15) / 16), d.shared_tiles = (int32_t)(((int64_t)p.shared_ffn + 15) / 16), d.down_tiles = (int32_t)((dim + 15) / 16);
       // every group but the last of an expert has MOE_GROUP rows
       const int64_t blocks = (rows + ROUTE_ROWS - 1) / ROUTE_ROWS, shared_groups = p.shared_ffn ? (rows + MOE_GROUP - 1) / MOE_GROUP : 0;
       const int64_t reached = std::min<int64_t>(p.experts, pairs), routed_groups = reached + (pairs - reached) / MOE_GROUP;
@@ -222,12 +221,12 @@ sk_status plan_moe(const sk_moe_problem *problems, int32_t n, int32_t compute_un
       add += (rows * ((p.dim + ADD_COLUMNS - 1) / ADD_COLUMNS) + 3) / 4;
       if (route > MOST_GRID || add > MOST_GRID) return refuse(err, SK_ERR_UNSUPPORTED, "more units of work than a launch's grid can hold");
       out.route_first.push_back((uint32_t)route), out.add_first.push_back((uint32_t)add);
-      tiles += std::max(d.most_groups * (int64_t)d.down_tiles, routed_groups * d.up_tiles + shared_groups * d.shared_tiles);
+      tiles += std::max(d.most_groups * ((dim + 15) / 16), routed_groups * ((ffn + 15) / 16) + shared_groups * (((int64_t)p.shared_ffn + 15) / 16));
       counters.take(d.routed, blocks * COUNTER_STEP), counters.take(d.blocks_routed, 1 * COUNTER_STEP);
       work.take(d.logits, rows * p.experts), work.take(d.ids, pairs), work.take(d.weights, pairs), work.take(d.row_of, pairs), work.take(d.place_at, pairs);
       work.take(d.groups, d.most_groups), work.take(d.first_begin, d.most_groups), work.take(d.second_begin, d.most_groups);
       d.h_stride = (std::max<int64_t>(ffn, p.shared_ffn) + 63) / 64 * 128;
-      d.y_stride = (int64_t)d.down_tiles * 16;
+      d.y_stride = dim;
       const int64_t places = pairs + (p.shared_ffn ? rows : 0);
       work.take(d.h, places * d.h_stride), work.take(d.y, places * d.y_stride);
       out.parts.push_back(d);

@@ -98,10 +98,9 @@ static void moes() {
       most += (pairs - most) / sk::MOE_GROUP + (d.shared_ffn ? (d.rows + sk::MOE_GROUP - 1) / sk::MOE_GROUP : 0);
       need(d.most_groups >= most, "groups");
       const int64_t blocks = (d.rows + sk::ROUTE_ROWS - 1) / sk::ROUTE_ROWS;
-      need((int64_t)d.up_tiles * 16 >= d.ffn && (int64_t)d.down_tiles * 16 >= d.dim && (int64_t)d.shared_tiles * 16 >= d.shared_ffn, "tiles");
       need(out.route_first[at + 1] - out.route_first[at] == blocks * ((d.experts + sk::ROUTE_EXPERTS - 1) / sk::ROUTE_EXPERTS), "units of the router");
       need(d.h_stride >= 2 * std::max(d.ffn, d.shared_ffn) && d.h_stride % 128 == 0, "strides of the workspace");
-      need(d.y_stride >= d.dim && d.y_stride == (int64_t)d.down_tiles * 16, "strides of the sums");
+      need(d.y_stride == d.dim, "strides of the sums");
       need((int64_t)(out.add_first[at + 1] - out.add_first[at]) * 4 * sk::ADD_COLUMNS >= (int64_t)d.rows * d.dim, "units of the sums");
       need(d.count == out.counts + at, "counts");
       counters.next(d.routed, blocks * sk::COUNTER_STEP), counters.next(d.blocks_routed, sk::COUNTER_STEP);
@@ -136,7 +135,9 @@ static void shares() {
   for (Part &p : parts) {
     const int32_t w = (int32_t)between(1, 2);
     for (int64_t n = between(0, between(0, 1) ? 3 : 90); n > 0; --n) {
-      const Group g{sk::moe::cost((int32_t)between(1, between(0, 1) ? 300 : 9000), w, sk::moe::mode_of((int32_t)between(1, 32))), ((int32_t)between(1, between(0, 1) ? 300 : 20000) + 15) / 16};
+      const int32_t mode = sk::moe::mode_of((int32_t)between(1, 32)), rows = (int32_t)between(1, between(0, 1) ? 300 : 20000);
+      const Group g{sk::moe::cost((int32_t)between(1, between(0, 1) ? 300 : 9000), w, mode), sk::moe::tiles_of(rows, w, mode)};
+      need((int64_t)g.tiles * sk::moe::rows_of_tile(w, mode) >= rows && (int64_t)(g.tiles - 1) * sk::moe::rows_of_tile(w, mode) < rows, "tiles");
       p.groups.push_back(g);
       p.begin.push_back(p.work);
       p.work += g.each * g.tiles;
