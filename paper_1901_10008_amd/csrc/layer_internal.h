@@ -62,7 +62,7 @@ constexpr int MOE_ROWS = 512;     // rows that are routed together; problems of 
 constexpr int MOE_EXPERTS = 512, MOE_TOP = 32;
 constexpr int MOE_GROUP = 32;     // rows of an expert that a unit of work takes at most
 constexpr int MOE_UP_RESIDENT = 3, MOE_DOWN_RESIDENT = 4;  // workgroups of the products that a compute unit holds (its registers)
-constexpr int ROUTE_EXPERTS = 8, ROUTE_ROWS = 4;  // of a unit of the router
+constexpr int ROUTE_ROWS = 4;  // of a unit of the router
 constexpr int ADD_COLUMNS = 256;                  // of a row that a wave adds up
 
 // Rows of an expert that go together: its number (or -1: the shared one), the first of their places, how many.
@@ -88,6 +88,7 @@ struct MoeDev {
   int32_t row0, rows, dim, experts, top_k, ffn, shared_ffn, act, scoring, normalize, dtype, router_f32;
   float scale;
   int32_t most_groups;                               // with those of the shared expert
+  int32_t route_experts;                             // of a unit of the router: 2 or 8
   // workspace
   double *logits;         // [rows][experts]
   int32_t *ids;           // [rows][top_k]: chosen experts

@@ -35,19 +35,21 @@ __device__ __forceinline__ Place place_of(const MoeArgs &a, const uint32_t *firs
 // ---------------------------------------------------------------------------
 // the router
 // ---------------------------------------------------------------------------
-// Scores of two experts a wave and ROUTE_ROWS rows.  Products of numbers of at most 24 and 11 bits are exact in 64 bits, and so, but for 2^-50 or
+// Scores of two experts a wave and ROUTE_ROWS rows; where there are few of them, of two experts a workgroup, a quarter of the reduction's pieces a wave.  Products of numbers of at most 24 and 11 bits are exact in 64 bits, and so, but for 2^-50 or
 // so, are their sums: which of two experts is chosen does not depend on the order of a sum.  Vector instructions of 64 bits have the rate of
 // those of 32 here, and E * D multiplications a row are little beside the experts' products.
 template <int DT, bool F32>
-__device__ __forceinline__ void route_scores(const SK_CONSTANT MoeDev &P, int32_t block, int32_t e0, int lane) {
+__device__ __forceinline__ void route_scores(const SK_CONSTANT MoeDev &P, int32_t block, int32_t e0, double (*joint)[2 * ROUTE_ROWS], int wave, int lane) {
   double sum[2][ROUTE_ROWS] = {};
   const int32_t last = P.experts - 1;
+  const bool split = P.route_experts == 2;
+  if (!split) e0 += 2 * wave;
   const char *w[2] = {P.router + (int64_t)min(e0, last) * P.router_stride, P.router + (int64_t)min(e0 + 1, last) * P.router_stride};
   const char *x[ROUTE_ROWS];
 #pragma unroll
   for (int r = 0; r < ROUTE_ROWS; ++r) x[r] = P.x + (int64_t)min(block * ROUTE_ROWS + r, P.rows - 1) * P.x_stride;  // (that there is a row is known later)
 #pragma unroll 2
-  for (int32_t k = lane * 8; k < P.dim; k += 512) {
+  for (int32_t k = (split ? wave * 64 + lane : lane) * 8; k < P.dim; k += split ? 8 * CACHE_THREADS : 512) {
     float a[2][8], b[ROUTE_ROWS][8];
 #pragma unroll
     for (int i = 0; i < 2; ++i) load8<F32 ? SK_F32 : DT, false>(w[i] + (int64_t)k * (F32 ? 4 : 2), a[i]);
@@ -69,9 +71,18 @@ __device__ __forceinline__ void route_scores(const SK_CONSTANT MoeDev &P, int32_
 #pragma unroll
     for (int r = 0; r < ROUTE_ROWS; ++r) {
       const double s = wave_sum(sum[i][r]);
-      const int32_t row = block * ROUTE_ROWS + r;
-      if (lane == 0 && e0 + i < P.experts && row < P.rows) put(P.logits + (int64_t)row * P.experts + e0 + i, s);
+      if (lane == 0) joint[wave][i * ROUTE_ROWS + r] = s;
     }
+  __syncthreads();
+  if ((wave == 0 || !split) && lane < 2 * ROUTE_ROWS) {
+    const int32_t e = e0 + lane / ROUTE_ROWS, row = block * ROUTE_ROWS + lane % ROUTE_ROWS;
+    double s = joint[wave][lane];
+    if (split) {
+#pragma unroll
+      for (int w = 1; w < CACHE_THREADS / 64; ++w) s += joint[w][lane];
+    }
+    if (e < P.experts && row < P.rows) put(P.logits + (int64_t)row * P.experts + e, s);
+  }
 }
 
 // Numbers of 64 bits as whole numbers of the same order; NaN below all others, and 0 for what is out.
@@ -258,17 +269,16 @@ __device__ __forceinline__ void sort_pairs(const SK_CONSTANT MoeDev &P, int32_t 
 
 __global__ void __launch_bounds__(CACHE_THREADS) sk_moe_route(MoeArgs a) {
   __shared__ Sorting sorting;
+  __shared__ double joint[CACHE_THREADS / 64][2 * ROUTE_ROWS];
   __shared__ uint32_t flag;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Place place = place_of(a, a.first);
   const SK_CONSTANT MoeDev &P = *place.part;
   const int32_t unit = place.unit;
-  const int32_t by_experts = (P.experts + ROUTE_EXPERTS - 1) / ROUTE_EXPERTS, blocks = (P.rows + ROUTE_ROWS - 1) / ROUTE_ROWS;
-  const int32_t block = unit / by_experts, e0 = unit % by_experts * ROUTE_EXPERTS + 2 * wave, rows = rows_of(P);
-  if (e0 < P.experts) {
-    if (P.dtype == SK_BF16) P.router_f32 ? route_scores<SK_BF16, true>(P, block, e0, lane) : route_scores<SK_BF16, false>(P, block, e0, lane);
-    else P.router_f32 ? route_scores<SK_F16, true>(P, block, e0, lane) : route_scores<SK_F16, false>(P, block, e0, lane);
-  }
+  const int32_t by_experts = (P.experts + P.route_experts - 1) / P.route_experts, blocks = (P.rows + ROUTE_ROWS - 1) / ROUTE_ROWS;
+  const int32_t block = unit / by_experts, e0 = unit % by_experts * P.route_experts, rows = rows_of(P);
+  if (P.dtype == SK_BF16) P.router_f32 ? route_scores<SK_BF16, true>(P, block, e0, joint, wave, lane) : route_scores<SK_BF16, false>(P, block, e0, joint, wave, lane);
+  else P.router_f32 ? route_scores<SK_F16, true>(P, block, e0, joint, wave, lane) : route_scores<SK_F16, false>(P, block, e0, joint, wave, lane);
   if (!last_to_arrive(P.routed + block * COUNTER_STEP, by_experts, &flag)) return;
   const int32_t row = block * ROUTE_ROWS + wave;
   int32_t *ids = blocks == 1 ? sorting.ids + row * P.top_k : nullptr;  // (then there are at most ROUTE_ROWS rows, and no other workgroup has any)

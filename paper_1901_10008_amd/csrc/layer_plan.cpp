@@ -155,6 +155,10 @@ sk_status plan_norm(const sk_norm_problem *problems, int32_t n, NormPlanHost &ou
 
 // ---- mixture of experts ----------------------------------------------------------------------------------------------------
 
+// The router splits its sums where that gives no more workgroups than the card holds at a time: 8 experts of 4096 and 2 rows 9.4 us instead of 11.6,
+// 60 of 2048 and 61 rows (480 workgroups) 12.5 instead of 12.8; but 33 of 1000 and 250 rows (1071) 18 instead of 13.5.
+constexpr int64_t ROUTE_SPLIT_UNITS = 512;
+
 sk_status plan_moe(const sk_moe_problem *problems, int32_t n, int32_t compute_units, int32_t workgroups, MoePlanHost &out, std::string &err) {
   Spans written;
   out.route_first.assign(1, 0u), out.add_first.assign(1, 0u);
@@ -217,7 +221,8 @@ sk_status plan_moe(const sk_moe_problem *problems, int32_t n, int32_t compute_un
       const int64_t blocks = (rows + ROUTE_ROWS - 1) / ROUTE_ROWS, shared_groups = p.shared_ffn ? (rows + MOE_GROUP - 1) / MOE_GROUP : 0;
       const int64_t reached = std::min<int64_t>(p.experts, pairs), routed_groups = reached + (pairs - reached) / MOE_GROUP;
       d.most_groups = (int32_t)(routed_groups + shared_groups);
-      route += blocks * ((p.experts + ROUTE_EXPERTS - 1) / ROUTE_EXPERTS);
+      d.route_experts = blocks * ((p.experts + 1) / 2) <= ROUTE_SPLIT_UNITS ? 2 : 8;
+      route += blocks * ((p.experts + d.route_experts - 1) / d.route_experts);
       add += (rows * ((p.dim + ADD_COLUMNS - 1) / ADD_COLUMNS) + 3) / 4;
       if (route > MOST_GRID || add > MOST_GRID) return refuse(err, SK_ERR_UNSUPPORTED, "more units of work than a launch's grid can hold");
       out.route_first.push_back((uint32_t)route), out.add_first.push_back((uint32_t)add);

@@ -98,7 +98,7 @@ static void moes() {
       most += (pairs - most) / sk::MOE_GROUP + (d.shared_ffn ? (d.rows + sk::MOE_GROUP - 1) / sk::MOE_GROUP : 0);
       need(d.most_groups >= most, "groups");
       const int64_t blocks = (d.rows + sk::ROUTE_ROWS - 1) / sk::ROUTE_ROWS;
-      need(out.route_first[at + 1] - out.route_first[at] == blocks * ((d.experts + sk::ROUTE_EXPERTS - 1) / sk::ROUTE_EXPERTS), "units of the router");
+      need(out.route_first[at + 1] - out.route_first[at] == blocks * ((d.experts + d.route_experts - 1) / d.route_experts), "units of the router");
       need(d.h_stride >= 2 * std::max(d.ffn, d.shared_ffn) && d.h_stride % 128 == 0, "strides of the workspace");
       need(d.y_stride == d.dim, "strides of the sums");
       need((int64_t)(out.add_first[at + 1] - out.add_first[at]) * 4 * sk::ADD_COLUMNS >= (int64_t)d.rows * d.dim, "units of the sums");
