@@ -41,7 +41,8 @@ __device__ __forceinline__ void norm_rows(const SK_CONSTANT NormDev &p, int64_t 
   constexpr bool LATE = T > 512 || DT == SK_F32;  // gates and weights are loaded when they are wanted: there are not the registers to keep them
   const int dim = p.dim;
   const float by = 1.f / (float)dim;
-  RowSum<T> sum{red, t >> 6};
+  const int wave_at = T >= 64 ? __builtin_amdgcn_readfirstlane(t & ~63) : 0;
+  RowSum<T> sum{red, wave_at >> 6};
   using Own = std::integral_constant<int, DT>;
   using Res = std::integral_constant<int, RT>;
 
@@ -96,7 +97,15 @@ __device__ __forceinline__ void norm_rows(const SK_CONSTANT NormDev &p, int64_t 
   auto each_piece = [&](auto f) {
 #pragma unroll
     for (int i = 0; i < P; ++i)
-      if (i * T * 8 < dim) f(i);
+      if ((i * T + wave_at) * 8 < dim) f(i);  // (the same in all lanes: what a wave has nothing of costs it nothing)
+  };
+
+  auto behind_is_zero = [&](int i, float(&x)[8]) {  // (a branch: most waves have nothing there)
+    const int at = (i * T + t) * 8;
+    if (at + 8 > dim) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = at + k < dim ? x[k] : 0.f;
+    }
   };
 
   const bool has_block = p.block != nullptr, has_gate = p.gate != nullptr, has_residual = p.residual != nullptr;
@@ -134,7 +143,8 @@ __device__ __forceinline__ void norm_rows(const SK_CONSTANT NormDev &p, int64_t 
       const float mean = sum(s) * by;
       each_piece([&](int i) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[i][k] = (i * T + t) * 8 + k < dim ? x[i][k] - mean : 0.f;
+        for (int k = 0; k < 8; ++k) x[i][k] -= mean;
+        behind_is_zero(i, x[i]);
       });
     }
     s = 0.f;
@@ -196,12 +206,17 @@ __device__ __forceinline__ void norm_rows(const SK_CONSTANT NormDev &p, int64_t 
   each_piece([&](int i) {
     // (a missing part adds nothing, not its scale times 0)
     if (has_residual) values(Res{}, now.residual[i], r[i]);
+    if (!has_block) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) r[i][k] = !has_block ? p.residual_scale * r[i][k] : !has_residual ? p.block_scale * u[i][k] : p.residual_scale * r[i][k] + p.block_scale * u[i][k];
-    if (p.post_bias) {  // (a bias stands behind the row's end as well)
+      for (int k = 0; k < 8; ++k) r[i][k] *= p.residual_scale;
+    } else if (!has_residual) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) r[i][k] = (i * T + t) * 8 + k < dim ? r[i][k] : 0.f;
+      for (int k = 0; k < 8; ++k) r[i][k] = p.block_scale * u[i][k];
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) r[i][k] = p.residual_scale * r[i][k] + p.block_scale * u[i][k];
     }
+    if (p.post_bias) behind_is_zero(i, r[i]);  // (a bias stands there as well)
     if (p.residual_out) store(Res{}, (char *)p.residual_out + row * p.residual_out_stride * RS, i, r[i]);
   });
   if (p.next) {
