@@ -202,9 +202,9 @@ struct Costs {
   __device__ __forceinline__ int64_t sum(int64_t counts) const { return of_mode(counts, 8) * of[0] + of_mode(counts, 16) * of[1] + of_mode(counts, 32) * of[2]; }
 };
 // (of all tiles of a group)
-__device__ __forceinline__ Costs costs_of(int32_t k_len, int32_t matrices, int32_t rows) {
-  return Costs{{moe::cost(k_len, matrices, 8) * moe::tiles_of(rows, matrices, 8), moe::cost(k_len, matrices, 16) * moe::tiles_of(rows, matrices, 16),
-                moe::cost(k_len, matrices, 32) * moe::tiles_of(rows, matrices, 32)}};
+__device__ __forceinline__ Costs costs_of(int32_t k_len, int32_t matrices, int32_t parts, int32_t rows) {
+  return Costs{{moe::cost(k_len, matrices, parts, 8) * moe::tiles_of(rows, matrices, 8), moe::cost(k_len, matrices, parts, 16) * moe::tiles_of(rows, matrices, 16),
+                moe::cost(k_len, matrices, parts, 32) * moe::tiles_of(rows, matrices, 32)}};
 }
 
 // here: ids and weights are in LDS already.
@@ -227,7 +227,7 @@ __device__ __forceinline__ void sort_pairs(const SK_CONSTANT MoeDev &P, int32_t 
   __syncthreads();
   if (tid < 64) {
     const int32_t matrices = P.gate ? 2 : 1;
-    const Costs up = costs_of(P.dim, matrices, P.ffn), down = costs_of(P.ffn, 1, P.dim);
+    const Costs up = costs_of(P.dim, matrices, 1, P.ffn), down = costs_of(P.ffn, 1, H_PARTS, P.dim);
     int64_t all = 0;
     for (int32_t e0 = 0; e0 < P.experts; e0 += 64) {
       const int32_t e = e0 + tid, n = e < P.experts ? s.count[e] : 0, g = (n + MOE_GROUP - 1) / MOE_GROUP;
@@ -244,7 +244,7 @@ __device__ __forceinline__ void sort_pairs(const SK_CONSTANT MoeDev &P, int32_t 
     MoeCount c{groups_in(all), rows, up.sum(all), down.sum(all)};
     if (P.shared_ffn) {  // (at most 16 groups)
       const int32_t g = (rows + MOE_GROUP - 1) / MOE_GROUP, n = min(MOE_GROUP, rows - tid * MOE_GROUP);
-      const Costs shared_up = costs_of(P.dim, matrices, P.shared_ffn), shared_down = costs_of(P.shared_ffn, 1, P.dim);
+      const Costs shared_up = costs_of(P.dim, matrices, 1, P.shared_ffn), shared_down = costs_of(P.shared_ffn, 1, H_PARTS, P.dim);
       if (tid < g) {
         P.groups[c.groups + tid] = MoeGroup{-1, tid * MOE_GROUP, n, 0};
         P.first_begin[c.groups + tid] = c.first_work + tid * shared_up.of[2];
@@ -330,9 +330,12 @@ constexpr int joint_floats(int w) { return 2 * 4 * w * MOE_GROUP * TILE; }
 // Loads by way of a buffer descriptor: a scalar base, and in each lane an offset below 2^31; a lane with OUTSIDE gets zeros and asks for nothing, so
 // that no load stands under a branch (which would leave the compiler in doubt how many are on their way).
 constexpr uint32_t OUTSIDE = 0x80000000u;
+// ONCE: past the caches, where activations and the small launches around these are (two tenants 52.6 + 33.6 -> 48 + 30.9 us, the router with them 11.4 ->
+// 9.3).  Not the weights of groups of more than 16 rows, which the next group of their expert is likely to read again (a chunk of 250 rows 42 + 56 -> 46 + 59).
+template <bool ONCE>
 __device__ __forceinline__ u32x4 load_from(const char *base, uint32_t lane_offset, int32_t offset) {
   const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)OUTSIDE, 0x00027000);
-  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)lane_offset, offset, 0));
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)lane_offset, offset, ONCE ? 2 : 0));
 }
 
 // (an address that is the same in all lanes, where the compiler cannot see it)
@@ -341,18 +344,19 @@ __device__ __forceinline__ const char *uniform(const char *p) {
   return (const char *)(uintptr_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int32_t)(a >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int32_t)a));
 }
 
-// W matrices of weights with the same rows and the same activations (gate and up), of each S times 16 rows.  The stream of loads runs R blocks ahead of the matrix instructions, from
+// W matrices of weights with the same rows and the same activations (gate and up), of each S times 16 rows; activations that
+// are the sum of L parts, x_part bytes apart.  The stream of loads runs R blocks ahead of the matrix instructions, from
 // tile to tile, so it is only empty at the beginning and the end of a run.  group(i) is the i-th group, base(g, m) its matrix m, x_base(g) and x_offset(g, i)
 // where its i-th row of activations stands; done(t, group, tile) takes up the sums of turn t.
-template <int DT, int MODE, int W, int S, int R, class G, class B, class XB, class XO, class D>
-__device__ __forceinline__ void stream(const Run &run, int32_t tiles, int64_t row_stride, int32_t rows_end, int32_t k_len, G group, B base, XB x_base, XO x_offset, D done, float *joint,
+template <int DT, int MODE, int W, int S, int L, int R, class G, class B, class XB, class XO, class D>
+__device__ __forceinline__ void stream(const Run &run, int32_t tiles, int64_t row_stride, int32_t rows_end, int32_t k_len, int32_t x_part, G group, B base, XB x_base, XO x_offset, D done, float *joint,
                                        int wave, int lane) {
   constexpr int NB = MODE == 32 ? 2 : 1, H = MODE == 8 ? 1 : 2, A = MODE == 8 ? 2 : NB;  // loads of activations for 16 rows, sums
   const int r16 = lane & 15, q = lane >> 4;
   const int32_t steps = (k_len + 255) / 256;  // of the four waves' blocks each
   const uint32_t w_piece = 16 * (q + 4 * (r16 >> 3)), x_piece = MODE == 8 ? w_piece : 16 * q;
   constexpr int WS = W * S;  // (matrix m, rows s at m * S + s)
-  u32x4 w[R][WS][2], b[R][NB][H];
+  u32x4 w[R][WS][2], b[R][L][NB][H];
   f32x4 acc[WS][A] = {};
 
   // loads
@@ -377,7 +381,7 @@ __device__ __forceinline__ void stream(const Run &run, int32_t tiles, int64_t ro
   };
   new_group();
   new_rows();
-  auto load = [&](u32x4(&w)[WS][2], u32x4(&b)[NB][H]) {
+  auto load = [&](u32x4(&w)[WS][2], u32x4(&b)[L][NB][H]) {
     // zeros behind the end of the reduction and behind the last tile
     const int32_t k = (wave + 4 * p_step) * 128, left = p_left > 0 ? 2 * k_len - k : 0;
     const bool in = (int32_t)w_piece < left;
@@ -387,14 +391,16 @@ __device__ __forceinline__ void stream(const Run &run, int32_t tiles, int64_t ro
       for (int s = 0; s < S; ++s) {
         const uint32_t at = in ? w_row[s][j] : OUTSIDE;
 #pragma unroll
-        for (int m = 0; m < W; ++m) w[m * S + s][j] = load_from(w_base[m * S + s], at, k);
+        for (int m = 0; m < W; ++m) w[m * S + s][j] = load_from<MODE < 32>(w_base[m * S + s], at, k);
       }
     }
 #pragma unroll
     for (int h = 0; h < H; ++h) {
       const bool in_x = (int32_t)x_piece + 64 * h < left;
 #pragma unroll
-      for (int n = 0; n < NB; ++n) b[n][h] = load_from(x_at, in_x ? x_row[n] + 64 * h : OUTSIDE, k);
+      for (int l = 0; l < L; ++l)
+#pragma unroll
+        for (int n = 0; n < NB; ++n) b[l][n][h] = load_from<false>(x_at, in_x ? x_row[n] + 64 * h : OUTSIDE, k + l * x_part);
     }
     if (++p_step == steps) {
       p_step = 0;
@@ -417,15 +423,18 @@ __device__ __forceinline__ void stream(const Run &run, int32_t tiles, int64_t ro
     for (int u = 0; u < R; ++u) {
 #pragma unroll
       for (int m = 0; m < WS; ++m) {
-        if constexpr (MODE == 8) {
-          mma16<DT>(w[u][m][0], b[u][0][0], acc[m][0]);
-          mma16<DT>(w[u][m][1], b[u][0][0], acc[m][1]);
-        } else {
-          const u32x4 lo = low_half(w[u][m][0], w[u][m][1]), hi = high_half(w[u][m][0], w[u][m][1]);
+        const u32x4 lo = MODE == 8 ? w[u][m][0] : low_half(w[u][m][0], w[u][m][1]), hi = MODE == 8 ? w[u][m][1] : high_half(w[u][m][0], w[u][m][1]);
 #pragma unroll
-          for (int n = 0; n < NB; ++n) {
-            mma16<DT>(lo, b[u][n][0], acc[m][n]);
-            mma16<DT>(hi, b[u][n][1], acc[m][n]);
+        for (int l = 0; l < L; ++l) {
+          if constexpr (MODE == 8) {
+            mma16<DT>(lo, b[u][l][0][0], acc[m][0]);
+            mma16<DT>(hi, b[u][l][0][0], acc[m][1]);
+          } else {
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+              mma16<DT>(lo, b[u][l][n][0], acc[m][n]);
+              mma16<DT>(hi, b[u][l][n][1], acc[m][n]);
+            }
           }
         }
       }
@@ -528,10 +537,21 @@ __device__ __forceinline__ void up_run(const SK_CONSTANT MoeDev &P, const Run &r
       for (int k = 0; k < 4; ++k) h[k] = activated(P.act, h[k]);
     }
     const int64_t place = (shared ? (int64_t)P.rows * P.top_k : 0) + g.first + i;
-    store8(P.h + place * P.h_stride + 2 * f, u32x2{pack2<DT>(h[0], h[1]), pack2<DT>(h[2], h[3])});
+    // h goes to the second products as the sum of what it is in 16 bits and of what is left of it: rounded to 16 bits alone it would be most of the
+    // output's error (bf16: 0.0023 of it instead of 0.0017)
+    const u32x2 whole{pack2<DT>(h[0], h[1]), pack2<DT>(h[2], h[3])};
+    f32x4 rest;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float part = elem<DT>(k % 2 ? whole[k / 2] >> 16 : whole[k / 2] & 0xffffu);
+      rest[k] = fabsf(part) < __builtin_inff() ? h[k] - part : 0.f;  // (infinities and NaN stand in the first part)
+    }
+    char *to = P.h + place * P.h_stride + 2 * f;
+    store8(to, whole);
+    store8(to + P.h_part, u32x2{pack2<DT>(rest[0], rest[1]), pack2<DT>(rest[2], rest[3])});
   };
-  stream<DT, MODE, W, S, MODE == 8 ? 3 : 2>(
-      run, moe::tiles_of(width, W, MODE), shared ? 2 * (int64_t)P.dim : P.up_row, width, P.dim, [&](int32_t i) { return group_of(P, i); }, base, [&](const MoeGroup &) { return P.x; },
+  stream<DT, MODE, W, S, 1, MODE == 8 ? 3 : 2>(
+      run, moe::tiles_of(width, W, MODE), shared ? 2 * (int64_t)P.dim : P.up_row, width, P.dim, 0, [&](int32_t i) { return group_of(P, i); }, base, [&](const MoeGroup &) { return P.x; },
       [&](const MoeGroup &g, int32_t i) { return (uint32_t)row_of[g.first - place0 + i] * (uint32_t)P.x_stride; }, done, joint, wave, lane);
 }
 
@@ -550,8 +570,8 @@ __device__ __forceinline__ void down_run(const SK_CONSTANT MoeDev &P, const Run 
     if (i >= g.rows || s >= S || d >= P.dim) return;  // (dim is a multiple of 8)
     *(f32x4 SK_GLOBAL *)(uintptr_t)(P.y + (place0 + g.first + i) * P.y_stride + d) = joined<MODE, S>(joint, t, s, i, tid & 3);
   };
-  stream<DT, MODE, 1, S, MODE == 8 ? 4 : 2>(
-      run, moe::tiles_of(P.dim, 1, MODE), shared ? 2 * (int64_t)width : P.down_row, P.dim, width, [&](int32_t i) { return group_of(P, i); },
+  stream<DT, MODE, 1, S, H_PARTS, MODE == 8 ? 4 : MODE == 16 ? 2 : 1>(
+      run, moe::tiles_of(P.dim, 1, MODE), shared ? 2 * (int64_t)width : P.down_row, P.dim, width, (int32_t)P.h_part, [&](int32_t i) { return group_of(P, i); },
       [&](const MoeGroup &g, int) { return shared ? P.shared_down : P.down + g.expert * P.down_expert; }, [&](const MoeGroup &g) { return P.h + (place0 + g.first) * P.h_stride; },
       [&](const MoeGroup &, int32_t i) { return (uint32_t)i * (uint32_t)P.h_stride; }, done, joint, wave, lane);
 }
@@ -564,7 +584,7 @@ struct Products {
     return moe::tiles_of(!UP ? P.dim : g.expert < 0 ? P.shared_ffn : P.ffn, UP && P.gate ? 2 : 1, moe::mode_of(g.rows));
   }
   static __device__ __forceinline__ int64_t cost(const SK_CONSTANT MoeDev &P, const MoeGroup &g) {
-    return UP ? moe::cost(P.dim, P.gate ? 2 : 1, moe::mode_of(g.rows)) : moe::cost(g.expert < 0 ? P.shared_ffn : P.ffn, 1, moe::mode_of(g.rows));
+    return UP ? moe::cost(P.dim, P.gate ? 2 : 1, 1, moe::mode_of(g.rows)) : moe::cost(g.expert < 0 ? P.shared_ffn : P.ffn, 1, H_PARTS, moe::mode_of(g.rows));
   }
 
   // From tile `tile` of group `group` on, up to (not with) tile `last_tile` of group `last`.

@@ -230,7 +230,7 @@ sk_status plan_moe(const sk_moe_problem *problems, int32_t n, int32_t compute_un
       counters.take(d.routed, blocks * COUNTER_STEP), counters.take(d.blocks_routed, 1 * COUNTER_STEP);
       work.take(d.logits, rows * p.experts), work.take(d.ids, pairs), work.take(d.weights, pairs), work.take(d.row_of, pairs), work.take(d.place_at, pairs);
       work.take(d.groups, d.most_groups), work.take(d.first_begin, d.most_groups), work.take(d.second_begin, d.most_groups);
-      d.h_stride = (std::max<int64_t>(ffn, p.shared_ffn) + 63) / 64 * 128;
+      d.h_part = (std::max<int64_t>(ffn, p.shared_ffn) + 63) / 64 * 128, d.h_stride = H_PARTS * d.h_part;
       d.y_stride = dim;
       const int64_t places = pairs + (p.shared_ffn ? rows : 0);
       work.take(d.h, places * d.h_stride), work.take(d.y, places * d.y_stride);

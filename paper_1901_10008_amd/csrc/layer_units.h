@@ -28,9 +28,11 @@ SK_BOTH int32_t tiles_of(int32_t rows, int32_t matrices, int32_t mode) {
   return rows / t + (rows % t != 0);
 }
 // All tiles of a launch stand in a row, each as long as it takes: the loads of a wave, and some for its beginning and end.  k_len: elements of its
-// reduction, `matrices` of weights.
+// reduction, `matrices` of weights, `parts` of the activations.
 constexpr int32_t EXTRA = 8;
-SK_BOTH int64_t cost(int32_t k_len, int32_t matrices, int32_t mode) { return (int64_t)((k_len + 255) / 256) * (matrices * rows_of_tile(matrices, mode) / 8 + mode / 8) + EXTRA; }
+SK_BOTH int64_t cost(int32_t k_len, int32_t matrices, int32_t parts, int32_t mode) {
+  return (int64_t)((k_len + 255) / 256) * (matrices * rows_of_tile(matrices, mode) / 8 + parts * mode / 8) + EXTRA;
+}
 
 // A workgroup has the tiles that begin in its share.
 struct Share {

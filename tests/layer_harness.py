@@ -226,7 +226,8 @@ class Moe:
         return ids, w * (self.scale or 1.0)
 
     def through(self, x, gate, up, down):
-        """An expert's output for rows x, and how far off it may be: products in fp32 in any order, act, a rounding of h, another product."""
+        """An expert's output for rows x, and how far off it may be: products in fp32 in any order, act, h as the sum of
+        two numbers of the type (the second is h less the first, rounded), another product of twice as many terms."""
         k, f = x.shape[-1], up.shape[0]
         z, tz = x @ up.T, (k + 8) * 2 * E * (x.abs() @ up.abs().T)
         if gate is not None:
@@ -236,8 +237,8 @@ class Moe:
         a, ta = activated(self.act, v)
         ta = ta + 1.2 * tv  # (no act's slope is larger)
         h, th = (a * z, ta * z.abs() + tz * a.abs() + ta * tz + E * (a * z).abs()) if gate is not None else (a, ta)
-        rounded = th + U[self.dtype] * (h.abs() + th) + TINY[self.dtype]
-        return h @ down.T, rounded @ down.abs().T + (f + 8) * 2 * E * (h.abs() @ down.abs().T)
+        rounded = th + U[self.dtype] ** 2 * (h.abs() + th) + TINY[self.dtype]
+        return h @ down.T, rounded @ down.abs().T + (2 * f + 8) * 2 * E * (h.abs() @ down.abs().T)
 
     def reference(self, n=None):
         n = self.used if n is None else n
@@ -267,9 +268,9 @@ def check_moe(m, label="", n=None):
         check(m.weights[:n], w, 4 * E * w.abs() + 2.0 ** -126, f"{label}: weights")
         assert (m.ids[n:] == -7).all() and torch.isnan(m.weights[n:]).all(), f"{label}: choices behind the last row were written"
     check(m.out[:n], out, tol, f"{label}: out")
-    # rounding errors have no common direction: rounded h and outputs together stay within two units, measured over all outputs
+    # the rounding of the outputs is at most one unit of each; what came before it is far smaller, measured over all outputs
     if n and float(out.norm()) > 0:
-        assert float((m.out[:n].double() - out).norm()) <= 2 * U[m.dtype] * float(out.norm()), f"{label}: {float((m.out[:n].double() - out).norm() / out.norm()):.3g}"
+        assert float((m.out[:n].double() - out).norm()) <= 1.1 * U[m.dtype] * float(out.norm()), f"{label}: {float((m.out[:n].double() - out).norm() / out.norm()):.3g}"
     assert torch.isnan(m.out_b[n:]).all() and (not m.pad or torch.isnan(m.out_b[:, m.dim:]).all()), f"{label}: written outside the rows"
 
 

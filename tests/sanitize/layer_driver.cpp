@@ -99,7 +99,7 @@ static void moes() {
       need(d.most_groups >= most, "groups");
       const int64_t blocks = (d.rows + sk::ROUTE_ROWS - 1) / sk::ROUTE_ROWS;
       need(out.route_first[at + 1] - out.route_first[at] == blocks * ((d.experts + d.route_experts - 1) / d.route_experts), "units of the router");
-      need(d.h_stride >= 2 * std::max(d.ffn, d.shared_ffn) && d.h_stride % 128 == 0, "strides of the workspace");
+      need(d.h_part >= 2 * std::max(d.ffn, d.shared_ffn) && d.h_part % 128 == 0 && d.h_stride == sk::H_PARTS * d.h_part, "strides of the workspace");
       need(d.y_stride == d.dim, "strides of the sums");
       need((int64_t)(out.add_first[at + 1] - out.add_first[at]) * 4 * sk::ADD_COLUMNS >= (int64_t)d.rows * d.dim, "units of the sums");
       need(d.count == out.counts + at, "counts");
@@ -136,7 +136,7 @@ static void shares() {
     const int32_t w = (int32_t)between(1, 2);
     for (int64_t n = between(0, between(0, 1) ? 3 : 90); n > 0; --n) {
       const int32_t mode = sk::moe::mode_of((int32_t)between(1, 32)), rows = (int32_t)between(1, between(0, 1) ? 300 : 20000);
-      const Group g{sk::moe::cost((int32_t)between(1, between(0, 1) ? 300 : 9000), w, mode), sk::moe::tiles_of(rows, w, mode)};
+      const Group g{sk::moe::cost((int32_t)between(1, between(0, 1) ? 300 : 9000), w, (int32_t)between(1, 2), mode), sk::moe::tiles_of(rows, w, mode)};
       need((int64_t)g.tiles * sk::moe::rows_of_tile(w, mode) >= rows && (int64_t)(g.tiles - 1) * sk::moe::rows_of_tile(w, mode) < rows, "tiles");
       p.groups.push_back(g);
       p.begin.push_back(p.work);
