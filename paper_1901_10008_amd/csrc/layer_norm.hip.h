@@ -10,7 +10,10 @@ namespace sk {
 //   u = N(block) w + b,  r = rs * residual + bs * u * act(gate),  next = N(r) w' + b'
 //
 // Each norm is one sum over the row, or two (the mean, then the squares of what lies beside it: nothing cancels).  All of a row's loads, those of the
-// weights among them, are on their way before the number of rows is known and before the first sum.
+// weights among them, are on their way before the number of rows is known and before the first sum.  Bound by memory where there is much (16000 rows of 4096
+// elements, bf16 beside a stream of 32 bits: 786 MB in 134 us, 5.9 TB/s), by that chain where there is little (64 rows of each of four widths 7.2 us, three
+// rows 3.3); rows of a few hundred to two thousand elements by the latency of their sums and by the vector unit (5003 of 1283 with both norms, biases and a
+// gate: 25.7 us, 2 TB/s).
 struct NormArgs {
   const NormTable *table;
   int32_t n;

@@ -81,6 +81,22 @@ def test_a_row_keeps_its_nan_to_itself():
     assert torch.isnan(n.next[2]).all() and torch.isnan(n.next[4]).any()
 
 
+@pytest.mark.parametrize("dim", [24, 200, 700, 1501])
+def test_many_rows_in_place_and_their_nan(dim):
+    """Several rows of a wave or workgroup: each reads and writes its own alone."""
+    H.check_norms([H.Norm(dim=dim, rows=2100, post=1, gate="rows", act="silu", in_place=True, used=2093, pad=3, seed=dim)])
+    n, clean = (H.Norm(dim=dim, rows=2100, kind="layer", post=1, seed=1) for _ in range(2))
+    n.block[2, dim // 2], n.block[6, 3], n.residual[2099, dim - 1] = float("nan"), float("inf"), float("nan")
+    for x in (n, clean):
+        with sk.sk_norm_plan_create([x.problem()]) as plan:
+            sk.sk_norm_launch(plan, H.stream_handle())
+            torch.cuda.synchronize()
+    others = torch.ones(2100, dtype=torch.bool, device="cuda")
+    others[[2, 6, 2099]] = False
+    assert torch.equal(n.next[others], clean.next[others]) and torch.equal(n.residual_out[others], clean.residual_out[others])
+    assert torch.isnan(n.next[~others]).any(1).all()
+
+
 def test_more_than_the_caches_hold():
     """Loads and stores past the caches: 190 MB, against the same rows in launches that fit the caches (the same bits) and 64 bits."""
     big = H.Norm(dim=2056, rows=10000, post=1, stream="f32", gate="rows", act="sigmoid", seed=3)
