@@ -136,6 +136,7 @@ struct VerifyDev {
   double *sums;            // [sequences][chunks]
   uint32_t *arrived;       // [sequences], COUNTER_STEP apart
 };
+constexpr int VERIFY_PIECES = 4;  // of 512 logits that a chunk has at most
 constexpr int32_t VERIFY_CHUNKS = 4;  // that a workgroup of the second launch takes
 constexpr int VERIFY_PROBLEMS = 16;  // of a launch
 struct VerifyTable {

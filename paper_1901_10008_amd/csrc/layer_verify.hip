@@ -97,7 +97,7 @@ struct Eight {
 };
 
 struct VerifyShared {
-  double begin, bound, piece[8];
+  double begin, bound, piece[VERIFY_PIECES];
   int32_t chunk, found;
 };
 
@@ -186,11 +186,10 @@ __device__ __forceinline__ void row_chunk(const SK_CONSTANT VerifyDev &P, uint32
   VerifyStat *out = P.stats + ((int64_t)row * 2 + draft) * P.chunks + chunk;
   if (P.pieces == 1) chunk_stat<DT, 1>(P, from, chunk, c, out, lane);
   else if (P.pieces == 2) chunk_stat<DT, 2>(P, from, chunk, c, out, lane);
-  else if (DT == SK_F32 || P.pieces == 4) chunk_stat<DT, 4>(P, from, chunk, c, out, lane);
-  else chunk_stat<DT, 8>(P, from, chunk, c, out, lane);
+  else chunk_stat<DT, VERIFY_PIECES>(P, from, chunk, c, out, lane);
 }
 
-__global__ void __launch_bounds__(CACHE_THREADS, 5) sk_verify_stats(VerifyArgs a) {
+__global__ void __launch_bounds__(CACHE_THREADS, 8) sk_verify_stats(VerifyArgs a) {
   const SK_CONSTANT VerifyTable &table = *(const SK_CONSTANT VerifyTable *)(uintptr_t)a.table;
   int i = 0;
   uint32_t first = 0;
@@ -266,43 +265,34 @@ __device__ __forceinline__ void weights8(const Draw &d, const Eight<DT> &p, cons
   }
 }
 
-// The weights of a chunk, by a workgroup: a wave has two of its eight pieces, whose sums go to LDS.  Returns the chunk's sum.
+// The weights of a chunk, by a workgroup: a wave has a piece, whose sum goes to LDS.  Returns the chunk's sum.
 template <int DT>
-__device__ __forceinline__ double chunk_weights(const SK_CONSTANT VerifyDev &P, const Draw &d, const char *p_row, const char *q_row, int32_t chunk, double c, double (&w)[2][8], int32_t (&places)[2],
+__device__ __forceinline__ double chunk_weights(const SK_CONSTANT VerifyDev &P, const Draw &d, const char *p_row, const char *q_row, int32_t chunk, double c, double (&w)[8], int32_t &place,
                                                 VerifyShared &s, int tid) {
+  static_assert(VERIFY_PIECES == CACHE_THREADS / 64, "a piece a wave");
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-
-  Eight<DT> p[2], q[2];
-  int32_t at[2];
+  const int32_t at = wave < P.pieces ? (chunk * P.pieces + wave) * 512 : P.vocab;
+  double sum = 0.0;
+  place = 0;
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int32_t i = wave + 4 * j;
-    at[j] = i < P.pieces ? (chunk * P.pieces + i) * 512 : P.vocab;
-    if (at[j] >= P.vocab) continue;  // (the same in all lanes)
-    p[j].template load<true>(p_row, at[j], lane, P.vocab);
-    q[j].template load<true>(q_row, at[j], lane, P.vocab);
+  for (int k = 0; k < 8; ++k) w[k] = 0.0;
+  if (at < P.vocab) {  // (the same in all lanes)
+    Eight<DT> p, q;
+    p.template load<true>(p_row, at, lane, P.vocab);
+    q.template load<true>(q_row, at, lane, P.vocab);
+    p.cut(at, lane, P.vocab);
+    q.cut(at, lane, P.vocab);
+    weights8<DT>(d, p, q, c, w);
+    place = p.first;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum += w[k];
+    sum = wave_sum(sum);
   }
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    double sum = 0.0;
-    places[j] = 0;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) w[j][k] = 0.0;
-    if (at[j] < P.vocab) {
-      p[j].cut(at[j], lane, P.vocab);
-      q[j].cut(at[j], lane, P.vocab);
-      weights8<DT>(d, p[j], q[j], c, w[j]);
-      places[j] = p[j].first;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) sum += w[j][k];
-      sum = wave_sum(sum);
-    }
-    if (lane == 0) s.piece[wave + 4 * j] = sum;
-  }
+  if (lane == 0) s.piece[wave] = sum;
   __syncthreads();
   double all = 0.0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) all += s.piece[i];
+  for (int i = 0; i < VERIFY_PIECES; ++i) all += s.piece[i];
   return all;
 }
 
@@ -364,36 +354,35 @@ __device__ __forceinline__ int32_t pick(const SK_CONSTANT VerifyDev &P, const Dr
   const double bound = s.bound;
   const int32_t chunk = s.chunk;
   if (chunk < 0) return -1;
-  double w[2][8];
-  int32_t places[2];
+  double mine[8];
+  int32_t place;
   if (tid == 0) s.found = -1;
-  chunk_weights<DT>(P, d, p_row, q_row, chunk, c, w, places, s, tid);
+  chunk_weights<DT>(P, d, p_row, q_row, chunk, c, mine, place, s, tid);
   // the piece that passes the bound, or the last with a weight
   double begin = s.begin, at_begin = 0.0;
   int32_t piece = -1;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < VERIFY_PIECES; ++i) {
     const double sum = s.piece[i];
     if (sum > 0.0 && (piece < 0 || !(at_begin + s.piece[piece] > bound))) piece = i, at_begin = begin;
     begin += sum;
   }
   if (piece < 0) return -1;  // (not where the chunk has a weight)
-  if (piece % 4 == wave) {
-    double mine[8], upto = 0.0;
+  if (piece == wave) {
+    double upto = 0.0;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) mine[k] = piece >= 4 ? w[1][k] : w[0][k], upto += mine[k];
+    for (int k = 0; k < 8; ++k) upto += mine[k];
     const double scanned = wave_scan(upto);
     const uint32_t lo = (uint32_t)__builtin_bit_cast(uint64_t, scanned), hi = (uint32_t)(__builtin_bit_cast(uint64_t, scanned) >> 32);
     const uint64_t below = (uint64_t)(uint32_t)__shfl_up((int)hi, 1) << 32 | (uint32_t)__shfl_up((int)lo, 1);
     double sum = at_begin + (lane ? __builtin_bit_cast(double, below) : 0.0);
-    const int32_t at = piece >= 4 ? places[1] : places[0];
     int32_t found = 0x7fffffff, last = -1;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       sum += mine[k];
       if (mine[k] > 0.0) {
-        if (sum > bound) found = min(found, at + k);
-        last = at + k;
+        if (sum > bound) found = min(found, place + k);
+        last = place + k;
       }
     }
     found = wave_min(found);
@@ -481,8 +470,8 @@ __device__ __forceinline__ void sample(const SK_CONSTANT VerifyDev &P, int32_t s
   const VerifyStat *stats = P.stats + (int64_t)(r0 + d.stop) * 2 * P.chunks;
   auto from_stats = [&](int32_t i) { return stats[i].top > -__builtin_inff() ? stats[i].sum * weight_of((double)stats[i].top - d.p.top, c) : 0.0; };
   int32_t token = -1;
-  double w[2][8];
-  int32_t places[2];
+  double w[8];
+  int32_t place;
   if (d.mode == FROM_DIFFERENCE) {  // a chunk a wave
     double *sums = P.sums + (int64_t)seq * P.chunks;
     const int32_t chunk = part * VERIFY_CHUNKS + __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -496,7 +485,7 @@ __device__ __forceinline__ void sample(const SK_CONSTANT VerifyDev &P, int32_t s
     return;
   } else if (d.mode == FROM_OTHERS) {
     const int32_t without = d.token / (512 * P.pieces);
-    const double rest = chunk_weights<DT>(P, d, p_row, q_row, without, c, w, places, s, tid);
+    const double rest = chunk_weights<DT>(P, d, p_row, q_row, without, c, w, place, s, tid);
     token = pick<DT>(P, d, p_row, q_row, c, random, [&](int32_t i) { return i == without ? rest : from_stats(i); }, s, tid);
   }
   if (d.mode == FROM_ONE) token = d.token;
