@@ -126,11 +126,12 @@ __device__ __forceinline__ int32_t wave_min(int32_t v) {
   return lane_of(v, 63);
 }
 
-// e^x to about 2 units of the last place: what x * log2(e) loses by rounding is put back.
+// e^x to about 2 units of the last place: what x * log2(e) loses by rounding is put back.  Not to an infinity (from x = 88.8 on, where it would be a
+// NaN if the rest is 0 or negative), and not a rest that is none itself.
 __device__ __forceinline__ float exp_of(float x) {
   const float p = x * 1.44269504f, e = exp2_fast(p);
-  const float rest = fmaf(x, 1.44269504f, -p) + x * 1.92596299e-8f;
-  return __builtin_isfinite(rest) ? fmaf(e, 0.693147181f * rest, e) : e;
+  const float rest = fmaf(x, 1.44269504f, -p) + x * 1.92596299e-8f, r = fmaf(e, 0.693147181f * rest, e);
+  return __builtin_isfinite(r) ? r : e;
 }
 // One exponential whatever the activation: z/2 (1 + tanh(w)) = z / (1 + e^-2w), and tanh(z) = 2 / (1 + e^-2z) - 1, near 0 by its series.
 // (e^-t overflows to infinity where it should; a NaN stays one.)

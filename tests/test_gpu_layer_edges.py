@@ -1,0 +1,50 @@
+"""Norms, mixture-of-experts layers and verification where their arithmetic and their rules of choice end: arguments far from 0, numbers of rows and vocabularies at
+both ends, the types' lowest values."""
+import pytest
+import torch
+
+import paper_1901_10008_amd as sk
+import layer_harness as H
+
+pytestmark = pytest.mark.gpu
+
+ACTS = ["none", "sigmoid", "silu", "tanh", "gelu", "relu"]
+
+
+def far_from_zero():
+    """Finite arguments of all sizes, many of them where e^-t passes the largest number of 32 bits: t = -88.8, which is z = -44.4 (tanh) and about -10 (gelu)."""
+    line = lambda a, b, n: torch.linspace(a, b, n, device="cuda", dtype=torch.float64)  # noqa: E731
+    z = torch.cat([line(-1e4, 1e4, 801), line(-120, -80, 641), line(-60, -40, 321), line(-16, -9, 449), line(80, 120, 161), line(9, 60, 205)])
+    return torch.cat([z, torch.tensor([s * v for v in (1e5, 1e8, 1e15, 1e25, 1e30) for s in (1, -1)], device="cuda", dtype=torch.float64)])
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_gates_far_from_zero(act, dtype):
+    z = far_from_zero().to(H.TORCH[dtype])
+    z = z[torch.isfinite(z)]
+    n = H.Norm(dtype=dtype, stream="f32", dim=z.numel(), rows=1, gate="one", act=act, residual=False, next=False, bs=1.0)
+    n.gate = z
+    u, z = n.block.double(), z.double()
+    y, _ = H.activated(act, z)
+    # As in the harness; but an argument t of the exponential counts up to 200, since 1 / (1 + e^-t) is 0 or 1 to 2^-126 beyond, and what fp32 arithmetic may take as 0
+    # (below 2^-126) is multiplied by z.
+    t = {"tanh": 2 * z, "gelu": 1.6 * (z + 0.045 * z ** 3)}.get(act, z).abs().clamp(max=200)
+    tol = 4 * H.E * (10 + t) * y.abs() + 2.0 ** -126 * (1 + z.abs()) if act not in ("none", "relu") else torch.zeros_like(z)
+    with sk.sk_norm_plan_create([n.problem()], keepalive=n) as plan:
+        sk.sk_norm_launch(plan, H.stream_handle())
+        torch.cuda.synchronize()
+    # (three roundings behind it: the product, the scale of 1, the output)
+    H.check(n.residual_out, u * y, u.abs() * tol + 3 * H.E * (u * y).abs() + H.TINY["f32"], f"{act} {dtype}")
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("gated", [True, False])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_experts_activations_far_from_zero(act, gated, dtype):
+    """What goes into the activations is spread over +- 100 and over +- 1000: every row meets what lies beyond the exponential's range."""
+    for spread in (40.0, 400.0):
+        m = H.Moe(rows=19, dim=64, ffn=48, act=act, dtype=dtype, gated=gated, shared=40, top_k=3, seed=int(spread))
+        for w in [m.gate_b if gated else m.up_b, m.s[0] if gated else m.s[1]]:
+            w.mul_(spread)
+        H.run_moe([m], f"{act} {spread}")
