@@ -282,10 +282,11 @@ sk_status plan_verify(const sk_verify_problem *problems, int32_t n, VerifyPlanHo
     d.first_row = p.first_row, d.drafted = p.drafted, d.logits = (const char *)p.logits, d.draft_logits = p.drafted ? (const char *)p.draft_logits : nullptr;
     d.temperatures = p.temperatures, d.accept_random = p.accept_random, d.sample_random = p.sample_random, d.tokens = p.tokens, d.accepted = p.accepted;
     d.dtype = p.dtype, d.sequences = p.sequences, d.rows = p.rows, d.vocab = p.vocab, d.temperature = p.temperature;
-    // larger chunks where there are enough of them (up to four pieces: a lane keeps its part in registers, and eight waves a SIMD take 24.4 -> 23.6 us)
+    // larger chunks where there are enough of them (up to four pieces: a lane keeps its part in registers, and eight waves a SIMD take 24.4 -> 23.6 us), and
+    // a row is longer than one (the kernels' chunks of several pieces are for rows of eight logits and more)
     const int64_t lines = (int64_t)p.rows * (d.draft_logits ? 2 : 1);
     d.pieces = 1;
-    while (d.pieces < VERIFY_PIECES && lines * ((p.vocab + 1024 * d.pieces - 1) / (1024 * d.pieces)) >= VERIFY_WAVES) d.pieces *= 2;
+    while (d.pieces < VERIFY_PIECES && p.vocab > 512 * d.pieces && lines * ((p.vocab + 1024 * d.pieces - 1) / (1024 * d.pieces)) >= VERIFY_WAVES) d.pieces *= 2;
     const int64_t chunk = 512 * (int64_t)d.pieces;
     d.chunks = (int32_t)((p.vocab + chunk - 1) / chunk);
     const int64_t stat = (lines * d.chunks + 3) / 4, sum = p.sequences * (((int64_t)d.chunks + VERIFY_CHUNKS - 1) / VERIFY_CHUNKS);

@@ -46,7 +46,7 @@ struct Eight {
   static constexpr int S = DT == SK_F32 ? 4 : 2;
   u32x4 raw[S / 2];
   int32_t first;
-  // SHORT: rows may have fewer than eight
+  // SHORT: rows may have fewer than eight (without it they must not: the planner gives those chunks of one piece)
   template <bool SHORT>
   __device__ __forceinline__ void load(const char *row, int32_t wave_at, int lane, int32_t vocab) {
     constexpr uint32_t lowest = DT == SK_F32 ? 0xff800000u : DT == SK_BF16 ? 0xff80u : 0xfc00u;

@@ -1,5 +1,7 @@
 """Norms, mixture-of-experts layers and verification where their arithmetic and their rules of choice end: arguments far from 0, numbers of rows and vocabularies at
 both ends, the types' lowest values."""
+import copy
+
 import pytest
 import torch
 
@@ -48,3 +50,28 @@ def test_experts_activations_far_from_zero(act, gated, dtype):
         for w in [m.gate_b if gated else m.up_b, m.s[0] if gated else m.s[1]]:
             w.mul_(spread)
         H.run_moe([m], f"{act} {spread}")
+
+
+def check_many(v, label):
+    """As H.check_verify, with the reference on the host: so many short rows are many small steps."""
+    host = copy.copy(v)
+    for name, x in vars(v).items():
+        if torch.is_tensor(x):
+            setattr(host, name, x.cpu())
+    tokens, accepted = host.reference()
+    with sk.sk_verify_plan_create([v.problem()], keepalive=v) as plan:
+        for turn in range(2):
+            v.tokens.fill_(-9), v.accepted.fill_(-9)
+            sk.sk_verify_launch(plan, H.stream_handle())
+            torch.cuda.synchronize()
+            assert v.accepted.tolist() == accepted, f"{label} launch {turn}: accepted"
+            assert v.tokens.tolist() == tokens, f"{label} launch {turn}: tokens"
+
+
+@pytest.mark.parametrize("vocab", [1, 3, 7, 8, 9, 513])
+@pytest.mark.parametrize("draft,rows", [("logits", 3001), ("certain", 6001), ("none", 6001)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_rows_of_short_vocabularies(vocab, draft, rows, dtype):
+    """So many rows that longer ones go in chunks of several pieces; padded with NaN, so that what is read beside a row is seen."""
+    counts = [3] * (rows // 3) + [rows % 3]
+    check_many(H.Verify(dtype=dtype, vocab=vocab, counts=counts, draft=draft, spread=0.7, pad=4, seed=vocab + rows), f"{vocab} {draft} {dtype}")
