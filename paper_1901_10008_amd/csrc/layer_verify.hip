@@ -154,7 +154,7 @@ __device__ __forceinline__ void chunk_stat(const SK_CONSTANT VerifyDev &P, const
     }
     r.at = wave_min(r.at);
   } else if (r.top > -__builtin_inff()) {
-    const double m = (double)fmaxf(top, -3.4e38f);  // (a lane may have nothing but -infinity: it stays behind all others)
+    const double m = (double)fmaxf(top, -3.402823466e+38f);  // (a lane may have nothing but -infinity: the lowest number is not above any other top)
     const double lowest = -990.0 / c;  // what is further below counts as this, for 10^-298
     double sum = 0.0;
 #pragma unroll

@@ -75,3 +75,29 @@ def test_many_rows_of_short_vocabularies(vocab, draft, rows, dtype):
     """So many rows that longer ones go in chunks of several pieces; padded with NaN, so that what is read beside a row is seen."""
     counts = [3] * (rows // 3) + [rows % 3]
     check_many(H.Verify(dtype=dtype, vocab=vocab, counts=counts, draft=draft, spread=0.7, pad=4, seed=vocab + rows), f"{vocab} {draft} {dtype}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("temperature", [1.0, 0.7, 1e-3, 1e30, 0.0])
+def test_logits_of_the_types_lowest_value(dtype, temperature):
+    """A usual mask: the lowest finite value.  Rows of it alone are uniform, whole chunks, pieces and lanes of it beside other logits count (almost) nothing."""
+    lowest = torch.finfo(H.TORCH[dtype]).min
+    for draft in ("logits", "certain"):
+        v = H.Verify(dtype=dtype, vocab=5000, counts=(2,) * 12 + (1, 1), draft=draft, temperature=temperature, seed=21)
+        v.accept_random.uniform_(0.0, 1e-3, generator=H.generator(5))  # a p of 1/5000 is accepted one time in five
+        for row, (first, last) in enumerate([(0, 5000), (0, 5000), (0, 512), (512, 1024), (100, 4900), (0, 4999), (1, 5000), (8, 16), (2048, 5000), (3, 4096)]):
+            v.logits[row, first:last] = lowest
+        v.logits[10, :] = lowest
+        v.logits[10, 4000:] = -float("inf")
+        v.logits[24:26, :] = lowest
+        if v.draft_logits is not None:
+            for row, (first, last) in {0: (0, 5000), 2: (0, 5000), 4: (0, 5000), 12: (0, 5000), 14: (17, 4500), 16: (512, 5000)}.items():
+                v.draft_logits[row, first:last] = lowest
+        H.check_verify([v], f"{draft} {temperature}")
+
+
+def test_many_rows_of_the_lowest_value_in_larger_chunks():
+    v = H.Verify(dtype="f32", vocab=4500, counts=(1,) * 3001, draft="none", seed=22)
+    v.logits[::2] = torch.finfo(torch.float32).min
+    v.logits[1::4, 700:] = torch.finfo(torch.float32).min
+    check_many(v, "lowest")
