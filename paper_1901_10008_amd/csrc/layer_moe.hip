@@ -14,7 +14,7 @@ struct MoeArgs {
 
 __device__ __forceinline__ int32_t rows_of(const SK_CONSTANT MoeDev &P) {
   const int32_t n = P.n_rows ? load_i32(P.n_rows) : 0x7fffffff;
-  return __builtin_amdgcn_readfirstlane(min(max(n - P.row0, 0), P.rows));
+  return __builtin_amdgcn_readfirstlane(min(max(max(n, 0) - P.row0, 0), P.rows));  // (the number is cut first: what is left of -2^31 less row0 would be positive)
 }
 
 // What a workgroup needs to find its part.

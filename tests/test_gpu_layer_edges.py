@@ -101,3 +101,11 @@ def test_many_rows_of_the_lowest_value_in_larger_chunks():
     v.logits[::2] = torch.finfo(torch.float32).min
     v.logits[1::4, 700:] = torch.finfo(torch.float32).min
     check_many(v, "lowest")
+
+
+@pytest.mark.parametrize("used", [-2 ** 31, -2 ** 31 + 1, -2 ** 31 + 511, -2 ** 31 + 512, -2 ** 31 + 1023, -513, -1, 2 ** 31 - 1])
+def test_numbers_of_rows_at_the_ends_of_their_type(used):
+    """A layer of more rows than are routed together: none of its parts has rows that the number does not give."""
+    m = H.Moe(rows=1100, dim=32, experts=4, top_k=2, ffn=16, shared=8, used=used)
+    H.run_moe([m], f"{used}")
+    H.check_norms([H.Norm(dim=100, rows=7, used=used), H.Norm(dim=64, rows=2100, used=used)], f"{used}")
