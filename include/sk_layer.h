@@ -101,8 +101,7 @@ sk_status sk_norm_launch(sk_norm_plan *plan, void *hip_stream);
  *     h_e = act(gate_e . x) * (up_e . x),               without gate: act(up_e . x)
  *     out = sum over the chosen, w_e * (down_e . h_e), and the same of the shared expert, which every row passes, with w = 1
  * Scores are computed in 64 bits, so that the choice between experts whose scores are next to each other does not depend on the order of sums.
- * Products of the experts are summed in fp32, h goes to the matrix units as the sum of two numbers of dtype, outputs are summed in fp32 and rounded
- * once.  An h beyond the type's range is infinite.  Each row's result depends on that row and the weights alone, up to the order of sums.
+ * Products of the experts are summed in fp32, h is fp32 and not rounded to dtype, outputs are summed in fp32 and rounded once.  Each row's result depends on that row and the weights alone, up to the order of sums.
  * The weights are read once for up to 32 rows of an expert; made for the rows of decoder steps, it takes any number.  A row's sum goes over its experts
  * in the order in which they were chosen, the shared one last.
  */

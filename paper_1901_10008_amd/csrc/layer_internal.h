@@ -62,7 +62,7 @@ constexpr int MOE_ROWS = 512;     // rows that are routed together; problems of 
 constexpr int MOE_EXPERTS = 512, MOE_TOP = 32;
 constexpr int MOE_GROUP = 32;     // rows of an expert that a unit of work takes at most
 constexpr int MOE_UP_RESIDENT = 3, MOE_DOWN_RESIDENT = 4;  // workgroups of the products that a compute unit holds (its registers)
-constexpr int H_PARTS = 2;     // that the first products' results are the sum of
+constexpr int H_PARTS = 2;     // planes of the first products' results, which are 32 bits: the even and the odd fours of a row
 constexpr int ROUTE_ROWS = 4;  // of a unit of the router
 constexpr int ADD_COLUMNS = 256;                  // of a row that a wave adds up
 
@@ -103,7 +103,7 @@ struct MoeDev {
   uint32_t *blocks_routed;
   char *h;                // [rows * top_k + rows], h_stride bytes apart
   float *y;               // of the second products, y_stride elements apart
-  int64_t h_stride, h_part, y_stride;  // h_part: from a row's first part to its second, in bytes
+  int64_t h_stride, h_part, y_stride;  // h_part: from a row's first plane to its second, in bytes
 };
 
 struct MoePlanHost {

@@ -28,7 +28,7 @@ SK_BOTH int32_t tiles_of(int32_t rows, int32_t matrices, int32_t mode) {
   return rows / t + (rows % t != 0);
 }
 // All tiles of a launch stand in a row, each as long as it takes: the loads of a wave, and some for its beginning and end.  k_len: elements of its
-// reduction, `matrices` of weights, `parts` of the activations.
+// reduction, `matrices` of weights, `parts` of the activations (their planes of as many bytes as 16-bit numbers).
 constexpr int32_t EXTRA = 8;
 SK_BOTH int64_t cost(int32_t k_len, int32_t matrices, int32_t parts, int32_t mode) {
   return (int64_t)((k_len + 255) / 256) * (matrices * rows_of_tile(matrices, mode) / 8 + parts * mode / 8) + EXTRA;

@@ -109,3 +109,57 @@ def test_numbers_of_rows_at_the_ends_of_their_type(used):
     m = H.Moe(rows=1100, dim=32, experts=4, top_k=2, ffn=16, shared=8, used=used)
     H.run_moe([m], f"{used}")
     H.check_norms([H.Norm(dim=100, rows=7, used=used), H.Norm(dim=64, rows=2100, used=used)], f"{used}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("rows", [1, 5, 12, 40, 100])
+@pytest.mark.parametrize("ffn", [16, 264, 1032])
+def test_nothing_is_rounded_between_the_products(dtype, rows, ffn):
+    """Whole numbers of up to 20 bits between the products, in pairs that differ by at most 63, and the second products take their differences: any rounding to fewer than 20 bits
+    is seen.  All sums of 32 bits are exact (16 numbers below 2^19 times +-1)."""
+    g = torch.Generator().manual_seed(rows + ffn)
+    m = H.Moe(dtype=dtype, rows=rows, dim=64, ffn=ffn, experts=3, top_k=1, gated=False, act="none", shared=ffn, normalize=1)
+    m.x.copy_(torch.randint(1, 64, (rows, 64), generator=g))
+
+    def weights(up, down):  # (of an expert) the number at place 2 p + 1 is that at 2 p with one weight of x less by 1
+        w = torch.randint(64, 128, (ffn, 64), generator=g)
+        w[1::2] = w[::2]
+        pairs = torch.arange(0, ffn, 2)
+        w[pairs + 1, torch.randint(0, 64, (len(pairs),), generator=g)] -= 1
+        up.copy_(w)
+        down.zero_()
+        for d in range(64):
+            for p in torch.randperm(ffn // 2, generator=g)[:4].tolist():
+                sign = 1 if p % 2 else -1
+                down[d, 2 * p], down[d, 2 * p + 1] = sign, -sign
+
+    for e in range(3):
+        up, down = torch.empty((ffn, 64)), torch.empty((64, ffn))
+        weights(up, down)
+        m.up_b[e], m.down_b[e] = up.to(m.up_b.dtype), down.to(m.up_b.dtype)
+    up, down = torch.empty((ffn, 64)), torch.empty((64, ffn))
+    weights(up, down)
+    m.s[1].copy_(up), m.s[2].copy_(down)
+    with sk.sk_moe_plan_create([m.problem()], keepalive=m) as plan:
+        sk.sk_moe_launch(plan, H.stream_handle())
+        torch.cuda.synchronize()
+    want = m.reference()[0]
+    assert (want == want.round()).all() and float(want.abs().max()) <= 8 * 63  # eight pairs: those of the routed and of the shared expert
+    assert torch.equal(m.out, want.to(m.out.dtype))  # (rounded once: what is above 256 may be odd)
+
+
+@pytest.mark.parametrize("gated", [True, False])
+@pytest.mark.parametrize("rows", [3, 14, 60])
+def test_f16_between_the_products_beyond_its_range(gated, rows):
+    """Numbers of 10^5 to 10^9 between the products, and of 2^-24 and less, where the outputs are ordinary."""
+    large = H.Moe(dtype="f16", rows=rows, dim=64, ffn=48, shared=24, act="silu", gated=gated, experts=3, top_k=2, seed=1)
+    small = H.Moe(dtype="f16", rows=rows, dim=64, ffn=48, shared=24, act="none", gated=gated, experts=3, top_k=2, seed=2)
+    for m, first, second in ((large, 2.0 ** 13 if gated else 2.0 ** 14, 2.0 ** -20 if gated else 2.0 ** -10), (small, 2.0 ** -10 if gated else 2.0 ** -17, 2.0 ** 12)):
+        for w in (m.gate_b, m.up_b, m.s[0], m.s[1]):
+            if w is not None:
+                w.mul_(first)
+        for w in (m.down_b, m.s[2]):
+            w.mul_(second)
+        m.x.mul_(2.0 if m is large else 2.0 ** -5 if not gated else 2.0 ** -3)
+    H.run_moe([large], "large")
+    H.run_moe([small], "small")
