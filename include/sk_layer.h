@@ -21,7 +21,8 @@
  *   - Norm plans have no workspace: their launches may overlap.  Plans of the other two own a workspace, so
  *     their launches must not: those on one stream are ordered by it, a launch on another stream gives SK_ERR_BUSY while the last one
  *     has not completed (best effort; launches of a graph are not tracked, and its replays are the caller's to order).
- *   - Outputs of a plan (of one problem or of several) whose spans from first to last element intersect give SK_ERR_OVERLAP.
+ *   - Outputs of a plan (of one problem or of several) whose spans from first to last element intersect give SK_ERR_OVERLAP.  What outputs may share with
+ *     inputs stands with each operator.
  *   - Plans created host_only (1) are checked and planned without a device; their launches give SK_ERR_STATE.
  */
 #ifndef SK_LAYER_H
@@ -101,6 +102,7 @@ sk_status sk_norm_launch(sk_norm_plan *plan, void *hip_stream);
  *     h_e = act(gate_e . x) * (up_e . x),               without gate: act(up_e . x)
  *     out = sum over the chosen, w_e * (down_e . h_e), and the same of the shared expert, which every row passes, with w = 1
  * Scores are computed in 64 bits, so that the choice between experts whose scores are next to each other does not depend on the order of sums.
+ * out may be x, or touch it: it is written when all of a plan's x have been read.  expert_ids and expert_weights must not touch inputs.
  * Products of the experts are summed in fp32, h is fp32 and not rounded to dtype, outputs are summed in fp32 and rounded once.  Each row's result depends on that row and the weights alone, up to the order of sums.
  * The weights are read once for up to 32 rows of an expert; made for the rows of decoder steps, it takes any number.  A row's sum goes over its experts
  * in the order in which they were chosen, the shared one last.
@@ -158,6 +160,7 @@ sk_status sk_moe_plan_info(const sk_moe_plan *plan, int32_t *launches, int64_t *
  *     token); after the last accepted draft from p of the last row.
  * Sampling: the first token k with  sum_{j <= k} w_j > sample_random[s] * sum_j w_j  (the last with w > 0 if rounding leaves none).
  * Temperature 0 (or below, or NaN): p is 1 at the first of the largest logits, and the draft is certain of its token.
+ * Outputs must not touch inputs of the plan, drafted among them (SK_ERR_OVERLAP): sequences and parts of a row are decided side by side.
  * Results: tokens[row] = accepted drafts, then the sampled token, then -1 up to the sequence's last row; accepted[s] = number of accepted
  * drafts.  Rows of no sequence are left as they are; a sequence without rows accepts 0.
  * A logit of -infinity is a token of probability 0.  A row of logits that holds NaN or +infinity, or -infinity only, has no distribution: it accepts

@@ -35,6 +35,32 @@ struct Spans {
   }
 };
 
+// The inputs of a plan whose outputs must not touch them: rows of `dim` bytes, `stride` bytes apart.
+struct Inputs {
+  struct Rows {
+    uintptr_t at;
+    uint64_t rows, stride, dim;
+  };
+  std::vector<Rows> list;
+  void add(const void *p, int64_t rows, int64_t stride, int64_t dim) {
+    if (p) list.push_back(Rows{(uintptr_t)p, (uint64_t)rows, (uint64_t)stride, (uint64_t)dim});
+  }
+  void add(const void *p, int64_t bytes) { add(p, 1, 0, bytes); }
+  // Whether one of them has a byte of an output (spans that are sorted, and do not overlap).  What lies between rows is not read.
+  bool touch(const Spans &outputs) const {
+    for (const Rows &r : list) {
+      const uintptr_t end = r.at + (r.rows - 1) * r.stride + r.dim;
+      auto it = std::upper_bound(outputs.list.begin(), outputs.list.end(), r.at, [](uintptr_t at, const std::pair<uintptr_t, uintptr_t> &o) { return at < o.second; });
+      for (; it != outputs.list.end() && it->first < end; ++it) {
+        // the first row that ends behind the output's beginning
+        const uint64_t behind = it->first < r.at + r.dim ? 0 : r.stride ? (it->first - r.at - r.dim) / r.stride + 1 : r.rows;
+        if (behind < r.rows && r.at + behind * r.stride < it->second) return true;
+      }
+    }
+    return false;
+  }
+};
+
 // A row stride as given, or packed.  false: it is negative, or rows would overlap (`one_for_all`: rows may share).
 bool stride_of(int64_t given, int64_t dim, int64_t rows, int64_t &stride) {
   stride = given ? given : dim;
@@ -257,6 +283,7 @@ constexpr int64_t VERIFY_WAVES = 6000;
 
 sk_status plan_verify(const sk_verify_problem *problems, int32_t n, VerifyPlanHost &out, std::string &err) {
   Spans written;
+  Inputs read;
   Layout counters, work;
   const sk_status st = each(problems, n, err, [&](const sk_verify_problem &p) -> sk_status {
     if (!known(p.dtype)) return refuse(err, SK_ERR_UNSUPPORTED, "dtype must be SK_F32, SK_BF16 or SK_F16");
@@ -279,6 +306,9 @@ sk_status plan_verify(const sk_verify_problem *problems, int32_t n, VerifyPlanHo
     written.add(p.tokens, 1, 0, p.rows, 4), written.add(p.accepted, 1, 0, p.sequences, 4);
     if (written.far || reach.far) return refuse(err, SK_ERR_UNSUPPORTED, "a stride reaches too far");
     d.logits_stride *= one, d.draft_stride *= one;
+    read.add(p.logits, p.rows, d.logits_stride, p.vocab * one), read.add(p.first_row, 4 * ((int64_t)p.sequences + 1)), read.add(p.sample_random, 4 * (int64_t)p.sequences);
+    read.add(p.temperatures, 4 * (int64_t)p.sequences);
+    if (p.drafted) read.add(p.drafted, 4 * (int64_t)p.rows), read.add(p.accept_random, 4 * (int64_t)p.rows), read.add(p.draft_logits, p.rows, d.draft_stride, p.vocab * one);
     d.first_row = p.first_row, d.drafted = p.drafted, d.logits = (const char *)p.logits, d.draft_logits = p.drafted ? (const char *)p.draft_logits : nullptr;
     d.temperatures = p.temperatures, d.accept_random = p.accept_random, d.sample_random = p.sample_random, d.tokens = p.tokens, d.accepted = p.accepted;
     d.dtype = p.dtype, d.sequences = p.sequences, d.rows = p.rows, d.vocab = p.vocab, d.temperature = p.temperature;
@@ -307,6 +337,7 @@ sk_status plan_verify(const sk_verify_problem *problems, int32_t n, VerifyPlanHo
   });
   if (st != SK_OK) return st;
   if (written.overlap()) return refuse(err, SK_ERR_OVERLAP, "ranges of tokens and accepted overlap");
+  if (read.touch(written)) return refuse(err, SK_ERR_OVERLAP, "tokens or accepted touch an input");
   out.counters = counters.bytes;
   out.workspace = work.bytes;
   return SK_OK;

@@ -163,3 +163,18 @@ def test_f16_between_the_products_beyond_its_range(gated, rows):
         m.x.mul_(2.0 if m is large else 2.0 ** -5 if not gated else 2.0 ** -3)
     H.run_moe([large], "large")
     H.run_moe([small], "small")
+
+
+@pytest.mark.parametrize("rows", [1, 30, 600])
+def test_experts_over_their_input(rows):
+    """out is x: nothing of it is written before all of it has been read, by tenants whose x is another's out too."""
+    ms = [H.Moe(rows=rows, dim=64, ffn=40, experts=6, top_k=2, shared=16, pad=8, seed=s) for s in (1, 2)]
+    wants = [m.reference() for m in ms]
+    problems = [m.problem() for m in ms]
+    problems[0].out, problems[1].out = ms[1].x.data_ptr(), ms[0].x.data_ptr()
+    with sk.sk_moe_plan_create(problems, keepalive=ms) as plan:
+        sk.sk_moe_launch(plan, H.stream_handle())
+        torch.cuda.synchronize()
+    for (out, tol, ids, w), m, at in zip(wants, ms, (ms[1].x, ms[0].x)):
+        H.check(at, out, tol)
+        assert torch.equal(m.ids.long(), ids)
