@@ -18,7 +18,7 @@
  *   - Row strides are in elements; 0 means packed.  Pointers are multiples of their element's size unless stated otherwise.
  *   - n_rows (norm, moe): a number on the device, read by every launch; rows from it on are left as they are.  Values outside [0, rows]
  *     are cut to it; null means `rows`.  So a plan serves every step with up to `rows` rows, also out of a HIP graph.
- *   - Norm plans have no workspace: their launches may overlap.  Plans of the other two own a workspace, so
+ *   - Norm plans have no workspace: their launches may overlap, and be made by several threads at once.  Plans of the other two own a workspace, so
  *     their launches must not: those on one stream are ordered by it, a launch on another stream gives SK_ERR_BUSY while the last one
  *     has not completed (best effort; launches of a graph are not tracked, and its replays are the caller's to order).
  *   - Outputs of a plan (of one problem or of several) whose spans from first to last element intersect give SK_ERR_OVERLAP.  What outputs may share with

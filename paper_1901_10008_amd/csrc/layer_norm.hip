@@ -1,4 +1,6 @@
 // Norms before and after a block: entry points.
+#include <atomic>
+
 #include "layer_host.h"
 #include "layer_norm.hip.h"
 
@@ -17,7 +19,7 @@ SK_NORM_FORM(1024, 4)
 
 struct sk_norm_plan : sk::PlanOnDevice {
   sk::NormPlanHost host;
-  bool launched = false;
+  std::atomic<bool> launched{false};  // (launches may overlap, from several threads too)
 };
 
 namespace {
@@ -62,7 +64,7 @@ sk_status sk_norm_plan_create(const sk_norm_problem *problems, int32_t n, const 
 
 sk_status sk_norm_plan_destroy(sk_norm_plan *plan) {
   if (!plan) return SK_OK;
-  return sk::guarded([&]() -> sk_status { return sk::destroy_plan(plan, plan->launched); });
+  return sk::guarded([&]() -> sk_status { return sk::destroy_plan(plan, plan->launched.load(std::memory_order_relaxed)); });
 }
 
 sk_status sk_norm_launch(sk_norm_plan *plan, void *hip_stream) {
@@ -70,10 +72,10 @@ sk_status sk_norm_launch(sk_norm_plan *plan, void *hip_stream) {
     sk_status st = sk::check_resident(plan);
     if (st != SK_OK) return st;
     const sk::NormTable *table = (const sk::NormTable *)plan->blob;
+    plan->launched.store(true, std::memory_order_relaxed);
     for (const sk::NormLaunch &l : plan->host.launches) {
       if (st != SK_OK) break;
       st = sk::launch(norm_kernel(l.form, l.once), l.grid, (hipStream_t)hip_stream, nullptr, sk::NormArgs{table++, l.n}, sk::norm_threads(l.form));
-      plan->launched = true;
     }
     return st;
   });

@@ -1,6 +1,7 @@
 """Norms, mixture-of-experts layers and verification where their arithmetic and their rules of choice end: arguments far from 0, numbers of rows and vocabularies at
 both ends, the types' lowest values."""
 import copy
+import threading
 
 import pytest
 import torch
@@ -178,3 +179,28 @@ def test_experts_over_their_input(rows):
     for (out, tol, ids, w), m, at in zip(wants, ms, (ms[1].x, ms[0].x)):
         H.check(at, out, tol)
         assert torch.equal(m.ids.long(), ids)
+
+
+def test_norms_launched_by_several_threads_at_once():
+    n = H.Norm(dim=700, rows=40, post=1, stream="f32", gate="rows", act="silu")
+    (r, y), (tr, ty) = n.reference()
+    streams, failed = [torch.cuda.Stream() for _ in range(4)], []
+    torch.cuda.synchronize()
+
+    def work(plan, stream):
+        try:
+            for _ in range(200):
+                sk.sk_norm_launch(plan, stream.cuda_stream)
+        except Exception as e:  # noqa: BLE001
+            failed.append(e)
+
+    plan = sk.sk_norm_plan_create([n.problem()], keepalive=n)
+    threads = [threading.Thread(target=work, args=(plan, s)) for s in streams]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    plan.close()  # (waits for all of them)
+    assert not failed and all(s.query() for s in streams)
+    H.check(n.residual_out, r, tr)
+    H.check(n.next, y, ty)
