@@ -204,3 +204,29 @@ def test_norms_launched_by_several_threads_at_once():
     assert not failed and all(s.query() for s in streams)
     H.check(n.residual_out, r, tr)
     H.check(n.next, y, ty)
+
+
+@pytest.mark.parametrize("dim,rows", [(2056, 10000), (200, 100000), (768, 30000), (5000, 5000), (12000, 2000)])
+def test_loads_and_stores_past_the_caches_give_the_same_bits(dim, rows):
+    """A launch of more than 160 MiB, which goes past the caches, and its rows in launches that do not."""
+    make = lambda: H.Norm(dim=dim, rows=rows, kind="layer", post=1, stream="f32", gate="rows", act="sigmoid", biases=True, seed=3)  # noqa: E731
+    a, b = make(), make()
+    assert rows * dim * (3 * 2 + 2 * 4) > 160 << 20
+    with sk.sk_norm_plan_create([a.problem()], keepalive=a) as plan:
+        sk.sk_norm_launch(plan, H.stream_handle())
+        torch.cuda.synchronize()
+    step = rows // 4 if dim > 2048 else max(2048, rows // 8)  # (of up to 2048 elements as many rows as give a plan of the same form)
+    for at in range(0, rows, step):
+        p, n = b.problem(), min(step, rows - at)
+        if dim <= 2048 and n < 2048:
+            at, n = rows - 2048, 2048
+        p.rows = n
+        for name, x in (("block", b.block), ("gate", b.gate), ("residual", b.residual), ("residual_out", b.residual_out), ("next", b.next)):
+            setattr(p, name, x[at:].data_ptr())
+        assert n * dim * (3 * 2 + 2 * 4) <= 160 << 20
+        with sk.sk_norm_plan_create([p], keepalive=b) as plan:
+            sk.sk_norm_launch(plan, H.stream_handle())
+            torch.cuda.synchronize()
+    assert torch.equal(a.residual_out, b.residual_out) and torch.equal(a.next, b.next)
+    (r, y), (tr, ty) = a.reference()
+    H.check(a.next, y, ty)
