@@ -324,7 +324,7 @@ def main(argv=None):
     kinds = [(768, (12, 12, 64), 0, 0), (2048, (16, 4, 128), 0, 0), (1024, (16, 4, 80), 256, 4)]
     if a.vocab:
         return _main_tokens(a, kinds)
-    tenants = [Tenant(h, heads, a.layers, a.children, a.prompt + 64 + a.steps, window=w, sinks=s, seed=i)
+    tenants = [Tenant(h, heads, a.layers, a.children, a.prompt + max(64, 7 * a.tenants) + a.steps, window=w, sinks=s, seed=i)
                for i, (h, heads, w, s) in ((i, kinds[i % len(kinds)]) for i in range(a.tenants))]
     g = torch.Generator(device="cuda").manual_seed(99)
     prompts = [unit(torch.randn((a.prompt + 7 * i, t.hidden), generator=g, device="cuda")) for i, t in enumerate(tenants)]
@@ -341,7 +341,7 @@ def main(argv=None):
 
 
 def _main_tokens(a, kinds):
-    tenants = [LanguageModel(h, heads, a.layers, a.children, a.prompt + 64 + a.steps * (a.drafts + 1), a.vocab, window=w, sinks=s, seed=i, shared=h if i % 2 else 0)
+    tenants = [LanguageModel(h, heads, a.layers, a.children, a.prompt + max(64, 7 * a.tenants) + a.steps * (a.drafts + 1), a.vocab, window=w, sinks=s, seed=i, shared=h if i % 2 else 0)
                for i, (h, heads, w, s) in ((i, kinds[i % len(kinds)]) for i in range(a.tenants))]
     g = torch.Generator().manual_seed(99)
     prompts = [torch.randint(0, a.vocab, (a.prompt + 7 * i,), generator=g).tolist() for i in range(a.tenants)]
