@@ -230,3 +230,84 @@ def test_loads_and_stores_past_the_caches_give_the_same_bits(dim, rows):
     assert torch.equal(a.residual_out, b.residual_out) and torch.equal(a.next, b.next)
     (r, y), (tr, ty) = a.reference()
     H.check(a.next, y, ty)
+
+
+@pytest.mark.parametrize("rows,experts,top_k", [(512, 512, 32), (600, 33, 32), (65, 512, 32), (512, 3, 1), (2000, 128, 8)])
+def test_most_choices(rows, experts, top_k):
+    """More pairs of a row and an expert than the router keeps at hand, and as many as there can be."""
+    H.run_moe([H.Moe(rows=rows, dim=16, ffn=8, experts=experts, top_k=top_k, scoring="sigmoid", bias=True, seed=rows), H.Moe(rows=3, dim=16, ffn=8, seed=1)], f"{rows} {experts}/{top_k}")
+
+
+@pytest.mark.parametrize("dim,ffn", [(1 << 20, 8), (8, 1 << 20), (8200, 9000)])
+def test_longest_rows_of_experts(dim, ffn):
+    H.run_moe([H.Moe(rows=34, dim=dim, ffn=ffn, experts=2, top_k=1, shared=8, seed=1)], f"{dim} x {ffn}")
+
+
+def test_two_layers_on_two_streams():
+    ms = [H.Moe(rows=40, dim=256, ffn=128, experts=8, top_k=2, shared=64, seed=s) for s in (1, 2)]
+    streams = [torch.cuda.Stream() for _ in ms]
+    plans = [sk.sk_moe_plan_create([m.problem()], keepalive=m) for m in ms]
+    torch.cuda.synchronize()
+    for _ in range(50):
+        for plan, stream in zip(plans, streams):
+            sk.sk_moe_launch(plan, stream.cuda_stream)
+    torch.cuda.synchronize()
+    for m, plan in zip(ms, plans):
+        H.check_moe(m)
+        plan.close()
+
+
+@pytest.mark.parametrize("counts,vocab,draft", [((1200,), 40, "logits"), ((700, 1, 700), 30, "certain"), ((3,) * 5000, 9, "certain"), ((2, 0, 1), 1 << 20, "logits"), ((300, 300), 2049, "logits")])
+def test_long_and_many_sequences(counts, vocab, draft):
+    v = H.Verify(dtype="f32", vocab=vocab, counts=counts, draft=draft, seed=31)
+    if draft == "logits":
+        v.draft_logits.copy_(v.logits)  # (all but a few are accepted)
+        v.draft_logits[-3:] += H.randn(H.generator(1), 3, vocab)
+    else:
+        v.logits.scatter_add_(1, v.drafted.long()[:, None], torch.full((v.rows, 1), 9.0, device="cuda"))
+    check_many(v, f"{len(counts)} x {vocab}")
+
+
+def test_rows_far_apart():
+    """Rows further apart than 2^31 elements, and more rows than 2^16."""
+    n = H.Norm(dim=40, rows=3, post=1, gate="rows", act="silu")
+    stride = (1 << 31) + 8
+    far = torch.zeros(2 * stride + 40, dtype=torch.bfloat16, device="cuda")
+    for row in range(3):
+        far[row * stride:row * stride + 40] = n.block[row]
+    p = n.problem()
+    p.block, p.block_stride = far.data_ptr(), stride
+    (r, y), (tr, ty) = n.reference()
+    with sk.sk_norm_plan_create([p], keepalive=(n, far)) as plan:
+        sk.sk_norm_launch(plan, H.stream_handle())
+        torch.cuda.synchronize()
+    H.check(n.residual_out, r, tr)
+    H.check(n.next, y, ty)
+    del far
+    H.check_norms([H.Norm(dim=8, rows=1 << 20, seed=1), H.Norm(dim=1, rows=70000, kind="layer", seed=2), H.Norm(dim=300, rows=100001, used=99999, seed=3)])
+
+
+@pytest.mark.parametrize("rows", [4, 13, 50])
+def test_infinity_and_the_largest_numbers_between_the_products(rows):
+    """One row is infinite between the products, one has numbers there that bf16 could only round to infinity: the first's outputs are infinite (no NaN), the second's as large as
+    they should be, and the others' what they are without those two."""
+    m, clean = (H.Moe(rows=rows, dim=64, ffn=48, experts=3, top_k=1, act="none", gated=False, seed=5) for _ in range(2))  # (one choice: with two, the second's weight is 0)
+    for x in (m, clean):
+        x.up_b.abs_(), x.down_b.abs_()
+    m.x[1], m.x[2] = 2.0 ** 127, 0.0
+    clean.x[2] = 0.0
+    m.x[2, 0] = 2.0 ** 127
+    m.up_b[:, :, 0] = 2.0 - 2.0 ** -7  # (the largest of bf16)
+    m.up_b[:, :, 1] = 2.0 ** -7 - 2.0 ** -13
+    m.x[2, 1] = 2.0 ** 127  # their sum: 2^128 less 2^114, between the largest of bf16 and that of 32 bits
+    m.down_b.mul_(2.0 ** -10)
+    clean.up_b.copy_(m.up_b), clean.down_b.copy_(m.down_b)
+    for x in (m, clean):
+        with sk.sk_moe_plan_create([x.problem()], keepalive=x) as plan:
+            sk.sk_moe_launch(plan, H.stream_handle())
+            torch.cuda.synchronize()
+    out, tol, _, _ = m.reference()
+    assert torch.isposinf(m.out[1]).all()
+    H.check(m.out[2], out[2], tol[2])
+    others = [r for r in range(rows) if r not in (1, 2)]
+    assert torch.equal(m.out[others], clean.out[others])
