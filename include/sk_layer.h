@@ -17,7 +17,8 @@
  *     arrays of problems themselves are copied.
  *   - Row strides are in elements; 0 means packed.  Pointers are multiples of their element's size unless stated otherwise.
  *   - n_rows (norm, moe): a number on the device, read by every launch; rows from it on are left as they are.  Values outside [0, rows]
- *     are cut to it; null means `rows`.  So a plan serves every step with up to `rows` rows, also out of a HIP graph.
+ *     are cut to it; null means `rows`.  So a plan serves every step with up to `rows` rows, also out of a HIP graph.  Inputs have `rows` rows whatever
+ *     the number is: those behind it may be read.
  *   - Norm plans have no workspace: their launches may overlap, and be made by several threads at once.  Plans of the other two own a workspace, so
  *     their launches must not: those on one stream are ordered by it, a launch on another stream gives SK_ERR_BUSY while the last one
  *     has not completed (best effort; launches of a graph are not tracked, and its replays are the caller's to order).
@@ -39,7 +40,7 @@ typedef enum { SK_ACT_NONE = 0, SK_ACT_SIGMOID = 1, SK_ACT_SILU = 2, SK_ACT_TANH
 
 typedef struct {
   int32_t host_only;
-  int32_t workgroups; /* workgroups at a time that the work is cut for; 0 = as many as the device holds */
+  int32_t workgroups; /* workgroups at a time that the products of sk_moe are cut for; 0 = as many as the device holds (the other operators have no use for it) */
   int32_t reserved[2];
 } sk_layer_params;
 
@@ -97,7 +98,8 @@ sk_status sk_norm_launch(sk_norm_plan *plan, void *hip_stream);
  * For every row x of `dim` elements:
  *     l_e = x . router_e                                of every expert e
  *     s   = softmax(l)  (SK_MOE_SOFTMAX)   or   s_e = 1 / (1 + e^-l_e)  (SK_MOE_SIGMOID)
- *     the top_k experts with the largest s_e + router_bias_e, in that order; equal ones by their number; NaN below all others
+ *     the top_k experts with the largest s_e + router_bias_e (SK_MOE_SOFTMAX without bias: with the largest l_e, which is the same order but tells apart
+ *     what the softmax rounds to the same), in that order; equal ones by their number; NaN below all others
  *     w_e = scale * s_e, with normalize = 1 divided by the sum of the chosen s_e
  *     h_e = act(gate_e . x) * (up_e . x),               without gate: act(up_e . x)
  *     out = sum over the chosen, w_e * (down_e . h_e), and the same of the shared expert, which every row passes, with w = 1
@@ -150,8 +152,8 @@ sk_status sk_moe_plan_info(const sk_moe_plan *plan, int32_t *launches, int64_t *
 
 /* ---- verification of drafted tokens -------------------------------------------------------------------------------------
  *
- * Rows of logits belong to sequences as in sk_cache.h: sequence s has rows first_row[s] .. first_row[s+1]-1 (none is fine; values are cut to
- * [0, rows]).  Row first_row[s] + i gives the target's distribution of the token behind the sequence's i-th token of this step; drafted[row] is the
+ * Rows of logits belong to sequences as in sk_cache.h: sequence s has rows first_row[s] .. first_row[s+1]-1 (entries that do not decrease; none for a
+ * sequence is fine; values are cut to [0, rows]).  Row first_row[s] + i gives the target's distribution of the token behind the sequence's i-th token of this step; drafted[row] is the
  * token that was drafted there, for all rows of the sequence but the last, which has no draft.  With one row a sequence this is plain sampling.
  *     p = softmax(logits / temperature), of the row
  *     q = softmax(draft_logits / temperature); without draft_logits the draft was certain of its token: q = 1 there, 0 elsewhere

@@ -297,8 +297,8 @@ __global__ void __launch_bounds__(CACHE_THREADS) sk_moe_route(MoeArgs a) {
 // ---------------------------------------------------------------------------
 // A tile is 16 or 32 rows of an expert's weights times the rows of activations of a group; the four waves of a workgroup take the blocks of 64 elements
 // (128 bytes a row) of its reduction in turn, and add their sums up in LDS.  Bound by the memory that the weights come from (two rows of eight experts of
-// 4096 x 12288 with gates: 1.06 GB in 198 us, 5.3 TB/s; the first products of 61 rows 5.9 TB/s), with more rows an expert by the activations, which come
-// out of the dies' caches for every tile (23 rows: 115 MB of weights in 42 and in 58 us).  An instruction loads
+// 4096 x 12288 with gates: 1.06 GB in 200 us, 5.3 TB/s; the first products of 61 rows 5.9 TB/s), with more rows an expert by the activations, which come
+// out of the dies' caches for every tile (23 rows: 115 MB of weights in 41 and in 59 us).  An instruction loads
 // eight whole lines of 128 bytes, lane (r, q) of the 16 x 4 that the matrix instruction sees row r % 8 (+ 8), bytes 16 (q + 4 (r / 8)).
 //   Up to 8 rows of activations (MODE 8): the matrix instruction takes the weights as they came, rows 0 .. 7 with the lower half of the block and once
 //     more with the upper; its other operand is laid out the same way, by one load.  Of the 16 x 16 sums the 8 x 8 on the diagonal count.

@@ -181,8 +181,8 @@ sk_status plan_norm(const sk_norm_problem *problems, int32_t n, NormPlanHost &ou
 
 // ---- mixture of experts ----------------------------------------------------------------------------------------------------
 
-// The router splits its sums where that gives no more workgroups than the card holds at a time: 8 experts of 4096 and 2 rows 9.4 us instead of 11.6,
-// 60 of 2048 and 61 rows (480 workgroups) 12.5 instead of 12.8; but 33 of 1000 and 250 rows (1071) 18 instead of 13.5.
+// The router splits its sums where that gives no more workgroups than the card holds at a time: 8 experts of 4096 and 2 rows 7.5 us instead of 11.1,
+// 60 of 2048 and 61 rows (480 workgroups) 11.0 instead of 12.5; but 33 of 1000 and 250 rows (1071) 15.7 instead of 13.7.
 constexpr int64_t ROUTE_SPLIT_UNITS = 512;
 
 sk_status plan_moe(const sk_moe_problem *problems, int32_t n, int32_t compute_units, int32_t workgroups, MoePlanHost &out, std::string &err) {

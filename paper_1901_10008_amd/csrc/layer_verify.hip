@@ -121,7 +121,7 @@ __device__ __forceinline__ Owner owner_of(const SK_CONSTANT VerifyDev &P, int32_
 }
 
 // A chunk of a row, 512 * PIECES logits, by a wave: a lane has eight of each piece, takes them relative to its own largest, and the lanes are joined at
-// the end.  Bound by the vector unit (17 instructions a logit, 16-bit logits) about as much as by memory: rows of 128000 and
+// the end.  Bound by the vector unit (19 to 20 instructions a logit, half of its time) about as much as by memory: rows of 128000 and
 // 50257, 29 million 16-bit logits in all, in 23 us (2.5 TB/s), 102 MB of 32-bit logits in 23 us (4.5 TB/s).
 template <int DT, int PIECES>
 __device__ __forceinline__ void chunk_stat(const SK_CONSTANT VerifyDev &P, const char *from, int32_t chunk, double c, VerifyStat *out, int lane) {
